@@ -251,23 +251,36 @@ def _distill_plain(st):
 
 
 # --------------------------------------------------------------------------
+# the framework's calls
+# --------------------------------------------------------------------------
+def _score_own(st):
+    from paper_2605_30574_gb300.decoder.scoring import token_logprobs
+    got = token_logprobs(st["logits"], st["tokens"], top=st["top"], temperature=st["temperature"])
+    out = dict(logprobs=got.logprobs, entropy=got.entropy)
+    if st["top"]:
+        out.update(top_logprobs=got.top_logprobs, top_ids=got.top_ids)
+    return out
+
+
+def _distill_own(st):
+    from paper_2605_30574_gb300.decoder.scoring import distill_loss_and_grad
+    loss, grad = distill_loss_and_grad(st["logits"], st["ids"], st["teacher"], weight=st["weight"], rest=st["rest"],
+                                       temperature=st["temperature"])
+    return dict(loss=loss, grad=grad)
+
+
+def _attn_own(st):
+    from paper_2605_30574_gb300.decoder.attention import attention_backward
+    dq, dk, dv = attention_backward(st["dout"], st["q"], st["k"], st["v"], st["out"], st["lse"], st["scale"])
+    return dict(dq=dq, dk=dk, dv=dv)
+
+
+# --------------------------------------------------------------------------
 # one pass
 # --------------------------------------------------------------------------
 def run(st):
     if own:
-        from paper_2605_30574_gb300.decoder import attention, scoring
-        if st["op"] == "score":
-            got = scoring.token_logprobs(st["logits"], st["tokens"], top=st["top"], temperature=st["temperature"])
-            out = dict(logprobs=got.logprobs, entropy=got.entropy)
-            if st["top"]:
-                out.update(top_logprobs=got.top_logprobs, top_ids=got.top_ids)
-            return out
-        if st["op"] == "distill":
-            loss, grad = scoring.distill_loss_and_grad(st["logits"], st["ids"], st["teacher"], weight=st["weight"],
-                                                       rest=st["rest"], temperature=st["temperature"])
-            return dict(loss=loss, grad=grad)
-        dq, dk, dv = attention.attention_backward(st["dout"], st["q"], st["k"], st["v"], st["out"], st["lse"], st["scale"])
-        return dict(dq=dq, dk=dk, dv=dv)
+        return {"score": _score_own, "distill": _distill_own, "attn": _attn_own}[st["op"]](st)
     return {"score": _score_plain, "distill": _distill_plain, "attn": _attn_plain}[st["op"]](st)
 
 
