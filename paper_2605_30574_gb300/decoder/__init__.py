@@ -49,7 +49,11 @@ def lib() -> ctypes.CDLL:
         L.decoder_distill_vocab.argtypes = [i]
         L.decoder_distill_vocab.restype = l
         L.decoder_distill.argtypes = [vp, i, l, l, l, vp, vp, i, vp, i, ctypes.c_double, vp, vp, vp]
-        for fn in (L.decoder_token_scores, L.decoder_distill, L.decoder_qkv, L.decoder_block, L.decoder_causal, L.decoder_gemm, L.decoder_gemm_plan, L.decoder_error, L.decoder_rms_norm, L.decoder_add_rms_norm, L.decoder_add, L.decoder_to_bf16, L.decoder_silu_mul,
+        L.decoder_attention.argtypes = [vp] * 3 + [ctypes.POINTER(l), vp, vp, l, l, l, i, i, i, f, vp]
+        L.decoder_attention_scratch.argtypes = [l, l, i]
+        L.decoder_attention_scratch.restype = l
+        L.decoder_attention_backward.argtypes = [vp] * 6 + [ctypes.POINTER(l), vp, vp, vp, vp, l, l, l, i, i, i, f, vp]
+        for fn in (L.decoder_attention, L.decoder_attention_backward, L.decoder_token_scores, L.decoder_distill, L.decoder_qkv, L.decoder_block, L.decoder_causal, L.decoder_gemm, L.decoder_gemm_plan, L.decoder_error, L.decoder_rms_norm, L.decoder_add_rms_norm, L.decoder_add, L.decoder_to_bf16, L.decoder_silu_mul,
                    L.decoder_qkv_post):
             fn.restype = i
         _LIB = L

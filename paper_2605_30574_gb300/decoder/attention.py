@@ -1,0 +1,144 @@
+"""Causal attention with its gradients, for one sequence or a batch.
+
+``attention`` is differentiable; ``attention_forward`` and
+``attention_backward`` are its halves for callers without autograd.  The
+queries are the last Tq positions of the Tk that keys and values cover: a whole
+prompt (Tq = Tk), a continuation of a cached span (Tq < Tk), one token
+(Tq = 1).  With Tq above Tk the first Tq - Tk rows see no key: their outputs
+and gradients are 0.
+
+q is [Tq, Hq, d] and k, v are [Hkv, Tk, d] (as the decoder's stores lay a layer
+out), or all with a batch in front; bf16, d 64, 128 or 256, Hq a multiple of
+Hkv, any strides (those that the kernels cannot read are copied).  Scores, sums
+and gradients are accumulated in fp32; probabilities and the gradients of scores
+are rounded to bf16 for their products.  The same inputs give the same bits.
+
+Kernels go to torch's current stream; a bounded wait that ran out shows in
+``decoder.check_device_error``.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from . import BF16, F32, _current_device, _launch, lib
+
+
+def _check(what, q, k, v):
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
+            raise TypeError(f"{what}: {name} must be a bf16 tensor")
+        if t.device.type != "cuda" or t.device != q.device:
+            raise ValueError(f"{what}: q, k and v must be on one CUDA device")
+    if q.dim() not in (3, 4) or k.dim() != q.dim() or k.shape != v.shape:
+        raise ValueError(f"{what}: q must be [Tq, Hq, d] and k, v [Hkv, Tk, d], or all with a batch in front")
+    Hq, d, Hkv = q.shape[-2], q.shape[-1], k.shape[-3]
+    if d not in (64, 128, 256) or k.shape[-1] != d or (q.dim() == 4 and k.shape[0] != q.shape[0]):
+        raise ValueError(f"{what}: heads of 64, 128 or 256, the same for q, k and v, and one batch")
+    if Hkv == 0 or Hq == 0 or Hq % Hkv:
+        raise ValueError(f"{what}: the query heads must be a multiple of the kv heads")
+
+
+def _operand(t, heads_first):
+    """The tensor, or a copy that the kernels can read, and its (row, head,
+    batch) strides."""
+    def strides(t):
+        s = t.stride()
+        return (s[-2], s[-3], s[0]) if heads_first else (s[-3], s[-2], s[0])
+
+    sizes = (t.shape[-2], t.shape[-3]) if heads_first else (t.shape[-3], t.shape[-2])
+    sizes += (t.shape[0] if t.dim() == 4 else 1,)
+    st = strides(t)
+    if t.stride(-1) != 1 or t.data_ptr() & 15 or t.is_neg() \
+            or any(n > 1 and (s <= 0 or s & 7 or s >= 1 << 38) for n, s in zip(sizes, st)):
+        t = t.resolve_neg().clone(memory_format=torch.contiguous_format)
+        st = strides(t)
+    return t, st
+
+
+def _sizes(q, k):
+    return (q.shape[0] if q.dim() == 4 else 1, *q.shape[-3:], k.shape[-3], k.shape[-2])
+
+
+def _scale(scale, d):
+    return 1.0 / math.sqrt(d) if scale is None else float(scale)
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                      scale: Optional[float] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention's output, like q and contiguous, and the rows' log sums of
+    e^(scale q . k), fp32 [Hq, Tq] ([B, Hq, Tq]); -inf for a row that sees no
+    key.  ``scale`` is 1 / sqrt(d) by default."""
+    _check("attention_forward", q, k, v)
+    if q.device.index != _current_device():
+        with torch.cuda.device(q.device):
+            return attention_forward(q, k, v, scale)
+    B, Tq, Hq, d, Hkv, Tk = _sizes(q, k)
+    out = torch.empty(q.shape, dtype=BF16, device=q.device)
+    lse = torch.empty((*q.shape[:-3], Hq, Tq), dtype=F32, device=q.device)
+    if B * Tq * Tk == 0:
+        return out.zero_(), lse.fill_(-math.inf)
+    (q, sq), (k, sk), (v, sv) = _operand(q, False), _operand(k, True), _operand(v, True)
+    _launch("decoder_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), (ctypes.c_long * 9)(*sq, *sk, *sv), out.data_ptr(),
+            lse.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
+    return out, lse
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                       lse: torch.Tensor, scale: Optional[float] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients with respect to q, k and v (bf16, contiguous), given the
+    output's, and output and log sums as ``attention_forward`` gave them."""
+    what = "attention_backward"
+    _check(what, q, k, v)
+    for name, t in (("dout", dout), ("out", out)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
+            raise TypeError(f"{what}: {name} must be a bf16 tensor")
+        if t.shape != q.shape or t.device != q.device:
+            raise ValueError(f"{what}: {name} must be like q")
+    B, Tq, Hq, d, Hkv, Tk = _sizes(q, k)
+    if not isinstance(lse, torch.Tensor) or lse.dtype is not F32:
+        raise TypeError(f"{what}: lse must be an fp32 tensor")
+    if lse.shape != (*q.shape[:-3], Hq, Tq) or lse.device != q.device:
+        raise ValueError(f"{what}: lse must be [Hq, Tq], or [B, Hq, Tq]")
+    if q.device.index != _current_device():
+        with torch.cuda.device(q.device):
+            return attention_backward(dout, q, k, v, out, lse, scale)
+    if B * Tq * Tk == 0:
+        return torch.zeros_like(q, memory_format=torch.contiguous_format), \
+            torch.zeros_like(k, memory_format=torch.contiguous_format), \
+            torch.zeros_like(v, memory_format=torch.contiguous_format)
+    dq = torch.empty(q.shape, dtype=BF16, device=q.device)
+    dk = torch.empty(k.shape, dtype=BF16, device=q.device)
+    dv = torch.empty(k.shape, dtype=BF16, device=q.device)
+    scratch = torch.empty(lib().decoder_attention_scratch(B, Tq, Hq), dtype=torch.uint8, device=q.device)
+    (dout, so), (q, sq), (out, su) = (_operand(t, False) for t in (dout, q, out))
+    (k, sk), (v, sv) = _operand(k, True), _operand(v, True)
+    lse = lse.resolve_neg().contiguous()
+    _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+            lse.data_ptr(), (ctypes.c_long * 15)(*so, *sq, *sk, *sv, *su), scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
+    return dq, dk, dv
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale):
+        out, lse = attention_forward(q, k, v, scale)
+        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.scale = scale
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse = ctx.saved_tensors
+        return (*attention_backward(dout, q, k, v, out, lse, ctx.scale), None)
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: Optional[float] = None) -> torch.Tensor:
+    """Causal attention of q over k and v, differentiable with respect to all
+    three; see the module for the layouts."""
+    return _Attention.apply(q, k, v, scale)

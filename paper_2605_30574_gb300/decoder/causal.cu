@@ -16,6 +16,9 @@
 // that torch picks: 256 tokens 7.2 us, 16.2; 1024 22.9, 53.4; 4096 143, 427; no
 // further from 64 bits at any size.
 //
+// With the rows' log sums (LSE), for the gradients of attention_grad.cu: a batch,
+// queries that are the last T of Tk positions, any strides.
+//
 // Every wait is bounded, as in gemm.cu.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -26,11 +29,17 @@
 
 #include "../csrc/per_device.h"
 #include "../csrc/tc_ptx.cuh"
+#include "attention.cuh"
 #include "decoder.h"
 
 namespace tc = splice::tc;
 
 namespace {
+
+using decoder::ex2;
+using decoder::mma_f16_ts;
+using decoder::tma_load_4d;
+using decoder::tmem_ld32_done;
 
 constexpr int kRows = 128, kBN = 64, kThreads = 192;     // softmax: warps 0-3
 constexpr int kLoadWarp = 4, kMmaWarp = 5;
@@ -48,47 +57,11 @@ struct Cfg {
     static_assert(COL_O + D <= TMEM && CTAS * TMEM <= 512 && (CTAS + 1) * (SMEM + 1024) > 228 * 1024);
 };
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// A = P (bf16 pairs, in TMEM), B = V (smem descriptor).
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int32_t x, int32_t y, int32_t z, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
-}
-
-// 32 columns of this thread's lane, complete when it returns (one statement, so
-// that nothing that uses the values can be moved between load and wait).
-__device__ __forceinline__ void tmem_ld32_done(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-template <int D>
+template <int D, bool LSE>
 __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     causal_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                  const __grid_constant__ CUtensorMap tm_v, __nv_bfloat16* out, int T, int Hq, int G, float scale_log2,
-                  unsigned* err) {
+                  const __grid_constant__ CUtensorMap tm_v, __nv_bfloat16* out, float* lse, int T, int Tk, int Hq, int G,
+                  int heads, float scale_log2, unsigned* err) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[15];
@@ -103,8 +76,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     auto sfull = [&](int i) { return bar0 + 88 + 8u * i; };
     auto pfull = [&](int i) { return bar0 + 104 + 8u * i; };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int head = int(blockIdx.x) % Hq, row0 = ((T + kRows - 1) / kRows - 1 - int(blockIdx.x) / Hq) * kRows;
-    const int nblk = (min(T, row0 + kRows) + kBN - 1) / kBN;
+    const int at = int(blockIdx.x) % heads, head = at % Hq, batch = at / Hq;
+    const int row0 = ((T + kRows - 1) / kRows - 1 - int(blockIdx.x) / heads) * kRows;
+    const int shift = Tk - T;            // row i sees the keys up to i + shift
+    const int nblk = max(0, (min(Tk, row0 + kRows + shift) + kBN - 1) / kBN);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 13; ++i) tc::mbar_init(bar0 + 8u * i, 1);
@@ -134,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
         if (leader) {
             tc::mbar_arrive_expect_tx(qfull, C::Q_BYTES);
 #pragma unroll
-            for (int p = 0; p < C::PANELS; ++p) tma_load_3d(sbase + p * (kRows * 128), &tm_q, p * 64, head, row0, qfull);
+            for (int p = 0; p < C::PANELS; ++p) tma_load_4d(sbase + p * (kRows * 128), &tm_q, p * 64, row0, head, batch, qfull);
         }
         int j = 0;
         for (; j < nblk; ++j) {
@@ -145,14 +120,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
                 tc::mbar_arrive_expect_tx(kfull(s), C::KV_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_3d(sbase + C::OFF_K + s * C::KV_BYTES + p * (kBN * 128), &tm_k, p * 64, j * kBN, hk, kfull(s));
+                    tma_load_4d(sbase + C::OFF_K + s * C::KV_BYTES + p * (kBN * 128), &tm_k, p * 64, j * kBN, hk, batch, kfull(s));
             }
             if (!__all_sync(0xffffffffu, tc::mbar_wait(vempty(s), phase, &s_abort, err, kErrLoad))) break;
             if (leader) {
                 tc::mbar_arrive_expect_tx(vfull(s), C::KV_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_3d(sbase + C::OFF_V + s * C::KV_BYTES + p * (kBN * 128), &tm_v, p * 64, j * kBN, hk, vfull(s));
+                    tma_load_4d(sbase + C::OFF_V + s * C::KV_BYTES + p * (kBN * 128), &tm_v, p * 64, j * kBN, hk, batch, vfull(s));
             }
         }
         // Every copy issued must land before the CTA may exit.  (A broken-off
@@ -206,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
                 for (int kk = 0; kk < kBN / 16; ++kk) {
                     const uint64_t b = tc::sw128_desc(sbase + C::OFF_V + s * C::KV_BYTES + kk * 16 * 128, kBN * 128, 1024);
                     mma_f16_ts(tmem + C::COL_O, tmem + s * kBN + kk * 8, b, idesc_pv, j > 0 || kk > 0 ? 1u : 0u);
+                    if constexpr (LSE) mma_f16_ts(tmem + C::COL_O, tmem + s * kBN + 32 + kk * 8, b, idesc_pv, 1u);
                 }
                 tc::mma_commit(vempty(s));
                 tc::mma_commit(pvdone);
@@ -220,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     } else {
         const int row = row0 + warp * 32 + lane;
         const uint32_t mine = tmem + (uint32_t(warp * 32) << 16);
-        float m = 0.f, l = 0.f;
+        float m = nblk ? 0.f : -INFINITY, l = 0.f;
         bool ok = true;
         // A positive scale goes in with the exponent's fma, past the masking and
         // the maximum; one of zero or below would make NaN or +inf of a masked
@@ -239,8 +215,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
 #pragma unroll
                 for (int i = 0; i < kBN; ++i) v[i >> 5][i & 31] *= scale_log2;
             }
-            if ((j + 1) * kBN > row0 + 1) {          // the diagonal's blocks
-                const int last = row - j * kBN;      // this row's last key in the block
+            if ((j + 1) * kBN > row0 + shift + 1) {          // the diagonal's blocks
+                const int last = row + shift - j * kBN;      // this row's last key in the block
 #pragma unroll
                 for (int i = 0; i < kBN; ++i)
                     if (i > last) v[i >> 5][i & 31] = -INFINITY;
@@ -272,24 +248,27 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
             // a row whose every score so far is -inf has no weights yet
             const float ref = m == -INFINITY ? 0.f : m;
             // (the weights as they are used, rounded: their sum then makes up
-            // for part of the rounding)
+            // for part of the rounding.  LSE: as they are, and used in two
+            // terms of bf16, as the gradients take the difference of their
+            // product with this output)
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                uint32_t pk[16];
+                uint32_t pk[16], low[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float a = ex2(fmaf(v[half][2 * i], scale_later, -ref)), b = ex2(fmaf(v[half][2 * i + 1], scale_later, -ref));
                     const __nv_bfloat162 p2 = __floats2bfloat162_rn(a, b);
                     pk[i] = *reinterpret_cast<const uint32_t*>(&p2);
-                    part[i & 3] += __low2float(p2) + __high2float(p2);
+                    if constexpr (LSE) {
+                        low[i] = decoder::pack_bf16(a - __low2float(p2), b - __high2float(p2));
+                        part[i & 3] += a + b;
+                    } else {
+                        part[i & 3] += __low2float(p2) + __high2float(p2);
+                    }
                 }
-                asm volatile(
-                    "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-                    "%14, %15, %16};" ::"r"(mine + s * kBN + half * 16),
-                    "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3]), "r"(pk[4]), "r"(pk[5]), "r"(pk[6]), "r"(pk[7]), "r"(pk[8]),
-                    "r"(pk[9]), "r"(pk[10]), "r"(pk[11]), "r"(pk[12]), "r"(pk[13]), "r"(pk[14]), "r"(pk[15])
-                    : "memory");
+                if constexpr (LSE) decoder::tmem_st16(mine + s * kBN + 32 + half * 16, low);
+                decoder::tmem_st16(mine + s * kBN + half * 16, pk);
             }
             l += (part[0] + part[1]) + (part[2] + part[3]);
             tc::tmem_wait_st();
@@ -303,15 +282,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
             tc::tc_fence_before();
             tc::mbar_arrive(pfull(s));
         }
-        if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(pvdone, uint32_t(nblk - 1) & 1u, &s_abort, err, kErrOut));
+        if (ok && nblk) ok = __all_sync(0xffffffffu, tc::mbar_wait(pvdone, uint32_t(nblk - 1) & 1u, &s_abort, err, kErrOut));
         if (ok) {
             tc::tc_fence_after();
             const float inv = l == 0.f ? 0.f : 1.f / l;   // (no weights at all: zeros)
-            uint4* dst = reinterpret_cast<uint4*>(out + (size_t(row) * Hq + head) * D);
+            if constexpr (LSE) {
+                if (row < T) lse[size_t(at) * T + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            }
+            uint4* dst = reinterpret_cast<uint4*>(out + ((size_t(batch) * T + row) * Hq + head) * D);
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
                 float o[32];
-                tmem_ld32_done(mine + C::COL_O + c, o);
+                if (nblk) {
+                    tmem_ld32_done(mine + C::COL_O + c, o);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0.f;
+                }
                 if (row < T) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -334,34 +321,24 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     if (warp == kMmaWarp) tc::tmem_dealloc(tmem, C::TMEM);
 }
 
-// [z][y][x] bf16, strides in elements (x: 1); box of bz x by x 64, 128-byte
-// swizzle, zeros outside.
-bool make_map(CUtensorMap* m, const void* base, int x, int y, int z, size_t sy, size_t sz, int by, int bz) {
-    decoder::EncodeFn enc = decoder::encode_fn();
-    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {sy * 2, sz * 2};
-    const cuuint32_t box[3] = {64, cuuint32_t(by), cuuint32_t(bz)}, es[3] = {1, 1, 1};
-    return enc && enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
-                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <int D>
-int launch(const void* q, const void* k, const void* v, void* out, int T, int Hq, int Hkv, float scale, cudaStream_t st) {
+template <int D, bool LSE>
+int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::Operand& v, void* out, float* lse, int B, int Tq, int Tk,
+           int Hq, int Hkv, float scale, cudaStream_t st) {
     using C = Cfg<D>;
     static splice::PerDevice<bool> kept;
     bool set = false;
     const cudaError_t e = kept.get(&set, [](int, bool* done) {
         *done = true;
-        return cudaFuncSetAttribute(causal_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM));
+        return cudaFuncSetAttribute(causal_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM));
     });
     if (e != cudaSuccess) return int(e);
     unsigned* err = decoder::error_word();
     CUtensorMap mq, mk, mv;
-    if (!err || !make_map(&mq, q, D, Hq, T, D, size_t(Hq) * D, 1, kRows) ||
-        !make_map(&mk, k, D, T, Hkv, D, size_t(T) * D, kBN, 1) || !make_map(&mv, v, D, T, Hkv, D, size_t(T) * D, kBN, 1))
+    if (!err || !decoder::operand_map(&mq, q, D, Tq, Hq, B, kRows) || !decoder::operand_map(&mk, k, D, Tk, Hkv, B, kBN) ||
+        !decoder::operand_map(&mv, v, D, Tk, Hkv, B, kBN))
         return int(cudaErrorInvalidValue);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((T + kRows - 1) / kRows) * unsigned(Hq));
+    cfg.gridDim = dim3(unsigned((Tq + kRows - 1) / kRows) * unsigned(Hq) * unsigned(B));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
@@ -370,8 +347,18 @@ int launch(const void* q, const void* k, const void* v, void* out, int T, int Hq
     a.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &a;
     cfg.numAttrs = 1;
-    return int(cudaLaunchKernelEx(&cfg, causal_kernel<D>, mq, mk, mv, static_cast<__nv_bfloat16*>(out), T, Hq, Hq / Hkv,
-                                  scale * 1.4426950408889634f, err));
+    return int(cudaLaunchKernelEx(&cfg, causal_kernel<D, LSE>, mq, mk, mv, static_cast<__nv_bfloat16*>(out), lse, Tq, Tk, Hq, Hq / Hkv,
+                                  Hq * B, scale * 1.4426950408889634f, err));
+}
+
+template <bool LSE>
+int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::Operand& v, void* out, float* lse, long B, long Tq, long Tk,
+           int Hq, int Hkv, int d, float scale, cudaStream_t st) {
+    if (!decoder::attention_takes(B, Tq, Tk, Hq, Hkv)) return int(cudaErrorInvalidValue);
+    if (d == 64) return launch<64, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
+    if (d == 128) return launch<128, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
+    if (d == 256) return launch<256, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
+    return int(cudaErrorInvalidValue);
 }
 
 }  // namespace
@@ -381,12 +368,21 @@ extern "C" {
 // See the head of this file; 16-byte aligned.  Returns a cudaError_t.
 int decoder_causal(const void* q, const void* k, const void* v, void* out, long T, int Hq, int Hkv, int d, float scale,
                    void* stream) {
-    if (T < 1 || T > (1 << 20) || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return int(cudaErrorInvalidValue);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (d == 64) return launch<64>(q, k, v, out, int(T), Hq, Hkv, scale, st);
-    if (d == 128) return launch<128>(q, k, v, out, int(T), Hq, Hkv, scale, st);
-    if (d == 256) return launch<256>(q, k, v, out, int(T), Hq, Hkv, scale, st);
-    return int(cudaErrorInvalidValue);
+    const decoder::Operand oq{q, long(Hq) * d, d, T * Hq * d}, ok{k, d, T * d, T * Hkv * d}, ov{v, d, T * d, T * Hkv * d};
+    return launch<false>(oq, ok, ov, out, nullptr, 1, T, T, Hq, Hkv, d, scale, static_cast<cudaStream_t>(stream));
+}
+
+// The same for B sequences whose queries are the last Tq positions of the Tk
+// (Tq above Tk: the first rows see nothing), with the rows' log sums: q
+// [B][Tq][Hq][d], k, v [B][Hkv][Tk][d] of any strides that are multiples of 8
+// elements (q row, head, batch, k row, head, batch, v row, head, batch), out
+// [B][Tq][Hq][d] contiguous, lse fp32 [B][Hq][Tq] (natural log of the sum of
+// e^(scale q . k), -inf for a row that sees nothing).
+int decoder_attention(const void* q, const void* k, const void* v, const long* strides, void* out, void* lse, long B, long Tq,
+                      long Tk, int Hq, int Hkv, int d, float scale, void* stream) {
+    const decoder::Operand oq{q, strides[0], strides[1], strides[2]}, ok{k, strides[3], strides[4], strides[5]},
+        ov{v, strides[6], strides[7], strides[8]};
+    return launch<true>(oq, ok, ov, out, static_cast<float*>(lse), B, Tq, Tk, Hq, Hkv, d, scale, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

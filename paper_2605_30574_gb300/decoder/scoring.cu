@@ -20,6 +20,7 @@
 
 #include "../csrc/per_device.h"
 #include "../csrc/tc_ptx.cuh"
+#include "attention.cuh"
 #include "decoder.h"
 
 namespace cg = cooperative_groups;
@@ -27,16 +28,13 @@ namespace tc = splice::tc;
 
 namespace {
 
+using decoder::bulk_load;
+using decoder::ex2;
+
 constexpr int kMaxTop = 128, kMaxCluster = 8;
 constexpr unsigned kErrRow = 256;
 constexpr float kNone = -INFINITY;
 constexpr double kLog2e = 1.4426950408889634;
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -449,12 +447,6 @@ struct DistillParams {
     void* grad;                 // or NULL
     unsigned* err;
 };
-
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(bar)
-                 : "memory");
-}
 
 // Sums a value of each thread, or takes the largest, in a fixed order.
 template <class V, class Op>
