@@ -27,7 +27,20 @@ import torch
 from . import BF16, F32, _current_device, _launch, lib
 
 
+def _fits(q, k, v):
+    """Whether the arguments are as they have to be."""
+    try:
+        (Hq, d), (Hkv, _, dk), device = q.shape[-2:], k.shape[-3:], q.device
+        return (q.dtype is k.dtype is v.dtype is BF16 and device.type == "cuda" and device == k.device == v.device
+                and k.shape == v.shape and q.dim() == k.dim() and (q.dim() == 3 or q.dim() == 4 and q.shape[0] == k.shape[0])
+                and d == dk and d in (64, 128, 256) and Hkv > 0 and Hq > 0 and Hq % Hkv == 0)
+    except (AttributeError, ValueError):
+        return False
+
+
 def _check(what, q, k, v):
+    if _fits(q, k, v):
+        return
     for name, t in (("q", q), ("k", k), ("v", v)):
         if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
             raise TypeError(f"{what}: {name} must be a bf16 tensor")
@@ -35,11 +48,13 @@ def _check(what, q, k, v):
             raise ValueError(f"{what}: q, k and v must be on one CUDA device")
     if q.dim() not in (3, 4) or k.dim() != q.dim() or k.shape != v.shape:
         raise ValueError(f"{what}: q must be [Tq, Hq, d] and k, v [Hkv, Tk, d], or all with a batch in front")
-    Hq, d, Hkv = q.shape[-2], q.shape[-1], k.shape[-3]
-    if d not in (64, 128, 256) or k.shape[-1] != d or (q.dim() == 4 and k.shape[0] != q.shape[0]):
+    if k.shape[-1] != q.shape[-1] or q.shape[-1] not in (64, 128, 256) or (q.dim() == 4 and k.shape[0] != q.shape[0]):
         raise ValueError(f"{what}: heads of 64, 128 or 256, the same for q, k and v, and one batch")
-    if Hkv == 0 or Hq == 0 or Hq % Hkv:
-        raise ValueError(f"{what}: the query heads must be a multiple of the kv heads")
+    raise ValueError(f"{what}: the query heads must be a multiple of the kv heads")
+
+
+def _plain(t):
+    return t.is_contiguous() and not t.data_ptr() & 15 and not t.is_neg()
 
 
 def _operand(t, heads_first):
@@ -57,6 +72,16 @@ def _operand(t, heads_first):
         t = t.resolve_neg().clone(memory_format=torch.contiguous_format)
         st = strides(t)
     return t, st
+
+
+def _operands(rows_first, heads_first):
+    """Both groups as the kernels can read them, and their strides as a C array
+    (None: all contiguous)."""
+    if all(map(_plain, rows_first)) and all(map(_plain, heads_first)):
+        return rows_first, heads_first, None
+    got = [[_operand(t, first) for t in ts] for ts, first in ((rows_first, False), (heads_first, True))]
+    flat = [s for ts in got for _, st in ts for s in st]
+    return [t for t, _ in got[0]], [t for t, _ in got[1]], (ctypes.c_long * len(flat))(*flat)
 
 
 def _sizes(q, k):
@@ -81,9 +106,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     lse = torch.empty((*q.shape[:-3], Hq, Tq), dtype=F32, device=q.device)
     if B * Tq * Tk == 0:
         return out.zero_(), lse.fill_(-math.inf)
-    (q, sq), (k, sk), (v, sv) = _operand(q, False), _operand(k, True), _operand(v, True)
-    _launch("decoder_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), (ctypes.c_long * 9)(*sq, *sk, *sv), out.data_ptr(),
-            lse.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
+    (q,), (k, v), strides = _operands((q,), (k, v))
+    _launch("decoder_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, out.data_ptr(), lse.data_ptr(), B, Tq, Tk, Hq,
+            Hkv, d, _scale(scale, d))
     return out, lse
 
 
@@ -114,12 +139,11 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     dk = torch.empty(k.shape, dtype=BF16, device=q.device)
     dv = torch.empty(k.shape, dtype=BF16, device=q.device)
     scratch = torch.empty(lib().decoder_attention_scratch(B, Tq, Hq), dtype=torch.uint8, device=q.device)
-    (dout, so), (q, sq), (out, su) = (_operand(t, False) for t in (dout, q, out))
-    (k, sk), (v, sv) = _operand(k, True), _operand(v, True)
+    (dout, q, out), (k, v), strides = _operands((dout, q, out), (k, v))
     lse = lse.resolve_neg().contiguous()
-    _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-            lse.data_ptr(), (ctypes.c_long * 15)(*so, *sq, *sk, *sv, *su), scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-            dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
+    _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), out.data_ptr(), k.data_ptr(), v.data_ptr(),
+            lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d,
+            _scale(scale, d))
     return dq, dk, dv
 
 

@@ -18,14 +18,17 @@
 //   kKeys    K   V    Q   dO    dV                  dK
 //   kQueries Q   dO   K   V     -                   dQ
 //
-// S = F1 X1^T and dP = F2 X2^T (128 x 64, fp32 in TMEM, two slots each), the
-// element operations by two warpgroups that take every other block (a thread
-// per row), P and dS rounded to bf16 over their slots as the A operands of the
-// second products.  One warp issues all MMAs in the order dV(j) dK(j) S(j+2)
-// dP(j+2): S(j+2) waits for dV(j)'s reading of its slot under dK(j), dP(j+2)
-// for dK(j)'s under S(j+2).
+// S = F1 X1^T and dP = F2 X2^T go to TMEM in fp32; two warpgroups, a thread per
+// row and each with half of a block's columns, make P and dS of them, rounded
+// to bf16 over their half as the A operands of the second products.  One warp
+// issues all MMAs.  By keys, TMEM is full with one slot each for S and dP and the
+// two sums (128 dims), and the order is dV(j) S(j+1) dK(j) dP(j+1): P(j+1) is made
+// under dK(j) and dP(j+1), dS(j+1) under dV(j+1) and S(j+2).  By queries there are
+// two slots for dP, and the order S(j+1) dP(j+1) dQ(j) leaves no gap.  Blocks are
+// of 128: an MMA of 64 columns reads its A operand twice as often, and takes 48
+// clocks in place of 32.
 //
-// 256 dims: blocks of 32, and dK and dV, which do not fit in TMEM together, in
+// 256 dims: blocks of 64, and dK and dV, which do not fit in TMEM together, in
 // a launch each.
 //
 // Every wait is bounded, as in gemm.cu.
@@ -55,25 +58,28 @@ using decoder::tma_load_4d;
 using decoder::tmem_ld32_done;
 using decoder::tmem_st16;
 
-constexpr int kRows = 128, kThreads = 320, kLoadWarp = 8, kMmaWarp = 9, kMaxStages = 4, kMaxShares = 8;
+constexpr int kRows = 128, kThreads = 320, kLoadWarp = 8, kMmaWarp = 9, kMaxStages = 3, kMaxShares = 8;
 constexpr unsigned kErrLoad = 512, kErrMma = 1024, kErrOut = 2048, kErrDrain = 4096;
 enum Pass { kKeys, kValuesOnly, kKeysOnly, kQueries };     // (both, dV, dK; dQ)
 
 template <int D, int PASS>
 struct Cfg {
     static constexpr bool BY_KEYS = PASS != kQueries, OUT_P = PASS == kKeys || PASS == kValuesOnly, OUT_S = PASS != kValuesOnly;
-    static constexpr bool DP = OUT_S;                      // whether dP is needed
-    static constexpr int BX = D == 256 ? 32 : 64, PANELS = D / 64;
-    static constexpr int STAGES = D == 256 ? 3 : 4;
+    static constexpr int BX = D == 256 ? 64 : 128, PANELS = D / 64, HALF = BX / 2;     // (a warpgroup's columns)
+    // rings of X1 and X2; X2 is done with when dP is, unless P meets it again
+    static constexpr int R1 = D == 64 ? 3 : 2, R2 = D == 64 ? 3 : D == 256 && !OUT_P ? 1 : 2;
     static constexpr uint32_t F_BYTES = kRows * D * 2, X_BYTES = BX * D * 2;
+    // the rows' statistics come with the operand that is kept longer
     static constexpr uint32_t STAT_BYTES = BY_KEYS ? 2 * BX * 4 : 0;
-    static constexpr uint32_t OFF_F2 = F_BYTES, OFF_X = OFF_F2 + (DP ? F_BYTES : 0);
-    static constexpr uint32_t OFF_STAT = OFF_X + STAGES * 2 * X_BYTES, BYTES = OFF_STAT + STAGES * STAT_BYTES;
+    static constexpr int RS = OUT_S ? R1 : R2;
+    static constexpr uint32_t OFF_F2 = F_BYTES, OFF_X1 = OFF_F2 + (OUT_S ? F_BYTES : 0), OFF_X2 = OFF_X1 + R1 * X_BYTES;
+    static constexpr uint32_t OFF_STAT = OFF_X2 + R2 * X_BYTES, BYTES = OFF_STAT + RS * STAT_BYTES;
     static constexpr int OUTS = (OUT_P ? 1 : 0) + (OUT_S ? 1 : 0);
     static constexpr int COLS = OUTS * D / 2;              // a warpgroup's columns of the sums
     static constexpr int UNITS = COLS / 16;
-    // TMEM columns
-    static constexpr uint32_t COL_S = 0, COL_DP = 128, COL_SUM = 256, COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
+    // TMEM columns; slots of S and of dP
+    static constexpr int NS = OUT_S ? 1 : 2, ND = !OUT_S ? 0 : OUT_P ? 1 : 2;
+    static constexpr uint32_t COL_DP = NS * BX, COL_SUM = COL_DP + ND * BX, COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
     static_assert(COL_S_SUM + (OUT_S ? D : 0) <= 512);
     static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * 2 * ((UNITS + shares - 1) / shares) * 16 * kRows * 4; }
     // (more than half of an SM's, so that no two CTAs of these kernels share one:
@@ -102,23 +108,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     grad_kernel(const __grid_constant__ CUtensorMap tm_f1, const __grid_constant__ CUtensorMap tm_f2,
                 const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const GradParams P) {
     using C = Cfg<D, PASS>;
-    constexpr int BX = C::BX, ST = C::STAGES;
+    constexpr int BX = C::BX, HALF = C::HALF, NS = C::NS, ND = C::ND > 0 ? C::ND : 1;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 15];
+    constexpr int kBars = 4 * kMaxStages + 16;
+    __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sbase = tc::smem_u32(smem), bar0 = tc::smem_u32(bars);
-    auto full = [&](int i) { return bar0 + 8u * i; };
-    auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
-    const uint32_t bar1 = bar0 + 8u * 2 * kMaxStages;
+    auto x1_full = [&](int i) { return bar0 + 8u * i; };
+    auto x1_empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
+    auto x2_full = [&](int i) { return bar0 + 8u * (2 * kMaxStages + i); };
+    auto x2_empty = [&](int i) { return bar0 + 8u * (3 * kMaxStages + i); };
+    const uint32_t bar1 = bar0 + 8u * 4 * kMaxStages;
     auto s_full = [&](int i) { return bar1 + 8u * i; };
     auto dp_full = [&](int i) { return bar1 + 8u * (2 + i); };
     auto p_ready = [&](int i) { return bar1 + 8u * (4 + i); };
     auto ds_ready = [&](int i) { return bar1 + 8u * (6 + i); };
     auto p_taken = [&](int i) { return bar1 + 8u * (8 + i); };
     auto ds_taken = [&](int i) { return bar1 + 8u * (10 + i); };
-    const uint32_t f_full = bar1 + 8u * 12, sums = bar1 + 8u * 13, drain = bar1 + 8u * 14;
+    const uint32_t f_full = bar1 + 8u * 12, sums = bar1 + 8u * 13, drain = bar1 + 8u * 14, s_read = bar1 + 8u * 15;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
     const int share = P.shares > 1 ? int(cluster.block_rank()) : 0;
@@ -143,11 +152,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int j0 = int(all * share / P.shares), n = int(all * (share + 1) / P.shares) - j0;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2 * kMaxStages + 15; ++i) tc::mbar_init(bar0 + 8u * i, 1);
+        for (int i = 0; i < kBars; ++i) tc::mbar_init(bar0 + 8u * i, 1);
         for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(p_ready(i), kRows);
-            tc::mbar_init(ds_ready(i), kRows);
+            tc::mbar_init(p_ready(i), 2 * kRows);
+            tc::mbar_init(ds_ready(i), 2 * kRows);
         }
+        tc::mbar_init(s_read, 2 * kRows);
         s_abort = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tm_f1);
@@ -175,118 +185,146 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == kLoadWarp) {
         const bool leader = tc::elect_one();
         if (n > 0 && leader) {
-            tc::mbar_arrive_expect_tx(f_full, C::DP ? 2 * C::F_BYTES : C::F_BYTES);
+            tc::mbar_arrive_expect_tx(f_full, C::OUT_S ? 2 * C::F_BYTES : C::F_BYTES);
 #pragma unroll
             for (int p = 0; p < C::PANELS; ++p) {
                 tma_load_4d(sbase + p * (kRows * 128), &tm_f1, p * 64, row0, head, batch, f_full);
-                if (C::DP) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
+                if (C::OUT_S) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
             }
         }
-        int j = 0;
-        for (; j < n; ++j) {
-            const int s = j % ST;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait(empty(s), (uint32_t(j / ST) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
+        int j1 = 0, j2 = 0;      // blocks asked for
+        for (int j = 0; j < n; ++j) {
+            const int at = (first + (j0 + j) % per) * BX;
+            const int x_head = C::BY_KEYS ? head * G + (j0 + j) / per : head / G;
+            auto statistics = [&](int s, uint32_t bar) {
+                const long stat = (long(batch) * P.Hq + x_head) * P.Tpad + at;
+                const uint32_t to = sbase + C::OFF_STAT + uint32_t(s) * C::STAT_BYTES;
+                decoder::bulk_load(to, P.lse2 + stat, BX * 4, bar);
+                decoder::bulk_load(to + BX * 4, P.delta + stat, BX * 4, bar);
+            };
+            const int s1 = j % C::R1, s2 = j % C::R2;
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(x1_empty(s1), (uint32_t(j / C::R1) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
             if (!ok) break;
             if (leader) {
-                const int at = (first + (j0 + j) % per) * BX;
-                const int x_head = C::BY_KEYS ? head * G + (j0 + j) / per : head / G;
-                const uint32_t to = sbase + C::OFF_X + uint32_t(s) * 2 * C::X_BYTES;
-                tc::mbar_arrive_expect_tx(full(s), 2 * C::X_BYTES + C::STAT_BYTES);
+                tc::mbar_arrive_expect_tx(x1_full(s1), C::X_BYTES + (C::OUT_S ? C::STAT_BYTES : 0));
 #pragma unroll
-                for (int p = 0; p < C::PANELS; ++p) {
-                    tma_load_4d(to + p * (BX * 128), &tm_x1, p * 64, at, x_head, batch, full(s));
-                    tma_load_4d(to + C::X_BYTES + p * (BX * 128), &tm_x2, p * 64, at, x_head, batch, full(s));
-                }
-                if constexpr (C::BY_KEYS) {
-                    const long stat = (long(batch) * P.Hq + x_head) * P.Tpad + at;
-                    const uint32_t st = sbase + C::OFF_STAT + uint32_t(s) * C::STAT_BYTES;
-                    decoder::bulk_load(st, P.lse2 + stat, BX * 4, full(s));
-                    decoder::bulk_load(st + BX * 4, P.delta + stat, BX * 4, full(s));
-                }
+                for (int p = 0; p < C::PANELS; ++p)
+                    tma_load_4d(sbase + C::OFF_X1 + uint32_t(s1) * C::X_BYTES + p * (BX * 128), &tm_x1, p * 64, at, x_head, batch, x1_full(s1));
+                if constexpr (C::BY_KEYS && C::OUT_S) statistics(s1, x1_full(s1));
             }
+            ++j1;
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(x2_empty(s2), (uint32_t(j / C::R2) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
+            if (!ok) break;
+            if (leader) {
+                tc::mbar_arrive_expect_tx(x2_full(s2), C::X_BYTES + (C::OUT_S ? 0 : C::STAT_BYTES));
+#pragma unroll
+                for (int p = 0; p < C::PANELS; ++p)
+                    tma_load_4d(sbase + C::OFF_X2 + uint32_t(s2) * C::X_BYTES + p * (BX * 128), &tm_x2, p * 64, at, x_head, batch, x2_full(s2));
+                if constexpr (C::BY_KEYS && !C::OUT_S) statistics(s2, x2_full(s2));
+            }
+            ++j2;
         }
         // Every copy issued must land before the CTA may exit, and the commits
         // on the stages' barriers must arrive.
         volatile int no_abort = 0;
         if (n > 0) tc::mbar_wait(f_full, 0, &no_abort, P.err, kErrDrain);
-        for (int i = max(0, j - ST); i < j; ++i) tc::mbar_wait(full(i % ST), uint32_t(i / ST) & 1u, &no_abort, P.err, kErrDrain);
-        for (int i = max(0, j - ST); ok && i < j; ++i)
-            ok = tc::mbar_wait(empty(i % ST), uint32_t(i / ST) & 1u, &s_abort, P.err, kErrDrain);
+        for (int i = max(0, j1 - C::R1); i < j1; ++i) tc::mbar_wait(x1_full(i % C::R1), uint32_t(i / C::R1) & 1u, &no_abort, P.err, kErrDrain);
+        for (int i = max(0, j2 - C::R2); i < j2; ++i) tc::mbar_wait(x2_full(i % C::R2), uint32_t(i / C::R2) & 1u, &no_abort, P.err, kErrDrain);
+        for (int i = max(0, j1 - C::R1); ok && i < j1; ++i)
+            ok = tc::mbar_wait(x1_empty(i % C::R1), uint32_t(i / C::R1) & 1u, &s_abort, P.err, kErrDrain);
+        for (int i = max(0, j2 - C::R2); ok && i < j2; ++i)
+            ok = tc::mbar_wait(x2_empty(i % C::R2), uint32_t(i / C::R2) & 1u, &s_abort, P.err, kErrDrain);
     } else if (warp == kMmaWarp) {
+        // Descriptors are made by the whole warp (see gemm.cu): issued from
+        // values of one lane, an MMA took 72 clocks.
         const bool leader = tc::elect_one();
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(kRows, BX, false), idesc_sum = tc::idesc_bf16_f32(kRows, D, true);
-        auto wait = [&](uint32_t bar, uint32_t phase) {
-            return __all_sync(0xffffffffu, tc::mbar_wait(bar, phase & 1u, &s_abort, P.err, kErrMma));
+        const uint64_t f1 = tc::sw128_desc(sbase, 16, 1024), f2 = tc::sw128_desc(sbase + C::OFF_F2, 16, 1024);
+        const uint64_t x1 = tc::sw128_desc(sbase + C::OFF_X1, 16, 1024), x2 = tc::sw128_desc(sbase + C::OFF_X2, 16, 1024);
+        const uint64_t x1_mn = tc::sw128_desc(sbase + C::OFF_X1, BX * 128, 1024), x2_mn = tc::sw128_desc(sbase + C::OFF_X2, BX * 128, 1024);
+        auto wait = [&](uint32_t bar, int phase) {
+            const bool is = __all_sync(0xffffffffu, tc::mbar_wait(bar, uint32_t(phase) & 1u, &s_abort, P.err, kErrMma));
+            tc::tc_fence_after();
+            return is;
         };
-        // F X^T of block j into its slot
-        auto first_product = [&](int j, uint32_t off_f, uint32_t off_x, uint32_t col, uint32_t done) {
-            const uint32_t x = sbase + C::OFF_X + uint32_t(j % ST) * 2 * C::X_BYTES + off_x;
+        // F X^T into a slot (descriptor units of 16 bytes)
+        auto first_product = [&](uint32_t to, uint64_t f, uint64_t x) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t a = tc::sw128_desc(sbase + off_f + (kk / 4) * (kRows * 128) + (kk % 4) * 32, 16, 1024);
-                const uint64_t b = tc::sw128_desc(x + (kk / 4) * (BX * 128) + (kk % 4) * 32, 16, 1024);
-                tc::mma_f16_ss(tmem + col + uint32_t(j & 1) * 64, a, b, idesc_s, kk > 0 ? 1u : 0u);
+                const uint64_t a = f + uint64_t((kk / 4) * (kRows * 8) + (kk % 4) * 2), b = x + uint64_t((kk / 4) * (BX * 8) + (kk % 4) * 2);
+                if (leader) tc::mma_f16_ss(to, a, b, idesc_s, kk > 0 ? 1u : 0u);
             }
-            tc::mma_commit(done);
         };
-        // the slot's bf16 times X, added up
-        auto second_product = [&](int j, uint32_t off_x, uint32_t col, uint32_t sum) {
-            const uint32_t x = sbase + C::OFF_X + uint32_t(j % ST) * 2 * C::X_BYTES + off_x;
+        // a slot's bf16, in two halves, times X, added up
+        auto second_product = [&](uint32_t sum, uint32_t slot, uint64_t x, bool add) {
 #pragma unroll
-            for (int kk = 0; kk < BX / 16; ++kk)
-                mma_f16_ts(tmem + sum, tmem + col + uint32_t(j & 1) * 64 + kk * 8, tc::sw128_desc(x + kk * 16 * 128, BX * 128, 1024), idesc_sum,
-                           j > 0 || kk > 0 ? 1u : 0u);
-        };
-        bool any = false;
-        ok = n == 0 || wait(f_full, 0);
-        // (j runs two behind the first products)
-        for (int j = -2; ok && j < n; ++j) {
-            const int s = j & 1;
-            const uint32_t phase = uint32_t(j >> 1);
-            if (j >= 0) {
-                if constexpr (C::OUT_P) {
-                    ok = wait(p_ready(s), phase);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    if (leader) {
-                        second_product(j, C::X_BYTES, C::COL_S, C::COL_SUM);
-                        tc::mma_commit(p_taken(s));
-                    }
-                }
-                if constexpr (C::OUT_S) {
-                    ok = wait(ds_ready(s), phase);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    if (leader) {
-                        second_product(j, 0, C::COL_DP, C::COL_S_SUM);
-                        tc::mma_commit(ds_taken(s));
-                    }
-                }
-                if (leader) tc::mma_commit(empty(j % ST));
+            for (int kk = 0; kk < BX / 16; ++kk) {
+                const uint32_t a = slot + (kk < HALF / 16 ? kk * 8 : HALF + (kk - HALF / 16) * 8);
+                const uint64_t b = x + uint64_t(kk * 128);
+                if (leader) mma_f16_ts(sum, a, b, idesc_sum, add || kk > 0 ? 1u : 0u);
             }
-            if (j + 2 >= n) continue;
-            const int next = j + 2;
-            ok = wait(full(next % ST), uint32_t(next / ST));
-            // (a slot's S has been read once its dS is there)
-            if constexpr (C::OUT_P) ok = ok && (j < 0 || wait(p_taken(s), phase));
-            if (!ok) break;
-            tc::tc_fence_after();
-            if (leader) first_product(next, 0, 0, C::COL_S, s_full(s));
-            any = true;
-            if constexpr (C::DP) {
-                ok = j < 0 || wait(ds_taken(s), phase);
-                if (!ok) break;
-                tc::tc_fence_after();
-                if (leader) first_product(next, C::OFF_F2, C::X_BYTES, C::COL_DP, dp_full(s));
+        };
+        auto commit = [&](uint32_t bar) {
+            if (leader) tc::mma_commit(bar);
+        };
+        constexpr uint32_t XSTEP = C::X_BYTES >> 4;
+        auto make_s = [&](int j) {
+            const int s = j % C::R1;
+            if (!wait(x1_full(s), j / C::R1)) return false;
+            if (C::OUT_P ? j >= NS && !wait(p_taken(j % NS), j / NS - 1) : j > 0 && !wait(s_read, j - 1)) return false;
+            first_product(tmem + uint32_t(j % NS) * BX, f1, x1 + uint64_t(s) * XSTEP);
+            commit(s_full(j % NS));
+            if constexpr (!C::OUT_S) commit(x1_empty(s));
+            return true;
+        };
+        auto make_dp = [&](int j) {
+            const int s = j % C::R2;
+            if (!wait(x2_full(s), j / C::R2)) return false;
+            if (j >= ND && !wait(ds_taken(j % ND), j / ND - 1)) return false;
+            first_product(tmem + C::COL_DP + uint32_t(j % ND) * BX, f2, x2 + uint64_t(s) * XSTEP);
+            commit(dp_full(j % ND));
+            if constexpr (!C::OUT_P) commit(x2_empty(s));
+            return true;
+        };
+        auto sum_p = [&](int j) {
+            const int s = j % C::R2;
+            if (!wait(p_ready(j % NS), j / NS)) return false;
+            if (C::OUT_P && !C::OUT_S && !wait(x2_full(s), j / C::R2)) return false;     // (else dP has waited)
+            second_product(tmem + C::COL_SUM, tmem + uint32_t(j % NS) * BX, x2_mn + uint64_t(s) * XSTEP, j > 0);
+            commit(p_taken(j % NS));
+            commit(x2_empty(s));
+            return true;
+        };
+        auto sum_s = [&](int j) {
+            const int s = j % C::R1;
+            if (!wait(ds_ready(j % ND), j / ND)) return false;
+            second_product(tmem + C::COL_S_SUM, tmem + C::COL_DP + uint32_t(j % ND) * BX, x1_mn + uint64_t(s) * XSTEP, j > 0);
+            commit(ds_taken(j % ND));
+            commit(x1_empty(s));
+            return true;
+        };
+        const bool any = n > 0 && (ok = wait(f_full, 0));
+        if (any) {
+            ok = make_s(0);
+            if constexpr (C::OUT_S) ok = ok && make_dp(0);
+        }
+        for (int j = 0; ok && j < n; ++j) {
+            const bool more = j + 1 < n;
+            if constexpr (PASS == kKeys) {
+                ok = sum_p(j) && (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
+            } else if constexpr (PASS == kValuesOnly) {
+                ok = (!more || make_s(j + 1)) && sum_p(j);
+            } else {
+                ok = (!more || (make_s(j + 1) && make_dp(j + 1))) && sum_s(j);
             }
         }
         if (ok && n > 0) {
-            if (leader) tc::mma_commit(sums);
+            commit(sums);
             // the commits that nothing else waits for
-            for (int j = max(0, n - 2); ok && j < n; ++j) {
-                if constexpr (C::OUT_P) ok = wait(p_taken(j & 1), uint32_t(j >> 1));
-                if constexpr (C::OUT_S) ok = ok && wait(ds_taken(j & 1), uint32_t(j >> 1));
-            }
+            if constexpr (C::OUT_P)
+                for (int j = max(0, n - NS); ok && j < n; ++j) ok = wait(p_taken(j % NS), j / NS);
+            if constexpr (C::OUT_S)
+                for (int j = max(0, n - ND); ok && j < n; ++j) ok = wait(ds_taken(j % ND), j / ND);
         }
         if (!ok && any && leader) {
             // let the MMAs already issued finish before TMEM is freed
@@ -297,7 +335,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         const int wg = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + r;
         const uint32_t mine = tmem + (uint32_t((warp & 3) * 32) << 16);
-        const uint32_t s_col = mine + C::COL_S + uint32_t(wg) * 64, dp_col = mine + C::COL_DP + uint32_t(wg) * 64;
+        auto wait = [&](uint32_t bar, int phase) {
+            const bool is = __all_sync(0xffffffffu, tc::mbar_wait(bar, uint32_t(phase) & 1u, &s_abort, P.err, kErrOut));
+            tc::tc_fence_after();
+            return is;
+        };
         float row_lse = INFINITY, row_delta = 0.f;
         if constexpr (!C::BY_KEYS) {
             const long stat = (long(batch) * P.Hq + head) * P.Tpad + row;
@@ -305,29 +347,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             row_lse = row + shift == 0 ? INFINITY : __ldcg(P.lse2 + stat);
             row_delta = __ldcg(P.delta + stat);
         }
-        for (int j = wg; j < n; j += 2) {
-            const uint32_t phase = uint32_t(j >> 1) & 1u;
-            const int at = (first + (j0 + j) % per) * BX;
+        for (int j = 0; j < n; ++j) {
+            const int at = (first + (j0 + j) % per) * BX + wg * HALF;
+            const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * HALF, dp_col = mine + C::COL_DP + uint32_t(j % ND) * BX + wg * HALF;
             // columns that the row's key is seen from, or the row sees: from lo, to hi
-            int lo = 0, hi = BX, single = -1;
+            int lo = 0, hi = HALF, single = -1;
             bool masked;
             if constexpr (C::BY_KEYS) {
                 masked = shift + at < row0 + kRows - 1;
                 lo = row - shift - at;
                 single = -(shift + at);
             } else {
-                masked = at + BX > row0 + shift + 1;
+                masked = at + HALF > row0 + shift + 1;
                 hi = row + shift + 1 - at;
             }
-            const float* stat = reinterpret_cast<const float*>(smem + C::OFF_STAT + (j % ST) * C::STAT_BYTES);
-            if constexpr (C::BY_KEYS) ok = __all_sync(0xffffffffu, tc::mbar_wait(full(j % ST), uint32_t(j / ST) & 1u, &s_abort, P.err, kErrOut));
-            ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(s_full(wg), phase, &s_abort, P.err, kErrOut));
+            const int stat_j = j % C::RS;
+            const float* stat = reinterpret_cast<const float*>(smem + C::OFF_STAT + stat_j * C::STAT_BYTES) + wg * HALF;
+            if constexpr (C::BY_KEYS) {
+                ok = wait(C::OUT_S ? x1_full(stat_j) : x2_full(stat_j), j / C::RS);
+                if (!ok) break;
+            }
+            ok = wait(s_full(j % NS), j / NS);
             if (!ok) break;
-            tc::tc_fence_after();
-            float p[BX / 32][32];
+            float p[HALF / 32][32];
 #pragma unroll
-            for (int b = 0; b < BX / 32; ++b) {
-                tmem_ld32_done(s_col + b * 32, p[b]);
+            for (int b = 0; b < HALF / 32; ++b) tmem_ld32_done(s_col + b * 32, p[b]);
+            if constexpr (!C::OUT_P) {
+                tc::tc_fence_before();
+                tc::mbar_arrive(s_read);
+            }
+#pragma unroll
+            for (int b = 0; b < HALF / 32; ++b) {
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
                     float l[4] = {row_lse, row_lse, row_lse, row_lse};
@@ -344,21 +394,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                     uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[b][2 * i], p[b][2 * i + 1]);
-                    // (over S: columns 0-15 are read by now, as are 0-31 of the second half's 16-31)
                     tmem_st16(s_col + b * 16, w);
                 }
             }
             if constexpr (C::OUT_P) {
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
-                tc::mbar_arrive(p_ready(wg));
+                tc::mbar_arrive(p_ready(j % NS));
             }
             if constexpr (C::OUT_S) {
-                ok = __all_sync(0xffffffffu, tc::mbar_wait(dp_full(wg), phase, &s_abort, P.err, kErrOut));
+                ok = wait(dp_full(j % ND), j / ND);
                 if (!ok) break;
-                tc::tc_fence_after();
 #pragma unroll
-                for (int b = 0; b < BX / 32; ++b) {
+                for (int b = 0; b < HALF / 32; ++b) {
                     float d[32];
                     tmem_ld32_done(dp_col + b * 32, d);
 #pragma unroll
@@ -380,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
-                tc::mbar_arrive(ds_ready(wg));
+                tc::mbar_arrive(ds_ready(j % ND));
             }
         }
         if (ok && n > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(sums, 0, &s_abort, P.err, kErrOut));
@@ -514,11 +562,11 @@ __global__ void __launch_bounds__(256)
 
 // CTAs that share an item's blocks (host arithmetic only): the longest share
 // no longer than half as much again as an SM's part of all blocks, as long as
-// a share keeps 4.  (Rows whose blocks grow with the position: the last tile's
+// a share keeps 2.  (Rows whose blocks grow with the position: the last tile's
 // are the most, the average over the tiles half of it and more.)
 int shares_of(long longest, long total, int sms) {
     int s = 1;
-    while (s < kMaxShares && longest >= 8L * s && longest * 2 * sms > 3L * total * s) s *= 2;
+    while (s < kMaxShares && longest >= 4L * s && longest * 2 * sms > 3L * total * s) s *= 2;
     return s;
 }
 
@@ -647,17 +695,21 @@ extern "C" {
 // Bytes of scratch that decoder_attention_backward needs.
 long decoder_attention_scratch(long B, long Tq, int Hq) { return 8 * B * Hq * ((Tq + kRows - 1) / kRows * kRows); }
 
-// Gradients of decoder_attention: dout, q [B][Tq][Hq][d], k, v [B][Hkv][Tk][d]
-// and out [B][Tq][Hq][d] of any strides that are multiples of 8 elements (row,
-// head, batch of each in this order), lse as that gives it; dq [B][Tq][Hq][d],
-// dk, dv [B][Hkv][Tk][d] contiguous; all bf16 and 16-byte aligned.  Returns a
-// cudaError_t.
-int decoder_attention_backward(const void* dout, const void* q, const void* k, const void* v, const void* out, const void* lse,
+// Gradients of decoder_attention: dout, q, out [B][Tq][Hq][d] and k, v
+// [B][Hkv][Tk][d] of any strides that are multiples of 8 elements (row, head,
+// batch of each in this order; NULL: contiguous), lse as that gives it; dq
+// [B][Tq][Hq][d], dk, dv [B][Hkv][Tk][d] contiguous; all bf16 and 16-byte
+// aligned.  Returns a cudaError_t.
+int decoder_attention_backward(const void* dout, const void* q, const void* out, const void* k, const void* v, const void* lse,
                                const long* strides, void* scratch, void* dq, void* dk, void* dv, long B, long Tq, long Tk, int Hq,
                                int Hkv, int d, float scale, void* stream) {
     if (!decoder::attention_takes(B, Tq, Tk, Hq, Hkv)) return int(cudaErrorInvalidValue);
-    auto operand = [&](const void* p, int i) { return Operand{p, strides[3 * i], strides[3 * i + 1], strides[3 * i + 2]}; };
-    const Args a{operand(dout, 0), operand(q, 1), operand(k, 2), operand(v, 3), operand(out, 4), static_cast<const float*>(lse),
+    const long of_q[3] = {long(Hq) * d, d, Tq * Hq * d}, of_k[3] = {d, Tk * d, Tk * Hkv * d};
+    auto operand = [&](const void* p, int i) {
+        const long* s = strides ? strides + 3 * i : i < 3 ? of_q : of_k;
+        return Operand{p, s[0], s[1], s[2]};
+    };
+    const Args a{operand(dout, 0), operand(q, 1), operand(k, 3), operand(v, 4), operand(out, 2), static_cast<const float*>(lse),
                  static_cast<float*>(scratch), static_cast<__nv_bfloat16*>(dq), static_cast<__nv_bfloat16*>(dk),
                  static_cast<__nv_bfloat16*>(dv), int(B), int(Tq), int(Tk), Hq, Hkv, scale};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

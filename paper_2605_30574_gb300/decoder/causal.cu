@@ -375,13 +375,18 @@ int decoder_causal(const void* q, const void* k, const void* v, void* out, long 
 // The same for B sequences whose queries are the last Tq positions of the Tk
 // (Tq above Tk: the first rows see nothing), with the rows' log sums: q
 // [B][Tq][Hq][d], k, v [B][Hkv][Tk][d] of any strides that are multiples of 8
-// elements (q row, head, batch, k row, head, batch, v row, head, batch), out
+// elements (q row, head, batch, k row, head, batch, v row, head, batch; NULL:
+// contiguous), out
 // [B][Tq][Hq][d] contiguous, lse fp32 [B][Hq][Tq] (natural log of the sum of
 // e^(scale q . k), -inf for a row that sees nothing).
 int decoder_attention(const void* q, const void* k, const void* v, const long* strides, void* out, void* lse, long B, long Tq,
                       long Tk, int Hq, int Hkv, int d, float scale, void* stream) {
-    const decoder::Operand oq{q, strides[0], strides[1], strides[2]}, ok{k, strides[3], strides[4], strides[5]},
-        ov{v, strides[6], strides[7], strides[8]};
+    const long of_q[3] = {long(Hq) * d, d, Tq * Hq * d}, of_k[3] = {d, Tk * d, Tk * Hkv * d};
+    auto operand = [&](const void* p, int i) {
+        const long* s = strides ? strides + 3 * i : i == 0 ? of_q : of_k;
+        return decoder::Operand{p, s[0], s[1], s[2]};
+    };
+    const decoder::Operand oq = operand(q, 0), ok = operand(k, 1), ov = operand(v, 2);
     return launch<true>(oq, ok, ov, out, static_cast<float*>(lse), B, Tq, Tk, Hq, Hkv, d, scale, static_cast<cudaStream_t>(stream));
 }
 

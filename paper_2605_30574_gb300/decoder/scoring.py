@@ -39,7 +39,7 @@ def _rows_of(logits: torch.Tensor, what: str) -> torch.Tensor:
     """The logits as [rows][V], V contiguous, without a copy where they can be."""
     if not isinstance(logits, torch.Tensor) or logits.dtype not in _TYPES:
         raise TypeError(f"{what}: logits must be a tensor of fp32, bf16 or fp16")
-    if logits.device.type != "cuda":
+    if not logits.is_cuda:
         raise ValueError(f"{what}: logits must be on a CUDA device")
     if logits.dim() == 0 or logits.shape[-1] == 0:
         raise ValueError(f"{what}: logits must be [..., V] with V > 0")
