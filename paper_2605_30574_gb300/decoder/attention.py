@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import BF16, F32, _current_device, _launch, lib
+from . import BF16, F32, _current_device, _launch
 
 
 def _fits(q, k, v):
@@ -53,10 +53,6 @@ def _check(what, q, k, v):
     raise ValueError(f"{what}: the query heads must be a multiple of the kv heads")
 
 
-def _plain(t):
-    return t.is_contiguous() and not t.data_ptr() & 15 and not t.is_neg()
-
-
 def _operand(t, heads_first):
     """The tensor, or a copy that the kernels can read, and its (row, head,
     batch) strides."""
@@ -77,15 +73,14 @@ def _operand(t, heads_first):
 def _operands(rows_first, heads_first):
     """Both groups as the kernels can read them, and their strides as a C array
     (None: all contiguous)."""
-    if all(map(_plain, rows_first)) and all(map(_plain, heads_first)):
-        return rows_first, heads_first, None
-    got = [[_operand(t, first) for t in ts] for ts, first in ((rows_first, False), (heads_first, True))]
-    flat = [s for ts in got for _, st in ts for s in st]
-    return [t for t, _ in got[0]], [t for t, _ in got[1]], (ctypes.c_long * len(flat))(*flat)
-
-
-def _sizes(q, k):
-    return (q.shape[0] if q.dim() == 4 else 1, *q.shape[-3:], k.shape[-3], k.shape[-2])
+    ts, low = (*rows_first, *heads_first), 0
+    for t in ts:
+        low |= t.data_ptr() if t.is_contiguous() and not t.is_neg() else 1
+    if not low & 15:
+        return ts, None
+    got = [_operand(t, False) for t in rows_first] + [_operand(t, True) for t in heads_first]
+    flat = [s for _, st in got for s in st]
+    return [t for t, _ in got], (ctypes.c_long * len(flat))(*flat)
 
 
 def _scale(scale, d):
@@ -98,15 +93,18 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     e^(scale q . k), fp32 [Hq, Tq] ([B, Hq, Tq]); -inf for a row that sees no
     key.  ``scale`` is 1 / sqrt(d) by default."""
     _check("attention_forward", q, k, v)
-    if q.device.index != _current_device():
-        with torch.cuda.device(q.device):
+    device = q.device
+    if device.index != _current_device():
+        with torch.cuda.device(device):
             return attention_forward(q, k, v, scale)
-    B, Tq, Hq, d, Hkv, Tk = _sizes(q, k)
-    out = torch.empty(q.shape, dtype=BF16, device=q.device)
-    lse = torch.empty((*q.shape[:-3], Hq, Tq), dtype=F32, device=q.device)
+    *B, Tq, Hq, d = q.shape
+    Hkv, Tk, _ = k.shape[-3:]
+    out = torch.empty(q.shape, dtype=BF16, device=device)
+    lse = torch.empty((*B, Hq, Tq), dtype=F32, device=device)
+    B = B[0] if B else 1
     if B * Tq * Tk == 0:
         return out.zero_(), lse.fill_(-math.inf)
-    (q,), (k, v), strides = _operands((q,), (k, v))
+    (q, k, v), strides = _operands((q,), (k, v))
     _launch("decoder_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, out.data_ptr(), lse.data_ptr(), B, Tq, Tk, Hq,
             Hkv, d, _scale(scale, d))
     return out, lse
@@ -118,29 +116,31 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     output's, and output and log sums as ``attention_forward`` gave them."""
     what = "attention_backward"
     _check(what, q, k, v)
+    shape, device = q.shape, q.device
+    *B, Tq, Hq, d = shape
     for name, t in (("dout", dout), ("out", out)):
         if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
             raise TypeError(f"{what}: {name} must be a bf16 tensor")
-        if t.shape != q.shape or t.device != q.device:
+        if t.shape != shape or t.device != device:
             raise ValueError(f"{what}: {name} must be like q")
-    B, Tq, Hq, d, Hkv, Tk = _sizes(q, k)
     if not isinstance(lse, torch.Tensor) or lse.dtype is not F32:
         raise TypeError(f"{what}: lse must be an fp32 tensor")
-    if lse.shape != (*q.shape[:-3], Hq, Tq) or lse.device != q.device:
+    if lse.shape != (*B, Hq, Tq) or lse.device != device:
         raise ValueError(f"{what}: lse must be [Hq, Tq], or [B, Hq, Tq]")
-    if q.device.index != _current_device():
-        with torch.cuda.device(q.device):
+    if device.index != _current_device():
+        with torch.cuda.device(device):
             return attention_backward(dout, q, k, v, out, lse, scale)
+    B, (Hkv, Tk, _) = B[0] if B else 1, k.shape[-3:]
     if B * Tq * Tk == 0:
-        return torch.zeros_like(q, memory_format=torch.contiguous_format), \
-            torch.zeros_like(k, memory_format=torch.contiguous_format), \
-            torch.zeros_like(v, memory_format=torch.contiguous_format)
-    dq = torch.empty(q.shape, dtype=BF16, device=q.device)
-    dk = torch.empty(k.shape, dtype=BF16, device=q.device)
-    dv = torch.empty(k.shape, dtype=BF16, device=q.device)
-    scratch = torch.empty(lib().decoder_attention_scratch(B, Tq, Hq), dtype=torch.uint8, device=q.device)
-    (dout, q, out), (k, v), strides = _operands((dout, q, out), (k, v))
-    lse = lse.resolve_neg().contiguous()
+        return torch.zeros(shape, dtype=BF16, device=device), torch.zeros(k.shape, dtype=BF16, device=device), \
+            torch.zeros(k.shape, dtype=BF16, device=device)
+    (dout, q, out, k, v), strides = _operands((dout, q, out), (k, v))
+    if not lse.is_contiguous() or lse.is_neg():
+        lse = lse.resolve_neg().contiguous()
+    dq = torch.empty(shape, dtype=BF16, device=device)
+    dk = torch.empty(k.shape, dtype=BF16, device=device)
+    dv = torch.empty(k.shape, dtype=BF16, device=device)
+    scratch = torch.empty(8 * B * Hq * ((Tq + 127) // 128 * 128), dtype=torch.uint8, device=device)
     _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), out.data_ptr(), k.data_ptr(), v.data_ptr(),
             lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d,
             _scale(scale, d))

@@ -18,9 +18,10 @@
 //   kKeys    K   V    Q   dO    dV                  dK
 //   kQueries Q   dO   K   V     -                   dQ
 //
-// S = F1 X1^T and dP = F2 X2^T go to TMEM in fp32; two warpgroups, a thread per
-// row and each with half of a block's columns, make P and dS of them, rounded
-// to bf16 over their half as the A operands of the second products.  One warp
+// S = F1 X1^T and dP = F2 X2^T go to TMEM in fp32; four warpgroups, a thread per
+// row and each with 32 of a block's columns, make P and dS of them, rounded to
+// bf16 over their columns as the A operands of the second products (two with 64
+// columns each took 1.9 times as long).  One warp
 // issues all MMAs.  By keys, TMEM is full with one slot each for S and dP and the
 // two sums (128 dims), and the order is dV(j) S(j+1) dK(j) dP(j+1): P(j+1) is made
 // under dK(j) and dP(j+1), dS(j+1) under dV(j+1) and S(j+2).  By queries there are
@@ -55,19 +56,24 @@ using decoder::mma_f16_ts;
 using decoder::Operand;
 using decoder::pack_bf16;
 using decoder::tma_load_4d;
+using decoder::tmem_ld16_done;
 using decoder::tmem_ld32_done;
 using decoder::tmem_st16;
 
-constexpr int kRows = 128, kThreads = 320, kLoadWarp = 8, kMmaWarp = 9, kMaxStages = 3, kMaxShares = 8;
+constexpr int kRows = 128, kMaxStages = 3, kMaxShares = 8;
 constexpr unsigned kErrLoad = 512, kErrMma = 1024, kErrOut = 2048, kErrDrain = 4096;
 enum Pass { kKeys, kValuesOnly, kKeysOnly, kQueries };     // (both, dV, dK; dQ)
 
 template <int D, int PASS>
 struct Cfg {
     static constexpr bool BY_KEYS = PASS != kQueries, OUT_P = PASS == kKeys || PASS == kValuesOnly, OUT_S = PASS != kValuesOnly;
-    static constexpr int BX = D == 256 ? 64 : 128, PANELS = D / 64, HALF = BX / 2;     // (a warpgroup's columns)
-    // rings of X1 and X2; X2 is done with when dP is, unless P meets it again
-    static constexpr int R1 = D == 64 ? 3 : 2, R2 = D == 64 ? 3 : D == 256 && !OUT_P ? 1 : 2;
+    static constexpr int BX = D == 256 ? 64 : 128, PANELS = D / 64;
+    // warpgroups of the element operations, 32 columns of a block each; then the
+    // warps that load and that issue
+    static constexpr int WGS = BX / 32, LOAD_WARP = 4 * WGS, MMA_WARP = LOAD_WARP + 1, THREADS = 32 * (MMA_WARP + 1);
+    // rings of X1 and X2.  S(j + 1) is issued before dQ(j) where P meets nothing:
+    // three blocks of X1 are then in use or on their way.
+    static constexpr int R1 = D == 64 || (D == 128 && !OUT_P) ? 3 : 2, R2 = D == 64 ? 3 : D == 256 && !OUT_P ? 1 : 2;
     static constexpr uint32_t F_BYTES = kRows * D * 2, X_BYTES = BX * D * 2;
     // the rows' statistics come with the operand that is kept longer
     static constexpr uint32_t STAT_BYTES = BY_KEYS ? 2 * BX * 4 : 0;
@@ -75,13 +81,13 @@ struct Cfg {
     static constexpr uint32_t OFF_F2 = F_BYTES, OFF_X1 = OFF_F2 + (OUT_S ? F_BYTES : 0), OFF_X2 = OFF_X1 + R1 * X_BYTES;
     static constexpr uint32_t OFF_STAT = OFF_X2 + R2 * X_BYTES, BYTES = OFF_STAT + RS * STAT_BYTES;
     static constexpr int OUTS = (OUT_P ? 1 : 0) + (OUT_S ? 1 : 0);
-    static constexpr int COLS = OUTS * D / 2;              // a warpgroup's columns of the sums
+    static constexpr int COLS = OUTS * D / WGS;            // a warpgroup's columns of the sums
     static constexpr int UNITS = COLS / 16;
     // TMEM columns; slots of S and of dP
     static constexpr int NS = OUT_S ? 1 : 2, ND = !OUT_S ? 0 : OUT_P ? 1 : 2;
     static constexpr uint32_t COL_DP = NS * BX, COL_SUM = COL_DP + ND * BX, COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
     static_assert(COL_S_SUM + (OUT_S ? D : 0) <= 512);
-    static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * 2 * ((UNITS + shares - 1) / shares) * 16 * kRows * 4; }
+    static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * ((WGS * UNITS + shares - 1) / shares) * 16 * kRows * 4; }
     // (more than half of an SM's, so that no two CTAs of these kernels share one:
     // each takes all of TMEM, and CTAs of two clusters that wait for one
     // another's would wait for ever)
@@ -104,11 +110,11 @@ struct GradParams {
 };
 
 template <int D, int PASS>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     grad_kernel(const __grid_constant__ CUtensorMap tm_f1, const __grid_constant__ CUtensorMap tm_f2,
                 const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const GradParams P) {
     using C = Cfg<D, PASS>;
-    constexpr int BX = C::BX, HALF = C::HALF, NS = C::NS, ND = C::ND > 0 ? C::ND : 1;
+    constexpr int BX = C::BX, NS = C::NS, ND = C::ND > 0 ? C::ND : 1;
     extern __shared__ uint8_t smem_raw[];
     constexpr int kBars = 4 * kMaxStages + 16;
     __shared__ __align__(8) uint64_t bars[kBars];
@@ -154,10 +160,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < kBars; ++i) tc::mbar_init(bar0 + 8u * i, 1);
         for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(p_ready(i), 2 * kRows);
-            tc::mbar_init(ds_ready(i), 2 * kRows);
+            tc::mbar_init(p_ready(i), C::WGS * kRows);
+            tc::mbar_init(ds_ready(i), C::WGS * kRows);
         }
-        tc::mbar_init(s_read, 2 * kRows);
+        tc::mbar_init(s_read, C::WGS * kRows);
         s_abort = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tm_f1);
@@ -165,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::prefetch_tmap(&tm_x1);
         tc::prefetch_tmap(&tm_x2);
     }
-    if (warp == kMmaWarp) {
+    if (warp == C::MMA_WARP) {
         tc::tmem_alloc(tc::smem_u32(&s_tmem), 512);
         tc::tmem_relinquish();
     }
@@ -182,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = s_tmem;
     bool ok = true;
 
-    if (warp == kLoadWarp) {
+    if (warp == C::LOAD_WARP) {
         const bool leader = tc::elect_one();
         if (n > 0 && leader) {
             tc::mbar_arrive_expect_tx(f_full, C::OUT_S ? 2 * C::F_BYTES : C::F_BYTES);
@@ -234,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = tc::mbar_wait(x1_empty(i % C::R1), uint32_t(i / C::R1) & 1u, &s_abort, P.err, kErrDrain);
         for (int i = max(0, j2 - C::R2); ok && i < j2; ++i)
             ok = tc::mbar_wait(x2_empty(i % C::R2), uint32_t(i / C::R2) & 1u, &s_abort, P.err, kErrDrain);
-    } else if (warp == kMmaWarp) {
+    } else if (warp == C::MMA_WARP) {
         // Descriptors are made by the whole warp (see gemm.cu): issued from
         // values of one lane, an MMA took 72 clocks.
         const bool leader = tc::elect_one();
@@ -255,11 +261,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (leader) tc::mma_f16_ss(to, a, b, idesc_s, kk > 0 ? 1u : 0u);
             }
         };
-        // a slot's bf16, in two halves, times X, added up
+        // a slot's bf16, 16 columns at the start of each 32, times X, added up
         auto second_product = [&](uint32_t sum, uint32_t slot, uint64_t x, bool add) {
 #pragma unroll
             for (int kk = 0; kk < BX / 16; ++kk) {
-                const uint32_t a = slot + (kk < HALF / 16 ? kk * 8 : HALF + (kk - HALF / 16) * 8);
+                const uint32_t a = slot + (kk / 2) * 32 + (kk % 2) * 8;
                 const uint64_t b = x + uint64_t(kk * 128);
                 if (leader) mma_f16_ts(sum, a, b, idesc_sum, add || kk > 0 ? 1u : 0u);
             }
@@ -348,56 +354,50 @@ __global__ void __launch_bounds__(kThreads, 1)
             row_delta = __ldcg(P.delta + stat);
         }
         for (int j = 0; j < n; ++j) {
-            const int at = (first + (j0 + j) % per) * BX + wg * HALF;
-            const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * HALF, dp_col = mine + C::COL_DP + uint32_t(j % ND) * BX + wg * HALF;
+            const int at = (first + (j0 + j) % per) * BX + wg * 32;
+            const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * 32, dp_col = mine + C::COL_DP + uint32_t(j % ND) * BX + wg * 32;
             // columns that the row's key is seen from, or the row sees: from lo, to hi
-            int lo = 0, hi = HALF, single = -1;
+            int lo = 0, hi = 32, single = -1;
             bool masked;
             if constexpr (C::BY_KEYS) {
                 masked = shift + at < row0 + kRows - 1;
                 lo = row - shift - at;
                 single = -(shift + at);
             } else {
-                masked = at + HALF > row0 + shift + 1;
+                masked = at + 32 > row0 + shift + 1;
                 hi = row + shift + 1 - at;
             }
             const int stat_j = j % C::RS;
-            const float* stat = reinterpret_cast<const float*>(smem + C::OFF_STAT + stat_j * C::STAT_BYTES) + wg * HALF;
+            const float* stat = reinterpret_cast<const float*>(smem + C::OFF_STAT + stat_j * C::STAT_BYTES) + wg * 32;
             if constexpr (C::BY_KEYS) {
                 ok = wait(C::OUT_S ? x1_full(stat_j) : x2_full(stat_j), j / C::RS);
                 if (!ok) break;
             }
             ok = wait(s_full(j % NS), j / NS);
             if (!ok) break;
-            float p[HALF / 32][32];
-#pragma unroll
-            for (int b = 0; b < HALF / 32; ++b) tmem_ld32_done(s_col + b * 32, p[b]);
+            float p[32];
+            uint32_t w[16];
+            tmem_ld32_done(s_col, p);
             if constexpr (!C::OUT_P) {
                 tc::tc_fence_before();
                 tc::mbar_arrive(s_read);
             }
 #pragma unroll
-            for (int b = 0; b < HALF / 32; ++b) {
+            for (int i = 0; i < 32; i += 4) {
+                float l[4] = {row_lse, row_lse, row_lse, row_lse};
+                if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + i);
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float l[4] = {row_lse, row_lse, row_lse, row_lse};
-                    if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + b * 32 + i);
+                for (int e = 0; e < 4; ++e) p[i + e] = ex2(fmaf(p[i + e], P.scale_log2, -l[e]));
+            }
+            if (masked) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[b][i + e] = ex2(fmaf(p[b][i + e], P.scale_log2, -l[e]));
-                }
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (b * 32 + i < lo || b * 32 + i >= hi) p[b][i] = 0.f;
-                }
-                if constexpr (C::OUT_P) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[b][2 * i], p[b][2 * i + 1]);
-                    tmem_st16(s_col + b * 16, w);
-                }
+                for (int i = 0; i < 32; ++i)
+                    if (i < lo || i >= hi) p[i] = 0.f;
             }
             if constexpr (C::OUT_P) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+                tmem_st16(s_col, w);
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
                 tc::mbar_arrive(p_ready(j % NS));
@@ -405,27 +405,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (C::OUT_S) {
                 ok = wait(dp_full(j % ND), j / ND);
                 if (!ok) break;
+                float d[32];
+                tmem_ld32_done(dp_col, d);
 #pragma unroll
-                for (int b = 0; b < HALF / 32; ++b) {
-                    float d[32];
-                    tmem_ld32_done(dp_col + b * 32, d);
+                for (int i = 0; i < 32; i += 4) {
+                    float l[4] = {row_delta, row_delta, row_delta, row_delta};
+                    if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + BX + i);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        float l[4] = {row_delta, row_delta, row_delta, row_delta};
-                        if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + BX + b * 32 + i);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) d[i + e] = p[b][i + e] * (d[i + e] - l[e]);
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (p[b][i] == 0.f || b * 32 + i == single) d[i] = 0.f;
-                    }
-                    uint32_t w[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(d[2 * i], d[2 * i + 1]);
-                    tmem_st16(dp_col + b * 16, w);
+                    for (int e = 0; e < 4; ++e) d[i + e] = p[i + e] * (d[i + e] - l[e]);
                 }
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (p[i] == 0.f || i == single) d[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack_bf16(d[2 * i], d[2 * i + 1]);
+                tmem_st16(dp_col, w);
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
                 tc::mbar_arrive(ds_ready(j % ND));
@@ -433,85 +429,63 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok && n > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(sums, 0, &s_abort, P.err, kErrOut));
         tc::tc_fence_after();
-        // Sums out: a warpgroup's columns are one of two sums, or half of the one.
-        // All lanes of a warp take part in the TMEM loads.
-        if (P.shares == 1 && ok) {
-            const bool of_p = C::OUT_P && (wg == 0 || !C::OUT_S), in = row < (C::BY_KEYS ? P.Tk : P.Tq);
-            const int c0 = C::OUTS == 2 ? 0 : wg * C::COLS;
-            __nv_bfloat16* out = of_p ? P.p_sum + batch * P.p_batch + head * P.p_head + row * P.p_row
-                                      : P.s_sum + batch * P.s_batch + head * P.s_head + row * P.s_row;
-            const float by = of_p ? 1.f : P.scale;
-            uint4* dst = reinterpret_cast<uint4*>(out + c0);
-#pragma unroll
-            for (int c = 0; c < C::COLS; c += 32) {
-                float o[32];
-                if (n > 0) {
-                    tmem_ld32_done(mine + C::COL_SUM + wg * C::COLS + c, o);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0.f;
-                }
-                if (in) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        dst[c / 8 + i] = make_uint4(pack_bf16(o[8 * i] * by, o[8 * i + 1] * by), pack_bf16(o[8 * i + 2] * by, o[8 * i + 3] * by),
-                                                    pack_bf16(o[8 * i + 4] * by, o[8 * i + 5] * by), pack_bf16(o[8 * i + 6] * by, o[8 * i + 7] * by));
-                }
-            }
-        }
     }
     __syncwarp();
+    // Sums out, 16 columns at a time.  With shares, the columns go round them:
+    // each adds up its part of everyone's in share order.  No CTA of the
+    // cluster has a copy or an MMA in flight any more then, so the operands'
+    // room is their inbox: [from share][part][16][128] fp32.
+    const int wg = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + r;
+    const uint32_t mine = tmem + (uint32_t((warp & 3) * 32) << 16) + C::COL_SUM + wg * C::COLS;
+    const int parts = (C::WGS * C::UNITS + P.shares - 1) / P.shares, u0 = wg * C::UNITS;
+    constexpr int UNIT = 16 * kRows;
+    float* inbox = reinterpret_cast<float*>(smem);
+    const bool takes = warp < C::LOAD_WARP && ok;
     if (P.shares > 1) {
-        // The sums, 16 columns at a time, go round the shares: each adds up its
-        // part of everyone's in share order.  No CTA of the cluster has a copy
-        // or an MMA in flight any more, so the operands' room is their inbox:
-        // [from share][warpgroup][part][16][128] fp32.
-        float* inbox = reinterpret_cast<float*>(smem);
-        const int parts = (C::UNITS + P.shares - 1) / P.shares;
-        constexpr int UNIT = 16 * kRows;
-        const int wg = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + r;
-        const uint32_t mine = tmem + (uint32_t((warp & 3) * 32) << 16) + C::COL_SUM + wg * C::COLS;
         cluster.sync();
-        if (warp < 8 && ok) {
+        if (takes) {
 #pragma unroll
-            for (int c = 0; c < C::COLS; c += 32) {
-                float o[32];
-                if (n > 0) {
-                    tmem_ld32_done(mine + c, o);
-                } else {
+            for (int u = 0; u < C::UNITS; ++u) {
+                float o[16];
+                tmem_ld16_done(mine + u * 16, o);
+                float* box = cluster.map_shared_rank(inbox, (u0 + u) % P.shares) + size_t(share * parts + (u0 + u) / P.shares) * UNIT + r;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0.f;
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int u = c / 16 + h;
-                    float* box = cluster.map_shared_rank(inbox, u % P.shares) + size_t((share * 2 + wg) * parts + u / P.shares) * UNIT + r;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) box[e * kRows] = o[h * 16 + e];
-                }
+                for (int e = 0; e < 16; ++e) box[e * kRows] = n > 0 ? o[e] : 0.f;
             }
         }
         cluster.sync();
-        if (warp < 8 && ok && row < (C::BY_KEYS ? P.Tk : P.Tq)) {
-            const bool of_p = C::OUT_P && (wg == 0 || !C::OUT_S);
-            const int c0 = C::OUTS == 2 ? 0 : wg * C::COLS;
-            __nv_bfloat16* out = of_p ? P.p_sum + batch * P.p_batch + head * P.p_head + row * P.p_row
-                                      : P.s_sum + batch * P.s_batch + head * P.s_head + row * P.s_row;
-            const float by = of_p ? 1.f : P.scale;
-            for (int u = share, part = 0; u < C::UNITS; u += P.shares, ++part) {
-                float sum[16];
+    }
+    if (takes) {
+        // (a warpgroup's columns are of one sum)
+        const int c0 = wg * C::COLS;
+        const bool of_p = C::OUT_P && c0 < D;
+        __nv_bfloat16* out = of_p ? P.p_sum + batch * P.p_batch + head * P.p_head + row * P.p_row + c0
+                                  : P.s_sum + batch * P.s_batch + head * P.s_head + row * P.s_row + (C::OUT_P ? c0 - D : c0);
+        const float by = of_p ? 1.f : P.scale;
+        const bool in = row < (C::BY_KEYS ? P.Tk : P.Tq);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+        for (int u = 0; u < C::UNITS; ++u) {
+            if ((u0 + u) % P.shares != share) continue;
+            float o[16];
+            if (P.shares > 1) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0.f;
                 for (int from = 0; from < P.shares; ++from) {
-                    const float* box = inbox + size_t((from * 2 + wg) * parts + part) * UNIT + r;
+                    const float* box = inbox + size_t(from * parts + (u0 + u) / P.shares) * UNIT + r;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[e] += box[e * kRows];
+                    for (int e = 0; e < 16; ++e) o[e] += box[e * kRows];
                 }
-                uint4* dst = reinterpret_cast<uint4*>(out + c0 + u * 16);
+            } else {
+                tmem_ld16_done(mine + u * 16, o);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = n > 0 || P.shares > 1 ? o[e] * by : 0.f;
+            if (in) {
+                uint4* dst = reinterpret_cast<uint4*>(out + u * 16);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    dst[i] = make_uint4(pack_bf16(sum[8 * i] * by, sum[8 * i + 1] * by), pack_bf16(sum[8 * i + 2] * by, sum[8 * i + 3] * by),
-                                        pack_bf16(sum[8 * i + 4] * by, sum[8 * i + 5] * by), pack_bf16(sum[8 * i + 6] * by, sum[8 * i + 7] * by));
+                    dst[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]),
+                                        pack_bf16(o[8 * i + 4], o[8 * i + 5]), pack_bf16(o[8 * i + 6], o[8 * i + 7]));
             }
         }
     }
@@ -519,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    if (warp == kMmaWarp) tc::tmem_dealloc(tmem, 512);
+    if (warp == C::MMA_WARP) tc::tmem_dealloc(tmem, 512);
     // (what follows on the stream waits for this grid alone)
     if constexpr (!C::BY_KEYS) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
@@ -584,7 +558,7 @@ int launch(const CUtensorMap (&maps)[4], GradParams p, long longest, long total,
     p.shares = shares_of(longest, total, sms);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(p.tiles) * unsigned(C::BY_KEYS ? p.Hkv : p.Hq) * unsigned(p.B) * unsigned(p.shares));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::smem(p.shares);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
