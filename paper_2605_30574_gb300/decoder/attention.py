@@ -140,7 +140,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     dq = torch.empty(shape, dtype=BF16, device=device)
     dk = torch.empty(k.shape, dtype=BF16, device=device)
     dv = torch.empty(k.shape, dtype=BF16, device=device)
-    scratch = torch.empty(8 * B * Hq * ((Tq + 127) // 128 * 128), dtype=torch.uint8, device=device)
+    scratch = torch.empty(40 * B * Hq * ((Tq + 127) // 128 * 128), dtype=torch.uint8, device=device)
     _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), out.data_ptr(), k.data_ptr(), v.data_ptr(),
             lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d,
             _scale(scale, d))

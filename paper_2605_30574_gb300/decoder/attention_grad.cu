@@ -21,13 +21,23 @@
 // S = F1 X1^T and dP = F2 X2^T go to TMEM in fp32; four warpgroups, a thread per
 // row and each with 32 of a block's columns, make P and dS of them, rounded to
 // bf16 over their columns as the A operands of the second products (two with 64
-// columns each took 1.9 times as long).  One warp
-// issues all MMAs.  By keys, TMEM is full with one slot each for S and dP and the
-// two sums (128 dims), and the order is dV(j) S(j+1) dK(j) dP(j+1): P(j+1) is made
-// under dK(j) and dP(j+1), dS(j+1) under dV(j+1) and S(j+2).  By queries there are
-// two slots for dP, and the order S(j+1) dP(j+1) dQ(j) leaves no gap.  Blocks are
-// of 128: an MMA of 64 columns reads its A operand twice as often, and takes 48
-// clocks in place of 32.
+// columns each took 1.9 times as long).  One warp issues all MMAs, blocks are of
+// 128 (an MMA of 64 columns reads its A operand twice as often, and takes 48
+// clocks in place of 32).
+//
+// What bounds the loop is shared memory, 128 bytes a clock: an SS MMA of 128 x
+// 128 x 16 reads 8 KB in its 64 clocks, and a block's arrival writes 64 KB.  So
+//
+// * by queries, Q and dO stay in TMEM, as A operands (256 dims: Q only);
+// * by keys, where a row of S is a key and lse and delta go by column, they are
+//   not read from shared memory (a broadcast of 16 bytes takes as long as 512
+//   different ones: 1024 clocks a block) but come with the products: S - lse /
+//   scale is one more MMA, of ones with the three bf16 terms of the number.
+//
+// By keys, TMEM is full with a slot each for S and dP and the two sums (128
+// dims); the order is dV(j) S(j+1) dK(j) dP(j+1), so that P(j+1) is made under
+// dK(j) and dP(j+1), dS(j+1) under dV(j+1) and S(j+2).  By queries it is S(j+1)
+// dQ(j) dP(j+1), or S(j+1) dP(j+1) dQ(j) where TMEM has a second slot for dP.
 //
 // 256 dims: blocks of 64, and dK and dV, which do not fit in TMEM together, in
 // a launch each.
@@ -40,6 +50,8 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "../csrc/per_device.h"
 #include "../csrc/tc_ptx.cuh"
@@ -59,9 +71,13 @@ using decoder::tma_load_4d;
 using decoder::tmem_ld16_done;
 using decoder::tmem_ld32_done;
 using decoder::tmem_st16;
+using decoder::tmem_st8;
 
 constexpr int kRows = 128, kMaxStages = 3, kMaxShares = 8;
 constexpr unsigned kErrLoad = 512, kErrMma = 1024, kErrOut = 2048, kErrDrain = 4096;
+// S - lse / scale, times the scale, has to be finite, and lse for a scale of 0:
+// below this the scores make no difference.
+constexpr float kLeastScale = 9.094947e-13f;               // 2^-40
 enum Pass { kKeys, kValuesOnly, kKeysOnly, kQueries };     // (both, dV, dK; dQ)
 
 template <int D, int PASS>
@@ -71,21 +87,24 @@ struct Cfg {
     // warpgroups of the element operations, 32 columns of a block each; then the
     // warps that load and that issue
     static constexpr int WGS = BX / 32, LOAD_WARP = 4 * WGS, MMA_WARP = LOAD_WARP + 1, THREADS = 32 * (MMA_WARP + 1);
+    // which of the fixed operands are in TMEM; slots of S and of dP there
+    static constexpr bool T1 = PASS == kQueries || D == 256, T2 = PASS == kQueries && D < 256;
+    static constexpr int NS = OUT_S ? 1 : 2, ND = !OUT_S ? 0 : PASS == kQueries && D == 64 ? 2 : 1;
     // rings of X1 and X2.  S(j + 1) is issued before dQ(j) where P meets nothing:
     // three blocks of X1 are then in use or on their way.
-    static constexpr int R1 = D == 64 || (D == 128 && !OUT_P) ? 3 : 2, R2 = D == 64 ? 3 : D == 256 && !OUT_P ? 1 : 2;
+    static constexpr int R1 = D == 64 || PASS == kQueries ? 3 : 2, R2 = D == 64 ? 3 : 2;
     static constexpr uint32_t F_BYTES = kRows * D * 2, X_BYTES = BX * D * 2;
-    // the rows' statistics come with the operand that is kept longer
-    static constexpr uint32_t STAT_BYTES = BY_KEYS ? 2 * BX * 4 : 0;
-    static constexpr int RS = OUT_S ? R1 : R2;
-    static constexpr uint32_t OFF_F2 = F_BYTES, OFF_X1 = OFF_F2 + (OUT_S ? F_BYTES : 0), OFF_X2 = OFF_X1 + R1 * X_BYTES;
-    static constexpr uint32_t OFF_STAT = OFF_X2 + R2 * X_BYTES, BYTES = OFF_STAT + RS * STAT_BYTES;
+    // the rows' numbers come with X1: see stats_kernel; ONES meets them
+    static constexpr uint32_t AUG_BYTES = BY_KEYS ? BX * 32 : 0, ONES_BYTES = BY_KEYS ? kRows * 32 + 128 : 0;
+    static constexpr int F_LOADS = (T1 ? 0 : 1) + (OUT_S && !T2 ? 1 : 0);
+    static constexpr uint32_t OFF_F2 = T1 ? 0 : F_BYTES, OFF_X1 = OFF_F2 + (OUT_S && !T2 ? F_BYTES : 0), OFF_X2 = OFF_X1 + R1 * X_BYTES;
+    static constexpr uint32_t OFF_AUG = OFF_X2 + R2 * X_BYTES, OFF_ONES = OFF_AUG + R1 * AUG_BYTES, BYTES = OFF_ONES + ONES_BYTES;
     static constexpr int OUTS = (OUT_P ? 1 : 0) + (OUT_S ? 1 : 0);
     static constexpr int COLS = OUTS * D / WGS;            // a warpgroup's columns of the sums
     static constexpr int UNITS = COLS / 16;
-    // TMEM columns; slots of S and of dP
-    static constexpr int NS = OUT_S ? 1 : 2, ND = !OUT_S ? 0 : OUT_P ? 1 : 2;
-    static constexpr uint32_t COL_DP = NS * BX, COL_SUM = COL_DP + ND * BX, COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
+    // TMEM columns
+    static constexpr uint32_t COL_DP = NS * BX, COL_F1 = COL_DP + ND * BX, COL_F2 = COL_F1 + (T1 ? D / 2 : 0);
+    static constexpr uint32_t COL_SUM = COL_F2 + (T2 ? D / 2 : 0), COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
     static_assert(COL_S_SUM + (OUT_S ? D : 0) <= 512);
     static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * ((WGS * UNITS + shares - 1) / shares) * 16 * kRows * 4; }
     // (more than half of an SM's, so that no two CTAs of these kernels share one:
@@ -98,14 +117,24 @@ struct Cfg {
     static_assert(smem(kMaxShares) <= 227 * 1024 - 512);
 };
 
+// An operand without swizzle: 8 rows of 16 bytes of K at a time, `k_bytes` to
+// the next 16 bytes of K, `rows_bytes` to the next 8 rows.
+__device__ __forceinline__ uint64_t plain_desc(uint32_t saddr, uint32_t k_bytes, uint32_t rows_bytes) {
+    return uint64_t((saddr >> 4) & 0x3FFFu) | uint64_t(k_bytes >> 4) << 16 | uint64_t(rows_bytes >> 4) << 32 | uint64_t(1) << 46;
+}
+
 struct GradParams {
-    const float *lse2, *delta;      // [B Hq][Tpad]: log2 of the row's sum (+inf where it has no weights), delta
+    // [B Hq][Tpad]: log2 of the row's sum (+inf where it has no weights), delta;
+    // the same for an MMA
+    const float *lse2, *delta;
+    const uint8_t* aug;
+    Operand f1, f2;                 // the fixed operands that go to TMEM
     __nv_bfloat16 *p_sum, *s_sum;   // outputs
     long p_row, p_head, p_batch, s_row, s_head, s_batch;
     int Tq, Tk, Tpad, Hq, Hkv, B;
     int tiles;                      // of 128 fixed rows
     int shares;
-    float scale, scale_log2;
+    float scale, scale_log2;        // scale_log2 by keys: not below kLeastScale
     unsigned* err;
 };
 
@@ -158,18 +187,26 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     const int j0 = int(all * share / P.shares), n = int(all * (share + 1) / P.shares) - j0;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kBars; ++i) tc::mbar_init(bar0 + 8u * i, 1);
-        for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(p_ready(i), C::WGS * kRows);
-            tc::mbar_init(ds_ready(i), C::WGS * kRows);
+        // (how many arrive: an issue or a commit, or all threads of the warpgroups)
+        constexpr int kAll = C::WGS * kRows;
+        for (int i = 0; i < kBars; ++i) {
+            const uint32_t bar = bar0 + 8u * i;
+            const bool threads = (bar >= p_ready(0) && bar <= ds_ready(1)) || bar == s_read;
+            tc::mbar_init(bar, threads ? kAll : bar == f_full ? (C::T1 ? kAll : 0) + (C::F_LOADS > 0 ? 1 : 0) : 1);
         }
-        tc::mbar_init(s_read, C::WGS * kRows);
         s_abort = 0;
         tc::fence_mbar_init();
         tc::prefetch_tmap(&tm_f1);
         tc::prefetch_tmap(&tm_f2);
         tc::prefetch_tmap(&tm_x1);
         tc::prefetch_tmap(&tm_x2);
+    }
+    if constexpr (C::BY_KEYS) {
+        // [8 rows][8 of K], ones in the first three of K, and as many zeros, in turn
+        uint4* ones = reinterpret_cast<uint4*>(smem + C::OFF_ONES);
+        for (int i = threadIdx.x; i < int(C::ONES_BYTES / 16); i += C::THREADS)
+            ones[i] = i & 8 ? make_uint4(0, 0, 0, 0) : make_uint4(0x3f803f80u, 0x3f80u, 0, 0);
+        tc::fence_proxy_async_smem();
     }
     if (warp == C::MMA_WARP) {
         tc::tmem_alloc(tc::smem_u32(&s_tmem), 512);
@@ -190,43 +227,38 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
 
     if (warp == C::LOAD_WARP) {
         const bool leader = tc::elect_one();
-        if (n > 0 && leader) {
-            tc::mbar_arrive_expect_tx(f_full, C::OUT_S ? 2 * C::F_BYTES : C::F_BYTES);
+        if (C::F_LOADS > 0 && n > 0 && leader) {
+            tc::mbar_arrive_expect_tx(f_full, C::F_LOADS * C::F_BYTES);
 #pragma unroll
             for (int p = 0; p < C::PANELS; ++p) {
-                tma_load_4d(sbase + p * (kRows * 128), &tm_f1, p * 64, row0, head, batch, f_full);
-                if (C::OUT_S) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
+                if (!C::T1) tma_load_4d(sbase + p * (kRows * 128), &tm_f1, p * 64, row0, head, batch, f_full);
+                if (C::OUT_S && !C::T2) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
             }
         }
         int j1 = 0, j2 = 0;      // blocks asked for
         for (int j = 0; j < n; ++j) {
             const int at = (first + (j0 + j) % per) * BX;
             const int x_head = C::BY_KEYS ? head * G + (j0 + j) / per : head / G;
-            auto statistics = [&](int s, uint32_t bar) {
-                const long stat = (long(batch) * P.Hq + x_head) * P.Tpad + at;
-                const uint32_t to = sbase + C::OFF_STAT + uint32_t(s) * C::STAT_BYTES;
-                decoder::bulk_load(to, P.lse2 + stat, BX * 4, bar);
-                decoder::bulk_load(to + BX * 4, P.delta + stat, BX * 4, bar);
-            };
             const int s1 = j % C::R1, s2 = j % C::R2;
             ok = __all_sync(0xffffffffu, tc::mbar_wait(x1_empty(s1), (uint32_t(j / C::R1) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
             if (!ok) break;
             if (leader) {
-                tc::mbar_arrive_expect_tx(x1_full(s1), C::X_BYTES + (C::OUT_S ? C::STAT_BYTES : 0));
+                tc::mbar_arrive_expect_tx(x1_full(s1), C::X_BYTES + C::AUG_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
                     tma_load_4d(sbase + C::OFF_X1 + uint32_t(s1) * C::X_BYTES + p * (BX * 128), &tm_x1, p * 64, at, x_head, batch, x1_full(s1));
-                if constexpr (C::BY_KEYS && C::OUT_S) statistics(s1, x1_full(s1));
+                if constexpr (C::BY_KEYS)
+                    decoder::bulk_load(sbase + C::OFF_AUG + uint32_t(s1) * C::AUG_BYTES, P.aug + ((long(batch) * P.Hq + x_head) * P.Tpad + at) * 32,
+                                       C::AUG_BYTES, x1_full(s1));
             }
             ++j1;
             ok = __all_sync(0xffffffffu, tc::mbar_wait(x2_empty(s2), (uint32_t(j / C::R2) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
             if (!ok) break;
             if (leader) {
-                tc::mbar_arrive_expect_tx(x2_full(s2), C::X_BYTES + (C::OUT_S ? 0 : C::STAT_BYTES));
+                tc::mbar_arrive_expect_tx(x2_full(s2), C::X_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
                     tma_load_4d(sbase + C::OFF_X2 + uint32_t(s2) * C::X_BYTES + p * (BX * 128), &tm_x2, p * 64, at, x_head, batch, x2_full(s2));
-                if constexpr (C::BY_KEYS && !C::OUT_S) statistics(s2, x2_full(s2));
             }
             ++j2;
         }
@@ -248,17 +280,27 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
         const uint64_t f1 = tc::sw128_desc(sbase, 16, 1024), f2 = tc::sw128_desc(sbase + C::OFF_F2, 16, 1024);
         const uint64_t x1 = tc::sw128_desc(sbase + C::OFF_X1, 16, 1024), x2 = tc::sw128_desc(sbase + C::OFF_X2, 16, 1024);
         const uint64_t x1_mn = tc::sw128_desc(sbase + C::OFF_X1, BX * 128, 1024), x2_mn = tc::sw128_desc(sbase + C::OFF_X2, BX * 128, 1024);
+        const uint64_t ones = plain_desc(sbase + C::OFF_ONES, 128, 256), augs = plain_desc(sbase + C::OFF_AUG, 128, 256);
         auto wait = [&](uint32_t bar, int phase) {
             const bool is = __all_sync(0xffffffffu, tc::mbar_wait(bar, uint32_t(phase) & 1u, &s_abort, P.err, kErrMma));
             tc::tc_fence_after();
             return is;
         };
-        // F X^T into a slot (descriptor units of 16 bytes)
-        auto first_product = [&](uint32_t to, uint64_t f, uint64_t x) {
+        // F X^T into a slot (descriptor units of 16 bytes), F by descriptor or in
+        // TMEM; by keys with the rows' numbers, from the half `core` of them
+        auto first_product = [&](auto in_tmem, uint32_t to, uint64_t f, uint32_t f_tmem, uint64_t x, int aug, int core) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t a = f + uint64_t((kk / 4) * (kRows * 8) + (kk % 4) * 2), b = x + uint64_t((kk / 4) * (BX * 8) + (kk % 4) * 2);
-                if (leader) tc::mma_f16_ss(to, a, b, idesc_s, kk > 0 ? 1u : 0u);
+                const uint64_t b = x + uint64_t((kk / 4) * (BX * 8) + (kk % 4) * 2);
+                if constexpr (decltype(in_tmem)::value) {
+                    if (leader) mma_f16_ts(to, f_tmem + kk * 8, b, idesc_s, kk > 0 ? 1u : 0u);
+                } else {
+                    const uint64_t a = f + uint64_t((kk / 4) * (kRows * 8) + (kk % 4) * 2);
+                    if (leader) tc::mma_f16_ss(to, a, b, idesc_s, kk > 0 ? 1u : 0u);
+                }
+            }
+            if constexpr (C::BY_KEYS) {
+                if (leader) tc::mma_f16_ss(to, ones + uint64_t(core * 8), augs + uint64_t(aug * (C::AUG_BYTES >> 4)), idesc_s, 1u);
             }
         };
         // a slot's bf16, 16 columns at the start of each 32, times X, added up
@@ -278,7 +320,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             const int s = j % C::R1;
             if (!wait(x1_full(s), j / C::R1)) return false;
             if (C::OUT_P ? j >= NS && !wait(p_taken(j % NS), j / NS - 1) : j > 0 && !wait(s_read, j - 1)) return false;
-            first_product(tmem + uint32_t(j % NS) * BX, f1, x1 + uint64_t(s) * XSTEP);
+            first_product(std::bool_constant<C::T1>(), tmem + uint32_t(j % NS) * BX, f1, tmem + C::COL_F1, x1 + uint64_t(s) * XSTEP, s, 0);
             commit(s_full(j % NS));
             if constexpr (!C::OUT_S) commit(x1_empty(s));
             return true;
@@ -287,7 +329,8 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             const int s = j % C::R2;
             if (!wait(x2_full(s), j / C::R2)) return false;
             if (j >= ND && !wait(ds_taken(j % ND), j / ND - 1)) return false;
-            first_product(tmem + C::COL_DP + uint32_t(j % ND) * BX, f2, x2 + uint64_t(s) * XSTEP);
+            first_product(std::bool_constant<C::T2>(), tmem + C::COL_DP + uint32_t(j % ND) * BX, f2, tmem + C::COL_F2, x2 + uint64_t(s) * XSTEP,
+                          j % C::R1, 1);
             commit(dp_full(j % ND));
             if constexpr (!C::OUT_P) commit(x2_empty(s));
             return true;
@@ -320,8 +363,10 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 ok = sum_p(j) && (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
             } else if constexpr (PASS == kValuesOnly) {
                 ok = (!more || make_s(j + 1)) && sum_p(j);
-            } else {
+            } else if constexpr (C::ND == 2) {
                 ok = (!more || (make_s(j + 1) && make_dp(j + 1))) && sum_s(j);
+            } else {
+                ok = (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
             }
         }
         if (ok && n > 0) {
@@ -353,6 +398,25 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             row_lse = row + shift == 0 ? INFINITY : __ldcg(P.lse2 + stat);
             row_delta = __ldcg(P.delta + stat);
         }
+        if constexpr (C::T1) {
+            // the fixed operands' rows into TMEM, a part of the dims to a warpgroup
+            const bool in = row < (C::BY_KEYS ? P.Tk : P.Tq);
+            auto keep = [&](const Operand& o, uint32_t col) {
+                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(o.p) + batch * o.batch + head * o.head + row * o.row);
+#pragma unroll
+                for (int u = 0; u < D / 16 / C::WGS; ++u) {
+                    const int at = wg * (D / 16 / C::WGS) + u;
+                    const uint4 none = make_uint4(0, 0, 0, 0), a = in ? src[2 * at] : none, b = in ? src[2 * at + 1] : none;
+                    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    tmem_st8(mine + col + at * 8, w);
+                }
+            };
+            keep(P.f1, C::COL_F1);
+            if constexpr (C::T2) keep(P.f2, C::COL_F2);
+            tc::tmem_wait_st();
+            tc::tc_fence_before();
+            tc::mbar_arrive(f_full);
+        }
         for (int j = 0; j < n; ++j) {
             const int at = (first + (j0 + j) % per) * BX + wg * 32;
             const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * 32, dp_col = mine + C::COL_DP + uint32_t(j % ND) * BX + wg * 32;
@@ -367,12 +431,6 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 masked = at + 32 > row0 + shift + 1;
                 hi = row + shift + 1 - at;
             }
-            const int stat_j = j % C::RS;
-            const float* stat = reinterpret_cast<const float*>(smem + C::OFF_STAT + stat_j * C::STAT_BYTES) + wg * 32;
-            if constexpr (C::BY_KEYS) {
-                ok = wait(C::OUT_S ? x1_full(stat_j) : x2_full(stat_j), j / C::RS);
-                if (!ok) break;
-            }
             ok = wait(s_full(j % NS), j / NS);
             if (!ok) break;
             float p[32];
@@ -383,12 +441,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 tc::mbar_arrive(s_read);
             }
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                float l[4] = {row_lse, row_lse, row_lse, row_lse};
-                if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[i + e] = ex2(fmaf(p[i + e], P.scale_log2, -l[e]));
-            }
+            for (int i = 0; i < 32; ++i) p[i] = ex2(C::BY_KEYS ? p[i] * P.scale_log2 : fmaf(p[i], P.scale_log2, -row_lse));
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
@@ -408,12 +461,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 float d[32];
                 tmem_ld32_done(dp_col, d);
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float l[4] = {row_delta, row_delta, row_delta, row_delta};
-                    if constexpr (C::BY_KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(stat + BX + i);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[i + e] = p[i + e] * (d[i + e] - l[e]);
-                }
+                for (int i = 0; i < 32; ++i) d[i] = p[i] * (C::BY_KEYS ? d[i] : d[i] - row_delta);
                 if (masked) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -498,11 +546,22 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     if constexpr (!C::BY_KEYS) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// The rows' statistics: log2 of the sum of weights, and delta.  A warp per
-// (row, head), rows behind the last as rows without weights.
+// A number as three bf16 whose sum has all 24 bits of it (an infinity as the first).
+__device__ __forceinline__ uint4 three_terms(float x) {
+    const float a = __bfloat162float(__float2bfloat16_rn(x)), ra = isinf(a) ? 0.f : x - a;
+    const float b = __bfloat162float(__float2bfloat16_rn(ra)), rb = ra - b;
+    return make_uint4(pack_bf16(a, b), pack_bf16(rb, 0.f), 0, 0);
+}
+
+// The rows' statistics: log2 of the sum of weights, and delta; and as an MMA by
+// keys takes them, per 8 rows [2][8 rows][8 bf16]: the terms of -lse2 / scale
+// and of -delta.  A row without weights has a number there that makes its
+// weights 0, but no infinity, which would meet zeros.  A warp per (row, head),
+// rows behind the last as rows without weights.
 template <int D>
 __global__ void __launch_bounds__(256)
-    stats_kernel(const Operand dout, const Operand out, const float* lse, float* lse2, float* delta, int Tq, int Tpad, int Hq, long units) {
+    stats_kernel(const Operand dout, const Operand out, const float* lse, float* lse2, float* delta, uint8_t* aug, float scale_log2, int Tq, int Tpad,
+                 int Hq, long units) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int V = D / 32;
@@ -529,8 +588,13 @@ __global__ void __launch_bounds__(256)
     if (lane == 0) {
         const long to = (batch * Hq + head) * Tpad + row;
         const float l = row < Tq ? lse[(batch * Hq + head) * Tq + row] : -INFINITY;
-        lse2[to] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
+        const bool none = l == -INFINITY;
+        const float l2 = l * 1.4426950408889634f;
+        lse2[to] = none ? INFINITY : l2;
         delta[to] = sum;
+        uint4* a = reinterpret_cast<uint4*>(aug + (to / 8) * 256 + to % 8 * 16);
+        a[0] = three_terms(none ? (scale_log2 > 0.f ? -1e30f : 1e30f) : -l2 / scale_log2);
+        a[8] = three_terms(-sum);
     }
 }
 
@@ -589,6 +653,9 @@ int backward(const Args& a, cudaStream_t st) {
     const int Tpad = padded(a.Tq), shift = a.Tk - a.Tq, G = a.Hq / a.Hkv;
     const long rows = long(a.B) * a.Hq * Tpad;
     float *lse2 = a.stats, *delta = a.stats + rows;
+    uint8_t* aug = reinterpret_cast<uint8_t*>(a.stats + 2 * rows);
+    const float scale_log2 = a.scale * 1.4426950408889634f;
+    const float by_keys_scale = std::fabs(scale_log2) >= kLeastScale ? scale_log2 : scale_log2 < 0.f ? -kLeastScale : kLeastScale;
     {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(unsigned((rows + 7) / 8));
@@ -599,7 +666,7 @@ int backward(const Args& a, cudaStream_t st) {
         attr.val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        const int e = int(cudaLaunchKernelEx(&cfg, stats_kernel<D>, a.dout, a.out, a.lse, lse2, delta, a.Tq, Tpad, a.Hq, rows));
+        const int e = int(cudaLaunchKernelEx(&cfg, stats_kernel<D>, a.dout, a.out, a.lse, lse2, delta, aug, by_keys_scale, a.Tq, Tpad, a.Hq, rows));
         if (e != 0) return e;
     }
     CUtensorMap fixed_k, fixed_v, fixed_q, fixed_o, block_k, block_v, block_q, block_o;
@@ -618,7 +685,10 @@ int backward(const Args& a, cudaStream_t st) {
     p.Hkv = a.Hkv;
     p.B = a.B;
     p.scale = a.scale;
-    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.scale_log2 = by_keys_scale;
+    p.aug = aug;
+    p.f1 = a.k;
+    p.f2 = a.v;
     p.err = decoder::error_word();
     if (!p.err) return int(cudaErrorInvalidValue);
     // by keys
@@ -646,6 +716,9 @@ int backward(const Args& a, cudaStream_t st) {
     }
     if (e != 0) return e;
     // by queries
+    p.scale_log2 = scale_log2;
+    p.f1 = a.q;
+    p.f2 = a.dout;
     p.s_sum = a.dq;
     p.s_row = long(a.Hq) * D;
     p.s_head = D;
@@ -667,7 +740,7 @@ int backward(const Args& a, cudaStream_t st) {
 extern "C" {
 
 // Bytes of scratch that decoder_attention_backward needs.
-long decoder_attention_scratch(long B, long Tq, int Hq) { return 8 * B * Hq * ((Tq + kRows - 1) / kRows * kRows); }
+long decoder_attention_scratch(long B, long Tq, int Hq) { return 40 * B * Hq * ((Tq + kRows - 1) / kRows * kRows); }
 
 // Gradients of decoder_attention: dout, q, out [B][Tq][Hq][d] and k, v
 // [B][Hkv][Tk][d] of any strides that are multiples of 8 elements (row, head,

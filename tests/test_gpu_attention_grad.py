@@ -273,7 +273,7 @@ def test_refusals():
             (ValueError, lambda: A.attention_backward(dout, q, k, v, out, lse[:1]))]:
         with pytest.raises(error):
             call()
-    assert K.lib().decoder_attention_scratch(2, 130, 4) == 2 * 4 * 256 * 8
+    assert K.lib().decoder_attention_scratch(2, 130, 4) == 2 * 4 * 256 * 40
     # a shape past the kernels' index range comes back as an error
     big = torch.empty(1, 1, 64, dtype=BF, device="cuda").expand((1 << 20) + 1, 1, 64)
     with pytest.raises(RuntimeError):
