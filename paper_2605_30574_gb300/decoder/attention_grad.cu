@@ -73,7 +73,7 @@ using decoder::tmem_ld32_done;
 using decoder::tmem_st16;
 using decoder::tmem_st8;
 
-constexpr int kRows = 128, kMaxStages = 3, kMaxShares = 8;
+constexpr int kRows = 128, kMaxStages = 4, kMaxShares = 8;
 constexpr unsigned kErrLoad = 512, kErrMma = 1024, kErrOut = 2048, kErrDrain = 4096;
 // S - lse / scale, times the scale, has to be finite, and lse for a scale of 0:
 // below this the scores make no difference.
@@ -83,16 +83,20 @@ enum Pass { kKeys, kValuesOnly, kKeysOnly, kQueries };     // (both, dV, dK; dQ)
 template <int D, int PASS>
 struct Cfg {
     static constexpr bool BY_KEYS = PASS != kQueries, OUT_P = PASS == kKeys || PASS == kValuesOnly, OUT_S = PASS != kValuesOnly;
-    static constexpr int BX = D == 256 ? 64 : 128, PANELS = D / 64;
+    static constexpr int BX = D == 256 || (D == 128 && PASS == kKeys) ? 64 : 128, PANELS = D / 64;
     // warpgroups of the element operations, 32 columns of a block each; then the
     // warps that load and that issue
     static constexpr int WGS = BX / 32, LOAD_WARP = 4 * WGS, MMA_WARP = LOAD_WARP + 1, THREADS = 32 * (MMA_WARP + 1);
-    // which of the fixed operands are in TMEM; slots of S and of dP there
-    static constexpr bool T1 = PASS == kQueries || D == 256, T2 = PASS == kQueries && D < 256;
-    static constexpr int NS = OUT_S ? 1 : 2, ND = !OUT_S ? 0 : PASS == kQueries && D == 64 ? 2 : 1;
-    // rings of X1 and X2.  S(j + 1) is issued before dQ(j) where P meets nothing:
-    // three blocks of X1 are then in use or on their way.
-    static constexpr int R1 = D == 64 || PASS == kQueries ? 3 : 2, R2 = D == 64 ? 3 : 2;
+    // which of the fixed operands are in TMEM; whether P and dS have columns of
+    // their own there (else they are written over S and dP, one slot each but
+    // two of S for P alone)
+    static constexpr bool T1 = D == 256 || (PASS == kKeys) == (D == 128), T2 = PASS == kQueries && D < 256;
+    static constexpr bool P_OWN = PASS == kKeys, DS_OWN = OUT_S && D < 256;
+    static constexpr int NS = OUT_S ? 1 : 2, ND = OUT_S ? 1 : 0;
+    // rings of X1 and X2.  S(j + 1) is issued before a block's sums: three blocks
+    // of X1 are then in use or on their way.
+    static constexpr int R1 = D == 128 && PASS == kKeys ? 4 : D == 64 || PASS == kQueries ? 3 : 2;
+    static constexpr int R2 = D == 128 && PASS == kKeys ? 4 : D == 64 ? 3 : 2;
     static constexpr uint32_t F_BYTES = kRows * D * 2, X_BYTES = BX * D * 2;
     // the rows' numbers come with X1: see stats_kernel; ONES meets them
     static constexpr uint32_t AUG_BYTES = BY_KEYS ? BX * 32 : 0, ONES_BYTES = BY_KEYS ? kRows * 32 + 128 : 0;
@@ -103,7 +107,8 @@ struct Cfg {
     static constexpr int COLS = OUTS * D / WGS;            // a warpgroup's columns of the sums
     static constexpr int UNITS = COLS / 16;
     // TMEM columns
-    static constexpr uint32_t COL_DP = NS * BX, COL_F1 = COL_DP + ND * BX, COL_F2 = COL_F1 + (T1 ? D / 2 : 0);
+    static constexpr uint32_t COL_DP = NS * BX, COL_P = COL_DP + ND * BX, COL_DS = COL_P + (P_OWN ? BX / 2 : 0);
+    static constexpr uint32_t COL_F1 = COL_DS + (DS_OWN ? BX / 2 : 0), COL_F2 = COL_F1 + (T1 ? D / 2 : 0);
     static constexpr uint32_t COL_SUM = COL_F2 + (T2 ? D / 2 : 0), COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
     static_assert(COL_S_SUM + (OUT_S ? D : 0) <= 512);
     static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * ((WGS * UNITS + shares - 1) / shares) * 16 * kRows * 4; }
@@ -122,6 +127,19 @@ struct Cfg {
 __device__ __forceinline__ uint64_t plain_desc(uint32_t saddr, uint32_t k_bytes, uint32_t rows_bytes) {
     return uint64_t((saddr >> 4) & 0x3FFFu) | uint64_t(k_bytes >> 4) << 16 | uint64_t(rows_bytes >> 4) << 32 | uint64_t(1) << 46;
 }
+
+// A ring's stage, and the parity of its round.
+template <int N>
+struct Ring {
+    int s = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == N) {
+            s = 0;
+            phase ^= 1u;
+        }
+    }
+};
 
 struct GradParams {
     // [B Hq][Tpad]: log2 of the row's sum (+inf where it has no weights), delta;
@@ -143,9 +161,9 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     grad_kernel(const __grid_constant__ CUtensorMap tm_f1, const __grid_constant__ CUtensorMap tm_f2,
                 const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const GradParams P) {
     using C = Cfg<D, PASS>;
-    constexpr int BX = C::BX, NS = C::NS, ND = C::ND > 0 ? C::ND : 1;
+    constexpr int BX = C::BX, NS = C::NS;
     extern __shared__ uint8_t smem_raw[];
-    constexpr int kBars = 4 * kMaxStages + 16;
+    constexpr int kBars = 4 * kMaxStages + 11;
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
@@ -156,13 +174,17 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     auto x2_full = [&](int i) { return bar0 + 8u * (2 * kMaxStages + i); };
     auto x2_empty = [&](int i) { return bar0 + 8u * (3 * kMaxStages + i); };
     const uint32_t bar1 = bar0 + 8u * 4 * kMaxStages;
-    auto s_full = [&](int i) { return bar1 + 8u * i; };
-    auto dp_full = [&](int i) { return bar1 + 8u * (2 + i); };
-    auto p_ready = [&](int i) { return bar1 + 8u * (4 + i); };
-    auto ds_ready = [&](int i) { return bar1 + 8u * (6 + i); };
-    auto p_taken = [&](int i) { return bar1 + 8u * (8 + i); };
-    auto ds_taken = [&](int i) { return bar1 + 8u * (10 + i); };
-    const uint32_t f_full = bar1 + 8u * 12, sums = bar1 + 8u * 13, drain = bar1 + 8u * 14, s_read = bar1 + 8u * 15;
+    auto p_ready = [&](int i) { return bar1 + 8u * i; };
+    const uint32_t ds_ready = bar1 + 8u * 2, s_read = bar1 + 8u * 3, dp_read = bar1 + 8u * 4;      // (arrivals of all threads, up to here)
+    const uint32_t s_full = bar1 + 8u * 5, dp_full = bar1 + 8u * 6, f_full = bar1 + 8u * 7, sums = bar1 + 8u * 8, drain = bar1 + 8u * 9;
+    // A product's one commit (a second one right behind it waits for the first:
+    // 300 clocks) tells all that it frees: the last that reads a block of X1 or X2
+    // that its stage is empty, and with that what it has read or made besides.
+    // Block j's S, dP and sums are complete with:
+    auto s_done = [&](int j, uint32_t& phase) { return C::OUT_S ? (phase = j, s_full) : (phase = j / C::R1, x1_empty(j % C::R1)); };
+    auto dp_done = [&](int j, uint32_t& phase) { return C::OUT_P ? (phase = j, dp_full) : (phase = j / C::R2, x2_empty(j % C::R2)); };
+    auto p_done = [&](int j, uint32_t& phase) { return phase = j / C::R2, x2_empty(j % C::R2); };
+    auto ds_done = [&](int j, uint32_t& phase) { return phase = j / C::R1, x1_empty(j % C::R1); };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
     const int share = P.shares > 1 ? int(cluster.block_rank()) : 0;
@@ -191,8 +213,8 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
         constexpr int kAll = C::WGS * kRows;
         for (int i = 0; i < kBars; ++i) {
             const uint32_t bar = bar0 + 8u * i;
-            const bool threads = (bar >= p_ready(0) && bar <= ds_ready(1)) || bar == s_read;
-            tc::mbar_init(bar, threads ? kAll : bar == f_full ? (C::T1 ? kAll : 0) + (C::F_LOADS > 0 ? 1 : 0) : 1);
+            const bool threads = bar >= p_ready(0) && bar <= dp_read;
+            tc::mbar_init(bar, threads ? kAll : bar == f_full ? (C::T1 || C::T2 ? kAll : 0) + (C::F_LOADS > 0 ? 1 : 0) : 1);
         }
         s_abort = 0;
         tc::fence_mbar_init();
@@ -225,163 +247,158 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     const uint32_t tmem = s_tmem;
     bool ok = true;
 
+    // One lane of its warp loads and one issues, all of the loop: with every lane
+    // in it, and each copy and MMA under a test for the one, an MMA took 35 to 50
+    // clocks to issue in place of 10, a wait on a complete barrier 140, and the
+    // whole backward pass 1.2 times as long.
     if (warp == C::LOAD_WARP) {
-        const bool leader = tc::elect_one();
-        if (C::F_LOADS > 0 && n > 0 && leader) {
-            tc::mbar_arrive_expect_tx(f_full, C::F_LOADS * C::F_BYTES);
+        if (tc::elect_one() && n > 0) {
+            auto wait = [&](uint32_t bar, uint32_t phase) { return tc::mbar_wait(bar, phase, &s_abort, P.err, kErrLoad); };
+            if constexpr (C::F_LOADS > 0) {
+                tc::mbar_arrive_expect_tx(f_full, C::F_LOADS * C::F_BYTES);
 #pragma unroll
-            for (int p = 0; p < C::PANELS; ++p) {
-                if (!C::T1) tma_load_4d(sbase + p * (kRows * 128), &tm_f1, p * 64, row0, head, batch, f_full);
-                if (C::OUT_S && !C::T2) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
-            }
-        }
-        int j1 = 0, j2 = 0;      // blocks asked for
-        for (int j = 0; j < n; ++j) {
-            const int at = (first + (j0 + j) % per) * BX;
-            const int x_head = C::BY_KEYS ? head * G + (j0 + j) / per : head / G;
-            const int s1 = j % C::R1, s2 = j % C::R2;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait(x1_empty(s1), (uint32_t(j / C::R1) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
-            if (!ok) break;
-            if (leader) {
-                tc::mbar_arrive_expect_tx(x1_full(s1), C::X_BYTES + C::AUG_BYTES);
-#pragma unroll
-                for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_4d(sbase + C::OFF_X1 + uint32_t(s1) * C::X_BYTES + p * (BX * 128), &tm_x1, p * 64, at, x_head, batch, x1_full(s1));
-                if constexpr (C::BY_KEYS)
-                    decoder::bulk_load(sbase + C::OFF_AUG + uint32_t(s1) * C::AUG_BYTES, P.aug + ((long(batch) * P.Hq + x_head) * P.Tpad + at) * 32,
-                                       C::AUG_BYTES, x1_full(s1));
-            }
-            ++j1;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait(x2_empty(s2), (uint32_t(j / C::R2) & 1u) ^ 1u, &s_abort, P.err, kErrLoad));
-            if (!ok) break;
-            if (leader) {
-                tc::mbar_arrive_expect_tx(x2_full(s2), C::X_BYTES);
-#pragma unroll
-                for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_4d(sbase + C::OFF_X2 + uint32_t(s2) * C::X_BYTES + p * (BX * 128), &tm_x2, p * 64, at, x_head, batch, x2_full(s2));
-            }
-            ++j2;
-        }
-        // Every copy issued must land before the CTA may exit, and the commits
-        // on the stages' barriers must arrive.
-        volatile int no_abort = 0;
-        if (n > 0) tc::mbar_wait(f_full, 0, &no_abort, P.err, kErrDrain);
-        for (int i = max(0, j1 - C::R1); i < j1; ++i) tc::mbar_wait(x1_full(i % C::R1), uint32_t(i / C::R1) & 1u, &no_abort, P.err, kErrDrain);
-        for (int i = max(0, j2 - C::R2); i < j2; ++i) tc::mbar_wait(x2_full(i % C::R2), uint32_t(i / C::R2) & 1u, &no_abort, P.err, kErrDrain);
-        for (int i = max(0, j1 - C::R1); ok && i < j1; ++i)
-            ok = tc::mbar_wait(x1_empty(i % C::R1), uint32_t(i / C::R1) & 1u, &s_abort, P.err, kErrDrain);
-        for (int i = max(0, j2 - C::R2); ok && i < j2; ++i)
-            ok = tc::mbar_wait(x2_empty(i % C::R2), uint32_t(i / C::R2) & 1u, &s_abort, P.err, kErrDrain);
-    } else if (warp == C::MMA_WARP) {
-        // Descriptors are made by the whole warp (see gemm.cu): issued from
-        // values of one lane, an MMA took 72 clocks.
-        const bool leader = tc::elect_one();
-        constexpr uint32_t idesc_s = tc::idesc_bf16_f32(kRows, BX, false), idesc_sum = tc::idesc_bf16_f32(kRows, D, true);
-        const uint64_t f1 = tc::sw128_desc(sbase, 16, 1024), f2 = tc::sw128_desc(sbase + C::OFF_F2, 16, 1024);
-        const uint64_t x1 = tc::sw128_desc(sbase + C::OFF_X1, 16, 1024), x2 = tc::sw128_desc(sbase + C::OFF_X2, 16, 1024);
-        const uint64_t x1_mn = tc::sw128_desc(sbase + C::OFF_X1, BX * 128, 1024), x2_mn = tc::sw128_desc(sbase + C::OFF_X2, BX * 128, 1024);
-        const uint64_t ones = plain_desc(sbase + C::OFF_ONES, 128, 256), augs = plain_desc(sbase + C::OFF_AUG, 128, 256);
-        auto wait = [&](uint32_t bar, int phase) {
-            const bool is = __all_sync(0xffffffffu, tc::mbar_wait(bar, uint32_t(phase) & 1u, &s_abort, P.err, kErrMma));
-            tc::tc_fence_after();
-            return is;
-        };
-        // F X^T into a slot (descriptor units of 16 bytes), F by descriptor or in
-        // TMEM; by keys with the rows' numbers, from the half `core` of them
-        auto first_product = [&](auto in_tmem, uint32_t to, uint64_t f, uint32_t f_tmem, uint64_t x, int aug, int core) {
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t b = x + uint64_t((kk / 4) * (BX * 8) + (kk % 4) * 2);
-                if constexpr (decltype(in_tmem)::value) {
-                    if (leader) mma_f16_ts(to, f_tmem + kk * 8, b, idesc_s, kk > 0 ? 1u : 0u);
-                } else {
-                    const uint64_t a = f + uint64_t((kk / 4) * (kRows * 8) + (kk % 4) * 2);
-                    if (leader) tc::mma_f16_ss(to, a, b, idesc_s, kk > 0 ? 1u : 0u);
+                for (int p = 0; p < C::PANELS; ++p) {
+                    if (!C::T1) tma_load_4d(sbase + p * (kRows * 128), &tm_f1, p * 64, row0, head, batch, f_full);
+                    if (C::OUT_S && !C::T2) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
                 }
             }
-            if constexpr (C::BY_KEYS) {
-                if (leader) tc::mma_f16_ss(to, ones + uint64_t(core * 8), augs + uint64_t(aug * (C::AUG_BYTES >> 4)), idesc_s, 1u);
-            }
-        };
-        // a slot's bf16, 16 columns at the start of each 32, times X, added up
-        auto second_product = [&](uint32_t sum, uint32_t slot, uint64_t x, bool add) {
+            int j1 = 0, j2 = 0;      // blocks asked for
+            int block = j0 % per, x_head = C::BY_KEYS ? head * G + j0 / per : head / G;
+            Ring<C::R1> r1;
+            Ring<C::R2> r2;
+            for (; j2 < n; ++j2) {
+                const int at = (first + block) * BX;
+                ok = wait(x1_empty(r1.s), r1.phase ^ 1u);
+                if (!ok) break;
+                const uint32_t to1 = sbase + C::OFF_X1 + uint32_t(r1.s) * C::X_BYTES, bar1 = x1_full(r1.s);
+                tc::mbar_arrive_expect_tx(bar1, C::X_BYTES + C::AUG_BYTES);
 #pragma unroll
-            for (int kk = 0; kk < BX / 16; ++kk) {
-                const uint32_t a = slot + (kk / 2) * 32 + (kk % 2) * 8;
-                const uint64_t b = x + uint64_t(kk * 128);
-                if (leader) mma_f16_ts(sum, a, b, idesc_sum, add || kk > 0 ? 1u : 0u);
+                for (int p = 0; p < C::PANELS; ++p) tma_load_4d(to1 + p * (BX * 128), &tm_x1, p * 64, at, x_head, batch, bar1);
+                if constexpr (C::BY_KEYS)
+                    decoder::bulk_load(sbase + C::OFF_AUG + uint32_t(r1.s) * C::AUG_BYTES, P.aug + ((long(batch) * P.Hq + x_head) * P.Tpad + at) * 32,
+                                       C::AUG_BYTES, bar1);
+                r1.next();
+                ++j1;
+                ok = wait(x2_empty(r2.s), r2.phase ^ 1u);
+                if (!ok) break;
+                const uint32_t to2 = sbase + C::OFF_X2 + uint32_t(r2.s) * C::X_BYTES, bar2 = x2_full(r2.s);
+                tc::mbar_arrive_expect_tx(bar2, C::X_BYTES);
+#pragma unroll
+                for (int p = 0; p < C::PANELS; ++p) tma_load_4d(to2 + p * (BX * 128), &tm_x2, p * 64, at, x_head, batch, bar2);
+                r2.next();
+                if (++block == per) {
+                    block = 0;
+                    x_head += C::BY_KEYS ? 1 : 0;
+                }
             }
-        };
-        auto commit = [&](uint32_t bar) {
-            if (leader) tc::mma_commit(bar);
-        };
-        constexpr uint32_t XSTEP = C::X_BYTES >> 4;
-        auto make_s = [&](int j) {
-            const int s = j % C::R1;
-            if (!wait(x1_full(s), j / C::R1)) return false;
-            if (C::OUT_P ? j >= NS && !wait(p_taken(j % NS), j / NS - 1) : j > 0 && !wait(s_read, j - 1)) return false;
-            first_product(std::bool_constant<C::T1>(), tmem + uint32_t(j % NS) * BX, f1, tmem + C::COL_F1, x1 + uint64_t(s) * XSTEP, s, 0);
-            commit(s_full(j % NS));
-            if constexpr (!C::OUT_S) commit(x1_empty(s));
-            return true;
-        };
-        auto make_dp = [&](int j) {
-            const int s = j % C::R2;
-            if (!wait(x2_full(s), j / C::R2)) return false;
-            if (j >= ND && !wait(ds_taken(j % ND), j / ND - 1)) return false;
-            first_product(std::bool_constant<C::T2>(), tmem + C::COL_DP + uint32_t(j % ND) * BX, f2, tmem + C::COL_F2, x2 + uint64_t(s) * XSTEP,
-                          j % C::R1, 1);
-            commit(dp_full(j % ND));
-            if constexpr (!C::OUT_P) commit(x2_empty(s));
-            return true;
-        };
-        auto sum_p = [&](int j) {
-            const int s = j % C::R2;
-            if (!wait(p_ready(j % NS), j / NS)) return false;
-            if (C::OUT_P && !C::OUT_S && !wait(x2_full(s), j / C::R2)) return false;     // (else dP has waited)
-            second_product(tmem + C::COL_SUM, tmem + uint32_t(j % NS) * BX, x2_mn + uint64_t(s) * XSTEP, j > 0);
-            commit(p_taken(j % NS));
-            commit(x2_empty(s));
-            return true;
-        };
-        auto sum_s = [&](int j) {
-            const int s = j % C::R1;
-            if (!wait(ds_ready(j % ND), j / ND)) return false;
-            second_product(tmem + C::COL_S_SUM, tmem + C::COL_DP + uint32_t(j % ND) * BX, x1_mn + uint64_t(s) * XSTEP, j > 0);
-            commit(ds_taken(j % ND));
-            commit(x1_empty(s));
-            return true;
-        };
-        const bool any = n > 0 && (ok = wait(f_full, 0));
-        if (any) {
-            ok = make_s(0);
-            if constexpr (C::OUT_S) ok = ok && make_dp(0);
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            const bool more = j + 1 < n;
-            if constexpr (PASS == kKeys) {
-                ok = sum_p(j) && (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
-            } else if constexpr (PASS == kValuesOnly) {
-                ok = (!more || make_s(j + 1)) && sum_p(j);
-            } else if constexpr (C::ND == 2) {
-                ok = (!more || (make_s(j + 1) && make_dp(j + 1))) && sum_s(j);
-            } else {
-                ok = (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
-            }
-        }
-        if (ok && n > 0) {
-            commit(sums);
-            // the commits that nothing else waits for
-            if constexpr (C::OUT_P)
-                for (int j = max(0, n - NS); ok && j < n; ++j) ok = wait(p_taken(j % NS), j / NS);
-            if constexpr (C::OUT_S)
-                for (int j = max(0, n - ND); ok && j < n; ++j) ok = wait(ds_taken(j % ND), j / ND);
-        }
-        if (!ok && any && leader) {
-            // let the MMAs already issued finish before TMEM is freed
-            tc::mma_commit(drain);
+            // Every copy issued must land before the CTA may exit, and the commits
+            // on the stages' barriers must arrive.
             volatile int no_abort = 0;
-            tc::mbar_wait(drain, 0, &no_abort, P.err, kErrDrain);
+            tc::mbar_wait(f_full, 0, &no_abort, P.err, kErrDrain);
+            for (int i = max(0, j1 - C::R1); i < j1; ++i) tc::mbar_wait(x1_full(i % C::R1), uint32_t(i / C::R1) & 1u, &no_abort, P.err, kErrDrain);
+            for (int i = max(0, j2 - C::R2); i < j2; ++i) tc::mbar_wait(x2_full(i % C::R2), uint32_t(i / C::R2) & 1u, &no_abort, P.err, kErrDrain);
+            for (int i = max(0, j1 - C::R1); ok && i < j1; ++i) ok = wait(x1_empty(i % C::R1), uint32_t(i / C::R1) & 1u);
+            for (int i = max(0, j2 - C::R2); ok && i < j2; ++i) ok = wait(x2_empty(i % C::R2), uint32_t(i / C::R2) & 1u);
+        }
+    } else if (warp == C::MMA_WARP) {
+        if (tc::elect_one() && n > 0) {
+            constexpr uint32_t idesc_s = tc::idesc_bf16_f32(kRows, BX, false), idesc_sum = tc::idesc_bf16_f32(kRows, D, true);
+            const uint64_t f1 = tc::sw128_desc(sbase, 16, 1024), f2 = tc::sw128_desc(sbase + C::OFF_F2, 16, 1024);
+            const uint64_t x1 = tc::sw128_desc(sbase + C::OFF_X1, 16, 1024), x2 = tc::sw128_desc(sbase + C::OFF_X2, 16, 1024);
+            const uint64_t x1_mn = tc::sw128_desc(sbase + C::OFF_X1, BX * 128, 1024), x2_mn = tc::sw128_desc(sbase + C::OFF_X2, BX * 128, 1024);
+            const uint64_t ones = plain_desc(sbase + C::OFF_ONES, 128, 256), augs = plain_desc(sbase + C::OFF_AUG, 128, 256);
+            auto wait = [&](uint32_t bar, uint32_t phase) {
+                const bool is = tc::mbar_wait(bar, phase & 1u, &s_abort, P.err, kErrMma);
+                tc::tc_fence_after();
+                return is;
+            };
+            // F X^T into a slot (descriptor units of 16 bytes), F by descriptor or in
+            // TMEM; by keys with the rows' numbers, from the half `core` of them
+            auto first_product = [&](auto in_tmem, uint32_t to, uint64_t f, uint32_t f_tmem, uint64_t x, int aug, int core) {
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint64_t b = x + uint64_t((kk / 4) * (BX * 8) + (kk % 4) * 2);
+                    if constexpr (decltype(in_tmem)::value)
+                        mma_f16_ts(to, f_tmem + kk * 8, b, idesc_s, kk > 0 ? 1u : 0u);
+                    else
+                        tc::mma_f16_ss(to, f + uint64_t((kk / 4) * (kRows * 8) + (kk % 4) * 2), b, idesc_s, kk > 0 ? 1u : 0u);
+                }
+                if constexpr (C::BY_KEYS) tc::mma_f16_ss(to, ones + uint64_t(core * 8), augs + uint64_t(aug) * (C::AUG_BYTES >> 4), idesc_s, 1u);
+            };
+            // bf16 in columns of their own, or 16 at the start of each 32 of a slot,
+            // times X, added up
+            auto second_product = [&](auto own, uint32_t sum, uint32_t slot, uint64_t x, bool add) {
+#pragma unroll
+                for (int kk = 0; kk < BX / 16; ++kk)
+                    mma_f16_ts(sum, slot + (decltype(own)::value ? kk * 8 : (kk / 2) * 32 + (kk % 2) * 8), x + uint64_t(kk * 128), idesc_sum,
+                               add || kk > 0 ? 1u : 0u);
+            };
+            constexpr uint32_t XSTEP = C::X_BYTES >> 4;
+            // the stages of each product's operand, in the order of its blocks
+            Ring<C::R1> s_ring, ss_ring, aug_ring;
+            Ring<C::R2> dp_ring, sp_ring;
+            auto make_s = [&](int j) {
+                const int s = s_ring.s;
+                if (!wait(x1_full(s), s_ring.phase)) return false;
+                uint32_t phase, bar = C::OUT_P && !C::P_OWN ? p_done(j - NS, phase) : (phase = j - 1, s_read);
+                if (j >= (C::OUT_P && !C::P_OWN ? NS : 1) && !wait(bar, phase)) return false;
+                first_product(std::bool_constant<C::T1>(), tmem + uint32_t(j % NS) * BX, f1, tmem + C::COL_F1, x1 + uint64_t(s) * XSTEP, s, 0);
+                tc::mma_commit(s_done(j, phase));
+                s_ring.next();
+                return true;
+            };
+            auto make_dp = [&](int j) {
+                const int s = dp_ring.s;
+                if (!wait(x2_full(s), dp_ring.phase)) return false;
+                uint32_t phase, bar = C::DS_OWN ? (phase = j - 1, dp_read) : ds_done(j - 1, phase);
+                if (j > 0 && !wait(bar, phase)) return false;
+                first_product(std::bool_constant<C::T2>(), tmem + C::COL_DP, f2, tmem + C::COL_F2, x2 + uint64_t(s) * XSTEP, aug_ring.s, 1);
+                tc::mma_commit(dp_done(j, phase));
+                dp_ring.next();
+                aug_ring.next();
+                return true;
+            };
+            auto sum_p = [&](int j) {
+                const int s = sp_ring.s;
+                if (!wait(p_ready(j % NS), j / NS)) return false;
+                if (C::OUT_P && !C::OUT_S && !wait(x2_full(s), sp_ring.phase)) return false;     // (else dP has waited)
+                second_product(std::bool_constant<C::P_OWN>(), tmem + C::COL_SUM, tmem + (C::P_OWN ? C::COL_P : uint32_t(j % NS) * BX),
+                               x2_mn + uint64_t(s) * XSTEP, j > 0);
+                tc::mma_commit(x2_empty(s));
+                sp_ring.next();
+                return true;
+            };
+            auto sum_s = [&](int j) {
+                const int s = ss_ring.s;
+                if (!wait(ds_ready, j)) return false;
+                second_product(std::bool_constant<C::DS_OWN>(), tmem + C::COL_S_SUM, tmem + (C::DS_OWN ? C::COL_DS : C::COL_DP),
+                               x1_mn + uint64_t(s) * XSTEP, j > 0);
+                tc::mma_commit(x1_empty(s));
+                ss_ring.next();
+                return true;
+            };
+            const bool any = ok = wait(f_full, 0);
+            ok = ok && make_s(0);
+            if constexpr (C::OUT_S) ok = ok && make_dp(0);
+            for (int j = 0; ok && j < n; ++j) {
+                const bool more = j + 1 < n;
+                if constexpr (PASS == kKeys) {
+                    ok = (!more || make_s(j + 1)) && sum_p(j) && (!more || make_dp(j + 1)) && sum_s(j);
+                } else if constexpr (PASS == kValuesOnly) {
+                    ok = (!more || make_s(j + 1)) && sum_p(j);
+                } else if constexpr (C::DS_OWN) {
+                    ok = (!more || (make_s(j + 1) && make_dp(j + 1))) && sum_s(j);
+                } else {
+                    ok = (!more || make_s(j + 1)) && sum_s(j) && (!more || make_dp(j + 1));
+                }
+            }
+            if (ok) tc::mma_commit(sums);
+            if (!ok && any) {
+                // let the MMAs already issued finish before TMEM is freed
+                tc::mma_commit(drain);
+                volatile int no_abort = 0;
+                tc::mbar_wait(drain, 0, &no_abort, P.err, kErrDrain);
+            }
         }
     } else {
         const int wg = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + r;
@@ -398,7 +415,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             row_lse = row + shift == 0 ? INFINITY : __ldcg(P.lse2 + stat);
             row_delta = __ldcg(P.delta + stat);
         }
-        if constexpr (C::T1) {
+        if constexpr (C::T1 || C::T2) {
             // the fixed operands' rows into TMEM, a part of the dims to a warpgroup
             const bool in = row < (C::BY_KEYS ? P.Tk : P.Tq);
             auto keep = [&](const Operand& o, uint32_t col) {
@@ -411,7 +428,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                     tmem_st8(mine + col + at * 8, w);
                 }
             };
-            keep(P.f1, C::COL_F1);
+            if constexpr (C::T1) keep(P.f1, C::COL_F1);
             if constexpr (C::T2) keep(P.f2, C::COL_F2);
             tc::tmem_wait_st();
             tc::tc_fence_before();
@@ -419,7 +436,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
         }
         for (int j = 0; j < n; ++j) {
             const int at = (first + (j0 + j) % per) * BX + wg * 32;
-            const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * 32, dp_col = mine + C::COL_DP + uint32_t(j % ND) * BX + wg * 32;
+            const uint32_t s_col = mine + uint32_t(j % NS) * BX + wg * 32, dp_col = mine + C::COL_DP + wg * 32;
             // columns that the row's key is seen from, or the row sees: from lo, to hi
             int lo = 0, hi = 32, single = -1;
             bool masked;
@@ -431,12 +448,13 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 masked = at + 32 > row0 + shift + 1;
                 hi = row + shift + 1 - at;
             }
-            ok = wait(s_full(j % NS), j / NS);
+            uint32_t phase, bar = s_done(j, phase);
+            ok = wait(bar, phase);
             if (!ok) break;
             float p[32];
             uint32_t w[16];
             tmem_ld32_done(s_col, p);
-            if constexpr (!C::OUT_P) {
+            if constexpr (!C::OUT_P || C::P_OWN) {
                 tc::tc_fence_before();
                 tc::mbar_arrive(s_read);
             }
@@ -450,16 +468,26 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             if constexpr (C::OUT_P) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-                tmem_st16(s_col, w);
+                if constexpr (C::P_OWN) {
+                    bar = p_done(j - 1, phase);
+                    ok = j == 0 || wait(bar, phase);
+                    if (!ok) break;
+                }
+                tmem_st16(C::P_OWN ? mine + C::COL_P + wg * 16 : s_col, w);
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
                 tc::mbar_arrive(p_ready(j % NS));
             }
             if constexpr (C::OUT_S) {
-                ok = wait(dp_full(j % ND), j / ND);
+                bar = dp_done(j, phase);
+                ok = wait(bar, phase);
                 if (!ok) break;
                 float d[32];
                 tmem_ld32_done(dp_col, d);
+                if constexpr (C::DS_OWN) {
+                    tc::tc_fence_before();
+                    tc::mbar_arrive(dp_read);
+                }
 #pragma unroll
                 for (int i = 0; i < 32; ++i) d[i] = p[i] * (C::BY_KEYS ? d[i] : d[i] - row_delta);
                 if (masked) {
@@ -469,10 +497,15 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack_bf16(d[2 * i], d[2 * i + 1]);
-                tmem_st16(dp_col, w);
+                if constexpr (C::DS_OWN) {
+                    bar = ds_done(j - 1, phase);
+                    ok = j == 0 || wait(bar, phase);
+                    if (!ok) break;
+                }
+                tmem_st16(C::DS_OWN ? mine + C::COL_DS + wg * 16 : dp_col, w);
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
-                tc::mbar_arrive(ds_ready(j % ND));
+                tc::mbar_arrive(ds_ready);
             }
         }
         if (ok && n > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(sums, 0, &s_abort, P.err, kErrOut));
@@ -649,7 +682,7 @@ int padded(int T) { return (T + kRows - 1) / kRows * kRows; }
 
 template <int D>
 int backward(const Args& a, cudaStream_t st) {
-    constexpr int BX = Cfg<D, kQueries>::BX;
+    constexpr int BX = Cfg<D, kQueries>::BX, BXK = Cfg<D, D == 256 ? kKeysOnly : kKeys>::BX;      // (of keys, of queries)
     const int Tpad = padded(a.Tq), shift = a.Tk - a.Tq, G = a.Hq / a.Hkv;
     const long rows = long(a.B) * a.Hq * Tpad;
     float *lse2 = a.stats, *delta = a.stats + rows;
@@ -673,7 +706,7 @@ int backward(const Args& a, cudaStream_t st) {
     if (!decoder::operand_map(&fixed_k, a.k, D, a.Tk, a.Hkv, a.B, kRows) || !decoder::operand_map(&fixed_v, a.v, D, a.Tk, a.Hkv, a.B, kRows) ||
         !decoder::operand_map(&fixed_q, a.q, D, a.Tq, a.Hq, a.B, kRows) || !decoder::operand_map(&fixed_o, a.dout, D, a.Tq, a.Hq, a.B, kRows) ||
         !decoder::operand_map(&block_k, a.k, D, a.Tk, a.Hkv, a.B, BX) || !decoder::operand_map(&block_v, a.v, D, a.Tk, a.Hkv, a.B, BX) ||
-        !decoder::operand_map(&block_q, a.q, D, a.Tq, a.Hq, a.B, BX) || !decoder::operand_map(&block_o, a.dout, D, a.Tq, a.Hq, a.B, BX))
+        !decoder::operand_map(&block_q, a.q, D, a.Tq, a.Hq, a.B, BXK) || !decoder::operand_map(&block_o, a.dout, D, a.Tq, a.Hq, a.B, BXK))
         return int(cudaErrorInvalidValue);
     GradParams p{};
     p.lse2 = lse2;
@@ -698,10 +731,10 @@ int backward(const Args& a, cudaStream_t st) {
     p.p_head = p.s_head = long(a.Tk) * D;
     p.p_batch = p.s_batch = long(a.Hkv) * a.Tk * D;
     p.tiles = (a.Tk + kRows - 1) / kRows;
-    const int blocks = (a.Tq + BX - 1) / BX;
+    const int blocks = (a.Tq + BXK - 1) / BXK;
     long longest = 0, total = 0;
     for (int t = 0; t < p.tiles; ++t) {
-        const long n = long(G) * std::max(0, blocks - std::max(0, t * kRows - shift) / BX);
+        const long n = long(G) * std::max(0, blocks - std::max(0, t * kRows - shift) / BXK);
         longest = std::max(longest, n);
         total += n;
     }
