@@ -53,9 +53,12 @@ def _check(what, q, k, v):
     raise ValueError(f"{what}: the query heads must be a multiple of the kv heads")
 
 
-def _operand(t, heads_first):
-    """The tensor, or a copy that the kernels can read, and its (row, head,
-    batch) strides."""
+_STRIDES = {n: ctypes.c_long * n for n in (9, 15)}
+
+
+def _readable(t, heads_first):
+    """A copy of the tensor that the kernels can read, or the tensor, and its
+    (row, head, batch) strides."""
     def strides(t):
         s = t.stride()
         return (s[-2], s[-3], s[0]) if heads_first else (s[-3], s[-2], s[0])
@@ -70,17 +73,32 @@ def _operand(t, heads_first):
     return t, st
 
 
-def _operands(rows_first, heads_first):
-    """Both groups as the kernels can read them, and their strides as a C array
-    (None: all contiguous)."""
-    ts, low = (*rows_first, *heads_first), 0
+def _operands(*ts):
+    """The tensors as the kernels can read them (the last two, k and v, have
+    their heads first), their addresses, and their strides as a C array (None:
+    all contiguous)."""
+    ptrs, low, plain = [], 0, True
     for t in ts:
-        low |= t.data_ptr() if t.is_contiguous() and not t.is_neg() else 1
+        p = t.data_ptr()
+        ptrs.append(p)
+        if t.is_neg():
+            low = 1
+        low |= p
+        plain = plain and t.is_contiguous()
     if not low & 15:
-        return ts, None
-    got = [_operand(t, False) for t in rows_first] + [_operand(t, True) for t in heads_first]
-    flat = [s for _, st in got for s in st]
-    return [t for t, _ in got], (ctypes.c_long * len(flat))(*flat)
+        if plain:
+            return ts, ptrs, None
+        flat, last = [], len(ts) - 2
+        for i, t in enumerate(ts):
+            s = t.stride()
+            b, (x, y, one) = s[0], s[-3:]
+            if one != 1 or (b | x | y) & 7 or not 0 < min(s) or max(s) >= 1 << 38:
+                break
+            flat += (y, x, b) if i >= last else (x, y, b)
+        else:
+            return ts, ptrs, _STRIDES[len(flat)](*flat)
+    got = [_readable(t, i >= len(ts) - 2) for i, t in enumerate(ts)]
+    return [t for t, _ in got], [t.data_ptr() for t, _ in got], _STRIDES[3 * len(ts)](*[s for _, st in got for s in st])
 
 
 def _scale(scale, d):
@@ -104,9 +122,8 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     B = B[0] if B else 1
     if B * Tq * Tk == 0:
         return out.zero_(), lse.fill_(-math.inf)
-    (q, k, v), strides = _operands((q,), (k, v))
-    _launch("decoder_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, out.data_ptr(), lse.data_ptr(), B, Tq, Tk, Hq,
-            Hkv, d, _scale(scale, d))
+    ts, ptrs, strides = _operands(q, k, v)      # (ts: copies live until the launch)
+    _launch("decoder_attention", *ptrs, strides, out.data_ptr(), lse.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
     return out, lse
 
 
@@ -134,16 +151,15 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     if B * Tq * Tk == 0:
         return torch.zeros(shape, dtype=BF16, device=device), torch.zeros(k.shape, dtype=BF16, device=device), \
             torch.zeros(k.shape, dtype=BF16, device=device)
-    (dout, q, out, k, v), strides = _operands((dout, q, out), (k, v))
+    ts, ptrs, strides = _operands(dout, q, out, k, v)      # (ts: copies live until the launch)
     if not lse.is_contiguous() or lse.is_neg():
         lse = lse.resolve_neg().contiguous()
     dq = torch.empty(shape, dtype=BF16, device=device)
     dk = torch.empty(k.shape, dtype=BF16, device=device)
     dv = torch.empty(k.shape, dtype=BF16, device=device)
     scratch = torch.empty(40 * B * Hq * ((Tq + 127) // 128 * 128), dtype=torch.uint8, device=device)
-    _launch("decoder_attention_backward", dout.data_ptr(), q.data_ptr(), out.data_ptr(), k.data_ptr(), v.data_ptr(),
-            lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d,
-            _scale(scale, d))
+    _launch("decoder_attention_backward", *ptrs, lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
     return dq, dk, dv
 
 

@@ -589,45 +589,59 @@ __device__ __forceinline__ uint4 three_terms(float x) {
 // The rows' statistics: log2 of the sum of weights, and delta; and as an MMA by
 // keys takes them, per 8 rows [2][8 rows][8 bf16]: the terms of -lse2 / scale
 // and of -delta.  A row without weights has a number there that makes its
-// weights 0, but no infinity, which would meet zeros.  A warp per (row, head),
-// rows behind the last as rows without weights.
+// weights 0, but no infinity, which would meet zeros.  A warp takes 8 rows of a
+// head, 16 bytes to a lane, all asked for at once; rows behind the last are rows
+// without weights.
 template <int D>
 __global__ void __launch_bounds__(256)
     stats_kernel(const Operand dout, const Operand out, const float* lse, float* lse2, float* delta, uint8_t* aug, float scale_log2, int Tq, int Tpad,
                  int Hq, long units) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    constexpr int V = D / 32;
-    struct alignas(2 * V) Vec {
-        __nv_bfloat16 x[V];
-    };
-    const int lane = threadIdx.x & 31;
+    constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, N = 8 / AT_ONCE;      // lanes to a row, rows of a load
+    const int lane = threadIdx.x & 31, part = lane % LANES;
     const long unit = long(blockIdx.x) * 8 + (threadIdx.x >> 5);
     if (unit >= units) return;
-    const int head = int(unit % Hq);
-    const long rest = unit / Hq, batch = rest / Tpad;
-    const int row = int(rest % Tpad);
-    float sum = 0.f;
-    if (row < Tq) {
-        const auto at = [&](const Operand& o) {
-            return reinterpret_cast<const Vec*>(static_cast<const __nv_bfloat16*>(o.p) + batch * o.batch + head * o.head + row * o.row)[lane];
-        };
-        const Vec a = at(dout), b = at(out);
+    const int groups = Tpad / 8, row0 = int(unit % groups) * 8;
+    const long at = unit / groups, batch = at / Hq, head = at % Hq;
+    auto load = [&](const Operand& o, int row) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(o.p) + batch * o.batch + head * o.head + row * o.row;
+        return row < Tq ? reinterpret_cast<const uint4*>(p)[part] : make_uint4(0, 0, 0, 0);
+    };
+    uint4 a[N], b[N];
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum = fmaf(__bfloat162float(a.x[i]), __bfloat162float(b.x[i]), sum);
-#pragma unroll
-        for (int off = 16; off > 0; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    for (int i = 0; i < N; ++i) {
+        const int row = row0 + i * AT_ONCE + lane / LANES;
+        a[i] = load(dout, row);
+        b[i] = load(out, row);
     }
-    if (lane == 0) {
-        const long to = (batch * Hq + head) * Tpad + row;
-        const float l = row < Tq ? lse[(batch * Hq + head) * Tq + row] : -INFINITY;
-        const bool none = l == -INFINITY;
-        const float l2 = l * 1.4426950408889634f;
-        lse2[to] = none ? INFINITY : l2;
-        delta[to] = sum;
-        uint4* a = reinterpret_cast<uint4*>(aug + (to / 8) * 256 + to % 8 * 16);
-        a[0] = three_terms(none ? (scale_log2 > 0.f ? -1e30f : 1e30f) : -l2 / scale_log2);
-        a[8] = three_terms(-sum);
+    float mine = 0.f;           // delta of row row0 + lane % 8
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float sum = 0.f;
+        const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162*>(&a[i]), *y = reinterpret_cast<const __nv_bfloat162*>(&b[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 u = __bfloat1622float2(x[e]), v = __bfloat1622float2(y[e]);
+            sum = fmaf(u.x, v.x, fmaf(u.y, v.y, sum));
+        }
+#pragma unroll
+        for (int off = LANES / 2; off > 0; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        const int r = lane % 8;
+        const float from = __shfl_sync(0xffffffffu, sum, r % AT_ONCE * LANES);
+        if (r / AT_ONCE == i) mine = from;
+    }
+    if (lane >= 16) return;
+    const int row = row0 + lane % 8;
+    const float l = row < Tq ? lse[at * Tq + row] : -INFINITY, l2 = l * 1.4426950408889634f;
+    const bool none = l == -INFINITY;
+    uint4* terms = reinterpret_cast<uint4*>(aug + (at * Tpad + row0) * 32);
+    if (lane < 8) {
+        lse2[at * Tpad + row] = none ? INFINITY : l2;
+        delta[at * Tpad + row] = mine;
+        terms[lane] = three_terms(none ? (scale_log2 > 0.f ? -1e30f : 1e30f) : -l2 / scale_log2);
+    } else {
+        terms[lane] = three_terms(-mine);
     }
 }
 
@@ -691,7 +705,7 @@ int backward(const Args& a, cudaStream_t st) {
     const float by_keys_scale = std::fabs(scale_log2) >= kLeastScale ? scale_log2 : scale_log2 < 0.f ? -kLeastScale : kLeastScale;
     {
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(unsigned((rows + 7) / 8));
+        cfg.gridDim = dim3(unsigned((rows / 8 + 7) / 8));
         cfg.blockDim = dim3(256);
         cfg.stream = st;
         cudaLaunchAttribute attr;
@@ -702,11 +716,15 @@ int backward(const Args& a, cudaStream_t st) {
         const int e = int(cudaLaunchKernelEx(&cfg, stats_kernel<D>, a.dout, a.out, a.lse, lse2, delta, aug, by_keys_scale, a.Tq, Tpad, a.Hq, rows));
         if (e != 0) return e;
     }
+    // (a map of 128 rows serves as the fixed operand's and as the blocks')
     CUtensorMap fixed_k, fixed_v, fixed_q, fixed_o, block_k, block_v, block_q, block_o;
-    if (!decoder::operand_map(&fixed_k, a.k, D, a.Tk, a.Hkv, a.B, kRows) || !decoder::operand_map(&fixed_v, a.v, D, a.Tk, a.Hkv, a.B, kRows) ||
-        !decoder::operand_map(&fixed_q, a.q, D, a.Tq, a.Hq, a.B, kRows) || !decoder::operand_map(&fixed_o, a.dout, D, a.Tq, a.Hq, a.B, kRows) ||
-        !decoder::operand_map(&block_k, a.k, D, a.Tk, a.Hkv, a.B, BX) || !decoder::operand_map(&block_v, a.v, D, a.Tk, a.Hkv, a.B, BX) ||
-        !decoder::operand_map(&block_q, a.q, D, a.Tq, a.Hq, a.B, BXK) || !decoder::operand_map(&block_o, a.dout, D, a.Tq, a.Hq, a.B, BXK))
+    auto maps = [&](CUtensorMap* fixed, CUtensorMap* block, const Operand& o, int T, int H, int rows) {
+        if (!decoder::operand_map(fixed, o, D, T, H, a.B, kRows)) return false;
+        *block = *fixed;
+        return rows == kRows || decoder::operand_map(block, o, D, T, H, a.B, rows);
+    };
+    if (!maps(&fixed_k, &block_k, a.k, a.Tk, a.Hkv, BX) || !maps(&fixed_v, &block_v, a.v, a.Tk, a.Hkv, BX) ||
+        !maps(&fixed_q, &block_q, a.q, a.Tq, a.Hq, BXK) || !maps(&fixed_o, &block_o, a.dout, a.Tq, a.Hq, BXK))
         return int(cudaErrorInvalidValue);
     GradParams p{};
     p.lse2 = lse2;
