@@ -6,7 +6,7 @@
 //   distillation   the divergence of p from a teacher's K alternatives, and its
 //                  gradient with respect to x
 //
-// A row is shared by a cluster of 1 to 8 CTAs, which trade their parts through
+// A row is shared by a cluster of 1 to 16 CTAs, which trade their parts through
 // distributed shared memory: no workspace, no second launch, and sums in a
 // fixed order.  Both are bound by HBM: the scores read x once, the
 // distillation reads it once and writes the gradient once.
@@ -31,7 +31,13 @@ namespace {
 using decoder::bulk_load;
 using decoder::ex2;
 
-constexpr int kMaxTop = 128, kMaxCluster = 8;
+constexpr int kMaxTop = 128, kMaxCluster = 16, kMaxWarps = 16;
+#ifndef SCORE_CTAS
+#define SCORE_CTAS 512
+#endif
+#ifndef DISTILL_KB
+#define DISTILL_KB 80
+#endif
 constexpr unsigned kErrRow = 256;
 constexpr float kNone = -INFINITY;
 constexpr double kLog2e = 1.4426950408889634;
@@ -77,18 +83,6 @@ struct Row {
 struct Sums {
     float m, s, t;
 
-    __device__ __forceinline__ void rise(float to, float c) {
-        if (to > m) {
-            shift(to, c);
-            m = to;
-        }
-    }
-    // (m at least x already; ref: m, or 0 while m is -inf)
-    __device__ __forceinline__ void add(float x, float ref, float c) {
-        const float by = x - ref, e = ex2(by * c);
-        s += e;
-        t = fmaf(e, fmaxf(by, -3.0e38f), t);
-    }
     __device__ __forceinline__ void join(const Sums& o, float c) {
         const float to = fmaxf(m, o.m);
         Sums a = *this, b = o;
@@ -112,6 +106,52 @@ struct Sums {
         return o;
     }
 };
+
+// A lane's sums, of the even and of the odd elements of its words.
+struct LaneSums {
+    float m = kNone;
+    float2 s = {0.f, 0.f}, t = {0.f, 0.f};
+
+    // `most`: the largest of the elements that follow
+    __device__ __forceinline__ void rise(float most, float c) {
+        if (most > m) {
+            if (m != kNone) {
+                const float by = m - most, f = ex2(by * c);
+                t.x = f == 0.f ? 0.f : f * fmaf(by, s.x, t.x);
+                t.y = f == 0.f ? 0.f : f * fmaf(by, s.y, t.y);
+                s.x *= f;
+                s.y *= f;
+            }
+            m = most;
+        }
+    }
+    __device__ __forceinline__ float2 minus_ref() const {
+        const float r = m == kNone ? 0.f : -m;
+        return make_float2(r, r);
+    }
+    template <bool WITH_T>
+    __device__ __forceinline__ void add(float2 x, float2 minus, float2 c) {
+        const float2 by = __fadd2_rn(x, minus), y = __fmul2_rn(by, c), e = make_float2(ex2(y.x), ex2(y.y));
+        s = __fadd2_rn(s, e);
+        // (0 times -inf is not wanted)
+        if constexpr (WITH_T) t = __ffma2_rn(e, make_float2(fmaxf(by.x, -3.0e38f), fmaxf(by.y, -3.0e38f)), t);
+    }
+    __device__ __forceinline__ Sums both() const { return Sums{m, s.x + s.y, t.x + t.y}; }
+};
+
+template <class T>
+__device__ __forceinline__ float largest(const Word<T>& w) {
+    float m = to_float(w.x[0]);
+#pragma unroll
+    for (int e = 1; e < Word<T>::N; ++e) m = fmaxf(m, to_float(w.x[e]));
+    return m;
+}
+
+template <bool WITH_T, class T>
+__device__ __forceinline__ void add_word(LaneSums& sums, const Word<T>& w, float2 minus, float2 c) {
+#pragma unroll
+    for (int e = 0; e < Word<T>::N; e += 2) sums.add<WITH_T>(make_float2(to_float(w.x[e]), to_float(w.x[e + 1])), minus, c);
+}
 
 // ---- the K largest ----
 //
@@ -224,176 +264,189 @@ struct ScoreParams {
     int64_t* ids;
 };
 
-// A warp looks at 512 elements at a time, 16 to a lane (256 for R = 4, for its
-// buffer's sake).  The softmax sums are
-// a lane's own, with its own running maximum.  For the K largest, the elements
-// above a bound go to the warp's buffer, and from there, 32 R sorted at a time,
-// into its sorted list.  The bound is the larger of the list's K-th and what
-// the CTA's warps know together: each has ceil(K / warps) lanes whose largest
-// elements are at least so and so large, so the least of those is no larger
-// than the K-th of all.  That is read and brought up to date after 1, 2, 4,
-// ... looks, and without it (each warp by its list alone) most looks of a warp
-// find candidates.
-// The bound stays as it is during a look, and looks go up the row, so an
-// element that equals the list's K-th comes behind it.
-template <class T, int R, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS) score_kernel(const ScoreParams P) {
-    constexpr int N = Word<T>::N, U = (R == 4 ? 8 : 16) / N;
-    constexpr int CAP = 32 * R + 32 * U * N;      // (what a flush leaves, and a look's)
+// The CTA looks at four words of each lane at a time (two for R = 4, for the
+// buffers' sake).  The softmax sums are a lane's own, with its own running
+// maximum.  For the K largest, a lane puts the places of its elements above a
+// bound into the warp's buffer (in any order), and from there they go, 32 R
+// sorted at a time, into the warp's sorted list.  The bound is the larger of
+// the list's K-th and what the CTA's warps know together: each has ceil(K /
+// warps) lanes whose largest elements are at least so and so large, so the least
+// of those is no larger than the K-th of all.  That is brought up to date after
+// 1, 2, 4, ... looks; without it, each warp by its own list, most looks of a
+// warp found candidates.  The bound stays as it is during a look, and a warp's
+// looks go up the row, so an element that equals the list's K-th comes behind it.
+template <class T, int R>
+struct ScoreShape {
+    static constexpr int N = Word<T>::N, U = R == 4 ? 2 : 4;
+    // of a buffer: what a flush leaves, and a look's (a list fits in, at the end)
+    static constexpr int CAP = 32 * R + 32 * U * N;
+    static_assert(CAP >= 2 * 32 * R);
+    static size_t smem(int warps, int cluster) { return R ? size_t(warps * CAP) * 4 + size_t(cluster) * 32 * R * sizeof(Key) : 0; }
+};
+
+template <class T, int R>
+__global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams P) {
+    using Shape = ScoreShape<T, R>;
+    constexpr int N = Shape::N, U = Shape::U, CAP = Shape::CAP;
     constexpr bool TOP = R > 0;
     constexpr int RR = TOP ? R : 1;
-    __shared__ Sums s_sums[WARPS], s_cta[kMaxCluster];
-    __shared__ Key s_keys[TOP ? WARPS * CAP : 1], s_lists[TOP ? kMaxCluster * 32 * RR : 1];
-    __shared__ volatile float s_known[WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    extern __shared__ __align__(16) int s_places[];
+    __shared__ Sums s_sums[kMaxWarps], s_cta[kMaxCluster];
+    __shared__ volatile float s_known[kMaxWarps];
+    __shared__ int s_held[kMaxWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = int(blockDim.x) >> 5;
+    Key *s_keys = reinterpret_cast<Key*>(s_places), *s_lists = s_keys + warps * CAP / 2;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
     const long row = long(blockIdx.x) / C;
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    if (lane == 0) s_held[warp] = 0;
+    __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
     const int w0 = int(long(in.words) * rank / C), w1 = int(long(in.words) * (rank + 1) / C);
     const float c = P.c;
-    Sums sums{kNone, 0.f, 0.f};
+    const float2 c2 = make_float2(c, c);
+    LaneSums sums;
     Keys<RR> list;
 #pragma unroll
     for (int r = 0; r < RR; ++r) list.k[r] = 0;
-    Key* buf = s_keys + warp * CAP;
-    int held = 0;
+    int* buf = s_places + warp * CAP;
     float bound = kNone, own = kNone;
-    const int share = TOP ? (P.K + WARPS - 1) / WARPS : 1;
+    // the warps whose every lane has elements, and the lanes of each that the
+    // bound goes by (more than there are: no bound)
+    const int full = min(warps, (w1 - w0) / 32), share = full > 0 ? (P.K + full - 1) / full : 33;
 
     auto offer = [&](float x, int i) {
-        const bool in_it = x > bound;
-        const unsigned who = __ballot_sync(0xffffffffu, in_it);
-        if (in_it) buf[held + __popc(who & ((1u << lane) - 1u))] = make_key(x, i);
-        held += __popc(who);
+        if (x > bound) buf[atomicAdd(&s_held[warp], 1)] = i;
     };
     // the buffer's last 32 R into the list, until no more than `left` are in it
     auto flush = [&](int left) {
+        __syncwarp();
+        int held = *const_cast<volatile int*>(&s_held[warp]);
+        if (held <= left) return;
         while (held > left) {
             Keys<RR> batch;
             const int from = max(0, held - 32 * RR);
-            __syncwarp();
 #pragma unroll
-            for (int r = 0; r < RR; ++r) batch.k[r] = from + r * 32 + lane < held ? buf[from + r * 32 + lane] : 0;
-            __syncwarp();
+            for (int r = 0; r < RR; ++r) {
+                const int b = from + r * 32 + lane, i = b < held ? buf[b] : -1;
+                batch.k[r] = i >= 0 ? make_key(to_float(in.x[i]), i) : 0;
+            }
             held = from;
             batch.sort(lane);
             list.merge(batch, lane);
         }
         own = key_value(list.nth(P.K - 1));
+        if (lane == 0) s_held[warp] = held;
+        __syncwarp();
+    };
+    // elements that are not in words: before the first, behind the last
+    auto single = [&](int i, bool is) {
+        const float x = is ? to_float(in.x[i]) : kNone;
+        sums.rise(x, c);
+        if (is) sums.add<true>(make_float2(x, kNone), sums.minus_ref(), c2);
+        if constexpr (TOP) {
+            if (is) offer(x, i);
+        }
     };
 
-    // the elements before the first word
-    if (rank == 0 && warp == 0) {
-        const float x = lane < in.head ? to_float(in.x[lane]) : kNone;
-        sums.rise(x, c);
-        if (lane < in.head) sums.add(x, sums.m == kNone ? 0.f : sums.m, c);
-        if constexpr (TOP) offer(x, lane);
-    }
+    if (rank == 0 && warp == 0) single(lane, lane < in.head);
     const Word<T>* body = in.body();
     int look = 0;
-    for (int base = w0 + warp * 32 * U; base < w1 || look == 0; base += WARPS * 32 * U, ++look) {
+    for (int base = w0; base < w1 || look == 0; base += 32 * warps * U, ++look) {
         Word<T> words[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int w = base + u * 32 + lane;
+            const int w = base + u * 32 * warps + int(threadIdx.x);
             if (w < w1) words[u] = body[w];
             else
 #pragma unroll
                 for (int e = 0; e < N; ++e) words[u].x[e] = from_float<T>(kNone);
         }
-        float most = kNone;
+        float top[U], most = kNone;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < N; ++e) most = fmaxf(most, to_float(words[u].x[e]));
+        for (int u = 0; u < U; ++u) most = fmaxf(most, top[u] = largest(words[u]));
         sums.rise(most, c);
-        const float ref = sums.m == kNone ? 0.f : sums.m;
+        const float2 minus = sums.minus_ref();
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < N; ++e) sums.add(to_float(words[u].x[e]), ref, c);
+        for (int u = 0; u < U; ++u) add_word<true>(sums, words[u], minus, c2);
         if constexpr (TOP) {
-            if ((look & (look + 1)) == 0) {
+            if ((look & (look + 1)) == 0 && share <= 32) {
                 const float mine = nth_of_lanes(sums.m, share, lane);
                 if (lane == 0) s_known[warp] = mine;
                 if (look == 0) __syncthreads();
-                float least = s_known[lane % WARPS];
+                float least = lane < full ? s_known[lane] : INFINITY;
 #pragma unroll
-                for (int off = WARPS / 2; off > 0; off /= 2) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
-                bound = below(least);
+                for (int off = kMaxWarps / 2; off > 0; off /= 2) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
+                bound = below(__shfl_sync(0xffffffffu, least, 0));
             }
             bound = fmaxf(bound, own);
             if (__any_sync(0xffffffffu, most > bound)) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
+                    if (top[u] > bound) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) offer(to_float(words[u].x[e]), in.at(base + u * 32 + lane) + e);
-                if (held >= 32 * RR) flush(32 * RR - 1);
+                        for (int e = 0; e < N; ++e) offer(to_float(words[u].x[e]), in.at(base + u * 32 * warps + int(threadIdx.x)) + e);
+                    }
+                }
+                flush(32 * RR - 1);
             }
         }
     }
-    // and those behind the last
     if (rank == C - 1 && warp == 0) {
-        const int i = P.V - in.tail + lane;
-        const float x = lane < in.tail ? to_float(in.x[i]) : kNone;
-        sums.rise(x, c);
-        if (lane < in.tail) sums.add(x, sums.m == kNone ? 0.f : sums.m, c);
-        if constexpr (TOP) {
-            bound = fmaxf(bound, own);
-            offer(x, i);
-        }
+        bound = fmaxf(bound, own);
+        single(P.V - in.tail + lane, lane < in.tail);
     }
 
     // lanes, warps, CTAs
+    Sums mine = sums.both();
 #pragma unroll
-    for (int off = 16; off > 0; off /= 2) sums.join(sums.from(off), c);
-    if (lane == 0) s_sums[warp] = sums;
+    for (int off = 16; off > 0; off /= 2) mine.join(mine.from(off), c);
+    if (lane == 0) s_sums[warp] = mine;
+    // the lists of a power of two of places, pairs at a time
+    auto merge_all = [&](Key* at, int step, int n) {
+        for (int half = n / 2; half > 0; half /= 2) {
+            __syncthreads();
+            if (warp < half) {
+                Keys<RR> o;
+                o.get(at + (warp + half) * step, lane);
+                list.merge(o, lane);
+                if (half > 1) list.put(at + warp * step, lane);
+            }
+        }
+    };
     if constexpr (TOP) {
         flush(0);
         __syncwarp();
-        list.put(buf, lane);
+        list.put(s_keys + warp * (CAP / 2), lane);
+        merge_all(s_keys, CAP / 2, warps);
     }
     __syncthreads();
-    if constexpr (TOP) {
-#pragma unroll
-        for (int half = WARPS / 2; half > 0; half /= 2) {
-            if (warp < half) {
-                Keys<RR> o;
-                o.get(s_keys + (warp + half) * CAP, lane);
-                list.merge(o, lane);
-                if (half > 1) list.put(buf, lane);
-            }
-            if (half > 1) __syncthreads();
-        }
-    }
     if (C > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
         if (warp == 0) {
             if (lane == 0) {
                 Sums all = s_sums[0];
-                for (int w = 1; w < WARPS; ++w) all.join(s_sums[w], c);
+                for (int w = 1; w < warps; ++w) all.join(s_sums[w], c);
                 *cluster.map_shared_rank(&s_cta[rank], 0) = all;
             }
             if constexpr (TOP) list.put(cluster.map_shared_rank(s_lists + rank * 32 * RR, 0), lane);
         }
         cluster.sync();
         if (rank != 0) return;
-    }
-    if (warp != 0) return;
-    Sums all = C > 1 ? s_cta[0] : s_sums[0];
-    for (int i = 1; i < (C > 1 ? C : WARPS); ++i) all.join(C > 1 ? s_cta[i] : s_sums[i], c);
-    if constexpr (TOP) {
-        for (int i = 1; i < C; ++i) {
-            Keys<RR> o;
-            o.get(s_lists + i * 32 * RR, lane);
-            list.merge(o, lane);
+        if constexpr (TOP) {
+            if (warp < C) list.get(s_lists + warp * 32 * RR, lane);
+            merge_all(s_lists, 32 * RR, C);
         }
     }
+    if (warp != 0) return;
+    const int parts = C > 1 ? C : warps;
+    Sums all = lane < parts ? (C > 1 ? s_cta[lane] : s_sums[lane]) : Sums{kNone, 0.f, 0.f};
+#pragma unroll
+    for (int off = 16; off > 0; off /= 2) all.join(all.from(off), c);
     const bool empty = all.m == kNone && !(all.s != all.s);
     const float log_s = logf(all.s);
     auto logprob = [&](float x) { return empty ? kNone : (x - all.m) * P.inv_T - log_s; };
@@ -432,7 +485,7 @@ __global__ void __launch_bounds__(32 * WARPS) score_kernel(const ScoreParams P) 
 
 // ---- distillation ----
 
-constexpr int kParts = 8;             // pieces that a CTA's slice arrives in
+constexpr int kPieces = 4;            // copies that a CTA's slice arrives in
 constexpr int kDistillThreads = 256;
 
 struct DistillParams {
@@ -440,6 +493,7 @@ struct DistillParams {
     long stride;
     int V, K, rest;
     float inv_T, c, c_low;      // 1 / T; log2(e) / T, and what its rounding left
+    float least;                // -160 / c
     const int64_t* ids;
     const float* teacher;
     const float* weight;        // or NULL
@@ -448,65 +502,58 @@ struct DistillParams {
     unsigned* err;
 };
 
-// Sums a value of each thread, or takes the largest, in a fixed order.
-template <class V, class Op>
-__device__ __forceinline__ V over_block(V v, Op op, V* s) {
-#pragma unroll
-    for (int off = 16; off > 0; off /= 2) v = op(v, __shfl_xor_sync(0xffffffffu, v, off));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = s[0];
-#pragma unroll
-    for (int w = 1; w < kDistillThreads / 32; ++w) v = op(v, s[w]);
-    __syncthreads();
-    return v;
-}
-
-// e^(by / T) of a difference of logits, for a gradient of type T.  In fp32 with
-// the exponent's rounding made good, which 30 below the maximum costs 1e-6 of
-// the value (5 instructions of a pass that waits for memory).
+// k e^((x - ref) / T) of two logits, for a gradient of type T.  In fp32 with the
+// exponent's rounding made good, which 30 below the maximum costs 1e-6 of the
+// value.
 template <class T>
-__device__ __forceinline__ float weight_of(float by, const DistillParams& P) {
-    if constexpr (sizeof(T) < 4) return ex2(by * P.c);
-    const float y = by * P.c, e = ex2(y);
-    const float low = fmaf(by, P.c_low, fmaf(by, P.c, -y));
-    return y < -150.f ? 0.f : fmaf(e, low * 0.69314718f, e);
+__device__ __forceinline__ float2 weights_of(float2 x, float ref, float k, const DistillParams& P) {
+    float2 by = __fadd2_rn(x, make_float2(-ref, -ref));
+    if constexpr (sizeof(T) < 4) {
+        const float2 y = __fmul2_rn(by, make_float2(P.c, P.c));
+        return __fmul2_rn(make_float2(ex2(y.x), ex2(y.y)), make_float2(k, k));
+    } else {
+        // (as good as none from 2^-160 on; a NaN's row has a k of NaN)
+        by = make_float2(fmaxf(by.x, P.least), fmaxf(by.y, P.least));
+        const float2 y = __fmul2_rn(by, make_float2(P.c, P.c)), minus_y = make_float2(-y.x, -y.y);
+        const float2 e = __fmul2_rn(make_float2(ex2(y.x), ex2(y.y)), make_float2(k, k));
+        const float2 low = __ffma2_rn(by, make_float2(P.c_low, P.c_low), __ffma2_rn(by, make_float2(P.c, P.c), minus_y));
+        return __ffma2_rn(e, __fmul2_rn(low, make_float2(0.69314718f, 0.69314718f)), e);
+    }
 }
 
-// A CTA's slice of the row comes into shared memory by bulk copies, all asked
-// for at the start, and stays there: the sums are taken piece by piece as they
-// land, and once the cluster has the row's, the gradient is made from the same
-// copy.  The teacher's tokens are taken out of the slice (-inf) before it is
-// summed up and put in their own way, so the sum of all others is a sum and not
-// a difference.
+// A CTA's slice of the row comes into shared memory by bulk copies and stays
+// there: the sums are taken from it, and once the cluster has the row's, the
+// gradient is made from the same copy.  The teacher's tokens are taken out of the
+// slice (-inf) before it is summed up and put in their own way, so the sum of all
+// others is a sum and not a difference.  Everything that needs the teacher alone
+// is done under the copies; the CTAs of other rows on the SM fill the waits.
 template <class T>
 __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams P) {
     constexpr int N = Word<T>::N;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[kParts];
-    __shared__ float2 s_cta[kMaxCluster];
-    __shared__ int64_t s_id[kMaxTop];
-    __shared__ float s_q[kMaxTop], s_f[kDistillThreads / 32];
-    __shared__ double s_d[kDistillThreads / 32];
+    __shared__ __align__(8) uint64_t s_bar;
+    __shared__ float2 s_warps[kDistillThreads / 32], s_cta[kMaxCluster];       // largest x, sum of the others' e^
+    __shared__ __align__(16) int s_id[kMaxTop];
+    __shared__ float s_q[kMaxTop];
+    __shared__ float2 s_ids;                // the same of the teacher's tokens
+    __shared__ float s_all[2];              // the teacher's sum, and its rest
     __shared__ volatile int s_abort;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
     const long row = long(blockIdx.x) / C;
-    const uint32_t bar0 = tc::smem_u32(bars);
+    const uint32_t bar = tc::smem_u32(&s_bar);
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (tid == 0) {
-        for (int i = 0; i < kParts; ++i) tc::mbar_init(bar0 + 8u * i, 1);
+        tc::mbar_init(bar, 1);
         s_abort = 0;
         tc::fence_mbar_init();
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __syncthreads();
 
     const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
     const int w0 = int(long(in.words) * rank / C), nw = int(long(in.words) * (rank + 1) / C) - w0;
-    const int per = (nw + kParts - 1) / kParts;              // words of a piece
     const float c = P.c, weight = P.weight ? P.weight[row] : 1.f;
     // the slice's edge elements, one to a thread: those before the row's first
     // word, those behind its last
@@ -532,134 +579,191 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
         if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         return;
     }
-    if (tid == 0) {
-        for (int i = 0; i < kParts; ++i) {
-            const int n = min(per, nw - i * per);
-            if (n <= 0) break;
-            tc::mbar_arrive_expect_tx(bar0 + 8u * i, uint32_t(n) * 16u);
-            bulk_load(tc::smem_u32(slice + i * per), in.body() + w0 + i * per, uint32_t(n) * 16u, bar0 + 8u * i);
+    if (tid == 0) {              // (it has made the barrier itself)
+        tc::mbar_arrive_expect_tx(bar, uint32_t(nw) * 16u);
+        for (int i = 0; i < kPieces; ++i) {
+            const int lo = int(long(nw) * i / kPieces), n = int(long(nw) * (i + 1) / kPieces) - lo;
+            if (n > 0) bulk_load(tc::smem_u32(slice + lo), in.body() + w0 + lo, uint32_t(n) * 16u, bar);
         }
     }
 
-    // the teacher's tokens
-    int64_t id = -1;
-    float q = 0.f, z = kNone;           // (z: x, before the temperature)
-    bool poison = false;
-    if (tid < P.K) {
-        id = P.ids[row * P.K + tid];
-        q = P.teacher[row * P.K + tid];
-        poison = id >= P.V;
-        if (id >= P.V) id = -1;
-        if (id >= 0) z = to_float(in.x[id]);
-        s_id[tid] = id;
+    // The teacher is warp 0's, four alternatives to a lane: tokens, their logits,
+    // weights, and what they add to the sums.
+    constexpr int J = kMaxTop / 32;
+    const int first_word = in.at(w0);
+    int id[J];
+    float q[J], z[J];
+    bool lead[J];                       // a token's first mention
+    if (warp == 0) {
+        bool poison = false;
+        float top = kNone, top_z = kNone;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int k = j * 32 + lane;
+            id[j] = -1;
+            q[j] = z[j] = kNone;
+            if (k < P.K) {
+                const int64_t asked = P.ids[row * P.K + k];
+                q[j] = P.teacher[row * P.K + k];
+                poison |= asked >= P.V;
+                if (asked >= 0 && asked < P.V) id[j] = int(asked);
+                if (id[j] >= 0) z[j] = to_float(in.x[id[j]]);
+                else q[j] = kNone;
+            }
+            s_id[k] = id[j];
+            top = fmaxf(top, q[j]);
+            top_z = fmaxf(top_z, z[j]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < J; ++j) lead[j] = id[j] >= 0;
+        for (int k = 0; k < P.K; k += 4) {
+            const int4 four = *reinterpret_cast<const int4*>(s_id + k);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int before = j * 32 + lane - k;      // how many of the four come before it
+                lead[j] = lead[j] && !((before > 0 && four.x == id[j]) || (before > 1 && four.y == id[j]) || (before > 2 && four.z == id[j]) ||
+                                       (before > 3 && four.w == id[j]));
+            }
+        }
+        poison = __any_sync(0xffffffffu, poison);
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            top_z = fmaxf(top_z, __shfl_xor_sync(0xffffffffu, top_z, off));
+        }
+        if (P.rest || top == kNone) top = 0.f;
+        float sum = 0.f, e = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            q[j] = expf(q[j] - top);
+            sum += q[j];
+            if (lead[j]) e += ex2((z[j] - (top_z == kNone ? 0.f : top_z)) * c);
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            e += __shfl_xor_sync(0xffffffffu, e, off);
+        }
+        // in fp64 what is left of 1 (NaN for a row with a token outside the vocabulary)
+        double q_all = 0.0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (!P.rest && sum != 0.f) q[j] /= sum;
+            if (poison) q[j] = NAN;
+            q_all += double(q[j]);
+            s_q[j * 32 + lane] = q[j];
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) q_all += __shfl_xor_sync(0xffffffffu, q_all, off);
+        if (lane == 0) {
+            s_ids = make_float2(top_z, e);
+            s_all[0] = float(q_all);
+            s_all[1] = P.rest ? float(1.0 - q_all > 0.0 || q_all != q_all ? 1.0 - q_all : 0.0) : 0.f;
+        }
+    }
+    float edge_x = edge >= 0 ? to_float(in.x[edge]) : kNone;
+    const bool landed = tc::mbar_wait(bar, 0, &s_abort, P.err, kErrRow);
+    if (warp == 0 && landed) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (id[j] >= first_word && id[j] < first_word + nw * N) flat[id[j] - first_word] = from_float<T>(kNone);
     }
     __syncthreads();
-    bool first = id >= 0;               // a token's first mention
-    for (int j = 0; first && j < tid; ++j) first = s_id[j] != id;
-    float edge_x = edge >= 0 ? to_float(in.x[edge]) : kNone;
     if (edge >= 0)
-        for (int j = 0; j < P.K; ++j)
-            if (s_id[j] == edge) edge_x = kNone;
-    const int place = id >= 0 ? int(id) - in.at(w0) : -1;     // in the slice's words
-    const bool here = place >= 0 && place < nw * N;
+        for (int k = 0; k < P.K; ++k)
+            if (s_id[k] == edge) edge_x = kNone;
 
     // the sum of all other tokens
-    Sums sums{kNone, 0.f, 0.f};
-    sums.rise(edge_x, c);
-    if (edge >= 0) sums.add(edge_x, sums.m == kNone ? 0.f : sums.m, c);
-    bool ok = true;
-    for (int i = 0; i < kParts && i * per < nw; ++i) {
-        const int lo = i * per, hi = min(nw, lo + per);
-        ok = ok && tc::mbar_wait(bar0 + 8u * i, 0, &s_abort, P.err, kErrRow);
-        if (here && ok && place >= lo * N && place < hi * N) flat[place] = from_float<T>(kNone);
-        __syncthreads();
-        for (int w = lo + tid; w < hi; w += kDistillThreads) {
-            const Word<T> v = slice[w];
-            float most = kNone;
-#pragma unroll
-            for (int e = 0; e < N; ++e) most = fmaxf(most, to_float(v.x[e]));
-            if (most > sums.m) {
-                if (sums.m != kNone) sums.s *= ex2((sums.m - most) * c);
-                sums.m = most;
-            }
-            const float ref = sums.m == kNone ? 0.f : sums.m;
-#pragma unroll
-            for (int e = 0; e < N; ++e) sums.s += ex2((to_float(v.x[e]) - ref) * c);
-        }
+    LaneSums sums;
+    const float2 c2 = make_float2(c, c);
+    if (edge >= 0) {
+        sums.rise(edge_x, c);
+        sums.add<false>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
     }
-    const float most = over_block(fmaxf(sums.m, z), [](float a, float b) { return fmaxf(a, b); }, s_f);
-    auto add = [](float a, float b) { return a + b; };
-    if (sums.m != kNone && sums.m != most) sums.s *= ex2((sums.m - most) * c);
-    float2 mine = make_float2(most, over_block(sums.s, add, s_f));
-    // over the cluster: every CTA gets every part
-    float m = mine.x, s_rest = mine.y;
-    if (C > 1) {
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
-        if (tid < C) *cluster.map_shared_rank(&s_cta[rank], tid) = mine;
-        cluster.sync();
-        for (int i = 0; i < C; ++i) m = fmaxf(m, s_cta[i].x);
-        s_rest = 0.f;
-        for (int i = 0; i < C; ++i) s_rest += s_cta[i].x == kNone || s_cta[i].x == m ? s_cta[i].y : s_cta[i].y * ex2((s_cta[i].x - m) * c);
+#pragma unroll 2
+    for (int w = tid; w < nw; w += kDistillThreads) {
+        const Word<T> v = slice[w];
+        sums.rise(largest(v), c);
+        add_word<false>(sums, v, sums.minus_ref(), c2);
     }
-    const float ref = m == kNone ? 0.f : m;
-    const float e_id = id >= 0 ? weight_of<T>(z - ref, P) : 0.f;
-    const float s_all = s_rest + over_block(first ? e_id : 0.f, add, s_f);
-
-    // the teacher's weights
-    const bool asked = id >= 0 && (q > kNone || q != q);
-    if (P.rest) {
-        q = asked ? expf(q) : 0.f;
-    } else {
-        const float top = over_block(asked ? q : kNone, [](float a, float b) { return fmaxf(a, b); }, s_f);
-        q = asked ? expf(q - top) : 0.f;
-        const float sum = over_block(q, add, s_f);
-        if (asked) q /= sum;
+    // of sums with their largest x, over `n` lanes (-inf: a sum of 0, or NaN)
+    auto together = [&](float2 v, int n) {
+        float m = v.x;
+        for (int off = n / 2; off > 0; off /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        if (v.x != kNone && v.x != m) v.y *= ex2((v.x - m) * c);
+        for (int off = n / 2; off > 0; off /= 2) v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
+        return make_float2(m, v.y);
+    };
+    const float2 mine = together(make_float2(sums.m, sums.s.x + sums.s.y), 32);
+    if (lane == 0) s_warps[warp] = mine;
+    if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
+    __syncthreads();
+    // to every CTA of the cluster
+    if (warp == 0) {
+        const float2 part = together(lane < kDistillThreads / 32 ? s_warps[lane] : make_float2(kNone, 0.f), 32);
+        if (lane < C) *cluster.map_shared_rank(&s_cta[rank], lane) = part;
     }
-    if (poison) q = NAN;
-    if (tid < P.K) s_q[tid] = q;
-    auto add_d = [](double a, double b) { return a + b; };
-    // (NaN for a row with a token outside the vocabulary)
-    const double q_all = over_block(double(q), add_d, s_d);
-    const float q_rest = P.rest ? float(1.0 - q_all > 0.0 || q_all != q_all ? 1.0 - q_all : 0.0) : 0.f;
-    // p_j = e_j / s_all; the gradient of a token that is not the teacher's is
+    if (C > 1) cluster.sync();
+    else __syncthreads();
+    const float2 others = together(lane < C ? s_cta[lane] : make_float2(kNone, 0.f), 32), ids = s_ids;
+    const float m = fmaxf(others.x, ids.x), ref = m == kNone ? 0.f : m;
+    const float s_rest = others.x == kNone ? others.y : others.y * ex2((others.x - ref) * c);
+    const float s_all_ids = ids.x == kNone ? ids.y : ids.y * ex2((ids.x - ref) * c), s_sum = s_rest + s_all_ids;
+    // p_j = e_j / s_sum; the gradient of a token that is not the teacher's is
     // f p_j, of one that is (all p_j - q_j)
-    const float all = P.rest ? 1.f : float(q_all), inv_s = s_all == 0.f ? 0.f : 1.f / s_all;
-    const float f = !P.rest ? all : s_rest == 0.f ? 1.f : 1.f - q_rest * s_all / s_rest;
+    const float q_rest = s_all[1], all = P.rest ? 1.f : s_all[0], inv_s = s_sum == 0.f ? 0.f : 1.f / s_sum;
+    const float f = !P.rest ? all : s_rest == 0.f ? 1.f : 1.f - q_rest * s_sum / s_rest;
 
-    if (rank == 0) {
-        // in fp64: the terms are small differences of log probabilities
-        const double log_s = s_all == 0.f ? 0.0 : log(double(s_all));
-        double term = 0.0;
-        if (q != 0.f && tid < P.K)
-            term = double(q) * (log(double(q)) - (s_all == 0.f ? -INFINITY : (double(z) - double(ref)) * double(P.inv_T) - log_s));
-        double total = over_block(term, add_d, s_d);
-        if (tid == 0) {
-            if (q_rest > 0.f) total += double(q_rest) * (log(double(q_rest)) - (log(double(s_rest)) - log_s));
-            P.loss[row] = float(total * double(weight));
-        }
-    }
     if (out) {
         const float scale = weight * P.inv_T, k = f * inv_s * scale;
-        const int lo = in.at(w0);
         if (words_out) {
+#pragma unroll 2
             for (int w = tid; w < nw; w += kDistillThreads) {
                 const Word<T> v = slice[w];
                 Word<T> g;
 #pragma unroll
-                for (int e = 0; e < N; ++e) g.x[e] = from_float<T>(weight_of<T>(to_float(v.x[e]) - ref, P) * k);
-                reinterpret_cast<Word<T>*>(out + lo)[w] = g;
+                for (int e = 0; e < N; e += 2) {
+                    const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), ref, k, P);
+                    g.x[e] = from_float<T>(two.x);
+                    g.x[e + 1] = from_float<T>(two.y);
+                }
+                reinterpret_cast<Word<T>*>(out + first_word)[w] = g;
             }
         } else {
-            for (int i = tid; i < nw * N; i += kDistillThreads) out[lo + i] = from_float<T>(weight_of<T>(to_float(flat[i]) - ref, P) * k);
+            for (int i = tid; i < nw * N; i += kDistillThreads)
+                out[first_word + i] = from_float<T>(weights_of<T>(make_float2(to_float(flat[i]), 0.f), ref, k, P).x);
         }
-        if (edge >= 0) out[edge] = from_float<T>(weight_of<T>(edge_x - ref, P) * k);
+        if (edge >= 0) out[edge] = from_float<T>(weights_of<T>(make_float2(edge_x, 0.f), ref, k, P).x);
         __syncthreads();
-        const bool on_edge = id >= 0 && ((rank == 0 && id < in.head) || (rank == C - 1 && id >= P.V - in.tail));
-        if (first && (here || on_edge)) {
-            float sum = 0.f;
-            for (int j = tid; j < P.K; ++j)
-                if (s_id[j] == id) sum += s_q[j];
-            out[id] = from_float<T>(scale * (all * e_id * inv_s - sum));
+        if (warp == 0) {
+            // the teacher's tokens, each by its first mention in the CTA that has it
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int i = id[j];
+                const bool here = (i >= first_word && i < first_word + nw * N) || (rank == 0 && i < in.head) || (rank == C - 1 && i >= P.V - in.tail);
+                if (!lead[j] || !here) continue;
+                float sum = 0.f;
+                for (int n = j * 32 + lane; n < P.K; ++n)
+                    if (s_id[n] == i) sum += s_q[n];
+                out[i] = from_float<T>(fmaf(scale * all, weights_of<T>(make_float2(z[j], 0.f), ref, inv_s, P).x, -scale * sum));
+            }
+        }
+    }
+    if (rank == 0 && warp == 0) {
+        // in fp64: the terms are small differences of log probabilities
+        const double log_s = s_sum == 0.f ? 0.0 : log(double(s_sum));
+        double total = 0.0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (q[j] != 0.f)
+                total += double(q[j]) * (log(double(q[j])) - (s_sum == 0.f ? -INFINITY : (double(z[j]) - double(ref)) * double(P.inv_T) - log_s));
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
+        if (lane == 0) {
+            if (q_rest > 0.f) total += double(q_rest) * (log(double(q_rest)) - (log(double(s_rest)) - log_s));
+            P.loss[row] = float(total * double(weight));
         }
     }
 }
@@ -682,22 +786,42 @@ int launch(Kernel kernel, long ctas, int threads, size_t smem, int cluster, cons
     return int(cudaLaunchKernelEx(&cfg, kernel, P));
 }
 
+// Clusters of more than 8 CTAs have to be allowed, and dynamic shared memory of
+// more than 48 KB.
+template <class Kernel>
+cudaError_t allow(splice::PerDevice<bool>& kept, Kernel kernel, size_t smem) {
+    bool set = false;
+    return kept.get(&set, [&](int, bool* done) {
+        *done = true;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        return e;
+    });
+}
+
 // CTAs that share a row: as many as fill the GPU, of 4096 elements at least.
 int score_cluster(long rows, long V) {
     int C = 1;
-    while (C < kMaxCluster && rows * C < 1216 && V >= 8192L * C) C *= 2;
+    while (C < kMaxCluster && rows * C < SCORE_CTAS && V >= 8192L * C) C *= 2;
     return C;
+}
+
+template <class T, int R>
+int scores(const ScoreParams& P, long rows, cudaStream_t st) {
+    using Shape = ScoreShape<T, R>;
+    static splice::PerDevice<bool> kept;
+    const cudaError_t e = allow(kept, score_kernel<T, R>, Shape::smem(kMaxWarps, kMaxCluster));
+    if (e != cudaSuccess) return int(e);
+    const int C = score_cluster(rows, P.V), warps = rows * C < 304 ? 16 : 8;
+    return launch(score_kernel<T, R>, rows * C, 32 * warps, Shape::smem(warps, C), C, P, st);
 }
 
 template <class T>
 int scores(const ScoreParams& P, long rows, cudaStream_t st) {
-    const int C = score_cluster(rows, P.V);
-    const long ctas = rows * C;
-    constexpr int W = 8;
-    if (P.K == 0) return launch(score_kernel<T, 0, W>, ctas, 32 * W, 0, C, P, st);
-    if (P.K <= 32) return launch(score_kernel<T, 1, W>, ctas, 32 * W, 0, C, P, st);
-    if (P.K <= 64) return launch(score_kernel<T, 2, W>, ctas, 32 * W, 0, C, P, st);
-    return launch(score_kernel<T, 4, W>, ctas, 32 * W, 0, C, P, st);
+    if (P.K == 0) return scores<T, 0>(P, rows, st);
+    if (P.K <= 32) return scores<T, 1>(P, rows, st);
+    if (P.K <= 64) return scores<T, 2>(P, rows, st);
+    return scores<T, 4>(P, rows, st);
 }
 
 // Bytes of a CTA's slice at the most.
@@ -707,7 +831,7 @@ size_t slice_bytes(long V, size_t size, int C) { return (size_t(V) * size / 16 /
 
 int distill_cluster(long rows, long V, size_t size) {
     int C = 1;
-    while (C < kMaxCluster && slice_bytes(V, size, C) > 56 * 1024) C *= 2;
+    while (C < kMaxCluster && slice_bytes(V, size, C) > DISTILL_KB * 1024) C *= 2;
     while (C < kMaxCluster && rows * C < 456 && V >= 8192L * C) C *= 2;
     return C;
 }
@@ -715,11 +839,7 @@ int distill_cluster(long rows, long V, size_t size) {
 template <class T>
 int distill(const DistillParams& P, long rows, cudaStream_t st) {
     static splice::PerDevice<bool> kept;
-    bool set = false;
-    const cudaError_t e = kept.get(&set, [](int, bool* done) {
-        *done = true;
-        return cudaFuncSetAttribute(distill_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSliceMax));
-    });
+    const cudaError_t e = allow(kept, distill_kernel<T>, kSliceMax);
     if (e != cudaSuccess) return int(e);
     const int C = distill_cluster(rows, P.V, sizeof(T));
     const size_t bytes = slice_bytes(P.V, sizeof(T), C);
@@ -747,8 +867,8 @@ int decoder_token_scores(const void* x, int dtype, long stride, long rows, long 
     return int(cudaErrorInvalidValue);
 }
 
-// The longest row that decoder_distill takes.
-long decoder_distill_vocab(int dtype) { return long((kSliceMax / 16 - 1) * kMaxCluster * (dtype == 0 ? 4 : 8)); }
+// The longest row that decoder_distill takes: what 8 CTAs hold.
+long decoder_distill_vocab(int dtype) { return long((kSliceMax / 16 - 1) * 8 * (dtype == 0 ? 4 : 8)); }
 
 // ids int64, teacher fp32 [rows][K]; weight fp32 [rows] or NULL; loss fp32
 // [rows]; grad [rows][V] contiguous, of the logits' type, or NULL.  Returns a
@@ -758,7 +878,7 @@ int decoder_distill(const void* x, int dtype, long stride, long rows, long V, co
     if (rows < 1 || rows > (1L << 27) || V < 1 || V > decoder_distill_vocab(dtype) || K < 1 || K > kMaxTop || !(inv_T > 0.0))
         return int(cudaErrorInvalidValue);
     const float c = float(inv_T * kLog2e);
-    const DistillParams P{x, stride, int(V), K, rest, float(inv_T), c, float(inv_T * kLog2e - double(c)), static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
+    const DistillParams P{x, stride, int(V), K, rest, float(inv_T), c, float(inv_T * kLog2e - double(c)), -160.f / c, static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
                           static_cast<const float*>(weight), static_cast<float*>(loss), grad, decoder::error_word()};
     if (!P.err) return int(cudaErrorInvalidValue);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
