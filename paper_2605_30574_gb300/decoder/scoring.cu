@@ -35,9 +35,6 @@ constexpr int kMaxTop = 128, kMaxCluster = 16, kMaxWarps = 16;
 #ifndef SCORE_CTAS
 #define SCORE_CTAS 512
 #endif
-#ifndef DISTILL_KB
-#define DISTILL_KB 80
-#endif
 constexpr unsigned kErrRow = 256;
 constexpr float kNone = -INFINITY;
 constexpr double kLog2e = 1.4426950408889634;
@@ -298,7 +295,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams
     Key *s_keys = reinterpret_cast<Key*>(s_places), *s_lists = s_keys + warps * CAP / 2;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
-    const long row = long(blockIdx.x) / C;
+    const int log2_C = __popc(C - 1);       // (C is a power of two)
+    const long row = blockIdx.x >> log2_C;
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (lane == 0) s_held[warp] = 0;
     __syncwarp();
@@ -306,7 +304,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
-    const int w0 = int(long(in.words) * rank / C), w1 = int(long(in.words) * (rank + 1) / C);
+    const int w0 = int(long(in.words) * rank >> log2_C), w1 = int(long(in.words) * (rank + 1) >> log2_C);
     const float c = P.c;
     const float2 c2 = make_float2(c, c);
     LaneSums sums;
@@ -485,14 +483,17 @@ __global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams
 
 // ---- distillation ----
 
-constexpr int kPieces = 4;            // copies that a CTA's slice arrives in
-constexpr int kDistillThreads = 256;
+constexpr int kPieces = 8;            // copies that a CTA's slice arrives in
+constexpr int kWorkers = 256, kDistillThreads = kWorkers + 32;
 
 struct DistillParams {
     const void* x;
     long stride;
+    long rows;
     int V, K, rest;
-    float inv_T, c, c_low;      // 1 / T; log2(e) / T, and what its rounding left
+    int piece;                  // words of a piece, of the longest slice
+    float inv_T, inv_T_low;     // 1 / T, and what its rounding left
+    float c, c_low;             // log2(e) / T, the same
     float least;                // -160 / c
     const int64_t* ids;
     const float* teacher;
@@ -521,255 +522,478 @@ __device__ __forceinline__ float2 weights_of(float2 x, float ref, float k, const
     }
 }
 
-// A CTA's slice of the row comes into shared memory by bulk copies and stays
-// there: the sums are taken from it, and once the cluster has the row's, the
-// gradient is made from the same copy.  The teacher's tokens are taken out of the
-// slice (-inf) before it is summed up and put in their own way, so the sum of all
-// others is a sum and not a difference.  Everything that needs the teacher alone
-// is done under the copies; the CTAs of other rows on the SM fill the waits.
-template <class T>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams P) {
-    constexpr int N = Word<T>::N;
+// A wait for arrivals of other CTAs of the cluster, and what they wrote before.
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err, unsigned code) {
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (uint32_t i = 1;; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((i & 63u) == 0) {
+            if (*abort) return false;
+            if (tc::globaltimer_ns() - t0 > 1000000000ull) {
+                *abort = 1;
+                atomicOr(err, code);
+                return false;
+            }
+        }
+    }
+}
+
+// Sums of two floats each: a pair's value is x + y, y the smaller.  (fp64, on this
+// part, takes 50 clocks an operation.)
+__device__ __forceinline__ float2 exact_sum(float a, float b) {            // Knuth's
+    const float s = __fadd_rn(a, b), t = __fadd_rn(s, -a);
+    return make_float2(s, __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -t)), __fadd_rn(b, -t)));
+}
+__device__ __forceinline__ float2 pair_sum(float2 a, float2 b) {
+    const float2 s = exact_sum(a.x, b.x);
+    return exact_sum(s.x, __fadd_rn(s.y, __fadd_rn(a.y, b.y)));
+}
+
+// log x as a pair, to 1e-9: 2 atanh(u) of u = (m - 1) / (m + 1), m the mantissa
+// between sqrt(1/2) and sqrt(2), by its series; u's first term and quotient's rest
+// exactly, the terms from u^3 on in fp32.
+__device__ __forceinline__ float2 log_pair(float x) {
+    if (!(x > 0.f)) return make_float2(x == 0.f ? -INFINITY : NAN, 0.f);
+    if (x > 3.4e38f) return make_float2(INFINITY, 0.f);
+    const bool small = x < 1.2e-38f;
+    if (small) x *= 18446744073709551616.f;         // 2^64
+    const int b = __float_as_int(x);
+    int e = (b >> 23) - 127 - (small ? 64 : 0);
+    float m = __int_as_float((b & 0x7fffff) | 0x3f800000);
+    if (m > 1.41421356f) {
+        m *= 0.5f;
+        ++e;
+    }
+    const float num = m - 1.f;                      // (exact)
+    const float2 den = exact_sum(m, 1.f);
+    const float u = num / den.x, rest = __fadd_rn(fmaf(-u, den.x, num), -u * den.y) / den.x, v = u * u;
+    float p = 1.f / 13.f;
+    p = fmaf(p, v, 1.f / 11.f);
+    p = fmaf(p, v, 1.f / 9.f);
+    p = fmaf(p, v, 1.f / 7.f);
+    p = fmaf(p, v, 1.f / 5.f);
+    p = fmaf(p, v, 1.f / 3.f);
+    // (ln 2 in two: e times the first is exact)
+    const float2 whole = exact_sum(float(e) * 0.693145752f, 2.f * u);
+    return exact_sum(whole.x, __fadd_rn(whole.y, fmaf(float(e), 1.42860677e-6f, fmaf(2.f * u * v, p, 2.f * rest))));
+}
+
+// What warp kWorkers / 32 makes of a row's teacher before the row is taken.
+struct Teacher {
+    alignas(16) int id[kMaxTop];        // -1: none
+    float q[kMaxTop], z[kMaxTop];       // probabilities; logits, before the temperature
+    float log_q[kMaxTop];               // and log q, less `shift`
+    float sum[kMaxTop];                 // of all mentions of the token, at its first; -1: not the first
+    float most, e;                      // the tokens' largest logit, and sum of e^(z - most)
+    float all, rest;                    // the teacher's sum, and what is left of 1
+    float norm;                         // shift is log(norm)
+    unsigned edges;                     // which of the first 8 elements, and of the 8 before the last word's end, are the teacher's
+};
+
+__device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
+
+// Clusters stay and take row after row.  A CTA's slice of a row comes into shared
+// memory by bulk copies: the sums are taken from it, and once the cluster has the
+// row's, the gradient is made from the same copy.  As soon as a piece of it has
+// been used for the last time, that piece of the next row is asked for in its
+// place; and the warp behind the workers' reads the next row's teacher.  So the
+// copies go on under the gradient, and with two CTAs to an SM under the other's
+// exchange.  (A cluster for each row, gone when it was done: 1.7 times as long.)
+//
+// The teacher's tokens are taken out of the slice (-inf) before it is summed up
+// and put in their own way, so the sum of all others is a sum and not a
+// difference.
+template <class T, bool GRAD>
+__global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams P) {
+    constexpr int N = Word<T>::N, J = kMaxTop / 32;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t s_bar;
-    __shared__ float2 s_warps[kDistillThreads / 32], s_cta[kMaxCluster];       // largest x, sum of the others' e^
-    __shared__ __align__(16) int s_id[kMaxTop];
-    __shared__ float s_q[kMaxTop];
-    __shared__ float2 s_ids;                // the same of the teacher's tokens
-    __shared__ float s_all[2];              // the teacher's sum, and its rest
+    __shared__ __align__(8) uint64_t bars[kPieces + 2];
+    __shared__ Teacher s_teacher[2];
+    __shared__ float2 s_warps[kWorkers / 32], s_cta[2][kMaxCluster];       // largest x, sum of the others' e^
     __shared__ volatile int s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
-    const long row = long(blockIdx.x) / C;
-    const uint32_t bar = tc::smem_u32(&s_bar);
-    if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const int log2_C = __popc(C - 1);       // (C is a power of two)
+    const long row0 = blockIdx.x >> log2_C, step = gridDim.x >> log2_C;
+    const uint32_t bar0 = tc::smem_u32(bars);
+    const Word<T>* slice = reinterpret_cast<const Word<T>*>(smem);
+    T* flat = reinterpret_cast<T*>(smem);
+    const float c = P.c;
+    const float2 c2 = make_float2(c, c);
     if (tid == 0) {
-        tc::mbar_init(bar, 1);
+        for (int i = 0; i < kPieces; ++i) tc::mbar_init(bar0 + 8u * i, 1);
+        for (int i = 0; i < 2; ++i) tc::mbar_init(bar0 + 8u * (kPieces + i), C);
         s_abort = 0;
         tc::fence_mbar_init();
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
-    const int w0 = int(long(in.words) * rank / C), nw = int(long(in.words) * (rank + 1) / C) - w0;
-    const float c = P.c, weight = P.weight ? P.weight[row] : 1.f;
-    // the slice's edge elements, one to a thread: those before the row's first
-    // word, those behind its last
-    const int heads = rank == 0 ? in.head : 0, tails = rank == C - 1 ? in.tail : 0;
-    const int edge = tid < heads ? tid : tid < heads + tails ? P.V - in.tail + tid - heads : -1;
-    const Word<T>* slice = reinterpret_cast<const Word<T>*>(smem);
-    T* flat = reinterpret_cast<T*>(smem);
-    T* out = P.grad ? static_cast<T*>(P.grad) + row * P.V : nullptr;
-    const bool words_out = out && (reinterpret_cast<uintptr_t>(out + in.head) & 15u) == 0;
-
-    if (weight == 0.f) {         // a row that is left out
-        if (rank == 0 && tid == 0) P.loss[row] = 0.f;
-        if (out) {
-            if (edge >= 0) out[edge] = from_float<T>(0.f);
-            const int lo = in.at(w0), n = nw * N;
-            if (words_out) {
-                for (int w = tid; w < nw; w += kDistillThreads) reinterpret_cast<uint4*>(out + lo)[w] = make_uint4(0, 0, 0, 0);
-            } else {
-                for (int i = tid; i < n; i += kDistillThreads) out[lo + i] = from_float<T>(0.f);
-            }
-        }
-        __syncwarp();
-        if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-        return;
-    }
-    if (tid == 0) {              // (it has made the barrier itself)
-        tc::mbar_arrive_expect_tx(bar, uint32_t(nw) * 16u);
-        for (int i = 0; i < kPieces; ++i) {
-            const int lo = int(long(nw) * i / kPieces), n = int(long(nw) * (i + 1) / kPieces) - lo;
-            if (n > 0) bulk_load(tc::smem_u32(slice + lo), in.body() + w0 + lo, uint32_t(n) * 16u, bar);
-        }
-    }
-
-    // The teacher is warp 0's, four alternatives to a lane: tokens, their logits,
-    // weights, and what they add to the sums.
-    constexpr int J = kMaxTop / 32;
-    const int first_word = in.at(w0);
+    // this CTA's part of a row: words, from w0 on
+    struct Part {
+        Row<T> in;
+        int w0, nw;
+    };
+    auto part_of = [&](long row) {
+        const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
+        const int w0 = int(long(in.words) * rank >> log2_C);
+        return Part{in, w0, int(long(in.words) * (rank + 1) >> log2_C) - w0};
+    };
+    // a piece of a row, by one thread (an empty one just arrives)
+    auto ask = [&](const Part& p, int i) {
+        const int lo = i * P.piece, n = max(0, min(P.piece, p.nw - lo));
+        tc::mbar_arrive_expect_tx(bar0 + 8u * i, uint32_t(n) * 16u);
+        if (n > 0) bulk_load(tc::smem_u32(slice + lo), p.in.body() + p.w0 + lo, uint32_t(n) * 16u, bar0 + 8u * i);
+    };
+    // The teacher of a row, up to four alternatives to a lane, in three steps, each
+    // a row ahead of the next so that none waits for memory: what is given for it,
+    // its tokens' logits, and what it comes to.
+    int64_t asked[J];
+    float given[J], q[J], z[J];
     int id[J];
-    float q[J], z[J];
-    bool lead[J];                       // a token's first mention
-    if (warp == 0) {
-        bool poison = false;
-        float top = kNone, top_z = kNone;
+    bool poison = false;
+    auto ask_teacher = [&](long row) {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int k = j * 32 + lane;
-            id[j] = -1;
-            q[j] = z[j] = kNone;
-            if (k < P.K) {
-                const int64_t asked = P.ids[row * P.K + k];
-                q[j] = P.teacher[row * P.K + k];
-                poison |= asked >= P.V;
-                if (asked >= 0 && asked < P.V) id[j] = int(asked);
-                if (id[j] >= 0) z[j] = to_float(in.x[id[j]]);
-                else q[j] = kNone;
+            asked[j] = -1;
+            given[j] = kNone;
+            if (k < P.K && row < P.rows) {
+                asked[j] = P.ids[row * P.K + k];
+                given[j] = P.teacher[row * P.K + k];
             }
-            s_id[k] = id[j];
+        }
+    };
+    auto look_up = [&](long row) {
+        const T* x = static_cast<const T*>(P.x) + row * P.stride;
+        poison = false;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            poison |= asked[j] >= P.V;
+            id[j] = asked[j] >= 0 && asked[j] < P.V ? int(asked[j]) : -1;
+            z[j] = id[j] >= 0 ? to_float(x[id[j]]) : kNone;
+            q[j] = id[j] >= 0 ? given[j] : kNone;
+        }
+    };
+    auto teach = [&](long row, Teacher& t) {
+        const Row<T> in(static_cast<const T*>(P.x) + row * P.stride, P.V);
+        unsigned edges = 0;
+        bool first[J];
+        float top = kNone, most = kNone;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (id[j] >= 0 && id[j] < in.head) edges |= 1u << id[j];
+            if (id[j] >= P.V - in.tail) edges |= 256u << (id[j] - (P.V - in.tail));
+            t.id[j * 32 + lane] = id[j];
             top = fmaxf(top, q[j]);
-            top_z = fmaxf(top_z, z[j]);
+            // first of its 32, and not among those before
+            first[j] = false;
+            if (j * 32 < P.K) {
+                const unsigned same = __match_any_sync(0xffffffffu, id[j]);
+                first[j] = id[j] >= 0 && (same & ((1u << lane) - 1u)) == 0;
+            }
         }
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < J; ++j) lead[j] = id[j] >= 0;
-        for (int k = 0; k < P.K; k += 4) {
-            const int4 four = *reinterpret_cast<const int4*>(s_id + k);
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int before = j * 32 + lane - k;      // how many of the four come before it
-                lead[j] = lead[j] && !((before > 0 && four.x == id[j]) || (before > 1 && four.y == id[j]) || (before > 2 && four.z == id[j]) ||
-                                       (before > 3 && four.w == id[j]));
+        for (int j = 1; j < J; ++j) {
+            if (j * 32 >= P.K) break;
+            for (int k = 0; k < j * 32; k += 4) {
+                const int4 four = *reinterpret_cast<const int4*>(t.id + k);
+                first[j] = first[j] && four.x != id[j] && four.y != id[j] && four.z != id[j] && four.w != id[j];
             }
         }
-        poison = __any_sync(0xffffffffu, poison);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            t.z[j * 32 + lane] = z[j];
+            most = fmaxf(most, z[j]);
+        }
+        const bool outside = __any_sync(0xffffffffu, poison);
+        edges = __reduce_or_sync(0xffffffffu, edges);
 #pragma unroll
         for (int off = 16; off > 0; off /= 2) {
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            top_z = fmaxf(top_z, __shfl_xor_sync(0xffffffffu, top_z, off));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
         }
         if (P.rest || top == kNone) top = 0.f;
         float sum = 0.f, e = 0.f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
+            t.log_q[j * 32 + lane] = q[j] - top;
             q[j] = expf(q[j] - top);
             sum += q[j];
-            if (lead[j]) e += ex2((z[j] - (top_z == kNone ? 0.f : top_z)) * c);
+            if (first[j]) e += ex2((z[j] - (most == kNone ? 0.f : most)) * c);
         }
 #pragma unroll
         for (int off = 16; off > 0; off /= 2) {
             sum += __shfl_xor_sync(0xffffffffu, sum, off);
             e += __shfl_xor_sync(0xffffffffu, e, off);
         }
-        // in fp64 what is left of 1 (NaN for a row with a token outside the vocabulary)
-        double q_all = 0.0;
+        // (NaN for a row with a token outside the vocabulary)
+        float2 all = make_float2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             if (!P.rest && sum != 0.f) q[j] /= sum;
-            if (poison) q[j] = NAN;
-            q_all += double(q[j]);
-            s_q[j * 32 + lane] = q[j];
+            if (outside) q[j] = NAN;
+            if (j * 32 < P.K) all = pair_sum(all, make_float2(q[j], 0.f));
+            t.q[j * 32 + lane] = q[j];
         }
 #pragma unroll
-        for (int off = 16; off > 0; off /= 2) q_all += __shfl_xor_sync(0xffffffffu, q_all, off);
-        if (lane == 0) {
-            s_ids = make_float2(top_z, e);
-            s_all[0] = float(q_all);
-            s_all[1] = P.rest ? float(1.0 - q_all > 0.0 || q_all != q_all ? 1.0 - q_all : 0.0) : 0.f;
-        }
-    }
-    float edge_x = edge >= 0 ? to_float(in.x[edge]) : kNone;
-    const bool landed = tc::mbar_wait(bar, 0, &s_abort, P.err, kErrRow);
-    if (warp == 0 && landed) {
+        for (int off = 16; off > 0; off /= 2)
+            all = pair_sum(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, off), __shfl_xor_sync(0xffffffffu, all.y, off)));
+        const float left = pair_sum(make_float2(1.f, 0.f), make_float2(-all.x, -all.y)).x;
+        __syncwarp();
+        bool again = false;
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (id[j] >= first_word && id[j] < first_word + nw * N) flat[id[j] - first_word] = from_float<T>(kNone);
-    }
-    __syncthreads();
-    if (edge >= 0)
-        for (int k = 0; k < P.K; ++k)
-            if (s_id[k] == edge) edge_x = kNone;
-
-    // the sum of all other tokens
-    LaneSums sums;
-    const float2 c2 = make_float2(c, c);
-    if (edge >= 0) {
-        sums.rise(edge_x, c);
-        sums.add<false>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
-    }
-#pragma unroll 2
-    for (int w = tid; w < nw; w += kDistillThreads) {
-        const Word<T> v = slice[w];
-        sums.rise(largest(v), c);
-        add_word<false>(sums, v, sums.minus_ref(), c2);
-    }
-    // of sums with their largest x, over `n` lanes (-inf: a sum of 0, or NaN)
-    auto together = [&](float2 v, int n) {
-        float m = v.x;
-        for (int off = n / 2; off > 0; off /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-        if (v.x != kNone && v.x != m) v.y *= ex2((v.x - m) * c);
-        for (int off = n / 2; off > 0; off /= 2) v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
-        return make_float2(m, v.y);
-    };
-    const float2 mine = together(make_float2(sums.m, sums.s.x + sums.s.y), 32);
-    if (lane == 0) s_warps[warp] = mine;
-    if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
-    __syncthreads();
-    // to every CTA of the cluster
-    if (warp == 0) {
-        const float2 part = together(lane < kDistillThreads / 32 ? s_warps[lane] : make_float2(kNone, 0.f), 32);
-        if (lane < C) *cluster.map_shared_rank(&s_cta[rank], lane) = part;
-    }
-    if (C > 1) cluster.sync();
-    else __syncthreads();
-    const float2 others = together(lane < C ? s_cta[lane] : make_float2(kNone, 0.f), 32), ids = s_ids;
-    const float m = fmaxf(others.x, ids.x), ref = m == kNone ? 0.f : m;
-    const float s_rest = others.x == kNone ? others.y : others.y * ex2((others.x - ref) * c);
-    const float s_all_ids = ids.x == kNone ? ids.y : ids.y * ex2((ids.x - ref) * c), s_sum = s_rest + s_all_ids;
-    // p_j = e_j / s_sum; the gradient of a token that is not the teacher's is
-    // f p_j, of one that is (all p_j - q_j)
-    const float q_rest = s_all[1], all = P.rest ? 1.f : s_all[0], inv_s = s_sum == 0.f ? 0.f : 1.f / s_sum;
-    const float f = !P.rest ? all : s_rest == 0.f ? 1.f : 1.f - q_rest * s_sum / s_rest;
-
-    if (out) {
-        const float scale = weight * P.inv_T, k = f * inv_s * scale;
-        if (words_out) {
-#pragma unroll 2
-            for (int w = tid; w < nw; w += kDistillThreads) {
-                const Word<T> v = slice[w];
-                Word<T> g;
-#pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), ref, k, P);
-                    g.x[e] = from_float<T>(two.x);
-                    g.x[e + 1] = from_float<T>(two.y);
-                }
-                reinterpret_cast<Word<T>*>(out + first_word)[w] = g;
-            }
-        } else {
-            for (int i = tid; i < nw * N; i += kDistillThreads)
-                out[first_word + i] = from_float<T>(weights_of<T>(make_float2(to_float(flat[i]), 0.f), ref, k, P).x);
-        }
-        if (edge >= 0) out[edge] = from_float<T>(weights_of<T>(make_float2(edge_x, 0.f), ref, k, P).x);
-        __syncthreads();
-        if (warp == 0) {
-            // the teacher's tokens, each by its first mention in the CTA that has it
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int i = id[j];
-                const bool here = (i >= first_word && i < first_word + nw * N) || (rank == 0 && i < in.head) || (rank == C - 1 && i >= P.V - in.tail);
-                if (!lead[j] || !here) continue;
-                float sum = 0.f;
-                for (int n = j * 32 + lane; n < P.K; ++n)
-                    if (s_id[n] == i) sum += s_q[n];
-                out[i] = from_float<T>(fmaf(scale * all, weights_of<T>(make_float2(z[j], 0.f), ref, inv_s, P).x, -scale * sum));
-            }
-        }
-    }
-    if (rank == 0 && warp == 0) {
-        // in fp64: the terms are small differences of log probabilities
-        const double log_s = s_sum == 0.f ? 0.0 : log(double(s_sum));
-        double total = 0.0;
+        for (int j = 0; j < J; ++j) again |= id[j] >= 0 && !first[j];
+        again = __any_sync(0xffffffffu, again);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (q[j] != 0.f)
-                total += double(q[j]) * (log(double(q[j])) - (s_sum == 0.f ? -INFINITY : (double(z[j]) - double(ref)) * double(P.inv_T) - log_s));
+            float own = q[j];
+            for (int k = j * 32 + lane + 1; again && k < P.K; ++k)
+                if (t.id[k] == id[j]) own += t.q[k];
+            t.sum[j * 32 + lane] = first[j] ? own : -1.f;
         }
-#pragma unroll
-        for (int off = 16; off > 0; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
         if (lane == 0) {
-            if (q_rest > 0.f) total += double(q_rest) * (log(double(q_rest)) - (log(double(s_rest)) - log_s));
-            P.loss[row] = float(total * double(weight));
+            t.most = most;
+            t.e = e;
+            t.edges = edges;
+            t.norm = P.rest || sum == 0.f ? 1.f : sum;
+            t.all = all.x;
+            t.rest = P.rest ? (left > 0.f || left != left ? left : 0.f) : 0.f;
         }
+    };
+    // of sums with their largest x, over a warp (-inf: a sum of 0, or NaN)
+    auto together = [&](float2 v) {
+        float m = v.x;
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        if (v.x != kNone && v.x != m) v.y *= ex2((v.x - m) * c);
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
+        return make_float2(m, v.y);
+    };
+
+    if (tid == 0 && row0 < P.rows) {          // (it has made the barriers itself)
+        const Part p = part_of(row0);
+        for (int i = 0; i < kPieces; ++i) ask(p, i);
     }
+    if (warp == kWorkers / 32 && row0 < P.rows) {
+        ask_teacher(row0);
+        look_up(row0);
+        ask_teacher(row0 + step);
+        teach(row0, s_teacher[0]);
+        look_up(row0 + step);
+        ask_teacher(row0 + 2 * step);
+    }
+    if (C > 1) cluster.sync();                // every CTA has begun
+    else __syncthreads();
+
+    // What a row's gradient goes by: p_j = e_j / s; the gradient of a token that is
+    // not the teacher's is f p_j, of one that is (all p_j - q_j); all times scale.
+    struct Stats {
+        float ref, rest, s, inv_s, all, f, scale;
+    };
+    uint32_t turn = 0, round = 0;        // row by row, and every other
+    // (once every CTA's sums are here)
+    auto stats_of = [&](const Teacher& t, float weight) {
+        const float2 others = together(lane < C ? s_cta[turn][lane] : make_float2(kNone, 0.f));
+        const float m = fmaxf(others.x, t.most);
+        Stats a;
+        a.ref = m == kNone ? 0.f : m;
+        a.rest = others.x == kNone ? others.y : others.y * ex2((others.x - a.ref) * c);
+        a.s = a.rest + (t.most == kNone ? t.e : t.e * ex2((t.most - a.ref) * c));
+        a.inv_s = a.s == 0.f ? 0.f : 1.f / a.s;
+        a.all = P.rest ? 1.f : t.all;
+        a.f = !P.rest ? a.all : a.rest == 0.f ? 1.f : 1.f - t.rest * a.s / a.rest;
+        a.scale = weight * P.inv_T;
+        return a;
+    };
+    auto exchanged = [&]() { return wait_cluster(bar0 + 8u * (kPieces + turn), round, &s_abort, P.err, kErrRow); };
+
+    if (warp < kWorkers / 32) {
+        for (long row = row0; row < P.rows; row += step) {
+            const Part p = part_of(row), next = part_of(min(row + step, P.rows - 1));
+            const bool more = row + step < P.rows;
+            const Teacher& t = s_teacher[turn];
+            const float weight = P.weight ? P.weight[row] : 1.f;
+            const int first_word = p.in.at(p.w0);
+            // the slice's edge elements, one to a thread: those before the row's
+            // first word, those behind its last
+            const int heads = rank == 0 ? p.in.head : 0, tails = rank == C - 1 ? p.in.tail : 0;
+            const int edge = tid < heads ? tid : tid < heads + tails ? P.V - p.in.tail + tid - heads : -1;
+            // the teacher's tokens out
+            float edge_x = kNone;
+            if (edge >= 0 && !(t.edges >> (tid < heads ? edge : 8 + tid - heads) & 1u)) edge_x = to_float(p.in.x[edge]);
+            bool landed = true;
+            for (int i = 0; i < kPieces; ++i) landed = landed && tc::mbar_wait(bar0 + 8u * i, turn, &s_abort, P.err, kErrRow);
+            if (tid < P.K && landed) {
+                const int at = t.id[tid] - first_word;
+                if (t.id[tid] >= 0 && at >= 0 && at < p.nw * N) flat[at] = from_float<T>(kNone);
+            }
+            workers_sync();
+            // the sum of all others
+            LaneSums sums;
+            if (edge >= 0) {
+                sums.rise(edge_x, c);
+                sums.add<false>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
+            }
+            for (int i = 0; i < kPieces; ++i) {
+                const int end = min(p.nw, (i + 1) * P.piece);
+                for (int w = i * P.piece + tid; w < end; w += 2 * kWorkers) {
+                    const Word<T> a = slice[w], b = slice[min(w + kWorkers, end - 1)];
+                    const bool two = w + kWorkers < end;
+                    sums.rise(two ? fmaxf(largest(a), largest(b)) : largest(a), c);
+                    const float2 minus = sums.minus_ref();
+                    add_word<false>(sums, a, minus, c2);
+                    if (two) add_word<false>(sums, b, minus, c2);
+                }
+                if constexpr (!GRAD) {
+                    tc::fence_proxy_async_smem();
+                    workers_sync();
+                    if (tid == 0 && more) ask(next, i);
+                }
+            }
+            const float2 mine = together(make_float2(sums.m, sums.s.x + sums.s.y));
+            if (lane == 0) s_warps[warp] = mine;
+            workers_sync();
+            // to every CTA of the cluster
+            if (warp == 0) {
+                const float2 part = together(lane < kWorkers / 32 ? s_warps[lane] : make_float2(kNone, 0.f));
+                if (lane < C) {
+                    *cluster.map_shared_rank(&s_cta[turn][rank], lane) = part;
+                    tc::mbar_arrive_cluster(tc::map_cta(bar0 + 8u * (kPieces + turn), uint32_t(lane)));
+                }
+                __syncwarp();
+            }
+            if constexpr (GRAD) {
+                exchanged();
+                const Stats a = stats_of(t, weight);
+                T* out = static_cast<T*>(P.grad) + row * P.V;
+                const bool words_out = (reinterpret_cast<uintptr_t>(out + p.in.head) & 15u) == 0;
+                const float k = a.f * a.inv_s * a.scale;
+                for (int i = 0; i < kPieces; ++i) {
+                    const int lo = i * P.piece, end = min(p.nw, lo + P.piece);
+                    if (weight == 0.f) {         // a row that is left out
+                        if (words_out) {
+                            for (int w = lo + tid; w < end; w += kWorkers) reinterpret_cast<uint4*>(out + first_word)[w] = make_uint4(0, 0, 0, 0);
+                        } else {
+                            for (int w = lo * N + tid; w < end * N; w += kWorkers) out[first_word + w] = from_float<T>(0.f);
+                        }
+                    } else if (words_out) {
+#pragma unroll 2
+                        for (int w = lo + tid; w < end; w += kWorkers) {
+                            const Word<T> v = slice[w];
+                            Word<T> g;
+#pragma unroll
+                            for (int e = 0; e < N; e += 2) {
+                                const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), a.ref, k, P);
+                                g.x[e] = from_float<T>(two.x);
+                                g.x[e + 1] = from_float<T>(two.y);
+                            }
+                            reinterpret_cast<Word<T>*>(out + first_word)[w] = g;
+                        }
+                    } else {
+                        for (int w = lo * N + tid; w < end * N; w += kWorkers)
+                            out[first_word + w] = from_float<T>(weights_of<T>(make_float2(to_float(flat[w]), 0.f), a.ref, k, P).x);
+                    }
+                    tc::fence_proxy_async_smem();
+                    workers_sync();
+                    if (tid == 0 && more) ask(next, i);
+                }
+                if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.ref, k, P).x);
+            }
+            __syncthreads();
+            round ^= turn;
+            turn ^= 1u;
+        }
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        return;
+    }
+
+    // The teacher's warp, a row behind and a row ahead: the gradients of the last
+    // row's tokens, which the workers have written as any others', are put right;
+    // the next row's teacher; this one's loss.
+    Stats last{};
+    auto put_right = [&](long row, const Teacher& t) {
+        if (!GRAD || last.scale == 0.f) return;
+        const Part p = part_of(row);
+        const int first_word = p.in.at(p.w0);
+        T* out = static_cast<T*>(P.grad) + row * P.V;
+        for (int k = lane; k < P.K; k += 32) {
+            const int i = t.id[k];
+            const bool here = (i >= first_word && i < first_word + p.nw * N) || (rank == 0 && i < p.in.head) ||
+                              (rank == C - 1 && i >= P.V - p.in.tail);
+            const float sum = t.sum[k];
+            if (i >= 0 && here && sum != -1.f)
+                out[i] = from_float<T>(fmaf(last.scale * last.all, weights_of<T>(make_float2(t.z[k], 0.f), last.ref, last.inv_s, P).x,
+                                            -last.scale * sum));
+        }
+    };
+    for (long row = row0; row < P.rows; row += step) {
+        const Teacher& t = s_teacher[turn];
+        const float weight = P.weight ? P.weight[row] : 1.f;
+        if (row > row0) put_right(row - step, s_teacher[turn ^ 1u]);
+        __syncwarp();
+        if (row + step < P.rows) {
+            teach(row + step, s_teacher[turn ^ 1u]);
+            look_up(row + 2 * step);
+            ask_teacher(row + 3 * step);
+        }
+        exchanged();
+        const Stats a = last = stats_of(t, weight);
+        if (rank == 0) {
+            // in pairs, as the terms are small differences of log probabilities; the
+            // four logarithms by a lane each
+            const float2 mine = log_pair(lane == 0 ? a.s : lane == 1 ? a.rest : lane == 2 ? t.rest : t.norm);
+            auto of = [&](int from) {
+                return make_float2(__shfl_sync(0xffffffffu, mine.x, from), __shfl_sync(0xffffffffu, mine.y, from));
+            };
+            auto minus = [](float2 a) { return make_float2(-a.x, -a.y); };
+            const float2 log_s = of(0), log_others = of(1), log_rest = of(2), log_norm = of(3);
+            float2 total = make_float2(0.f, 0.f);
+            for (int k = lane; k < P.K; k += 32) {
+                const float q = t.q[k];
+                if (q == 0.f) continue;
+                // log q - log p; p is 0 where its logit is -inf or no token has one
+                const float2 by = exact_sum(t.z[k], -a.ref);
+                const float z = by.x * P.inv_T, low = fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low);
+                const bool none = a.s == 0.f || t.z[k] == kNone;
+                const float2 log_p = pair_sum(make_float2(z, low), minus(log_s)), log_q = pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm));
+                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_q, minus(log_p));
+                const float x = q * d.x;
+                total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(q, d.x, -x) + q * d.y));
+            }
+            if (lane == 0 && t.rest > 0.f) {
+                const bool none = a.rest == 0.f;
+                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_rest, minus(pair_sum(log_others, minus(log_s))));
+                const float x = t.rest * d.x;
+                total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(t.rest, d.x, -x) + t.rest * d.y));
+            }
+            // (an infinity's rest would be NaN)
+            const bool finite = __all_sync(0xffffffffu, fabsf(total.x) < INFINITY);
+#pragma unroll
+            for (int off = 16; off > 0; off /= 2) {
+                const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, total.x, off), __shfl_xor_sync(0xffffffffu, total.y, off));
+                total = finite ? pair_sum(total, o) : make_float2(total.x + o.x, 0.f);
+            }
+            if (lane == 0) P.loss[row] = weight == 0.f ? 0.f : (total.x + total.y) * weight;
+        }
+        __syncthreads();
+        round ^= turn;
+        turn ^= 1u;
+        if (row + step >= P.rows) put_right(row, s_teacher[turn ^ 1u]);
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 template <class Kernel, class Params>
-int launch(Kernel kernel, long ctas, int threads, size_t smem, int cluster, const Params& P, cudaStream_t st) {
+int launch(Kernel kernel, long ctas, int threads, size_t smem, int cluster, const Params& P, cudaStream_t st, bool early = true) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ctas));
     cfg.blockDim = dim3(unsigned(threads));
@@ -777,7 +1001,7 @@ int launch(Kernel kernel, long ctas, int threads, size_t smem, int cluster, cons
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].val.programmaticStreamSerializationAllowed = early;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = unsigned(cluster);
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
@@ -824,27 +1048,68 @@ int scores(const ScoreParams& P, long rows, cudaStream_t st) {
     return scores<T, 4>(P, rows, st);
 }
 
-// Bytes of a CTA's slice at the most.
-constexpr size_t kSliceMax = 216 * 1024;
+// Bytes of a CTA's slice with four, two and one CTA to an SM.
+constexpr int kClasses = 3;
+constexpr size_t kSlices[kClasses] = {49 * 1024, 104 * 1024, 216 * 1024}, kSliceMax = kSlices[kClasses - 1];
 
 size_t slice_bytes(long V, size_t size, int C) { return (size_t(V) * size / 16 / C + 1) * 16; }
 
 int distill_cluster(long rows, long V, size_t size) {
     int C = 1;
-    while (C < kMaxCluster && slice_bytes(V, size, C) > DISTILL_KB * 1024) C *= 2;
-    while (C < kMaxCluster && rows * C < 456 && V >= 8192L * C) C *= 2;
+    while (C < kMaxCluster && slice_bytes(V, size, C) > kSlices[0]) C *= 2;
+    while (C < kMaxCluster && rows * C < 304 && V >= 8192L * C) C *= 2;
     return C;
 }
 
-template <class T>
-int distill(const DistillParams& P, long rows, cudaStream_t st) {
-    static splice::PerDevice<bool> kept;
-    const cudaError_t e = allow(kept, distill_kernel<T>, kSliceMax);
+// Clusters of 1, 2, 4, 8 and 16 CTAs that are resident together.
+struct Clusters {
+    int n[5][kClasses];
+};
+
+template <class T, bool GRAD>
+int distill(DistillParams P, cudaStream_t st) {
+    static splice::PerDevice<Clusters> kept;
+    Clusters clusters;
+    const cudaError_t e = kept.get(&clusters, [](int, Clusters* r) {
+        auto kernel = distill_kernel<T, GRAD>;
+        cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSliceMax));
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        for (int i = 0; i < 5 * kClasses && err == cudaSuccess; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << (i / kClasses));
+            cfg.blockDim = dim3(kDistillThreads);
+            cfg.dynamicSmemBytes = kSlices[i % kClasses];
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 1u << (i / kClasses);
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            err = cudaOccupancyMaxActiveClusters(&r->n[i / kClasses][i % kClasses], kernel, &cfg);
+        }
+        return err;
+    });
     if (e != cudaSuccess) return int(e);
-    const int C = distill_cluster(rows, P.V, sizeof(T));
+    const int C = distill_cluster(P.rows, P.V, sizeof(T));
     const size_t bytes = slice_bytes(P.V, sizeof(T), C);
     if (bytes > kSliceMax) return int(cudaErrorInvalidValue);
-    return launch(distill_kernel<T>, rows * C, kDistillThreads, bytes, C, P, st);
+    // (whole rounds of the workers, two words each)
+    P.piece = int((bytes / 16 + kPieces * 2 * kWorkers - 1) / (kPieces * 2 * kWorkers)) * 2 * kWorkers;
+    int log2 = 0;
+    while (1 << log2 < C) ++log2;
+    int size = 0;
+    while (bytes > kSlices[size]) ++size;
+    const long n = std::min(P.rows, long(std::max(1, clusters.n[log2][size])));
+    // Clusters that stay have to be resident all at once.  Set up while another
+    // kernel's CTAs leave they do not fit as they would on an empty GPU, and the
+    // last begin when the first have ended (190 us in place of 115): only few come
+    // before their time.
+    return launch(distill_kernel<T, GRAD>, n * C, kDistillThreads, kSlices[size], C, P, st, n * C <= 152);
+}
+
+template <class T>
+int distill(const DistillParams& P, cudaStream_t st) {
+    return P.grad ? distill<T, true>(P, st) : distill<T, false>(P, st);
 }
 
 }  // namespace
@@ -878,13 +1143,13 @@ int decoder_distill(const void* x, int dtype, long stride, long rows, long V, co
     if (rows < 1 || rows > (1L << 27) || V < 1 || V > decoder_distill_vocab(dtype) || K < 1 || K > kMaxTop || !(inv_T > 0.0))
         return int(cudaErrorInvalidValue);
     const float c = float(inv_T * kLog2e);
-    const DistillParams P{x, stride, int(V), K, rest, float(inv_T), c, float(inv_T * kLog2e - double(c)), -160.f / c, static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
+    const DistillParams P{x, stride, rows, int(V), K, rest, 0, float(inv_T), float(inv_T - double(float(inv_T))), c, float(inv_T * kLog2e - double(c)), -160.f / c, static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
                           static_cast<const float*>(weight), static_cast<float*>(loss), grad, decoder::error_word()};
     if (!P.err) return int(cudaErrorInvalidValue);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == 0) return distill<float>(P, rows, st);
-    if (dtype == 1) return distill<__nv_bfloat16>(P, rows, st);
-    if (dtype == 2) return distill<__half>(P, rows, st);
+    if (dtype == 0) return distill<float>(P, st);
+    if (dtype == 1) return distill<__nv_bfloat16>(P, st);
+    if (dtype == 2) return distill<__half>(P, st);
     return int(cudaErrorInvalidValue);
 }
 
