@@ -522,7 +522,16 @@ __device__ __forceinline__ float2 weights_of(float2 x, float ref, float k, const
     }
 }
 
-// A wait for arrivals of other CTAs of the cluster, and what they wrote before.
+// 8 bytes to another CTA of the cluster, which count on its barrier.  (A store and
+// an arrival that releases it wait for all that the thread has written before, its
+// gradients among it: 2 us.)
+__device__ __forceinline__ void store_async(uint32_t to, float2 v, uint32_t bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.x), "f"(v.y),
+                 "r"(bar)
+                 : "memory");
+}
+
+// A wait for what other CTAs of the cluster send.
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err, unsigned code) {
     const uint64_t t0 = tc::globaltimer_ns();
     for (uint32_t i = 1;; ++i) {
@@ -609,9 +618,9 @@ __device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" 
 // The teacher's tokens are taken out of the slice (-inf) before it is summed up
 // and put in their own way, so the sum of all others is a sum and not a
 // difference.
-template <class T, bool GRAD>
+template <class T, bool GRAD, int J>
 __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams P) {
-    constexpr int N = Word<T>::N, J = kMaxTop / 32;
+    constexpr int N = Word<T>::N;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[kPieces + 2];
     __shared__ Teacher s_teacher[2];
@@ -629,7 +638,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     const float2 c2 = make_float2(c, c);
     if (tid == 0) {
         for (int i = 0; i < kPieces; ++i) tc::mbar_init(bar0 + 8u * i, 1);
-        for (int i = 0; i < 2; ++i) tc::mbar_init(bar0 + 8u * (kPieces + i), C);
+        for (int i = 0; i < 2; ++i) tc::mbar_init(bar0 + 8u * (kPieces + i), 1);
         s_abort = 0;
         tc::fence_mbar_init();
     }
@@ -651,7 +660,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         tc::mbar_arrive_expect_tx(bar0 + 8u * i, uint32_t(n) * 16u);
         if (n > 0) bulk_load(tc::smem_u32(slice + lo), p.in.body() + p.w0 + lo, uint32_t(n) * 16u, bar0 + 8u * i);
     };
-    // The teacher of a row, up to four alternatives to a lane, in three steps, each
+    // The teacher of a row, J alternatives to a lane, in three steps, each
     // a row ahead of the next so that none waits for memory: what is given for it,
     // its tokens' logits, and what it comes to.
     int64_t asked[J];
@@ -694,7 +703,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             top = fmaxf(top, q[j]);
             // first of its 32, and not among those before
             first[j] = false;
-            if (j * 32 < P.K) {
+            {
                 const unsigned same = __match_any_sync(0xffffffffu, id[j]);
                 first[j] = id[j] >= 0 && (same & ((1u << lane) - 1u)) == 0;
             }
@@ -702,7 +711,6 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         __syncwarp();
 #pragma unroll
         for (int j = 1; j < J; ++j) {
-            if (j * 32 >= P.K) break;
             for (int k = 0; k < j * 32; k += 4) {
                 const int4 four = *reinterpret_cast<const int4*>(t.id + k);
                 first[j] = first[j] && four.x != id[j] && four.y != id[j] && four.z != id[j] && four.w != id[j];
@@ -740,7 +748,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         for (int j = 0; j < J; ++j) {
             if (!P.rest && sum != 0.f) q[j] /= sum;
             if (outside) q[j] = NAN;
-            if (j * 32 < P.K) all = pair_sum(all, make_float2(q[j], 0.f));
+            all = pair_sum(all, make_float2(q[j], 0.f));
             t.q[j * 32 + lane] = q[j];
         }
 #pragma unroll
@@ -865,11 +873,9 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             // to every CTA of the cluster
             if (warp == 0) {
                 const float2 part = together(lane < kWorkers / 32 ? s_warps[lane] : make_float2(kNone, 0.f));
-                if (lane < C) {
-                    *cluster.map_shared_rank(&s_cta[turn][rank], lane) = part;
-                    tc::mbar_arrive_cluster(tc::map_cta(bar0 + 8u * (kPieces + turn), uint32_t(lane)));
-                }
-                __syncwarp();
+                const uint32_t to = tc::smem_u32(&s_cta[turn][rank]), bar = bar0 + 8u * (kPieces + turn);
+                if (lane == 0) tc::mbar_arrive_expect_tx(bar, uint32_t(C) * 8u);
+                if (lane < C) store_async(tc::map_cta(to, uint32_t(lane)), part, tc::map_cta(bar, uint32_t(lane)));
             }
             if constexpr (GRAD) {
                 exchanged();
@@ -1066,12 +1072,12 @@ struct Clusters {
     int n[5][kClasses];
 };
 
-template <class T, bool GRAD>
+template <class T, bool GRAD, int J>
 int distill(DistillParams P, cudaStream_t st) {
     static splice::PerDevice<Clusters> kept;
     Clusters clusters;
     const cudaError_t e = kept.get(&clusters, [](int, Clusters* r) {
-        auto kernel = distill_kernel<T, GRAD>;
+        auto kernel = distill_kernel<T, GRAD, J>;
         cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSliceMax));
         if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         for (int i = 0; i < 5 * kClasses && err == cudaSuccess; ++i) {
@@ -1104,7 +1110,12 @@ int distill(DistillParams P, cudaStream_t st) {
     // kernel's CTAs leave they do not fit as they would on an empty GPU, and the
     // last begin when the first have ended (190 us in place of 115): only few come
     // before their time.
-    return launch(distill_kernel<T, GRAD>, n * C, kDistillThreads, kSlices[size], C, P, st, n * C <= 152);
+    return launch(distill_kernel<T, GRAD, J>, n * C, kDistillThreads, kSlices[size], C, P, st, n * C <= 152);
+}
+
+template <class T, bool GRAD>
+int distill(const DistillParams& P, cudaStream_t st) {
+    return P.K <= 32 ? distill<T, GRAD, 1>(P, st) : P.K <= 64 ? distill<T, GRAD, 2>(P, st) : distill<T, GRAD, 4>(P, st);
 }
 
 template <class T>
