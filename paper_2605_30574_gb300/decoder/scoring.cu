@@ -32,9 +32,6 @@ using decoder::bulk_load;
 using decoder::ex2;
 
 constexpr int kMaxTop = 128, kMaxCluster = 16, kMaxWarps = 16;
-#ifndef SCORE_CTAS
-#define SCORE_CTAS 512
-#endif
 constexpr unsigned kErrRow = 256;
 constexpr float kNone = -INFINITY;
 constexpr double kLog2e = 1.4426950408889634;
@@ -165,71 +162,6 @@ __device__ __forceinline__ float key_value(Key k) {
 }
 __device__ __forceinline__ int key_index(Key k) { return int(~uint32_t(k)); }
 
-// 32 R keys over a warp, the p-th in lane p % 32's element p / 32.
-template <int R>
-struct Keys {
-    Key k[R];
-
-    template <int J>
-    __device__ __forceinline__ void exchange(int lane, int up_bit) {
-        // descending where position & up_bit is 0 (up_bit 0: everywhere)
-        if constexpr (J >= 32) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (r & (J / 32)) continue;
-                const int q = r | (J / 32);
-                const bool desc = ((r * 32 + lane) & up_bit) == 0;
-                const Key a = k[r], b = k[q];
-                const bool swap = desc ? a < b : a > b;
-                k[r] = swap ? b : a;
-                k[q] = swap ? a : b;
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const bool desc = ((r * 32 + lane) & up_bit) == 0, low = (lane & J) == 0;
-                const Key o = __shfl_xor_sync(0xffffffffu, k[r], J);
-                if (low == desc ? o > k[r] : o < k[r]) k[r] = o;
-            }
-        }
-    }
-    template <int J>
-    __device__ __forceinline__ void tidy(int lane, int up_bit) {
-        exchange<J>(lane, up_bit);
-        if constexpr (J > 1) tidy<J / 2>(lane, up_bit);
-    }
-    template <int W>
-    __device__ __forceinline__ void sort_by(int lane) {
-        tidy<W / 2>(lane, W == 32 * R ? 0 : W);
-        if constexpr (W < 32 * R) sort_by<W * 2>(lane);
-    }
-    __device__ __forceinline__ void sort(int lane) { sort_by<2>(lane); }
-    // The 32 R largest of this and another, both in order.
-    __device__ __forceinline__ void merge(const Keys& o, int lane) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const Key b = __shfl_xor_sync(0xffffffffu, o.k[R - 1 - r], 31);
-            if (b > k[r]) k[r] = b;
-        }
-        tidy<16 * R>(lane, 0);
-    }
-    __device__ __forceinline__ void put(Key* to, int lane) const {
-#pragma unroll
-        for (int r = 0; r < R; ++r) to[r * 32 + lane] = k[r];
-    }
-    __device__ __forceinline__ void get(const Key* from, int lane) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) k[r] = from[r * 32 + lane];
-    }
-    __device__ __forceinline__ Key nth(int n) const {
-        Key v = 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (n / 32 == r) v = __shfl_sync(0xffffffffu, k[r], n % 32);
-        return v;
-    }
-};
-
 // The n-th largest of the lanes' values, n from 1 on.
 __device__ __forceinline__ float nth_of_lanes(float x, int n, int lane) {
 #pragma unroll
@@ -244,13 +176,6 @@ __device__ __forceinline__ float nth_of_lanes(float x, int n, int lane) {
     return __shfl_sync(0xffffffffu, x, n - 1);
 }
 
-// The largest float below x (x finite), -inf for -inf.
-__device__ __forceinline__ float below(float x) {
-    const int b = __float_as_int(x);
-    if (x == kNone) return x;
-    return __int_as_float(x > 0.f ? b - 1 : x == 0.f ? int(0x80000001u) : b + 1);
-}
-
 struct ScoreParams {
     const void* x;
     long stride;
@@ -259,47 +184,145 @@ struct ScoreParams {
     const int64_t* tokens;      // or NULL
     float *logprobs, *entropy, *top;
     int64_t* ids;
+    int buckets;                // of a thread
 };
 
-// The CTA looks at four words of each lane at a time (two for R = 4, for the
-// buffers' sake).  The softmax sums are a lane's own, with its own running
-// maximum.  For the K largest, a lane puts the places of its elements above a
-// bound into the warp's buffer (in any order), and from there they go, 32 R
-// sorted at a time, into the warp's sorted list.  The bound is the larger of
-// the list's K-th and what the CTA's warps know together: each has ceil(K /
-// warps) lanes whose largest elements are at least so and so large, so the least
-// of those is no larger than the K-th of all.  That is brought up to date after
-// 1, 2, 4, ... looks; without it, each warp by its own list, most looks of a
-// warp found candidates.  The bound stays as it is during a look, and a warp's
-// looks go up the row, so an element that equals the list's K-th comes behind it.
-template <class T, int R>
-struct ScoreShape {
-    static constexpr int N = Word<T>::N, U = R == 4 ? 2 : 4;
-    // of a buffer: what a flush leaves, and a look's (a list fits in, at the end)
-    static constexpr int CAP = 32 * R + 32 * U * N;
-    static_assert(CAP >= 2 * 32 * R);
-    static size_t smem(int warps, int cluster) { return R ? size_t(warps * CAP) * 4 + size_t(cluster) * 32 * R * sizeof(Key) : 0; }
-};
+constexpr int kBuckets = 32;          // of a thread's words, by the order in which it takes them
+constexpr int kCandidates = 1024;
 
-template <class T, int R>
-__global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams P) {
-    using Shape = ScoreShape<T, R>;
-    constexpr int N = Shape::N, U = Shape::U, CAP = Shape::CAP;
-    constexpr bool TOP = R > 0;
-    constexpr int RR = TOP ? R : 1;
-    extern __shared__ __align__(16) int s_places[];
+// The ordered bits of a value above -inf, 0 for the others and NaN.
+__device__ __forceinline__ uint32_t order_of(float x) { return x > kNone ? uint32_t(make_key(x, 0) >> 32) : 0u; }
+
+// The K largest of a CTA's slice (words w0 to w1 and an edge element of the first
+// threads), or all above -inf if there are fewer, as keys in any order: the K-th's
+// value by four rounds of 8 bits, then the larger ones, then the first of its
+// equals.  Returns how many; all threads take part.
+template <class T>
+__device__ __noinline__ int select(const ScoreParams& P, const Row<T>& in, int w0, int w1, int edge, float edge_x, Key* s_out, int* s_count) {
+    constexpr int N = Word<T>::N;
+    __shared__ int s_bins[256], s_warp[kMaxWarps + 1];
+    __shared__ uint32_t s_prefix;
+    __shared__ int s_left;
+    const int tid = threadIdx.x, threads = int(blockDim.x), warp = tid >> 5, lane = tid & 31;
+    const Word<T>* body = in.body();
+    auto each = [&](auto&& f) {
+        if (edge >= 0) f(edge_x, edge);
+        for (int w = w0 + tid; w < w1; w += threads) {
+            const Word<T> v = body[w];
+#pragma unroll
+            for (int e = 0; e < N; ++e) f(to_float(v.x[e]), in.at(w) + e);
+        }
+    };
+    uint32_t prefix = 0;
+    int left = P.K;             // how many are wanted of those that begin with prefix
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int b = tid; b < 256; b += threads) s_bins[b] = 0;
+        __syncthreads();
+        each([&](float x, int) {
+            const uint32_t o = order_of(x);
+            if (o != 0 && (shift == 24 || o >> (shift + 8) == prefix)) atomicAdd(&s_bins[o >> shift & 255u], 1);
+        });
+        __syncthreads();
+        if (tid == 0) {
+            int b = 255, above = 0;
+            while (b > 0 && above + s_bins[b] < left) above += s_bins[b--];
+            s_prefix = prefix << 8 | uint32_t(b);
+            s_left = left - above;
+        }
+        __syncthreads();
+        prefix = s_prefix;
+        left = s_left;
+        __syncthreads();
+    }
+    // (prefix 0: fewer than K above -inf)
+    if (tid == 0) *s_count = 0;
+    __syncthreads();
+    each([&](float x, int i) {
+        if (order_of(x) > prefix) s_out[atomicAdd(s_count, 1)] = make_key(x, i);
+    });
+    __syncthreads();
+    int at = *s_count;
+    __syncthreads();
+    if (prefix == 0) return at;
+    // equals, in the order of the row: edge elements before the words, words a
+    // round of the threads at a time, those behind them
+    const int end = at + left;
+    auto round = [&](int n, auto&& put) {        // n: this thread's
+        int before = n;
+#pragma unroll
+        for (int off = 1; off < 32; off *= 2) {
+            const int o = __shfl_up_sync(0xffffffffu, before, off);
+            if (lane >= off) before += o;
+        }
+        if (lane == 31) s_warp[warp] = before;
+        __syncthreads();
+        int sum = 0, from = 0;
+        for (int w = 0; w < threads / 32; ++w) {
+            if (w == warp) from = sum;
+            sum += s_warp[w];
+        }
+        put(at + from + before - n);
+        at += sum;
+        __syncthreads();
+    };
+    const bool is_edge = edge >= 0 && order_of(edge_x) == prefix;
+    auto edges = [&](bool mine) {
+        round(mine ? 1 : 0, [&](int p) {
+            if (mine && p < end) s_out[p] = make_key(edge_x, edge);
+        });
+    };
+    edges(is_edge && edge < in.at(w0));
+    for (int base = w0; base < w1 && at < end; base += threads) {
+        const int w = base + tid;
+        unsigned is = 0;
+        Word<T> v;
+        if (w < w1) {
+            v = body[w];
+#pragma unroll
+            for (int e = 0; e < N; ++e) is |= order_of(to_float(v.x[e])) == prefix ? 1u << e : 0u;
+        }
+        round(__popc(is), [&](int p) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (is >> e & 1u) {
+                    if (p < end) s_out[p] = make_key(to_float(v.x[e]), in.at(w) + e);
+                    ++p;
+                }
+        });
+    }
+    if (at < end) edges(is_edge && edge >= in.at(w0));
+    return min(at, end);
+}
+
+// A thread takes its CTA's words in turn, four at a time: the softmax sums are
+// its own, with its own running maximum.  For the K largest it keeps no more than
+// the largest element of each of up to 32 buckets of its words.  Once the slice is
+// through, each warp has ceil(K / warps) lanes whose largest elements are at least
+// so and so large, so the least of those, over the warps, is no larger than the
+// K-th of all; the few buckets that reach it are read again (from L2), and the
+// elements that do, 1.5 K or so, are ranked by counting.  So the pass itself does
+// hardly more than without the K (sorted lists that are kept up to date on the way
+// took 2.5 times as long at 64 of 100003, for their instructions).  Rows with more
+// candidates than there is room for (equal elements; an order that leaves a warp
+// only small ones) take `select`, a radix selection by further reads.
+template <class T, bool TOP>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScoreParams P) {
+    constexpr int N = Word<T>::N, U = 4;
+    extern __shared__ __align__(16) float s_bucket[];       // [bucket][thread]
     __shared__ Sums s_sums[kMaxWarps], s_cta[kMaxCluster];
-    __shared__ volatile float s_known[kMaxWarps];
-    __shared__ int s_held[kMaxWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = int(blockDim.x) >> 5;
-    Key *s_keys = reinterpret_cast<Key*>(s_places), *s_lists = s_keys + warps * CAP / 2;
+    __shared__ float s_known[kMaxWarps];
+    __shared__ int s_count;
+    __shared__ Key s_cand[TOP ? kCandidates : 1], s_best[TOP ? kMaxTop : 1];
+    const int tid = threadIdx.x, threads = int(blockDim.x), warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
     const int log2_C = __popc(C - 1);       // (C is a power of two)
     const long row = blockIdx.x >> log2_C;
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    if (lane == 0) s_held[warp] = 0;
-    __syncwarp();
+    if (TOP) {
+        if (tid == 0) s_count = 0;
+        for (int k = tid; k < P.K; k += threads) s_best[k] = 0;
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -307,144 +330,144 @@ __global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams
     const int w0 = int(long(in.words) * rank >> log2_C), w1 = int(long(in.words) * (rank + 1) >> log2_C);
     const float c = P.c;
     const float2 c2 = make_float2(c, c);
-    LaneSums sums;
-    Keys<RR> list;
-#pragma unroll
-    for (int r = 0; r < RR; ++r) list.k[r] = 0;
-    int* buf = s_places + warp * CAP;
-    float bound = kNone, own = kNone;
-    // the warps whose every lane has elements, and the lanes of each that the
-    // bound goes by (more than there are: no bound)
-    const int full = min(warps, (w1 - w0) / 32), share = full > 0 ? (P.K + full - 1) / full : 33;
-
-    auto offer = [&](float x, int i) {
-        if (x > bound) buf[atomicAdd(&s_held[warp], 1)] = i;
-    };
-    // the buffer's last 32 R into the list, until no more than `left` are in it
-    auto flush = [&](int left) {
-        __syncwarp();
-        int held = *const_cast<volatile int*>(&s_held[warp]);
-        if (held <= left) return;
-        while (held > left) {
-            Keys<RR> batch;
-            const int from = max(0, held - 32 * RR);
-#pragma unroll
-            for (int r = 0; r < RR; ++r) {
-                const int b = from + r * 32 + lane, i = b < held ? buf[b] : -1;
-                batch.k[r] = i >= 0 ? make_key(to_float(in.x[i]), i) : 0;
-            }
-            held = from;
-            batch.sort(lane);
-            list.merge(batch, lane);
-        }
-        own = key_value(list.nth(P.K - 1));
-        if (lane == 0) s_held[warp] = held;
-        __syncwarp();
-    };
-    // elements that are not in words: before the first, behind the last
-    auto single = [&](int i, bool is) {
-        const float x = is ? to_float(in.x[i]) : kNone;
-        sums.rise(x, c);
-        if (is) sums.add<true>(make_float2(x, kNone), sums.minus_ref(), c2);
-        if constexpr (TOP) {
-            if (is) offer(x, i);
-        }
-    };
-
-    if (rank == 0 && warp == 0) single(lane, lane < in.head);
     const Word<T>* body = in.body();
-    int look = 0;
-    for (int base = w0; base < w1 || look == 0; base += 32 * warps * U, ++look) {
+    const int per_look = threads * U, looks = (w1 - w0 + per_look - 1) / per_look, per_bucket = (looks + kBuckets - 1) / kBuckets;
+    LaneSums sums;
+    // the slice's edge elements, one to a thread: those before the row's first
+    // word, those behind its last
+    const int heads = rank == 0 ? in.head : 0, tails = rank == C - 1 ? in.tail : 0;
+    const int edge = tid < heads ? tid : tid < heads + tails ? P.V - in.tail + tid - heads : -1;
+    float edge_x = kNone;
+    if (edge >= 0) {
+        edge_x = to_float(in.x[edge]);
+        sums.rise(edge_x, c);
+        sums.add<true>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
+    }
+    float bucket = kNone;
+    int in_bucket = 0;
+    float* s_mine = s_bucket + tid;
+    Key* s_inbox = reinterpret_cast<Key*>(s_bucket + P.buckets * threads);      // of the cluster's keys
+    for (int base = w0 + tid; base - tid < w1; base += per_look) {
         Word<T> words[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int w = base + u * 32 * warps + int(threadIdx.x);
+            const int w = base + u * threads;
             if (w < w1) words[u] = body[w];
             else
 #pragma unroll
                 for (int e = 0; e < N; ++e) words[u].x[e] = from_float<T>(kNone);
         }
-        float top[U], most = kNone;
+        float most = largest(words[0]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) most = fmaxf(most, top[u] = largest(words[u]));
+        for (int u = 1; u < U; ++u) most = fmaxf(most, largest(words[u]));
         sums.rise(most, c);
         const float2 minus = sums.minus_ref();
 #pragma unroll
         for (int u = 0; u < U; ++u) add_word<true>(sums, words[u], minus, c2);
         if constexpr (TOP) {
-            if ((look & (look + 1)) == 0 && share <= 32) {
-                const float mine = nth_of_lanes(sums.m, share, lane);
-                if (lane == 0) s_known[warp] = mine;
-                if (look == 0) __syncthreads();
-                float least = lane < full ? s_known[lane] : INFINITY;
-#pragma unroll
-                for (int off = kMaxWarps / 2; off > 0; off /= 2) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
-                bound = below(__shfl_sync(0xffffffffu, least, 0));
-            }
-            bound = fmaxf(bound, own);
-            if (__any_sync(0xffffffffu, most > bound)) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (top[u] > bound) {
-#pragma unroll
-                        for (int e = 0; e < N; ++e) offer(to_float(words[u].x[e]), in.at(base + u * 32 * warps + int(threadIdx.x)) + e);
-                    }
-                }
-                flush(32 * RR - 1);
+            bucket = fmaxf(bucket, most);
+            if (++in_bucket == per_bucket) {
+                *s_mine = bucket;
+                s_mine += threads;
+                bucket = kNone;
+                in_bucket = 0;
             }
         }
     }
-    if (rank == C - 1 && warp == 0) {
-        bound = fmaxf(bound, own);
-        single(P.V - in.tail + lane, lane < in.tail);
-    }
+    if (TOP && in_bucket) *s_mine = bucket;
 
     // lanes, warps, CTAs
-    Sums mine = sums.both();
+    auto joined = [&](Sums v) {          // over a warp
 #pragma unroll
-    for (int off = 16; off > 0; off /= 2) mine.join(mine.from(off), c);
+        for (int off = 16; off > 0; off /= 2) v.join(v.from(off), c);
+        return v;
+    };
+    const Sums mine = joined(sums.both());
     if (lane == 0) s_sums[warp] = mine;
-    // the lists of a power of two of places, pairs at a time
-    auto merge_all = [&](Key* at, int step, int n) {
-        for (int half = n / 2; half > 0; half /= 2) {
-            __syncthreads();
-            if (warp < half) {
-                Keys<RR> o;
-                o.get(at + (warp + half) * step, lane);
-                list.merge(o, lane);
-                if (half > 1) list.put(at + warp * step, lane);
+    if constexpr (TOP) {
+        // the warps whose every lane has elements
+        const int full = min(warps, (w1 - w0) / 32), share = full > 0 ? (P.K + full - 1) / full : 33;
+        if (share <= 32) {
+            const float known = nth_of_lanes(sums.m, share, lane);
+            if (lane == 0) s_known[warp] = known;
+        }
+        __syncthreads();
+        float bound = kNone;
+        if (share <= 32) {
+            bound = s_known[0];
+            for (int w = 1; w < full; ++w) bound = fminf(bound, s_known[w]);
+        }
+        auto candidate = [&](float x, int i) {
+            if (x >= bound && x > kNone) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kCandidates) s_cand[at] = make_key(x, i);
+            }
+        };
+        if (edge >= 0) candidate(edge_x, edge);
+        for (int b = 0; b * per_bucket < looks; ++b) {
+            const float top = s_bucket[b * threads + tid];
+            if (!(top >= bound && top > kNone)) continue;
+            for (int l = b * per_bucket; l < min(looks, (b + 1) * per_bucket); ++l) {
+                Word<T> words[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) words[u] = body[min(w0 + l * per_look + u * threads + tid, w1 - 1)];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int w = w0 + l * per_look + u * threads + tid;
+                    if (w >= w1 || !(largest(words[u]) >= bound)) continue;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) candidate(to_float(words[u].x[e]), in.at(w) + e);
+                }
             }
         }
-    };
-    if constexpr (TOP) {
-        flush(0);
-        __syncwarp();
-        list.put(s_keys + warp * (CAP / 2), lane);
-        merge_all(s_keys, CAP / 2, warps);
+        __syncthreads();
+        int found = s_count;
+        if (found > kCandidates) found = select<T>(P, in, w0, w1, edge, edge_x, s_cand, &s_count);
+        // ranks
+        for (int i = tid; i < found; i += threads) {
+            const Key k = s_cand[i];
+            int r = 0;
+#pragma unroll 4
+            for (int j = 0; j < found; ++j) r += s_cand[j] > k;
+            if (r < P.K) s_best[r] = k;
+        }
     }
     __syncthreads();
     if (C > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
         if (warp == 0) {
-            if (lane == 0) {
-                Sums all = s_sums[0];
-                for (int w = 1; w < warps; ++w) all.join(s_sums[w], c);
-                *cluster.map_shared_rank(&s_cta[rank], 0) = all;
-            }
-            if constexpr (TOP) list.put(cluster.map_shared_rank(s_lists + rank * 32 * RR, 0), lane);
+            const Sums all = joined(lane < warps ? s_sums[lane] : Sums{kNone, 0.f, 0.f});
+            if (lane == 0) *cluster.map_shared_rank(&s_cta[rank], 0) = all;
         }
+        if constexpr (TOP)
+            for (int k = tid; k < P.K; k += threads) *cluster.map_shared_rank(s_inbox + rank * P.K + k, 0) = s_best[k];
         cluster.sync();
         if (rank != 0) return;
         if constexpr (TOP) {
-            if (warp < C) list.get(s_lists + warp * 32 * RR, lane);
-            merge_all(s_lists, 32 * RR, C);
+            // each CTA's are in order: those of the others before a key by bisection
+            for (int i = tid; i < C * P.K; i += threads) {
+                const Key k = s_inbox[i];
+                const int own = i / P.K;
+                int r = i - own * P.K;
+                if (k == 0) continue;
+                for (int o = 0; o < C && r < P.K; ++o) {
+                    if (o == own) continue;
+                    int lo = 0, hi = P.K;
+                    while (lo < hi) {
+                        const int mid = (lo + hi) >> 1;
+                        if (s_inbox[o * P.K + mid] > k) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    r += lo;
+                }
+                if (r < P.K) s_cand[r] = k;
+            }
+            __syncthreads();
         }
     }
     if (warp != 0) return;
     const int parts = C > 1 ? C : warps;
-    Sums all = lane < parts ? (C > 1 ? s_cta[lane] : s_sums[lane]) : Sums{kNone, 0.f, 0.f};
-#pragma unroll
-    for (int off = 16; off > 0; off /= 2) all.join(all.from(off), c);
+    const Sums all = joined(lane < parts ? (C > 1 ? s_cta[lane] : s_sums[lane]) : Sums{kNone, 0.f, 0.f});
     const bool empty = all.m == kNone && !(all.s != all.s);
     const float log_s = logf(all.s);
     auto logprob = [&](float x) { return empty ? kNone : (x - all.m) * P.inv_T - log_s; };
@@ -456,13 +479,20 @@ __global__ void __launch_bounds__(32 * kMaxWarps) score_kernel(const ScoreParams
         P.entropy[row] = empty ? 0.f : log_s - all.t / all.s * P.inv_T;
     }
     if constexpr (TOP) {
-        int found = 0;
+        // (of a cluster there are as many as its CTAs have found, or K)
+        int have = 0;
+        if (C > 1) {
+            for (int i = lane; i < C * P.K; i += 32) have += s_inbox[i] != 0;
 #pragma unroll
-        for (int r = 0; r < RR; ++r) {
-            const int p = r * 32 + lane;
-            const Key k = list.k[r];
+            for (int off = 16; off > 0; off /= 2) have += __shfl_xor_sync(0xffffffffu, have, off);
+            have = min(have, P.K);
+        }
+        int found = 0;
+        for (int base = 0; base < P.K; base += 32) {
+            const int p = base + lane;
+            const Key k = p >= P.K ? 0 : C == 1 ? s_best[p] : p < have ? s_cand[p] : 0;
             found += __popc(__ballot_sync(0xffffffffu, k != 0));
-            if (p < P.K && k != 0) {
+            if (k != 0) {
                 P.top[row * P.K + p] = logprob(key_value(k));
                 P.ids[row * P.K + p] = key_index(k);
             }
@@ -1029,29 +1059,28 @@ cudaError_t allow(splice::PerDevice<bool>& kept, Kernel kernel, size_t smem) {
     });
 }
 
-// CTAs that share a row: as many as fill the GPU, of 4096 elements at least.
+// CTAs that share a row: as many as fill the GPU, of 4096 elements at least.  (512
+// rows of 151936 fp32, 20 alternatives: alone 70 us, in fours 91.)
 int score_cluster(long rows, long V) {
     int C = 1;
-    while (C < kMaxCluster && rows * C < SCORE_CTAS && V >= 8192L * C) C *= 2;
+    while (C < kMaxCluster && rows * C < 512 && V >= 8192L * C) C *= 2;
     return C;
 }
 
-template <class T, int R>
-int scores(const ScoreParams& P, long rows, cudaStream_t st) {
-    using Shape = ScoreShape<T, R>;
+template <class T, bool TOP>
+int scores(ScoreParams P, long rows, cudaStream_t st) {
     static splice::PerDevice<bool> kept;
-    const cudaError_t e = allow(kept, score_kernel<T, R>, Shape::smem(kMaxWarps, kMaxCluster));
+    const cudaError_t e = allow(kept, score_kernel<T, TOP>, kBuckets * kMaxWarps * 32 * 4 + kMaxCluster * kMaxTop * sizeof(Key));
     if (e != cudaSuccess) return int(e);
     const int C = score_cluster(rows, P.V), warps = rows * C < 304 ? 16 : 8;
-    return launch(score_kernel<T, R>, rows * C, 32 * warps, Shape::smem(warps, C), C, P, st);
+    P.buckets = int(std::min(P.V / (Word<T>::N * 4L * 32 * warps * C) + 1, long(kBuckets)));
+    const size_t smem = TOP ? size_t(P.buckets) * warps * 32 * 4 + (C > 1 ? size_t(C) * P.K * sizeof(Key) : 0) : 0;
+    return launch(score_kernel<T, TOP>, rows * C, 32 * warps, smem, C, P, st);
 }
 
 template <class T>
 int scores(const ScoreParams& P, long rows, cudaStream_t st) {
-    if (P.K == 0) return scores<T, 0>(P, rows, st);
-    if (P.K <= 32) return scores<T, 1>(P, rows, st);
-    if (P.K <= 64) return scores<T, 2>(P, rows, st);
-    return scores<T, 4>(P, rows, st);
+    return P.K ? scores<T, true>(P, rows, st) : scores<T, false>(P, rows, st);
 }
 
 // Bytes of a CTA's slice with four, two and one CTA to an SM.
@@ -1135,7 +1164,7 @@ int decoder_token_scores(const void* x, int dtype, long stride, long rows, long 
     if (rows < 1 || rows > (1L << 27) || V < 1 || V > (1L << 30) || K < 0 || K > kMaxTop || K > V || !(inv_T > 0.0))
         return int(cudaErrorInvalidValue);
     const ScoreParams P{x, stride, int(V), K, float(inv_T), float(inv_T * kLog2e), static_cast<const int64_t*>(tokens), static_cast<float*>(logprobs),
-                        static_cast<float*>(entropy), static_cast<float*>(top), static_cast<int64_t*>(ids)};
+                        static_cast<float*>(entropy), static_cast<float*>(top), static_cast<int64_t*>(ids), 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == 0) return scores<float>(P, rows, st);
     if (dtype == 1) return scores<__nv_bfloat16>(P, rows, st);
