@@ -152,6 +152,7 @@ struct GradParams {
     int Tq, Tk, Tpad, Hq, Hkv, B;
     int tiles;                      // of 128 fixed rows
     int shares;
+    bool leads;                     // whether this pass is the first
     float scale, scale_log2;        // scale_log2 by keys: not below kLeastScale
     unsigned* err;
 };
@@ -238,21 +239,27 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    // By keys: a programmatic dependent of what makes the rows' statistics.  By
-    // queries: of the pass by keys, which it neither needs nor disturbs; its
-    // CTAs start as that one's leave (all of them have begun by then, and with
-    // that the statistics are there), and end after it.
-    if constexpr (C::BY_KEYS) asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = s_tmem;
     bool ok = true;
+    // The pass that leads is a programmatic dependent of what makes the rows'
+    // statistics, and of nothing else (that has waited for all that is before): the
+    // fixed operands are asked for first.  The others are dependents of the one
+    // before them, which they neither need nor disturb: their CTAs start as that
+    // one's leave (all of them have begun by then, and with that the statistics are
+    // there), and end after it.
+    auto statistics_are_there = [&]() {
+        if (P.leads) asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    };
 
     // One lane of its warp loads and one issues, all of the loop: with every lane
     // in it, and each copy and MMA under a test for the one, an MMA took 35 to 50
     // clocks to issue in place of 10, a wait on a complete barrier 140, and the
     // whole backward pass 1.2 times as long.
     if (warp == C::LOAD_WARP) {
-        if (tc::elect_one() && n > 0) {
+        const bool leader = tc::elect_one();
+        if (!leader || n == 0) statistics_are_there();
+        if (leader && n > 0) {
             auto wait = [&](uint32_t bar, uint32_t phase) { return tc::mbar_wait(bar, phase, &s_abort, P.err, kErrLoad); };
             if constexpr (C::F_LOADS > 0) {
                 tc::mbar_arrive_expect_tx(f_full, C::F_LOADS * C::F_BYTES);
@@ -262,6 +269,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
                     if (C::OUT_S && !C::T2) tma_load_4d(sbase + C::OFF_F2 + p * (kRows * 128), &tm_f2, p * 64, row0, head, batch, f_full);
                 }
             }
+            statistics_are_there();
             int j1 = 0, j2 = 0;      // blocks asked for
             int block = j0 % per, x_head = C::BY_KEYS ? head * G + j0 / per : head / G;
             Ring<C::R1> r1;
@@ -301,6 +309,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             for (int i = max(0, j2 - C::R2); ok && i < j2; ++i) ok = wait(x2_empty(i % C::R2), uint32_t(i / C::R2) & 1u);
         }
     } else if (warp == C::MMA_WARP) {
+        statistics_are_there();
         if (tc::elect_one() && n > 0) {
             constexpr uint32_t idesc_s = tc::idesc_bf16_f32(kRows, BX, false), idesc_sum = tc::idesc_bf16_f32(kRows, D, true);
             const uint64_t f1 = tc::sw128_desc(sbase, 16, 1024), f2 = tc::sw128_desc(sbase + C::OFF_F2, 16, 1024);
@@ -408,13 +417,6 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             tc::tc_fence_after();
             return is;
         };
-        float row_lse = INFINITY, row_delta = 0.f;
-        if constexpr (!C::BY_KEYS) {
-            const long stat = (long(batch) * P.Hq + head) * P.Tpad + row;
-            // (a row of one key: its weight is 1, whatever the scores are)
-            row_lse = row + shift == 0 ? INFINITY : __ldcg(P.lse2 + stat);
-            row_delta = __ldcg(P.delta + stat);
-        }
         if constexpr (C::T1 || C::T2) {
             // the fixed operands' rows into TMEM, a part of the dims to a warpgroup
             const bool in = row < (C::BY_KEYS ? P.Tk : P.Tq);
@@ -433,6 +435,14 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
             tc::tmem_wait_st();
             tc::tc_fence_before();
             tc::mbar_arrive(f_full);
+        }
+        statistics_are_there();
+        float row_lse = INFINITY, row_delta = 0.f;
+        if constexpr (!C::BY_KEYS) {
+            const long stat = (long(batch) * P.Hq + head) * P.Tpad + row;
+            // (a row of one key: its weight is 1, whatever the scores are)
+            row_lse = row + shift == 0 ? INFINITY : __ldcg(P.lse2 + stat);
+            row_delta = __ldcg(P.delta + stat);
         }
         for (int j = 0; j < n; ++j) {
             const int at = (first + (j0 + j) % per) * BX + wg * 32;
@@ -576,7 +586,7 @@ __global__ void __launch_bounds__(Cfg<D, PASS>::THREADS, 1)
     tc::tc_fence_after();
     if (warp == C::MMA_WARP) tc::tmem_dealloc(tmem, 512);
     // (what follows on the stream waits for this grid alone)
-    if constexpr (!C::BY_KEYS) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!P.leads) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // A number as three bf16 whose sum has all 24 bits of it (an infinity as the first).
@@ -645,18 +655,33 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// CTAs that share an item's blocks (host arithmetic only): the longest share
-// no longer than half as much again as an SM's part of all blocks, as long as
-// a share keeps 2.  (Rows whose blocks grow with the position: the last tile's
-// are the most, the average over the tiles half of it and more.)
-int shares_of(long longest, long total, int sms) {
-    int s = 1;
-    while (s < kMaxShares && longest >= 4L * s && longest * 2 * sms > 3L * total * s) s *= 2;
-    return s;
+// What one pass has to do: items, the blocks of the longest and of all.
+struct Work {
+    long items, longest, total;
+};
+
+// CTAs that share an item's blocks (host arithmetic only), for the least time in
+// blocks: the longest share, or everything shared out evenly, and once more a CTA's
+// own time (operands in, sums out, with shares traded: 8 blocks' and 15) where an
+// SM gets a second.  32 / 8 heads of 128 by keys, alone, in twos and fours: 1024
+// positions 73, 50, 60 us; 1500 107, 78, 98; 2048 146, 119, 142; 3000 234, 219,
+// 263; 4096 340, 361, 417 (of both passes).
+int shares_of(const Work& w, int sms) {
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= kMaxShares && (s == 1 || w.longest >= 2L * s); s *= 2) {
+        const double own = s > 1 ? 15 : 8, ctas = double(w.items) * s, longest = double(w.longest) / s + own;
+        const double time = ctas <= sms ? longest : std::max(longest, (double(w.total) + ctas * own) / sms) + own;
+        if (s == 1 || time < least) {
+            least = time;
+            best = s;
+        }
+    }
+    return best;
 }
 
 template <int D, int PASS>
-int launch(const CUtensorMap (&maps)[4], GradParams p, long longest, long total, cudaStream_t st) {
+int launch(const CUtensorMap (&maps)[4], GradParams p, const Work& w, bool leads, cudaStream_t st) {
     using C = Cfg<D, PASS>;
     static splice::PerDevice<int> kept;
     int sms = 0;
@@ -666,9 +691,10 @@ int launch(const CUtensorMap (&maps)[4], GradParams p, long longest, long total,
         return err;
     });
     if (e != cudaSuccess) return int(e);
-    p.shares = shares_of(longest, total, sms);
+    p.shares = shares_of(w, sms);
+    p.leads = leads;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(p.tiles) * unsigned(C::BY_KEYS ? p.Hkv : p.Hq) * unsigned(p.B) * unsigned(p.shares));
+    cfg.gridDim = dim3(unsigned(w.items * p.shares));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::smem(p.shares);
     cfg.stream = st;
@@ -750,40 +776,41 @@ int backward(const Args& a, cudaStream_t st) {
     p.p_batch = p.s_batch = long(a.Hkv) * a.Tk * D;
     p.tiles = (a.Tk + kRows - 1) / kRows;
     const int blocks = (a.Tq + BXK - 1) / BXK;
-    long longest = 0, total = 0;
+    Work keys{long(p.tiles) * a.Hkv * a.B, 0, 0}, queries{long(Tpad / kRows) * a.Hq * a.B, 0, 0};
     for (int t = 0; t < p.tiles; ++t) {
         const long n = long(G) * std::max(0, blocks - std::max(0, t * kRows - shift) / BXK);
-        longest = std::max(longest, n);
-        total += n;
+        keys.longest = std::max(keys.longest, n);
+        keys.total += n * a.Hkv * a.B;
     }
-    total *= long(a.Hkv) * a.B;
-    const CUtensorMap by_keys[4] = {fixed_k, fixed_v, block_q, block_o};
-    int e;
-    if constexpr (D == 256) {
-        e = launch<D, kValuesOnly>(by_keys, p, longest, total, st);
-        if (e == 0) e = launch<D, kKeysOnly>(by_keys, p, longest, total, st);
-    } else {
-        e = launch<D, kKeys>(by_keys, p, longest, total, st);
-    }
-    if (e != 0) return e;
-    // by queries
-    p.scale_log2 = scale_log2;
-    p.f1 = a.q;
-    p.f2 = a.dout;
-    p.s_sum = a.dq;
-    p.s_row = long(a.Hq) * D;
-    p.s_head = D;
-    p.s_batch = long(a.Tq) * a.Hq * D;
-    p.tiles = Tpad / kRows;
-    longest = total = 0;
-    for (int t = 0; t < p.tiles; ++t) {
+    for (int t = 0; t < Tpad / kRows; ++t) {
         const long n = std::max(0, (std::min(a.Tk, (t + 1) * kRows + shift) + BX - 1) / BX);
-        longest = std::max(longest, n);
-        total += n;
+        queries.longest = std::max(queries.longest, n);
+        queries.total += n * a.Hq * a.B;
     }
-    total *= long(a.Hq) * a.B;
+    // The pass of the longer items leads: the other's fill the SMs that it leaves.
+    // (Blocks by keys of 128 dims are half as long.)
+    const bool keys_lead = keys.longest * BXK >= queries.longest * BX;
+    const CUtensorMap by_keys[4] = {fixed_k, fixed_v, block_q, block_o};
+    GradParams r = p;           // by queries
+    r.scale_log2 = scale_log2;
+    r.f1 = a.q;
+    r.f2 = a.dout;
+    r.s_sum = a.dq;
+    r.s_row = long(a.Hq) * D;
+    r.s_head = D;
+    r.s_batch = long(a.Tq) * a.Hq * D;
+    r.tiles = Tpad / kRows;
     const CUtensorMap by_queries[4] = {fixed_q, fixed_o, block_k, block_v};
-    return launch<D, kQueries>(by_queries, p, longest, total, st);
+    int e = 0;
+    if (!keys_lead) e = launch<D, kQueries>(by_queries, r, queries, true, st);
+    if constexpr (D == 256) {
+        if (e == 0) e = launch<D, kValuesOnly>(by_keys, p, keys, keys_lead, st);
+        if (e == 0) e = launch<D, kKeysOnly>(by_keys, p, keys, false, st);
+    } else {
+        if (e == 0) e = launch<D, kKeys>(by_keys, p, keys, keys_lead, st);
+    }
+    if (keys_lead && e == 0) e = launch<D, kQueries>(by_queries, r, queries, false, st);
+    return e;
 }
 
 }  // namespace
