@@ -70,6 +70,13 @@ struct Row {
     __device__ int at(int word) const { return head + word * Word<T>::N; }
 };
 
+// The largest of a warp's; NaN is passed over.
+__device__ __forceinline__ float max_of_warp(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // sum e^(z - m) and sum e^(z - m) (x - m) of elements whose largest x is m, in
 // fp32.  Elements of -inf weigh nothing; a NaN or +inf makes s NaN (m passes
 // over NaN).  Differences x - m come before the product with 1 / T: masks of
@@ -77,27 +84,24 @@ struct Row {
 struct Sums {
     float m, s, t;
 
-    __device__ __forceinline__ void join(const Sums& o, float c) {
-        const float to = fmaxf(m, o.m);
-        Sums a = *this, b = o;
-        a.shift(to, c);
-        b.shift(to, c);
-        m = to;
-        s = a.s + b.s;
-        t = a.t + b.t;
+    // of a warp
+    __device__ __forceinline__ Sums joined(float c) const {
+        Sums a = *this;
+        a.shift(max_of_warp(m), c);
+#pragma unroll
+        for (int off = 16; off > 0; off /= 2) {
+            a.s += __shfl_xor_sync(0xffffffffu, a.s, off);
+            a.t += __shfl_xor_sync(0xffffffffu, a.t, off);
+        }
+        return a;
     }
     __device__ __forceinline__ void shift(float to, float c) {
-        if (m == kNone || m == to) return;          // (-inf: s is 0, or NaN)
-        const float by = m - to, f = ex2(by * c);
-        t = f == 0.f ? 0.f : f * fmaf(by, s, t);    // (by may be the type's lowest value)
-        s *= f;
-    }
-    __device__ __forceinline__ Sums from(int lane_mask) const {
-        Sums o;
-        o.m = __shfl_xor_sync(0xffffffffu, m, lane_mask);
-        o.s = __shfl_xor_sync(0xffffffffu, s, lane_mask);
-        o.t = __shfl_xor_sync(0xffffffffu, t, lane_mask);
-        return o;
+        if (m != kNone && m != to) {                // (-inf: s is 0, or NaN)
+            const float by = m - to, f = ex2(by * c);
+            t = f == 0.f ? 0.f : f * fmaf(by, s, t);    // (by may be the type's lowest value)
+            s *= f;
+        }
+        m = to;
     }
 };
 
@@ -299,30 +303,28 @@ __device__ __noinline__ int select(const ScoreParams& P, const Row<T>& in, int w
 // the largest element of each of up to 32 buckets of its words.  Once the slice is
 // through, each warp has ceil(K / warps) lanes whose largest elements are at least
 // so and so large, so the least of those, over the warps, is no larger than the
-// K-th of all; the few buckets that reach it are read again (from L2), and the
-// elements that do, 1.5 K or so, are ranked by counting.  So the pass itself does
-// hardly more than without the K (sorted lists that are kept up to date on the way
-// took 2.5 times as long at 64 of 100003, for their instructions).  Rows with more
-// candidates than there is room for (equal elements; an order that leaves a warp
-// only small ones) take `select`, a radix selection by further reads.
+// K-th of all; the few buckets that reach it are listed and read again (from L2),
+// a word to a thread, and the elements that do, 1.5 K or so, are ranked by counting.
+// (Each thread reading its own buckets, one after another, and a rank to a thread
+// took 1.25 to 1.4 times as long in all.)  Rows with more candidates than there is
+// room for (equal elements; an order that leaves a warp only small ones) take
+// `select`, a radix selection by further reads.
 template <class T, bool TOP>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScoreParams P) {
     constexpr int N = Word<T>::N, U = 4;
     extern __shared__ __align__(16) float s_bucket[];       // [bucket][thread]
     __shared__ Sums s_sums[kMaxWarps], s_cta[kMaxCluster];
     __shared__ float s_known[kMaxWarps];
-    __shared__ int s_count;
-    __shared__ Key s_cand[TOP ? kCandidates : 1], s_best[TOP ? kMaxTop : 1];
+    __shared__ int s_count, s_listed;
+    __shared__ Key s_cand[TOP ? kCandidates : 1];
+    __shared__ uint16_t s_list[TOP ? kCandidates : 1];
     const int tid = threadIdx.x, threads = int(blockDim.x), warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
     const int log2_C = __popc(C - 1);       // (C is a power of two)
     const long row = blockIdx.x >> log2_C;
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    if (TOP) {
-        if (tid == 0) s_count = 0;
-        for (int k = tid; k < P.K; k += threads) s_best[k] = 0;
-    }
+    if (TOP && tid == 0) s_count = s_listed = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -343,6 +345,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
         sums.rise(edge_x, c);
         sums.add<true>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
     }
+    const int64_t token = rank == 0 && P.tokens ? P.tokens[row] : 0;       // (on its way until it is needed)
     float bucket = kNone;
     int in_bucket = 0;
     float* s_mine = s_bucket + tid;
@@ -376,19 +379,17 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     }
     if (TOP && in_bucket) *s_mine = bucket;
 
+    const float token_x = rank == 0 && warp == 0 && token >= 0 && token < P.V ? to_float(in.x[token]) : NAN;
+
     // lanes, warps, CTAs
-    auto joined = [&](Sums v) {          // over a warp
-#pragma unroll
-        for (int off = 16; off > 0; off /= 2) v.join(v.from(off), c);
-        return v;
-    };
-    const Sums mine = joined(sums.both());
+    const Sums mine = sums.both().joined(c);
     if (lane == 0) s_sums[warp] = mine;
+    int found = 0;              // of the CTA's largest, above -inf, in any order
     if constexpr (TOP) {
         // the warps whose every lane has elements
         const int full = min(warps, (w1 - w0) / 32), share = full > 0 ? (P.K + full - 1) / full : 33;
         if (share <= 32) {
-            const float known = nth_of_lanes(sums.m, share, lane);
+            const float known = share == 1 ? mine.m : nth_of_lanes(sums.m, share, lane);
             if (lane == 0) s_known[warp] = known;
         }
         __syncthreads();
@@ -397,6 +398,15 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
             bound = s_known[0];
             for (int w = 1; w < full; ++w) bound = fminf(bound, s_known[w]);
         }
+        const int filled = (looks + per_bucket - 1) / per_bucket;
+#pragma unroll 4
+        for (int b = 0; b < filled; ++b) {
+            const float top = s_bucket[b * threads + tid];
+            if (top >= bound && top > kNone) {
+                const int at = atomicAdd(&s_listed, 1);
+                if (at < kCandidates) s_list[at] = uint16_t(b * threads + tid);
+            }
+        }
         auto candidate = [&](float x, int i) {
             if (x >= bound && x > kNone) {
                 const int at = atomicAdd(&s_count, 1);
@@ -404,46 +414,68 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
             }
         };
         if (edge >= 0) candidate(edge_x, edge);
-        for (int b = 0; b * per_bucket < looks; ++b) {
-            const float top = s_bucket[b * threads + tid];
-            if (!(top >= bound && top > kNone)) continue;
-            for (int l = b * per_bucket; l < min(looks, (b + 1) * per_bucket); ++l) {
-                Word<T> words[U];
+        __syncthreads();
+        const int listed = s_listed, span = per_bucket * U;       // (more: there are more candidates than that, too)
+        for (int i = tid; i < listed * span && listed <= kCandidates; i += threads) {
+            const int of = s_list[i / span], k = i % span, b = of / threads;
+            const int w = w0 + b * per_bucket * per_look + k * threads + of % threads;
+            if (w >= w1) continue;
+            const Word<T> word = body[w];
+            if (!(largest(word) >= bound)) continue;
 #pragma unroll
-                for (int u = 0; u < U; ++u) words[u] = body[min(w0 + l * per_look + u * threads + tid, w1 - 1)];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int w = w0 + l * per_look + u * threads + tid;
-                    if (w >= w1 || !(largest(words[u]) >= bound)) continue;
-#pragma unroll
-                    for (int e = 0; e < N; ++e) candidate(to_float(words[u].x[e]), in.at(w) + e);
-                }
-            }
+            for (int e = 0; e < N; ++e) candidate(to_float(word.x[e]), in.at(w) + e);
         }
         __syncthreads();
-        int found = s_count;
+        found = listed <= kCandidates ? s_count : kCandidates + 1;
         if (found > kCandidates) found = select<T>(P, in, w0, w1, edge, edge_x, s_cand, &s_count);
-        // ranks
-        for (int i = tid; i < found; i += threads) {
-            const Key k = s_cand[i];
+    } else {
+        __syncthreads();
+    }
+    // The candidates' ranks by counting, as many lanes to each as there are
+    auto ranked = [&](auto&& put) {
+        int log2 = 0;
+        while (log2 < 5 && found << (log2 + 1) <= threads) ++log2;
+        for (int base = 0; base < found << log2; base += threads) {
+            const int i = (base + tid) >> log2;
+            const Key k = i < found ? s_cand[i] : 0;
             int r = 0;
 #pragma unroll 4
-            for (int j = 0; j < found; ++j) r += s_cand[j] > k;
-            if (r < P.K) s_best[r] = k;
+            for (int j = tid & ((1 << log2) - 1); j < found; j += 1 << log2) r += s_cand[j] > k;
+            for (int off = 1 << log2 >> 1; off > 0; off /= 2) r += __shfl_xor_sync(0xffffffffu, r, off);
+            if (k != 0 && r < P.K && (tid & ((1 << log2) - 1)) == 0) put(r, k);
         }
-    }
-    __syncthreads();
+    };
     if (C > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (every CTA has begun)
         if (warp == 0) {
-            const Sums all = joined(lane < warps ? s_sums[lane] : Sums{kNone, 0.f, 0.f});
+            const Sums all = (lane < warps ? s_sums[lane] : Sums{kNone, 0.f, 0.f}).joined(c);
             if (lane == 0) *cluster.map_shared_rank(&s_cta[rank], 0) = all;
         }
-        if constexpr (TOP)
-            for (int k = tid; k < P.K; k += threads) *cluster.map_shared_rank(s_inbox + rank * P.K + k, 0) = s_best[k];
+        if constexpr (TOP) {
+            Key* to = cluster.map_shared_rank(s_inbox + rank * P.K, 0);
+            ranked([&](int r, Key k) { to[r] = k; });
+            for (int k = found + tid; k < P.K; k += threads) to[k] = 0;
+        }
         cluster.sync();
         if (rank != 0) return;
-        if constexpr (TOP) {
+    }
+    const int parts = C > 1 ? C : warps;
+    const Sums all = (lane < parts ? (C > 1 ? s_cta[lane] : s_sums[lane]) : Sums{kNone, 0.f, 0.f}).joined(c);
+    const bool empty = all.m == kNone && !(all.s != all.s);
+    const float log_s = logf(all.s);
+    auto logprob = [&](float x) { return empty ? kNone : (x - all.m) * P.inv_T - log_s; };
+    if (tid == 0) {
+        if (P.tokens) P.logprobs[row] = token < 0 ? 0.f : token >= P.V ? NAN : logprob(token_x);
+        P.entropy[row] = empty ? 0.f : log_s - all.t / all.s * P.inv_T;
+    }
+    if constexpr (TOP) {
+        auto put = [&](int r, Key k) {
+            P.top[row * P.K + r] = logprob(key_value(k));
+            P.ids[row * P.K + r] = key_index(k);
+        };
+        if (C == 1) {
+            ranked(put);
+        } else {
             // each CTA's are in order: those of the others before a key by bisection
             for (int i = tid; i < C * P.K; i += threads) {
                 const Key k = s_inbox[i];
@@ -460,44 +492,16 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
                     }
                     r += lo;
                 }
-                if (r < P.K) s_cand[r] = k;
-            }
-            __syncthreads();
-        }
-    }
-    if (warp != 0) return;
-    const int parts = C > 1 ? C : warps;
-    const Sums all = joined(lane < parts ? (C > 1 ? s_cta[lane] : s_sums[lane]) : Sums{kNone, 0.f, 0.f});
-    const bool empty = all.m == kNone && !(all.s != all.s);
-    const float log_s = logf(all.s);
-    auto logprob = [&](float x) { return empty ? kNone : (x - all.m) * P.inv_T - log_s; };
-    if (lane == 0) {
-        if (P.tokens) {
-            const int64_t tok = P.tokens[row];
-            P.logprobs[row] = tok < 0 ? 0.f : tok >= P.V ? NAN : logprob(to_float(in.x[tok]));
-        }
-        P.entropy[row] = empty ? 0.f : log_s - all.t / all.s * P.inv_T;
-    }
-    if constexpr (TOP) {
-        // (of a cluster there are as many as its CTAs have found, or K)
-        int have = 0;
-        if (C > 1) {
-            for (int i = lane; i < C * P.K; i += 32) have += s_inbox[i] != 0;
-#pragma unroll
-            for (int off = 16; off > 0; off /= 2) have += __shfl_xor_sync(0xffffffffu, have, off);
-            have = min(have, P.K);
-        }
-        int found = 0;
-        for (int base = 0; base < P.K; base += 32) {
-            const int p = base + lane;
-            const Key k = p >= P.K ? 0 : C == 1 ? s_best[p] : p < have ? s_cand[p] : 0;
-            found += __popc(__ballot_sync(0xffffffffu, k != 0));
-            if (k != 0) {
-                P.top[row * P.K + p] = logprob(key_value(k));
-                P.ids[row * P.K + p] = key_index(k);
+                if (r < P.K) put(r, k);
             }
         }
+        if (warp != 0) return;
         // fewer than K above -inf: the first of the others
+        if (C > 1) {
+            found = 0;
+            for (int i = lane; i < C * P.K; i += 32) found += s_inbox[i] != 0;
+            found = int(__reduce_add_sync(0xffffffffu, unsigned(found)));
+        }
         for (int base = 0; found < P.K && base < P.V; base += 32) {
             const bool is = base + lane < P.V && !(to_float(in.x[min(base + lane, P.V - 1)]) > kNone);
             const unsigned who = __ballot_sync(0xffffffffu, is);
