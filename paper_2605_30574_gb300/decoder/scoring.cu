@@ -17,6 +17,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../csrc/per_device.h"
 #include "../csrc/tc_ptx.cuh"
@@ -137,12 +138,16 @@ struct LaneSums {
     __device__ __forceinline__ Sums both() const { return Sums{m, s.x + s.y, t.x + t.y}; }
 };
 
+// (NaN is passed over; pairs of two bytes each take one instruction)
 template <class T>
 __device__ __forceinline__ float largest(const Word<T>& w) {
-    float m = to_float(w.x[0]);
-#pragma unroll
-    for (int e = 1; e < Word<T>::N; ++e) m = fmaxf(m, to_float(w.x[e]));
-    return m;
+    if constexpr (sizeof(T) == 2) {
+        using T2 = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+        const T2 *v = reinterpret_cast<const T2*>(&w), m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+        return to_float(__hmax(m.x, m.y));
+    } else {
+        return fmaxf(fmaxf(w.x[0], w.x[1]), fmaxf(w.x[2], w.x[3]));
+    }
 }
 
 template <bool WITH_T, class T>
@@ -317,7 +322,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     __shared__ float s_known[kMaxWarps];
     __shared__ int s_count, s_listed;
     __shared__ Key s_cand[TOP ? kCandidates : 1];
-    __shared__ uint16_t s_list[TOP ? kCandidates : 1];
+    __shared__ int s_list[TOP ? kCandidates : 1];
     const int tid = threadIdx.x, threads = int(blockDim.x), warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
@@ -333,7 +338,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     const float c = P.c;
     const float2 c2 = make_float2(c, c);
     const Word<T>* body = in.body();
-    const int per_look = threads * U, looks = (w1 - w0 + per_look - 1) / per_look, per_bucket = (looks + kBuckets - 1) / kBuckets;
+    const int per_look = threads * U, looks = (w1 - w0 + per_look - 1) / per_look;
+    int log2_bucket = 0;            // of the looks to a bucket
+    while (looks > kBuckets << log2_bucket) ++log2_bucket;
     LaneSums sums;
     // the slice's edge elements, one to a thread: those before the row's first
     // word, those behind its last
@@ -350,16 +357,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     int in_bucket = 0;
     float* s_mine = s_bucket + tid;
     Key* s_inbox = reinterpret_cast<Key*>(s_bucket + P.buckets * threads);      // of the cluster's keys
-    for (int base = w0 + tid; base - tid < w1; base += per_look) {
-        Word<T> words[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int w = base + u * threads;
-            if (w < w1) words[u] = body[w];
-            else
-#pragma unroll
-                for (int e = 0; e < N; ++e) words[u].x[e] = from_float<T>(kNone);
-        }
+    auto take = [&](const Word<T>(&words)[U]) {
         float most = largest(words[0]);
 #pragma unroll
         for (int u = 1; u < U; ++u) most = fmaxf(most, largest(words[u]));
@@ -369,13 +367,32 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
         for (int u = 0; u < U; ++u) add_word<true>(sums, words[u], minus, c2);
         if constexpr (TOP) {
             bucket = fmaxf(bucket, most);
-            if (++in_bucket == per_bucket) {
+            if (++in_bucket == 1 << log2_bucket) {
                 *s_mine = bucket;
                 s_mine += threads;
                 bucket = kNone;
                 in_bucket = 0;
             }
         }
+    };
+    int base = w0 + tid;
+    for (; base - tid + per_look <= w1; base += per_look) {
+        Word<T> words[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) words[u] = body[base + u * threads];
+        take(words);
+    }
+    if (base - tid < w1) {
+        Word<T> words[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int w = base + u * threads;
+            if (w < w1) words[u] = body[w];
+            else
+#pragma unroll
+                for (int e = 0; e < N; ++e) words[u].x[e] = from_float<T>(kNone);
+        }
+        take(words);
     }
     if (TOP && in_bucket) *s_mine = bucket;
 
@@ -393,37 +410,49 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
             if (lane == 0) s_known[warp] = known;
         }
         __syncthreads();
-        float bound = kNone;
+        float bound = -3.4028235e38f;       // (what is above -inf)
         if (share <= 32) {
-            bound = s_known[0];
-            for (int w = 1; w < full; ++w) bound = fminf(bound, s_known[w]);
+            float least = s_known[0];
+            for (int w = 1; w < full; ++w) least = fminf(least, s_known[w]);
+            bound = fmaxf(bound, least);
         }
-        const int filled = (looks + per_bucket - 1) / per_bucket;
-#pragma unroll 4
-        for (int b = 0; b < filled; ++b) {
-            const float top = s_bucket[b * threads + tid];
-            if (top >= bound && top > kNone) {
-                const int at = atomicAdd(&s_listed, 1);
-                if (at < kCandidates) s_list[at] = uint16_t(b * threads + tid);
-            }
+        unsigned reach = 0;
+#pragma unroll 8
+        for (int b = 0; b << log2_bucket < looks; ++b) reach |= s_bucket[b * threads + tid] >= bound ? 1u << b : 0u;
+        if (reach) {
+            int at = atomicAdd(&s_listed, __popc(reach));
+            for (; reach && at < kCandidates; reach &= reach - 1) s_list[at++] = ((__ffs(reach) - 1) << log2_bucket) * per_look + tid;
         }
-        auto candidate = [&](float x, int i) {
-            if (x >= bound && x > kNone) {
-                const int at = atomicAdd(&s_count, 1);
-                if (at < kCandidates) s_cand[at] = make_key(x, i);
-            }
-        };
-        if (edge >= 0) candidate(edge_x, edge);
+        if (edge_x >= bound) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kCandidates) s_cand[at] = make_key(edge_x, edge);
+        }
         __syncthreads();
-        const int listed = s_listed, span = per_bucket * U;       // (more: there are more candidates than that, too)
-        for (int i = tid; i < listed * span && listed <= kCandidates; i += threads) {
-            const int of = s_list[i / span], k = i % span, b = of / threads;
-            const int w = w0 + b * per_bucket * per_look + k * threads + of % threads;
-            if (w >= w1) continue;
-            const Word<T> word = body[w];
-            if (!(largest(word) >= bound)) continue;
+        // (more listed: there are more candidates than that, too)
+        const int listed = s_listed, log2_span = log2_bucket + 2, all = listed <= kCandidates ? listed << log2_span : 0;
+        static_assert(U == 4);
+        for (int base = tid; base < all; base += U * threads) {
+            Word<T> words[U];
+            int w[U];
 #pragma unroll
-            for (int e = 0; e < N; ++e) candidate(to_float(word.x[e]), in.at(w) + e);
+            for (int u = 0; u < U; ++u) {
+                const int i = base + u * threads;
+                w[u] = i < all ? w0 + s_list[i >> log2_span] + (i & ((1 << log2_span) - 1)) * threads : w1;
+                if (w[u] < w1) words[u] = body[w[u]];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (w[u] >= w1 || !(largest(words[u]) >= bound)) continue;
+                unsigned is = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) is |= to_float(words[u].x[e]) >= bound ? 1u << e : 0u;
+                int at = atomicAdd(&s_count, __popc(is));
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (is >> e & 1u && at < kCandidates) s_cand[at] = make_key(to_float(words[u].x[e]), in.at(w[u]) + e);
+                    at += is >> e & 1u;
+                }
+            }
         }
         __syncthreads();
         found = listed <= kCandidates ? s_count : kCandidates + 1;
@@ -431,18 +460,19 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     } else {
         __syncthreads();
     }
-    // The candidates' ranks by counting, as many lanes to each as there are
+    // The candidates' ranks by counting, as many lanes to each as there are.  (A
+    // bitonic sort takes as long from 250 on, and longer below.)
     auto ranked = [&](auto&& put) {
         int log2 = 0;
         while (log2 < 5 && found << (log2 + 1) <= threads) ++log2;
         for (int base = 0; base < found << log2; base += threads) {
-            const int i = (base + tid) >> log2;
+            const int i = (base + tid) >> log2, part = tid & ((1 << log2) - 1);
             const Key k = i < found ? s_cand[i] : 0;
             int r = 0;
-#pragma unroll 4
-            for (int j = tid & ((1 << log2) - 1); j < found; j += 1 << log2) r += s_cand[j] > k;
+#pragma unroll 8
+            for (int j = part; j < found; j += 1 << log2) r += s_cand[j] > k;
             for (int off = 1 << log2 >> 1; off > 0; off /= 2) r += __shfl_xor_sync(0xffffffffu, r, off);
-            if (k != 0 && r < P.K && (tid & ((1 << log2) - 1)) == 0) put(r, k);
+            if (k != 0 && r < P.K && part == 0) put(r, k);
         }
     };
     if (C > 1) {
