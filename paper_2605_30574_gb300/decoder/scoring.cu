@@ -460,19 +460,38 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
     } else {
         __syncthreads();
     }
-    // The candidates' ranks by counting, as many lanes to each as there are.  (A
-    // bitonic sort takes as long from 250 on, and longer below.)
+    // The candidates' ranks by counting: four to as many lanes as there are, up to
+    // eight, as reading the others is what it costs.  (A bitonic sort takes longer.)
     auto ranked = [&](auto&& put) {
+        constexpr int B = 4;
+        const int groups = (found + B - 1) / B;
         int log2 = 0;
-        while (log2 < 5 && found << (log2 + 1) <= threads) ++log2;
-        for (int base = 0; base < found << log2; base += threads) {
-            const int i = (base + tid) >> log2, part = tid & ((1 << log2) - 1);
-            const Key k = i < found ? s_cand[i] : 0;
-            int r = 0;
-#pragma unroll 8
-            for (int j = part; j < found; j += 1 << log2) r += s_cand[j] > k;
-            for (int off = 1 << log2 >> 1; off > 0; off /= 2) r += __shfl_xor_sync(0xffffffffu, r, off);
-            if (k != 0 && r < P.K && part == 0) put(r, k);
+        while (log2 < 3 && groups << (log2 + 1) <= threads) ++log2;
+        for (int base = 0; base < groups << log2; base += threads) {
+            const int g = (base + tid) >> log2, part = tid & ((1 << log2) - 1);
+            Key k[B];
+            int r[B] = {};
+#pragma unroll
+            for (int i = 0; i < B; ++i) k[i] = g * B + i < found ? s_cand[g * B + i] : 0;
+#pragma unroll 4
+            for (int j = part; j < found; j += 1 << log2) {
+                const Key o = s_cand[j];
+#pragma unroll
+                for (int i = 0; i < B; ++i) r[i] += o > k[i];
+            }
+            // (two counts to a number)
+            int two[B / 2];
+#pragma unroll
+            for (int i = 0; i < B / 2; ++i) two[i] = r[2 * i] | r[2 * i + 1] << 16;
+            for (int off = 1 << log2 >> 1; off > 0; off /= 2)
+#pragma unroll
+                for (int i = 0; i < B / 2; ++i) two[i] += __shfl_xor_sync(0xffffffffu, two[i], off);
+            if (part == 0)
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const int at = i & 1 ? two[i / 2] >> 16 : two[i / 2] & 0xffff;
+                    if (k[i] != 0 && at < P.K) put(at, k[i]);
+                }
         }
     };
     if (C > 1) {
