@@ -1112,12 +1112,23 @@ cudaError_t allow(splice::PerDevice<bool>& kept, Kernel kernel, size_t smem) {
     });
 }
 
-// CTAs that share a row: as many as fill the GPU, of 4096 elements at least.  (512
-// rows of 151936 fp32, 20 alternatives: alone 70 us, in fours 91.)
-int score_cluster(long rows, long V) {
+// CTAs that share a row: as many as leave one to an SM, of 16384 elements at least
+// and with 256 alternatives in all at most, which one of them merges.  (151936 fp32,
+// 20 alternatives: 20 rows in twos, fours and eights 11.3, 9.4 and 9.8 us; 80 rows
+// alone, in twos and fours 13.5, 13.9 and 16; 512 rows 54, 62 and 72; one row with
+// 128 in twos and eights 11.7 and 22.9.)
+int score_cluster(long rows, long V, int K) {
     int C = 1;
-    while (C < kMaxCluster && rows * C < 512 && V >= 8192L * C) C *= 2;
+    while (C < kMaxCluster && rows * 2 * C <= 152 && V >= 32768L * C && 2 * C * K <= 256) C *= 2;
     return C;
+}
+
+// Warps of a CTA: 16 where it has an SM to itself and enough to read, or half of
+// one and much, else 8.  (Slices of 76, 100, 152, 200 KB with an SM each, 8 and 16
+// warps: 8.8 and 9.6 us, 9.7 and 10.1, 9.9 and 9.4, 11.7 and 10.8; 200 rows of 200
+// and 608 KB: 14.9 and 17.2, 35.4 and 27.4; 512 rows of 608 KB: 54 and 60.)
+int score_warps(long ctas, long slice_bytes) {
+    return ctas <= 152 && slice_bytes >= 112 * 1024 || ctas <= 304 && slice_bytes >= 400 * 1024 ? 16 : 8;
 }
 
 template <class T, bool TOP>
@@ -1125,7 +1136,7 @@ int scores(ScoreParams P, long rows, cudaStream_t st) {
     static splice::PerDevice<bool> kept;
     const cudaError_t e = allow(kept, score_kernel<T, TOP>, kBuckets * kMaxWarps * 32 * 4 + kMaxCluster * kMaxTop * sizeof(Key));
     if (e != cudaSuccess) return int(e);
-    const int C = score_cluster(rows, P.V), warps = rows * C < 304 ? 16 : 8;
+    const int C = score_cluster(rows, P.V, P.K), warps = score_warps(rows * C, P.V * long(sizeof(T)) / C);
     P.buckets = int(std::min(P.V / (Word<T>::N * 4L * 32 * warps * C) + 1, long(kBuckets)));
     const size_t smem = TOP ? size_t(P.buckets) * warps * 32 * 4 + (C > 1 ? size_t(C) * P.K * sizeof(Key) : 0) : 0;
     return launch(score_kernel<T, TOP>, rows * C, 32 * warps, smem, C, P, st);
