@@ -119,12 +119,12 @@ struct Cfg {
     static constexpr uint32_t COL_SUM = COL_F2 + (T2 ? D / 2 : 0), COL_S_SUM = COL_SUM + (OUT_P ? D : 0);
     static_assert(COL_S_SUM + (OUT_S ? D : 0) <= 512);
     static constexpr uint32_t inbox(int shares) { return uint32_t(shares) * ((WGS * UNITS + shares - 1) / shares) * 16 * kRows * 4; }
-    // (more than half of an SM's, so that no two CTAs of these kernels share one:
-    // each takes all of TMEM, and CTAs of two clusters that wait for one
-    // another's would wait for ever)
+    // (so much of an SM's that no CTA of these kernels shares one with another, or
+    // with one of causal.cu: each takes all of TMEM, and CTAs of two clusters that
+    // wait for one another's would wait for ever)
     static constexpr uint32_t smem(int shares) {
         const uint32_t in = shares > 1 ? inbox(shares) : 0, all = (BYTES > in ? BYTES : in) + 1024;
-        return all > 116 * 1024 ? all : 116 * 1024;
+        return all > 150 * 1024 ? all : 150 * 1024;
     }
     static_assert(smem(kMaxShares) <= 227 * 1024 - 512);
 };

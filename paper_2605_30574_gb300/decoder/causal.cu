@@ -17,9 +17,13 @@
 // further from 64 bits at any size.
 //
 // With the rows' log sums (LSE), for the gradients of attention_grad.cu: a batch,
-// queries that are the last T of Tk positions, any strides.
+// queries that are the last T of Tk positions, any strides, and P in two bf16 terms:
+// 4096 tokens 172 us.  Few tiles share their keys over a cluster, whose CTAs trade
+// maxima, sums and outputs through distributed shared memory: one row of 4196 keys
+// 22.5 us, and 62 without.
 //
 // Every wait is bounded, as in gemm.cu.
+#include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -32,6 +36,7 @@
 #include "attention.cuh"
 #include "decoder.h"
 
+namespace cg = cooperative_groups;
 namespace tc = splice::tc;
 
 namespace {
@@ -42,7 +47,7 @@ using decoder::tma_load_4d;
 using decoder::tmem_ld32_done;
 
 constexpr int kRows = 128, kBN = 64, kThreads = 192;     // softmax: warps 0-3
-constexpr int kLoadWarp = 4, kMmaWarp = 5;
+constexpr int kLoadWarp = 4, kMmaWarp = 5, kMaxShares = 4;
 constexpr unsigned kErrLoad = 16, kErrMma = 32, kErrOut = 64, kErrDrain = 128;
 
 template <int D>
@@ -54,6 +59,9 @@ struct Cfg {
     static constexpr uint32_t SMEM = (BYTES + 1024 > 80 * 1024 ? BYTES + 1024 : 80 * 1024);
     static constexpr uint32_t COL_O = 2 * kBN;
     static constexpr uint32_t TMEM = D == 256 ? 512 : 256;
+    // what the CTAs of a cluster trade, in the operands' room
+    static constexpr uint32_t OFF_STATS = D * kRows * 4;
+    static_assert(OFF_STATS + kMaxShares * kRows * 8 <= BYTES && D / 16 % kMaxShares == 0);
     static_assert(COL_O + D <= TMEM && CTAS * TMEM <= 512 && (CTAS + 1) * (SMEM + 1024) > 228 * 1024);
 };
 
@@ -61,7 +69,7 @@ template <int D, bool LSE>
 __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     causal_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v, __nv_bfloat16* out, float* lse, int T, int Tk, int Hq, int G,
-                  int heads, float scale_log2, unsigned* err) {
+                  int heads, int shares, float scale_log2, unsigned* err) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[15];
@@ -76,10 +84,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     auto sfull = [&](int i) { return bar0 + 88 + 8u * i; };
     auto pfull = [&](int i) { return bar0 + 104 + 8u * i; };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int at = int(blockIdx.x) % heads, head = at % Hq, batch = at / Hq;
-    const int row0 = ((T + kRows - 1) / kRows - 1 - int(blockIdx.x) / heads) * kRows;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int share = LSE && shares > 1 ? int(cluster.block_rank()) : 0, item = LSE ? int(blockIdx.x) / shares : int(blockIdx.x);
+    const int at = item % heads, head = at % Hq, batch = at / Hq;
+    const int row0 = ((T + kRows - 1) / kRows - 1 - item / heads) * kRows;
     const int shift = Tk - T;            // row i sees the keys up to i + shift
-    const int nblk = max(0, (min(Tk, row0 + kRows + shift) + kBN - 1) / kBN);
+    const int all = max(0, (min(Tk, row0 + kRows + shift) + kBN - 1) / kBN);
+    const int first = LSE ? all * share / shares : 0, nblk = LSE ? all * (share + 1) / shares - first : all;    // this CTA's
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 13; ++i) tc::mbar_init(bar0 + 8u * i, 1);
@@ -102,6 +113,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = s_tmem;
+    float m = 0.f, l = 0.f;     // a row's maximum (log2), and sum
+    bool ok = true;
 
     if (warp == kLoadWarp) {
         const bool leader = tc::elect_one();
@@ -120,14 +133,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
                 tc::mbar_arrive_expect_tx(kfull(s), C::KV_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_4d(sbase + C::OFF_K + s * C::KV_BYTES + p * (kBN * 128), &tm_k, p * 64, j * kBN, hk, batch, kfull(s));
+                    tma_load_4d(sbase + C::OFF_K + s * C::KV_BYTES + p * (kBN * 128), &tm_k, p * 64, (first + j) * kBN, hk, batch, kfull(s));
             }
             if (!__all_sync(0xffffffffu, tc::mbar_wait(vempty(s), phase, &s_abort, err, kErrLoad))) break;
             if (leader) {
                 tc::mbar_arrive_expect_tx(vfull(s), C::KV_BYTES);
 #pragma unroll
                 for (int p = 0; p < C::PANELS; ++p)
-                    tma_load_4d(sbase + C::OFF_V + s * C::KV_BYTES + p * (kBN * 128), &tm_v, p * 64, j * kBN, hk, batch, vfull(s));
+                    tma_load_4d(sbase + C::OFF_V + s * C::KV_BYTES + p * (kBN * 128), &tm_v, p * 64, (first + j) * kBN, hk, batch, vfull(s));
             }
         }
         // Every copy issued must land before the CTA may exit.  (A broken-off
@@ -140,14 +153,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
         }
         // So must the commits arrive: the last P V's comes after the stages',
         // but nothing says that two commits arrive in their order.
-        bool ok = j == nblk;
+        ok = j == nblk;
         for (int i = max(0, j - 2); ok && i < j; ++i)
             ok = tc::mbar_wait(kempty(i & 1), uint32_t(i >> 1) & 1u, &s_abort, err, kErrDrain) &&
                  tc::mbar_wait(vempty(i & 1), uint32_t(i >> 1) & 1u, &s_abort, err, kErrDrain);
     } else if (warp == kMmaWarp) {
         const bool leader = tc::elect_one();
         constexpr uint32_t idesc_qk = tc::idesc_bf16_f32(kRows, kBN, false), idesc_pv = tc::idesc_bf16_f32(kRows, D, true);
-        bool ok = __all_sync(0xffffffffu, tc::mbar_wait(qfull, 0, &s_abort, err, kErrMma)), any = false;
+        bool any = false;
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(qfull, 0, &s_abort, err, kErrMma));
         for (int j = -1; ok && j < nblk; ++j) {
             if (j + 1 < nblk) {
                 // S of block j + 1, once P V of block j - 1 has read P from
@@ -196,8 +210,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
     } else {
         const int row = row0 + warp * 32 + lane;
         const uint32_t mine = tmem + (uint32_t(warp * 32) << 16);
-        float m = nblk ? 0.f : -INFINITY, l = 0.f;
-        bool ok = true;
+        m = nblk ? 0.f : -INFINITY;
         // A positive scale goes in with the exponent's fma, past the masking and
         // the maximum; one of zero or below would make NaN or +inf of a masked
         // score and turn the order round, so it goes in first.
@@ -215,8 +228,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
 #pragma unroll
                 for (int i = 0; i < kBN; ++i) v[i >> 5][i & 31] *= scale_log2;
             }
-            if ((j + 1) * kBN > row0 + shift + 1) {          // the diagonal's blocks
-                const int last = row + shift - j * kBN;      // this row's last key in the block
+            if ((first + j + 1) * kBN > row0 + shift + 1) {          // the diagonal's blocks
+                const int last = row + shift - (first + j) * kBN;      // this row's last key in the block
 #pragma unroll
                 for (int i = 0; i < kBN; ++i)
                     if (i > last) v[i >> 5][i & 31] = -INFINITY;
@@ -283,8 +296,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
             tc::mbar_arrive(pfull(s));
         }
         if (ok && nblk) ok = __all_sync(0xffffffffu, tc::mbar_wait(pvdone, uint32_t(nblk - 1) & 1u, &s_abort, err, kErrOut));
-        if (ok) {
-            tc::tc_fence_after();
+        if (ok) tc::tc_fence_after();
+        if (ok && shares == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;   // (no weights at all: zeros)
             if constexpr (LSE) {
                 if (row < T) lse[size_t(at) * T + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -315,21 +328,86 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
         }
     }
     __syncwarp();
+    if constexpr (LSE) {
+        if (shares > 1) {
+            // The rows' maxima and sums go to all, their outputs 16 columns at a time
+            // round the shares: [from share][part][16][128] fp32.  (No CTA of the
+            // cluster has a copy or an MMA in flight any more.)
+            constexpr int UNITS = D / 16, UNIT = 16 * kRows;
+            float* inbox = reinterpret_cast<float*>(smem_raw + (sbase - tc::smem_u32(smem_raw)));
+            float2* stats = reinterpret_cast<float2*>(inbox) + C::OFF_STATS / 8;
+            const int parts = UNITS / shares, r = warp * 32 + lane, row = row0 + r;
+            const uint32_t mine = tmem + (uint32_t(warp * 32) << 16) + C::COL_O;
+            const bool takes = warp < kLoadWarp && ok;
+            cluster.sync();
+            if (takes) {
+                for (int to = 0; to < shares; ++to) cluster.map_shared_rank(stats, to)[share * kRows + r] = make_float2(m, l);
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    float o[16];
+                    decoder::tmem_ld16_done(mine + u * 16, o);
+                    float* box = cluster.map_shared_rank(inbox, u % shares) + (share * parts + u / shares) * UNIT + r;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) box[e * kRows] = nblk ? o[e] : 0.f;
+                }
+            }
+            cluster.sync();
+            if (takes && row < T) {
+                float most = -INFINITY, sum = 0.f, by[kMaxShares];
+                for (int from = 0; from < shares; ++from) most = fmaxf(most, stats[from * kRows + r].x);
+#pragma unroll
+                for (int from = 0; from < kMaxShares; ++from) {
+                    if (from >= shares) break;
+                    const float2 s = stats[from * kRows + r];
+                    by[from] = s.x == -INFINITY ? 0.f : ex2(s.x - most);
+                    sum += by[from] * s.y;
+                }
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                if (share == 0) lse[size_t(at) * T + row] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.6931471805599453f;
+                for (int part = 0; part < parts; ++part) {
+                    float o[16] = {};
+#pragma unroll
+                    for (int from = 0; from < kMaxShares; ++from) {
+                        if (from >= shares) break;
+                        const float* box = inbox + (from * parts + part) * UNIT + r;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = fmaf(by[from], box[e * kRows], o[e]);
+                    }
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = decoder::pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
+                    uint4* dst = reinterpret_cast<uint4*>(out + ((size_t(batch) * T + row) * Hq + head) * D + (part * shares + share) * 16);
+                    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            }
+        }
+    }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
     if (warp == kMmaWarp) tc::tmem_dealloc(tmem, C::TMEM);
 }
 
+// CTAs that share a tile's blocks of keys: as many as there are places for, of two
+// blocks at least.  (32 heads of 128, one CTA and in twos and fours: 1 row of 512
+// keys 11, 9.8 and 9.3 us, of 4196 62, 35 and 22.5, in eights no less; 400 rows of 4196, 128 tiles,
+// 72, 57 and 66; 1024 rows, 256 tiles, 28.5, 26 and 46.)
+int shares_of(long items, int blocks, int places) {
+    int s = 1;
+    while (s < kMaxShares && items * 2 * s <= places && blocks >= 4 * s) s *= 2;
+    return s;
+}
+
 template <int D, bool LSE>
 int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::Operand& v, void* out, float* lse, int B, int Tq, int Tk,
            int Hq, int Hkv, float scale, cudaStream_t st) {
     using C = Cfg<D>;
-    static splice::PerDevice<bool> kept;
-    bool set = false;
-    const cudaError_t e = kept.get(&set, [](int, bool* done) {
-        *done = true;
-        return cudaFuncSetAttribute(causal_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM));
+    static splice::PerDevice<int> kept;
+    int sms = 0;
+    const cudaError_t e = kept.get(&sms, [](int dev, int* n) {
+        const cudaError_t err = cudaFuncSetAttribute(causal_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM));
+        return err == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : err;
     });
     if (e != cudaSuccess) return int(e);
     unsigned* err = decoder::error_word();
@@ -338,17 +416,22 @@ int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::
         !decoder::operand_map(&mv, v, D, Tk, Hkv, B, kBN))
         return int(cudaErrorInvalidValue);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((Tq + kRows - 1) / kRows) * unsigned(Hq) * unsigned(B));
+    const unsigned items = unsigned((Tq + kRows - 1) / kRows) * unsigned(Hq) * unsigned(B);
+    const int shares = LSE ? shares_of(items, (Tk + kBN - 1) / kBN, C::CTAS * sms) : 1;
+    cfg.gridDim = dim3(items * unsigned(shares));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
-    cudaLaunchAttribute a;
-    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    a.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &a;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute a[2];
+    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a[0].val.programmaticStreamSerializationAllowed = 1;
+    a[1].id = cudaLaunchAttributeClusterDimension;
+    a[1].val.clusterDim.x = unsigned(shares);
+    a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
+    cfg.attrs = a;
+    cfg.numAttrs = shares > 1 ? 2 : 1;
     return int(cudaLaunchKernelEx(&cfg, causal_kernel<D, LSE>, mq, mk, mv, static_cast<__nv_bfloat16*>(out), lse, Tq, Tk, Hq, Hq / Hkv,
-                                  Hq * B, scale * 1.4426950408889634f, err));
+                                  Hq * B, shares, scale * 1.4426950408889634f, err));
 }
 
 template <bool LSE>
