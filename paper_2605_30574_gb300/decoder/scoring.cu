@@ -566,7 +566,6 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) score_kernel(const ScorePar
 
 // ---- distillation ----
 
-constexpr int kPieces = 8;            // copies that a CTA's slice arrives in
 constexpr int kWorkers = 256, kDistillThreads = kWorkers + 32;
 
 struct DistillParams {
@@ -574,7 +573,6 @@ struct DistillParams {
     long stride;
     long rows;
     int V, K, rest;
-    int piece;                  // words of a piece, of the longest slice
     float inv_T, inv_T_low;     // 1 / T, and what its rounding left
     float c, c_low;             // log2(e) / T, the same
     float least;                // -160 / c
@@ -691,12 +689,13 @@ struct Teacher {
 __device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
 
 // Clusters stay and take row after row.  A CTA's slice of a row comes into shared
-// memory by bulk copies: the sums are taken from it, and once the cluster has the
-// row's, the gradient is made from the same copy.  As soon as a piece of it has
-// been used for the last time, that piece of the next row is asked for in its
-// place; and the warp behind the workers' reads the next row's teacher.  So the
-// copies go on under the gradient, and with two CTAs to an SM under the other's
-// exchange.  (A cluster for each row, gone when it was done: 1.7 times as long.)
+// memory by one bulk copy: the sums are taken from it, and once the cluster has the
+// row's, the gradient is made from the same copy and the next row's slice asked for
+// in its place; the warp behind the workers' reads the next row's teacher.  The
+// other CTAs of an SM work under a CTA's copy and exchange.  (A cluster for each
+// row, gone when it was done: 1.7 times as long.  A slice in eight pieces, each
+// replaced by the next row's as soon as it is used: 1.15 times, as the
+// instructions of eight loops cost more than the copies' earlier start gives.)
 //
 // The teacher's tokens are taken out of the slice (-inf) before it is summed up
 // and put in their own way, so the sum of all others is a sum and not a
@@ -705,7 +704,7 @@ template <class T, bool GRAD, int J>
 __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams P) {
     constexpr int N = Word<T>::N;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[kPieces + 2];
+    __shared__ __align__(8) uint64_t bars[3];
     __shared__ Teacher s_teacher[2];
     __shared__ float2 s_warps[kWorkers / 32], s_cta[2][kMaxCluster];       // largest x, sum of the others' e^
     __shared__ volatile int s_abort;
@@ -720,8 +719,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     const float c = P.c;
     const float2 c2 = make_float2(c, c);
     if (tid == 0) {
-        for (int i = 0; i < kPieces; ++i) tc::mbar_init(bar0 + 8u * i, 1);
-        for (int i = 0; i < 2; ++i) tc::mbar_init(bar0 + 8u * (kPieces + i), 1);
+        for (int i = 0; i < 3; ++i) tc::mbar_init(bar0 + 8u * i, 1);
         s_abort = 0;
         tc::fence_mbar_init();
     }
@@ -737,11 +735,10 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         const int w0 = int(long(in.words) * rank >> log2_C);
         return Part{in, w0, int(long(in.words) * (rank + 1) >> log2_C) - w0};
     };
-    // a piece of a row, by one thread (an empty one just arrives)
-    auto ask = [&](const Part& p, int i) {
-        const int lo = i * P.piece, n = max(0, min(P.piece, p.nw - lo));
-        tc::mbar_arrive_expect_tx(bar0 + 8u * i, uint32_t(n) * 16u);
-        if (n > 0) bulk_load(tc::smem_u32(slice + lo), p.in.body() + p.w0 + lo, uint32_t(n) * 16u, bar0 + 8u * i);
+    // a slice, by one thread (an empty one just arrives)
+    auto ask = [&](const Part& p) {
+        tc::mbar_arrive_expect_tx(bar0, uint32_t(p.nw) * 16u);
+        if (p.nw > 0) bulk_load(tc::smem_u32(slice), p.in.body() + p.w0, uint32_t(p.nw) * 16u, bar0);
     };
     // The teacher of a row, J alternatives to a lane, in three steps, each
     // a row ahead of the next so that none waits for memory: what is given for it,
@@ -870,10 +867,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         return make_float2(m, v.y);
     };
 
-    if (tid == 0 && row0 < P.rows) {          // (it has made the barriers itself)
-        const Part p = part_of(row0);
-        for (int i = 0; i < kPieces; ++i) ask(p, i);
-    }
+    if (tid == 0 && row0 < P.rows) ask(part_of(row0));         // (it has made the barriers itself)
     if (warp == kWorkers / 32 && row0 < P.rows) {
         ask_teacher(row0);
         look_up(row0);
@@ -905,7 +899,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         a.scale = weight * P.inv_T;
         return a;
     };
-    auto exchanged = [&]() { return wait_cluster(bar0 + 8u * (kPieces + turn), round, &s_abort, P.err, kErrRow); };
+    auto exchanged = [&]() { return wait_cluster(bar0 + 8u * (1 + turn), round, &s_abort, P.err, kErrRow); };
 
     if (warp < kWorkers / 32) {
         for (long row = row0; row < P.rows; row += step) {
@@ -921,9 +915,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             // the teacher's tokens out
             float edge_x = kNone;
             if (edge >= 0 && !(t.edges >> (tid < heads ? edge : 8 + tid - heads) & 1u)) edge_x = to_float(p.in.x[edge]);
-            bool landed = true;
-            for (int i = 0; i < kPieces; ++i) landed = landed && tc::mbar_wait(bar0 + 8u * i, turn, &s_abort, P.err, kErrRow);
-            if (tid < P.K && landed) {
+            if (tc::mbar_wait(bar0, turn, &s_abort, P.err, kErrRow) && tid < P.K) {
                 const int at = t.id[tid] - first_word;
                 if (t.id[tid] >= 0 && at >= 0 && at < p.nw * N) flat[at] = from_float<T>(kNone);
             }
@@ -934,21 +926,18 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 sums.rise(edge_x, c);
                 sums.add<false>(make_float2(edge_x, kNone), sums.minus_ref(), c2);
             }
-            for (int i = 0; i < kPieces; ++i) {
-                const int end = min(p.nw, (i + 1) * P.piece);
-                for (int w = i * P.piece + tid; w < end; w += 2 * kWorkers) {
-                    const Word<T> a = slice[w], b = slice[min(w + kWorkers, end - 1)];
-                    const bool two = w + kWorkers < end;
-                    sums.rise(two ? fmaxf(largest(a), largest(b)) : largest(a), c);
-                    const float2 minus = sums.minus_ref();
-                    add_word<false>(sums, a, minus, c2);
-                    if (two) add_word<false>(sums, b, minus, c2);
-                }
-                if constexpr (!GRAD) {
-                    tc::fence_proxy_async_smem();
-                    workers_sync();
-                    if (tid == 0 && more) ask(next, i);
-                }
+            for (int w = tid; w < p.nw; w += 2 * kWorkers) {
+                const Word<T> a = slice[w], b = slice[min(w + kWorkers, p.nw - 1)];
+                const bool two = w + kWorkers < p.nw;
+                sums.rise(two ? fmaxf(largest(a), largest(b)) : largest(a), c);
+                const float2 minus = sums.minus_ref();
+                add_word<false>(sums, a, minus, c2);
+                if (two) add_word<false>(sums, b, minus, c2);
+            }
+            if constexpr (!GRAD) {
+                tc::fence_proxy_async_smem();
+                workers_sync();
+                if (tid == 0 && more) ask(next);
             }
             const float2 mine = together(make_float2(sums.m, sums.s.x + sums.s.y));
             if (lane == 0) s_warps[warp] = mine;
@@ -956,7 +945,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             // to every CTA of the cluster
             if (warp == 0) {
                 const float2 part = together(lane < kWorkers / 32 ? s_warps[lane] : make_float2(kNone, 0.f));
-                const uint32_t to = tc::smem_u32(&s_cta[turn][rank]), bar = bar0 + 8u * (kPieces + turn);
+                const uint32_t to = tc::smem_u32(&s_cta[turn][rank]), bar = bar0 + 8u * (1 + turn);
                 if (lane == 0) tc::mbar_arrive_expect_tx(bar, uint32_t(C) * 8u);
                 if (lane < C) store_async(tc::map_cta(to, uint32_t(lane)), part, tc::map_cta(bar, uint32_t(lane)));
             }
@@ -966,35 +955,32 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 T* out = static_cast<T*>(P.grad) + row * P.V;
                 const bool words_out = (reinterpret_cast<uintptr_t>(out + p.in.head) & 15u) == 0;
                 const float k = a.f * a.inv_s * a.scale;
-                for (int i = 0; i < kPieces; ++i) {
-                    const int lo = i * P.piece, end = min(p.nw, lo + P.piece);
-                    if (weight == 0.f) {         // a row that is left out
-                        if (words_out) {
-                            for (int w = lo + tid; w < end; w += kWorkers) reinterpret_cast<uint4*>(out + first_word)[w] = make_uint4(0, 0, 0, 0);
-                        } else {
-                            for (int w = lo * N + tid; w < end * N; w += kWorkers) out[first_word + w] = from_float<T>(0.f);
-                        }
-                    } else if (words_out) {
-#pragma unroll 2
-                        for (int w = lo + tid; w < end; w += kWorkers) {
-                            const Word<T> v = slice[w];
-                            Word<T> g;
-#pragma unroll
-                            for (int e = 0; e < N; e += 2) {
-                                const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), a.ref, k, P);
-                                g.x[e] = from_float<T>(two.x);
-                                g.x[e + 1] = from_float<T>(two.y);
-                            }
-                            reinterpret_cast<Word<T>*>(out + first_word)[w] = g;
-                        }
+                if (weight == 0.f) {         // a row that is left out
+                    if (words_out) {
+                        for (int w = tid; w < p.nw; w += kWorkers) reinterpret_cast<uint4*>(out + first_word)[w] = make_uint4(0, 0, 0, 0);
                     } else {
-                        for (int w = lo * N + tid; w < end * N; w += kWorkers)
-                            out[first_word + w] = from_float<T>(weights_of<T>(make_float2(to_float(flat[w]), 0.f), a.ref, k, P).x);
+                        for (int w = tid; w < p.nw * N; w += kWorkers) out[first_word + w] = from_float<T>(0.f);
                     }
-                    tc::fence_proxy_async_smem();
-                    workers_sync();
-                    if (tid == 0 && more) ask(next, i);
+                } else if (words_out) {
+#pragma unroll 2
+                    for (int w = tid; w < p.nw; w += kWorkers) {
+                        const Word<T> v = slice[w];
+                        Word<T> g;
+#pragma unroll
+                        for (int e = 0; e < N; e += 2) {
+                            const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), a.ref, k, P);
+                            g.x[e] = from_float<T>(two.x);
+                            g.x[e + 1] = from_float<T>(two.y);
+                        }
+                        reinterpret_cast<Word<T>*>(out + first_word)[w] = g;
+                    }
+                } else {
+                    for (int w = tid; w < p.nw * N; w += kWorkers)
+                        out[first_word + w] = from_float<T>(weights_of<T>(make_float2(to_float(flat[w]), 0.f), a.ref, k, P).x);
                 }
+                tc::fence_proxy_async_smem();
+                workers_sync();
+                if (tid == 0 && more) ask(next);
                 if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.ref, k, P).x);
             }
             __syncthreads();
@@ -1192,8 +1178,6 @@ int distill(DistillParams P, cudaStream_t st) {
     const int C = distill_cluster(P.rows, P.V, sizeof(T));
     const size_t bytes = slice_bytes(P.V, sizeof(T), C);
     if (bytes > kSliceMax) return int(cudaErrorInvalidValue);
-    // (whole rounds of the workers, two words each)
-    P.piece = int((bytes / 16 + kPieces * 2 * kWorkers - 1) / (kPieces * 2 * kWorkers)) * 2 * kWorkers;
     int log2 = 0;
     while (1 << log2 < C) ++log2;
     int size = 0;
@@ -1247,7 +1231,7 @@ int decoder_distill(const void* x, int dtype, long stride, long rows, long V, co
     if (rows < 1 || rows > (1L << 27) || V < 1 || V > decoder_distill_vocab(dtype) || K < 1 || K > kMaxTop || !(inv_T > 0.0))
         return int(cudaErrorInvalidValue);
     const float c = float(inv_T * kLog2e);
-    const DistillParams P{x, stride, rows, int(V), K, rest, 0, float(inv_T), float(inv_T - double(float(inv_T))), c, float(inv_T * kLog2e - double(c)), -160.f / c, static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
+    const DistillParams P{x, stride, rows, int(V), K, rest, float(inv_T), float(inv_T - double(float(inv_T))), c, float(inv_T * kLog2e - double(c)), -160.f / c, static_cast<const int64_t*>(ids), static_cast<const float*>(teacher),
                           static_cast<const float*>(weight), static_cast<float*>(loss), grad, decoder::error_word()};
     if (!P.err) return int(cudaErrorInvalidValue);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
