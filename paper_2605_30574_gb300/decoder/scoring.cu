@@ -884,6 +884,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     struct Stats {
         float ref, rest, s, inv_s, all, f, scale;
     };
+    __shared__ Stats s_stats;
     uint32_t turn = 0, round = 0;        // row by row, and every other
     // (once every CTA's sums are here)
     auto stats_of = [&](const Teacher& t, float weight) {
@@ -950,8 +951,14 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 if (lane < C) store_async(tc::map_cta(to, uint32_t(lane)), part, tc::map_cta(bar, uint32_t(lane)));
             }
             if constexpr (GRAD) {
-                exchanged();
-                const Stats a = stats_of(t, weight);
+                // (by one warp: the others would take the issue slots of CTAs that work)
+                if (warp == 0) {
+                    exchanged();
+                    const Stats a = stats_of(t, weight);
+                    if (lane == 0) s_stats = a;
+                }
+                workers_sync();
+                const Stats a = s_stats;
                 T* out = static_cast<T*>(P.grad) + row * P.V;
                 const bool words_out = (reinterpret_cast<uintptr_t>(out + p.in.head) & 15u) == 0;
                 const float k = a.f * a.inv_s * a.scale;
@@ -962,7 +969,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                         for (int w = tid; w < p.nw * N; w += kWorkers) out[first_word + w] = from_float<T>(0.f);
                     }
                 } else if (words_out) {
-#pragma unroll 2
+#pragma unroll 4
                     for (int w = tid; w < p.nw; w += kWorkers) {
                         const Word<T> v = slice[w];
                         Word<T> g;
