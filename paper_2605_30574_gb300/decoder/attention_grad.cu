@@ -42,6 +42,11 @@
 // 256 dims: blocks of 64, and dK and dV, which do not fit in TMEM together, in
 // a launch each.
 //
+// 32 heads of 128, 8 for keys: 4096 positions 340 us (1.01 PFLOP/s of the five
+// products that the gradients are, 1.41 of the seven), 1024 49; 4 x 100 rows of
+// 4196 135.  The loops take 84% (by keys) and 81% of the tensor cores' rate; a CTA's
+// operands in, and its sums out, the time of 8 blocks more.
+//
 // delta has the error of an output in bf16, which rows of few keys show: dQ and dK
 // of 2, 6, 17, 28 and 64 positions are off by 0.0047, 0.0044, 0.0030, 0.0024 and
 // 0.0024 of their size, where P, dS and the outputs in bf16 make 0.0024.  dS sums to
