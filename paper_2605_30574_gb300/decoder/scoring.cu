@@ -10,10 +10,10 @@
 // distributed shared memory: no workspace, no second launch, and sums in a
 // fixed order.  Both are bound by HBM: the scores read x once, the
 // distillation reads it once and writes the gradient once.  512 rows of 151936
-// fp32: scores with 20 alternatives 54.7 us (5.7 TB/s), divergence from 32 64.5
-// (4.8), with its gradient 111 (5.6).  bf16 has twice the elements to a byte, and
-// their exponentials and sums come to as much: 2047 rows of 100003, scores with 64
-// alternatives 98 us (74 with none), divergence and gradient 141.
+// fp32: scores with 20 alternatives 54.7 us (5.7 TB/s), divergence from 32 65 (4.8),
+// with its gradient 112 (5.6).  bf16 has twice the elements to a byte, and their
+// exponentials and sums come to as much: scores of 2047 rows of 100003 with 64
+// alternatives 98 us (74 with none), divergence and gradient of 1999 143.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -994,11 +994,17 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 if (tid == 0 && more) ask(next);
                 if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.ref, k, P).x);
             }
-            __syncthreads();
+            if (__syncthreads_or(s_abort)) {         // (a wait ran out; the copy on its way lands first)
+                volatile int no_abort = 0;
+                if (tid == 0 && more) tc::mbar_wait(bar0, turn ^ 1u, &no_abort, P.err, kErrRow);
+                break;
+            }
             round ^= turn;
             turn ^= 1u;
         }
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        // (no CTA leaves while another may send it something)
+        if (C > 1) cluster.sync();
         return;
     }
 
@@ -1070,12 +1076,13 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             }
             if (lane == 0) P.loss[row] = weight == 0.f ? 0.f : (total.x + total.y) * weight;
         }
-        __syncthreads();
+        if (__syncthreads_or(s_abort)) break;
         round ^= turn;
         turn ^= 1u;
         if (row + step >= P.rows) put_right(row, s_teacher[turn ^ 1u]);
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (C > 1) cluster.sync();
 }
 
 template <class Kernel, class Params>
