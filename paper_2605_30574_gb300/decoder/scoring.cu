@@ -883,10 +883,14 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     if (C > 1) cluster.sync();                // every CTA has begun
     else __syncthreads();
 
-    // What a row's gradient goes by: p_j = e_j / s; the gradient of a token that is
-    // not the teacher's is f p_j, of one that is (all p_j - q_j); all times scale.
+    // What a row's gradient goes by: p_j = e^((x_j - ref) / T) / s; the gradient of
+    // a token that is not the teacher's is out e^((x_j - out_ref) / T), of one that
+    // is (all p_j - q_j); all times scale.  Where the rest has weight, the others go
+    // by their own largest logit and sum: what the rest gives them is q_rest times
+    // their shares of it, and does not vanish where p_rest does, 87 nats below ref.
     struct Stats {
-        float ref, rest, s, inv_s, all, f, scale;
+        float2 others;              // largest x, sum of e^ from there
+        float ref, s, inv_s, all, out_ref, out, scale;
     };
     __shared__ Stats s_stats;
     uint32_t turn = 0, round = 0;        // row by row, and every other
@@ -895,12 +899,18 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         const float2 others = together(lane < C ? s_cta[turn][lane] : make_float2(kNone, 0.f));
         const float m = fmaxf(others.x, t.most);
         Stats a;
+        a.others = others;
         a.ref = m == kNone ? 0.f : m;
-        a.rest = others.x == kNone ? others.y : others.y * ex2((others.x - a.ref) * c);
-        a.s = a.rest + (t.most == kNone ? t.e : t.e * ex2((t.most - a.ref) * c));
+        a.s = (others.x == kNone ? others.y : others.y * ex2((others.x - a.ref) * c)) +
+              (t.most == kNone ? t.e : t.e * ex2((t.most - a.ref) * c));
         a.inv_s = a.s == 0.f ? 0.f : 1.f / a.s;
         a.all = P.rest ? 1.f : t.all;
-        a.f = !P.rest ? a.all : a.rest == 0.f ? 1.f : 1.f - t.rest * a.s / a.rest;
+        a.out_ref = a.ref;
+        a.out = a.all * a.inv_s;
+        if (t.rest != 0.f && others.y > 0.f) {      // (of 0: nothing to share it)
+            a.out_ref = others.x;
+            a.out = weights_of<float>(make_float2(others.x, 0.f), a.ref, a.inv_s, P).x - t.rest / others.y;
+        }
         a.scale = weight * P.inv_T;
         return a;
     };
@@ -965,7 +975,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 const Stats a = s_stats;
                 T* out = static_cast<T*>(P.grad) + row * P.V;
                 const bool words_out = (reinterpret_cast<uintptr_t>(out + p.in.head) & 15u) == 0;
-                const float k = a.f * a.inv_s * a.scale;
+                const float k = a.out * a.scale;
                 if (weight == 0.f) {         // a row that is left out
                     if (words_out) {
                         for (int w = tid; w < p.nw; w += kWorkers) reinterpret_cast<uint4*>(out + first_word)[w] = make_uint4(0, 0, 0, 0);
@@ -979,7 +989,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                         Word<T> g;
 #pragma unroll
                         for (int e = 0; e < N; e += 2) {
-                            const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), a.ref, k, P);
+                            const float2 two = weights_of<T>(make_float2(to_float(v.x[e]), to_float(v.x[e + 1])), a.out_ref, k, P);
                             g.x[e] = from_float<T>(two.x);
                             g.x[e + 1] = from_float<T>(two.y);
                         }
@@ -987,12 +997,12 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                     }
                 } else {
                     for (int w = tid; w < p.nw * N; w += kWorkers)
-                        out[first_word + w] = from_float<T>(weights_of<T>(make_float2(to_float(flat[w]), 0.f), a.ref, k, P).x);
+                        out[first_word + w] = from_float<T>(weights_of<T>(make_float2(to_float(flat[w]), 0.f), a.out_ref, k, P).x);
                 }
                 tc::fence_proxy_async_smem();
                 workers_sync();
                 if (tid == 0 && more) ask(next);
-                if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.ref, k, P).x);
+                if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.out_ref, k, P).x);
             }
             if (__syncthreads_or(s_abort)) {         // (a wait ran out; the copy on its way lands first)
                 volatile int no_abort = 0;
@@ -1042,28 +1052,32 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         if (rank == 0) {
             // in pairs, as the terms are small differences of log probabilities; the
             // four logarithms by a lane each
-            const float2 mine = log_pair(lane == 0 ? a.s : lane == 1 ? a.rest : lane == 2 ? t.rest : t.norm);
+            const float2 mine = log_pair(lane == 0 ? a.s : lane == 1 ? a.others.y : lane == 2 ? t.rest : t.norm);
             auto of = [&](int from) {
                 return make_float2(__shfl_sync(0xffffffffu, mine.x, from), __shfl_sync(0xffffffffu, mine.y, from));
             };
             auto minus = [](float2 a) { return make_float2(-a.x, -a.y); };
             const float2 log_s = of(0), log_others = of(1), log_rest = of(2), log_norm = of(3);
+            auto z_of = [&](float x) {          // (x - ref) / T
+                const float2 by = exact_sum(x, -a.ref);
+                const float z = by.x * P.inv_T;
+                return make_float2(z, fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low));
+            };
             float2 total = make_float2(0.f, 0.f);
             for (int k = lane; k < P.K; k += 32) {
                 const float q = t.q[k];
                 if (q == 0.f) continue;
                 // log q - log p; p is 0 where its logit is -inf or no token has one
-                const float2 by = exact_sum(t.z[k], -a.ref);
-                const float z = by.x * P.inv_T, low = fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low);
                 const bool none = a.s == 0.f || t.z[k] == kNone;
-                const float2 log_p = pair_sum(make_float2(z, low), minus(log_s)), log_q = pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm));
+                const float2 log_p = pair_sum(z_of(t.z[k]), minus(log_s)), log_q = pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm));
                 const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_q, minus(log_p));
                 const float x = q * d.x;
                 total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(q, d.x, -x) + q * d.y));
             }
             if (lane == 0 && t.rest > 0.f) {
-                const bool none = a.rest == 0.f;
-                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_rest, minus(pair_sum(log_others, minus(log_s))));
+                const bool none = a.others.y == 0.f;
+                const float2 log_p = pair_sum(pair_sum(z_of(a.others.x), log_others), minus(log_s));
+                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_rest, minus(log_p));
                 const float x = t.rest * d.x;
                 total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(t.rest, d.x, -x) + t.rest * d.y));
             }

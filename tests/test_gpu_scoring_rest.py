@@ -1,0 +1,101 @@
+"""The distillation's rest (all tokens but the teacher's, as one outcome) against
+its definition in fp64, where the others lie far below or above the teacher's.
+
+Tolerances.  As for the other scores, log probabilities and weights are within
+2^-19 of their size.  What the teacher leaves of 1 is 1 less a sum of up to 128
+exponentials, each within 2^-23 of itself: known to 2^-22, which the loss has
+times |log q_rest - log p_rest|, and the others' gradients times their share of
+p_rest.
+"""
+import pytest
+import torch
+
+from paper_2605_30574_gb300 import build as B
+from paper_2605_30574_gb300 import decoder as K
+from paper_2605_30574_gb300.decoder import scoring
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+HALF_ULP = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+EPS, KNOWN = 2.0 ** -19, 2.0 ** -22
+INF = float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    B.build()
+    yield
+    K.check_device_error()
+
+
+def gen(seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def definition(x, ids, teacher, T, known=None):
+    """Loss and gradient with the rest counted, in fp64, and their bounds; `known`
+    is how well the rows' rests are."""
+    known = torch.full(x.shape[:1], KNOWN, device="cuda", dtype=torch.double) if known is None else known
+    lp, t = torch.log_softmax(x.double() / T, -1), teacher.double()
+    q, inside = t.exp(), torch.zeros(x.shape, dtype=torch.bool, device="cuda").scatter_(1, ids, True)
+    rest = (1 - q.sum(-1)).clamp(min=0)
+    lpr = torch.logsumexp(lp.masked_fill(inside, -INF), -1)
+    zero = torch.zeros_like(rest)
+    at = lp.gather(1, ids)
+    loss = torch.where(q > 0, q * (t - at), torch.zeros_like(q)).sum(-1) + torch.where(rest > 0, rest * (rest.log() - lpr), zero)
+    size = torch.where(q > 0, q * (1 + t.abs() + at.abs()), torch.zeros_like(q)).sum(-1)
+    apart = torch.where(rest > 0, 1 + rest.log().abs() + lpr.abs(), zero)
+    share = torch.where((lpr > -INF)[:, None], (lp - lpr[:, None]).exp(), torch.zeros_like(lp)).masked_fill(inside, 0)
+    target = torch.zeros_like(lp).scatter_add_(1, ids, q) + share * rest[:, None]
+    return loss, (lp.exp() - target) / T, EPS * (size + rest * apart) + known * apart, (EPS * (lp.exp() + target) + known[:, None] * share) / T
+
+
+def near(got, want, bound):
+    got = got.double()
+    assert torch.equal(got.isnan(), want.isnan())
+    off = ((got - want).abs() / bound).masked_fill((got == want) | got.isnan(), 0.0)
+    assert float(off.max()) <= 1.0, float(off.max())
+
+
+def check(x, ids, teacher, T=1.0):
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=True, temperature=T)
+    want, dwant, off, doff = definition(x, ids, teacher, T)
+    near(loss, want, off + 1e-30)
+    near(grad, dwant, doff + HALF_ULP[x.dtype] * dwant.abs() + (2.0 ** -25 if x.dtype is F16 else 1e-37))
+    leaf = x.detach().requires_grad_()
+    each = scoring.distill_loss(leaf, ids, teacher, rest=True, temperature=T)
+    assert torch.equal(each.detach(), loss)
+    (again,) = torch.autograd.grad(each.sum(), leaf)
+    assert torch.equal(again, grad)
+    return loss, grad
+
+
+@pytest.mark.parametrize("T", [1.0, 0.1])
+@pytest.mark.parametrize("gap", [30, 60, 86, 88, 100, 300, 2000, -60, -100, -2000])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("V,top", [(4, 2), (1003, 40), (60011, 128)])
+def test_others_far_from_the_teachers(V, top, dtype, gap, T):
+    """The others' logits `gap` nats below the teacher's, by the temperature."""
+    g = gen(V + top)
+    x = torch.randn(6, V, generator=g, device="cuda")
+    ids = torch.rand(6, V, generator=g, device="cuda").topk(top, -1).indices
+    x -= gap
+    x.scatter_(1, ids, torch.randn(6, top, generator=g, device="cuda"))
+    x = (x * T).to(dtype)
+    left = torch.tensor([0.3, 0.2, 1e-2, 1e-4, 0.999, 0.5], device="cuda")
+    teacher = torch.log_softmax(torch.randn(6, top, generator=g, device="cuda"), -1) + torch.log1p(-left)[:, None]
+    loss, grad = check(x, ids, teacher, T)
+    assert bool(loss.isfinite().all())
+    # what the others gain, the teacher's lose
+    off = (HALF_ULP[dtype] + EPS) * grad.double().abs().sum(-1) + KNOWN / T + (V * 2.0 ** -25 if dtype is F16 else 0)
+    assert bool((grad.double().sum(-1).abs() <= off + EPS / T).all())
+
+
+def test_two_alternatives_and_two_others_a_long_way_off():
+    x = torch.tensor([[0.0, -1.0, -89.0, -90.0]], device="cuda")
+    ids = torch.tensor([[0, 1]], device="cuda")
+    teacher = torch.tensor([[0.5, 0.3]], device="cuda").log()
+    loss, grad = check(x, ids, teacher)
+    assert 17 < float(loss) < 19 and abs(float(grad[0, 2:].sum()) + 0.2) < 1e-6
