@@ -82,7 +82,7 @@ def attribute(run, prompt: int, slot: int, tokens: torch.Tensor, L: int = 0, top
     tokens, after = tokens[:-1], tokens[1:]
     clean_k, clean_v = list(run.k_clean[prompt]), list(run.v_clean[prompt])
     with torch.no_grad():
-        clean = scoring.token_logprobs(continuation_logits(model, tokens, clean_k, clean_v), after, top=min(top, model.dims.vocab - 1))
+        clean = scoring.token_logprobs(continuation_logits(model, tokens, clean_k, clean_v), after, top=min(top, model.dims.vocab))
     spans = [[t.detach().clone().requires_grad_(l >= L) for l, t in enumerate(span)] for span in spliced_spans(run, prompt, slot, L)]
     with torch.enable_grad():
         logits = continuation_logits(model, tokens, *spans)
@@ -103,7 +103,7 @@ def restored(run, prompt: int, slot: int, tokens: torch.Tensor, layer: int, L: i
     tokens = tokens[:-1]
     k, v = spliced_spans(run, prompt, slot, L)
     clean = continuation_logits(model, tokens, list(run.k_clean[prompt]), list(run.v_clean[prompt]))
-    teacher = scoring.token_logprobs(clean, top=min(top, model.dims.vocab - 1))
+    teacher = scoring.token_logprobs(clean, top=min(top, model.dims.vocab))
     k[layer], v[layer] = run.k_clean[prompt, layer], run.v_clean[prompt, layer]
     return float(scoring.distill_loss(continuation_logits(model, tokens, k, v), teacher.top_ids, teacher.top_logprobs, rest=True).mean())
 

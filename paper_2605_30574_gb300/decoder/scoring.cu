@@ -813,18 +813,20 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
         }
         if (P.rest || top == kNone) top = 0.f;
-        float sum = 0.f, e = 0.f;
+        float sum = 0.f, e = 0.f, sizes = 0.f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            t.log_q[j * 32 + lane] = q[j] - top;
-            q[j] = expf(q[j] - top);
+            const float log_q = t.log_q[j * 32 + lane] = q[j] - top;
+            q[j] = expf(log_q);
             sum += q[j];
+            if (q[j] > 0.f) sizes = fmaf(q[j], 1.f + fabsf(log_q), sizes);
             if (first[j]) e += ex2((z[j] - (most == kNone ? 0.f : most)) * c);
         }
 #pragma unroll
         for (int off = 16; off > 0; off /= 2) {
             sum += __shfl_xor_sync(0xffffffffu, sum, off);
             e += __shfl_xor_sync(0xffffffffu, e, off);
+            sizes += __shfl_xor_sync(0xffffffffu, sizes, off);
         }
         // (NaN for a row with a token outside the vocabulary)
         float2 all = make_float2(0.f, 0.f);
@@ -838,7 +840,11 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
 #pragma unroll
         for (int off = 16; off > 0; off /= 2)
             all = pair_sum(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, off), __shfl_xor_sync(0xffffffffu, all.y, off)));
-        const float left = pair_sum(make_float2(1.f, 0.f), make_float2(-all.x, -all.y)).x;
+        // What is left of 1 is no weight up to what rounding makes of K log
+        // probabilities whose sum is 1: each is off by some 2^-24 of itself and of
+        // the row's log sum, its exponential by 2^-23.  (Whole distributions of 2 to
+        // 128 tokens: left at up to 2.9 x 2^-23 sum q (1 + |log q|), in fp32.)
+        const float left = pair_sum(make_float2(1.f, 0.f), make_float2(-all.x, -all.y)).x, least = 0x1p-21f * sizes;
         __syncwarp();
         bool again = false;
 #pragma unroll
@@ -857,7 +863,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             t.edges = edges;
             t.norm = P.rest || sum == 0.f ? 1.f : sum;
             t.all = all.x;
-            t.rest = P.rest ? (left > 0.f || left != left ? left : 0.f) : 0.f;
+            t.rest = P.rest && (left > least || left != left) ? left : 0.f;
         }
     };
     // of sums with their largest x, over a warp (-inf: a sum of 0, or NaN)

@@ -180,7 +180,9 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
       probabilities made to sum to 1 over the K (so logits over temperature
       serve as well);
     * ``rest`` True: q as they are, and all other tokens together as one more
-      outcome, with what is left of 1.
+      outcome, with what is left of 1: with nothing, where that is no more than
+      the rounding of log probabilities that are all there are, 2^-21 sum_k q_k (1
+      + |log q_k|).
 
     An id below 0 is no alternative; a row with none has the loss 0, and so has a
     row of weight 0, whatever else it holds.  An id that comes twice counts

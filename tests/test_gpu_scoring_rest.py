@@ -99,3 +99,65 @@ def test_two_alternatives_and_two_others_a_long_way_off():
     teacher = torch.tensor([[0.5, 0.3]], device="cuda").log()
     loss, grad = check(x, ids, teacher)
     assert 17 < float(loss) < 19 and abs(float(grad[0, 2:].sum()) + 0.2) < 1e-6
+
+
+# ---- what rounding leaves of 1 ----
+#
+# K log probabilities that are a whole distribution are each off by some units of
+# 2^-24 of themselves and of their sum's logarithm; e^ of them by 2^-23 of itself.
+# Up to 4 x 2^-23 sum q (1 + |log q|) in all is no weight.
+
+def slack(teacher):
+    t = teacher.double()
+    return 2.0 ** -21 * torch.where(t > -INF, t.exp() * (1 + t.abs()), torch.zeros_like(t)).sum(-1)
+
+
+@pytest.mark.parametrize("T", [1.0, 0.6])
+@pytest.mark.parametrize("others", ["none", "-inf", "lowest"])
+@pytest.mark.parametrize("top", [2, 20, 128])
+def test_alternatives_that_are_all_a_row_can_say(top, others, T):
+    """A row against itself, the other tokens missing or masked."""
+    g, rows = gen(top), 400
+    V = top if others == "none" else 1003
+    x = torch.full((rows, V), -INF if others == "-inf" else torch.finfo(F32).min, device="cuda")
+    ids = torch.rand(rows, V, generator=g, device="cuda").topk(top, -1).indices
+    x.scatter_(1, ids, 2 * torch.randn(rows, top, generator=g, device="cuda"))
+    own = scoring.token_logprobs(x, top=top, temperature=T)
+    for at, teacher in ((own.top_ids, own.top_logprobs), (ids, torch.log_softmax(x.gather(1, ids) / T, -1))):
+        assert bool(((1 - teacher.exp().sum(-1)) != 0).any())
+        loss, grad = scoring.distill_loss_and_grad(x, at, teacher, rest=True, temperature=T)
+        q = teacher.double().exp()
+        assert bool((loss.double().abs() <= EPS * (q * (1 + 2 * teacher.double().abs())).sum(-1)).all())
+        inside = grad.gather(1, at).double()
+        assert bool((inside.abs() <= 2 * EPS * q / T).all())
+        assert not grad.scatter(1, at, 0.0).any()
+        assert torch.equal(scoring.distill_loss(x, at, teacher, rest=True, temperature=T), loss)
+
+
+@pytest.mark.parametrize("gap", [0, 20, 100, 1000])
+def test_alternatives_that_are_all_a_teacher_says(gap):
+    """The student can say others, the teacher none but by rounding."""
+    g, V, top = gen(gap), 701, 30
+    x = torch.randn(200, V, generator=g, device="cuda") - gap
+    ids = torch.rand(200, V, generator=g, device="cuda").topk(top, -1).indices
+    x.scatter_(1, ids, torch.randn(200, top, generator=g, device="cuda"))
+    teacher = torch.log_softmax(2 * torch.randn(200, top, generator=g, device="cuda"), -1)
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=True)
+    want, dwant, off, doff = definition(x, ids, teacher, 1.0, slack(teacher))
+    near(loss, want, off)
+    near(grad, dwant, doff + HALF_ULP[F32] * dwant.abs() + 1e-37)
+    # and what is left by rounding is nothing
+    share = -grad.scatter(1, ids, 0.0).double()
+    assert bool((share <= 0).all())
+
+
+def test_a_rest_of_weight_is_kept():
+    """Of 1e-5 on: +inf where no other token can be said, the definition else."""
+    g, V, top = gen(1), 501, 12
+    x = torch.randn(3, V, generator=g, device="cuda")
+    ids = torch.rand(3, V, generator=g, device="cuda").topk(top, -1).indices
+    teacher = torch.log_softmax(torch.randn(3, top, generator=g, device="cuda"), -1) + torch.log1p(torch.tensor([[-1e-5]], device="cuda"))
+    check(x, ids, teacher)
+    none = torch.full_like(x, -INF).scatter(1, ids, x.gather(1, ids))
+    loss, grad = scoring.distill_loss_and_grad(none, ids, teacher, rest=True)
+    assert bool((loss == INF).all()) and bool(grad.isfinite().all())
