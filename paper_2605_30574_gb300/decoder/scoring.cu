@@ -1069,6 +1069,11 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 const float z = by.x * P.inv_T;
                 return make_float2(z, fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low));
             };
+            // (an infinity's rest would be NaN)
+            auto plus = [](float2 a, float2 b) {
+                const float x = a.x + b.x;
+                return fabsf(x) < INFINITY ? pair_sum(a, b) : make_float2(x, 0.f);
+            };
             float2 total = make_float2(0.f, 0.f);
             for (int k = lane; k < P.K; k += 32) {
                 const float q = t.q[k];
@@ -1078,22 +1083,18 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 const float2 log_p = pair_sum(z_of(t.z[k]), minus(log_s)), log_q = pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm));
                 const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_q, minus(log_p));
                 const float x = q * d.x;
-                total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(q, d.x, -x) + q * d.y));
+                total = plus(total, make_float2(x, none ? 0.f : fmaf(q, d.x, -x) + q * d.y));
             }
             if (lane == 0 && t.rest > 0.f) {
                 const bool none = a.others.y == 0.f;
                 const float2 log_p = pair_sum(pair_sum(z_of(a.others.x), log_others), minus(log_s));
                 const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_rest, minus(log_p));
                 const float x = t.rest * d.x;
-                total = none ? make_float2(total.x + x, 0.f) : pair_sum(total, make_float2(x, fmaf(t.rest, d.x, -x) + t.rest * d.y));
+                total = plus(total, make_float2(x, none ? 0.f : fmaf(t.rest, d.x, -x) + t.rest * d.y));
             }
-            // (an infinity's rest would be NaN)
-            const bool finite = __all_sync(0xffffffffu, fabsf(total.x) < INFINITY);
 #pragma unroll
-            for (int off = 16; off > 0; off /= 2) {
-                const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, total.x, off), __shfl_xor_sync(0xffffffffu, total.y, off));
-                total = finite ? pair_sum(total, o) : make_float2(total.x + o.x, 0.f);
-            }
+            for (int off = 16; off > 0; off /= 2)
+                total = plus(total, make_float2(__shfl_xor_sync(0xffffffffu, total.x, off), __shfl_xor_sync(0xffffffffu, total.y, off)));
             if (lane == 0) P.loss[row] = weight == 0.f ? 0.f : (total.x + total.y) * weight;
         }
         if (__syncthreads_or(s_abort)) break;
