@@ -1064,34 +1064,34 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             };
             auto minus = [](float2 a) { return make_float2(-a.x, -a.y); };
             const float2 log_s = of(0), log_others = of(1), log_rest = of(2), log_norm = of(3);
-            auto z_of = [&](float x) {          // (x - ref) / T
-                const float2 by = exact_sum(x, -a.ref);
-                const float z = by.x * P.inv_T;
-                return make_float2(z, fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low));
-            };
             // (an infinity's rest would be NaN)
             auto plus = [](float2 a, float2 b) {
                 const float x = a.x + b.x;
                 return fabsf(x) < INFINITY ? pair_sum(a, b) : make_float2(x, 0.f);
             };
             float2 total = make_float2(0.f, 0.f);
-            for (int k = lane; k < P.K; k += 32) {
-                const float q = t.q[k];
-                if (q == 0.f) continue;
-                // log q - log p; p is 0 where its logit is -inf or no token has one
-                const bool none = a.s == 0.f || t.z[k] == kNone;
-                const float2 log_p = pair_sum(z_of(t.z[k]), minus(log_s)), log_q = pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm));
-                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_q, minus(log_p));
-                const float x = q * d.x;
-                total = plus(total, make_float2(x, none ? 0.f : fmaf(q, d.x, -x) + q * d.y));
-            }
-            if (lane == 0 && t.rest > 0.f) {
-                const bool none = a.others.y == 0.f;
-                const float2 log_p = pair_sum(pair_sum(z_of(a.others.x), log_others), minus(log_s));
-                const float2 d = none ? make_float2(INFINITY, 0.f) : pair_sum(log_rest, minus(log_p));
-                const float x = t.rest * d.x;
-                total = plus(total, make_float2(x, none ? 0.f : fmaf(t.rest, d.x, -x) + t.rest * d.y));
-            }
+            // q (log q - log p) of log p = (x - ref) / T + log_w - log s; p is 0 where
+            // x is -inf or no token has any
+            auto add = [&](float q, float2 log_q, float x, float2 log_w, bool none) {
+                const float2 by = exact_sum(x, -a.ref);
+                const float z = by.x * P.inv_T, v = q * P.inv_T;
+                float2 y;
+                if (none) {
+                    y = make_float2(q * INFINITY, 0.f);
+                } else if (!(fabsf(z) < INFINITY)) {
+                    // (a mask of the type's lowest value: past fp32, its product with q perhaps not)
+                    y = make_float2(fabsf(by.x) < INFINITY ? -v * by.x : v * a.ref - v * x, 0.f);
+                } else {
+                    const float2 log_p = pair_sum(pair_sum(make_float2(z, fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low)), log_w), minus(log_s));
+                    const float2 d = pair_sum(log_q, minus(log_p));
+                    y = make_float2(q * d.x, fmaf(q, d.x, -(q * d.x)) + q * d.y);
+                }
+                total = plus(total, y);
+            };
+            for (int k = lane; k < P.K; k += 32)
+                if (t.q[k] != 0.f)
+                    add(t.q[k], pair_sum(make_float2(t.log_q[k], 0.f), minus(log_norm)), t.z[k], make_float2(0.f, 0.f), a.s == 0.f || t.z[k] == kNone);
+            if (lane == 0 && t.rest > 0.f) add(t.rest, log_rest, a.others.x, log_others, a.others.y == 0.f);
 #pragma unroll
             for (int off = 16; off > 0; off /= 2)
                 total = plus(total, make_float2(__shfl_xor_sync(0xffffffffu, total.x, off), __shfl_xor_sync(0xffffffffu, total.y, off)));

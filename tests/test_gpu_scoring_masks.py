@@ -1,4 +1,8 @@
-"""Divergences where logits are masked."""
+"""Divergences where logits are masked, by -inf or by their type's lowest value.
+
+Tolerance: 2^-19 of the loss' terms, as tests/test_gpu_scoring.py derives it; a
+term that is past the range of fp32 is an infinity.
+"""
 import pytest
 import torch
 
@@ -7,7 +11,8 @@ from paper_2605_30574_gb300 import decoder as K
 from paper_2605_30574_gb300.decoder import scoring
 
 pytestmark = pytest.mark.gpu
-INF = float("inf")
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+EPS, INF = 2.0 ** -19, float("inf")
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -33,3 +38,40 @@ def test_tokens_that_cannot_be_said_among_many(top, rest):
     assert bool((loss[:top] == INF).all()), loss
     assert bool(loss[top].isfinite()) and bool(grad.isfinite().all())
     assert torch.equal(scoring.distill_loss(x, ids, teacher, rest=rest), loss)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("T", [1.0, 0.6, 3.0])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_a_teachers_token_of_the_lowest_logit(dtype, T, rest):
+    V, low = 1003, torch.finfo(dtype).min
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x = torch.randn(5, V, generator=g, device="cuda").to(dtype)
+    ids = torch.tensor([[3, 1000, 77]], device="cuda").repeat(5, 1)
+    x[0, 77] = low                       # of weight 0.1 to the teacher
+    x[1, [3, 1000]] = low                # of 0.7
+    x[2] = low                           # all alike
+    x[3, :] = low
+    x[3, 500] = 1.0                      # one token that can be said, not the teacher's
+    x[4, 3], x[4, 77] = -low, low        # further apart than the type reaches
+    teacher = torch.tensor([[0.5, 0.2, 0.1]], device="cuda").log().repeat(5, 1)
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=rest, temperature=T)
+    z = x.double() / T
+    lp, t = torch.log_softmax(z, -1), teacher.double()
+    t = t if rest else torch.log_softmax(t, -1)
+    q, at = t.exp(), lp.gather(1, ids)
+    want, size = (q * (t - at)).sum(-1), (q * (1 + t.abs() + at.abs())).sum(-1)
+    target = torch.zeros_like(lp).scatter_(1, ids, q)
+    if rest:
+        left = 1 - q.sum(-1)
+        lpr = torch.logsumexp(lp.scatter(1, ids, -INF), -1)
+        want, size = want + left * (left.log() - lpr), size + 1 + left * (left.log().abs() + lpr.abs())
+        # (from the logits: log probabilities of 1e38 have no digits for the others' own)
+        target += torch.softmax(z.scatter(1, ids, -INF), -1) * left[:, None]
+    top = torch.finfo(F32).max
+    assert not loss.isnan().any()
+    assert bool((torch.where(want > top, loss == INF, (loss.double() - want).abs() <= EPS * size)).all()), (loss, want)
+    dwant = (lp.exp() - target) / T
+    ulp = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}[dtype]
+    assert bool(((grad.double() - dwant).abs() <= (EPS * (lp.exp() + target) + 2.0 ** -22) / T + ulp * dwant.abs() + 2.0 ** -25).all())
