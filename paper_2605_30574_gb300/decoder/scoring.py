@@ -67,8 +67,10 @@ def _tokens(what: str, name: str, t: torch.Tensor, shape) -> torch.Tensor:
 
 
 def _inverse(what: str, temperature: float) -> float:
-    if not (temperature > 0 and math.isfinite(temperature)):
-        raise ValueError(f"{what}: the temperature must be positive and finite")
+    # (finite in fp32: 1 / T, log2(e) / T, and 111 T, from where on below the
+    # maximum a weight counts as 2^-160)
+    if not 2.0 ** -127 <= temperature <= 2.0 ** 120:
+        raise ValueError(f"{what}: the temperature must be positive and finite, between 2^-127 and 2^120")
     return 1.0 / temperature
 
 

@@ -1,4 +1,5 @@
-"""Divergences where logits are masked, by -inf or by their type's lowest value.
+"""Divergences where logits are masked, by -inf or by their type's lowest value,
+and temperatures at and past the ends of their range.
 
 Tolerance: 2^-19 of the loss' terms, as tests/test_gpu_scoring.py derives it; a
 term that is past the range of fp32 is an infinity.
@@ -75,3 +76,40 @@ def test_a_teachers_token_of_the_lowest_logit(dtype, T, rest):
     dwant = (lp.exp() - target) / T
     ulp = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}[dtype]
     assert bool(((grad.double() - dwant).abs() <= (EPS * (lp.exp() + target) + 2.0 ** -22) / T + ulp * dwant.abs() + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("T", [2.0 ** -127, 1e-30, 1e30, 2.0 ** 120])
+def test_temperatures_at_the_ends(T):
+    V = 1003
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randn(4, V, generator=g, device="cuda")
+    x[1:, torch.rand(V, generator=g, device="cuda") < 0.5] = -INF
+    x[2, 7:300] = torch.finfo(F32).min
+    x[3] *= T ** 0.5
+    ids = x.topk(3, -1).indices
+    teacher = torch.tensor([[0.5, 0.2, 0.1]], device="cuda").log().repeat(4, 1)
+    got = scoring.token_logprobs(x, ids[:, 0], top=5, temperature=T)
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, temperature=T)
+    z = x.double() / T
+    lp = torch.log_softmax(z, -1)
+    p = lp.exp()
+    assert bool(((got.logprobs.double() - lp.gather(1, ids[:, :1])[:, 0]).abs() <= EPS * 40).all())
+    H = -torch.where(p > 0, p * lp, torch.zeros_like(p)).sum(-1)
+    assert bool(((got.entropy.double() - H).abs() <= EPS * 40).all())
+    t = torch.log_softmax(teacher.double(), -1)
+    q, at = t.exp(), lp.gather(1, ids)
+    want, size = (q * (t - at)).sum(-1), (q * (1 + t.abs() + at.abs())).sum(-1)
+    assert bool((torch.where(want > torch.finfo(F32).max, loss == INF, (loss.double() - want).abs() <= EPS * size)).all()), (loss, want)
+    target = torch.zeros_like(lp).scatter_(1, ids, q)
+    assert bool(((grad.double() - (p - target) / T).abs() <= EPS * (p + target) / T + 1e-37).all())
+
+
+def test_temperatures_past_the_ends_are_refused():
+    x = torch.zeros(2, 9, device="cuda")
+    ids, teacher = torch.zeros(2, 1, dtype=torch.long, device="cuda"), torch.zeros(2, 1, device="cuda")
+    for T in (3e-39, 1e-45, 1e-310, 2e36, 1e45, 1e300, INF):
+        for call in (lambda: scoring.token_logprobs(x, temperature=T), lambda: scoring.distill_loss(x, ids, teacher, temperature=T),
+                     lambda: scoring.distill_loss_and_grad(x, ids, teacher, temperature=T)):
+            with pytest.raises(ValueError, match="temperature"):
+                call()
