@@ -83,6 +83,20 @@ def plain(acts, weights) -> bool:
     return True
 
 
+_RECORDERS = tuple(getattr(torch._C._TorchDispatchModeKey, n) for n in ("FAKE", "PROXY", "FUNCTIONAL"))
+
+
+def untraced(what, function=False) -> None:
+    """Refuses a call where operations are recorded or only made believe
+    (``torch.jit.trace``, ``make_fx``, fake tensors): a launch is none of them, and
+    the graph would hold outputs that nothing fills.  (``torch.jit.trace`` records
+    an autograd ``function`` as itself, and ``torch.compile`` breaks its graph at
+    these calls: both run them.)"""
+    if (not function and torch.jit.is_tracing()) or (torch._C._len_torch_dispatch_stack()
+                                                     and any(torch._C._get_dispatch_mode(m) is not None for m in _RECORDERS)):
+        raise RuntimeError(f"{what} launches kernels that a tracer cannot record")
+
+
 def _values(t, dev) -> bool:
     """Whether the tensor's values are what lies at its address: not those of a
     negated view, nor none (an empty tensor, one of zeros without memory)."""

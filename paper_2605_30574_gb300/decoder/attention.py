@@ -14,7 +14,7 @@ and gradients are accumulated in fp32; probabilities and the gradients of scores
 are rounded to bf16 for their products.  The same inputs give the same bits.
 
 Kernels go to torch's current stream; a bounded wait that ran out shows in
-``decoder.check_device_error``.
+``decoder.check_device_error``.  Tracers, which would not record them, are refused.
 """
 from __future__ import annotations
 
@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import BF16, F32, _current_device, _launch
+from . import BF16, F32, _current_device, _launch, untraced
 
 
 def _fits(q, k, v):
@@ -110,11 +110,16 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     """Attention's output, like q and contiguous, and the rows' log sums of
     e^(scale q . k), fp32 [Hq, Tq] ([B, Hq, Tq]); -inf for a row that sees no
     key.  ``scale`` is 1 / sqrt(d) by default."""
+    return _forward(q, k, v, scale, False)
+
+
+def _forward(q, k, v, scale, function):
+    untraced("attention_forward", function)
     _check("attention_forward", q, k, v)
     device = q.device
     if device.index != _current_device():
         with torch.cuda.device(device):
-            return attention_forward(q, k, v, scale)
+            return _forward(q, k, v, scale, function)
     *B, Tq, Hq, d = q.shape
     Hkv, Tk, _ = k.shape[-3:]
     out = torch.empty(q.shape, dtype=BF16, device=device)
@@ -132,6 +137,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """Gradients with respect to q, k and v (bf16, contiguous), given the
     output's, and output and log sums as ``attention_forward`` gave them."""
     what = "attention_backward"
+    untraced(what)
     _check(what, q, k, v)
     shape, device = q.shape, q.device
     *B, Tq, Hq, d = shape
@@ -166,7 +172,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale):
-        out, lse = attention_forward(q, k, v, scale)
+        out, lse = _forward(q, k, v, scale, True)
         ctx.save_for_backward(q, k, v, out, lse)
         ctx.scale = scale
         return out

@@ -10,6 +10,7 @@ logits where the rows' weights are known beforehand.
 Logits are CUDA tensors [..., V] of fp32, bf16 or fp16 whose rows may lie apart
 (a slice of a padded vocabulary); tokens of other strides or int32 are copied.
 Kernels go to torch's current stream and read and write on the device only.
+Tracers, which would not record them, are refused.
 Sums are in fp32 in a fixed order: the same inputs give the same bits.
 """
 from __future__ import annotations
@@ -19,7 +20,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from . import _current_device, _launch, lib
+from . import _current_device, _launch, lib, untraced
 
 TOP_MAX = 128
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -87,6 +88,7 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     numbers NaN; NaN comes last in the order of tokens, with -inf.  No gradient
     (``distill_loss`` of one alternative has it)."""
     what = "token_logprobs"
+    untraced(what)
     x = _rows_of(logits, what)
     rows, V = x.shape
     lead = logits.shape[:-1]
@@ -140,11 +142,12 @@ def _f32(t):
     return t
 
 
-def _distill(x, ids, teacher, weight, rest, inv_T, grad):
+def _distill(x, ids, teacher, weight, rest, inv_T, grad, function=True):
     """Loss [rows] and, if asked for, the gradient [rows][V]."""
+    untraced("distillation", function)
     if x.device.index != _current_device():
         with torch.cuda.device(x.device):
-            return _distill(x, ids, teacher, weight, rest, inv_T, grad)
+            return _distill(x, ids, teacher, weight, rest, inv_T, grad, function)
     rows, V = x.shape
     loss = torch.empty(rows, dtype=torch.float32, device=x.device)
     dx = torch.empty((rows, V), dtype=x.dtype, device=x.device) if grad else None
@@ -206,7 +209,7 @@ def distill_loss_and_grad(logits: torch.Tensor, ids: torch.Tensor, teacher: torc
     their type, contiguous), in one pass."""
     x, ids, teacher, weight, inv_T = _distill_args("distill_loss_and_grad", logits, ids, teacher, weight, temperature)
     with torch.no_grad():
-        loss, dx = _distill(x, ids, teacher, weight, rest, inv_T, True)
+        loss, dx = _distill(x, ids, teacher, weight, rest, inv_T, True, False)
     if logits.dim() != 2:
         loss, dx = loss.view(logits.shape[:-1]), dx.view(logits.shape)
     return loss, dx
