@@ -103,6 +103,14 @@ def _values(t, dev) -> bool:
     return t.device == dev and t.is_contiguous() and not t.is_neg() and t.numel() > 0 and t.data_ptr() != 0
 
 
+def there(what, name, t):
+    """The tensor, if it has memory or needs none: torch's tensors of zeros
+    without any, and those whose storage was given back, are at address 0."""
+    if t.data_ptr() == 0 and t.numel() > 0:
+        raise ValueError(f"{what}: {name} has no memory")
+    return t
+
+
 def joined(*ws):
     """The matrices as one, when they are consecutive rows of one contiguous
     matrix (as the decoder lays them out), else None."""

@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import BF16, F32, _current_device, _launch, untraced
+from . import BF16, F32, _current_device, _launch, there, untraced
 
 
 def _fits(q, k, v):
@@ -80,6 +80,8 @@ def _operands(*ts):
     ptrs, low, plain = [], 0, True
     for t in ts:
         p = t.data_ptr()
+        if not p:
+            raise ValueError("attention: an operand has no memory")
         ptrs.append(p)
         if t.is_neg():
             low = 1
@@ -160,6 +162,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     ts, ptrs, strides = _operands(dout, q, out, k, v)      # (ts: copies live until the launch)
     if not lse.is_contiguous() or lse.is_neg():
         lse = lse.resolve_neg().contiguous()
+    there(what, "lse", lse)
     dq = torch.empty(shape, dtype=BF16, device=device)
     dk = torch.empty(k.shape, dtype=BF16, device=device)
     dv = torch.empty(k.shape, dtype=BF16, device=device)

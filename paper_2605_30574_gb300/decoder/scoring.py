@@ -20,7 +20,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from . import _current_device, _launch, lib, untraced
+from . import _current_device, _launch, lib, there, untraced
 
 TOP_MAX = 128
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -50,7 +50,7 @@ def _rows_of(logits: torch.Tensor, what: str) -> torch.Tensor:
         logits = logits.reshape(-1, logits.shape[-1])
     if logits.stride(1) != 1 and logits.shape[1] > 1:
         logits = logits.contiguous()
-    return logits
+    return there(what, "logits", logits)
 
 
 def _same_device(what: str, logits: torch.Tensor, **others) -> None:
@@ -64,7 +64,7 @@ def _tokens(what: str, name: str, t: torch.Tensor, shape) -> torch.Tensor:
         raise TypeError(f"{what}: {name} must be a tensor of int64 or int32")
     if t.shape != shape:
         raise ValueError(f"{what}: {name} must have the shape {tuple(shape)}")
-    return t if t.dtype is torch.int64 and t.is_contiguous() else t.long().contiguous()
+    return there(what, name, t if t.dtype is torch.int64 and t.is_contiguous() else t.long().contiguous())
 
 
 def _inverse(what: str, temperature: float) -> float:
@@ -133,13 +133,13 @@ def _distill_args(what, logits, ids, teacher, weight, temperature):
         if weight.shape != lead:
             raise ValueError(f"{what}: weight must have the shape {tuple(lead)}")
     _same_device(what, x, ids=ids, teacher=teacher, weight=weight)
-    return x, ids, _f32(teacher), None if weight is None else _f32(weight), _inverse(what, temperature)
+    return x, ids, _f32(what, "teacher", teacher), None if weight is None else _f32(what, "weight", weight), _inverse(what, temperature)
 
 
-def _f32(t):
+def _f32(what, name, t):
     if t.dtype is not torch.float32 or not t.is_contiguous() or t.is_neg():
         t = t.detach().to(torch.float32).resolve_neg().contiguous()
-    return t
+    return there(what, name, t)
 
 
 def _distill(x, ids, teacher, weight, rest, inv_T, grad, function=True):
@@ -171,7 +171,7 @@ class _DistillLoss(torch.autograd.Function):
         # (the row's sums again, from the read that the gradient needs anyway)
         x, ids, teacher, weight = ctx.saved_tensors
         w = grad_loss if weight is None else grad_loss * weight
-        return (_distill(x, ids, teacher, _f32(w), ctx.rest, ctx.inv_T, True)[1],) + (None,) * 5
+        return (_distill(x, ids, teacher, _f32("distill_loss", "the loss' gradient", w), ctx.rest, ctx.inv_T, True)[1],) + (None,) * 5
 
 
 def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, *,
