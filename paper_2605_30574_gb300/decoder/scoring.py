@@ -64,7 +64,9 @@ def _tokens(what: str, name: str, t: torch.Tensor, shape) -> torch.Tensor:
         raise TypeError(f"{what}: {name} must be a tensor of int64 or int32")
     if t.shape != shape:
         raise ValueError(f"{what}: {name} must have the shape {tuple(shape)}")
-    return there(what, name, t if t.dtype is torch.int64 and t.is_contiguous() else t.long().contiguous())
+    if t.dtype is not torch.int64 or not t.is_contiguous() or t.is_neg():
+        t = t.long().resolve_neg().contiguous()
+    return there(what, name, t)
 
 
 def _inverse(what: str, temperature: float) -> float:

@@ -1,5 +1,5 @@
 """Tensors without memory (torch's zeros that have none, storage given back) are
-refused before a kernel could read address 0."""
+refused before a kernel could read address 0; negated views are read as such."""
 import pytest
 import torch
 
@@ -33,3 +33,10 @@ def test_operands_without_memory(nothing):
     # (none is needed)
     empty = torch.zeros(0, dtype=torch.int64)
     assert scoring._tokens("a call", "tokens", empty, (0,)).shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
+def test_tokens_that_are_a_negated_view(dtype):
+    t = torch._neg_view(torch.tensor([1, -2, 3], dtype=dtype))
+    got = scoring._tokens("a call", "tokens", t, (3,))
+    assert not got.is_neg() and got.is_contiguous() and got.tolist() == [-1, 2, -3]
