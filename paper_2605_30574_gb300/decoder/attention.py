@@ -9,7 +9,8 @@ and gradients are 0.
 
 q is [Tq, Hq, d] and k, v are [Hkv, Tk, d] (as the decoder's stores lay a layer
 out), or all with a batch in front; bf16, d 64, 128 or 256, Hq a multiple of
-Hkv, any strides (those that the kernels cannot read are copied).  Scores, sums
+Hkv, any strides (those that the kernels cannot read are copied); lengths, and
+batch times heads, of up to 2^20.  Scores, sums
 and gradients are accumulated in fp32; probabilities and the gradients of scores
 are rounded to bf16 for their products.  The same inputs give the same bits.
 

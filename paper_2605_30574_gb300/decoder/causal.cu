@@ -437,7 +437,6 @@ int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::
 template <bool LSE>
 int launch(const decoder::Operand& q, const decoder::Operand& k, const decoder::Operand& v, void* out, float* lse, long B, long Tq, long Tk,
            int Hq, int Hkv, int d, float scale, cudaStream_t st) {
-    if (!decoder::attention_takes(B, Tq, Tk, Hq, Hkv)) return int(cudaErrorInvalidValue);
     if (d == 64) return launch<64, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
     if (d == 128) return launch<128, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
     if (d == 256) return launch<256, LSE>(q, k, v, out, lse, int(B), int(Tq), int(Tk), Hq, Hkv, scale, st);
@@ -451,6 +450,7 @@ extern "C" {
 // See the head of this file; 16-byte aligned.  Returns a cudaError_t.
 int decoder_causal(const void* q, const void* k, const void* v, void* out, long T, int Hq, int Hkv, int d, float scale,
                    void* stream) {
+    if (T < 1 || T > (1 << 20) || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return int(cudaErrorInvalidValue);
     const decoder::Operand oq{q, long(Hq) * d, d, T * Hq * d}, ok{k, d, T * d, T * Hkv * d}, ov{v, d, T * d, T * Hkv * d};
     return launch<false>(oq, ok, ov, out, nullptr, 1, T, T, Hq, Hkv, d, scale, static_cast<cudaStream_t>(stream));
 }
@@ -464,6 +464,7 @@ int decoder_causal(const void* q, const void* k, const void* v, void* out, long 
 // e^(scale q . k), -inf for a row that sees nothing).
 int decoder_attention(const void* q, const void* k, const void* v, const long* strides, void* out, void* lse, long B, long Tq,
                       long Tk, int Hq, int Hkv, int d, float scale, void* stream) {
+    if (!decoder::attention_takes(B, Tq, Tk, Hq, Hkv)) return int(cudaErrorInvalidValue);
     const long of_q[3] = {long(Hq) * d, d, Tq * Hq * d}, of_k[3] = {d, Tk * d, Tk * Hkv * d};
     auto operand = [&](const void* p, int i) {
         const long* s = strides ? strides + 3 * i : i == 0 ? of_q : of_k;

@@ -22,8 +22,8 @@ bool gemm_takes(int M, int N, int K);
 int gemm(int mode, const void* x, const void* w0, const void* w1, const void* h, void* y, int M, int N, int K,
          cudaStream_t stream);
 
-// The shapes that the attention kernels take: lengths whose row indices and
-// grids stay within 32 bits.
+// The shapes that attention with log sums and its gradients take: lengths whose
+// row indices and grids stay within 32 bits.
 inline bool attention_takes(long B, long Tq, long Tk, int Hq, int Hkv) {
     constexpr long kMax = 1L << 20;
     return B >= 1 && B <= 65536 && Tq >= 1 && Tq <= kMax && Tk >= 1 && Tk <= kMax && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 &&
