@@ -87,7 +87,8 @@ def attribute(run, prompt: int, slot: int, tokens: torch.Tensor, L: int = 0, top
     with torch.enable_grad():
         logits = continuation_logits(model, tokens, *spans)
         loss = scoring.distill_loss(logits, clean.top_ids, clean.top_logprobs, rest=True)
-        loss.mean().backward()
+        if loss.requires_grad:          # (L past the last layer: nothing is spliced)
+            loss.mean().backward()
     spliced = scoring.token_logprobs(logits.detach(), after)
     attribution = torch.zeros(model.dims.num_layers, clean_k[0].shape[1], device=tokens.device)
     for clean_span, span in zip((clean_k, clean_v), spans):
