@@ -25,7 +25,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import BF16, F32, _current_device, _launch, there, untraced
+from . import BF16, F32, _current_device, _launch, lib, there, untraced
 
 
 def _fits(q, k, v):
@@ -167,7 +167,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     dq = torch.empty(shape, dtype=BF16, device=device)
     dk = torch.empty(k.shape, dtype=BF16, device=device)
     dv = torch.empty(k.shape, dtype=BF16, device=device)
-    scratch = torch.empty(40 * B * Hq * ((Tq + 127) // 128 * 128), dtype=torch.uint8, device=device)
+    scratch = torch.empty(lib().decoder_attention_scratch(B, Tq, Hq), dtype=torch.uint8, device=device)
     _launch("decoder_attention_backward", *ptrs, lse.data_ptr(), strides, scratch.data_ptr(), dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), B, Tq, Tk, Hq, Hkv, d, _scale(scale, d))
     return dq, dk, dv
