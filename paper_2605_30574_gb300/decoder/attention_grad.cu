@@ -774,7 +774,7 @@ int backward(const Args& a, cudaStream_t st) {
         attr.val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        const int e = int(cudaLaunchKernelEx(&cfg, stats_kernel<D>, a.dout, a.out, a.lse, lse2, delta, aug, by_keys_scale, a.Tq, Tpad, a.Hq, rows));
+        const int e = int(cudaLaunchKernelEx(&cfg, stats_kernel<D>, a.dout, a.out, a.lse, lse2, delta, aug, by_keys_scale, a.Tq, Tpad, a.Hq, rows / 8));
         if (e != 0) return e;
     }
     // (a map of 128 rows serves as the fixed operand's and as the blocks')
