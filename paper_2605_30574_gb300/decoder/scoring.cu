@@ -891,11 +891,12 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
 
     // What a row's gradient goes by: p_j = e^((x_j - ref) / T) / s; the gradient of
     // a token that is not the teacher's is out e^((x_j - out_ref) / T), of one that
-    // is (all p_j - q_j); all times scale.  Where the rest has weight, the others go
-    // by their own largest logit and sum: what the rest gives them is q_rest times
-    // their shares of it, and does not vanish where p_rest does, 87 nats below ref.
+    // is (all p_j - q_j); all times scale.  Where the others lie far below ref they
+    // go by their own largest logit: what the rest gives them is q_rest times their
+    // shares of it, and does not vanish where p_rest does.  Else p_rest is taken from
+    // the same sum as s: an error in it then counts p_rest - q_rest times in the loss.
     struct Stats {
-        float2 others;              // largest x, sum of e^ from there
+        float2 others;              // an x, and the others' sum of e^ from there
         float ref, s, inv_s, all, out_ref, out, scale;
     };
     __shared__ Stats s_stats;
@@ -905,17 +906,19 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         const float2 others = together(lane < C ? s_cta[turn][lane] : make_float2(kNone, 0.f));
         const float m = fmaxf(others.x, t.most);
         Stats a;
-        a.others = others;
         a.ref = m == kNone ? 0.f : m;
-        a.s = (others.x == kNone ? others.y : others.y * ex2((others.x - a.ref) * c)) +
-              (t.most == kNone ? t.e : t.e * ex2((t.most - a.ref) * c));
+        // (-inf: a sum of 0, or NaN)
+        const float2 f = weights_of<float>(make_float2(others.x, t.most), a.ref, 1.f, P);
+        const bool far = f.x < 0x1p-64f;
+        a.others = far ? others : make_float2(a.ref, others.y * f.x);
+        a.s = others.y * f.x + t.e * f.y;
         a.inv_s = a.s == 0.f ? 0.f : 1.f / a.s;
         a.all = P.rest ? 1.f : t.all;
         a.out_ref = a.ref;
         a.out = a.all * a.inv_s;
         if (t.rest != 0.f && others.y > 0.f) {      // (of 0: nothing to share it)
-            a.out_ref = others.x;
-            a.out = weights_of<float>(make_float2(others.x, 0.f), a.ref, a.inv_s, P).x - t.rest / others.y;
+            if (far) a.out_ref = others.x;
+            a.out = (far ? f.x * a.inv_s : a.inv_s) - t.rest / a.others.y;
         }
         a.scale = weight * P.inv_T;
         return a;

@@ -161,3 +161,22 @@ def test_a_rest_of_weight_is_kept():
     none = torch.full_like(x, -INF).scatter(1, ids, x.gather(1, ids))
     loss, grad = scoring.distill_loss_and_grad(none, ids, teacher, rest=True)
     assert bool((loss == INF).all()) and bool(grad.isfinite().all())
+
+
+@pytest.mark.parametrize("T", [1.5, 1.0])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_small_divergences(dtype, T):
+    """Of rows that the teacher has all but right: the loss is a small difference
+    of log probabilities.  The row's sums are rounded (2^-24) independently from row
+    to row; what all rows share may not come to more."""
+    g, rows, V = gen(21), 1000, 20011
+    x = torch.randn(rows, V, generator=g, device="cuda") * (1 + 2 * torch.rand(rows, 1, generator=g, device="cuda"))
+    x.scatter_add_(1, torch.randint(0, V, (rows, 4), generator=g, device="cuda"), 4 + 8 * torch.rand(rows, 4, generator=g, device="cuda"))
+    t = (x + 0.1 * torch.randn(rows, V, generator=g, device="cuda")) / T
+    teacher, ids = t.topk(40, -1)
+    teacher = teacher - t.logsumexp(-1, keepdim=True)
+    x = x.to(dtype)
+    loss = scoring.distill_loss(x, ids, teacher, rest=True, temperature=T)
+    want = definition(x, ids, teacher, T)[0]
+    off = (loss.double() - want).square().mean().sqrt()
+    assert float(off) <= 2.0 ** -24, float(off)
