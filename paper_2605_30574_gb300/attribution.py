@@ -2,8 +2,8 @@
 
 A sweep measures what happens when a donor's K and V stand in for the prompt
 span from layer L on.  This module asks how much of that each layer and position
-accounts for, with one backward pass in place of a sweep over them (attribution
-patching): the clean run's continuation is fed to the spliced model, the loss is
+accounts for, to first order and with one backward pass (attribution patching):
+the clean run's continuation is fed to the spliced model, the loss is
 the divergence of its next-token distributions from the clean run's top
 alternatives, and
 
@@ -16,6 +16,9 @@ The continuation's attention over span and own keys and its gradients are
 ``decoder.attention``'s, the clean run's alternatives and both runs' token
 scores ``decoder.scoring.token_logprobs``', the loss ``distill_loss``'.  Where a
 gradient is asked for, the decoder's other pieces are its torch expressions.
+
+Nothing here waits for the GPU but ``restored``: a kernel's bounded wait that ran
+out shows in ``decoder.check_device_error``.
 
 ``python -m paper_2605_30574_gb300.attribution`` prints the attribution of every
 layer for each donor kind, beside what restoring the whole layer really does.

@@ -42,17 +42,22 @@
 // 256 dims: blocks of 64, and dK and dV, which do not fit in TMEM together, in
 // a launch each.
 //
-// 32 heads of 128, 8 for keys: 4096 positions 340 us (1.01 PFLOP/s of the five
-// products that the gradients are, 1.41 of the seven), 1024 49; 4 x 100 rows of
-// 4196 135.  The loops take 84% (by keys) and 81% of the tensor cores' rate; a CTA's
+// 32 heads of 128, 8 for keys: 4096 positions 335 us in a row of calls of its own,
+// 355 among others (1.03 and 0.97 PFLOP/s of the five products that the gradients
+// are, 1.44 and 1.36 of the seven), 1024 49 and 52; 4 x 100 rows of 4196 136.  The
+// loops take 84% (by keys) and 81% of the tensor cores' rate; a CTA's
 // operands in, and its sums out, the time of 8 blocks more.
 //
-// delta has the error of an output in bf16, which rows of few keys show: dQ and dK
-// of 2, 6, 17, 28 and 64 positions are off by 0.0047, 0.0044, 0.0030, 0.0024 and
-// 0.0024 of their size, where P, dS and the outputs in bf16 make 0.0024.  dS sums to
-// 0 over a row; so where the 32 keys of a thread by queries, or of a warp by keys,
-// are all that there are, the sum that it has all the same, times P, is taken from
-// it: 0.0025, 0.0027, 0.0025 and 0.0023, in 14.6 us for 12.7 (8 heads of 64).
+// P, dS and the outputs in bf16, 1.7e-3 of their size each, make errors of 2.3e-3;
+// an fp32 product of P and dS has the outputs' 1.7e-3 alone, at tf32's half rate or
+// of two bf16 terms each (ten products for seven).  delta has the error of an output
+// in bf16 besides, which rows of few keys show: dQ and dK of 2, 6, 17 and 28
+// positions would be off by 4.7e-3, 4.4e-3, 3.0e-3 and 2.4e-3.  dS sums to 0 over a
+// row; so where the 32 keys of a thread by queries, or of a warp by keys, are all
+// that there are, the sum that it has all the same, times P, is taken from it: 2.3e-3
+// to 2.7e-3, in 14.6 us for 12.7 (8 heads of 64).  From 33 keys on it is not: 2.6e-3
+// to 2.7e-3 at 33 to 40, 2.5e-3 to 2.6e-3 at 64 to 256, 2.4e-3 from 1000 on (means of
+// 4 inputs; single ones of few rows up to 2.9e-3).
 //
 // Every wait is bounded, as in gemm.cu.
 #include <cooperative_groups.h>

@@ -18,7 +18,9 @@
 //
 // With the rows' log sums (LSE), for the gradients of attention_grad.cu: a batch,
 // queries that are the last T of Tk positions, any strides, and P in two bf16 terms:
-// 4096 tokens 172 us.  Few tiles share their keys over a cluster, whose CTAs trade
+// 4096 tokens 173 us.  The second term makes the output the exact one's rounding
+// (off by 1.5e-3 to 1.6e-3 of its size at 32 to 2000 keys, for 1.7e-3 to 2.0e-3); the
+// gradients, whose delta takes it, gain no more than 2% of their error.  Few tiles share their keys over a cluster, whose CTAs trade
 // maxima, sums and outputs through distributed shared memory: one row of 4196 keys
 // 22.5 us, and 62 without.
 //
@@ -262,8 +264,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::CTAS)
             const float ref = m == -INFINITY ? 0.f : m;
             // (the weights as they are used, rounded: their sum then makes up
             // for part of the rounding.  LSE: as they are, and used in two
-            // terms of bf16, as the gradients take the difference of their
-            // product with this output)
+            // terms of bf16)
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {

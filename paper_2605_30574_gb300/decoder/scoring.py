@@ -9,8 +9,10 @@ logits where the rows' weights are known beforehand.
 
 Logits are CUDA tensors [..., V] of fp32, bf16 or fp16 whose rows may lie apart
 (a slice of a padded vocabulary); tokens of other strides or int32 are copied.
-Kernels go to torch's current stream and read and write on the device only.
-Tracers, which would not record them, are refused.
+Kernels go to torch's current stream and read and write on the device only; a
+bounded wait of a distillation that ran out shows in
+``decoder.check_device_error``.  Tracers, which would not record the launches, are
+refused.
 Sums are in fp32 in a fixed order: the same inputs give the same bits.
 """
 from __future__ import annotations
