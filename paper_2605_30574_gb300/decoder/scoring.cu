@@ -1077,6 +1077,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 return fabsf(x) < INFINITY ? pair_sum(a, b) : make_float2(x, 0.f);
             };
             float2 total = make_float2(0.f, 0.f);
+            const float no_number = a.s - a.s;      // NaN in a row with NaN or +inf, else 0
             // q (log q - log p) of log p = (x - ref) / T + log_w - log s; p is 0 where
             // x is -inf or no token has any
             auto add = [&](float q, float2 log_q, float x, float2 log_w, bool none) {
@@ -1084,10 +1085,10 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 const float z = by.x * P.inv_T, v = q * P.inv_T;
                 float2 y;
                 if (none) {
-                    y = make_float2(q * INFINITY, 0.f);
+                    y = make_float2(q * INFINITY + no_number, 0.f);
                 } else if (!(fabsf(z) < INFINITY)) {
                     // (a mask of the type's lowest value: past fp32, its product with q perhaps not)
-                    y = make_float2(fabsf(by.x) < INFINITY ? -v * by.x : v * a.ref - v * x, 0.f);
+                    y = make_float2((fabsf(by.x) < INFINITY ? -v * by.x : v * a.ref - v * x) + no_number, 0.f);
                 } else {
                     const float2 log_p = pair_sum(pair_sum(make_float2(z, fmaf(by.x, P.inv_T, -z) + fmaf(by.y, P.inv_T, by.x * P.inv_T_low)), log_w), minus(log_s));
                     const float2 d = pair_sum(log_q, minus(log_p));

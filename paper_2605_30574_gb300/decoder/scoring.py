@@ -197,8 +197,9 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
     row of weight 0, whatever else it holds.  An id that comes twice counts
     twice; one past the vocabulary makes its row NaN.  Where the teacher has
     weight on a logit of -inf the loss is +inf, and where it has some on the rest
-    and all other logits are -inf.  Differentiable with respect to the logits; the
-    teacher and the weights get no gradient."""
+    and all other logits are -inf; a NaN or +inf among a row's logits makes it NaN.
+    Differentiable with respect to the logits; the teacher and the weights get no
+    gradient."""
     x, ids, teacher, weight, inv_T = _distill_args("distill_loss", logits, ids, teacher, weight, temperature)
     if weight is not None:
         weight = weight.reshape(-1)

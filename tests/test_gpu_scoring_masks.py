@@ -113,3 +113,25 @@ def test_temperatures_past_the_ends_are_refused():
                      lambda: scoring.distill_loss_and_grad(x, ids, teacher, temperature=T)):
             with pytest.raises(ValueError, match="temperature"):
                 call()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_rows_with_infinity_or_nan(dtype, rest):
+    """Their loss and gradient are NaN, whatever the teacher's tokens are."""
+    V, low = 517, torch.finfo(dtype).min
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x = torch.randn(8, V, generator=g, device="cuda").to(dtype)
+    ids = torch.tensor([[3, 500, 77]], device="cuda").repeat(8, 1)
+    teacher = torch.tensor([[0.5, 0.2, 0.1]], device="cuda").log().repeat(8, 1)
+    for r, bad in enumerate((INF, float("nan"))):
+        x[4 * r:4 * r + 4, 100] = bad
+        x[4 * r + 1, ids[0]] = -INF
+        x[4 * r + 2, ids[0]] = low
+        x[4 * r + 3, :] = -INF
+        x[4 * r + 3, 100] = bad
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=rest, temperature=0.6)
+    assert bool(loss.isnan().all()), loss
+    assert bool(grad.isnan().any(-1).all())
+    assert bool(scoring.distill_loss(x, ids, teacher, rest=rest, temperature=0.6).isnan().all())
