@@ -913,7 +913,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         a.ref = m == kNone ? 0.f : m;
         // (-inf: a sum of 0, or NaN)
         const float2 f = weights_of<float>(make_float2(others.x, t.most), a.ref, 1.f, P);
-        const bool far = f.x < 0x1p-64f;
+        const bool far = f.x < 0x1p-24f;
         a.others = far ? others : make_float2(a.ref, others.y * f.x);
         a.s = others.y * f.x + t.e * f.y;
         a.inv_s = a.s == 0.f ? 0.f : 1.f / a.s;

@@ -180,3 +180,17 @@ def test_small_divergences(dtype, T):
     want = definition(x, ids, teacher, T)[0]
     off = (loss.double() - want).square().mean().sqrt()
     assert float(off) <= 2.0 ** -24, float(off)
+
+
+@pytest.mark.parametrize("gap", [20, 40, 44, 60])
+def test_shares_of_the_rest_over_many_nats(gap):
+    """Each other token's share of what the rest gives, down to e^-50 of the
+    largest: its exponent, of up to 50, is rounded by 2^-24 of itself twice."""
+    V = 701
+    x = torch.linspace(0, -50, V, device="cuda")[None] - gap
+    ids = torch.tensor([[5, 350, 700]], device="cuda")
+    x[0, ids[0]] = torch.tensor([0.0, -1.0, -2.0], device="cuda")
+    teacher = torch.tensor([[0.4, 0.2, 0.1]], device="cuda").log()
+    _, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=True)
+    _, want, _, _ = definition(x, ids, teacher, 1.0)
+    assert bool(((grad.double() - want).abs() <= (EPS + 100 * 2.0 ** -24) * want.abs() + 2 * EPS * torch.softmax(x.double(), -1)).all())
