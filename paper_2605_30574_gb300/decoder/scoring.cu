@@ -690,6 +690,7 @@ struct Teacher {
     float sum[kMaxTop];                 // of all mentions of the token, at its first; -1: not the first
     float most, e;                      // the tokens' largest logit, and sum of e^(z - most)
     float all, rest;                    // the teacher's sum, and what is left of 1
+    bool none;                          // whether it says nothing of the row
     float norm;                         // shift is log(norm)
     unsigned edges;                     // which of the first 8 elements, and of the 8 before the last word's end, are the teacher's
 };
@@ -850,10 +851,14 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         // 128 tokens: left at up to 2.9 x 2^-23 sum q (1 + |log q|), in fp32.)
         const float left = pair_sum(make_float2(1.f, 0.f), make_float2(-all.x, -all.y)).x, least = 0x1p-21f * sizes;
         __syncwarp();
-        bool again = false;
+        bool again = false, any = outside;
 #pragma unroll
-        for (int j = 0; j < J; ++j) again |= id[j] >= 0 && !first[j];
+        for (int j = 0; j < J; ++j) {
+            again |= id[j] >= 0 && !first[j];
+            any |= P.rest ? id[j] >= 0 : q[j] != 0.f;
+        }
         again = __any_sync(0xffffffffu, again);
+        any = __any_sync(0xffffffffu, any);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             float own = q[j];
@@ -867,7 +872,8 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             t.edges = edges;
             t.norm = P.rest || sum == 0.f ? 1.f : sum;
             t.all = all.x;
-            t.rest = P.rest && (left > least || left != left) ? left : 0.f;
+            t.rest = P.rest && any && (left > least || left != left) ? left : 0.f;
+            t.none = !any;
         }
     };
     // of sums with their largest x, over a warp (-inf: a sum of 0, or NaN)
@@ -924,7 +930,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             if (far) a.out_ref = others.x;
             a.out = (far ? f.x * a.inv_s : a.inv_s) - t.rest / a.others.y;
         }
-        a.scale = weight * P.inv_T;
+        a.scale = t.none ? 0.f : weight * P.inv_T;
         return a;
     };
     auto exchanged = [&]() { return wait_cluster(bar0 + 8u * (1 + turn), round, &s_abort, P.err, kErrRow); };
@@ -989,7 +995,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 T* out = static_cast<T*>(P.grad) + row * P.V;
                 const bool words_out = (reinterpret_cast<uintptr_t>(out + p.in.head) & 15u) == 0;
                 const float k = a.out * a.scale;
-                if (weight == 0.f) {         // a row that is left out
+                if (a.scale == 0.f) {        // a row that is left out
                     if (words_out) {
                         for (int w = tid; w < p.nw; w += kWorkers) reinterpret_cast<uint4*>(out + first_word)[w] = make_uint4(0, 0, 0, 0);
                     } else {
@@ -1015,7 +1021,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
                 tc::fence_proxy_async_smem();
                 workers_sync();
                 if (tid == 0 && more) ask(next);
-                if (edge >= 0) out[edge] = from_float<T>(weight == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.out_ref, k, P).x);
+                if (edge >= 0) out[edge] = from_float<T>(a.scale == 0.f ? 0.f : weights_of<T>(make_float2(edge_x, 0.f), a.out_ref, k, P).x);
             }
             if (__syncthreads_or(s_abort)) {         // (a wait ran out; the copy on its way lands first)
                 volatile int no_abort = 0;

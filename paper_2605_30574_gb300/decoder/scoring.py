@@ -193,8 +193,8 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
       the rounding of log probabilities that are all there are, 2^-21 sum_k q_k (1
       + |log q_k|).
 
-    An id below 0 is no alternative; a row with none has the loss 0, and so has a
-    row of weight 0, whatever else it holds.  An id that comes twice counts
+    An id below 0 is no alternative; a row with none has the loss 0 and no
+    gradient, and so has a row of weight 0, whatever else they hold.  An id that comes twice counts
     twice; one past the vocabulary makes its row NaN.  Where the teacher has
     weight on a logit of -inf the loss is +inf, and where it has some on the rest
     and all other logits are -inf; a NaN or +inf among a row's logits makes it NaN.

@@ -135,3 +135,22 @@ def test_rows_with_infinity_or_nan(dtype, rest):
     assert bool(loss.isnan().all()), loss
     assert bool(grad.isnan().any(-1).all())
     assert bool(scoring.distill_loss(x, ids, teacher, rest=rest, temperature=0.6).isnan().all())
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_rows_without_alternatives(dtype, rest):
+    """No loss and no gradient, whatever else they hold."""
+    x = torch.randn(7, 517, device="cuda").to(dtype)
+    x[1, 5], x[2, 516], x[3, 0] = float("nan"), INF, -INF
+    x[4], x[5], x[6] = -INF, float("nan"), torch.finfo(dtype).min
+    teacher = torch.full((7, 40), -3.0, device="cuda")
+    cases = [(torch.full((7, 40), -1, device="cuda"), teacher)]
+    if not rest:
+        cases.append((torch.arange(40, device="cuda").repeat(7, 1), torch.full_like(teacher, -INF)))
+    for ids, t in cases:
+        for y in (x, torch.cat([x, x], -1)[:, 3:520], x[:, 2:3]):
+            if ids.max() < y.shape[1]:
+                loss, grad = scoring.distill_loss_and_grad(y, ids, t, rest=rest)
+                assert not loss.any() and not grad.any(), loss
+                assert not scoring.distill_loss(y, ids, t, rest=rest).any()
