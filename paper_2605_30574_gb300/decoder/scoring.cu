@@ -930,6 +930,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             if (far) a.out_ref = others.x;
             a.out = (far ? f.x * a.inv_s : a.inv_s) - t.rest / a.others.y;
         }
+        if (t.rest != t.rest) a.out = t.rest;
         a.scale = t.none ? 0.f : weight * P.inv_T;
         return a;
     };

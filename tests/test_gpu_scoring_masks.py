@@ -154,3 +154,14 @@ def test_rows_without_alternatives(dtype, rest):
                 loss, grad = scoring.distill_loss_and_grad(y, ids, t, rest=rest)
                 assert not loss.any() and not grad.any(), loss
                 assert not scoring.distill_loss(y, ids, t, rest=rest).any()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_an_id_past_the_vocabulary_makes_its_row_nan(dtype, rest):
+    x = torch.randn(4, 517, device="cuda").to(dtype)
+    x[2:] = -INF
+    ids = torch.tensor([[517], [5], [600], [5]], device="cuda")
+    loss, grad = scoring.distill_loss_and_grad(x, ids, torch.zeros(4, 1, device="cuda"), rest=rest)
+    assert loss.isnan().tolist() == [True, False, True, False]
+    assert grad.isnan().all(-1).tolist() == [True, False, True, False] and not grad[[1, 3]].isnan().any()
