@@ -1080,8 +1080,8 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             const float2 log_s = of(0), log_others = of(1), log_rest = of(2), log_norm = of(3);
             // (an infinity's rest would be NaN)
             auto plus = [](float2 a, float2 b) {
-                const float x = a.x + b.x;
-                return fabsf(x) < INFINITY ? pair_sum(a, b) : make_float2(x, 0.f);
+                const float2 x = pair_sum(a, b);
+                return fabsf(x.x) < INFINITY ? x : make_float2(a.x + b.x, 0.f);
             };
             float2 total = make_float2(0.f, 0.f);
             const float no_number = a.s - a.s;      // NaN in a row with NaN or +inf, else 0

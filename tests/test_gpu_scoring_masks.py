@@ -165,3 +165,20 @@ def test_an_id_past_the_vocabulary_makes_its_row_nan(dtype, rest):
     loss, grad = scoring.distill_loss_and_grad(x, ids, torch.zeros(4, 1, device="cuda"), rest=rest)
     assert loss.isnan().tolist() == [True, False, True, False]
     assert grad.isnan().all(-1).tolist() == [True, False, True, False] and not grad[[1, 3]].isnan().any()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("top", [5, 20, 64])
+def test_divergences_at_the_end_of_the_range(top, rest):
+    """All that the teacher says masked by the lowest value: as much as a logit
+    can be, or +inf."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(top)
+    low = torch.finfo(F32).min
+    x = torch.randn(400, 517, generator=g, device="cuda")
+    ids = torch.rand(400, 517, generator=g, device="cuda").topk(top, -1).indices
+    x.scatter_(1, ids, low)
+    teacher = torch.log_softmax(torch.randn(400, top, generator=g, device="cuda"), -1)
+    loss, grad = scoring.distill_loss_and_grad(x, ids, teacher, rest=rest)
+    assert bool((loss >= -low * (1 - 1e-6)).all()), loss
+    assert bool(grad.isfinite().all())
