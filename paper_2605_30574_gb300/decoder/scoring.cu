@@ -13,7 +13,7 @@
 // fp32: scores with 20 alternatives 54.9 us (5.7 TB/s), divergence from 32 69 (4.5),
 // with its gradient 114 (5.5).  bf16 has twice the elements to a byte, and their
 // exponentials and sums come to as much: scores of 2047 rows of 100003 with 64
-// alternatives 98 us (74 with none), divergence and gradient of 1999 144.
+// alternatives 98 us (74 with none), divergence and gradient of 1999 146.
 //
 // Gradients are contiguous; where that leaves a row on another 16-byte alignment
 // than its logits have, they go out element by element: 512 x 151936 at odd starts
