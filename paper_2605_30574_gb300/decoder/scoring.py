@@ -17,7 +17,6 @@ Sums are in fp32 in a fixed order: the same inputs give the same bits.
 """
 from __future__ import annotations
 
-import math
 from typing import NamedTuple, Optional, Tuple
 
 import torch
