@@ -1,0 +1,295 @@
+"""A key/value cache of pages, held in 4 bits: rows into it and out of it,
+attention over it, and its pages copied.
+
+A ``PageCache`` holds, for every layer, pages of ``page`` tokens with all their kv
+heads.  A row (one token's key or value of one head, of d elements) is kept as
+whole numbers c between -7 and 7, with a scale for each 32 elements:
+
+    A = max |x|,  E = floor(log2 A),  r = max(2^-14, (max of the 32 |x|) 2^(2 - E) / 7),
+    s = r 2^(E - 2),  c = x / s,
+
+r rounded to four significant bits and c to whole numbers (ties to even), so a value
+is off by half of s at most.  Rows with A below 2^-100 are held as zeros; those with A
+of 2^100 or more, an infinity or a NaN are NaN.  At 128 dims that is 69 bytes for the
+256 of bf16.  c s is exact in bf16.
+
+The calls take ``table`` [B][W], ``starts`` [B + 1] and ``lengths`` [B], int32 on the
+cache's device: sequence b has ``lengths[b]`` tokens in the pages ``table[b]`` (behind
+its last one the table may hold anything), and its newest tokens are the rows
+``starts[b]`` to ``starts[b + 1]`` of what is stored, loaded or attends; one token
+each is ``starts`` = 0 .. B.  The kernels read the three on the device, so a captured
+graph goes by what they hold when it is replayed.  Rows before ``starts[0]`` and behind
+``starts[B]`` are left as they are.  ``PageTables`` keeps them for sequences that share
+pages.
+
+Tensors are bf16, d 64, 128 or 256, pages of 16, 32, 64, 128 or 256 tokens; k, v and q
+may have any strides (those that the kernels cannot read are copied).  Kernels go to
+torch's current stream; tracers, which would not record them, are refused.  No
+gradients.  The same inputs give the same bits.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import List, Optional, Sequence, Tuple
+
+import torch
+
+from . import BF16, _current_device, _launch, lib, there, untraced
+
+_PAGES = {16: 4, 32: 5, 64: 6, 128: 7, 256: 8}
+_U8, _I32 = torch.uint8, torch.int32
+_LONGS2, _LONGS4 = ctypes.c_long * 2, ctypes.c_long * 4
+
+
+class PageCache:
+    """The cache's tensors, uint8 and contiguous, on one CUDA device:
+
+    * ``codes`` [layers][pages][2][heads][page][d / 2]: c + 8 in a nibble, the low one
+      first; keys, then values.  In a key the 8 elements 32 i + 8 t come at place
+      t d / 32 + i, in a value the 4 elements 32 i + 4 g at place g d / 32 + i;
+    * ``ratios`` [layers][pages][2][heads][page][d / 32]: bits 14 to 7 of r in fp16;
+    * ``exponents`` [layers][pages][heads][page][2]: E + 127 of key and value, 255 for
+      a row of NaN.
+    """
+
+    def __init__(self, codes: torch.Tensor, ratios: torch.Tensor, exponents: torch.Tensor):
+        what = "PageCache"
+        for name, t, dims in (("codes", codes, 6), ("ratios", ratios, 6), ("exponents", exponents, 5)):
+            if not isinstance(t, torch.Tensor) or t.dtype is not _U8:
+                raise TypeError(f"{what}: {name} must be a uint8 tensor")
+            if t.device.type != "cuda" or t.device != codes.device:
+                raise ValueError(f"{what}: the tensors must be on one CUDA device")
+            if t.dim() != dims or not t.is_contiguous() or there(what, name, t).data_ptr() & 15:
+                raise ValueError(f"{what}: {name} must be contiguous, at a 16-byte boundary, of {dims} dimensions")
+        layers, pages, two, heads, page, half = codes.shape
+        if half not in (32, 64, 128) or page not in _PAGES or two != 2:
+            raise ValueError(f"{what}: heads of 64, 128 or 256, and pages of {', '.join(map(str, _PAGES))} tokens")
+        if not 1 <= heads <= 1024 or not 1 <= layers <= 65535 or not 1 <= pages < 1 << 31:
+            raise ValueError(f"{what}: between 1 and 1024 heads, 1 and 65535 layers, and a page at least")
+        if ratios.shape != (layers, pages, 2, heads, page, half // 16) or exponents.shape != (layers, pages, heads, page, 2):
+            raise ValueError(f"{what}: ratios and exponents must be of the codes' sizes")
+        self.codes, self.ratios, self.exponents = codes, ratios, exponents
+        self.layers, self.pages, self.kv_heads, self.page, self.head_dim = layers, pages, heads, page, 2 * half
+        self.device = codes.device
+        self._sizes = (pages, heads, 2 * half, _PAGES[page])
+        self._strides = (codes.stride(0), ratios.stride(0), exponents.stride(0))
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> "PageCache":
+        """A cache whose pages hold anything."""
+        if head_dim not in (64, 128, 256) or page not in _PAGES:
+            raise ValueError(f"PageCache: heads of 64, 128 or 256, and pages of {', '.join(map(str, _PAGES))} tokens")
+        one = (layers, pages, 2, kv_heads, page)
+        return cls(*(torch.empty(s, dtype=_U8, device=device)
+                     for s in ((*one, head_dim // 2), (*one, head_dim // 32), (layers, pages, kv_heads, page, 2))))
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.numel() for t in (self.codes, self.ratios, self.exponents))
+
+    def _layer(self, what: str, layer: int) -> Tuple[int, int, int]:
+        if not isinstance(layer, int) or not 0 <= layer < self.layers:
+            raise ValueError(f"{what}: the cache has layers 0 to {self.layers - 1}")
+        ptrs = (self.codes.data_ptr(), self.ratios.data_ptr(), self.exponents.data_ptr())
+        if not all(ptrs):
+            raise ValueError(f"{what}: the cache has no memory")
+        return tuple(p + layer * s for p, s in zip(ptrs, self._strides))
+
+
+def _where(what, cache, table, starts, lengths):
+    """The three, as addresses, with the table's width and the sequences."""
+    if not isinstance(cache, PageCache):
+        raise TypeError(f"{what}: cache must be a PageCache")
+    for name, t, dims in (("table", table, 2), ("starts", starts, 1), ("lengths", lengths, 1)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not _I32:
+            raise TypeError(f"{what}: {name} must be an int32 tensor")
+        if t.device != cache.device:
+            raise ValueError(f"{what}: {name} must be on the cache's device")
+        if t.dim() != dims or not t.is_contiguous() or t.is_neg():
+            raise ValueError(f"{what}: {name} must be contiguous, of {dims} dimension{'s' * (dims > 1)}")
+        there(what, name, t)
+    B, W = table.shape
+    if starts.shape[0] != B + 1 or lengths.shape[0] != B:
+        raise ValueError(f"{what}: of B sequences, table must be [B][W], starts [B + 1] and lengths [B]")
+    if B and not W:
+        raise ValueError(f"{what}: the table has no pages")
+    return (table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), W, B)
+
+
+def _bf16(what, name, t, cache, shape):
+    if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
+        raise TypeError(f"{what}: {name} must be a bf16 tensor")
+    if t.device != cache.device:
+        raise ValueError(f"{what}: {name} must be on the cache's device")
+    if t.dim() != 3 or t.shape[-1] != cache.head_dim or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what}: {name} must be [tokens][heads][{cache.head_dim}]" + (f", here {tuple(shape)}" if shape else ""))
+    return there(what, name, t)
+
+
+def _reads(t):
+    """Whether the kernels can read the tensor where it is."""
+    token, head, one = t.stride()
+    return one == 1 and not (token | head | t.data_ptr() >> 1) & 7 and not t.is_neg() and max(token, head) < 1 << 38
+
+
+def _readable(t):
+    return t if _reads(t) else t.resolve_neg().clone(memory_format=torch.contiguous_format)
+
+
+def _written(*ts):
+    for t in ts:
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
+def _overlaps(t):
+    """Whether two of its rows may lie in the same place."""
+    sizes = sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1)
+    return any(s < (sizes[i - 1][0] * sizes[i - 1][1] if i else 1) for i, (s, _) in enumerate(sizes))
+
+
+def _target(what, name, t):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: {name} requires a gradient and is written to")
+    if t.is_inference() and not torch.is_inference_mode_enabled():
+        raise ValueError(f"{what}: {name} is an inference tensor and is written to")
+    if t.numel() and _overlaps(t):
+        raise ValueError(f"{what}: rows of {name} overlap")
+
+
+def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
+                lengths: torch.Tensor) -> None:
+    """Rounds the newest tokens' keys and values, k and v [tokens][heads][d], to 4 bits
+    into the layer's pages: those of sequence b take its last places below ``lengths[b]``.
+    A token without a place (before position 0, behind the table's pages, or in a page
+    that is none of the cache's) is left out.  Pages that are written to belong to one
+    sequence each."""
+    what = "store_pages"
+    untraced(what)
+    where = _where(what, cache, table, starts, lengths)
+    rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    _bf16(what, "k", k, cache, shape)
+    _bf16(what, "v", v, cache, shape)
+    at = cache._layer(what, layer)
+    if rows >= 1 << 31:
+        raise ValueError(f"{what}: fewer than 2^31 tokens")
+    if not rows or not where[-1]:
+        return
+    if cache.device.index != _current_device():
+        with torch.cuda.device(cache.device):
+            return store_pages(cache, layer, k, v, table, starts, lengths)
+    k, v = _readable(k), _readable(v)
+    _launch("decoder_page_rows", 0, *at, *cache._sizes, k.data_ptr(), v.data_ptr(), _LONGS4(*k.stride()[:2], *v.stride()[:2]),
+            *where, rows)
+
+
+def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
+               lengths: torch.Tensor) -> None:
+    """Writes the values that the newest tokens are held as to k and v [tokens][heads][d];
+    with ``starts`` that go by the lengths, those of whole sequences.  A token before
+    position 0 is zeros, one in a page that is none of the cache's, or behind the
+    table's, NaN."""
+    what = "load_pages"
+    untraced(what)
+    where = _where(what, cache, table, starts, lengths)
+    rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    for name, t in (("k", k), ("v", v)):
+        _bf16(what, name, t, cache, shape)
+        _target(what, name, t)
+    at = cache._layer(what, layer)
+    if rows >= 1 << 31:
+        raise ValueError(f"{what}: fewer than 2^31 tokens")
+    if not rows or not where[-1]:
+        return
+    if cache.device.index != _current_device():
+        with torch.cuda.device(cache.device):
+            return load_pages(cache, layer, k, v, table, starts, lengths)
+    # (what the kernels cannot write to gets its rows by way of a copy)
+    to, tv = _readable(k), _readable(v)
+    _launch("decoder_page_rows", 1, *at, *cache._sizes, to.data_ptr(), tv.data_ptr(), _LONGS4(*to.stride()[:2], *tv.stride()[:2]),
+            *where, rows)
+    for a, b in ((k, to), (v, tv)):
+        if a is b:
+            _written(a)
+        else:
+            with torch.no_grad():
+                a.copy_(b)
+
+
+def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
+                   lengths: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the newest tokens' queries, q [tokens][Hq][d], over their sequences'
+    keys and values, the newest tokens' own included (which are stored before): token i
+    of the n newest of a sequence is at position p = length - n + i and sees those up to
+    p, with ``window`` above 0 only those above p - window.  Query head h reads kv head
+    h // (Hq / heads).  One token that sees nothing gives 0; a page among a sequence's that
+    is none of the cache's, or is missing from the table, makes its rows NaN.  ``scale`` is
+    1 / sqrt(d) by default.
+
+    Returns [tokens][Hq][d], bf16: ``out`` (contiguous) if given, else a new tensor whose
+    rows outside of all sequences hold anything.  Scores and sums are in fp32, q to the
+    bits of fp16 below 2^15 times its row's largest, weights in fp16."""
+    what = "page_attention"
+    untraced(what)
+    where = _where(what, cache, table, starts, lengths)
+    _bf16(what, "q", q, cache, None)
+    rows, hq, d = q.shape
+    if hq == 0 or hq % cache.kv_heads:
+        raise ValueError(f"{what}: the query heads must be a multiple of the cache's {cache.kv_heads}")
+    if not isinstance(window, int) or not 0 <= window < 1 << 31:
+        raise ValueError(f"{what}: window must be a whole number, 0 (none) to 2^31 - 1")
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    at = cache._layer(what, layer)
+    if out is not None:
+        _bf16(what, "out", out, cache, q.shape)
+        _target(what, "out", out)
+        if not out.is_contiguous() or out.is_neg() or out.data_ptr() & 15:
+            raise ValueError(f"{what}: out must be contiguous, at a 16-byte boundary")
+    if cache.device.index != _current_device():
+        with torch.cuda.device(cache.device):
+            return page_attention(cache, layer, q, table, starts, lengths, scale=scale, window=window, out=out)
+    y = torch.empty(q.shape, dtype=BF16, device=q.device) if out is None else out
+    if not rows or not where[-1]:
+        return y
+    size = lib().decoder_page_attention_scratch(where[-1], rows, hq, cache.kv_heads, d)
+    if size <= 0:
+        raise RuntimeError(f"{what}: CUDA error {-size}") if size else ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
+    q = _readable(q)
+    scratch = torch.empty(size, dtype=_U8, device=q.device)
+    _launch("decoder_page_attention", *at, *cache._sizes, q.data_ptr(), _LONGS2(*q.stride()[:2]), *where, rows, hq, scale, window,
+            y.data_ptr(), scratch.data_ptr())
+    if out is not None:
+        _written(out)
+    return y
+
+
+def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None:
+    """Copies pages ``src[i]`` to ``dst[i]`` in all layers.  No page may be written twice,
+    or written and read."""
+    what = "copy_pages"
+    untraced(what)
+    if not isinstance(cache, PageCache):
+        raise TypeError(f"{what}: cache must be a PageCache")
+    n = len(src)
+    if len(dst) != n:
+        raise ValueError(f"{what}: as many pages to copy to as from")
+    if n == 0:
+        return
+    try:
+        ints = (ctypes.c_int * n)(*src), (ctypes.c_int * n)(*dst)
+    except TypeError:
+        raise TypeError(f"{what}: pages must be whole numbers") from None
+    if min(src) < 0 or min(dst) < 0 or max(src) >= cache.pages or max(dst) >= cache.pages:
+        raise ValueError(f"{what}: the cache has pages 0 to {cache.pages - 1}")
+    to = set(dst)
+    if len(to) != n or not to.isdisjoint(src):
+        raise ValueError(f"{what}: a page is written twice, or written and read")
+    at = cache._layer(what, 0)
+    if cache.device.index != _current_device():
+        with torch.cuda.device(cache.device):
+            return copy_pages(cache, src, dst)
+    _launch("decoder_page_copy", *at, cache.layers, *cache._sizes, *ints, n)
