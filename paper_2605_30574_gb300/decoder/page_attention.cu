@@ -29,18 +29,22 @@
 // them in the warps' order: the same inputs give the same bits.
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "../csrc/per_device.h"
+#include "../csrc/tc_ptx.cuh"
 #include "decoder.h"
 #include "pages.cuh"
 
 namespace decoder {
 namespace {
 
+using splice::tc::smem_u32;
+
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
-constexpr float kTau = 8.f;             // how far weights may pass the reference, in bits
 constexpr int kMinShare = 4;            // blocks of 16 keys to a warp, at least
 
 struct Args {
@@ -56,7 +60,7 @@ struct Args {
 };
 
 template <int D>
-constexpr int ctas_per_sm(int nt) { return D == 256 || nt == 2 ? 1 : 2; }
+constexpr int ctas_per_sm(int nt) { return D == 256 || nt == 2 ? 2 : 4; }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -65,9 +69,15 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma0(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
@@ -89,32 +99,27 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     return reinterpret_cast<const uint32_t&>(h);
 }
 
-__device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
-    const __half2 h = __hadd2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
-    return reinterpret_cast<const uint32_t&>(h);
-}
-
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     const __half2 h = __hmul2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
     return reinterpret_cast<const uint32_t&>(h);
 }
 
-// `N` consecutive bytes at their own alignment as words (a half word: zero-extended).
+// `N` bytes of shared memory at their own alignment, as words.
 template <int N>
-__device__ __forceinline__ void load_bytes(uint32_t* to, const uint8_t* p) {
-    if constexpr (N == 2) to[0] = *reinterpret_cast<const uint16_t*>(p);
-    if constexpr (N == 4) to[0] = *reinterpret_cast<const uint32_t*>(p);
-    if constexpr (N == 8) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
-        to[0] = x.x, to[1] = x.y;
+__device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
+    if constexpr (N == 2) {
+        uint16_t y;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(from));
+        x[0] = y;
     }
-    if constexpr (N >= 16) {
+    if constexpr (N == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(from));
+    if constexpr (N == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from));
+    if constexpr (N >= 16)
 #pragma unroll
-        for (int i = 0; i < N / 16; ++i) {
-            const uint4 x = reinterpret_cast<const uint4*>(p)[i];
-            to[4 * i] = x.x, to[4 * i + 1] = x.y, to[4 * i + 2] = x.z, to[4 * i + 3] = x.w;
-        }
-    }
+        for (int i = 0; i < N / 16; ++i)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[4 * i]), "=r"(x[4 * i + 1]), "=r"(x[4 * i + 2]), "=r"(x[4 * i + 3])
+                         : "r"(from + 16 * i));
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
@@ -131,7 +136,7 @@ __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     q.new_ = end - first;
     q.length = max(0, A.s.lengths[b]);
     q.tiles = int((long(q.new_) * A.G + R - 1) / R);
-    int blocks = (q.length + 15) / 16;
+    int blocks = q.length / 16 + (q.length % 16 != 0);
     if (A.window) blocks = min(blocks, int((long(A.window) + (R + A.G - 2) / A.G + 30) / 16));
     q.blocks = max(1, blocks);
     return q;
@@ -142,40 +147,24 @@ __device__ __forceinline__ long size_of(const Args& A, const Seq& q) {
     return long(q.tiles) * A.c.hkv * q.blocks;
 }
 
-// What a lane holds of a block of 16 keys: keys g and g + 8 (its words t + 4 i), and for
-// the values 2t, 2t + 1, 2t + 8, 2t + 9 (its runs g + 8 i), with ratios and exponents.
+// A stage of a warp's ring: 16 keys of one head as they lie in their page.
 template <int D>
-struct Block {
-    static constexpr int kI = D / 32;
-    uint32_t k[2][kI], v[4][(kI + 1) / 2];
-    uint32_t kr[2][(kI + 3) / 4], vr[4][(kI + 3) / 4], e[2];
+struct Ring {
+    static constexpr int kI = D / 32, kStages = D == 256 ? 4 : 6;
+    static constexpr int kV = 8 * D, kKr = 16 * D, kVr = kKr + 16 * kI, kE = kKr + 32 * kI;      // where each part is
+    static constexpr int kBytes = kE + 32;
+    static constexpr int kSmem = kWarps * kStages * kBytes;
 };
 
-template <int D>
-__device__ __forceinline__ void fetch(const Args& A, Block<D>& x, int page, int head, int slot) {
-    constexpr int kI = D / 32;
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const size_t kr = page_row(A.c, page, 0, head, slot), vr = page_row(A.c, page, 1, head, slot),
-                 er = exponent_row(A.c, page, head, slot);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const size_t row = kr + g + 8 * h;
-        load_bytes<4 * kI>(x.k[h], A.c.codes + row * (D / 2) + t * 4 * kI);
-        load_bytes<kI>(x.kr[h], A.c.ratios + row * kI);
-        x.e[h] = *reinterpret_cast<const uint16_t*>(A.c.exponents + (er + g + 8 * h) * 2);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const size_t row = vr + 2 * t + (j & 1) + 8 * (j >> 1);
-        load_bytes<2 * kI>(x.v[j], A.c.codes + row * (D / 2) + g * 2 * kI);
-        load_bytes<kI>(x.vr[j], A.c.ratios + row * kI);
-    }
+__device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-// A row's state as it leaves the kernel: O for the reference m and the sum l.
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel(const Args A, int workers) {
     constexpr int kI = D / 32, R = 8 * NT;
+    using Rg = Ring<D>;
+    extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kWarps];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
@@ -209,6 +198,20 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
     long at = before[lo];
     int b = lo * run;
     Seq sq = sequence<R>(A, b);
+
+    // the warp's ring, and what a lane copies of a stage: 16 bytes of every 512 of the
+    // codes, and of the rest its share
+    const uint32_t ring = smem_u32(smem) + warp_in * Rg::kStages * Rg::kBytes, ring_end = ring + Rg::kStages * Rg::kBytes;
+    const int kind = lane < kI ? 0 : lane < 2 * kI ? 1 : 2;         // (ratios of keys, of values; exponents)
+    const bool rest = lane < 2 * kI + 2;
+    const int rest_row = kind < 2 ? kI : 2;
+    const uint32_t rest_to = Rg::kKr + 16 * lane;
+    const uint32_t page_rows = 1u << A.c.log_page, both = page_rows * A.c.hkv;      // (of keys or values, of a page)
+    const uint8_t* rest_from = (kind < 2 ? A.c.ratios + (kind ? size_t(both) * kI : 0) : A.c.exponents) +
+                               16 * (lane - (kind == 0 ? 0 : kind == 1 ? kI : 2 * kI));
+    const uint32_t rest_page = both * (kind < 2 ? 2 * kI : 2);
+    const int log_blocks = A.c.log_page - 4, in_page = (1 << log_blocks) - 1;
+
     while (x < end) {
         while (at + size_of<R>(A, sq) <= x) {
             at += size_of<R>(A, sq);
@@ -222,12 +225,59 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
         const long item_at = x - j0;
         x += j1 - j0;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
+        const int base = sq.length - sq.new_;
+        const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
+        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / 16 : 0;
+        const int kb_end = min(kb0 + j1, (last_pos + 16) / 16);
+        int kb = kb0 + j0, kb_in = kb;
+
+        // ---- stages on their way: the pages of 32 places at a time in the lanes ----
+        const int* table = A.s.table + size_t(b) * A.s.width;
+        int ids_at = kb >> log_blocks;
+        auto pages_from = [&](int i) { return i + lane < A.s.width ? __ldg(table + i + lane) : -1; };
+        int ids = pages_from(ids_at), more = pages_from(ids_at + 32);
+        const uint8_t* codes = A.c.codes + size_t(page_rows) * head * (D / 2) + 16 * lane;
+        const uint8_t* others = rest_from + size_t(page_rows) * head * rest_row;
+        const uint8_t *k_in, *rest_in;
+        bool broken = false;                     // a page that is none of the cache's
+        auto locate = [&]() {
+            const int i = kb_in >> log_blocks;
+            if (i - ids_at >= 32) {
+                ids = more;
+                ids_at += 32;
+                more = pages_from(ids_at + 32);
+            }
+            int page = __shfl_sync(kFull, ids, i - ids_at);
+            if (page < 0 || page >= A.c.pages) broken = true, page = 0;
+            const uint32_t slot = 16 * (kb_in & in_page);
+            k_in = codes + uint64_t(uint32_t(page)) * (both * D) + slot * (D / 2);
+            rest_in = others + uint64_t(uint32_t(page)) * rest_page + slot * rest_row;
+        };
+        uint32_t in_at = ring, out_at = ring;
+        auto fill = [&]() {
+            if (kb_in < kb_end) {
+                const uint8_t* v_in = k_in + both * (D / 2);
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) cp16(in_at + 16 * lane + 512 * j, k_in + 512 * j);
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) cp16(in_at + 16 * lane + Rg::kV + 512 * j, v_in + 512 * j);
+                if (rest) cp16(in_at + rest_to, rest_in);
+                in_at += Rg::kBytes;
+                if (in_at == ring_end) in_at = ring;
+                k_in += 8 * D;
+                rest_in += 16 * rest_row;
+                if ((++kb_in & in_page) == 0 && kb_in < kb_end) locate();
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        if (kb < kb_end) locate();
+#pragma unroll 1
+        for (int i = 0; i < Rg::kStages - 1; ++i) fill();
 
         // ---- the rows: q as an operand, and what is known of each column ----
-        uint32_t qf[NT][kI][4];
-        float start[NT][kI][2], factor[NT][2], l[NT][2], ref[NT][2];
+        uint32_t qf[NT][kI][4], minus[NT][kI > 4 ? 4 : 2];
+        float factor[NT][2], l[NT][2], ref[NT][2];
         int pos[NT][2];
-        const int base = sq.length - sq.new_;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int col = 8 * n + g, r = tile * R + col, token = r / A.G;
@@ -248,31 +298,42 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
             // (a row with infinities or NaN: NaN)
             const float up = E == 255 ? __int_as_float(0x7fffffff) : power_of(268 - E);
             const float down = power_of(E < 255 ? E - 14 : 1);
-            float qs[kI];
+            uint32_t hi[kI], mid[kI], low[kI];       // -8 sum q of a group, as three fp16
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
                 // elements 8t + j of group i, j = 0 .. 7; pairs (j, j + 4) to an operand
-                float f[8];
+                float f[8], sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     f[j] = __uint_as_float(j & 1 ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
-                qs[i] = 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     qf[n][i][j] = half2_of(f[j], f[j + 4]);
                     const float2 y = __half22float2(reinterpret_cast<const __half2&>(qf[n][i][j]));
-                    qs[i] = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, qs[i]);
+                    sum = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, sum);
                 }
-                qs[i] += __shfl_xor_sync(kFull, qs[i], 1);
-                qs[i] += __shfl_xor_sync(kFull, qs[i], 2);
+                sum += __shfl_xor_sync(kFull, sum, 1);
+                sum += __shfl_xor_sync(kFull, sum, 2);
+                const __half a = __float2half_rn(sum), c = __float2half_rn(sum - __half2float(a)),
+                             e = __float2half_rn(sum - __half2float(a) - __half2float(c));
+                hi[i] = __half_as_ushort(a), mid[i] = __half_as_ushort(c), low[i] = __half_as_ushort(e);
+            }
+            // as an operand against the keys' ratios (see below)
+            auto two = [](const uint32_t* y, int i) { return y[i] | y[i + 1] << 16; };
+            if constexpr (kI == 2) {
+                minus[n][0] = t == 0 ? two(hi, 0) : t == 1 ? two(mid, 0) : t == 2 ? two(low, 0) : 0u;
+                minus[n][1] = 0u;
+            } else if constexpr (kI == 4) {
+                minus[n][0] = t == 0 ? two(hi, 0) : t == 1 ? two(hi, 2) : t == 2 ? two(mid, 0) : two(mid, 2);
+                minus[n][1] = t == 0 ? two(low, 0) : t == 1 ? two(low, 2) : 0u;
+            } else {
+                auto by_t = [&](const uint32_t* y) { return t == 0 ? two(y, 0) : t == 1 ? two(y, 2) : t == 2 ? two(y, 4) : two(y, 6); };
+                minus[n][0] = by_t(hi), minus[n][1] = by_t(mid), minus[n][2] = by_t(low), minus[n][3] = 0u;
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int from = 4 * (2 * t + c);
-#pragma unroll
-                for (int i = 0; i < kI; ++i) start[n][i][c] = __shfl_sync(kFull, qs[i], from);
                 // S 2^(E_k - 2) 2^24 / up, in bits
-                factor[n][c] = __shfl_sync(kFull, down, from) * (0x1p22f * kLog2e) * A.scale;
+                factor[n][c] = __shfl_sync(kFull, down, 4 * (2 * t + c)) * (0x1p22f * kLog2e) * A.scale;
                 const int column = 8 * n + 2 * t + c;
                 pos[n][c] = column < rows ? base + (tile * R + column) / A.G : -1;
                 l[n][c] = 0.f;
@@ -280,97 +341,112 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
             }
         }
         float acc[NT][kI][2][4] = {};
+        // values 2t and 2t + 1 are read in turn and back, by t: half the bank conflicts
+        const uint32_t even = t & 1 ? 0x1054u : 0x5410u, odd = t & 1 ? 0x3276u : 0x7632u;
 
         // ---- the keys ----
-        const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
-        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / 16 : 0;
-        const int kb_end = min(kb0 + j1, (last_pos + 16) / 16);
-        const int log_blocks = A.c.log_page - 4, in_page = (1 << log_blocks) - 1;
-        const int* table = A.s.table + size_t(b) * A.s.width;
-        bool broken = false;                     // a page that is none of the cache's
-        auto page_of = [&](int kb) {
-            const int i = kb >> log_blocks;
-            return kb < kb_end ? i < A.s.width ? __ldg(table + i) : -1 : 0;
-        };
-        auto checked = [&](int page) {
-            if (page >= 0 && page < A.c.pages) return page;
-            broken = true;
-            return 0;
-        };
-        int kb = kb0 + j0;
-        int next_page = page_of(kb + 1);
-        Block<D> now;
-        if (kb < kb_end) fetch<D>(A, now, checked(page_of(kb)), head, (kb & in_page) * 16);
-        for (; kb < kb_end; ++kb) {
-            Block<D> next;
-            if (kb + 1 < kb_end) {
-                fetch<D>(A, next, checked(next_page), head, (kb + 1 & in_page) * 16);
-                next_page = page_of(kb + 2);
+        const uint32_t k_of = 4 * kI * lane, v_of = Rg::kV + g * 2 * kI, v0_of = v_of + (2 * t + (t & 1)) * (D / 2),
+                       v1_of = v_of + (2 * t + 1 - (t & 1)) * (D / 2), e_of = Rg::kE + 2 * g;
+        auto block = [&](auto at_edge) {
+            constexpr bool kEdge = decltype(at_edge)::value;
+            // (the stage is there when all but the newest kStages - 2 are; all lanes have
+            // read the one before, which is filled anew)
+            asm volatile("cp.async.wait_group %0;" ::"n"(Rg::kStages - 2) : "memory");
+            __syncwarp();
+            fill();
+            const int key0 = 16 * kb;
+            uint32_t kc[2][kI], kr[2][(kI + 3) / 4], ex[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                lds<4 * kI>(kc[h], out_at + k_of + h * 8 * (D / 2));
+                lds<kI>(kr[h], out_at + Rg::kKr + g * kI + 8 * h * kI);
+                lds<2>(&ex[h], out_at + e_of + 16 * h);
             }
-            const bool edge = 16 * kb + 15 > first_pos || (A.window && 16 * kb <= last_pos - A.window) || rows < 1;
-
-            // scores
-            float s[NT][4] = {};
+            // scores: first what the codes' 8 adds to all groups, by the ratios of two of
+            // them as fp16 (bytes of a word, with their signs, 0, between them)
+            uint32_t ratio[2][kI / 2];
+            float s[NT][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < kI; i += 2) ratio[h][i / 2] = bytes_of(kr[h][i / 4], 0, i % 4 ? 0xb3a2u : 0x9180u) << 7;
+            {
+                auto mine = [&](int h) {
+                    if constexpr (kI == 2) return ratio[h][0];
+                    if constexpr (kI == 4) return t & 1 ? ratio[h][1] : ratio[h][0];
+                    if constexpr (kI == 8) return t & 2 ? (t & 1 ? ratio[h][3] : ratio[h][2]) : t & 1 ? ratio[h][1] : ratio[h][0];
+                };
+                const uint32_t ra = mine(0), rc = mine(1);
+                const uint32_t r4[4] = {ra, rc, ra, rc};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma0(s[n], r4, minus[n][0], minus[n][1]);
+                    if constexpr (kI > 4) mma(s[n], r4, minus[n][2], minus[n][3]);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
-                float part[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    part[n][0] = part[n][2] = start[n][i][0], part[n][1] = part[n][3] = start[n][i][1];
-                const uint32_t a = now.k[0][i], c = now.k[1][i];
-                const uint32_t lo[4] = {a & 0x000f000fu, c & 0x000f000fu, a & 0x00f000f0u, c & 0x00f000f0u};
+                const uint32_t a = kc[0][i], c = kc[1][i];
+                const uint32_t lo4[4] = {a & 0x000f000fu, c & 0x000f000fu, a & 0x00f000f0u, c & 0x00f000f0u};
                 const uint32_t a8 = a >> 8, c8 = c >> 8;
-                const uint32_t hi[4] = {a8 & 0x000f000fu, c8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x00f000f0u};
+                const uint32_t hi4[4] = {a8 & 0x000f000fu, c8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x00f000f0u};
+                const __half2 ra = reinterpret_cast<const __half2&>(ratio[0][i / 2]), rc = reinterpret_cast<const __half2&>(ratio[1][i / 2]);
+                const float fa = i & 1 ? __high2float(ra) : __low2float(ra), fc = i & 1 ? __high2float(rc) : __low2float(rc);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    mma(part[n], lo, qf[n][i][0], qf[n][i][1]);
-                    mma(part[n], hi, qf[n][i][2], qf[n][i][3]);
-                }
-                const uint32_t ra = now.kr[0][i / 4], rc = now.kr[1][i / 4];
-                const int sh = 8 * (i & 3);
-                const float fa = __uint_as_float((((sh <= 20 ? ra << (20 - sh) : ra >> (sh - 20)) & 0x07f00000u) | 0x38000000u));
-                const float fc = __uint_as_float((((sh <= 20 ? rc << (20 - sh) : rc >> (sh - 20)) & 0x07f00000u) | 0x38000000u));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    s[n][0] = fmaf(part[n][0], fa, s[n][0]);
-                    s[n][1] = fmaf(part[n][1], fa, s[n][1]);
-                    s[n][2] = fmaf(part[n][2], fc, s[n][2]);
-                    s[n][3] = fmaf(part[n][3], fc, s[n][3]);
+                    float part[4];
+                    mma0(part, lo4, qf[n][i][0], qf[n][i][1]);
+                    mma(part, hi4, qf[n][i][2], qf[n][i][3]);
+                    s[n][0] = fmaf(part[0], fa, s[n][0]);
+                    s[n][1] = fmaf(part[1], fa, s[n][1]);
+                    s[n][2] = fmaf(part[2], fc, s[n][2]);
+                    s[n][3] = fmaf(part[3], fc, s[n][3]);
                 }
             }
             // weights, of keys g and g + 8
-            float ek[2], ev[2], up[2];
+            float ek[2], up[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int e = now.e[h] >> 8;
-                ek[h] = power_of(now.e[h] & 255);
-                up[h] = power_of(e);
+                ek[h] = power_of(ex[h] & 255);
+                up[h] = power_of(ex[h] >> 8);
                 // (infinite, of a key or value of NaN: the score is NaN)
                 ek[h] = fmaf(up[h], 0.f, fmaf(ek[h], 0.f, ek[h]));
                 up[h] *= 0x1p6f;
-                ev[h] = float(e - 127);
             }
             uint32_t w[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+                float x[4], p[4], pv[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[n][j] *= factor[n][j & 1] * ek[j >> 1];
-                if (edge) {
+                for (int j = 0; j < 4; ++j) x[j] = fmaf(s[n][j], factor[n][j & 1] * ek[j >> 1], -ref[n][j & 1]);
+                if (kEdge) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int key = 16 * kb + g + 8 * (j >> 1), p = pos[n][j & 1];
-                        if (key > p || (A.window && key <= p - A.window)) s[n][j] = -INFINITY;
+                        const int key = key0 + g + 8 * (j >> 1), last = pos[n][j & 1];
+                        if (key > last || (A.window && key <= last - A.window)) x[j] = -INFINITY;
                     }
                 }
-                float top[2];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) top[c] = fmaxf(s[n][c] + ev[0], s[n][2 + c] + ev[1]);
-                if (__any_sync(kFull, top[0] > ref[n][0] + kTau || top[1] > ref[n][1] + kTau)) {
+                for (int j = 0; j < 4; ++j) {
+                    p[j] = ex2(x[j]);
+                    pv[j] = p[j] * up[j >> 1];
+                }
+                if (kEdge) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (x[j] == -INFINITY) pv[j] = 0.f;          // (whatever the value is)
+                }
+                // what is past the reference is found by the weights: infinite, or too large
+                if (__any_sync(kFull, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])) > 0x1p14f)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[n][j] = kEdge && x[j] == -INFINITY ? -INFINITY : s[n][j] * (factor[n][j & 1] * ek[j >> 1]);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
+                        float top = fmaxf(s[n][c] + float(int(ex[0] >> 8) - 127), s[n][2 + c] + float(int(ex[1] >> 8) - 127));
 #pragma unroll
-                        for (int o = 4; o < 32; o *= 2) top[c] = fmaxf(top[c], __shfl_xor_sync(kFull, top[c], o));
-                        const float m = fmaxf(ref[n][c], top[c]), f = ex2(ref[n][c] - m);
+                        for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+                        const float m = fmaxf(ref[n][c], top), f = ex2(ref[n][c] - m);
                         ref[n][c] = m;
                         l[n][c] *= f;
 #pragma unroll
@@ -378,52 +454,73 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
 #pragma unroll
                             for (int h = 0; h < 2; ++h) acc[n][i][h][c] *= f, acc[n][i][h][2 + c] *= f;
                     }
-                }
-                float p[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p[j] = ex2(s[n][j] - ref[n][j & 1]);
+                    for (int j = 0; j < 4; ++j) {
+                        p[j] = ex2(s[n][j] - ref[n][j & 1]);
+                        pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
+                    }
+                }
                 l[n][0] += p[0] + p[2];
                 l[n][1] += p[1] + p[3];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[j] = edge && s[n][j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
-                w[n][0] = transposed(half2_of(p[0], p[1]));
-                w[n][1] = transposed(half2_of(p[2], p[3]));
-            }
-            // what no row sees may hold anything: its ratios are left out
-            if (edge) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = 16 * kb + 2 * t + (j & 1) + 8 * (j >> 1);
-                    if (key > last_pos || (A.window && key <= first_pos - A.window))
-#pragma unroll
-                        for (int i = 0; i < (kI + 3) / 4; ++i) now.vr[j][i] = 0;
-                }
+                w[n][0] = transposed(half2_of(pv[0], pv[1]));
+                w[n][1] = transposed(half2_of(pv[2], pv[3]));
             }
             // output
+            uint32_t v[4][(kI + 1) / 2], vr[2][(2 * kI + 3) / 4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                lds<2 * kI>(v[2 * h], out_at + v0_of + h * 8 * (D / 2));
+                lds<2 * kI>(v[2 * h + 1], out_at + v1_of + h * 8 * (D / 2));
+                lds<2 * kI>(vr[h], out_at + Rg::kVr + 2 * t * kI + 8 * h * kI);
+            }
+            if (kEdge) {
+                // what no row sees may hold anything: its ratios are left out
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = key0 + 2 * t + (j & 1) + 8 * (j >> 1);
+                    if (key > last_pos || (A.window && key <= first_pos - A.window)) {
+                        if constexpr (kI == 2) vr[j >> 1][0] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+                        if constexpr (kI > 2)
+#pragma unroll
+                            for (int i = 0; i < kI / 4; ++i) vr[j >> 1][(j & 1) * (kI / 4) + i] = 0;
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
-                // bytes i of two keys' ratios, as fp16 (the third and fourth: a sign, 0)
-                const int sel = (i & 3) | 8 << 4 | (4 + (i & 3)) << 8 | 12 << 12;
-                const uint32_t r0 = bytes_of(now.vr[0][i / 4], now.vr[1][i / 4], sel) << 7;
-                const uint32_t r1 = bytes_of(now.vr[2][i / 4], now.vr[3][i / 4], sel) << 7;
-                const int pick = i & 1 ? 0x7632 : 0x5410;
-                const uint32_t a = bytes_of(now.v[0][i / 2], now.v[1][i / 2], pick);
-                const uint32_t c = bytes_of(now.v[2][i / 2], now.v[3][i / 2], pick);
-                constexpr uint32_t k8 = 0x80088008u, k128 = 0x80808080u;        // -8 2^-24, -128 2^-24
-                const uint32_t lo[4] = {add2(a & 0x000f000fu, k8), add2(a & 0x00f000f0u, k128),
-                                        add2(c & 0x000f000fu, k8), add2(c & 0x00f000f0u, k128)};
+                // bytes i of two keys' ratios, as fp16
+                constexpr int kNext = kI == 2 ? 2 : 4;               // (the second key's byte 0)
+                const uint32_t sel = (i & 3) | 8 << 4 | (kNext + (i & 3)) << 8 | 8 << 12;
+                const uint32_t r0 = bytes_of(vr[0][i / 4], vr[0][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
+                const uint32_t r1 = bytes_of(vr[1][i / 4], vr[1][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
+                const uint32_t a = bytes_of(v[0][i / 2], v[1][i / 2], i & 1 ? odd : even);
+                const uint32_t c = bytes_of(v[2][i / 2], v[3][i / 2], i & 1 ? odd : even);
+                const uint32_t lo4[4] = {a & 0x000f000fu, a & 0x00f000f0u, c & 0x000f000fu, c & 0x00f000f0u};
                 const uint32_t a8 = a >> 8, c8 = c >> 8;
-                const uint32_t hi[4] = {add2(a8 & 0x000f000fu, k8), add2(a8 & 0x00f000f0u, k128),
-                                        add2(c8 & 0x000f000fu, k8), add2(c8 & 0x00f000f0u, k128)};
+                const uint32_t hi4[4] = {a8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x000f000fu, c8 & 0x00f000f0u};
+                const uint32_t eights[4] = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};     // -8 2^-24, -128 2^-24
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const uint32_t b0 = mul2(w[n][0], r0), b1 = mul2(w[n][1], r1);
-                    mma(acc[n][i][0], lo, b0, b1);
-                    mma(acc[n][i][1], hi, b0, b1);
+                    mma(acc[n][i][0], lo4, b0, b1);
+                    mma(acc[n][i][1], hi4, b0, b1);
+                    mma(acc[n][i][0], eights, b0, b1);
+                    mma(acc[n][i][1], eights, b0, b1);
                 }
             }
-            now = next;
+            out_at += Rg::kBytes;
+            if (out_at == ring_end) out_at = ring;
+        };
+        // (blocks all of whose keys all rows see, and the others)
+        const int inner = A.window && last_pos >= A.window ? (last_pos - A.window) / 16 + 1 : 0, inner_end = (first_pos + 1) / 16;
+        for (; kb < kb_end; ++kb) {
+            if (kb >= inner && kb < inner_end)
+                block(std::false_type());
+            else
+                block(std::true_type());
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
 
         // ---- the rows' states: out, or left for the join ----
         const bool whole = j0 == 0 && j1 == sq.blocks;
@@ -493,7 +590,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Args A, int worker
         __syncthreads();
         const int head = x.z & 0x3fffffff, r = tile * R + col, token = r / A.G;
         __nv_bfloat16* to = A.out + (size_t(x.x + token) * A.c.hkv * A.G + head * A.G + r - token * A.G) * D;
-        if (threadIdx.x < D) {
+        for (int e = threadIdx.x; e < D; e += kThreads) {
             float M = kNone, sum = 0.f, y = 0.f;
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) M = fmaxf(M, part[k][D]);
@@ -501,9 +598,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Args A, int worker
             for (int k = 0; k < kWarps; ++k) {
                 const float f = ex2(part[k][D] - M);
                 sum += part[k][D + 1] * f;
-                y += part[k][threadIdx.x] * f;
+                y += part[k][e] * f;
             }
-            to[threadIdx.x] = __float2bfloat16_rn(sum == 0.f ? 0.f : y / sum);
+            to[e] = __float2bfloat16_rn(sum == 0.f ? 0.f : y / sum);
         }
     }
 }
@@ -512,7 +609,10 @@ template <int D, int NT>
 int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     static splice::PerDevice<int> counts;
     int sms = 0;
-    const cudaError_t e = counts.get(&sms, [](int dev, int* n) { return cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev); });
+    const cudaError_t e = counts.get(&sms, [](int dev, int* n) {
+        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D>::kSmem);
+        return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
+    });
     if (e != cudaSuccess) return int(e);
     const int grid = sms * ctas_per_sm<D>(NT), workers = grid * kWarps;
     const long states = long(workers) * 2 * 8 * NT * (D + 4) * 4;
@@ -523,7 +623,8 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     Args A = a;
     A.states = static_cast<float*>(scratch);
     A.begun = reinterpret_cast<int4*>(static_cast<char*>(scratch) + states);
-    attention_kernel<D, NT><<<grid, kThreads, 0, stream>>>(A, workers);
+    constexpr int kSmem = Ring<D>::kSmem;
+    attention_kernel<D, NT><<<grid, kThreads, kSmem, stream>>>(A, workers);
     join_kernel<D, NT><<<dim3(unsigned(sms), 8 * NT), kThreads, 0, stream>>>(A, workers);
     return int(cudaGetLastError());
 }
