@@ -42,10 +42,9 @@ namespace {
 using splice::tc::smem_u32;
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
-constexpr int kMinShare = 4;            // blocks of 16 keys to a warp, at least
+constexpr int kMinShare = 2;            // blocks of 32 keys to a warp, at least
 
 struct Args {
     PageLayer c;
@@ -59,8 +58,10 @@ struct Args {
     int4* begun;            // per worker: the tile whose keys begin with it and go on
 };
 
-template <int D>
-constexpr int ctas_per_sm(int nt) { return D == 256 || nt == 2 ? 2 : 4; }
+// Warps to an SM, all of one CTA: as many as their registers allow.
+template <int D, int NT>
+constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
+constexpr int kJoin = 128;              // threads of a CTA that joins states
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -123,7 +124,7 @@ __device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
-// blocks of 16 keys as the one that sees most.
+// blocks of 32 keys as the one that sees most.
 struct Seq {
     int first, new_, length, tiles, blocks;     // (its first row of q; its tokens, its keys)
 };
@@ -136,8 +137,8 @@ __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     q.new_ = end - first;
     q.length = max(0, A.s.lengths[b]);
     q.tiles = int((long(q.new_) * A.G + R - 1) / R);
-    int blocks = q.length / 16 + (q.length % 16 != 0);
-    if (A.window) blocks = min(blocks, int((long(A.window) + (R + A.G - 2) / A.G + 30) / 16));
+    int blocks = q.length / 32 + (q.length % 32 != 0);
+    if (A.window) blocks = min(blocks, int((long(A.window) + (R + A.G - 2) / A.G + 62) / 32));
     q.blocks = max(1, blocks);
     return q;
 }
@@ -147,13 +148,14 @@ __device__ __forceinline__ long size_of(const Args& A, const Seq& q) {
     return long(q.tiles) * A.c.hkv * q.blocks;
 }
 
-// A stage of a warp's ring: 16 keys of one head as they lie in their page.
-template <int D>
+// A stage of a warp's ring: 32 keys of one head as they lie in their page (or two).
+template <int D, int NT>
 struct Ring {
-    static constexpr int kI = D / 32, kStages = D == 256 ? 4 : 6;
-    static constexpr int kV = 8 * D, kKr = 16 * D, kVr = kKr + 16 * kI, kE = kKr + 32 * kI;      // where each part is
-    static constexpr int kBytes = kE + 32;
-    static constexpr int kSmem = kWarps * kStages * kBytes;
+    static constexpr int kI = D / 32, kStages = D == 256 ? 3 : 4;
+    static constexpr int kV = 16 * D, kKr = 32 * D, kVr = kKr + 32 * kI, kE = kKr + 64 * kI;      // where each part is
+    static constexpr int kBytes = kE + 64;
+    static constexpr int kSmem = kWarps<D, NT> * kStages * kBytes;
+    static constexpr int kRest = 4 * kI + 4;            // copies of 16 bytes that bring ratios and exponents
 };
 
 __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
@@ -161,12 +163,12 @@ __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel(const Args A, int workers) {
-    constexpr int kI = D / 32, R = 8 * NT;
-    using Rg = Ring<D>;
+__global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const Args A, int workers) {
+    constexpr int kI = D / 32, R = 8 * NT, kThreads = 32 * kWarps<D, NT>;
+    using Rg = Ring<D, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
-    __shared__ long sums[kWarps];
+    __shared__ long sums[kThreads / 32];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
     const int run = (A.s.batch + kThreads - 1) / kThreads;
     {
@@ -193,24 +195,38 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
     if (lane == 0) A.begun[worker] = make_int4(-1, 0, 0, 0);
     if (x >= end) return;
     int lo = 0;                                  // the run of sequences that x is in
-    for (int step = kThreads / 2; step; step /= 2)
-        if (before[lo + step] <= x) lo += step;
+    for (int step = 256; step; step /= 2)
+        if (lo + step < kThreads && before[lo + step] <= x) lo += step;
     long at = before[lo];
     int b = lo * run;
     Seq sq = sequence<R>(A, b);
 
     // the warp's ring, and what a lane copies of a stage: 16 bytes of every 512 of the
-    // codes, and of the rest its share
+    // codes, and of the rest its share: of K's ratios, V's, and the exponents, 2 kI, 2 kI
+    // and 4 lanes' worth (past 32: a second time)
     const uint32_t ring = smem_u32(smem) + warp_in * Rg::kStages * Rg::kBytes, ring_end = ring + Rg::kStages * Rg::kBytes;
-    const int kind = lane < kI ? 0 : lane < 2 * kI ? 1 : 2;         // (ratios of keys, of values; exponents)
-    const bool rest = lane < 2 * kI + 2;
-    const int rest_row = kind < 2 ? kI : 2;
-    const uint32_t rest_to = Rg::kKr + 16 * lane;
     const uint32_t page_rows = 1u << A.c.log_page, both = page_rows * A.c.hkv;      // (of keys or values, of a page)
-    const uint8_t* rest_from = (kind < 2 ? A.c.ratios + (kind ? size_t(both) * kI : 0) : A.c.exponents) +
-                               16 * (lane - (kind == 0 ? 0 : kind == 1 ? kI : 2 * kI));
-    const uint32_t rest_page = both * (kind < 2 ? 2 * kI : 2);
-    const int log_blocks = A.c.log_page - 4, in_page = (1 << log_blocks) - 1;
+    constexpr int kMore = Rg::kRest > 32 ? 2 : 1;
+    uint32_t rest_to[kMore], rest_page[kMore];
+    const uint8_t* rest_from[kMore];
+    int rest_row[kMore];
+    bool rest_late[kMore];                       // (of the second half of the stage's keys)
+#pragma unroll
+    for (int m = 0; m < kMore; ++m) {
+        const int i = lane + 32 * m, kind = i < 2 * kI ? 0 : i < 4 * kI ? 1 : 2, j = i - 2 * kI * kind;
+        rest_to[m] = i < Rg::kRest ? Rg::kKr + 16 * i : 0;
+        rest_row[m] = kind < 2 ? kI : 2;
+        rest_page[m] = both * (kind < 2 ? 2 * kI : 2);
+        rest_late[m] = j * 16 >= 16 * rest_row[m];
+        rest_from[m] = (kind < 2 ? A.c.ratios + (kind ? size_t(both) * kI : 0) : A.c.exponents) + 16 * j;
+    }
+    const int log_blocks = A.c.log_page - 5;     // (below 0: pages of 16, two to a stage)
+    const int in_page = log_blocks > 0 ? (1 << log_blocks) - 1 : 0;
+    const bool small = log_blocks < 0;
+    // (kept in registers: as constants they are made anew for every product)
+    uint32_t eights[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(eights[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));   // -128, -8 (2^-24)
 
     while (x < end) {
         while (at + size_of<R>(A, sq) <= x) {
@@ -227,46 +243,66 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
         const int base = sq.length - sq.new_;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
-        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / 16 : 0;
-        const int kb_end = min(kb0 + j1, (last_pos + 16) / 16);
+        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / 32 : 0;
+        const int kb_end = min(kb0 + j1, (last_pos + 32) / 32);
         int kb = kb0 + j0, kb_in = kb;
 
         // ---- stages on their way: the pages of 32 places at a time in the lanes ----
         const int* table = A.s.table + size_t(b) * A.s.width;
-        int ids_at = kb >> log_blocks;
+        auto place = [&](int at) { return small ? 2 * at : at >> log_blocks; };
+        int ids_at = place(kb);
         auto pages_from = [&](int i) { return i + lane < A.s.width ? __ldg(table + i + lane) : -1; };
         int ids = pages_from(ids_at), more = pages_from(ids_at + 32);
         const uint8_t* codes = A.c.codes + size_t(page_rows) * head * (D / 2) + 16 * lane;
-        const uint8_t* others = rest_from + size_t(page_rows) * head * rest_row;
-        const uint8_t *k_in, *rest_in;
+        const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the second 16 keys')
         bool broken = false;                     // a page that is none of the cache's
         auto locate = [&]() {
-            const int i = kb_in >> log_blocks;
+            const int i = place(kb_in);
             if (i - ids_at >= 32) {
                 ids = more;
                 ids_at += 32;
                 more = pages_from(ids_at + 32);
             }
-            int page = __shfl_sync(kFull, ids, i - ids_at);
-            if (page < 0 || page >= A.c.pages) broken = true, page = 0;
-            const uint32_t slot = 16 * (kb_in & in_page);
-            k_in = codes + uint64_t(uint32_t(page)) * (both * D) + slot * (D / 2);
-            rest_in = others + uint64_t(uint32_t(page)) * rest_page + slot * rest_row;
+            auto checked = [&](int at) {
+                const int page = __shfl_sync(kFull, ids, at);
+                if (page >= 0 && page < A.c.pages) return uint32_t(page);
+                broken = true;
+                return 0u;
+            };
+            const uint32_t page = checked(i - ids_at);
+            uint32_t late = page;
+            if (small) late = 32 * kb_in + 16 <= last_pos ? checked(i - ids_at + 1) : page;
+            const uint32_t slot = 32 * (kb_in & in_page);
+            k_in = codes + uint64_t(page) * (both * D) + slot * (D / 2);
+            late_in = small ? codes + uint64_t(late) * (both * D) : k_in + 8 * D;
+#pragma unroll
+            for (int m = 0; m < kMore; ++m)
+                rest_in[m] = rest_from[m] + size_t(page_rows) * head * rest_row[m] + uint64_t(rest_late[m] ? late : page) * rest_page[m] +
+                             slot * rest_row[m] - (small && rest_late[m] ? 16 * rest_row[m] : 0);
         };
         uint32_t in_at = ring, out_at = ring;
         auto fill = [&]() {
             if (kb_in < kb_end) {
-                const uint8_t* v_in = k_in + both * (D / 2);
+                const uint32_t values = both * (D / 2);
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) cp16(in_at + 16 * lane + 512 * j, k_in + 512 * j);
+                for (int j = 0; j < D / 32; ++j) {
+                    const uint8_t* from = (j < D / 64 ? k_in : late_in) + 512 * (j % (D / 64));
+                    cp16(in_at + 16 * lane + 512 * j, from);
+                    cp16(in_at + 16 * lane + Rg::kV + 512 * j, from + values);
+                }
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) cp16(in_at + 16 * lane + Rg::kV + 512 * j, v_in + 512 * j);
-                if (rest) cp16(in_at + rest_to, rest_in);
+                for (int m = 0; m < kMore; ++m)
+                    if (rest_to[m]) cp16(in_at + rest_to[m], rest_in[m]);
                 in_at += Rg::kBytes;
                 if (in_at == ring_end) in_at = ring;
-                k_in += 8 * D;
-                rest_in += 16 * rest_row;
-                if ((++kb_in & in_page) == 0 && kb_in < kb_end) locate();
+                if ((++kb_in & in_page) == 0) {
+                    if (kb_in < kb_end) locate();
+                } else {
+                    k_in += 16 * D;
+                    late_in += 16 * D;
+#pragma unroll
+                    for (int m = 0; m < kMore; ++m) rest_in[m] += 32 * rest_row[m];
+                }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
@@ -347,20 +383,16 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
         // ---- the keys ----
         const uint32_t k_of = 4 * kI * lane, v_of = Rg::kV + g * 2 * kI, v0_of = v_of + (2 * t + (t & 1)) * (D / 2),
                        v1_of = v_of + (2 * t + 1 - (t & 1)) * (D / 2), e_of = Rg::kE + 2 * g;
-        auto block = [&](auto at_edge) {
+        auto block = [&](auto at_edge, const int half) {
             constexpr bool kEdge = decltype(at_edge)::value;
-            // (the stage is there when all but the newest kStages - 2 are; all lanes have
-            // read the one before, which is filled anew)
-            asm volatile("cp.async.wait_group %0;" ::"n"(Rg::kStages - 2) : "memory");
-            __syncwarp();
-            fill();
-            const int key0 = 16 * kb;
+            const int key0 = 32 * kb + 16 * half;
+            const uint32_t codes_at = out_at + half * 8 * D, ratios_at = out_at + half * 16 * kI;
             uint32_t kc[2][kI], kr[2][(kI + 3) / 4], ex[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                lds<4 * kI>(kc[h], out_at + k_of + h * 8 * (D / 2));
-                lds<kI>(kr[h], out_at + Rg::kKr + g * kI + 8 * h * kI);
-                lds<2>(&ex[h], out_at + e_of + 16 * h);
+                lds<4 * kI>(kc[h], codes_at + k_of + h * 8 * (D / 2));
+                lds<kI>(kr[h], ratios_at + Rg::kKr + g * kI + 8 * h * kI);
+                lds<2>(&ex[h], out_at + e_of + 32 * half + 16 * h);
             }
             // scores: first what the codes' 8 adds to all groups, by the ratios of two of
             // them as fp16 (bytes of a word, with their signs, 0, between them)
@@ -469,9 +501,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
             uint32_t v[4][(kI + 1) / 2], vr[2][(2 * kI + 3) / 4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                lds<2 * kI>(v[2 * h], out_at + v0_of + h * 8 * (D / 2));
-                lds<2 * kI>(v[2 * h + 1], out_at + v1_of + h * 8 * (D / 2));
-                lds<2 * kI>(vr[h], out_at + Rg::kVr + 2 * t * kI + 8 * h * kI);
+                lds<2 * kI>(v[2 * h], codes_at + v0_of + h * 8 * (D / 2));
+                lds<2 * kI>(v[2 * h + 1], codes_at + v1_of + h * 8 * (D / 2));
+                lds<2 * kI>(vr[h], ratios_at + Rg::kVr + 2 * t * kI + 8 * h * kI);
             }
             if (kEdge) {
                 // what no row sees may hold anything: its ratios are left out
@@ -498,7 +530,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
                 const uint32_t lo4[4] = {a & 0x000f000fu, a & 0x00f000f0u, c & 0x000f000fu, c & 0x00f000f0u};
                 const uint32_t a8 = a >> 8, c8 = c >> 8;
                 const uint32_t hi4[4] = {a8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x000f000fu, c8 & 0x00f000f0u};
-                const uint32_t eights[4] = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};     // -8 2^-24, -128 2^-24
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const uint32_t b0 = mul2(w[n][0], r0), b1 = mul2(w[n][1], r1);
@@ -508,16 +539,25 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
                     mma(acc[n][i][1], eights, b0, b1);
                 }
             }
+        };
+        // (stages all of whose keys all rows see, and the others)
+        const int inner = A.window && last_pos >= A.window ? (last_pos - A.window) / 32 + 1 : 0, inner_end = (first_pos + 1) / 32;
+        for (; kb < kb_end; ++kb) {
+            // (the stage is there when all but the newest kStages - 2 are; all lanes have
+            // read the one before, which is filled anew)
+            asm volatile("cp.async.wait_group %0;" ::"n"(Rg::kStages - 2) : "memory");
+            __syncwarp();
+            fill();
+            if (kb >= inner && kb < inner_end) {
+                block(std::false_type(), 0);
+                block(std::false_type(), 1);
+            } else {
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half)
+                    if (32 * kb + 16 * half <= last_pos) block(std::true_type(), half);
+            }
             out_at += Rg::kBytes;
             if (out_at == ring_end) out_at = ring;
-        };
-        // (blocks all of whose keys all rows see, and the others)
-        const int inner = A.window && last_pos >= A.window ? (last_pos - A.window) / 16 + 1 : 0, inner_end = (first_pos + 1) / 16;
-        for (; kb < kb_end; ++kb) {
-            if (kb >= inner && kb < inner_end)
-                block(std::false_type());
-            else
-                block(std::true_type());
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -565,9 +605,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<D>(NT)) attention_kernel
 
 // Joins the states of a tile whose keys went to several workers: a block per row.
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads) join_kernel(const Args A, int workers) {
+__global__ void __launch_bounds__(kJoin) join_kernel(const Args A, int workers) {
     constexpr int R = 8 * NT, kVec = D / 32;
-    __shared__ float part[kWarps][D + 2];
+    __shared__ float part[kJoin / 32][D + 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, col = blockIdx.y;
     for (int w0 = blockIdx.x; w0 < workers; w0 += gridDim.x) {
         const int4 x = A.begun[w0];
@@ -575,7 +615,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Args A, int worker
         if (x.x < 0 || col >= rows) continue;
         // (the first worker's state is its second, if it did not begin with the tile)
         float m = kNone, l = 0.f, o[kVec] = {};
-        for (int w = w0 + warp; w <= x.w; w += kWarps) {
+        for (int w = w0 + warp; w <= x.w; w += kJoin / 32) {
             const float* from = A.states + ((size_t(w) * 2 + (w == w0 ? x.z >> 30 & 1 : 0)) * R + col) * (D + 4);
             const float mw = from[D], lw = from[D + 1], M = fmaxf(m, mw), f = ex2(m - M), fw = ex2(mw - M);
             m = M;
@@ -590,12 +630,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Args A, int worker
         __syncthreads();
         const int head = x.z & 0x3fffffff, r = tile * R + col, token = r / A.G;
         __nv_bfloat16* to = A.out + (size_t(x.x + token) * A.c.hkv * A.G + head * A.G + r - token * A.G) * D;
-        for (int e = threadIdx.x; e < D; e += kThreads) {
+        for (int e = threadIdx.x; e < D; e += kJoin) {
             float M = kNone, sum = 0.f, y = 0.f;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) M = fmaxf(M, part[k][D]);
+            for (int k = 0; k < kJoin / 32; ++k) M = fmaxf(M, part[k][D]);
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) {
+            for (int k = 0; k < kJoin / 32; ++k) {
                 const float f = ex2(part[k][D] - M);
                 sum += part[k][D + 1] * f;
                 y += part[k][e] * f;
@@ -610,11 +650,11 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     static splice::PerDevice<int> counts;
     int sms = 0;
     const cudaError_t e = counts.get(&sms, [](int dev, int* n) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D>::kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NT>::kSmem);
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
     if (e != cudaSuccess) return int(e);
-    const int grid = sms * ctas_per_sm<D>(NT), workers = grid * kWarps;
+    const int grid = sms, workers = grid * kWarps<D, NT>;
     const long states = long(workers) * 2 * 8 * NT * (D + 4) * 4;
     if (bytes) {
         *bytes = states + long(workers) * 16;
@@ -623,9 +663,9 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     Args A = a;
     A.states = static_cast<float*>(scratch);
     A.begun = reinterpret_cast<int4*>(static_cast<char*>(scratch) + states);
-    constexpr int kSmem = Ring<D>::kSmem;
-    attention_kernel<D, NT><<<grid, kThreads, kSmem, stream>>>(A, workers);
-    join_kernel<D, NT><<<dim3(unsigned(sms), 8 * NT), kThreads, 0, stream>>>(A, workers);
+    constexpr int kSmem = Ring<D, NT>::kSmem;
+    attention_kernel<D, NT><<<grid, 32 * kWarps<D, NT>, kSmem, stream>>>(A, workers);
+    join_kernel<D, NT><<<dim3(unsigned(sms), 8 * NT), kJoin, 0, stream>>>(A, workers);
     return int(cudaGetLastError());
 }
 
