@@ -44,7 +44,7 @@ using splice::tc::smem_u32;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
-constexpr int kMinShare = 2;            // blocks of 32 keys to a warp, at least
+constexpr int kMinKeys = 64;            // keys to a warp, at least
 
 struct Args {
     PageLayer c;
@@ -58,9 +58,24 @@ struct Args {
     int4* begun;            // per worker: the tile whose keys begin with it and go on
 };
 
-// Warps to an SM, all of one CTA: as many as their registers allow.
-template <int D, int NT>
-constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
+// A warp's products have 8 NT columns: rows of one kv head, or of P heads next to each
+// other, 8 / P of each.
+template <int D_, int NT_, int P_>
+struct Shape {
+    static constexpr int D = D_, NT = NT_, P = P_, kI = D / 32;
+    static constexpr int kCols = 8 * NT, kRows = kCols / P;         // (rows of a head, to a tile)
+    static constexpr int kKeys = 32 / P;                            // keys to a stage: two runs of 16, or of two heads
+    // warps to an SM, all of one CTA: as many as their registers allow
+    static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
+    static constexpr int kThreads = 32 * kWarps;
+    // a stage of a warp's ring: where its parts are
+    static constexpr int kStages = D == 256 ? 2 : D == 128 ? 3 : 4;
+    static constexpr int kV = 16 * D, kKr = 32 * D, kVr = kKr + 32 * kI, kE = kKr + 64 * kI, kBytes = kE + 64;
+    static constexpr int kRest = 4 * kI + 4;                        // copies of 16 bytes that bring ratios and exponents
+    static constexpr int kQ = P * NT * kI * 512;                    // q as operands
+    static constexpr int kWarpBytes = kStages * kBytes + kQ, kSmem = kWarps * kWarpBytes;
+    static_assert(kSmem <= 224 * 1024);
+};
 constexpr int kJoin = 128;              // threads of a CTA that joins states
 
 __device__ __forceinline__ float ex2(float x) {
@@ -124,48 +139,41 @@ __device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
-// blocks of 32 keys as the one that sees most.
+// stages of keys as the one that sees most.
 struct Seq {
     int first, new_, length, tiles, blocks;     // (its first row of q; its tokens, its keys)
 };
 
-template <int R>
+template <class S>
 __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     Seq q;
     const int first = max(0, min(A.s.starts[b], A.s.rows)), end = max(first, min(A.s.starts[b + 1], A.s.rows));
     q.first = first;
     q.new_ = end - first;
     q.length = max(0, A.s.lengths[b]);
-    q.tiles = int((long(q.new_) * A.G + R - 1) / R);
-    int blocks = q.length / 32 + (q.length % 32 != 0);
-    if (A.window) blocks = min(blocks, int((long(A.window) + (R + A.G - 2) / A.G + 62) / 32));
+    q.tiles = int((long(q.new_) * A.G + S::kRows - 1) / S::kRows);
+    int blocks = q.length / S::kKeys + (q.length % S::kKeys != 0);
+    if (A.window) blocks = min(blocks, int((long(A.window) + (S::kRows + A.G - 2) / A.G + 2 * S::kKeys - 2) / S::kKeys));
     q.blocks = max(1, blocks);
     return q;
 }
 
-template <int R>
+template <class S>
 __device__ __forceinline__ long size_of(const Args& A, const Seq& q) {
-    return long(q.tiles) * A.c.hkv * q.blocks;
+    return long(q.tiles) * (A.c.hkv / S::P) * q.blocks;
 }
 
-// A stage of a warp's ring: 32 keys of one head as they lie in their page (or two).
-template <int D, int NT>
-struct Ring {
-    static constexpr int kI = D / 32, kStages = D == 256 ? 3 : 4;
-    static constexpr int kV = 16 * D, kKr = 32 * D, kVr = kKr + 32 * kI, kE = kKr + 64 * kI;      // where each part is
-    static constexpr int kBytes = kE + 64;
-    static constexpr int kSmem = kWarps<D, NT> * kStages * kBytes;
-    static constexpr int kRest = 4 * kI + 4;            // copies of 16 bytes that bring ratios and exponents
-};
+__device__ __forceinline__ void sts16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 
 __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-template <int D, int NT>
-__global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const Args A, int workers) {
-    constexpr int kI = D / 32, R = 8 * NT, kThreads = 32 * kWarps<D, NT>;
-    using Rg = Ring<D, NT>;
+template <class S>
+__global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A, int workers) {
+    constexpr int D = S::D, NT = S::NT, P = S::P, kI = S::kI, kThreads = S::kThreads, R = S::kRows;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kThreads / 32];
@@ -173,7 +181,7 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
     const int run = (A.s.batch + kThreads - 1) / kThreads;
     {
         long mine = 0;
-        for (int b = threadIdx.x * run; b < min(A.s.batch, int(threadIdx.x + 1) * run); ++b) mine += size_of<R>(A, sequence<R>(A, b));
+        for (int b = threadIdx.x * run; b < min(A.s.batch, int(threadIdx.x + 1) * run); ++b) mine += size_of<S>(A, sequence<S>(A, b));
         long x = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -188,7 +196,7 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
         __syncthreads();
     }
     const long total = before[kThreads];
-    const long share = max(long(kMinShare), (total + workers - 1) / workers);
+    const long share = max(long(kMinKeys / S::kKeys), (total + workers - 1) / workers);
     const int worker = warp_in * gridDim.x + blockIdx.x;
     long x = worker * share;
     const long end = min(total, x + share);
@@ -199,28 +207,29 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
         if (lo + step < kThreads && before[lo + step] <= x) lo += step;
     long at = before[lo];
     int b = lo * run;
-    Seq sq = sequence<R>(A, b);
+    Seq sq = sequence<S>(A, b);
 
     // the warp's ring, and what a lane copies of a stage: 16 bytes of every 512 of the
     // codes, and of the rest its share: of K's ratios, V's, and the exponents, 2 kI, 2 kI
     // and 4 lanes' worth (past 32: a second time)
-    const uint32_t ring = smem_u32(smem) + warp_in * Rg::kStages * Rg::kBytes, ring_end = ring + Rg::kStages * Rg::kBytes;
+    const uint32_t ring = smem_u32(smem) + warp_in * S::kWarpBytes, ring_end = ring + S::kStages * S::kBytes;
+    const uint32_t q_at = ring_end + 16 * lane;
     const uint32_t page_rows = 1u << A.c.log_page, both = page_rows * A.c.hkv;      // (of keys or values, of a page)
-    constexpr int kMore = Rg::kRest > 32 ? 2 : 1;
+    constexpr int kMore = S::kRest > 32 ? 2 : 1;
     uint32_t rest_to[kMore], rest_page[kMore];
     const uint8_t* rest_from[kMore];
     int rest_row[kMore];
-    bool rest_late[kMore];                       // (of the second half of the stage's keys)
+    bool rest_late[kMore];                       // (of the stage's second half)
 #pragma unroll
     for (int m = 0; m < kMore; ++m) {
         const int i = lane + 32 * m, kind = i < 2 * kI ? 0 : i < 4 * kI ? 1 : 2, j = i - 2 * kI * kind;
-        rest_to[m] = i < Rg::kRest ? Rg::kKr + 16 * i : 0;
+        rest_to[m] = i < S::kRest ? S::kKr + 16 * i : 0;
         rest_row[m] = kind < 2 ? kI : 2;
         rest_page[m] = both * (kind < 2 ? 2 * kI : 2);
         rest_late[m] = j * 16 >= 16 * rest_row[m];
         rest_from[m] = (kind < 2 ? A.c.ratios + (kind ? size_t(both) * kI : 0) : A.c.exponents) + 16 * j;
     }
-    const int log_blocks = A.c.log_page - 5;     // (below 0: pages of 16, two to a stage)
+    const int log_blocks = A.c.log_page - (P == 2 ? 4 : 5);     // (below 0: pages of 16, two to a stage)
     const int in_page = log_blocks > 0 ? (1 << log_blocks) - 1 : 0;
     const bool small = log_blocks < 0;
     // (kept in registers: as constants they are made anew for every product)
@@ -229,22 +238,22 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
     for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(eights[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));   // -128, -8 (2^-24)
 
     while (x < end) {
-        while (at + size_of<R>(A, sq) <= x) {
-            at += size_of<R>(A, sq);
+        while (at + size_of<S>(A, sq) <= x) {
+            at += size_of<S>(A, sq);
             if (++b >= A.s.batch) return;        // (lengths that changed under the call)
-            sq = sequence<R>(A, b);
+            sq = sequence<S>(A, b);
         }
         const long rel = x - at;
         const int item = int(rel / sq.blocks), j0 = int(rel - long(item) * sq.blocks);
         const int j1 = int(min(long(sq.blocks), j0 + (end - x)));
-        const int head = item / sq.tiles, tile = item - head * sq.tiles;
+        const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
         const long item_at = x - j0;
         x += j1 - j0;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
         const int base = sq.length - sq.new_;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
-        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / 32 : 0;
-        const int kb_end = min(kb0 + j1, (last_pos + 32) / 32);
+        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / S::kKeys : 0;
+        const int kb_end = min(kb0 + j1, (last_pos + S::kKeys) / S::kKeys);
         int kb = kb0 + j0, kb_in = kb;
 
         // ---- stages on their way: the pages of 32 places at a time in the lanes ----
@@ -254,7 +263,7 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
         auto pages_from = [&](int i) { return i + lane < A.s.width ? __ldg(table + i + lane) : -1; };
         int ids = pages_from(ids_at), more = pages_from(ids_at + 32);
         const uint8_t* codes = A.c.codes + size_t(page_rows) * head * (D / 2) + 16 * lane;
-        const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the second 16 keys')
+        const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the stage's second half)
         bool broken = false;                     // a page that is none of the cache's
         auto locate = [&]() {
             const int i = place(kb_in);
@@ -272,13 +281,13 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
             const uint32_t page = checked(i - ids_at);
             uint32_t late = page;
             if (small) late = 32 * kb_in + 16 <= last_pos ? checked(i - ids_at + 1) : page;
-            const uint32_t slot = 32 * (kb_in & in_page);
+            const uint32_t slot = S::kKeys * (kb_in & in_page);
             k_in = codes + uint64_t(page) * (both * D) + slot * (D / 2);
-            late_in = small ? codes + uint64_t(late) * (both * D) : k_in + 8 * D;
+            late_in = P == 2 ? k_in + page_rows * (D / 2) : small ? codes + uint64_t(late) * (both * D) : k_in + 8 * D;
 #pragma unroll
             for (int m = 0; m < kMore; ++m)
                 rest_in[m] = rest_from[m] + size_t(page_rows) * head * rest_row[m] + uint64_t(rest_late[m] ? late : page) * rest_page[m] +
-                             slot * rest_row[m] - (small && rest_late[m] ? 16 * rest_row[m] : 0);
+                             slot * rest_row[m] + (rest_late[m] ? (P == 2 ? int(page_rows) - 16 : small ? -16 : 0) * rest_row[m] : 0);
         };
         uint32_t in_at = ring, out_at = ring;
         auto fill = [&]() {
@@ -288,37 +297,37 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
                 for (int j = 0; j < D / 32; ++j) {
                     const uint8_t* from = (j < D / 64 ? k_in : late_in) + 512 * (j % (D / 64));
                     cp16(in_at + 16 * lane + 512 * j, from);
-                    cp16(in_at + 16 * lane + Rg::kV + 512 * j, from + values);
+                    cp16(in_at + 16 * lane + S::kV + 512 * j, from + values);
                 }
 #pragma unroll
                 for (int m = 0; m < kMore; ++m)
                     if (rest_to[m]) cp16(in_at + rest_to[m], rest_in[m]);
-                in_at += Rg::kBytes;
+                in_at += S::kBytes;
                 if (in_at == ring_end) in_at = ring;
                 if ((++kb_in & in_page) == 0) {
                     if (kb_in < kb_end) locate();
                 } else {
-                    k_in += 16 * D;
-                    late_in += 16 * D;
+                    k_in += S::kKeys * (D / 2);
+                    late_in += S::kKeys * (D / 2);
 #pragma unroll
-                    for (int m = 0; m < kMore; ++m) rest_in[m] += 32 * rest_row[m];
+                    for (int m = 0; m < kMore; ++m) rest_in[m] += S::kKeys * rest_row[m];
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         if (kb < kb_end) locate();
 #pragma unroll 1
-        for (int i = 0; i < Rg::kStages - 1; ++i) fill();
+        for (int i = 0; i < S::kStages - 1; ++i) fill();
 
         // ---- the rows: q as an operand, and what is known of each column ----
-        uint32_t qf[NT][kI][4], minus[NT][kI > 4 ? 4 : 2];
+        uint32_t minus[P][NT][kI > 4 ? 4 : 2];
         float factor[NT][2], l[NT][2], ref[NT][2];
         int pos[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int col = 8 * n + g, r = tile * R + col, token = r / A.G;
+            const int mine = P == 2 ? g >> 2 : 0, col = P == 2 ? g & 3 : 8 * n + g, r = tile * R + col, token = r / A.G;
             const __nv_bfloat16* p = A.q + (sq.first + (col < rows ? token : 0)) * A.q_token +
-                                     (head * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
+                                     ((head + mine) * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
             uint32_t raw[kI][4], top2 = 0;
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
@@ -344,9 +353,16 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
                     f[j] = __uint_as_float(j & 1 ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    qf[n][i][j] = half2_of(f[j], f[j + 4]);
-                    const float2 y = __half22float2(reinterpret_cast<const __half2&>(qf[n][i][j]));
+                    raw[i][j] = half2_of(f[j], f[j + 4]);
+                    const float2 y = __half22float2(reinterpret_cast<const __half2&>(raw[i][j]));
                     sum = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, sum);
+                }
+                // (a head's operand has zeros for the other's columns; a lane reads its own)
+#pragma unroll
+                for (int ph = 0; ph < P; ++ph) {
+                    const bool zero = P == 2 && ph != mine;
+                    sts16(q_at + ((ph * NT + n) * kI + i) * 512, zero ? 0 : raw[i][0], zero ? 0 : raw[i][1], zero ? 0 : raw[i][2],
+                          zero ? 0 : raw[i][3]);
                 }
                 sum += __shfl_xor_sync(kFull, sum, 1);
                 sum += __shfl_xor_sync(kFull, sum, 2);
@@ -356,21 +372,26 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
             }
             // as an operand against the keys' ratios (see below)
             auto two = [](const uint32_t* y, int i) { return y[i] | y[i + 1] << 16; };
+            uint32_t m[kI > 4 ? 4 : 2];
             if constexpr (kI == 2) {
-                minus[n][0] = t == 0 ? two(hi, 0) : t == 1 ? two(mid, 0) : t == 2 ? two(low, 0) : 0u;
-                minus[n][1] = 0u;
+                m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(mid, 0) : t == 2 ? two(low, 0) : 0u;
+                m[1] = 0u;
             } else if constexpr (kI == 4) {
-                minus[n][0] = t == 0 ? two(hi, 0) : t == 1 ? two(hi, 2) : t == 2 ? two(mid, 0) : two(mid, 2);
-                minus[n][1] = t == 0 ? two(low, 0) : t == 1 ? two(low, 2) : 0u;
+                m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(hi, 2) : t == 2 ? two(mid, 0) : two(mid, 2);
+                m[1] = t == 0 ? two(low, 0) : t == 1 ? two(low, 2) : 0u;
             } else {
                 auto by_t = [&](const uint32_t* y) { return t == 0 ? two(y, 0) : t == 1 ? two(y, 2) : t == 2 ? two(y, 4) : two(y, 6); };
-                minus[n][0] = by_t(hi), minus[n][1] = by_t(mid), minus[n][2] = by_t(low), minus[n][3] = 0u;
+                m[0] = by_t(hi), m[1] = by_t(mid), m[2] = by_t(low), m[3] = 0u;
             }
+#pragma unroll
+            for (int ph = 0; ph < P; ++ph)
+#pragma unroll
+                for (int j = 0; j < (kI > 4 ? 4 : 2); ++j) minus[ph][n][j] = P == 2 && ph != mine ? 0u : m[j];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 // S 2^(E_k - 2) 2^24 / up, in bits
                 factor[n][c] = __shfl_sync(kFull, down, 4 * (2 * t + c)) * (0x1p22f * kLog2e) * A.scale;
-                const int column = 8 * n + 2 * t + c;
+                const int column = P == 2 ? 2 * t + c & 3 : 8 * n + 2 * t + c;
                 pos[n][c] = column < rows ? base + (tile * R + column) / A.G : -1;
                 l[n][c] = 0.f;
                 ref[n][c] = kNone;
@@ -381,58 +402,79 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
         const uint32_t even = t & 1 ? 0x1054u : 0x5410u, odd = t & 1 ? 0x3276u : 0x7632u;
 
         // ---- the keys ----
-        const uint32_t k_of = 4 * kI * lane, v_of = Rg::kV + g * 2 * kI, v0_of = v_of + (2 * t + (t & 1)) * (D / 2),
-                       v1_of = v_of + (2 * t + 1 - (t & 1)) * (D / 2), e_of = Rg::kE + 2 * g;
+        const uint32_t k_of = 4 * kI * lane, v_of = S::kV + g * 2 * kI, v0_of = v_of + (2 * t + (t & 1)) * (D / 2),
+                       v1_of = v_of + (2 * t + 1 - (t & 1)) * (D / 2), e_of = S::kE + 2 * g + (P == 2 ? 32 * (t >> 1) : 0);
+        // 16 keys: the stage's half, or (P = 2) both heads'
         auto block = [&](auto at_edge, const int half) {
             constexpr bool kEdge = decltype(at_edge)::value;
-            const int key0 = 32 * kb + 16 * half;
+            const int key0 = S::kKeys * kb + 16 * half;
             const uint32_t codes_at = out_at + half * 8 * D, ratios_at = out_at + half * 16 * kI;
-            uint32_t kc[2][kI], kr[2][(kI + 3) / 4], ex[2];
+            uint32_t kc[P][2][kI], ratio[P][2][kI / 2], ex[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                lds<4 * kI>(kc[h], codes_at + k_of + h * 8 * (D / 2));
-                lds<kI>(kr[h], ratios_at + Rg::kKr + g * kI + 8 * h * kI);
+#pragma unroll
+                for (int ph = 0; ph < P; ++ph) {
+                    lds<4 * kI>(kc[ph][h], codes_at + ph * 8 * D + k_of + h * 8 * (D / 2));
+                    uint32_t kr[(kI + 3) / 4];
+                    lds<kI>(kr, ratios_at + ph * 16 * kI + S::kKr + g * kI + 8 * h * kI);
+                    // two groups' ratios as fp16 (bytes of a word, with their signs, 0, between)
+#pragma unroll
+                    for (int i = 0; i < kI; i += 2) ratio[ph][h][i / 2] = bytes_of(kr[i / 4], 0, i % 4 ? 0xb3a2u : 0x9180u) << 7;
+                }
                 lds<2>(&ex[h], out_at + e_of + 32 * half + 16 * h);
             }
-            // scores: first what the codes' 8 adds to all groups, by the ratios of two of
-            // them as fp16 (bytes of a word, with their signs, 0, between them)
-            uint32_t ratio[2][kI / 2];
+            // scores: first what the codes' 8 adds to all groups
             float s[NT][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < kI; i += 2) ratio[h][i / 2] = bytes_of(kr[h][i / 4], 0, i % 4 ? 0xb3a2u : 0x9180u) << 7;
-            {
+            for (int ph = 0; ph < P; ++ph) {
                 auto mine = [&](int h) {
-                    if constexpr (kI == 2) return ratio[h][0];
-                    if constexpr (kI == 4) return t & 1 ? ratio[h][1] : ratio[h][0];
-                    if constexpr (kI == 8) return t & 2 ? (t & 1 ? ratio[h][3] : ratio[h][2]) : t & 1 ? ratio[h][1] : ratio[h][0];
+                    const uint32_t* r = ratio[ph][h];
+                    if constexpr (kI == 2) return r[0];
+                    if constexpr (kI == 4) return t & 1 ? r[1] : r[0];
+                    if constexpr (kI == 8) return t & 2 ? (t & 1 ? r[3] : r[2]) : t & 1 ? r[1] : r[0];
                 };
                 const uint32_t ra = mine(0), rc = mine(1);
                 const uint32_t r4[4] = {ra, rc, ra, rc};
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    mma0(s[n], r4, minus[n][0], minus[n][1]);
-                    if constexpr (kI > 4) mma(s[n], r4, minus[n][2], minus[n][3]);
+                    if (ph == 0)
+                        mma0(s[n], r4, minus[ph][n][0], minus[ph][n][1]);
+                    else
+                        mma(s[n], r4, minus[ph][n][0], minus[ph][n][1]);
+                    if constexpr (kI > 4) mma(s[n], r4, minus[ph][n][2], minus[ph][n][3]);
                 }
             }
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
-                const uint32_t a = kc[0][i], c = kc[1][i];
-                const uint32_t lo4[4] = {a & 0x000f000fu, c & 0x000f000fu, a & 0x00f000f0u, c & 0x00f000f0u};
-                const uint32_t a8 = a >> 8, c8 = c >> 8;
-                const uint32_t hi4[4] = {a8 & 0x000f000fu, c8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x00f000f0u};
-                const __half2 ra = reinterpret_cast<const __half2&>(ratio[0][i / 2]), rc = reinterpret_cast<const __half2&>(ratio[1][i / 2]);
+                float part[NT][4];
+#pragma unroll
+                for (int ph = 0; ph < P; ++ph) {
+                    const uint32_t a = kc[ph][0][i], c = kc[ph][1][i];
+                    const uint32_t lo4[4] = {a & 0x000f000fu, c & 0x000f000fu, a & 0x00f000f0u, c & 0x00f000f0u};
+                    const uint32_t a8 = a >> 8, c8 = c >> 8;
+                    const uint32_t hi4[4] = {a8 & 0x000f000fu, c8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x00f000f0u};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t qf[4];
+                        lds<16>(qf, q_at + ((ph * NT + n) * kI + i) * 512);
+                        if (ph == 0)
+                            mma0(part[n], lo4, qf[0], qf[1]);
+                        else
+                            mma(part[n], lo4, qf[0], qf[1]);
+                        mma(part[n], hi4, qf[2], qf[3]);
+                    }
+                }
+                // (by the ratios of the lane's columns' head)
+                const uint32_t r0 = P == 2 && t >= 2 ? ratio[P - 1][0][i / 2] : ratio[0][0][i / 2],
+                               r1 = P == 2 && t >= 2 ? ratio[P - 1][1][i / 2] : ratio[0][1][i / 2];
+                const __half2 ra = reinterpret_cast<const __half2&>(r0), rc = reinterpret_cast<const __half2&>(r1);
                 const float fa = i & 1 ? __high2float(ra) : __low2float(ra), fc = i & 1 ? __high2float(rc) : __low2float(rc);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    float part[4];
-                    mma0(part, lo4, qf[n][i][0], qf[n][i][1]);
-                    mma(part, hi4, qf[n][i][2], qf[n][i][3]);
-                    s[n][0] = fmaf(part[0], fa, s[n][0]);
-                    s[n][1] = fmaf(part[1], fa, s[n][1]);
-                    s[n][2] = fmaf(part[2], fc, s[n][2]);
-                    s[n][3] = fmaf(part[3], fc, s[n][3]);
+                    s[n][0] = fmaf(part[n][0], fa, s[n][0]);
+                    s[n][1] = fmaf(part[n][1], fa, s[n][1]);
+                    s[n][2] = fmaf(part[n][2], fc, s[n][2]);
+                    s[n][3] = fmaf(part[n][3], fc, s[n][3]);
                 }
             }
             // weights, of keys g and g + 8
@@ -498,65 +540,74 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
                 w[n][1] = transposed(half2_of(pv[2], pv[3]));
             }
             // output
-            uint32_t v[4][(kI + 1) / 2], vr[2][(2 * kI + 3) / 4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                lds<2 * kI>(v[2 * h], codes_at + v0_of + h * 8 * (D / 2));
-                lds<2 * kI>(v[2 * h + 1], codes_at + v1_of + h * 8 * (D / 2));
-                lds<2 * kI>(vr[h], ratios_at + Rg::kVr + 2 * t * kI + 8 * h * kI);
-            }
-            if (kEdge) {
-                // what no row sees may hold anything: its ratios are left out
+            for (int ph = 0; ph < P; ++ph) {
+                uint32_t v[4][(kI + 1) / 2], vr[2][(2 * kI + 3) / 4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = key0 + 2 * t + (j & 1) + 8 * (j >> 1);
-                    if (key > last_pos || (A.window && key <= first_pos - A.window)) {
-                        if constexpr (kI == 2) vr[j >> 1][0] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
-                        if constexpr (kI > 2)
+                for (int h = 0; h < 2; ++h) {
+                    lds<2 * kI>(v[2 * h], codes_at + ph * 8 * D + v0_of + h * 8 * (D / 2));
+                    lds<2 * kI>(v[2 * h + 1], codes_at + ph * 8 * D + v1_of + h * 8 * (D / 2));
+                    lds<2 * kI>(vr[h], ratios_at + ph * 16 * kI + S::kVr + 2 * t * kI + 8 * h * kI);
+                }
+                if (kEdge) {
+                    // what no row sees may hold anything: its ratios are left out
 #pragma unroll
-                            for (int i = 0; i < kI / 4; ++i) vr[j >> 1][(j & 1) * (kI / 4) + i] = 0;
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = key0 + 2 * t + (j & 1) + 8 * (j >> 1);
+                        if (key > last_pos || (A.window && key <= first_pos - A.window)) {
+                            if constexpr (kI == 2) vr[j >> 1][0] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+                            if constexpr (kI > 2)
+#pragma unroll
+                                for (int i = 0; i < kI / 4; ++i) vr[j >> 1][(j & 1) * (kI / 4) + i] = 0;
+                        }
                     }
                 }
-            }
+                // (a head's products add to its own columns)
+                uint32_t wh[NT][2];
 #pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                // bytes i of two keys' ratios, as fp16
-                constexpr int kNext = kI == 2 ? 2 : 4;               // (the second key's byte 0)
-                const uint32_t sel = (i & 3) | 8 << 4 | (kNext + (i & 3)) << 8 | 8 << 12;
-                const uint32_t r0 = bytes_of(vr[0][i / 4], vr[0][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
-                const uint32_t r1 = bytes_of(vr[1][i / 4], vr[1][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
-                const uint32_t a = bytes_of(v[0][i / 2], v[1][i / 2], i & 1 ? odd : even);
-                const uint32_t c = bytes_of(v[2][i / 2], v[3][i / 2], i & 1 ? odd : even);
-                const uint32_t lo4[4] = {a & 0x000f000fu, a & 0x00f000f0u, c & 0x000f000fu, c & 0x00f000f0u};
-                const uint32_t a8 = a >> 8, c8 = c >> 8;
-                const uint32_t hi4[4] = {a8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x000f000fu, c8 & 0x00f000f0u};
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint32_t b0 = mul2(w[n][0], r0), b1 = mul2(w[n][1], r1);
-                    mma(acc[n][i][0], lo4, b0, b1);
-                    mma(acc[n][i][1], hi4, b0, b1);
-                    mma(acc[n][i][0], eights, b0, b1);
-                    mma(acc[n][i][1], eights, b0, b1);
+                    for (int h = 0; h < 2; ++h) wh[n][h] = P == 2 && (g >> 2) != ph ? 0u : w[n][h];
+#pragma unroll
+                for (int i = 0; i < kI; ++i) {
+                    // bytes i of two keys' ratios, as fp16
+                    constexpr int kNext = kI == 2 ? 2 : 4;               // (the second key's byte 0)
+                    const uint32_t sel = (i & 3) | 8 << 4 | (kNext + (i & 3)) << 8 | 8 << 12;
+                    const uint32_t r0 = bytes_of(vr[0][i / 4], vr[0][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
+                    const uint32_t r1 = bytes_of(vr[1][i / 4], vr[1][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
+                    const uint32_t a = bytes_of(v[0][i / 2], v[1][i / 2], i & 1 ? odd : even);
+                    const uint32_t c = bytes_of(v[2][i / 2], v[3][i / 2], i & 1 ? odd : even);
+                    const uint32_t lo4[4] = {a & 0x000f000fu, a & 0x00f000f0u, c & 0x000f000fu, c & 0x00f000f0u};
+                    const uint32_t a8 = a >> 8, c8 = c >> 8;
+                    const uint32_t hi4[4] = {a8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x000f000fu, c8 & 0x00f000f0u};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t b0 = mul2(wh[n][0], r0), b1 = mul2(wh[n][1], r1);
+                        mma(acc[n][i][0], lo4, b0, b1);
+                        mma(acc[n][i][1], hi4, b0, b1);
+                        mma(acc[n][i][0], eights, b0, b1);
+                        mma(acc[n][i][1], eights, b0, b1);
+                    }
                 }
             }
         };
         // (stages all of whose keys all rows see, and the others)
-        const int inner = A.window && last_pos >= A.window ? (last_pos - A.window) / 32 + 1 : 0, inner_end = (first_pos + 1) / 32;
+        const int inner = A.window && last_pos >= A.window ? (last_pos - A.window) / S::kKeys + 1 : 0, inner_end = (first_pos + 1) / S::kKeys;
         for (; kb < kb_end; ++kb) {
             // (the stage is there when all but the newest kStages - 2 are; all lanes have
             // read the one before, which is filled anew)
-            asm volatile("cp.async.wait_group %0;" ::"n"(Rg::kStages - 2) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
             __syncwarp();
             fill();
             if (kb >= inner && kb < inner_end) {
                 block(std::false_type(), 0);
-                block(std::false_type(), 1);
+                if (P == 1) block(std::false_type(), 1);
             } else {
 #pragma unroll 1
-                for (int half = 0; half < 2; ++half)
-                    if (32 * kb + 16 * half <= last_pos) block(std::true_type(), half);
+                for (int half = 0; half < 2 / P; ++half)
+                    if (S::kKeys * kb + 16 * half <= last_pos) block(std::true_type(), half);
             }
-            out_at += Rg::kBytes;
+            out_at += S::kBytes;
             if (out_at == ring_end) out_at = ring;
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -576,12 +627,12 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
 #pragma unroll
                 for (int o = 4; o < 32; o *= 2) sum += __shfl_xor_sync(kFull, sum, o);
                 if (__any_sync(kFull, broken)) sum = __int_as_float(0x7fffffff);
-                const int col = 8 * n + 2 * t + c;
-                if (col >= rows) continue;
+                const int col = 8 * n + 2 * t + c, mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col;
+                if (row >= rows) continue;
                 const float f = whole ? (sum == 0.f ? 0.f : 0x1p16f / sum) : 0x1p16f;
                 if (whole) {
-                    const int r = tile * R + col, token = r / A.G;
-                    __nv_bfloat16* to = A.out + (size_t(sq.first + token) * A.c.hkv * A.G + head * A.G + r - token * A.G) * D;
+                    const int r = tile * R + row, token = r / A.G;
+                    __nv_bfloat16* to = A.out + ((size_t(sq.first + token) * A.c.hkv + head + mine) * A.G + r - token * A.G) * D;
 #pragma unroll
                     for (int i = 0; i < kI; ++i) {
                         const __nv_bfloat162 x0 = __floats2bfloat162_rn(acc[n][i][0][c] * f, acc[n][i][0][2 + c] * (f * 0.0625f));
@@ -590,7 +641,7 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
                             make_uint2(reinterpret_cast<const uint32_t&>(x0), reinterpret_cast<const uint32_t&>(x1));
                     }
                 } else {
-                    float* to = A.states + ((size_t(worker) * 2 + slot) * R + col) * (D + 4);
+                    float* to = A.states + ((size_t(worker) * 2 + slot) * S::kCols + col) * (D + 4);
 #pragma unroll
                     for (int i = 0; i < kI; ++i)
                         *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
@@ -604,19 +655,19 @@ __global__ void __launch_bounds__(32 * kWarps<D, NT>, 1) attention_kernel(const 
 }
 
 // Joins the states of a tile whose keys went to several workers: a block per row.
-template <int D, int NT>
+template <class S>
 __global__ void __launch_bounds__(kJoin) join_kernel(const Args A, int workers) {
-    constexpr int R = 8 * NT, kVec = D / 32;
+    constexpr int D = S::D, R = S::kRows, kVec = D / 32;
     __shared__ float part[kJoin / 32][D + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, col = blockIdx.y;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
     for (int w0 = blockIdx.x; w0 < workers; w0 += gridDim.x) {
         const int4 x = A.begun[w0];
         const int rows = x.y >> 24, tile = x.y & 0xffffff;
-        if (x.x < 0 || col >= rows) continue;
+        if (x.x < 0 || row >= rows) continue;
         // (the first worker's state is its second, if it did not begin with the tile)
         float m = kNone, l = 0.f, o[kVec] = {};
         for (int w = w0 + warp; w <= x.w; w += kJoin / 32) {
-            const float* from = A.states + ((size_t(w) * 2 + (w == w0 ? x.z >> 30 & 1 : 0)) * R + col) * (D + 4);
+            const float* from = A.states + ((size_t(w) * 2 + (w == w0 ? x.z >> 30 & 1 : 0)) * S::kCols + col) * (D + 4);
             const float mw = from[D], lw = from[D + 1], M = fmaxf(m, mw), f = ex2(m - M), fw = ex2(mw - M);
             m = M;
             l = l * f + lw * fw;
@@ -628,8 +679,8 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const Args A, int workers) 
         for (int i = 0; i < kVec; ++i) part[warp][lane + 32 * i] = o[i];
         if (lane == 0) part[warp][D] = m, part[warp][D + 1] = l;
         __syncthreads();
-        const int head = x.z & 0x3fffffff, r = tile * R + col, token = r / A.G;
-        __nv_bfloat16* to = A.out + (size_t(x.x + token) * A.c.hkv * A.G + head * A.G + r - token * A.G) * D;
+        const int head = (x.z & 0x3fffffff) + mine, r = tile * R + row, token = r / A.G;
+        __nv_bfloat16* to = A.out + ((size_t(x.x + token) * A.c.hkv + head) * A.G + r - token * A.G) * D;
         for (int e = threadIdx.x; e < D; e += kJoin) {
             float M = kNone, sum = 0.f, y = 0.f;
 #pragma unroll
@@ -645,17 +696,17 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const Args A, int workers) 
     }
 }
 
-template <int D, int NT>
+template <class S>
 int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     static splice::PerDevice<int> counts;
     int sms = 0;
     const cudaError_t e = counts.get(&sms, [](int dev, int* n) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D, NT>::kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
     if (e != cudaSuccess) return int(e);
-    const int grid = sms, workers = grid * kWarps<D, NT>;
-    const long states = long(workers) * 2 * 8 * NT * (D + 4) * 4;
+    const int workers = sms * S::kWarps;
+    const long states = long(workers) * 2 * S::kCols * (S::D + 4) * 4;
     if (bytes) {
         *bytes = states + long(workers) * 16;
         return 0;
@@ -663,19 +714,25 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
     Args A = a;
     A.states = static_cast<float*>(scratch);
     A.begun = reinterpret_cast<int4*>(static_cast<char*>(scratch) + states);
-    constexpr int kSmem = Ring<D, NT>::kSmem;
-    attention_kernel<D, NT><<<grid, 32 * kWarps<D, NT>, kSmem, stream>>>(A, workers);
-    join_kernel<D, NT><<<dim3(unsigned(sms), 8 * NT), kJoin, 0, stream>>>(A, workers);
+    attention_kernel<S><<<sms, S::kThreads, S::kSmem, stream>>>(A, workers);
+    join_kernel<S><<<dim3(unsigned(sms), S::kCols), kJoin, 0, stream>>>(A, workers);
     return int(cudaGetLastError());
 }
 
+template <int D>
+int run(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
+    // By the rows of a kv head that a sequence has on average: up to four share the
+    // columns with those of the next head, more than eight take sixteen columns (the
+    // codes are made operands once for both halves).
+    const long rows = long(a.s.rows) * a.G, all = a.s.batch;
+    if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream, bytes);
+    if constexpr (D < 256)
+        if (rows > 8 * all) return launch<Shape<D, 2, 1>>(a, scratch, stream, bytes);
+    return launch<Shape<D, 1, 1>>(a, scratch, stream, bytes);
+}
+
 int run(const Args& a, int d, void* scratch, cudaStream_t stream, long* bytes) {
-    // Sixteen rows to a tile where there are more than eight: the codes are made
-    // operands once for both halves.
-    const bool two = a.G > 8 || (a.s.rows > a.s.batch && long(a.s.rows) * a.G > 8L * a.s.batch);
-    if (d == 64) return two ? launch<64, 2>(a, scratch, stream, bytes) : launch<64, 1>(a, scratch, stream, bytes);
-    if (d == 128) return two ? launch<128, 2>(a, scratch, stream, bytes) : launch<128, 1>(a, scratch, stream, bytes);
-    return launch<256, 1>(a, scratch, stream, bytes);
+    return d == 64 ? run<64>(a, scratch, stream, bytes) : d == 128 ? run<128>(a, scratch, stream, bytes) : run<256>(a, scratch, stream, bytes);
 }
 
 }  // namespace
@@ -688,7 +745,7 @@ using namespace decoder;
 extern "C" long decoder_page_attention_scratch(int batch, int rows, int hq, int hkv, int d) {
     if (batch < 1 || rows < 1 || hkv < 1 || hq < 1 || hq % hkv || (d != 64 && d != 128 && d != 256) || long(rows) * hq >= 1L << 26) return 0;
     Args a = {};
-    a.s.batch = batch, a.s.rows = rows, a.G = hq / hkv;
+    a.s.batch = batch, a.s.rows = rows, a.G = hq / hkv, a.c.hkv = hkv;
     long bytes = 0;
     const int rc = run(a, d, nullptr, nullptr, &bytes);
     return rc ? -rc : bytes;
