@@ -115,6 +115,11 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     return reinterpret_cast<const uint32_t&>(h);
 }
 
+__device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
+    const __half2 h = __hadd2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
+    return reinterpret_cast<const uint32_t&>(h);
+}
+
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     const __half2 h = __hmul2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
     return reinterpret_cast<const uint32_t&>(h);
@@ -577,16 +582,14 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
                     const uint32_t r1 = bytes_of(vr[1][i / 4], vr[1][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
                     const uint32_t a = bytes_of(v[0][i / 2], v[1][i / 2], i & 1 ? odd : even);
                     const uint32_t c = bytes_of(v[2][i / 2], v[3][i / 2], i & 1 ? odd : even);
-                    const uint32_t lo4[4] = {a & 0x000f000fu, a & 0x00f000f0u, c & 0x000f000fu, c & 0x00f000f0u};
+                    const uint32_t lo4[4] = {add2(a & 0x000f000fu, eights[0]), add2(a & 0x00f000f0u, eights[1]), add2(c & 0x000f000fu, eights[0]), add2(c & 0x00f000f0u, eights[1])};
                     const uint32_t a8 = a >> 8, c8 = c >> 8;
-                    const uint32_t hi4[4] = {a8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x000f000fu, c8 & 0x00f000f0u};
+                    const uint32_t hi4[4] = {add2(a8 & 0x000f000fu, eights[0]), add2(a8 & 0x00f000f0u, eights[1]), add2(c8 & 0x000f000fu, eights[0]), add2(c8 & 0x00f000f0u, eights[1])};
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const uint32_t b0 = mul2(wh[n][0], r0), b1 = mul2(wh[n][1], r1);
                         mma(acc[n][i][0], lo4, b0, b1);
                         mma(acc[n][i][1], hi4, b0, b1);
-                        mma(acc[n][i][0], eights, b0, b1);
-                        mma(acc[n][i][1], eights, b0, b1);
                     }
                 }
             }
