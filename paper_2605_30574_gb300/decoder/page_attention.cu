@@ -45,6 +45,29 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
 constexpr int kMinKeys = 64;            // keys to a warp, at least
+constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
+
+// Every kernel is launched as a programmatic dependent of what precedes it on the stream:
+// set up while that still runs, it waits for all of it before it reads or writes.
+__device__ __forceinline__ void wait_for_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <class... Params, class... Given>
+int dependent(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, const Given&... given) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return int(cudaLaunchKernelEx(&cfg, kernel, given...));
+}
 
 struct Args {
     PageLayer c;
@@ -54,8 +77,8 @@ struct Args {
     __nv_bfloat16* out;
     int G, window;
     float scale;
-    float* states;          // [worker][2][rows][d + 2]
-    int4* begun;            // per worker: the tile whose keys begin with it and go on
+    float *states, *joined; // of warps and of CTAs: [each][2][columns][d + 4]
+    int4* begun;            // per CTA: the tile whose keys begin with it and go on
 };
 
 // A warp's products have 8 NT columns: rows of one kv head, or of P heads next to each
@@ -65,6 +88,7 @@ struct Shape {
     static constexpr int D = D_, NT = NT_, P = P_, kI = D / 32;
     static constexpr int kCols = 8 * NT, kRows = kCols / P;         // (rows of a head, to a tile)
     static constexpr int kKeys = 32 / P;                            // keys to a stage: two runs of 16, or of two heads
+    static constexpr int kBegin = 2;                                // stages that a tile's begin and end take as long as
     // warps to an SM, all of one CTA: as many as their registers allow
     static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
     static constexpr int kThreads = 32 * kWarps;
@@ -144,7 +168,7 @@ __device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
-// stages of keys as the one that sees most.
+// stages of keys, and kBegin more, as the one that sees most.
 struct Seq {
     int first, new_, length, tiles, blocks;     // (its first row of q; its tokens, its keys)
 };
@@ -159,7 +183,7 @@ __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     q.tiles = int((long(q.new_) * A.G + S::kRows - 1) / S::kRows);
     int blocks = q.length / S::kKeys + (q.length % S::kKeys != 0);
     if (A.window) blocks = min(blocks, int((long(A.window) + (S::kRows + A.G - 2) / A.G + 2 * S::kKeys - 2) / S::kKeys));
-    q.blocks = max(1, blocks);
+    q.blocks = max(1, blocks) + S::kBegin;
     return q;
 }
 
@@ -176,12 +200,68 @@ __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
+// Rows' states joined, a warp to a row: O for the reference m and the sum l, at D and D + 1.
+template <int D>
+struct State {
+    static constexpr int kVec = D / 32;
+    float m = kNone, l = 0.f, o[kVec] = {};
+
+    __device__ __forceinline__ void add(const float* from) {
+        float y[kVec];
+        const int lane = threadIdx.x & 31;
+        if constexpr (kVec == 2) {
+            const float2 v = reinterpret_cast<const float2*>(from)[lane];
+            y[0] = v.x, y[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec / 4; ++i) {
+                const float4 v = reinterpret_cast<const float4*>(from)[lane + 32 * i];
+                y[4 * i] = v.x, y[4 * i + 1] = v.y, y[4 * i + 2] = v.z, y[4 * i + 3] = v.w;
+            }
+        }
+        const float2 ml = *reinterpret_cast<const float2*>(from + D);
+        const float M = fmaxf(m, ml.x), f = ex2(m - M), fy = ex2(ml.x - M);
+        m = M;
+        l = l * f + ml.y * fy;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) o[i] = o[i] * f + y[i] * fy;
+    }
+    __device__ __forceinline__ void keep(float* to) const {
+        const int lane = threadIdx.x & 31;
+        if constexpr (kVec == 2) reinterpret_cast<float2*>(to)[lane] = make_float2(o[0], o[1]);
+        if constexpr (kVec > 2)
+#pragma unroll
+            for (int i = 0; i < kVec / 4; ++i)
+                reinterpret_cast<float4*>(to)[lane + 32 * i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        if (lane == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
+    }
+    __device__ __forceinline__ void write(__nv_bfloat16* to) const {
+        const int lane = threadIdx.x & 31;
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        constexpr int kRun = kVec == 2 ? 2 : 4;
+#pragma unroll
+        for (int i = 0; i < kVec; i += kRun)
+#pragma unroll
+            for (int j = 0; j < kRun; j += 2)
+                *reinterpret_cast<__nv_bfloat162*>(to + 32 * i + kRun * lane + j) = __floats2bfloat162_rn(o[i + j] * f, o[i + j + 1] * f);
+    }
+};
+
+// The row of out of a tile's row.
 template <class S>
-__global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A, int workers) {
+__device__ __forceinline__ size_t row_of(const Args& A, const int4& info, int mine, int row) {
+    const int r = (info.y & 0xffffff) * S::kRows + row, token = r / A.G;
+    return (size_t(info.x + token) * A.c.hkv + (info.z & 0x3fffffff) + mine) * A.G + r - token * A.G;
+}
+
+template <class S>
+__global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A) {
     constexpr int D = S::D, NT = S::NT, P = S::P, kI = S::kI, kThreads = S::kThreads, R = S::kRows;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kThreads / 32];
+    __shared__ int4 runs[S::kWarps + 1];        // tiles that warps share: the one that goes on here, and each warp's that goes on
+    wait_for_previous();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
     const int run = (A.s.batch + kThreads - 1) / kThreads;
     {
@@ -201,17 +281,23 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
         __syncthreads();
     }
     const long total = before[kThreads];
-    const long share = max(long(kMinKeys / S::kKeys), (total + workers - 1) / workers);
-    const int worker = warp_in * gridDim.x + blockIdx.x;
+    // few keys: four warps and more of as many CTAs as there are shares for
+    const long least = kMinKeys / S::kKeys;
+    const int active = int(max(long(kMinWarps), min(long(S::kWarps), (total + least * gridDim.x - 1) / (least * gridDim.x))));
+    const long share = max(least, (total + long(active) * gridDim.x - 1) / (long(active) * gridDim.x));
+    const int worker0 = active * blockIdx.x, worker = worker0 + warp_in;
     long x = worker * share;
-    const long end = min(total, x + share);
-    if (lane == 0) A.begun[worker] = make_int4(-1, 0, 0, 0);
-    if (x >= end) return;
+    const long end = warp_in < active ? min(total, x + share) : x;
+    if (lane == 0) {
+        runs[1 + warp_in].x = -1;
+        if (warp_in == 0) runs[0].x = -1;
+    }
+    __syncthreads();
     int lo = 0;                                  // the run of sequences that x is in
     for (int step = 256; step; step /= 2)
         if (lo + step < kThreads && before[lo + step] <= x) lo += step;
     long at = before[lo];
-    int b = lo * run;
+    int b = min(lo * run, A.s.batch - 1);
     Seq sq = sequence<S>(A, b);
 
     // the warp's ring, and what a lane copies of a stage: 16 bytes of every 512 of the
@@ -245,9 +331,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
     while (x < end) {
         while (at + size_of<S>(A, sq) <= x) {
             at += size_of<S>(A, sq);
-            if (++b >= A.s.batch) return;        // (lengths that changed under the call)
+            if (++b >= A.s.batch) break;         // (lengths that changed under the call)
             sq = sequence<S>(A, b);
         }
+        if (b >= A.s.batch) break;
         const long rel = x - at;
         const int item = int(rel / sq.blocks), j0 = int(rel - long(item) * sq.blocks);
         const int j1 = int(min(long(sq.blocks), j0 + (end - x)));
@@ -258,8 +345,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
         const int base = sq.length - sq.new_;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
         const int kb0 = A.window ? max(0, first_pos - A.window + 1) / S::kKeys : 0;
-        const int kb_end = min(kb0 + j1, (last_pos + S::kKeys) / S::kKeys);
-        int kb = kb0 + j0, kb_in = kb;
+        const int kb_end = min(kb0 + j1 - S::kBegin, (last_pos + S::kKeys) / S::kKeys);
+        int kb = kb0 + max(0, j0 - S::kBegin), kb_in = kb;
 
         // ---- stages on their way: the pages of 32 places at a time in the lanes ----
         const int* table = A.s.table + size_t(b) * A.s.width;
@@ -619,9 +706,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
         // ---- the rows' states: out, or left for the join ----
         const bool whole = j0 == 0 && j1 == sq.blocks;
         const int slot = item_at <= worker * share ? 0 : 1;
-        if (!whole && j0 == 0 && lane == 0)
-            A.begun[worker] = make_int4(sq.first, tile | rows << 24, head | slot << 30, int(min(long(workers) - 1, (item_at + sq.blocks - 1) / share)));
-        if (__any_sync(kFull, broken)) l[0][0] = __int_as_float(0x7fffffff);
+        if (!whole && lane == 0) {
+            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, int((item_at + sq.blocks - 1) / share));
+            if (j0 == 0) runs[1 + warp_in] = info;
+            if (j0 > 0 && warp_in == 0) runs[0] = info;
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -655,48 +744,53 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A,
             }
         }
     }
+
+    // ---- tiles that several warps of the CTA share: their states in one, a warp per row ----
+    __syncthreads();
+    for (int u = warp_in; u < (active + 1) * S::kCols; u += S::kWarps) {
+        const int r = u / S::kCols, col = u - r * S::kCols;
+        const int4 info = runs[r];
+        const int mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col, last = min(info.w, worker0 + active - 1);
+        if (info.x < 0 || row >= info.y >> 24) continue;
+        const int w0 = worker0 + max(0, r - 1);
+        State<D> st;
+#pragma unroll 4
+        for (int w = w0; w <= last; ++w)
+            st.add(A.states + ((size_t(w) * 2 + (r && w == w0 ? info.z >> 30 & 1 : 0)) * S::kCols + col) * (D + 4));
+        if (r && info.w < worker0 + active)
+            st.write(A.out + row_of<S>(A, info, mine, row) * D);
+        else
+            st.keep(A.joined + ((size_t(blockIdx.x) * 2 + (r ? 1 : 0)) * S::kCols + col) * (D + 4));
+    }
+    if (threadIdx.x == 0) {
+        int4 going = make_int4(-1, 0, 0, 0);
+        for (int r = 1; r <= active; ++r)
+            if (runs[r].x >= 0 && runs[r].w >= worker0 + active) going = runs[r], going.w /= active;
+        going.w = min(going.w, int(gridDim.x) - 1);
+        A.begun[blockIdx.x] = going;
+    }
 }
 
-// Joins the states of a tile whose keys went to several workers: a block per row.
+// Joins the states of a tile whose keys went to several CTAs: a block per row.
 template <class S>
-__global__ void __launch_bounds__(kJoin) join_kernel(const Args A, int workers) {
-    constexpr int D = S::D, R = S::kRows, kVec = D / 32;
-    __shared__ float part[kJoin / 32][D + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
-    for (int w0 = blockIdx.x; w0 < workers; w0 += gridDim.x) {
-        const int4 x = A.begun[w0];
-        const int rows = x.y >> 24, tile = x.y & 0xffffff;
-        if (x.x < 0 || row >= rows) continue;
-        // (the first worker's state is its second, if it did not begin with the tile)
-        float m = kNone, l = 0.f, o[kVec] = {};
-        for (int w = w0 + warp; w <= x.w; w += kJoin / 32) {
-            const float* from = A.states + ((size_t(w) * 2 + (w == w0 ? x.z >> 30 & 1 : 0)) * S::kCols + col) * (D + 4);
-            const float mw = from[D], lw = from[D + 1], M = fmaxf(m, mw), f = ex2(m - M), fw = ex2(mw - M);
-            m = M;
-            l = l * f + lw * fw;
+__global__ void __launch_bounds__(kJoin) join_kernel(const Args A) {
+    constexpr int D = S::D;
+    __shared__ __align__(16) float part[kJoin / 32][D + 4];
+    wait_for_previous();
+    const int warp = threadIdx.x / 32, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
+    const int4 info = A.begun[blockIdx.x];
+    if (info.x < 0 || row >= info.y >> 24) return;
+    State<D> st;
+#pragma unroll 4
+    for (int c = blockIdx.x + warp; c <= info.w; c += kJoin / 32)
+        st.add(A.joined + ((size_t(c) * 2 + (c == blockIdx.x ? 1 : 0)) * S::kCols + col) * (D + 4));
+    st.keep(part[warp]);
+    __syncthreads();
+    if (warp) return;
+    State<D> all;
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) o[i] = o[i] * f + from[lane + 32 * i] * fw;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) part[warp][lane + 32 * i] = o[i];
-        if (lane == 0) part[warp][D] = m, part[warp][D + 1] = l;
-        __syncthreads();
-        const int head = (x.z & 0x3fffffff) + mine, r = tile * R + row, token = r / A.G;
-        __nv_bfloat16* to = A.out + ((size_t(x.x + token) * A.c.hkv + head) * A.G + r - token * A.G) * D;
-        for (int e = threadIdx.x; e < D; e += kJoin) {
-            float M = kNone, sum = 0.f, y = 0.f;
-#pragma unroll
-            for (int k = 0; k < kJoin / 32; ++k) M = fmaxf(M, part[k][D]);
-#pragma unroll
-            for (int k = 0; k < kJoin / 32; ++k) {
-                const float f = ex2(part[k][D] - M);
-                sum += part[k][D + 1] * f;
-                y += part[k][e] * f;
-            }
-            to[e] = __float2bfloat16_rn(sum == 0.f ? 0.f : y / sum);
-        }
-    }
+    for (int k = 0; k < kJoin / 32; ++k) all.add(part[k]);
+    all.write(A.out + row_of<S>(A, info, mine, row) * D);
 }
 
 template <class S>
@@ -708,18 +802,18 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
     if (e != cudaSuccess) return int(e);
-    const int workers = sms * S::kWarps;
-    const long states = long(workers) * 2 * S::kCols * (S::D + 4) * 4;
+    const long state = 2L * S::kCols * (S::D + 4) * 4, states = sms * S::kWarps * state, joined = sms * state;
     if (bytes) {
-        *bytes = states + long(workers) * 16;
+        *bytes = states + joined + sms * 16L;
         return 0;
     }
     Args A = a;
-    A.states = static_cast<float*>(scratch);
-    A.begun = reinterpret_cast<int4*>(static_cast<char*>(scratch) + states);
-    attention_kernel<S><<<sms, S::kThreads, S::kSmem, stream>>>(A, workers);
-    join_kernel<S><<<dim3(unsigned(sms), S::kCols), kJoin, 0, stream>>>(A, workers);
-    return int(cudaGetLastError());
+    char* at = static_cast<char*>(scratch);
+    A.states = reinterpret_cast<float*>(at);
+    A.joined = reinterpret_cast<float*>(at + states);
+    A.begun = reinterpret_cast<int4*>(at + states + joined);
+    const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
+    return rc ? rc : dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
 
 template <int D>
