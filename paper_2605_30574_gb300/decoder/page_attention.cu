@@ -44,7 +44,7 @@ using splice::tc::smem_u32;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
-constexpr int kMinKeys = 64;            // keys to a warp, at least
+constexpr int kMinKeys = 32;            // keys to a warp, at least
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
 
 // Every kernel is launched as a programmatic dependent of what precedes it on the stream:
@@ -200,50 +200,41 @@ __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-// Rows' states joined, a warp to a row: O for the reference m and the sum l, at D and D + 1.
+// Rows' states joined, 8 lanes to a row: O for the reference m and the sum l, at D and
+// D + 1.
 template <int D>
 struct State {
-    static constexpr int kVec = D / 32;
-    float m = kNone, l = 0.f, o[kVec] = {};
+    static constexpr int kVec = D / 32;         // by four elements
+    float m = kNone, l = 0.f;
+    float4 o[kVec] = {};
 
     __device__ __forceinline__ void add(const float* from) {
-        float y[kVec];
-        const int lane = threadIdx.x & 31;
-        if constexpr (kVec == 2) {
-            const float2 v = reinterpret_cast<const float2*>(from)[lane];
-            y[0] = v.x, y[1] = v.y;
-        } else {
+        const int lane = threadIdx.x & 7;
+        float4 y[kVec];
 #pragma unroll
-            for (int i = 0; i < kVec / 4; ++i) {
-                const float4 v = reinterpret_cast<const float4*>(from)[lane + 32 * i];
-                y[4 * i] = v.x, y[4 * i + 1] = v.y, y[4 * i + 2] = v.z, y[4 * i + 3] = v.w;
-            }
-        }
+        for (int i = 0; i < kVec; ++i) y[i] = reinterpret_cast<const float4*>(from)[lane + 8 * i];
         const float2 ml = *reinterpret_cast<const float2*>(from + D);
         const float M = fmaxf(m, ml.x), f = ex2(m - M), fy = ex2(ml.x - M);
         m = M;
         l = l * f + ml.y * fy;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) o[i] = o[i] * f + y[i] * fy;
+        for (int i = 0; i < kVec; ++i)
+            o[i] = make_float4(o[i].x * f + y[i].x * fy, o[i].y * f + y[i].y * fy, o[i].z * f + y[i].z * fy, o[i].w * f + y[i].w * fy);
     }
     __device__ __forceinline__ void keep(float* to) const {
-        const int lane = threadIdx.x & 31;
-        if constexpr (kVec == 2) reinterpret_cast<float2*>(to)[lane] = make_float2(o[0], o[1]);
-        if constexpr (kVec > 2)
+        const int lane = threadIdx.x & 7;
 #pragma unroll
-            for (int i = 0; i < kVec / 4; ++i)
-                reinterpret_cast<float4*>(to)[lane + 32 * i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int i = 0; i < kVec; ++i) reinterpret_cast<float4*>(to)[lane + 8 * i] = o[i];
         if (lane == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
     }
     __device__ __forceinline__ void write(__nv_bfloat16* to) const {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x & 7;
         const float f = l == 0.f ? 0.f : 1.f / l;
-        constexpr int kRun = kVec == 2 ? 2 : 4;
 #pragma unroll
-        for (int i = 0; i < kVec; i += kRun)
-#pragma unroll
-            for (int j = 0; j < kRun; j += 2)
-                *reinterpret_cast<__nv_bfloat162*>(to + 32 * i + kRun * lane + j) = __floats2bfloat162_rn(o[i + j] * f, o[i + j + 1] * f);
+        for (int i = 0; i < kVec; ++i) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(o[i].x * f, o[i].y * f), b = __floats2bfloat162_rn(o[i].z * f, o[i].w * f);
+            *reinterpret_cast<uint2*>(to + 4 * (lane + 8 * i)) = make_uint2(reinterpret_cast<const uint32_t&>(a), reinterpret_cast<const uint32_t&>(b));
+        }
     }
 };
 
@@ -282,12 +273,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     }
     const long total = before[kThreads];
     // few keys: four warps and more of as many CTAs as there are shares for
-    const long least = kMinKeys / S::kKeys;
-    const int active = int(max(long(kMinWarps), min(long(S::kWarps), (total + least * gridDim.x - 1) / (least * gridDim.x))));
-    const long share = max(least, (total + long(active) * gridDim.x - 1) / (long(active) * gridDim.x));
+    const long shares = max(1L, total / (kMinKeys / S::kKeys));
+    const int active = int(max(long(kMinWarps), min(long(S::kWarps), (shares + gridDim.x - 1) / gridDim.x)));
+    const long workers = min(shares, long(active) * gridDim.x);
     const int worker0 = active * blockIdx.x, worker = worker0 + warp_in;
-    long x = worker * share;
-    const long end = warp_in < active ? min(total, x + share) : x;
+    const bool works = warp_in < active && worker < workers;
+    const long begin = works ? total * worker / workers : 0, end = works ? total * (worker + 1) / workers : 0;
+    long x = begin;
     if (lane == 0) {
         runs[1 + warp_in].x = -1;
         if (warp_in == 0) runs[0].x = -1;
@@ -705,9 +697,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 
         // ---- the rows' states: out, or left for the join ----
         const bool whole = j0 == 0 && j1 == sq.blocks;
-        const int slot = item_at <= worker * share ? 0 : 1;
+        const int slot = item_at <= begin ? 0 : 1;
         if (!whole && lane == 0) {
-            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, int((item_at + sq.blocks - 1) / share));
+            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, int(((item_at + sq.blocks) * workers - 1) / total));
             if (j0 == 0) runs[1 + warp_in] = info;
             if (j0 > 0 && warp_in == 0) runs[0] = info;
         }
@@ -745,9 +737,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         }
     }
 
-    // ---- tiles that several warps of the CTA share: their states in one, a warp per row ----
+    // ---- tiles that several warps of the CTA share: their states in one, 8 lanes to a row ----
     __syncthreads();
-    for (int u = warp_in; u < (active + 1) * S::kCols; u += S::kWarps) {
+    for (int u = threadIdx.x / 8; u < (active + 1) * S::kCols; u += kThreads / 8) {
         const int r = u / S::kCols, col = u - r * S::kCols;
         const int4 info = runs[r];
         const int mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col, last = min(info.w, worker0 + active - 1);
@@ -774,22 +766,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 // Joins the states of a tile whose keys went to several CTAs: a block per row.
 template <class S>
 __global__ void __launch_bounds__(kJoin) join_kernel(const Args A) {
-    constexpr int D = S::D;
-    __shared__ __align__(16) float part[kJoin / 32][D + 4];
+    constexpr int D = S::D, kEach = kJoin / 8;
+    __shared__ __align__(16) float part[kEach][D + 4];
     wait_for_previous();
-    const int warp = threadIdx.x / 32, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
+    const int group = threadIdx.x / 8, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
     const int4 info = A.begun[blockIdx.x];
     if (info.x < 0 || row >= info.y >> 24) return;
     State<D> st;
-#pragma unroll 4
-    for (int c = blockIdx.x + warp; c <= info.w; c += kJoin / 32)
+#pragma unroll 2
+    for (int c = blockIdx.x + group; c <= info.w; c += kEach)
         st.add(A.joined + ((size_t(c) * 2 + (c == blockIdx.x ? 1 : 0)) * S::kCols + col) * (D + 4));
-    st.keep(part[warp]);
+    st.keep(part[group]);
     __syncthreads();
-    if (warp) return;
+    if (group) return;
     State<D> all;
-#pragma unroll
-    for (int k = 0; k < kJoin / 32; ++k) all.add(part[k]);
+    for (int k = 0; k < kEach && k <= info.w - int(blockIdx.x); ++k) all.add(part[k]);
     all.write(A.out + row_of<S>(A, info, mine, row) * D);
 }
 
