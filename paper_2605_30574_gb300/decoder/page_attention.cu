@@ -77,7 +77,7 @@ struct Args {
     __nv_bfloat16* out;
     int G, window;
     float scale;
-    float *states, *joined; // of warps and of CTAs: [each][2][columns][d + 4]
+    float *states, *joined; // of warps [each][columns][d + 4], and of CTAs [each][2][columns][d + 4]
     int4* begun;            // per CTA: the tile whose keys begin with it and go on
 };
 
@@ -98,7 +98,7 @@ struct Shape {
     static constexpr int kRest = 4 * kI + 4;                        // copies of 16 bytes that bring ratios and exponents
     static constexpr int kQ = P * NT * kI * 512;                    // q as operands
     static constexpr int kWarpBytes = kStages * kBytes + kQ, kSmem = kWarps * kWarpBytes;
-    static_assert(kSmem <= 224 * 1024);
+    static_assert(kSmem <= 224 * 1024 && kStages * kBytes >= kCols * (D + 4) * 4);
 };
 constexpr int kJoin = 128;              // threads of a CTA that joins states
 
@@ -165,6 +165,11 @@ __device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(x[4 * i]), "=r"(x[4 * i + 1]), "=r"(x[4 * i + 2]), "=r"(x[4 * i + 3])
                          : "r"(from + 16 * i));
+}
+
+// a / b, of numbers that rarely need 64 bits.
+__device__ __forceinline__ long quotient(long a, long b) {
+    return (a | b) >> 32 ? a / b : long(uint32_t(a) / uint32_t(b));
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
@@ -251,6 +256,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kThreads / 32];
+    __shared__ float* places[S::kWarps][2];     // states of tiles that go on here, and that go on behind this warp
     __shared__ int4 runs[S::kWarps + 1];        // tiles that warps share: the one that goes on here, and each warp's that goes on
     wait_for_previous();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
@@ -273,12 +279,17 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     }
     const long total = before[kThreads];
     // few keys: four warps and more of as many CTAs as there are shares for
-    const long shares = max(1L, total / (kMinKeys / S::kKeys));
-    const int active = int(max(long(kMinWarps), min(long(S::kWarps), (shares + gridDim.x - 1) / gridDim.x)));
+    const long shares = max(1L, quotient(total, kMinKeys / S::kKeys));
+    const int active = int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
     const long workers = min(shares, long(active) * gridDim.x);
     const int worker0 = active * blockIdx.x, worker = worker0 + warp_in;
     const bool works = warp_in < active && worker < workers;
-    const long begin = works ? total * worker / workers : 0, end = works ? total * (worker + 1) / workers : 0;
+    // (the first total % workers have one stage more)
+    const long each = quotient(total, workers), longer = total - each * workers;
+    const long begin = works ? each * worker + min(long(worker), longer) : 0, end = works ? begin + each + (worker < longer) : 0;
+    auto worker_of = [&](long at) {
+        return int(at < longer * (each + 1) ? quotient(at, each + 1) : longer + quotient(at - longer * (each + 1), max(1L, each)));
+    };
     long x = begin;
     if (lane == 0) {
         runs[1 + warp_in].x = -1;
@@ -328,7 +339,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         }
         if (b >= A.s.batch) break;
         const long rel = x - at;
-        const int item = int(rel / sq.blocks), j0 = int(rel - long(item) * sq.blocks);
+        const int item = int(quotient(rel, sq.blocks)), j0 = int(rel - long(item) * sq.blocks);
         const int j1 = int(min(long(sq.blocks), j0 + (end - x)));
         const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
         const long item_at = x - j0;
@@ -346,6 +357,19 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         int ids_at = place(kb);
         auto pages_from = [&](int i) { return i + lane < A.s.width ? __ldg(table + i + lane) : -1; };
         int ids = pages_from(ids_at), more = pages_from(ids_at + 32);
+        // (q on its way meanwhile: columns are a head's rows, 8 / P or 8 NT of them)
+        uint32_t raw[NT][kI][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = P == 2 ? g & 3 : 8 * n + g, r = tile * R + col, token = r / A.G;
+            const __nv_bfloat16* p = A.q + (sq.first + (col < rows ? token : 0)) * A.q_token +
+                                     ((head + (P == 2 ? g >> 2 : 0)) * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                const uint4 y = __ldg(reinterpret_cast<const uint4*>(p + 32 * i + 8 * t));
+                raw[n][i][0] = y.x, raw[n][i][1] = y.y, raw[n][i][2] = y.z, raw[n][i][3] = y.w;
+            }
+        }
         const uint8_t* codes = A.c.codes + size_t(page_rows) * head * (D / 2) + 16 * lane;
         const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the stage's second half)
         bool broken = false;                     // a page that is none of the cache's
@@ -409,17 +433,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         int pos[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int mine = P == 2 ? g >> 2 : 0, col = P == 2 ? g & 3 : 8 * n + g, r = tile * R + col, token = r / A.G;
-            const __nv_bfloat16* p = A.q + (sq.first + (col < rows ? token : 0)) * A.q_token +
-                                     ((head + mine) * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
-            uint32_t raw[kI][4], top2 = 0;
+            const int mine = P == 2 ? g >> 2 : 0;
+            uint32_t top2 = 0;
 #pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                const uint4 y = *reinterpret_cast<const uint4*>(p + 32 * i + 8 * t);
-                raw[i][0] = y.x, raw[i][1] = y.y, raw[i][2] = y.z, raw[i][3] = y.w;
+            for (int i = 0; i < kI; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) top2 = __vmaxu2(top2, raw[i][j] & 0x7fff7fffu);
-            }
+                for (int j = 0; j < 4; ++j) top2 = __vmaxu2(top2, raw[n][i][j] & 0x7fff7fffu);
             unsigned top = max(top2 & 0xffffu, top2 >> 16);
             top = max(top, __shfl_xor_sync(kFull, top, 1));
             top = max(top, __shfl_xor_sync(kFull, top, 2));
@@ -434,19 +453,19 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 float f[8], sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    f[j] = __uint_as_float(j & 1 ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
+                    f[j] = __uint_as_float(j & 1 ? raw[n][i][j / 2] & 0xffff0000u : raw[n][i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    raw[i][j] = half2_of(f[j], f[j + 4]);
-                    const float2 y = __half22float2(reinterpret_cast<const __half2&>(raw[i][j]));
+                    raw[n][i][j] = half2_of(f[j], f[j + 4]);
+                    const float2 y = __half22float2(reinterpret_cast<const __half2&>(raw[n][i][j]));
                     sum = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, sum);
                 }
                 // (a head's operand has zeros for the other's columns; a lane reads its own)
 #pragma unroll
                 for (int ph = 0; ph < P; ++ph) {
                     const bool zero = P == 2 && ph != mine;
-                    sts16(q_at + ((ph * NT + n) * kI + i) * 512, zero ? 0 : raw[i][0], zero ? 0 : raw[i][1], zero ? 0 : raw[i][2],
-                          zero ? 0 : raw[i][3]);
+                    sts16(q_at + ((ph * NT + n) * kI + i) * 512, zero ? 0 : raw[n][i][0], zero ? 0 : raw[n][i][1], zero ? 0 : raw[n][i][2],
+                          zero ? 0 : raw[n][i][3]);
                 }
                 sum += __shfl_xor_sync(kFull, sum, 1);
                 sum += __shfl_xor_sync(kFull, sum, 2);
@@ -698,8 +717,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         // ---- the rows' states: out, or left for the join ----
         const bool whole = j0 == 0 && j1 == sq.blocks;
         const int slot = item_at <= begin ? 0 : 1;
+        // (a warp's last state goes where its ring was)
+        float* const state = x >= end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
+                                      : A.states + size_t(worker) * S::kCols * (D + 4);
+        if (!whole && lane == 0) places[warp_in][slot] = state;
         if (!whole && lane == 0) {
-            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, int(((item_at + sq.blocks) * workers - 1) / total));
+            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, worker_of(item_at + sq.blocks - 1));
             if (j0 == 0) runs[1 + warp_in] = info;
             if (j0 > 0 && warp_in == 0) runs[0] = info;
         }
@@ -725,7 +748,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                             make_uint2(reinterpret_cast<const uint32_t&>(x0), reinterpret_cast<const uint32_t&>(x1));
                     }
                 } else {
-                    float* to = A.states + ((size_t(worker) * 2 + slot) * S::kCols + col) * (D + 4);
+                    float* to = state + col * (D + 4);
 #pragma unroll
                     for (int i = 0; i < kI; ++i)
                         *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
@@ -748,7 +771,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         State<D> st;
 #pragma unroll 4
         for (int w = w0; w <= last; ++w)
-            st.add(A.states + ((size_t(w) * 2 + (r && w == w0 ? info.z >> 30 & 1 : 0)) * S::kCols + col) * (D + 4));
+            st.add(places[w - worker0][r && w == w0 ? info.z >> 30 & 1 : 0] + col * (D + 4));
         if (r && info.w < worker0 + active)
             st.write(A.out + row_of<S>(A, info, mine, row) * D);
         else
@@ -793,7 +816,7 @@ int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
     if (e != cudaSuccess) return int(e);
-    const long state = 2L * S::kCols * (S::D + 4) * 4, states = sms * S::kWarps * state, joined = sms * state;
+    const long state = long(S::kCols) * (S::D + 4) * 4, states = sms * S::kWarps * state, joined = 2 * sms * state;
     if (bytes) {
         *bytes = states + joined + sms * 16L;
         return 0;
