@@ -210,11 +210,11 @@ def test_nan_that_is_seen(which):
 
 def test_pages_that_are_none_make_their_rows_nan():
     cache, (table, starts, lengths) = filled([40, 40, 40], [1, 2, 1], 2, 64, 16)
-    clean = P.page_attention(cache, 0, queries(4, 4, 64), table, starts, lengths)
+    want, bound = definition(cache, queries(4, 4, 64), table, starts, lengths, 1 / 8, 0)
     table[1, 1] = cache.pages
     lengths[2] = 16 * table.shape[1] + 1
     got = P.page_attention(cache, 0, queries(4, 4, 64), table, starts, lengths)
-    assert torch.equal(got[0], clean[0]) and bool(got[1:].isnan().all())
+    assert bool(((got[0].cpu().double() - want[0]).abs() <= bound[0]).all()) and bool(got[1:].isnan().all())
 
 
 @pytest.mark.parametrize("how", ["joined", "transposed", "unaligned", "negated"])
