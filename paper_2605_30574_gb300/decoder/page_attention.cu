@@ -47,28 +47,6 @@ constexpr float kNone = -1e30f;         // the reference of rows that have seen 
 constexpr int kMinKeys = 32;            // keys to a warp, at least
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
 
-// Every kernel is launched as a programmatic dependent of what precedes it on the stream:
-// set up while that still runs, it waits for all of it before it reads or writes.
-__device__ __forceinline__ void wait_for_previous() {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-
-template <class... Params, class... Given>
-int dependent(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, const Given&... given) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(unsigned(threads));
-    cfg.dynamicSmemBytes = size_t(smem);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return int(cudaLaunchKernelEx(&cfg, kernel, given...));
-}
-
 struct Args {
     PageLayer c;
     PageRows s;

@@ -13,11 +13,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr unsigned kFull = 0xffffffffu;
 
-// Where token `row` lies: its sequence b (starts[b] <= row < starts[b + 1]), or -1
-// behind the last.  32 places at a time: a look or two for a batch.
+// The sequence of token `row`, starts[b] <= row < starts[b + 1], one that has tokens: 32
+// places at a time, so a look or two for a batch.  row lies between the first start and
+// the last.
 __device__ int sequence_of(const PageRows& s, int row) {
     const int lane = threadIdx.x & 31;
-    if (row >= s.starts[s.batch] || row < s.starts[0]) return -1;
     int lo = 0, n = s.batch;                    // the sequence is one of lo .. lo + n - 1
     while (n > 1) {
         const int step = (n + 31) / 32, at = lo + lane * step;
@@ -29,10 +29,11 @@ __device__ int sequence_of(const PageRows& s, int row) {
     return lo;
 }
 
-// The token's page and slot.  -1: no place (a position before the first), -2: a page
-// that is none of the cache's.
+// The page and slot of a token.  Page -1: no place (a position before the first), -2: a
+// page that is none of the cache's, -3: nobody's token.
 __device__ __forceinline__ int place_of(const PageLayer& c, const PageRows& s, int b, int row, int* slot) {
-    const int first = s.starts[b], at = s.lengths[b] - (s.starts[b + 1] - first) + (row - first);
+    const int first = s.starts[b], last = s.starts[b + 1], at = s.lengths[b] - (last - first) + (row - first);
+    if (row < first || row >= last) return -3;
     if (at < 0) return -1;
     const int i = at >> c.log_page;
     if (i >= s.width) return -2;
@@ -41,15 +42,68 @@ __device__ __forceinline__ int place_of(const PageLayer& c, const PageRows& s, i
     return page < 0 || page >= c.pages ? -2 : page;
 }
 
+// The places of tokens row .. row + n - 1, in lanes 0 .. n - 1.
+__device__ __forceinline__ int places_of(const PageLayer& c, const PageRows& s, int row, int n, int* slot) {
+    const int lane = threadIdx.x & 31, mine = row + lane;
+    const int begin = s.starts[0], end = s.starts[s.batch];
+    if (row + n <= begin || row >= end) return -3;
+    int b = sequence_of(s, min(max(row, begin), end - 1));
+    if (n > 1) {
+        // the next 32 starts say how many sequences further (behind them a lane goes on by
+        // itself)
+        const int next = b + 1 + lane <= s.batch ? s.starts[b + 1 + lane] : 0x7fffffff;
+        int past = 0;
+#pragma unroll
+        for (int step = 16; step; step /= 2)
+            if (__shfl_sync(kFull, next, past + step - 1) <= mine) past += step;
+        b += past;
+        while (b < s.batch - 1 && s.starts[b + 1] <= mine) ++b;
+    }
+    return lane < n && b < s.batch ? place_of(c, s, b, mine, slot) : -3;
+}
+
 struct Rows {
     const __nv_bfloat16 *k, *v;     // (written by a load)
     long k_token, k_head, v_token, v_head;
 };
 
-// Eight elements of a row in each lane; D / 8 lanes to a row.
+// Eight elements of a row in each lane, D / 8 lanes to a row: where a lane's parts of
+// page 0 are, and what is from page to page.  (A page is below 2^27 bytes.)
 template <int D>
-__device__ __forceinline__ void quantise_and_store(const PageLayer& c, uint4 x, int kv, int page, int head, int slot) {
-    constexpr int kLanes = D / 8;
+struct Lane {
+    static constexpr int kLanes = D / 8, kI = D / 32;
+    uint8_t *codes, *ratios, *exponents;
+    uint32_t rows;                          // of a page: keys, or values
+
+    __device__ __forceinline__ Lane(const PageLayer& c, int kv, int head) {
+        const int w = threadIdx.x & (kLanes - 1), i = w >> 2, t = w & 3;
+        rows = uint32_t(c.hkv) << c.log_page;
+        const uint32_t row = (kv ? rows : 0) + (uint32_t(head) << c.log_page);
+        codes = c.codes + row * (D / 2) + (kv ? 4 * t * kI + 2 * i : 4 * (t * kI + i));     // (a value's first run)
+        ratios = c.ratios + row * kI + i;
+        exponents = c.exponents + ((uint32_t(head) << c.log_page) * 2 + kv);
+    }
+};
+
+// Where a lane's parts of a token are.
+template <int D>
+struct Place {
+    uint8_t *codes, *ratio, *exponent;
+    __device__ __forceinline__ Place(const Lane<D>& at, int page, int slot) {
+        const uint64_t n = uint64_t(uint32_t(page)) * at.rows;
+        codes = at.codes + n * D + slot * (D / 2);
+        ratio = at.ratios + n * (D / 16) + slot * (D / 32);
+        exponent = at.exponents + n * 2 + slot * 2;
+    }
+    // (of the token i places on, in the same page)
+    __device__ __forceinline__ uint8_t* codes_at(int i) const { return codes + i * (D / 2); }
+    __device__ __forceinline__ uint8_t* ratio_at(int i) const { return ratio + i * (D / 32); }
+    __device__ __forceinline__ uint8_t* exponent_at(int i) const { return exponent + i * 2; }
+};
+
+template <int D>
+__device__ __forceinline__ void quantise_and_store(const Place<D>& at, int n, uint4 x, int kv, bool out) {
+    constexpr int kLanes = D / 8, kI = D / 32;
     const int w = threadIdx.x & (kLanes - 1);
     const uint32_t raw[4] = {x.x, x.y, x.z, x.w};
     // magnitudes as whole numbers: infinities are above all numbers, and NaN above those
@@ -65,99 +119,135 @@ __device__ __forceinline__ void quantise_and_store(const PageLayer& c, uint4 x, 
     int E = most >> 7;
     const bool bad = E > kMostExponent, none = E < kLeastExponent;
     if (bad || none) E = kLeastExponent;
-    // r to four significant bits, ties to even: the quotient is either halfway, and
-    // then exact, or further than 2^-11 from it
-    float ratio = bad || none ? 0.f : __fdiv_rn(__uint_as_float(top << 16) * power_of(256 - E), 7.f);
-    uint32_t bits = __float_as_uint(fmaxf(ratio, 0x1p-14f));
+    // r to four significant bits, ties to even.  A quotient of 8 bits by 7 that is halfway
+    // between two of them has to be found as such; x (1 / 7) is within an ulp of it, and
+    // any other quotient 2^11 ulps away: so to multiples of 16 ulps first.
+    uint32_t bits = __float_as_uint(__uint_as_float(top << 16) * power_of(256 - E) * (1.f / 7.f));
+    bits = (bits + 8u) & ~15u;
     bits = (bits + 0x7ffffu + ((bits >> 20) & 1u)) & 0xfff00000u;
-    // x / s halfway between two codes has to be found as such, and x (1 / s) is within
-    // 2^-20 of it, while quotients of 8 by 4 bits that are not halfway are 2^-10 away:
-    // the first sum rounds to multiples of 2^-12, the second of 1
-    const float inv = __frcp_rn(__uint_as_float(bits) * power_of(E - 2));
-    uint32_t word = 0;
+    bits = bad || none ? 0x38800000u : max(bits, 0x38800000u);         // (at least 2^-14)
+    // Likewise x / s, halfway between two codes: x (1 / s) is within 2^-19 of it, while
+    // quotients of 8 by 4 bits that are not halfway are 2^-10 away: the first sum rounds to
+    // multiples of 2^-12, the second to whole numbers, which start at bit 0 of y.  They
+    // are 1 to 15 without a bound, as 7 (1 + 2^-4) rounds to 7.
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(bits) * power_of(E - 2)));
+    uint32_t word = 0u - 0x4b400000u * 0x11111111u;          // (what all the ys add but for their codes)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float v = __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
-        float y = __fadd_rn(fmaf(v, inv, 0x1.8p11f), 0x1.8p23f + 8.f - 0x1.8p11f);
-        y = fminf(fmaxf(y, 0x1.8p23f + 1.f), 0x1.8p23f + 15.f);
-        word |= (__float_as_uint(y) & 15u) << (4 * i);
+        word += __float_as_uint(__fadd_rn(fmaf(v, inv, 0x1.8p11f), 0x1.8p23f + 8.f - 0x1.8p11f)) << (4 * i);
     }
     if (bad || none) word = 0x88888888u;
     const int i = w >> 2, t = w & 3;
-    int at = t * (D / 32) + i;
+    uint8_t* to = at.codes_at(n);
     if (kv) {
-        // lanes of two groups trade their runs of four, so that each writes a word
+        // lanes of two groups trade their runs of four, so that each writes a word: run 2t
+        // of the even group and the next, and run 2t + 1
         const uint32_t got = __shfl_xor_sync(kFull, i & 1 ? word & 0xffffu : word >> 16, 4);
         word = i & 1 ? (word & 0xffff0000u) | got : (word & 0xffffu) | (got << 16);
-        at = (2 * t + (i & 1)) * (D / 64) + (i >> 1);
+        if (i & 1) to += 2 * kI - 2;
     }
-    if (page < 0) return;
-    const size_t row = page_row(c, page, kv, head, slot);
-    reinterpret_cast<uint32_t*>(c.codes + row * (D / 2))[at] = word;
-    if (t == 0) c.ratios[row * (D / 32) + i] = uint8_t((bits >> 20) - (112u << 3));
-    if (w == 0) c.exponents[exponent_row(c, page, head, slot) * 2 + kv] = uint8_t(bad ? kBadExponent : E);
+    if (!out) return;
+    *reinterpret_cast<uint32_t*>(to) = word;
+    if (t == 0) *at.ratio_at(n) = uint8_t((bits >> 20) - (112u << 3));
+    if (w == 0) *at.exponent_at(n) = uint8_t(bad ? kBadExponent : E);
 }
 
-template <int D>
-__device__ __forceinline__ uint4 loaded(const PageLayer& c, int kv, int page, int head, int slot) {
-    constexpr int kLanes = D / 8;
-    const int w = threadIdx.x & (kLanes - 1), i = w >> 2, t = w & 3;
-    if (page < 0) {
-        const uint32_t x = page == -1 ? 0u : 0x7fff7fffu;
-        return make_uint4(x, x, x, x);
-    }
-    const size_t row = page_row(c, page, kv, head, slot);
-    const uint8_t* codes = c.codes + row * (D / 2);
+// What eight elements are held as.
+struct Held {
     uint32_t word;
-    if (kv) {
-        const uint16_t* runs = reinterpret_cast<const uint16_t*>(codes);
-        word = runs[2 * t * (D / 32) + i] | uint32_t(runs[(2 * t + 1) * (D / 32) + i]) << 16;
-    } else {
-        word = reinterpret_cast<const uint32_t*>(codes)[t * (D / 32) + i];
-    }
-    const int E = c.exponents[exponent_row(c, page, head, slot) * 2 + kv];
-    const float ratio = __uint_as_float((uint32_t(c.ratios[row * (D / 32) + i]) + (112u << 3)) << 20);
-    const float s = E == kBadExponent ? __int_as_float(0x7fffffff) : ratio * power_of(E - 2);
-    uint32_t out[4];
+    uint8_t ratio, exponent;
+};
+
+template <int D>
+__device__ __forceinline__ Held read(const Place<D>& at, int n, int kv) {
+    Held x;
+    const uint8_t* codes = at.codes_at(n);
+    if (kv)
+        x.word = *reinterpret_cast<const uint16_t*>(codes) | uint32_t(*reinterpret_cast<const uint16_t*>(codes + 2 * (D / 32))) << 16;
+    else
+        x.word = *reinterpret_cast<const uint32_t*>(codes);
+    x.ratio = *at.ratio_at(n);
+    x.exponent = *at.exponent_at(n);
+    return x;
+}
+
+__device__ __forceinline__ uint4 values_of(const Held& x) {
+    // c as bf16 is (128 + n) - 136, and c s, of three bits by four, is exact
+    const uint32_t scale = x.exponent == kBadExponent ? 0x7fffu : (uint32_t(x.ratio) + (112u << 3) << 4) + uint32_t(x.exponent - 129) * 128u;
+    const uint32_t s2 = scale * 0x10001u, k136 = 0xc308c308u;
+    uint32_t pair[4], out[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        // (exact: three bits by four)
-        const float a = (float(word >> (8 * j) & 15u) - 8.f) * s, b = (float(word >> (8 * j + 4) & 15u) - 8.f) * s;
-        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-        out[j] = reinterpret_cast<const uint32_t&>(p);
+        // elements j and j + 4
+        const uint32_t n = ((x.word >> (4 * j)) & 0x000f000fu) | 0x43004300u;
+        const __nv_bfloat162 c = __hadd2(reinterpret_cast<const __nv_bfloat162&>(n), reinterpret_cast<const __nv_bfloat162&>(k136));
+        const __nv_bfloat162 y = __hmul2(c, reinterpret_cast<const __nv_bfloat162&>(s2));
+        pair[j] = reinterpret_cast<const uint32_t&>(y);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = __byte_perm(pair[2 * (j & 1)], pair[2 * (j & 1) + 1], j < 2 ? 0x5410 : 0x7632);
     return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// A warp takes a run of tokens and as many heads of K or of V as fill its lanes.
-template <int D, bool Store>
-__global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s, Rows x, int per_warp) {
+// A warp takes up to 32 tokens, whose places its lanes find at once, and as many heads of
+// K or of V as fill its lanes.  N rows are on their way together; the first of those to
+// store, before their places are known.
+template <int D, bool Store, int N>
+__global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s, Rows x, int per_warp, unsigned kinds) {
+    wait_for_previous();
     constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
-    const int slices = (c.hkv + kHeads - 1) / kHeads;
-    const long warp = (long(blockIdx.x) * kThreads + threadIdx.x) / 32;
-    const int kind = int(warp % (2 * slices)), kv = kind / slices;
-    const int head = (kind - kv * slices) * kHeads + (threadIdx.x & 31) / kLanes, w = threadIdx.x & (kLanes - 1);
-    const long first = warp / (2 * slices) * per_warp;
+    const unsigned group = blockIdx.x / kinds, kind = blockIdx.x - group * kinds;
+    const int kv = kind >= kinds / 2, lane = threadIdx.x & 31, head = int(kind - kv * (kinds / 2)) * kHeads + lane / kLanes;
+    const long first = (long(group) * (kThreads / 32) + threadIdx.x / 32) * per_warp;
     if (first >= s.rows) return;
-    const int last = int(min(long(s.rows), first + per_warp));
+    const int n = int(min(long(per_warp), s.rows - first));
     const bool mine = head < c.hkv;
     const long token = kv ? x.v_token : x.k_token;
-    const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + 8 * w;
-    int b = sequence_of(s, int(first));
-    for (int row = int(first); row < last; ++row) {
-        uint4 data = {};
-        const bool out = b < 0;
-        if (Store && mine) data = *reinterpret_cast<const uint4*>(p + row * token);
-        if (out) return;
-        while (b < s.batch && s.starts[b + 1] <= row) ++b;
-        if (b >= s.batch) return;
-        int slot = 0, page = place_of(c, s, b, row, &slot);
-        if (Store) {
-            quantise_and_store<D>(c, data, kv, mine ? page : -1, head, slot);
-        } else if (mine) {
-            data = loaded<D>(c, kv, page, head, slot);
-            *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + row * token) = data;
+    const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + 8 * (lane & (kLanes - 1)) + first * token;
+    const Lane<D> at(c, kv, mine ? head : 0);
+    uint4 data[N];
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) data[i] = *reinterpret_cast<const uint4*>(p + min(from + i, n - 1) * token);
+    };
+    if (Store) fetch(0);
+    int slot = 0;
+    const int page = places_of(c, s, int(first), n, &slot);
+    for (int from = 0; from < n; from += N) {
+        // rows of one page, one behind the other, are a constant apart
+        const int page0 = __shfl_sync(kFull, page, from), slot0 = __shfl_sync(kFull, slot, from);
+        const bool run = N > 1 && __all_sync(kFull, lane < from || lane >= from + N || (page == page0 && slot == slot0 + lane - from)) &&
+                         page0 >= 0;
+        const Place<D> first_at(at, max(page0, 0), page0 < 0 ? 0 : slot0);
+        if (run) {
+            if (Store) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) quantise_and_store<D>(first_at, i, data[i], kv, mine);
+            } else {
+                Held held[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) held[i] = read<D>(first_at, i, kv);
+                if (mine)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) = values_of(held[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int to = __shfl_sync(kFull, page, (from + i) & 31), in = __shfl_sync(kFull, slot, (from + i) & 31);
+                const Place<D> place(at, max(to, 0), to < 0 ? 0 : in);
+                if (Store) {
+                    quantise_and_store<D>(place, 0, data[i], kv, mine && to >= 0);
+                } else if (mine && to > -3) {
+                    const uint32_t none = to == -1 ? 0u : 0x7fff7fffu;
+                    *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) =
+                        to < 0 ? make_uint4(none, none, none, none) : values_of(read<D>(place, 0, kv));
+                }
+            }
         }
+        if (Store && from + N < n) fetch(from + N);
     }
 }
 
@@ -174,6 +264,7 @@ struct Part {
 };
 
 __global__ void __launch_bounds__(kThreads) copy_kernel(Part a, Part b, Part e, int pages, const __grid_constant__ Copies copies) {
+    wait_for_previous();
     const int src = copies.src[blockIdx.x], dst = copies.dst[blockIdx.x];
     const Part parts[3] = {a, b, e};
 #pragma unroll
@@ -190,13 +281,16 @@ template <bool Store>
 int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream_t stream) {
     const int heads = 32 / (d / 8);
     const long kinds = 2L * ((c.hkv + heads - 1) / heads);
-    const int per_warp = 1;
-    const long warps = (s.rows + per_warp - 1) / per_warp * kinds;
-    const long blocks = (warps * 32 + kThreads - 1) / kThreads;
+    // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
+    // shortest chain of loads.
+    const int per_warp = s.rows / 32 * kinds >= 152 * 32 ? 32 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
+    const long blocks = (s.rows + 8L * per_warp - 1) / (8L * per_warp) * kinds;
     if (blocks >= 1L << 31) return int(cudaErrorInvalidValue);
-    const auto kernel = d == 64 ? rows_kernel<64, Store> : d == 128 ? rows_kernel<128, Store> : rows_kernel<256, Store>;
-    kernel<<<unsigned(blocks), kThreads, 0, stream>>>(c, s, x, per_warp);
-    return int(cudaGetLastError());
+    const bool many = per_warp > 1;
+    const auto kernel = d == 64    ? (many ? rows_kernel<64, Store, 8> : rows_kernel<64, Store, 1>)
+                        : d == 128 ? (many ? rows_kernel<128, Store, 8> : rows_kernel<128, Store, 1>)
+                                   : (many ? rows_kernel<256, Store, 8> : rows_kernel<256, Store, 1>);
+    return dependent(kernel, dim3(unsigned(blocks)), kThreads, 0, stream, c, s, x, per_warp, unsigned(kinds));
 }
 
 bool takes(int pages, int hkv, int d, int log_page, int width, int batch, int rows) {
@@ -236,8 +330,7 @@ extern "C" int decoder_page_copy(void* codes, void* ratios, void* exponents, int
             copies.dst[i] = dst[at + i];
             if (src[at + i] < 0 || src[at + i] >= pages || dst[at + i] < 0 || dst[at + i] >= pages) return int(cudaErrorInvalidValue);
         }
-        copy_kernel<<<dim3(unsigned(m), unsigned(layers)), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, b, e, pages, copies);
-        const int rc = int(cudaGetLastError());
+        const int rc = dependent(copy_kernel, dim3(unsigned(m), unsigned(layers)), kThreads, 0, static_cast<cudaStream_t>(stream), a, b, e, pages, copies);
         if (rc) return rc;
     }
     return 0;

@@ -40,15 +40,29 @@ constexpr int kBadExponent = 255;       // a row of NaN
 constexpr int kLeastExponent = 27;      // 2^-100, biased
 constexpr int kMostExponent = 226;
 
-__device__ __forceinline__ size_t page_row(const PageLayer& c, int page, int kv, int head, int slot) {
-    return ((((size_t(page) * 2 + kv) * c.hkv + head) << c.log_page) + slot);
-}
-
-__device__ __forceinline__ size_t exponent_row(const PageLayer& c, int page, int head, int slot) {
-    return ((size_t(page) * c.hkv + head) << c.log_page) + slot;
-}
-
 // 2^(biased - 127).
 __device__ __forceinline__ float power_of(int biased) { return __int_as_float(biased << 23); }
+
+// Every kernel is launched as a programmatic dependent of what precedes it on the stream:
+// set up while that still runs, it waits for all of it before it reads or writes.
+__device__ __forceinline__ void wait_for_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <class... Params, class... Given>
+inline int dependent(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, const Given&... given) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return int(cudaLaunchKernelEx(&cfg, kernel, given...));
+}
 
 }  // namespace decoder
