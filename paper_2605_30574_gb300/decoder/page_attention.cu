@@ -29,6 +29,7 @@
 // them in the warps' order: the same inputs give the same bits.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "../csrc/per_device.h"
@@ -785,43 +786,42 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const Args A) {
     all.write(A.out + row_of<S>(A, info, mine, row) * D);
 }
 
+// The current device's multiprocessors, with the kernels' shared memory allowed.
 template <class S>
-int launch(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
+cudaError_t prepared(int* sms) {
     static splice::PerDevice<int> counts;
-    int sms = 0;
-    const cudaError_t e = counts.get(&sms, [](int dev, int* n) {
+    return counts.get(sms, [](int dev, int* n) {
         const cudaError_t e = cudaFuncSetAttribute(attention_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
+}
+
+template <class S>
+constexpr long scratch_of(int sms) { return sms * ((S::kWarps + 2L) * S::kCols * (S::D + 4) * 4 + 16); }
+
+template <class S>
+int launch(const Args& a, void* scratch, cudaStream_t stream) {
+    int sms = 0;
+    const cudaError_t e = prepared<S>(&sms);
     if (e != cudaSuccess) return int(e);
-    const long state = long(S::kCols) * (S::D + 4) * 4, states = sms * S::kWarps * state, joined = 2 * sms * state;
-    if (bytes) {
-        *bytes = states + joined + sms * 16L;
-        return 0;
-    }
     Args A = a;
-    char* at = static_cast<char*>(scratch);
-    A.states = reinterpret_cast<float*>(at);
-    A.joined = reinterpret_cast<float*>(at + states);
-    A.begun = reinterpret_cast<int4*>(at + states + joined);
+    A.states = static_cast<float*>(scratch);
+    A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
+    A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
     const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
     return rc ? rc : dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
 
 template <int D>
-int run(const Args& a, void* scratch, cudaStream_t stream, long* bytes) {
+int run(const Args& a, void* scratch, cudaStream_t stream) {
     // By the rows of a kv head that a sequence has on average: up to four share the
     // columns with those of the next head, more than eight take sixteen columns (the
     // codes are made operands once for both halves).
     const long rows = long(a.s.rows) * a.G, all = a.s.batch;
-    if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream, bytes);
+    if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream);
     if constexpr (D < 256)
-        if (rows > 8 * all) return launch<Shape<D, 2, 1>>(a, scratch, stream, bytes);
-    return launch<Shape<D, 1, 1>>(a, scratch, stream, bytes);
-}
-
-int run(const Args& a, int d, void* scratch, cudaStream_t stream, long* bytes) {
-    return d == 64 ? run<64>(a, scratch, stream, bytes) : d == 128 ? run<128>(a, scratch, stream, bytes) : run<256>(a, scratch, stream, bytes);
+        if (rows > 8 * all) return launch<Shape<D, 2, 1>>(a, scratch, stream);
+    return launch<Shape<D, 1, 1>>(a, scratch, stream);
 }
 
 }  // namespace
@@ -829,31 +829,32 @@ int run(const Args& a, int d, void* scratch, cudaStream_t stream, long* bytes) {
 
 using namespace decoder;
 
-// Bytes of scratch of a call with these numbers, 0 for those that it does not take;
-// below 0: a CUDA error, negated.
-extern "C" long decoder_page_attention_scratch(int batch, int rows, int hq, int hkv, int d) {
-    if (batch < 1 || rows < 1 || hkv < 1 || hq < 1 || hq % hkv || (d != 64 && d != 128 && d != 256) || long(rows) * hq >= 1L << 26) return 0;
-    Args a = {};
-    a.s.batch = batch, a.s.rows = rows, a.G = hq / hkv, a.c.hkv = hkv;
-    long bytes = 0;
-    const int rc = run(a, d, nullptr, nullptr, &bytes);
-    return rc ? -rc : bytes;
+// Bytes of scratch of any call for heads of d on the current device; below 0: a CUDA
+// error, negated.
+extern "C" long decoder_page_attention_scratch(int d) {
+    if (d != 64 && d != 128 && d != 256) return -long(cudaErrorInvalidValue);
+    int sms = 0;
+    const cudaError_t e = prepared<Shape<64, 1, 1>>(&sms);
+    if (e != cudaSuccess) return -long(e);
+    return d == 64    ? std::max(scratch_of<Shape<64, 2, 1>>(sms), scratch_of<Shape<64, 1, 1>>(sms))
+           : d == 128 ? std::max(scratch_of<Shape<128, 2, 1>>(sms), scratch_of<Shape<128, 1, 1>>(sms))
+                      : scratch_of<Shape<256, 1, 1>>(sms);
 }
 
 // q [rows][hq][d] (its strides: token, head) over the layer's pages; out [rows][hq][d].
-extern "C" int decoder_page_attention(const void* codes, const void* ratios, const void* exponents, int pages, int hkv, int d, int log_page,
-                                      const void* q, const long* strides, const void* table, const void* starts, const void* lengths,
-                                      int width, int batch, int rows, int hq, float scale, int window, void* out, void* scratch,
-                                      void* stream) {
-    if (pages < 1 || log_page < 4 || log_page > 8 || width < 1 || window < 0 || decoder_page_attention_scratch(batch, rows, hq, hkv, d) <= 0)
+extern "C" int decoder_page_attention(const PageCache* cache, int layer, const void* q, long q_token, long q_head, const void* table,
+                                      const void* starts, const void* lengths, int width, int batch, int rows, int hq, float scale, int window,
+                                      void* out, void* scratch, void* stream) {
+    if (!cache->valid() || layer < 0 || layer >= cache->layers || width < 1 || batch < 1 || rows < 1 || hq < 1 || hq % cache->hkv ||
+        window < 0 || long(rows) * hq >= 1L << 26)
         return int(cudaErrorInvalidValue);
-    const auto bytes = [](const void* p) { return const_cast<uint8_t*>(static_cast<const uint8_t*>(p)); };
     Args a = {};
-    a.c = {bytes(codes), bytes(ratios), bytes(exponents), pages, hkv, log_page};
+    a.c = cache->layer(layer);
     a.s = {static_cast<const int*>(table), static_cast<const int*>(starts), static_cast<const int*>(lengths), width, batch, rows};
     a.q = static_cast<const __nv_bfloat16*>(q);
-    a.q_token = strides[0], a.q_head = strides[1];
+    a.q_token = q_token, a.q_head = q_head;
     a.out = static_cast<__nv_bfloat16*>(out);
-    a.G = hq / hkv, a.window = window, a.scale = scale;
-    return run(a, d, scratch, static_cast<cudaStream_t>(stream), nullptr);
+    a.G = hq / cache->hkv, a.window = window, a.scale = scale;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return cache->d == 64 ? run<64>(a, scratch, s) : cache->d == 128 ? run<128>(a, scratch, s) : run<256>(a, scratch, s);
 }

@@ -283,7 +283,7 @@ int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream
     const long kinds = 2L * ((c.hkv + heads - 1) / heads);
     // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
     // shortest chain of loads.
-    const int per_warp = s.rows / 32 * kinds >= 152 * 32 ? 32 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
+    const int per_warp = s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
     const long blocks = (s.rows + 8L * per_warp - 1) / (8L * per_warp) * kinds;
     if (blocks >= 1L << 31) return int(cudaErrorInvalidValue);
     const bool many = per_warp > 1;
@@ -293,11 +293,6 @@ int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream
     return dependent(kernel, dim3(unsigned(blocks)), kThreads, 0, stream, c, s, x, per_warp, unsigned(kinds));
 }
 
-bool takes(int pages, int hkv, int d, int log_page, int width, int batch, int rows) {
-    return pages >= 1 && hkv >= 1 && hkv <= 1024 && (d == 64 || d == 128 || d == 256) && log_page >= 4 && log_page <= 8 && width >= 1 &&
-           batch >= 1 && rows >= 1;
-}
-
 }  // namespace
 }  // namespace decoder
 
@@ -305,32 +300,30 @@ using namespace decoder;
 
 // Rows k, v [rows][hkv][d] (strides: token and head of k, then of v) into the layer's
 // pages (out 0), or out of them (out 1).
-extern "C" int decoder_page_rows(int out, void* codes, void* ratios, void* exponents, int pages, int hkv, int d, int log_page,
-                                 const void* k, const void* v, const long* strides, const void* table, const void* starts,
-                                 const void* lengths, int width, int batch, int rows_, void* stream) {
-    if (!takes(pages, hkv, d, log_page, width, batch, rows_)) return int(cudaErrorInvalidValue);
-    const PageLayer c = {static_cast<uint8_t*>(codes), static_cast<uint8_t*>(ratios), static_cast<uint8_t*>(exponents), pages, hkv, log_page};
+extern "C" int decoder_page_rows(int out, const PageCache* cache, int layer, const void* k, const void* v, long k_token, long k_head,
+                                 long v_token, long v_head, const void* table, const void* starts, const void* lengths, int width, int batch,
+                                 int rows_, void* stream) {
+    if (!cache->valid() || layer < 0 || layer >= cache->layers || width < 1 || batch < 1 || rows_ < 1) return int(cudaErrorInvalidValue);
+    const PageLayer c = cache->layer(layer);
     const PageRows s = {static_cast<const int*>(table), static_cast<const int*>(starts), static_cast<const int*>(lengths), width, batch, rows_};
-    const Rows x = {static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), strides[0], strides[1], strides[2], strides[3]};
-    return out ? rows<false>(c, s, x, d, static_cast<cudaStream_t>(stream)) : rows<true>(c, s, x, d, static_cast<cudaStream_t>(stream));
+    const Rows x = {static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), k_token, k_head, v_token, v_head};
+    return out ? rows<false>(c, s, x, cache->d, static_cast<cudaStream_t>(stream))
+               : rows<true>(c, s, x, cache->d, static_cast<cudaStream_t>(stream));
 }
 
 // Pages src[i] to dst[i] of all layers; no dst is another's, or a src.
-extern "C" int decoder_page_copy(void* codes, void* ratios, void* exponents, int layers, int pages, int hkv, int d, int log_page,
-                                 const int* src, const int* dst, int n, void* stream) {
-    if (!takes(pages, hkv, d, log_page, 1, 1, 1) || layers < 1 || layers > 65535 || n < 0) return int(cudaErrorInvalidValue);
-    const unsigned rows = unsigned(hkv) << log_page;        // of keys, and as many of values
-    const Part a = {static_cast<uint8_t*>(codes), rows * unsigned(d)}, b = {static_cast<uint8_t*>(ratios), rows * unsigned(d / 16)},
-               e = {static_cast<uint8_t*>(exponents), rows * 2};
+extern "C" int decoder_page_copy(const PageCache* cache, const int* src, const int* dst, int n, void* stream) {
+    if (!cache->valid() || cache->layers > 65535 || n < 0) return int(cudaErrorInvalidValue);
+    for (int i = 0; i < n; ++i)
+        if (src[i] < 0 || src[i] >= cache->pages || dst[i] < 0 || dst[i] >= cache->pages) return int(cudaErrorInvalidValue);
+    const unsigned rows = unsigned(cache->hkv) << cache->log_page, d = unsigned(cache->d);      // (rows of keys, and as many of values)
+    const Part a = {cache->codes, rows * d}, b = {cache->ratios, rows * (d / 16)}, e = {cache->exponents, rows * 2};
     for (int at = 0; at < n; at += kPairs) {
         const int m = n - at < kPairs ? n - at : kPairs;
         Copies copies;
-        for (int i = 0; i < m; ++i) {
-            copies.src[i] = src[at + i];
-            copies.dst[i] = dst[at + i];
-            if (src[at + i] < 0 || src[at + i] >= pages || dst[at + i] < 0 || dst[at + i] >= pages) return int(cudaErrorInvalidValue);
-        }
-        const int rc = dependent(copy_kernel, dim3(unsigned(m), unsigned(layers)), kThreads, 0, static_cast<cudaStream_t>(stream), a, b, e, pages, copies);
+        for (int i = 0; i < m; ++i) copies.src[i] = src[at + i], copies.dst[i] = dst[at + i];
+        const int rc = dependent(copy_kernel, dim3(unsigned(m), unsigned(cache->layers)), kThreads, 0, static_cast<cudaStream_t>(stream), a, b, e,
+                                 cache->pages, copies);
         if (rc) return rc;
     }
     return 0;

@@ -29,6 +29,20 @@ struct PageLayer {
     int pages, hkv, log_page;
 };
 
+// A cache as its owner describes it, once for all calls.
+struct PageCache {
+    uint8_t *codes, *ratios, *exponents;
+    int layers, pages, hkv, d, log_page;
+
+    bool valid() const {
+        return layers >= 1 && pages >= 1 && hkv >= 1 && hkv <= 1024 && (d == 64 || d == 128 || d == 256) && log_page >= 4 && log_page <= 8;
+    }
+    PageLayer layer(int i) const {
+        const size_t rows = (size_t(pages) * hkv << log_page) * size_t(i);       // (of keys, or values, of the layers before)
+        return {codes + rows * d, ratios + rows * (d / 16), exponents + rows * 2, pages, hkv, log_page};
+    }
+};
+
 // Sequences: their newest tokens are rows starts[b] to starts[b + 1] of what is
 // stored, loaded or attends, and end at lengths[b]; their pages are table[b].
 struct PageRows {

@@ -39,7 +39,12 @@ from . import BF16, _current_device, _launch, lib, there, untraced
 
 _PAGES = {16: 4, 32: 5, 64: 6, 128: 7, 256: 8}
 _U8, _I32 = torch.uint8, torch.int32
-_LONGS2, _LONGS4 = ctypes.c_long * 2, ctypes.c_long * 4
+
+
+class _Described(ctypes.Structure):
+    """A cache as the kernels' launches take it."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("codes", "ratios", "exponents")] + [
+        (n, ctypes.c_int) for n in ("layers", "pages", "heads", "head_dim", "log_page")]
 
 
 class PageCache:
@@ -69,11 +74,19 @@ class PageCache:
             raise ValueError(f"{what}: between 1 and 1024 heads, 1 and 65535 layers, and a page at least")
         if ratios.shape != (layers, pages, 2, heads, page, half // 16) or exponents.shape != (layers, pages, heads, page, 2):
             raise ValueError(f"{what}: ratios and exponents must be of the codes' sizes")
-        self.codes, self.ratios, self.exponents = codes, ratios, exponents
-        self.layers, self.pages, self.kv_heads, self.page, self.head_dim = layers, pages, heads, page, 2 * half
-        self.device = codes.device
-        self._sizes = (pages, heads, 2 * half, _PAGES[page])
-        self._strides = (codes.stride(0), ratios.stride(0), exponents.stride(0))
+        self._hold(codes, ratios, exponents)
+        with torch.cuda.device(codes.device):
+            self._scratch = lib().decoder_page_attention_scratch(2 * half)
+        if self._scratch < 0:
+            raise RuntimeError(f"{what}: CUDA error {-self._scratch}")
+
+    def _hold(self, codes, ratios, exponents):
+        self.codes, self.ratios, self.exponents, self.device = codes, ratios, exponents, codes.device
+        self.layers, self.pages, _, self.kv_heads, self.page, half = codes.shape
+        self.head_dim = 2 * half
+        self._described = _Described(codes.data_ptr(), ratios.data_ptr(), exponents.data_ptr(), self.layers, self.pages, self.kv_heads,
+                                     self.head_dim, _PAGES[self.page])
+        self._at = ctypes.addressof(self._described)
 
     @classmethod
     def empty(cls, layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> "PageCache":
@@ -88,19 +101,29 @@ class PageCache:
     def nbytes(self) -> int:
         return sum(t.numel() for t in (self.codes, self.ratios, self.exponents))
 
-    def _layer(self, what: str, layer: int) -> Tuple[int, int, int]:
+    def _layer(self, what: str, layer: int) -> int:
+        """The address of the cache's description, for a layer that there is."""
         if not isinstance(layer, int) or not 0 <= layer < self.layers:
             raise ValueError(f"{what}: the cache has layers 0 to {self.layers - 1}")
-        ptrs = (self.codes.data_ptr(), self.ratios.data_ptr(), self.exponents.data_ptr())
-        if not all(ptrs):
+        if not (self.codes.data_ptr() and self.ratios.data_ptr() and self.exponents.data_ptr()):
             raise ValueError(f"{what}: the cache has no memory")
-        return tuple(p + layer * s for p, s in zip(ptrs, self._strides))
+        return self._at
 
 
 def _where(what, cache, table, starts, lengths):
     """The three, as addresses, with the table's width and the sequences."""
     if not isinstance(cache, PageCache):
         raise TypeError(f"{what}: cache must be a PageCache")
+    try:
+        device, (B, W) = cache.device, table.shape
+        if (table.dtype is starts.dtype is lengths.dtype is _I32 and table.device == device == starts.device and lengths.device == device
+                and starts.shape == (B + 1,) and lengths.shape == (B,) and table.is_contiguous() and starts.is_contiguous()
+                and lengths.is_contiguous() and not (table.is_neg() or starts.is_neg() or lengths.is_neg())):
+            at = (table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), W, B)
+            if at[0] and at[1] and at[2] and W:
+                return at
+    except (AttributeError, ValueError):
+        pass
     for name, t, dims in (("table", table, 2), ("starts", starts, 1), ("lengths", lengths, 1)):
         if not isinstance(t, torch.Tensor) or t.dtype is not _I32:
             raise TypeError(f"{what}: {name} must be an int32 tensor")
@@ -118,6 +141,8 @@ def _where(what, cache, table, starts, lengths):
 
 
 def _bf16(what, name, t, cache, shape):
+    if isinstance(t, torch.Tensor) and t.dtype is BF16 and t.shape == shape and t.device == cache.device and t.data_ptr():
+        return t
     if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
         raise TypeError(f"{what}: {name} must be a bf16 tensor")
     if t.device != cache.device:
@@ -130,7 +155,7 @@ def _bf16(what, name, t, cache, shape):
 def _reads(t):
     """Whether the kernels can read the tensor where it is."""
     token, head, one = t.stride()
-    return one == 1 and not (token | head | t.data_ptr() >> 1) & 7 and not t.is_neg() and max(token, head) < 1 << 38
+    return one == 1 and not (token | head | t.data_ptr() >> 1) & 7 and not t.is_neg() and token < 1 << 38 and head < 1 << 38
 
 
 def _readable(t):
@@ -154,7 +179,7 @@ def _target(what, name, t):
         raise ValueError(f"{what}: {name} requires a gradient and is written to")
     if t.is_inference() and not torch.is_inference_mode_enabled():
         raise ValueError(f"{what}: {name} is an inference tensor and is written to")
-    if t.numel() and _overlaps(t):
+    if not t.is_contiguous() and t.numel() and _overlaps(t):
         raise ValueError(f"{what}: rows of {name} overlap")
 
 
@@ -181,8 +206,7 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
         with torch.cuda.device(cache.device):
             return store_pages(cache, layer, k, v, table, starts, lengths)
     k, v = _readable(k), _readable(v)
-    _launch("decoder_page_rows", 0, *at, *cache._sizes, k.data_ptr(), v.data_ptr(), _LONGS4(*k.stride()[:2], *v.stride()[:2]),
-            *where, rows)
+    _launch("decoder_page_rows", 0, at, layer, k.data_ptr(), v.data_ptr(), *k.stride()[:2], *v.stride()[:2], *where, rows)
 
 
 def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
@@ -209,8 +233,7 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
             return load_pages(cache, layer, k, v, table, starts, lengths)
     # (what the kernels cannot write to gets its rows by way of a copy)
     to, tv = _readable(k), _readable(v)
-    _launch("decoder_page_rows", 1, *at, *cache._sizes, to.data_ptr(), tv.data_ptr(), _LONGS4(*to.stride()[:2], *tv.stride()[:2]),
-            *where, rows)
+    _launch("decoder_page_rows", 1, at, layer, to.data_ptr(), tv.data_ptr(), *to.stride()[:2], *tv.stride()[:2], *where, rows)
     for a, b in ((k, to), (v, tv)):
         if a is b:
             _written(a)
@@ -236,8 +259,10 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     what = "page_attention"
     untraced(what)
     where = _where(what, cache, table, starts, lengths)
-    _bf16(what, "q", q, cache, None)
+    _bf16(what, "q", q, cache, (*q.shape[:-1], cache.head_dim) if isinstance(q, torch.Tensor) and q.dim() == 3 else None)
     rows, hq, d = q.shape
+    if rows * hq >= 1 << 26:
+        raise ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
     if hq == 0 or hq % cache.kv_heads:
         raise ValueError(f"{what}: the query heads must be a multiple of the cache's {cache.kv_heads}")
     if not isinstance(window, int) or not 0 <= window < 1 << 31:
@@ -255,13 +280,10 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     y = torch.empty(q.shape, dtype=BF16, device=q.device) if out is None else out
     if not rows or not where[-1]:
         return y
-    size = lib().decoder_page_attention_scratch(where[-1], rows, hq, cache.kv_heads, d)
-    if size <= 0:
-        raise RuntimeError(f"{what}: CUDA error {-size}") if size else ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
     q = _readable(q)
-    scratch = torch.empty(size, dtype=_U8, device=q.device)
-    _launch("decoder_page_attention", *at, *cache._sizes, q.data_ptr(), _LONGS2(*q.stride()[:2]), *where, rows, hq, scale, window,
-            y.data_ptr(), scratch.data_ptr())
+    scratch = torch.empty(cache._scratch, dtype=_U8, device=q.device)
+    _launch("decoder_page_attention", at, layer, q.data_ptr(), *q.stride()[:2], *where, rows, hq, scale, window, y.data_ptr(),
+            scratch.data_ptr())
     if out is not None:
         _written(out)
     return y
@@ -292,4 +314,4 @@ def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None
     if cache.device.index != _current_device():
         with torch.cuda.device(cache.device):
             return copy_pages(cache, src, dst)
-    _launch("decoder_page_copy", *at, cache.layers, *cache._sizes, *ints, n)
+    _launch("decoder_page_copy", at, *ints, n)

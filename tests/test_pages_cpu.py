@@ -16,12 +16,8 @@ class OnCpu(P.PageCache):
 
     def __init__(self, layers=2, pages=5, heads=2, d=64, page=16):
         one = (layers, pages, 2, heads, page)
-        self.codes, self.ratios = (torch.zeros(*one, n, dtype=torch.uint8) for n in (d // 2, d // 32))
-        self.exponents = torch.zeros(layers, pages, heads, page, 2, dtype=torch.uint8)
-        self.layers, self.pages, self.kv_heads, self.page, self.head_dim = layers, pages, heads, page, d
-        self.device = torch.device("cpu")
-        self._sizes = (pages, heads, d, P._PAGES[page])
-        self._strides = tuple(t.stride(0) for t in (self.codes, self.ratios, self.exponents))
+        self._hold(*(torch.zeros(s, dtype=torch.uint8) for s in ((*one, d // 2), (*one, d // 32), (layers, pages, heads, page, 2))))
+        self._scratch = 64
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -34,11 +30,6 @@ def launched(monkeypatch):
     calls = []
     monkeypatch.setattr(P, "_current_device", lambda: None)
     monkeypatch.setattr(P, "_launch", lambda *a: calls.append(a))
-
-    class Lib:
-        decoder_page_attention_scratch = staticmethod(lambda *a: 64)
-
-    monkeypatch.setattr(P, "lib", lambda: Lib)
     return calls
 
 
@@ -81,11 +72,22 @@ def test_what_calls_take(launched):
         call()
     assert [c[0] for c in launched] == ["decoder_page_rows", "decoder_page_rows", "decoder_page_attention"]
     assert [c[1] for c in launched[:2]] == [0, 1]
-    # (pages, heads, d, log2 of the page)
-    assert launched[0][5:9] == (5, 2, 64, 4) and launched[2][4:8] == (5, 2, 64, 4)
     P.page_attention(cache, 1, torch.zeros(2, 4, 64, dtype=BF), *where())
-    for i, t in enumerate((cache.codes, cache.ratios, cache.exponents)):
-        assert launched[2][1 + i] == t.data_ptr() and launched[3][1 + i] == t[1].data_ptr()
+    assert launched[0][2:4] == launched[2][1:3] == (cache._at, 0) and launched[3][1:3] == (cache._at, 1)
+    d = cache._described
+    assert (d.codes, d.ratios, d.exponents) == tuple(t.data_ptr() for t in (cache.codes, cache.ratios, cache.exponents))
+    assert (d.layers, d.pages, d.heads, d.head_dim, d.log_page) == (2, 5, 2, 64, 4)
+
+
+def test_a_cache_that_was_given_back(launched):
+    cache = OnCpu()
+    cache.ratios.untyped_storage().resize_(0)
+    for call in calls(cache, where()):
+        with pytest.raises(ValueError, match="no memory"):
+            call()
+    with pytest.raises(ValueError, match="no memory"):
+        P.copy_pages(cache, [0], [1])
+    assert not launched
 
 
 def test_nothing_to_do(launched):
@@ -165,21 +167,26 @@ def test_copies(launched):
     assert not launched
     P.copy_pages(cache, [0, 0], [2, 4])
     P.copy_pages(cache, torch.tensor([1]), (3,))
-    name, *at, layers, pages, heads, d, log_page, src, dst, n = launched[0]
-    assert (name, layers, pages, heads, d, log_page, n) == ("decoder_page_copy", 2, 5, 2, 64, 4, 2) and list(src) == [0, 0] and list(dst) == [2, 4]
+    name, at, src, dst, n = launched[0]
+    assert (name, at, n) == ("decoder_page_copy", cache._at, 2) and list(src) == [0, 0] and list(dst) == [2, 4]
 
 
 def test_the_library_refuses_sizes():
     L = K.lib()
-    assert L.decoder_page_attention_scratch(0, 1, 1, 1, 64) == L.decoder_page_attention_scratch(1, 1, 3, 2, 64) == 0
-    assert L.decoder_page_attention_scratch(1, 1, 1, 1, 96) == L.decoder_page_attention_scratch(1, 1 << 20, 64, 1, 64) == 0
-    longs = (P.ctypes.c_long * 4)()
-    for pages, heads, d, log_page, width in ((0, 1, 64, 4, 1), (1, 0, 64, 4, 1), (1, 1, 32, 4, 1), (1, 1, 64, 3, 1), (1, 1, 64, 9, 1), (1, 1, 64, 4, 0)):
-        assert L.decoder_page_rows(0, None, None, None, pages, heads, d, log_page, None, None, longs, None, None, None, width, 1, 1, None) != 0
-        assert L.decoder_page_attention(None, None, None, pages, heads, d, log_page, None, longs, None, None, None, width, 1, 1, 4, 1.0, 0, None,
-                                        None, None) != 0
-    ids = (P.ctypes.c_int * 1)(7)
-    assert L.decoder_page_copy(None, None, None, 1, 7, 1, 64, 4, ids, ids, 1, None) != 0
+    assert L.decoder_page_attention_scratch(96) < 0
+    byref = P.ctypes.byref
+    good = (1, 1, 1, 64, 4)
+    for sizes, layer, width in (((0, 1, 1, 64, 4), 0, 1), ((1, 0, 1, 64, 4), 0, 1), ((1, 1, 0, 64, 4), 0, 1), ((1, 1, 1025, 64, 4), 0, 1),
+                                ((1, 1, 1, 32, 4), 0, 1), ((1, 1, 1, 64, 3), 0, 1), ((1, 1, 1, 64, 9), 0, 1), (good, 1, 1), (good, -1, 1), (good, 0, 0)):
+        c = P._Described(None, None, None, *sizes)
+        assert L.decoder_page_rows(0, byref(c), layer, None, None, 0, 0, 0, 0, None, None, None, width, 1, 1, None) != 0
+        assert L.decoder_page_attention(byref(c), layer, None, 0, 0, None, None, None, width, 1, 1, 2, 1.0, 0, None, None, None) != 0
+    c = P._Described(None, None, None, 1, 1, 2, 64, 4)
+    for rows, hq, window in ((1, 3, 0), (1, 0, 0), (0, 2, 0), (1 << 25, 2, 0), (1, 2, -1)):
+        assert L.decoder_page_attention(byref(c), 0, None, 0, 0, None, None, None, 1, 1, rows, hq, 1.0, window, None, None, None) != 0
+    for page in (-1, 1):
+        ids = (P.ctypes.c_int * 1)(page)
+        assert L.decoder_page_copy(byref(c), ids, ids, 1, None) != 0
 
 
 @pytest.mark.parametrize("mode", ["real", "fake"])
