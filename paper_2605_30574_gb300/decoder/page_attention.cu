@@ -184,6 +184,16 @@ __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
+// What a warp does with its share, in shared memory: between two tiles it is all that a
+// warp knows, so that the loop over the keys has the registers.
+template <class S>
+struct Walk {
+    long x, end, begin, at, item_at;            // on the line: where it is, its share, its sequence's begin, its tile's
+    int b, line, first, new_, base, head, tile, rows;
+    int pos[S::kCols];                          // of the columns' rows
+    int ids[64];                                // pages of the sequence, two times 32 places
+};
+
 // Rows' states joined, 8 lanes to a row: O for the reference m and the sum l, at D and
 // D + 1.
 template <int D>
@@ -236,6 +246,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kThreads / 32];
     __shared__ float* places[S::kWarps][2];     // states of tiles that go on here, and that go on behind this warp
+    __shared__ Walk<S> walks[S::kWarps];
+    __shared__ long shares_of[2];               // stages to a worker, and how many have one more
     __shared__ int4 runs[S::kWarps + 1];        // tiles that warps share: the one that goes on here, and each warp's that goes on
     wait_for_previous();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
@@ -261,56 +273,49 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     const long shares = max(1L, quotient(total, kMinKeys / S::kKeys));
     const int active = int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
     const long workers = min(shares, long(active) * gridDim.x);
-    const int worker0 = active * blockIdx.x, worker = worker0 + warp_in;
-    const bool works = warp_in < active && worker < workers;
+    const int worker0 = active * blockIdx.x;
     // (the first total % workers have one stage more)
     const long each = quotient(total, workers), longer = total - each * workers;
-    const long begin = works ? each * worker + min(long(worker), longer) : 0, end = works ? begin + each + (worker < longer) : 0;
-    auto worker_of = [&](long at) {
-        return int(at < longer * (each + 1) ? quotient(at, each + 1) : longer + quotient(at - longer * (each + 1), max(1L, each)));
-    };
-    long x = begin;
+    Walk<S>& walk = walks[warp_in];
     if (lane == 0) {
+        const int worker = worker0 + warp_in;
+        const bool works = warp_in < active && worker < workers;
+        walk.x = walk.begin = works ? each * worker + min(long(worker), longer) : 0;
+        walk.end = works ? walk.begin + each + (worker < longer) : 0;
+        int lo = 0;                              // the run of sequences that x is in
+        for (int step = 256; step; step /= 2)
+            if (lo + step < kThreads && before[lo + step] <= walk.x) lo += step;
+        walk.at = before[lo];
+        walk.b = min(lo * run, A.s.batch - 1);
         runs[1 + warp_in].x = -1;
-        if (warp_in == 0) runs[0].x = -1;
+        if (warp_in == 0) {
+            runs[0].x = -1;
+            shares_of[0] = each, shares_of[1] = longer;
+        }
     }
     __syncthreads();
-    int lo = 0;                                  // the run of sequences that x is in
-    for (int step = 256; step; step /= 2)
-        if (lo + step < kThreads && before[lo + step] <= x) lo += step;
-    long at = before[lo];
-    int b = min(lo * run, A.s.batch - 1);
-    Seq sq = sequence<S>(A, b);
 
     // the warp's ring, and what a lane copies of a stage: 16 bytes of every 512 of the
     // codes, and of the rest its share: of K's ratios, V's, and the exponents, 2 kI, 2 kI
     // and 4 lanes' worth (past 32: a second time)
     const uint32_t ring = smem_u32(smem) + warp_in * S::kWarpBytes, ring_end = ring + S::kStages * S::kBytes;
     const uint32_t q_at = ring_end + 16 * lane;
-    const uint32_t page_rows = 1u << A.c.log_page, both = page_rows * A.c.hkv;      // (of keys or values, of a page)
     constexpr int kMore = S::kRest > 32 ? 2 : 1;
-    uint32_t rest_to[kMore], rest_page[kMore];
-    const uint8_t* rest_from[kMore];
-    int rest_row[kMore];
-    bool rest_late[kMore];                       // (of the stage's second half)
-#pragma unroll
-    for (int m = 0; m < kMore; ++m) {
-        const int i = lane + 32 * m, kind = i < 2 * kI ? 0 : i < 4 * kI ? 1 : 2, j = i - 2 * kI * kind;
-        rest_to[m] = i < S::kRest ? S::kKr + 16 * i : 0;
-        rest_row[m] = kind < 2 ? kI : 2;
-        rest_page[m] = both * (kind < 2 ? 2 * kI : 2);
-        rest_late[m] = j * 16 >= 16 * rest_row[m];
-        rest_from[m] = (kind < 2 ? A.c.ratios + (kind ? size_t(both) * kI : 0) : A.c.exponents) + 16 * j;
-    }
+    auto rest_kind = [&](int m) { return lane + 32 * m < 2 * kI ? 0 : lane + 32 * m < 4 * kI ? 1 : 2; };
+    auto rest_row = [&](int m) { return lane + 32 * m < 4 * kI ? kI : 2; };
     const int log_blocks = A.c.log_page - (P == 2 ? 4 : 5);     // (below 0: pages of 16, two to a stage)
     const int in_page = log_blocks > 0 ? (1 << log_blocks) - 1 : 0;
     const bool small = log_blocks < 0;
     // (kept in registers: as constants they are made anew for every product)
-    uint32_t eights[4];
+    uint32_t eights[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(eights[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));   // -128, -8 (2^-24)
+    for (int i = 0; i < 2; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(eights[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));   // -128, -8 (2^-24)
 
-    while (x < end) {
+    while (walk.x < walk.end) {
+        const long x = walk.x;
+        long at = walk.at;
+        int b = walk.b;
+        Seq sq = sequence<S>(A, b);
         while (at + size_of<S>(A, sq) <= x) {
             at += size_of<S>(A, sq);
             if (++b >= A.s.batch) break;         // (lengths that changed under the call)
@@ -319,23 +324,32 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         if (b >= A.s.batch) break;
         const long rel = x - at;
         const int item = int(quotient(rel, sq.blocks)), j0 = int(rel - long(item) * sq.blocks);
-        const int j1 = int(min(long(sq.blocks), j0 + (end - x)));
+        const int j1 = int(min(long(sq.blocks), j0 + (walk.end - x)));
         const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
-        const long item_at = x - j0;
-        x += j1 - j0;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
         const int base = sq.length - sq.new_;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
         const int kb0 = A.window ? max(0, first_pos - A.window + 1) / S::kKeys : 0;
         const int kb_end = min(kb0 + j1 - S::kBegin, (last_pos + S::kKeys) / S::kKeys);
         int kb = kb0 + max(0, j0 - S::kBegin), kb_in = kb;
-
-        // ---- stages on their way: the pages of 32 places at a time in the lanes ----
-        const int* table = A.s.table + size_t(b) * A.s.width;
+        __syncwarp();
+        if (lane == 0) {
+            walk.x = x + (j1 - j0), walk.at = at, walk.item_at = x - j0;
+            walk.b = b, walk.line = sq.blocks, walk.first = sq.first, walk.new_ = sq.new_, walk.base = base;
+            walk.head = head, walk.tile = tile, walk.rows = rows;
+        }
+        // ---- stages on their way: the numbers of 64 pages in the walk ----
         auto place = [&](int at) { return small ? 2 * at : at >> log_blocks; };
-        int ids_at = place(kb);
-        auto pages_from = [&](int i) { return i + lane < A.s.width ? __ldg(table + i + lane) : -1; };
-        int ids = pages_from(ids_at), more = pages_from(ids_at + 32);
+        auto look_up = [&](const int* table, int first) {
+            const int i = first + lane;
+            walk.ids[i & 63] = i < A.s.width ? __ldg(table + i) : -1;
+        };
+        {
+            const int* table = A.s.table + size_t(b) * A.s.width;
+            look_up(table, place(kb) & ~31);
+            look_up(table, (place(kb) & ~31) + 32);
+        }
+        __syncwarp();
         // (q on its way meanwhile: columns are a head's rows, 8 / P or 8 NT of them)
         uint32_t raw[NT][kI][4];
 #pragma unroll
@@ -349,37 +363,42 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 raw[n][i][0] = y.x, raw[n][i][1] = y.y, raw[n][i][2] = y.z, raw[n][i][3] = y.w;
             }
         }
-        const uint8_t* codes = A.c.codes + size_t(page_rows) * head * (D / 2) + 16 * lane;
         const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the stage's second half)
         bool broken = false;                     // a page that is none of the cache's
         auto locate = [&]() {
             const int i = place(kb_in);
-            if (i - ids_at >= 32) {
-                ids = more;
-                ids_at += 32;
-                more = pages_from(ids_at + 32);
+            if ((i & 31) == 0) {
+                __syncwarp();
+                look_up(A.s.table + size_t(walk.b) * A.s.width, i + 32);
+                __syncwarp();
             }
             auto checked = [&](int at) {
-                const int page = __shfl_sync(kFull, ids, at);
+                const int page = walk.ids[at & 63];
                 if (page >= 0 && page < A.c.pages) return uint32_t(page);
                 broken = true;
                 return 0u;
             };
-            const uint32_t page = checked(i - ids_at);
+            const uint32_t page = checked(i);
             uint32_t late = page;
-            if (small) late = 32 * kb_in + 16 <= last_pos ? checked(i - ids_at + 1) : page;
-            const uint32_t slot = S::kKeys * (kb_in & in_page);
-            k_in = codes + uint64_t(page) * (both * D) + slot * (D / 2);
-            late_in = P == 2 ? k_in + page_rows * (D / 2) : small ? codes + uint64_t(late) * (both * D) : k_in + 8 * D;
+            if (small) late = 32 * kb_in + 16 <= last_pos ? checked(i + 1) : page;
+            const uint32_t page_rows = 1u << A.c.log_page, both = page_rows * A.c.hkv;      // (of keys or values, of a page)
+            const uint32_t slot = S::kKeys * (kb_in & in_page), row = page_rows * walk.head;
+            const uint8_t* codes = A.c.codes + 16 * lane;
+            k_in = codes + uint64_t(page) * (both * D) + (row + slot) * (D / 2);
+            late_in = P == 2 ? k_in + page_rows * (D / 2) : small ? codes + uint64_t(late) * (both * D) + row * (D / 2) : k_in + 8 * D;
 #pragma unroll
-            for (int m = 0; m < kMore; ++m)
-                rest_in[m] = rest_from[m] + size_t(page_rows) * head * rest_row[m] + uint64_t(rest_late[m] ? late : page) * rest_page[m] +
-                             slot * rest_row[m] + (rest_late[m] ? (P == 2 ? int(page_rows) - 16 : small ? -16 : 0) * rest_row[m] : 0);
+            for (int m = 0; m < kMore; ++m) {
+                const int kind = rest_kind(m), each_row = rest_row(m), j = lane + 32 * m - 2 * kI * kind;
+                const bool second = j >= each_row;               // (of the stage's second half)
+                rest_in[m] = (kind < 2 ? A.c.ratios + (kind ? both * kI : 0) : A.c.exponents) + 16 * j +
+                             uint64_t(second ? late : page) * (both * (kind < 2 ? 2 * kI : 2)) +
+                             int64_t(int(row + slot) + (second ? (P == 2 ? int(page_rows) - 16 : small ? -16 : 0) : 0)) * each_row;
+            }
         };
         uint32_t in_at = ring, out_at = ring;
         auto fill = [&]() {
             if (kb_in < kb_end) {
-                const uint32_t values = both * (D / 2);
+                const uint32_t values = (uint32_t(A.c.hkv) << A.c.log_page) * (D / 2);
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) {
                     const uint8_t* from = (j < D / 64 ? k_in : late_in) + 512 * (j % (D / 64));
@@ -388,7 +407,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 }
 #pragma unroll
                 for (int m = 0; m < kMore; ++m)
-                    if (rest_to[m]) cp16(in_at + rest_to[m], rest_in[m]);
+                    if (lane + 32 * m < S::kRest) cp16(in_at + S::kKr + 16 * (lane + 32 * m), rest_in[m]);
                 in_at += S::kBytes;
                 if (in_at == ring_end) in_at = ring;
                 if ((++kb_in & in_page) == 0) {
@@ -397,7 +416,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     k_in += S::kKeys * (D / 2);
                     late_in += S::kKeys * (D / 2);
 #pragma unroll
-                    for (int m = 0; m < kMore; ++m) rest_in[m] += S::kKeys * rest_row[m];
+                    for (int m = 0; m < kMore; ++m) rest_in[m] += S::kKeys * rest_row(m);
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -409,7 +428,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         // ---- the rows: q as an operand, and what is known of each column ----
         uint32_t minus[P][NT][kI > 4 ? 4 : 2];
         float factor[NT][2], l[NT][2], ref[NT][2];
-        int pos[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int mine = P == 2 ? g >> 2 : 0;
@@ -474,11 +492,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 // S 2^(E_k - 2) 2^24 / up, in bits
                 factor[n][c] = __shfl_sync(kFull, down, 4 * (2 * t + c)) * (0x1p22f * kLog2e) * A.scale;
                 const int column = P == 2 ? 2 * t + c & 3 : 8 * n + 2 * t + c;
-                pos[n][c] = column < rows ? base + (tile * R + column) / A.G : -1;
+                if (g == 0) walk.pos[8 * n + 2 * t + c] = column < rows ? base + (tile * R + column) / A.G : -1;
                 l[n][c] = 0.f;
                 ref[n][c] = kNone;
             }
         }
+        __syncwarp();
         float acc[NT][kI][2][4] = {};
         // values 2t and 2t + 1 are read in turn and back, by t: half the bank conflicts
         const uint32_t even = t & 1 ? 0x1054u : 0x5410u, odd = t & 1 ? 0x3276u : 0x7632u;
@@ -578,7 +597,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 if (kEdge) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int key = key0 + g + 8 * (j >> 1), last = pos[n][j & 1];
+                        const int key = key0 + g + 8 * (j >> 1), last = walk.pos[8 * n + 2 * t + (j & 1)];
                         if (key > last || (A.window && key <= last - A.window)) x[j] = -INFINITY;
                     }
                 }
@@ -694,16 +713,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         __syncwarp();
 
         // ---- the rows' states: out, or left for the join ----
-        const bool whole = j0 == 0 && j1 == sq.blocks;
-        const int slot = item_at <= begin ? 0 : 1;
+        const long item_at = walk.item_at, item_end = item_at + walk.line;
+        const bool whole = item_at >= walk.begin && item_end <= walk.x;
         // (a warp's last state goes where its ring was)
-        float* const state = x >= end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
-                                      : A.states + size_t(worker) * S::kCols * (D + 4);
-        if (!whole && lane == 0) places[warp_in][slot] = state;
+        float* const state = walk.x >= walk.end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
+                                                : A.states + size_t(worker0 + warp_in) * S::kCols * (D + 4);
         if (!whole && lane == 0) {
-            const int4 info = make_int4(sq.first, tile | rows << 24, head | slot << 30, worker_of(item_at + sq.blocks - 1));
-            if (j0 == 0) runs[1 + warp_in] = info;
-            if (j0 > 0 && warp_in == 0) runs[0] = info;
+            const int slot = item_at <= walk.begin ? 0 : 1;
+            const long each = shares_of[0], longer = shares_of[1];
+            auto worker_of = [&](long at) {
+                return int(at < longer * (each + 1) ? quotient(at, each + 1) : longer + quotient(at - longer * (each + 1), max(1L, each)));
+            };
+            places[warp_in][slot] = state;
+            const int4 info = make_int4(walk.first, walk.tile | walk.rows << 24, walk.head | slot << 30, worker_of(item_end - 1));
+            if (item_at >= walk.begin) runs[1 + warp_in] = info;
+            if (item_at < walk.begin && warp_in == 0) runs[0] = info;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -714,11 +738,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 for (int o = 4; o < 32; o *= 2) sum += __shfl_xor_sync(kFull, sum, o);
                 if (__any_sync(kFull, broken)) sum = __int_as_float(0x7fffffff);
                 const int col = 8 * n + 2 * t + c, mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col;
-                if (row >= rows) continue;
+                if (row >= walk.rows) continue;
                 const float f = whole ? (sum == 0.f ? 0.f : 0x1p16f / sum) : 0x1p16f;
                 if (whole) {
-                    const int r = tile * R + row, token = r / A.G;
-                    __nv_bfloat16* to = A.out + ((size_t(sq.first + token) * A.c.hkv + head + mine) * A.G + r - token * A.G) * D;
+                    const int r = walk.tile * R + row, token = r / A.G;
+                    __nv_bfloat16* to = A.out + ((size_t(walk.first + token) * A.c.hkv + walk.head + mine) * A.G + r - token * A.G) * D;
 #pragma unroll
                     for (int i = 0; i < kI; ++i) {
                         const __nv_bfloat162 x0 = __floats2bfloat162_rn(acc[n][i][0][c] * f, acc[n][i][0][2 + c] * (f * 0.0625f));
