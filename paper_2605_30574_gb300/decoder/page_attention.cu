@@ -45,7 +45,6 @@ using splice::tc::smem_u32;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
-constexpr int kMinKeys = 32;            // keys to a warp, at least
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
 
 struct Args {
@@ -67,7 +66,8 @@ struct Shape {
     static constexpr int D = D_, NT = NT_, P = P_, kI = D / 32;
     static constexpr int kCols = 8 * NT, kRows = kCols / P;         // (rows of a head, to a tile)
     static constexpr int kKeys = 32 / P;                            // keys to a stage: two runs of 16, or of two heads
-    static constexpr int kBegin = 2;                                // stages that a tile's begin and end take as long as
+    static constexpr int kBegin = D == 256 ? 2 : 2 * P;             // stages that a tile's begin and end take as long as
+    static constexpr int kLeast = 32 / kKeys;                       // stages to a warp, at least
     // warps to an SM, all of one CTA: as many as their registers allow
     static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
     static constexpr int kThreads = 32 * kWarps;
@@ -269,9 +269,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         __syncthreads();
     }
     const long total = before[kThreads];
-    // few keys: four warps and more of as many CTAs as there are shares for
-    const long shares = max(1L, quotient(total, kMinKeys / S::kKeys));
-    const int active = int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
+    // few keys: one CTA, or four warps and more of as many as there are shares for
+    const long shares = max(1L, quotient(total, S::kLeast));
+    const int active = shares <= S::kWarps ? int(shares) : int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
     const long workers = min(shares, long(active) * gridDim.x);
     const int worker0 = active * blockIdx.x;
     // (the first total % workers have one stage more)
@@ -307,9 +307,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     const int in_page = log_blocks > 0 ? (1 << log_blocks) - 1 : 0;
     const bool small = log_blocks < 0;
     // (kept in registers: as constants they are made anew for every product)
-    uint32_t eights[2];
+    uint32_t centre[2];                          // -136 and -128, times 2^-24
 #pragma unroll
-    for (int i = 0; i < 2; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(eights[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));   // -128, -8 (2^-24)
+    for (int i = 0; i < 2; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(centre[i]) : "r"(i ? 0x80808080u : 0x80888088u));
 
     while (walk.x < walk.end) {
         const long x = walk.x;
@@ -678,9 +678,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     const uint32_t r1 = bytes_of(vr[1][i / 4], vr[1][kI == 2 ? 0 : kI / 4 + i / 4], sel) << 7;
                     const uint32_t a = bytes_of(v[0][i / 2], v[1][i / 2], i & 1 ? odd : even);
                     const uint32_t c = bytes_of(v[2][i / 2], v[3][i / 2], i & 1 ? odd : even);
-                    const uint32_t lo4[4] = {add2(a & 0x000f000fu, eights[0]), add2(a & 0x00f000f0u, eights[1]), add2(c & 0x000f000fu, eights[0]), add2(c & 0x00f000f0u, eights[1])};
-                    const uint32_t a8 = a >> 8, c8 = c >> 8;
-                    const uint32_t hi4[4] = {add2(a8 & 0x000f000fu, eights[0]), add2(a8 & 0x00f000f0u, eights[1]), add2(c8 & 0x000f000fu, eights[0]), add2(c8 & 0x00f000f0u, eights[1])};
+                    // a byte is n + 16 n', its upper nibble 16 n': the first sum less the second
+                    // is what n alone gives
+                    const uint32_t a8 = bytes_of(a, 0, 0x4341), c8 = bytes_of(c, 0, 0x4341);
+                    const uint32_t lo4[4] = {add2(a & 0x00ff00ffu, centre[0]), add2(a & 0x00f000f0u, centre[1]),
+                                             add2(c & 0x00ff00ffu, centre[0]), add2(c & 0x00f000f0u, centre[1])};
+                    const uint32_t hi4[4] = {add2(a8, centre[0]), add2(a8 & 0x00f000f0u, centre[1]), add2(c8, centre[0]),
+                                             add2(c8 & 0x00f000f0u, centre[1])};
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const uint32_t b0 = mul2(wh[n][0], r0), b1 = mul2(wh[n][1], r1);
@@ -745,8 +749,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     __nv_bfloat16* to = A.out + ((size_t(walk.first + token) * A.c.hkv + walk.head + mine) * A.G + r - token * A.G) * D;
 #pragma unroll
                     for (int i = 0; i < kI; ++i) {
-                        const __nv_bfloat162 x0 = __floats2bfloat162_rn(acc[n][i][0][c] * f, acc[n][i][0][2 + c] * (f * 0.0625f));
-                        const __nv_bfloat162 x1 = __floats2bfloat162_rn(acc[n][i][1][c] * f, acc[n][i][1][2 + c] * (f * 0.0625f));
+                        const __nv_bfloat162 x0 = __floats2bfloat162_rn((acc[n][i][0][c] - acc[n][i][0][2 + c]) * f, acc[n][i][0][2 + c] * (f * 0.0625f));
+                        const __nv_bfloat162 x1 = __floats2bfloat162_rn((acc[n][i][1][c] - acc[n][i][1][2 + c]) * f, acc[n][i][1][2 + c] * (f * 0.0625f));
                         *reinterpret_cast<uint2*>(to + 32 * i + 4 * g) =
                             make_uint2(reinterpret_cast<const uint32_t&>(x0), reinterpret_cast<const uint32_t&>(x1));
                     }
@@ -755,8 +759,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll
                     for (int i = 0; i < kI; ++i)
                         *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
-                            make_float4(acc[n][i][0][c] * f, acc[n][i][0][2 + c] * (f * 0.0625f), acc[n][i][1][c] * f,
-                                        acc[n][i][1][2 + c] * (f * 0.0625f));
+                            make_float4((acc[n][i][0][c] - acc[n][i][0][2 + c]) * f, acc[n][i][0][2 + c] * (f * 0.0625f),
+                                        (acc[n][i][1][c] - acc[n][i][1][2 + c]) * f, acc[n][i][1][2 + c] * (f * 0.0625f));
                     if (g == 0) to[D] = ref[n][c], to[D + 1] = sum;
                 }
             }
@@ -833,7 +837,10 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
     A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
     A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
     const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
-    return rc ? rc : dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
+    // (no more work than one CTA takes, however long the sequences are: nothing to join)
+    const long tiles = a.s.batch + long(a.s.rows) * a.G / S::kRows, stages = ((long(a.s.width) << a.c.log_page) + S::kKeys - 1) / S::kKeys;
+    if (rc || tiles * (a.c.hkv / S::P) * (stages + S::kBegin) <= long(S::kLeast) * S::kWarps) return rc;
+    return dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
 
 template <int D>

@@ -31,7 +31,7 @@ from __future__ import annotations
 
 import ctypes
 import math
-from typing import List, Optional, Sequence, Tuple
+from typing import Dict, Iterable, List, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -315,3 +315,168 @@ def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None
         with torch.cuda.device(cache.device):
             return copy_pages(cache, src, dst)
     _launch("decoder_page_copy", at, *ints, n)
+
+
+class PageTables:
+    """Which pages of a cache hold which sequences, and how many tokens: kept on the host,
+    by numbers that sequences are given.  Sequences may share pages; a page that others
+    hold too is never written, ``extend`` copies one that is begun.
+
+    The calls that copy pages do so on torch's current stream, in that order with the
+    calls that read and write them; ``tensors`` gives what those take, as of then."""
+
+    def __init__(self, cache: PageCache):
+        if not isinstance(cache, PageCache):
+            raise TypeError("PageTables: cache must be a PageCache")
+        self.cache = cache
+        self._users = [0] * cache.pages
+        self._free = list(range(cache.pages - 1, -1, -1))
+        self._pages: Dict[int, List[int]] = {}
+        self._lengths: Dict[int, int] = {}
+        self._next = 0
+
+    def _known(self, what: str, ids) -> List[int]:
+        ids = list(ids)
+        for i in ids:
+            if i not in self._pages:
+                raise ValueError(f"PageTables.{what}: there is no sequence {i!r}")
+        return ids
+
+    @property
+    def free(self) -> int:
+        """Pages that no sequence holds."""
+        return len(self._free)
+
+    def length(self, sequence: int) -> int:
+        return self._lengths[self._known("length", [sequence])[0]]
+
+    def pages(self, sequence: int) -> Tuple[int, ...]:
+        return tuple(self._pages[self._known("pages", [sequence])[0]])
+
+    def _new(self, pages: List[int], length: int) -> int:
+        self._next += 1
+        self._pages[self._next], self._lengths[self._next] = pages, length
+        for p in pages:
+            self._users[p] += 1
+        return self._next
+
+    def _release(self, page: int) -> None:
+        self._users[page] -= 1
+        if not self._users[page]:
+            self._free.append(page)
+
+    def add(self, length: int = 0) -> int:
+        """A new sequence with room for its first ``length`` tokens."""
+        _whole("add", "length", length)
+        n = -(-length // self.cache.page)
+        if n > len(self._free):
+            raise RuntimeError(f"PageTables.add: {n} pages, and {len(self._free)} are free")
+        return self._new([self._free.pop() for _ in range(n)], length)
+
+    def extend(self, sequences: Iterable[int], tokens: Union[int, Iterable[int]] = 1) -> None:
+        """Makes the sequences longer, by as many tokens (one number, or one for each), which
+        ``store_pages`` may then write.  A begun page that another sequence holds too is
+        copied first.  With too few free pages nothing is done."""
+        ids = self._known("extend", sequences)
+        more = [tokens] * len(ids) if isinstance(tokens, int) else list(tokens)
+        if len(set(ids)) != len(ids) or len(more) != len(ids):
+            raise ValueError("PageTables.extend: each sequence once, and as many numbers of tokens as sequences")
+        for n in more:
+            _whole("extend", "tokens", n)
+        page, left, copied, added = self.cache.page, {}, [], []
+        for i, n in zip(ids, more):
+            held, length = self._pages[i], self._lengths[i]
+            if n and length % page:
+                last = held[-1]
+                users = left.get(last, self._users[last])
+                if users > 1:                        # (the last of them keeps it)
+                    copied.append((i, last))
+                    left[last] = users - 1
+            added.append(-(-(length + n) // page) - len(held))
+        if len(copied) + sum(added) > len(self._free):
+            raise RuntimeError(f"PageTables.extend: {len(copied) + sum(added)} pages, and {len(self._free)} are free")
+        src, dst = [], []
+        for i, last in copied:
+            src.append(last)
+            dst.append(self._free.pop())
+            self._users[last] -= 1
+            self._users[dst[-1]] = 1
+            self._pages[i][-1] = dst[-1]
+        for i, n, new in zip(ids, more, added):
+            for _ in range(new):
+                self._pages[i].append(self._free.pop())
+                self._users[self._pages[i][-1]] = 1
+            self._lengths[i] += n
+        copy_pages(self.cache, src, dst)
+
+    def fork(self, sequence: int, n: int = 1) -> List[int]:
+        """``n`` sequences that hold what this one does; nothing is copied yet."""
+        self._known("fork", [sequence])
+        _whole("fork", "n", n)
+        return [self._new(list(self._pages[sequence]), self._lengths[sequence]) for _ in range(n)]
+
+    def splice(self, sequence: int, donor: int, tokens: int) -> None:
+        """The sequence's first ``tokens`` become the donor's, by reference: whole pages
+        that both have."""
+        self._known("splice", [sequence, donor])
+        _whole("splice", "tokens", tokens)
+        n, odd = divmod(tokens, self.cache.page)
+        if odd or tokens > min(self._lengths[sequence], self._lengths[donor]):
+            raise ValueError(f"PageTables.splice: whole pages of {self.cache.page} tokens that both sequences have")
+        if sequence == donor:
+            return
+        held, given = self._pages[sequence], self._pages[donor]
+        for i in range(n):
+            self._users[given[i]] += 1
+            self._release(held[i])
+            held[i] = given[i]
+
+    def drop(self, sequences: Iterable[int]) -> None:
+        """Gives the sequences up, and pages that no other holds."""
+        ids = self._known("drop", sequences)
+        if len(set(ids)) != len(ids):
+            raise ValueError("PageTables.drop: each sequence once")
+        for i in ids:
+            for p in self._pages.pop(i):
+                self._release(p)
+            del self._lengths[i]
+
+    def compact(self) -> int:
+        """Moves the pages in use to the cache's first, and returns their number.  Tables
+        that ``tensors`` gave before are of no use then."""
+        used = [p for p, n in enumerate(self._users) if n]
+        k = len(used)
+        src = [p for p in used if p >= k]
+        dst = [p for p in range(k) if not self._users[p]]
+        to = dict(zip(src, dst))
+        copy_pages(self.cache, src, dst)
+        for p, q in to.items():
+            self._users[q], self._users[p] = self._users[p], 0
+        for i, held in self._pages.items():
+            self._pages[i] = [to.get(p, p) for p in held]
+        self._free = list(range(self.cache.pages - 1, k - 1, -1))
+        return k
+
+    def tensors(self, sequences: Iterable[int], new: Union[None, int, Iterable[int]] = 1,
+                width: int = 0) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """``table``, ``starts`` and ``lengths`` of the sequences on the cache's device, of
+        which the ``new`` last tokens are stored, loaded or attend (one number, or one for
+        each; None: all).  The table has ``width`` columns, or as many more as it needs."""
+        ids = self._known("tensors", sequences)
+        lengths = [self._lengths[i] for i in ids]
+        new = lengths if new is None else [new] * len(ids) if isinstance(new, int) else list(new)
+        if len(new) != len(ids) or any(not isinstance(n, int) or not 0 <= n <= m for n, m in zip(new, lengths)):
+            raise ValueError("PageTables.tensors: as many new tokens as each sequence has, at most")
+        starts = [0]
+        for n in new:
+            starts.append(starts[-1] + n)
+        width = max([1, width] + [len(self._pages[i]) for i in ids])
+        flat = [p for i in ids for p in self._pages[i] + [-1] * (width - len(self._pages[i]))]
+        B = len(ids)
+        t = torch.tensor(flat + starts + lengths, dtype=_I32).to(self.cache.device)
+        return t[:B * width].view(B, width), t[B * width:B * width + B + 1], t[B * width + B + 1:]
+
+
+def _whole(what, name, n):
+    if not isinstance(n, int) or n < 0:
+        raise ValueError(f"PageTables.{what}: {name} must be a whole number, 0 or more")

@@ -10,9 +10,11 @@ group's scale: 2 17 15 2^-23 < 2^-14 of s |q|, so e = 2^-14 scale sum of s |q| w
 groups' and the third product's; a weight is off by e relatively, and so is the row's
 sum.  Weights are rounded to fp16 before and after the group's scale, 2^-11 each (below
 fp16's normal range by 2^-25, against the largest of 2^6 and more: 2^-31 of it, for each
-key); fp32 sums leave 2^-16.  Together, with S the sum of p |v| and N keys,
+key); fp32 sums leave 2^-16.  Output: the codes of two elements in one, of up to 119 s, and
+what the second adds to them, for 16 keys at once: 2 17 119 2^-23 < 2^-11 of the largest
+p s among them, s the value's scale.  Together, with S the sum of p |v| and N keys,
 
-  (2^-10 + 2^-16 + 2 max e) S + 2^-28 N max p |v|,
+  (2^-10 + 2^-16 + 2 max e) S + 2^-11 sum p s + 2^-28 N max p |v|,
 
 and the output's rounding, 2^-8 |o|.
 """
@@ -73,7 +75,8 @@ def definition(cache, q, table, starts, lengths, scale, window):
         ids = [int(table[b, i]) for i in range(-(-L // page))]
         n = int(starts[b + 1]) - int(starts[b])
         for h in range(heads):
-            k, v, ks = ((torch.cat([x[i, j, h] for i in ids])[:L] if ids else x[:0, j, h].flatten(0, 1)) for x, j in ((all_, 0), (all_, 1), (s_all, 0)))
+            k, v, ks, vs = ((torch.cat([x[i, j, h] for i in ids])[:L] if ids else x[:0, j, h].flatten(0, 1))
+                            for x, j in ((all_, 0), (all_, 1), (s_all, 0), (s_all, 1)))
             for i in range(n):
                 pos = int(lengths[b]) - n + i
                 lo = max(0, pos - window + 1) if window else 0
@@ -87,7 +90,9 @@ def definition(cache, q, table, starts, lengths, scale, window):
                     e = abs(scale) * float((kss @ q[row, x].abs().view(-1, 32).sum(-1)).max()) * 2.0 ** -14
                     out[row, x] = p @ vv
                     pv = p[:, None] * vv.abs()
-                    bound[row, x] = (2.0 ** -10 + 2.0 ** -16 + 2 * e) * pv.sum(0) + 2.0 ** -28 * len(s) * pv.max() + 2.0 ** -8 * out[row, x].abs()
+                    ps = (p @ vs[lo:pos + 1]).repeat_interleave(32)
+                    bound[row, x] = ((2.0 ** -10 + 2.0 ** -16 + 2 * e) * pv.sum(0) + 2.0 ** -11 * ps + 2.0 ** -28 * len(s) * pv.max()
+                                     + 2.0 ** -8 * out[row, x].abs())
     return out, bound
 
 
