@@ -67,19 +67,19 @@ struct Rows {
     long k_token, k_head, v_token, v_head;
 };
 
-// Eight elements of a row in each lane, D / 8 lanes to a row: where a lane's parts of
-// page 0 are, and what is from page to page.  (A page is below 2^27 bytes.)
-template <int D>
+// E elements of a row in each lane (8 or 16): where a lane's parts of page 0 are, and what
+// is from page to page.  (A page is below 2^27 bytes.)
+template <int D, int E>
 struct Lane {
-    static constexpr int kLanes = D / 8, kI = D / 32;
+    static constexpr int kLanes = D / E, kI = D / 32;
     uint8_t *codes, *ratios, *exponents;
     uint32_t rows;                          // of a page: keys, or values
 
     __device__ __forceinline__ Lane(const PageLayer& c, int kv, int head) {
-        const int w = threadIdx.x & (kLanes - 1), i = w >> 2, t = w & 3;
+        const int w = threadIdx.x & (kLanes - 1), i = w / (32 / E), t = w % (32 / E);
         rows = uint32_t(c.hkv) << c.log_page;
         const uint32_t row = (kv ? rows : 0) + (uint32_t(head) << c.log_page);
-        codes = c.codes + row * (D / 2) + (kv ? 4 * t * kI + 2 * i : 4 * (t * kI + i));     // (a value's first run)
+        codes = c.codes + row * (D / 2) + (kv ? E / 2 * t * kI + 2 * i : 4 * (E / 8 * t * kI + i));     // (the first word, or run)
         ratios = c.ratios + row * kI + i;
         exponents = c.exponents + ((uint32_t(head) << c.log_page) * 2 + kv);
     }
@@ -89,7 +89,8 @@ struct Lane {
 template <int D>
 struct Place {
     uint8_t *codes, *ratio, *exponent;
-    __device__ __forceinline__ Place(const Lane<D>& at, int page, int slot) {
+    template <int E>
+    __device__ __forceinline__ Place(const Lane<D, E>& at, int page, int slot) {
         const uint64_t n = uint64_t(uint32_t(page)) * at.rows;
         codes = at.codes + n * D + slot * (D / 2);
         ratio = at.ratios + n * (D / 16) + slot * (D / 32);
@@ -101,21 +102,23 @@ struct Place {
     __device__ __forceinline__ uint8_t* exponent_at(int i) const { return exponent + i * 2; }
 };
 
-template <int D>
-__device__ __forceinline__ void quantise_and_store(const Place<D>& at, int n, uint4 x, int kv, bool out) {
-    constexpr int kLanes = D / 8, kI = D / 32;
+template <int D, int N>
+__device__ __forceinline__ void quantise_and_store(const Place<D>& at, int n, const uint4* x, int kv, bool out) {
+    constexpr int kLanes = D / N, kGroup = 32 / N, kI = D / 32;      // (lanes to a row, and to a group)
     const int w = threadIdx.x & (kLanes - 1);
-    const uint32_t raw[4] = {x.x, x.y, x.z, x.w};
+    uint32_t raw[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) raw[4 * i] = x[i].x, raw[4 * i + 1] = x[i].y, raw[4 * i + 2] = x[i].z, raw[4 * i + 3] = x[i].w;
     // magnitudes as whole numbers: infinities are above all numbers, and NaN above those
     uint32_t top2 = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, raw[i] & 0x7fff7fffu);
+    for (int i = 0; i < N / 2; ++i) top2 = __vmaxu2(top2, raw[i] & 0x7fff7fffu);
     unsigned top = max(top2 & 0xffffu, top2 >> 16);
-    top = max(top, __shfl_xor_sync(kFull, top, 1));
-    top = max(top, __shfl_xor_sync(kFull, top, 2));
+#pragma unroll
+    for (int o = 1; o < kGroup; o *= 2) top = max(top, __shfl_xor_sync(kFull, top, o));
     unsigned most = top;
 #pragma unroll
-    for (int o = 4; o < kLanes; o *= 2) most = max(most, __shfl_xor_sync(kFull, most, o));
+    for (int o = kGroup; o < kLanes; o *= 2) most = max(most, __shfl_xor_sync(kFull, most, o));
     int E = most >> 7;
     const bool bad = E > kMostExponent, none = E < kLeastExponent;
     if (bad || none) E = kLeastExponent;
@@ -132,24 +135,36 @@ __device__ __forceinline__ void quantise_and_store(const Place<D>& at, int n, ui
     // are 1 to 15 without a bound, as 7 (1 + 2^-4) rounds to 7.
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(bits) * power_of(E - 2)));
-    uint32_t word = 0u - 0x4b400000u * 0x11111111u;          // (what all the ys add but for their codes)
+    uint32_t word[N / 8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
-        word += __float_as_uint(__fadd_rn(fmaf(v, inv, 0x1.8p11f), 0x1.8p23f + 8.f - 0x1.8p11f)) << (4 * i);
+    for (int k = 0; k < N / 8; ++k) {
+        word[k] = 0u - 0x4b400000u * 0x11111111u;            // (what all the ys add but for their codes)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t two = raw[4 * k + i / 2];
+            const float v = __uint_as_float(i & 1 ? two & 0xffff0000u : two << 16);
+            word[k] += __float_as_uint(__fadd_rn(fmaf(v, inv, 0x1.8p11f), 0x1.8p23f + 8.f - 0x1.8p11f)) << (4 * i);
+        }
+        if (bad || none) word[k] = 0x88888888u;
     }
-    if (bad || none) word = 0x88888888u;
-    const int i = w >> 2, t = w & 3;
+    const int i = w / kGroup, t = w % kGroup;
     uint8_t* to = at.codes_at(n);
+    int step = 4 * kI;                           // (bytes to the next word)
     if (kv) {
-        // lanes of two groups trade their runs of four, so that each writes a word: run 2t
-        // of the even group and the next, and run 2t + 1
-        const uint32_t got = __shfl_xor_sync(kFull, i & 1 ? word & 0xffffu : word >> 16, 4);
-        word = i & 1 ? (word & 0xffff0000u) | got : (word & 0xffffu) | (got << 16);
-        if (i & 1) to += 2 * kI - 2;
+        // lanes of two groups trade half of their runs of four, so that each writes words:
+        // the first half of the runs of the even group and the next, and the second half
+        const bool odd = i & 1;
+        const uint32_t mine = N == 8 ? (odd ? word[0] >> 16 : word[0] & 0xffffu) : word[odd ? N / 8 - 1 : 0];
+        const uint32_t theirs = N == 8 ? (odd ? word[0] & 0xffffu : word[0] >> 16) : word[odd ? 0 : N / 8 - 1];
+        const uint32_t got = __shfl_xor_sync(kFull, theirs, kGroup), first = odd ? got : mine, second = odd ? mine : got;
+        word[0] = __byte_perm(first, second, 0x5410);
+        if (N == 16) word[N / 8 - 1] = __byte_perm(first, second, 0x7632);
+        if (odd) to += N / 4 * kI - 2;
+        step = 2 * kI;
     }
     if (!out) return;
-    *reinterpret_cast<uint32_t*>(to) = word;
+#pragma unroll
+    for (int k = 0; k < N / 8; ++k) *reinterpret_cast<uint32_t*>(to + k * step) = word[k];
     if (t == 0) *at.ratio_at(n) = uint8_t((bits >> 20) - (112u << 3));
     if (w == 0) *at.exponent_at(n) = uint8_t(bad ? kBadExponent : E);
 }
@@ -194,10 +209,11 @@ __device__ __forceinline__ uint4 values_of(const Held& x) {
 // A warp takes up to 32 tokens, whose places its lanes find at once, and as many heads of
 // K or of V as fill its lanes.  N rows are on their way together; the first of those to
 // store, before their places are known.
-template <int D, bool Store, int N>
+template <int D, bool Store, int N, int E>
 __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s, Rows x, int per_warp, unsigned kinds) {
     wait_for_previous();
-    constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
+    constexpr int kLanes = D / E, kHeads = 32 / kLanes;
+    static_assert(Store || E == 8);
     const unsigned group = blockIdx.x / kinds, kind = blockIdx.x - group * kinds;
     const int kv = kind >= kinds / 2, lane = threadIdx.x & 31, head = int(kind - kv * (kinds / 2)) * kHeads + lane / kLanes;
     const long first = (long(group) * (kThreads / 32) + threadIdx.x / 32) * per_warp;
@@ -205,12 +221,14 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
     const int n = int(min(long(per_warp), s.rows - first));
     const bool mine = head < c.hkv;
     const long token = kv ? x.v_token : x.k_token;
-    const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + 8 * (lane & (kLanes - 1)) + first * token;
-    const Lane<D> at(c, kv, mine ? head : 0);
-    uint4 data[N];
+    const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + E * (lane & (kLanes - 1)) + first * token;
+    const Lane<D, E> at(c, kv, mine ? head : 0);
+    uint4 data[N][E / 8];
     auto fetch = [&](int from) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) data[i] = *reinterpret_cast<const uint4*>(p + min(from + i, n - 1) * token);
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < E / 8; ++k) data[i][k] = reinterpret_cast<const uint4*>(p + min(from + i, n - 1) * token)[k];
     };
     if (Store) fetch(0);
     int slot = 0;
@@ -224,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
         if (run) {
             if (Store) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) quantise_and_store<D>(first_at, i, data[i], kv, mine);
+                for (int i = 0; i < N; ++i) quantise_and_store<D, E>(first_at, i, data[i], kv, mine);
             } else {
                 Held held[N];
 #pragma unroll
@@ -239,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
                 const int to = __shfl_sync(kFull, page, (from + i) & 31), in = __shfl_sync(kFull, slot, (from + i) & 31);
                 const Place<D> place(at, max(to, 0), to < 0 ? 0 : in);
                 if (Store) {
-                    quantise_and_store<D>(place, 0, data[i], kv, mine && to >= 0);
+                    quantise_and_store<D, E>(place, 0, data[i], kv, mine && to >= 0);
                 } else if (mine && to > -3) {
                     const uint32_t none = to == -1 ? 0u : 0x7fff7fffu;
                     *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) =
@@ -277,19 +295,27 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(Part a, Part b, Part e, 
     }
 }
 
+// The kernel of a call: N rows on their way, E elements of each to a lane.
+template <bool Store, int N, int E>
+auto kernel_of(int d) {
+    return d == 64 ? rows_kernel<64, Store, N, E> : d == 128 ? rows_kernel<128, Store, N, E> : rows_kernel<256, Store, N, E>;
+}
+
 template <bool Store>
 int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream_t stream) {
-    const int heads = 32 / (d / 8);
+    // Sixteen elements to a lane halve what a row's scales cost, where a warp's lanes are
+    // filled by a row of all heads.
+    const bool wide = Store && c.hkv * d >= 1024;
+    const int heads = 32 * (wide ? 16 : 8) / d;
     const long kinds = 2L * ((c.hkv + heads - 1) / heads);
     // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
     // shortest chain of loads.
     const int per_warp = s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
     const long blocks = (s.rows + 8L * per_warp - 1) / (8L * per_warp) * kinds;
     if (blocks >= 1L << 31) return int(cudaErrorInvalidValue);
-    const bool many = per_warp > 1;
-    const auto kernel = d == 64    ? (many ? rows_kernel<64, Store, 8> : rows_kernel<64, Store, 1>)
-                        : d == 128 ? (many ? rows_kernel<128, Store, 8> : rows_kernel<128, Store, 1>)
-                                   : (many ? rows_kernel<256, Store, 8> : rows_kernel<256, Store, 1>);
+    auto kernel = per_warp > 1 ? kernel_of<Store, 8, 8>(d) : kernel_of<Store, 1, 8>(d);
+    if constexpr (Store)
+        if (wide) kernel = per_warp > 1 ? kernel_of<Store, 4, 16>(d) : kernel_of<Store, 1, 16>(d);
     return dependent(kernel, dim3(unsigned(blocks)), kThreads, 0, stream, c, s, x, per_warp, unsigned(kinds));
 }
 

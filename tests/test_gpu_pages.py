@@ -36,7 +36,7 @@ def same(a, b):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("heads,page", [(1, 16), (3, 32), (8, 64), (2, 256)])
+@pytest.mark.parametrize("heads,page", [(1, 16), (3, 32), (8, 64), (2, 256), (17, 16), (5, 32)])
 @pytest.mark.parametrize("new,old", [([1], [0]), ([1] * 9, [0, 15, 16, 17, 63, 64, 300, 1, 2]),
                                      ([5, 0, 100, 33, 1, 0], [3, 9, 0, 31, 64, 0])])
 def test_rows_come_back_as_they_are_held(d, heads, page, new, old):
