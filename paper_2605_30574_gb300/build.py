@@ -88,7 +88,7 @@ def build(force: bool = False, verbose: bool = False) -> None:
     synth_src = [os.path.join(PKG, "synth", "synth.cu")]
     decoder_headers = [os.path.join(csrc, "tc_ptx.cuh"), os.path.join(csrc, "per_device.h"),
                        os.path.join(PKG, "decoder", "decoder.h"), os.path.join(PKG, "decoder", "attention.cuh"),
-                       os.path.join(PKG, "decoder", "pages.cuh"), os.path.join(PKG, "decoder", "page_attention.cuh")]
+                       os.path.join(PKG, "decoder", "pages.cuh")]
     decoder_src = sorted(glob.glob(os.path.join(PKG, "decoder", "*.cu")))
     with cf.ThreadPoolExecutor(max_workers=3) as ex:
         a = ex.submit(build_lib, "splice", sources, headers, splice_lib_path(), force, verbose)

@@ -27,40 +27,130 @@
 // each warp, whatever the sequences' lengths, which only the device knows.  A tile whose
 // keys fall to several warps leaves a state (m, l, O) per warp, and a second kernel joins
 // them in the warps' order: the same inputs give the same bits.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 #include <type_traits>
 
 #include "../csrc/per_device.h"
+#include "../csrc/tc_ptx.cuh"
 #include "decoder.h"
-#include "page_attention.cuh"
+#include "pages.cuh"
 
 namespace decoder {
 namespace {
 
-using namespace page;
+using splice::tc::smem_u32;
 
+constexpr unsigned kFull = 0xffffffffu;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
 
-// A warp's products have eight columns: rows of one kv head, or of P = 2 heads next to
-// each other, four of each.
-template <int D_, int P_>
+struct Args {
+    PageLayer c;
+    PageRows s;
+    const __nv_bfloat16* q;
+    long q_token, q_head;
+    __nv_bfloat16* out;
+    int G, window;
+    float scale;
+    float *states, *joined; // of warps [each][columns][d + 4], and of CTAs [each][2][columns][d + 4]
+    int4* begun;            // per CTA: the tile whose keys begin with it and go on
+};
+
+// A warp's products have 8 NT columns: rows of one kv head, or of P heads next to each
+// other, 8 / P of each.
+template <int D_, int NT_, int P_>
 struct Shape {
-    static constexpr int D = D_, P = P_, kI = D / 32;
-    static constexpr int kCols = 8, kRows = kCols / P;              // (rows of a head, to a tile)
+    static constexpr int D = D_, NT = NT_, P = P_, kI = D / 32;
+    static constexpr int kCols = 8 * NT, kRows = kCols / P;         // (rows of a head, to a tile)
     static constexpr int kKeys = 32 / P;                            // keys to a stage: two runs of 16, or of two heads
     static constexpr int kBegin = D == 256 ? 2 : 2 * P;             // stages that a tile's begin and end take as long as
     static constexpr int kLeast = 32 / kKeys;                       // stages to a warp, at least
     // warps to an SM, all of one CTA: as many as their registers allow
-    static constexpr int kWarps = D == 256 ? 8 : D == 128 ? 12 : 16;
+    static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
     static constexpr int kThreads = 32 * kWarps;
     // a stage of a warp's ring: where its parts are
     static constexpr int kStages = D == 256 ? 2 : D == 128 ? 3 : 4;
     static constexpr int kV = 16 * D, kKr = 32 * D, kVr = kKr + 32 * kI, kE = kKr + 64 * kI, kBytes = kE + 64;
     static constexpr int kRest = 4 * kI + 4;                        // copies of 16 bytes that bring ratios and exponents
-    static constexpr int kQ = P * kI * 512;                    // q as operands
+    static constexpr int kQ = P * NT * kI * 512;                    // q as operands
     static constexpr int kWarpBytes = kStages * kBytes + kQ, kSmem = kWarps * kWarpBytes;
     static_assert(kSmem <= 224 * 1024 && kStages * kBytes >= kCols * (D + 4) * 4);
 };
+constexpr int kJoin = 128;              // threads of a CTA that joins states
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma0(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Bytes of a and b (numbers 4 to 7) by the selector's digits; with 8 in a digit, the
+// byte's sign.
+__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t select) {
+    uint32_t y;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(select));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return reinterpret_cast<const uint32_t&>(h);
+}
+
+__device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
+    const __half2 h = __hadd2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
+    return reinterpret_cast<const uint32_t&>(h);
+}
+
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    const __half2 h = __hmul2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
+    return reinterpret_cast<const uint32_t&>(h);
+}
+
+// `N` bytes of shared memory at their own alignment, as words.
+template <int N>
+__device__ __forceinline__ void lds(uint32_t* x, uint32_t from) {
+    if constexpr (N == 2) {
+        uint16_t y;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(from));
+        x[0] = y;
+    }
+    if constexpr (N == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(from));
+    if constexpr (N == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from));
+    if constexpr (N >= 16)
+#pragma unroll
+        for (int i = 0; i < N / 16; ++i)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[4 * i]), "=r"(x[4 * i + 1]), "=r"(x[4 * i + 2]), "=r"(x[4 * i + 3])
+                         : "r"(from + 16 * i));
+}
+
+// a / b, of numbers that rarely need 64 bits.
+__device__ __forceinline__ long quotient(long a, long b) {
+    return (a | b) >> 32 ? a / b : long(uint32_t(a) / uint32_t(b));
+}
+
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
 // stages of keys, and kBegin more, as the one that sees most.
 struct Seq {
@@ -86,6 +176,14 @@ __device__ __forceinline__ long size_of(const Args& A, const Seq& q) {
     return long(q.tiles) * (A.c.hkv / S::P) * q.blocks;
 }
 
+__device__ __forceinline__ void sts16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
 // What a warp does with its share, in shared memory: between two tiles it is all that a
 // warp knows, so that the loop over the keys has the registers.
 template <class S>
@@ -96,9 +194,54 @@ struct Walk {
     int ids[64];                                // pages of the sequence, two times 32 places
 };
 
+// Rows' states joined, 8 lanes to a row: O for the reference m and the sum l, at D and
+// D + 1.
+template <int D>
+struct State {
+    static constexpr int kVec = D / 32;         // by four elements
+    float m = kNone, l = 0.f;
+    float4 o[kVec] = {};
+
+    __device__ __forceinline__ void add(const float* from) {
+        const int lane = threadIdx.x & 7;
+        float4 y[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) y[i] = reinterpret_cast<const float4*>(from)[lane + 8 * i];
+        const float2 ml = *reinterpret_cast<const float2*>(from + D);
+        const float M = fmaxf(m, ml.x), f = ex2(m - M), fy = ex2(ml.x - M);
+        m = M;
+        l = l * f + ml.y * fy;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            o[i] = make_float4(o[i].x * f + y[i].x * fy, o[i].y * f + y[i].y * fy, o[i].z * f + y[i].z * fy, o[i].w * f + y[i].w * fy);
+    }
+    __device__ __forceinline__ void keep(float* to) const {
+        const int lane = threadIdx.x & 7;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) reinterpret_cast<float4*>(to)[lane + 8 * i] = o[i];
+        if (lane == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
+    }
+    __device__ __forceinline__ void write(__nv_bfloat16* to) const {
+        const int lane = threadIdx.x & 7;
+        const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(o[i].x * f, o[i].y * f), b = __floats2bfloat162_rn(o[i].z * f, o[i].w * f);
+            *reinterpret_cast<uint2*>(to + 4 * (lane + 8 * i)) = make_uint2(reinterpret_cast<const uint32_t&>(a), reinterpret_cast<const uint32_t&>(b));
+        }
+    }
+};
+
+// The row of out of a tile's row.
+template <class S>
+__device__ __forceinline__ size_t row_of(const Args& A, const int4& info, int mine, int row) {
+    const int r = (info.y & 0xffffff) * S::kRows + row, token = r / A.G;
+    return (size_t(info.x + token) * A.c.hkv + (info.z & 0x3fffffff) + mine) * A.G + r - token * A.G;
+}
+
 template <class S>
 __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A) {
-    constexpr int D = S::D, P = S::P, kI = S::kI, kThreads = S::kThreads, R = S::kRows;
+    constexpr int D = S::D, NT = S::NT, P = S::P, kI = S::kI, kThreads = S::kThreads, R = S::kRows;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long before[kThreads + 1];       // work before each run of sequences
     __shared__ long sums[kThreads / 32];
@@ -207,15 +350,18 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             look_up(table, (place(kb) & ~31) + 32);
         }
         __syncwarp();
-        // (q on its way meanwhile: columns are a head's rows, 8 / P of them)
-        uint32_t raw[kI][4];
-        const int col = P == 2 ? g & 3 : g, r = tile * R + col, token = r / A.G;
-        const __nv_bfloat16* p = A.q + (sq.first + (col < rows ? token : 0)) * A.q_token +
-                                 ((head + (P == 2 ? g >> 2 : 0)) * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
+        // (q on its way meanwhile: columns are a head's rows, 8 / P or 8 NT of them)
+        uint32_t raw[NT][kI][4];
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-            const uint4 y = __ldg(reinterpret_cast<const uint4*>(p + 32 * i + 8 * t));
-            raw[i][0] = y.x, raw[i][1] = y.y, raw[i][2] = y.z, raw[i][3] = y.w;
+        for (int n = 0; n < NT; ++n) {
+            const int col = P == 2 ? g & 3 : 8 * n + g, r = tile * R + col, token = r / A.G;
+            const __nv_bfloat16* p = A.q + (sq.first + (col < rows ? token : 0)) * A.q_token +
+                                     ((head + (P == 2 ? g >> 2 : 0)) * A.G + (col < rows ? r - token * A.G : 0)) * A.q_head;
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                const uint4 y = __ldg(reinterpret_cast<const uint4*>(p + 32 * i + 8 * t));
+                raw[n][i][0] = y.x, raw[n][i][1] = y.y, raw[n][i][2] = y.z, raw[n][i][3] = y.w;
+            }
         }
         const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the stage's second half)
         bool broken = false;                     // a page that is none of the cache's
@@ -280,76 +426,79 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         for (int i = 0; i < S::kStages - 1; ++i) fill();
 
         // ---- the rows: q as an operand, and what is known of each column ----
-        uint32_t minus[P][kI > 4 ? 4 : 2];
-        float factor[2], l[2], ref[2];
-        const int mine = P == 2 ? g >> 2 : 0;
-        uint32_t top2 = 0;
+        uint32_t minus[P][NT][kI > 4 ? 4 : 2];
+        float factor[NT][2], l[NT][2], ref[NT][2];
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
+        for (int n = 0; n < NT; ++n) {
+            const int mine = P == 2 ? g >> 2 : 0;
+            uint32_t top2 = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top2 = __vmaxu2(top2, raw[i][j] & 0x7fff7fffu);
-        unsigned top = max(top2 & 0xffffu, top2 >> 16);
-        top = max(top, __shfl_xor_sync(kFull, top, 1));
-        top = max(top, __shfl_xor_sync(kFull, top, 2));
-        const int E = max(int(top >> 7), kLeastExponent);
-        // (a row with infinities or NaN: NaN)
-        const float up = E == 255 ? __int_as_float(0x7fffffff) : power_of(268 - E);
-        const float down = power_of(E < 255 ? E - 14 : 1);
-        uint32_t hi[kI], mid[kI], low[kI];       // -8 sum q of a group, as three fp16
+            for (int i = 0; i < kI; ++i)
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-            // elements 8t + j of group i, j = 0 .. 7; pairs (j, j + 4) to an operand
-            float f[8], sum = 0.f;
+                for (int j = 0; j < 4; ++j) top2 = __vmaxu2(top2, raw[n][i][j] & 0x7fff7fffu);
+            unsigned top = max(top2 & 0xffffu, top2 >> 16);
+            top = max(top, __shfl_xor_sync(kFull, top, 1));
+            top = max(top, __shfl_xor_sync(kFull, top, 2));
+            const int E = max(int(top >> 7), kLeastExponent);
+            // (a row with infinities or NaN: NaN)
+            const float up = E == 255 ? __int_as_float(0x7fffffff) : power_of(268 - E);
+            const float down = power_of(E < 255 ? E - 14 : 1);
+            uint32_t hi[kI], mid[kI], low[kI];       // -8 sum q of a group, as three fp16
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                f[j] = __uint_as_float(j & 1 ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
+            for (int i = 0; i < kI; ++i) {
+                // elements 8t + j of group i, j = 0 .. 7; pairs (j, j + 4) to an operand
+                float f[8], sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                raw[i][j] = half2_of(f[j], f[j + 4]);
-                const float2 y = __half22float2(reinterpret_cast<const __half2&>(raw[i][j]));
-                sum = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, sum);
+                for (int j = 0; j < 8; ++j)
+                    f[j] = __uint_as_float(j & 1 ? raw[n][i][j / 2] & 0xffff0000u : raw[n][i][j / 2] << 16) * up * (j & 1 ? 0.0625f : 1.f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    raw[n][i][j] = half2_of(f[j], f[j + 4]);
+                    const float2 y = __half22float2(reinterpret_cast<const __half2&>(raw[n][i][j]));
+                    sum = fmaf(y.x + y.y, j & 1 ? -128.f * 0x1p-24f : -8.f * 0x1p-24f, sum);
+                }
+                // (a head's operand has zeros for the other's columns; a lane reads its own)
+#pragma unroll
+                for (int ph = 0; ph < P; ++ph) {
+                    const bool zero = P == 2 && ph != mine;
+                    sts16(q_at + ((ph * NT + n) * kI + i) * 512, zero ? 0 : raw[n][i][0], zero ? 0 : raw[n][i][1], zero ? 0 : raw[n][i][2],
+                          zero ? 0 : raw[n][i][3]);
+                }
+                sum += __shfl_xor_sync(kFull, sum, 1);
+                sum += __shfl_xor_sync(kFull, sum, 2);
+                const __half a = __float2half_rn(sum), c = __float2half_rn(sum - __half2float(a)),
+                             e = __float2half_rn(sum - __half2float(a) - __half2float(c));
+                hi[i] = __half_as_ushort(a), mid[i] = __half_as_ushort(c), low[i] = __half_as_ushort(e);
             }
-            // (a head's operand has zeros for the other's columns; a lane reads its own)
-#pragma unroll
-            for (int ph = 0; ph < P; ++ph) {
-                const bool zero = P == 2 && ph != mine;
-                sts16(q_at + (ph * kI + i) * 512, zero ? 0 : raw[i][0], zero ? 0 : raw[i][1], zero ? 0 : raw[i][2],
-                      zero ? 0 : raw[i][3]);
+            // as an operand against the keys' ratios (see below)
+            auto two = [](const uint32_t* y, int i) { return y[i] | y[i + 1] << 16; };
+            uint32_t m[kI > 4 ? 4 : 2];
+            if constexpr (kI == 2) {
+                m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(mid, 0) : t == 2 ? two(low, 0) : 0u;
+                m[1] = 0u;
+            } else if constexpr (kI == 4) {
+                m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(hi, 2) : t == 2 ? two(mid, 0) : two(mid, 2);
+                m[1] = t == 0 ? two(low, 0) : t == 1 ? two(low, 2) : 0u;
+            } else {
+                auto by_t = [&](const uint32_t* y) { return t == 0 ? two(y, 0) : t == 1 ? two(y, 2) : t == 2 ? two(y, 4) : two(y, 6); };
+                m[0] = by_t(hi), m[1] = by_t(mid), m[2] = by_t(low), m[3] = 0u;
             }
-            sum += __shfl_xor_sync(kFull, sum, 1);
-            sum += __shfl_xor_sync(kFull, sum, 2);
-            const __half a = __float2half_rn(sum), c = __float2half_rn(sum - __half2float(a)),
-                         e = __float2half_rn(sum - __half2float(a) - __half2float(c));
-            hi[i] = __half_as_ushort(a), mid[i] = __half_as_ushort(c), low[i] = __half_as_ushort(e);
-        }
-        // as an operand against the keys' ratios (see below)
-        auto two = [](const uint32_t* y, int i) { return y[i] | y[i + 1] << 16; };
-        uint32_t m[kI > 4 ? 4 : 2];
-        if constexpr (kI == 2) {
-            m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(mid, 0) : t == 2 ? two(low, 0) : 0u;
-            m[1] = 0u;
-        } else if constexpr (kI == 4) {
-            m[0] = t == 0 ? two(hi, 0) : t == 1 ? two(hi, 2) : t == 2 ? two(mid, 0) : two(mid, 2);
-            m[1] = t == 0 ? two(low, 0) : t == 1 ? two(low, 2) : 0u;
-        } else {
-            auto by_t = [&](const uint32_t* y) { return t == 0 ? two(y, 0) : t == 1 ? two(y, 2) : t == 2 ? two(y, 4) : two(y, 6); };
-            m[0] = by_t(hi), m[1] = by_t(mid), m[2] = by_t(low), m[3] = 0u;
-        }
 #pragma unroll
-        for (int ph = 0; ph < P; ++ph)
+            for (int ph = 0; ph < P; ++ph)
 #pragma unroll
-            for (int j = 0; j < (kI > 4 ? 4 : 2); ++j) minus[ph][j] = P == 2 && ph != mine ? 0u : m[j];
+                for (int j = 0; j < (kI > 4 ? 4 : 2); ++j) minus[ph][n][j] = P == 2 && ph != mine ? 0u : m[j];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            // S 2^(E_k - 2) 2^24 / up, in bits
-            factor[c] = __shfl_sync(kFull, down, 4 * (2 * t + c)) * (0x1p22f * kLog2e) * A.scale;
-            const int column = P == 2 ? 2 * t + c & 3 : 2 * t + c;
-            if (g == 0) walk.pos[2 * t + c] = column < rows ? base + (tile * R + column) / A.G : -1;
-            l[c] = 0.f;
-            ref[c] = kNone;
+            for (int c = 0; c < 2; ++c) {
+                // S 2^(E_k - 2) 2^24 / up, in bits
+                factor[n][c] = __shfl_sync(kFull, down, 4 * (2 * t + c)) * (0x1p22f * kLog2e) * A.scale;
+                const int column = P == 2 ? 2 * t + c & 3 : 8 * n + 2 * t + c;
+                if (g == 0) walk.pos[8 * n + 2 * t + c] = column < rows ? base + (tile * R + column) / A.G : -1;
+                l[n][c] = 0.f;
+                ref[n][c] = kNone;
+            }
         }
         __syncwarp();
-        float acc[kI][2][4] = {};
+        float acc[NT][kI][2][4] = {};
         // values 2t and 2t + 1 are read in turn and back, by t: half the bank conflicts
         const uint32_t even = t & 1 ? 0x1054u : 0x5410u, odd = t & 1 ? 0x3276u : 0x7632u;
 
@@ -376,7 +525,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 lds<2>(&ex[h], out_at + e_of + 32 * half + 16 * h);
             }
             // scores: first what the codes' 8 adds to all groups
-            float s[4];
+            float s[NT][4];
 #pragma unroll
             for (int ph = 0; ph < P; ++ph) {
                 auto mine = [&](int h) {
@@ -387,38 +536,47 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 };
                 const uint32_t ra = mine(0), rc = mine(1);
                 const uint32_t r4[4] = {ra, rc, ra, rc};
-                if (ph == 0)
-                    mma0(s, r4, minus[ph][0], minus[ph][1]);
-                else
-                    mma(s, r4, minus[ph][0], minus[ph][1]);
-                if constexpr (kI > 4) mma(s, r4, minus[ph][2], minus[ph][3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (ph == 0)
+                        mma0(s[n], r4, minus[ph][n][0], minus[ph][n][1]);
+                    else
+                        mma(s[n], r4, minus[ph][n][0], minus[ph][n][1]);
+                    if constexpr (kI > 4) mma(s[n], r4, minus[ph][n][2], minus[ph][n][3]);
+                }
             }
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
-                float part[4];
+                float part[NT][4];
 #pragma unroll
                 for (int ph = 0; ph < P; ++ph) {
                     const uint32_t a = kc[ph][0][i], c = kc[ph][1][i];
                     const uint32_t lo4[4] = {a & 0x000f000fu, c & 0x000f000fu, a & 0x00f000f0u, c & 0x00f000f0u};
                     const uint32_t a8 = a >> 8, c8 = c >> 8;
                     const uint32_t hi4[4] = {a8 & 0x000f000fu, c8 & 0x000f000fu, a8 & 0x00f000f0u, c8 & 0x00f000f0u};
-                    uint32_t qf[4];
-                    lds<16>(qf, q_at + (ph * kI + i) * 512);
-                    if (ph == 0)
-                        mma0(part, lo4, qf[0], qf[1]);
-                    else
-                        mma(part, lo4, qf[0], qf[1]);
-                    mma(part, hi4, qf[2], qf[3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t qf[4];
+                        lds<16>(qf, q_at + ((ph * NT + n) * kI + i) * 512);
+                        if (ph == 0)
+                            mma0(part[n], lo4, qf[0], qf[1]);
+                        else
+                            mma(part[n], lo4, qf[0], qf[1]);
+                        mma(part[n], hi4, qf[2], qf[3]);
+                    }
                 }
                 // (by the ratios of the lane's columns' head)
                 const uint32_t r0 = P == 2 && t >= 2 ? ratio[P - 1][0][i / 2] : ratio[0][0][i / 2],
                                r1 = P == 2 && t >= 2 ? ratio[P - 1][1][i / 2] : ratio[0][1][i / 2];
                 const __half2 ra = reinterpret_cast<const __half2&>(r0), rc = reinterpret_cast<const __half2&>(r1);
                 const float fa = i & 1 ? __high2float(ra) : __low2float(ra), fc = i & 1 ? __high2float(rc) : __low2float(rc);
-                s[0] = fmaf(part[0], fa, s[0]);
-                s[1] = fmaf(part[1], fa, s[1]);
-                s[2] = fmaf(part[2], fc, s[2]);
-                s[3] = fmaf(part[3], fc, s[3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    s[n][0] = fmaf(part[n][0], fa, s[n][0]);
+                    s[n][1] = fmaf(part[n][1], fa, s[n][1]);
+                    s[n][2] = fmaf(part[n][2], fc, s[n][2]);
+                    s[n][3] = fmaf(part[n][3], fc, s[n][3]);
+                }
             }
             // weights, of keys g and g + 8
             float ek[2], up[2];
@@ -430,55 +588,58 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 ek[h] = fmaf(up[h], 0.f, fmaf(ek[h], 0.f, ek[h]));
                 up[h] *= 0x1p6f;
             }
-            uint32_t w[2];
-            float x[4], p[4], pv[4];
+            uint32_t w[NT][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = fmaf(s[j], factor[j & 1] * ek[j >> 1], -ref[j & 1]);
-            if (kEdge) {
+            for (int n = 0; n < NT; ++n) {
+                float x[4], p[4], pv[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = key0 + g + 8 * (j >> 1), last = walk.pos[2 * t + (j & 1)];
-                    if (key > last || (A.window && key <= last - A.window)) x[j] = -INFINITY;
-                }
-            }
+                for (int j = 0; j < 4; ++j) x[j] = fmaf(s[n][j], factor[n][j & 1] * ek[j >> 1], -ref[n][j & 1]);
+                if (kEdge) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                p[j] = ex2(x[j]);
-                pv[j] = p[j] * up[j >> 1];
-            }
-            if (kEdge) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (x[j] == -INFINITY) pv[j] = 0.f;          // (whatever the value is)
-            }
-            // what is past the reference is found by the weights: infinite, or too large
-            if (__any_sync(kFull, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])) > 0x1p14f)) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    s[j] = kEdge && x[j] == -INFINITY ? -INFINITY : s[j] * (factor[j & 1] * ek[j >> 1]);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float top = fmaxf(s[c] + float(int(ex[0] >> 8) - 127), s[2 + c] + float(int(ex[1] >> 8) - 127));
-#pragma unroll
-                    for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-                    const float m = fmaxf(ref[c], top), f = ex2(ref[c] - m);
-                    ref[c] = m;
-                    l[c] *= f;
-#pragma unroll
-                    for (int i = 0; i < kI; ++i)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) acc[i][h][c] *= f, acc[i][h][2 + c] *= f;
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = key0 + g + 8 * (j >> 1), last = walk.pos[8 * n + 2 * t + (j & 1)];
+                        if (key > last || (A.window && key <= last - A.window)) x[j] = -INFINITY;
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    p[j] = ex2(s[j] - ref[j & 1]);
-                    pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
+                    p[j] = ex2(x[j]);
+                    pv[j] = p[j] * up[j >> 1];
                 }
+                if (kEdge) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (x[j] == -INFINITY) pv[j] = 0.f;          // (whatever the value is)
+                }
+                // what is past the reference is found by the weights: infinite, or too large
+                if (__any_sync(kFull, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])) > 0x1p14f)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[n][j] = kEdge && x[j] == -INFINITY ? -INFINITY : s[n][j] * (factor[n][j & 1] * ek[j >> 1]);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float top = fmaxf(s[n][c] + float(int(ex[0] >> 8) - 127), s[n][2 + c] + float(int(ex[1] >> 8) - 127));
+#pragma unroll
+                        for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+                        const float m = fmaxf(ref[n][c], top), f = ex2(ref[n][c] - m);
+                        ref[n][c] = m;
+                        l[n][c] *= f;
+#pragma unroll
+                        for (int i = 0; i < kI; ++i)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) acc[n][i][h][c] *= f, acc[n][i][h][2 + c] *= f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p[j] = ex2(s[n][j] - ref[n][j & 1]);
+                        pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
+                    }
+                }
+                l[n][0] += p[0] + p[2];
+                l[n][1] += p[1] + p[3];
+                w[n][0] = transposed(half2_of(pv[0], pv[1]));
+                w[n][1] = transposed(half2_of(pv[2], pv[3]));
             }
-            l[0] += p[0] + p[2];
-            l[1] += p[1] + p[3];
-            w[0] = transposed(half2_of(pv[0], pv[1]));
-            w[1] = transposed(half2_of(pv[2], pv[3]));
             // output
 #pragma unroll
             for (int ph = 0; ph < P; ++ph) {
@@ -503,9 +664,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     }
                 }
                 // (a head's products add to its own columns)
-                uint32_t wh[2];
+                uint32_t wh[NT][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) wh[h] = P == 2 && (g >> 2) != ph ? 0u : w[h];
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) wh[n][h] = P == 2 && (g >> 2) != ph ? 0u : w[n][h];
 #pragma unroll
                 for (int i = 0; i < kI; ++i) {
                     // bytes i of two keys' ratios, as fp16
@@ -522,9 +685,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                                              add2(c & 0x00ff00ffu, centre[0]), add2(c & 0x00f000f0u, centre[1])};
                     const uint32_t hi4[4] = {add2(a8, centre[0]), add2(a8 & 0x00f000f0u, centre[1]), add2(c8, centre[0]),
                                              add2(c8 & 0x00f000f0u, centre[1])};
-                    const uint32_t b0 = mul2(wh[0], r0), b1 = mul2(wh[1], r1);
-                    mma(acc[i][0], lo4, b0, b1);
-                    mma(acc[i][1], hi4, b0, b1);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t b0 = mul2(wh[n][0], r0), b1 = mul2(wh[n][1], r1);
+                        mma(acc[n][i][0], lo4, b0, b1);
+                        mma(acc[n][i][1], hi4, b0, b1);
+                    }
                 }
             }
         };
@@ -568,32 +734,35 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             if (item_at < walk.begin && warp_in == 0) runs[0] = info;
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float sum = l[c];
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int o = 4; o < 32; o *= 2) sum += __shfl_xor_sync(kFull, sum, o);
-            if (__any_sync(kFull, broken)) sum = __int_as_float(0x7fffffff);
-            const int col = 2 * t + c, mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col;
-            if (row >= walk.rows) continue;
-            const float f = whole ? (sum == 0.f ? 0.f : 0x1p16f / sum) : 0x1p16f;
-            if (whole) {
-                const int r = walk.tile * R + row, token = r / A.G;
-                __nv_bfloat16* to = A.out + ((size_t(walk.first + token) * A.c.hkv + walk.head + mine) * A.G + r - token * A.G) * D;
+            for (int c = 0; c < 2; ++c) {
+                float sum = l[n][c];
 #pragma unroll
-                for (int i = 0; i < kI; ++i) {
-                    const __nv_bfloat162 x0 = __floats2bfloat162_rn((acc[i][0][c] - acc[i][0][2 + c]) * f, acc[i][0][2 + c] * (f * 0.0625f));
-                    const __nv_bfloat162 x1 = __floats2bfloat162_rn((acc[i][1][c] - acc[i][1][2 + c]) * f, acc[i][1][2 + c] * (f * 0.0625f));
-                    *reinterpret_cast<uint2*>(to + 32 * i + 4 * g) =
-                        make_uint2(reinterpret_cast<const uint32_t&>(x0), reinterpret_cast<const uint32_t&>(x1));
+                for (int o = 4; o < 32; o *= 2) sum += __shfl_xor_sync(kFull, sum, o);
+                if (__any_sync(kFull, broken)) sum = __int_as_float(0x7fffffff);
+                const int col = 8 * n + 2 * t + c, mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col;
+                if (row >= walk.rows) continue;
+                const float f = whole ? (sum == 0.f ? 0.f : 0x1p16f / sum) : 0x1p16f;
+                if (whole) {
+                    const int r = walk.tile * R + row, token = r / A.G;
+                    __nv_bfloat16* to = A.out + ((size_t(walk.first + token) * A.c.hkv + walk.head + mine) * A.G + r - token * A.G) * D;
+#pragma unroll
+                    for (int i = 0; i < kI; ++i) {
+                        const __nv_bfloat162 x0 = __floats2bfloat162_rn((acc[n][i][0][c] - acc[n][i][0][2 + c]) * f, acc[n][i][0][2 + c] * (f * 0.0625f));
+                        const __nv_bfloat162 x1 = __floats2bfloat162_rn((acc[n][i][1][c] - acc[n][i][1][2 + c]) * f, acc[n][i][1][2 + c] * (f * 0.0625f));
+                        *reinterpret_cast<uint2*>(to + 32 * i + 4 * g) =
+                            make_uint2(reinterpret_cast<const uint32_t&>(x0), reinterpret_cast<const uint32_t&>(x1));
+                    }
+                } else {
+                    float* to = state + col * (D + 4);
+#pragma unroll
+                    for (int i = 0; i < kI; ++i)
+                        *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
+                            make_float4((acc[n][i][0][c] - acc[n][i][0][2 + c]) * f, acc[n][i][0][2 + c] * (f * 0.0625f),
+                                        (acc[n][i][1][c] - acc[n][i][1][2 + c]) * f, acc[n][i][1][2 + c] * (f * 0.0625f));
+                    if (g == 0) to[D] = ref[n][c], to[D + 1] = sum;
                 }
-            } else {
-                float* to = state + col * (D + 4);
-#pragma unroll
-                for (int i = 0; i < kI; ++i)
-                    *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
-                        make_float4((acc[i][0][c] - acc[i][0][2 + c]) * f, acc[i][0][2 + c] * (f * 0.0625f),
-                                    (acc[i][1][c] - acc[i][1][2 + c]) * f, acc[i][1][2 + c] * (f * 0.0625f));
-                if (g == 0) to[D] = ref[c], to[D + 1] = sum;
             }
         }
     }
@@ -611,7 +780,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         for (int w = w0; w <= last; ++w)
             st.add(places[w - worker0][r && w == w0 ? info.z >> 30 & 1 : 0] + col * (D + 4));
         if (r && info.w < worker0 + active)
-            st.write(A.out + row_of<S::kRows>(A, info, mine, row) * D);
+            st.write(A.out + row_of<S>(A, info, mine, row) * D);
         else
             st.keep(A.joined + ((size_t(blockIdx.x) * 2 + (r ? 1 : 0)) * S::kCols + col) * (D + 4));
     }
@@ -622,6 +791,27 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         going.w = min(going.w, int(gridDim.x) - 1);
         A.begun[blockIdx.x] = going;
     }
+}
+
+// Joins the states of a tile whose keys went to several CTAs: a block per row.
+template <class S>
+__global__ void __launch_bounds__(kJoin) join_kernel(const Args A) {
+    constexpr int D = S::D, kEach = kJoin / 8;
+    __shared__ __align__(16) float part[kEach][D + 4];
+    wait_for_previous();
+    const int group = threadIdx.x / 8, col = blockIdx.y, mine = S::P == 2 ? col >> 2 : 0, row = S::P == 2 ? col & 3 : col;
+    const int4 info = A.begun[blockIdx.x];
+    if (info.x < 0 || row >= info.y >> 24) return;
+    State<D> st;
+#pragma unroll 2
+    for (int c = blockIdx.x + group; c <= info.w; c += kEach)
+        st.add(A.joined + ((size_t(c) * 2 + (c == blockIdx.x ? 1 : 0)) * S::kCols + col) * (D + 4));
+    st.keep(part[group]);
+    __syncthreads();
+    if (group) return;
+    State<D> all;
+    for (int k = 0; k < kEach && k <= info.w - int(blockIdx.x); ++k) all.add(part[k]);
+    all.write(A.out + row_of<S>(A, info, mine, row) * D);
 }
 
 // The current device's multiprocessors, with the kernels' shared memory allowed.
@@ -650,18 +840,19 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
     // (no more work than one CTA takes, however long the sequences are: nothing to join)
     const long tiles = a.s.batch + long(a.s.rows) * a.G / S::kRows, stages = ((long(a.s.width) << a.c.log_page) + S::kKeys - 1) / S::kKeys;
     if (rc || tiles * (a.c.hkv / S::P) * (stages + S::kBegin) <= long(S::kLeast) * S::kWarps) return rc;
-    return dependent(join_kernel<S::D, S::kRows, S::P>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
+    return dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
 
 template <int D>
 int run(const Args& a, void* scratch, cudaStream_t stream) {
     // By the rows of a kv head that a sequence has on average: up to four share the
-    // columns with those of the next head; more than eight make the other kernel's
-    // conversion worth its while (but for heads of 256, whose rows it has no room for).
+    // columns with those of the next head, more than eight take sixteen columns (the
+    // codes are made operands once for both halves).
     const long rows = long(a.s.rows) * a.G, all = a.s.batch;
-    if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 2>>(a, scratch, stream);
-    if (D < 256 && rows > 8 * all) return many_rows(a, D, scratch, stream);
-    return launch<Shape<D, 1>>(a, scratch, stream);
+    if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream);
+    if constexpr (D < 256)
+        if (rows > 8 * all) return launch<Shape<D, 2, 1>>(a, scratch, stream);
+    return launch<Shape<D, 1, 1>>(a, scratch, stream);
 }
 
 }  // namespace
@@ -674,11 +865,11 @@ using namespace decoder;
 extern "C" long decoder_page_attention_scratch(int d) {
     if (d != 64 && d != 128 && d != 256) return -long(cudaErrorInvalidValue);
     int sms = 0;
-    long many = 0;
-    cudaError_t e = prepared<Shape<64, 1>>(&sms);
-    if (e == cudaSuccess && d < 256) e = many_rows_scratch(d, &many);
+    const cudaError_t e = prepared<Shape<64, 1, 1>>(&sms);
     if (e != cudaSuccess) return -long(e);
-    return std::max(many, d == 64 ? scratch_of<Shape<64, 1>>(sms) : d == 128 ? scratch_of<Shape<128, 1>>(sms) : scratch_of<Shape<256, 1>>(sms));
+    return d == 64    ? std::max(scratch_of<Shape<64, 2, 1>>(sms), scratch_of<Shape<64, 1, 1>>(sms))
+           : d == 128 ? std::max(scratch_of<Shape<128, 2, 1>>(sms), scratch_of<Shape<128, 1, 1>>(sms))
+                      : scratch_of<Shape<256, 1, 1>>(sms);
 }
 
 // q [rows][hq][d] (its strides: token, head) over the layer's pages; out [rows][hq][d].
