@@ -44,7 +44,7 @@ using splice::tc::smem_u32;
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNone = -1e30f;         // the reference of rows that have seen nothing
+constexpr float kNone = -3e38f;         // the reference of rows that have seen nothing
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
 
 struct Args {
@@ -154,16 +154,20 @@ __device__ __forceinline__ long quotient(long a, long b) {
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
 // stages of keys, and kBegin more, as the one that sees most.
 struct Seq {
-    int first, new_, length, tiles, blocks;     // (its first row of q; its tokens, its keys)
+    int first, new_, base, length, tiles, blocks;       // (its first row of q, its rows; the first one's position)
+    bool broken;                                        // (it is longer than its pages are)
 };
 
 template <class S>
 __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     Seq q;
-    const int first = max(0, min(A.s.starts[b], A.s.rows)), end = max(first, min(A.s.starts[b + 1], A.s.rows));
-    q.first = first;
-    q.new_ = end - first;
-    q.length = max(0, A.s.lengths[b]);
+    const int from = A.s.starts[b], to = A.s.starts[b + 1], length = A.s.lengths[b];
+    const long room = long(A.s.width) << A.c.log_page;
+    q.first = max(0, min(from, A.s.rows));
+    q.new_ = max(0, min(to, A.s.rows) - q.first);
+    q.broken = length > room;
+    q.length = int(min(long(max(0, length)), room));    // (no more keys than there are places, whatever it says)
+    q.base = q.length - (to - from) + (q.first - from);
     q.tiles = int((long(q.new_) * A.G + S::kRows - 1) / S::kRows);
     int blocks = q.length / S::kKeys + (q.length % S::kKeys != 0);
     if (A.window) blocks = min(blocks, int((long(A.window) + (S::kRows + A.G - 2) / A.G + 2 * S::kKeys - 2) / S::kKeys));
@@ -327,7 +331,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const int j1 = int(min(long(sq.blocks), j0 + (walk.end - x)));
         const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
-        const int base = sq.length - sq.new_;
+        const int base = sq.base;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
         const int kb0 = A.window ? max(0, first_pos - A.window + 1) / S::kKeys : 0;
         const int kb_end = min(kb0 + j1 - S::kBegin, (last_pos + S::kKeys) / S::kKeys);
@@ -364,7 +368,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             }
         }
         const uint8_t *k_in, *late_in, *rest_in[kMore];         // (late: the stage's second half)
-        bool broken = false;                     // a page that is none of the cache's
+        bool broken = sq.broken;                 // (or with a page that is none of the cache's)
         auto locate = [&]() {
             const int i = place(kb_in);
             if ((i & 31) == 0) {
@@ -593,7 +597,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             for (int n = 0; n < NT; ++n) {
                 float x[4], p[4], pv[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = fmaf(s[n][j], factor[n][j & 1] * ek[j >> 1], -ref[n][j & 1]);
+                for (int j = 0; j < 4; ++j) {
+                    // (rounded before the reference is taken off, which was rounded so: of two
+                    // scores in the millions the one that is the reference leaves 0)
+                    s[n][j] = __fmul_rn(s[n][j], factor[n][j & 1] * ek[j >> 1]);
+                    x[j] = __fsub_rn(s[n][j], ref[n][j & 1]);
+                }
                 if (kEdge) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -615,10 +624,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 if (__any_sync(kFull, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])) > 0x1p14f)) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        s[n][j] = kEdge && x[j] == -INFINITY ? -INFINITY : s[n][j] * (factor[n][j & 1] * ek[j >> 1]);
+                        if (kEdge && x[j] == -INFINITY) s[n][j] = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float top = fmaxf(s[n][c] + float(int(ex[0] >> 8) - 127), s[n][2 + c] + float(int(ex[1] >> 8) - 127));
+                        float top = fmaxf(__fadd_rn(s[n][c], float(int(ex[0] >> 8) - 127)), __fadd_rn(s[n][2 + c], float(int(ex[1] >> 8) - 127)));
 #pragma unroll
                         for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
                         const float m = fmaxf(ref[n][c], top), f = ex2(ref[n][c] - m);
@@ -631,7 +640,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        p[j] = ex2(s[n][j] - ref[n][j & 1]);
+                        p[j] = ex2(__fsub_rn(s[n][j], ref[n][j & 1]));
                         pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
                     }
                 }

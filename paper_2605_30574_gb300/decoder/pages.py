@@ -174,6 +174,12 @@ def _overlaps(t):
     return any(s < (sizes[i - 1][0] * sizes[i - 1][1] if i else 1) for i, (s, _) in enumerate(sizes))
 
 
+def _meet(a, b):
+    """Whether the places from the first to the last of both have any in common."""
+    (a0, a1), (b0, b1) = ((t.data_ptr(), t.data_ptr() + 2 * sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 2) for t in (a, b))
+    return a.numel() > 0 and b.numel() > 0 and a0 < b1 and b0 < a1
+
+
 def _target(what, name, t):
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{what}: {name} requires a gradient and is written to")
@@ -211,8 +217,8 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
 
 def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
                lengths: torch.Tensor) -> None:
-    """Writes the values that the newest tokens are held as to k and v [tokens][heads][d];
-    with ``starts`` that go by the lengths, those of whole sequences.  A token before
+    """Writes the values that the newest tokens are held as to k and v [tokens][heads][d], which
+    have no place in common; with ``starts`` that go by the lengths, those of whole sequences.  A token before
     position 0 is zeros, one in a page that is none of the cache's, or behind the
     table's, NaN."""
     what = "load_pages"
@@ -226,6 +232,8 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
+    if rows and k.data_ptr() == v.data_ptr():
+        raise ValueError(f"{what}: k and v are in the same place")
     if not rows or not where[-1]:
         return
     if cache.device.index != _current_device():
@@ -249,9 +257,10 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     keys and values, the newest tokens' own included (which are stored before): token i
     of the n newest of a sequence is at position p = length - n + i and sees those up to
     p, with ``window`` above 0 only those above p - window.  Query head h reads kv head
-    h // (Hq / heads).  One token that sees nothing gives 0; a page among a sequence's that
-    is none of the cache's, or is missing from the table, makes its rows NaN.  ``scale`` is
-    1 / sqrt(d) by default.
+    h // (Hq / heads).  A token that sees nothing gives 0; one whose keys or values hold NaN,
+    NaN.  A page that a row looks into and that is none of the cache's makes its tile's rows
+    NaN, and a sequence longer than the table is wide all its rows.  ``scale`` is
+    1 / sqrt(d) by default; scores have to be numbers of fp32.
 
     Returns [tokens][Hq][d], bf16: ``out`` (contiguous) if given, else a new tensor whose
     rows outside of all sequences hold anything.  Scores and sums are in fp32, q to the
@@ -274,6 +283,8 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
         _target(what, "out", out)
         if not out.is_contiguous() or out.is_neg() or out.data_ptr() & 15:
             raise ValueError(f"{what}: out must be contiguous, at a 16-byte boundary")
+        if _meet(out, q):
+            raise ValueError(f"{what}: out and q overlap")
     if cache.device.index != _current_device():
         with torch.cuda.device(cache.device):
             return page_attention(cache, layer, q, table, starts, lengths, scale=scale, window=window, out=out)

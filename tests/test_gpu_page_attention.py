@@ -191,6 +191,23 @@ def test_what_no_row_sees_may_be_nan():
     check(cache, queries(1, 4, 64), where, window=32)
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size(sign):
+    """One key's score is far above the others', all of them far below (or above) 0."""
+    cache, where = filled([100], [1], 1, 64, 64)
+    k, v = torch.zeros(100, 1, 64, device="cuda"), queries(100, 1, 64, 6)
+    k[:, 0, 0] = sign * 2.0 ** 60 * torch.linspace(1, 2, 100, device="cuda")
+    q = torch.zeros(1, 2, 64, dtype=BF, device="cuda")
+    q[..., 0] = 2.0 ** 50
+    P.store_pages(cache, 0, k.to(BF), v, where[0], ints(0, 100), ints(100))
+    got = P.page_attention(cache, 0, q, *where, scale=1.0)
+    held_k, held_v = values(cache, 0)[int(where[0][0, 0]), :, 0, :, :], values(cache, 0)[int(where[0][0, 1]), :, 0, :36, :]
+    kk, vv = (torch.cat([held_k[i], held_v[i]]) for i in (0, 1))
+    best = kk[:, 0] == kk[:, 0].max()                  # (equal scores share)
+    want = vv[best].mean(0)
+    assert bool(((got[0].cpu().double() - want).abs() <= 2.0 ** -7 * vv[best].abs().mean(0) + 2.0 ** -10).all())
+
+
 @pytest.mark.parametrize("which", ["k", "v", "q"])
 def test_nan_that_is_seen(which):
     cache, where = filled([40, 40], [2, 2], 2, 64, 64)
@@ -220,6 +237,20 @@ def test_pages_that_are_none_make_their_rows_nan():
     lengths[2] = 16 * table.shape[1] + 1
     got = P.page_attention(cache, 0, queries(4, 4, 64), table, starts, lengths)
     assert bool(((got[0].cpu().double() - want[0]).abs() <= bound[0]).all()) and bool(got[1:].isnan().all())
+
+
+def test_lengths_and_starts_that_say_too_much():
+    """A length past the table's pages: its rows are NaN, and no more keys are gone through
+    than the table has.  Starts past the rows that there are: those that there are."""
+    cache, (table, starts, lengths) = filled([40, 40], [1, 3], 2, 64, 16)
+    want, bound = definition(cache, queries(4, 4, 64), table, starts, lengths, 1 / 8, 0)
+    long_ = lengths.clone()
+    for n in (16 * table.shape[1] + 1, 1 << 20, (1 << 31) - 1):
+        long_[0] = n
+        got = P.page_attention(cache, 0, queries(4, 4, 64), table, starts, long_)
+        assert bool(got[0].isnan().all()) and bool(((got[1:].cpu().double() - want[1:]).abs() <= bound[1:]).all())
+    got = P.page_attention(cache, 0, queries(4, 4, 64)[:3].contiguous(), table, starts, lengths)
+    assert bool(((got.cpu().double() - want[:3]).abs() <= bound[:3]).all())
 
 
 @pytest.mark.parametrize("how", ["joined", "transposed", "unaligned", "negated"])

@@ -160,8 +160,15 @@ def test_offsets_past_32_bits():
     to = [torch.empty_like(k) for _ in range(2)]
     P.load_pages(cache, 0, *to, *where)
     assert same(to[0], expected(k)) and same(to[1], expected(v))
+    P.store_pages(cache, 0, *rows(256, 1, 256, 4), ints([pages - 1]), ints(0, 256), ints(256))
     P.copy_pages(cache, [pages - 1], [pages - 2])
     assert torch.equal(cache.codes[0, -1], cache.codes[0, -2])
+    # the copy as the last page of a cache of its own, which small offsets reach
+    small = P.PageCache(*(t[:, -2:].contiguous() for t in (cache.codes, cache.ratios, cache.exponents)))
+    q = rows(2, 4, 256, 5)[0]
+    for window in (0, 50):
+        got, want = (P.page_attention(c, 0, q, ints([i]), ints(0, 2), ints(256), window=window) for c, i in ((cache, pages - 1), (small, 0)))
+        assert torch.equal(got, want) and not bool(want.isnan().any())
 
 
 @pytest.mark.parametrize("layers,heads,d,page,n", [(1, 1, 64, 16, 1), (3, 2, 128, 32, 5), (2, 3, 256, 16, 1000), (36, 8, 128, 64, 3)])

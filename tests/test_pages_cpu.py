@@ -152,6 +152,12 @@ def test_outputs_that_are_refused(launched):
                        (q[:1], "out must be"), (q.float(), "bf16"), (q.clone().requires_grad_(), "gradient"), (torch._neg_view(q.clone()), "contiguous")):
         with pytest.raises((TypeError, ValueError), match=match):
             P.page_attention(cache, 0, q, *w, out=bad)
+    flat = torch.zeros(1024, dtype=BF)
+    for a, out in ((q, q), (flat[:512].view(2, 4, 64), flat[256:768].view(2, 4, 64))):
+        with pytest.raises(ValueError, match="overlap"):
+            P.page_attention(cache, 0, a, *w, out=out)
+    with pytest.raises(ValueError, match="same place"):
+        P.load_pages(cache, 0, k, k, *w)
     assert not launched
     with torch.no_grad():
         P.load_pages(cache, 0, k.requires_grad_(), torch.zeros(2, 2, 64, dtype=BF), *w)
