@@ -8,25 +8,45 @@
 // and what a kernel may spend on making operands of 4-bit codes is about three
 // instructions of a lane to an element.  Products therefore take the codes as they
 // are: a nibble n = c + 8, masked in place, is the fp16 number n 2^-24 (bits 0 to 3) or
-// 16 n 2^-24 (bits 4 to 7), so that one shift and four ANDs make eight elements.
+// 16 n 2^-24 (bits 4 to 7).  In order of what each measured, at 512 sequences of 4224
+// tokens, 32 / 8 heads of 128 (2.4 GB; 355 us at the copy rate, now 375):
 //
-//  * Scores: S[key][row], keys on the 16-row side of m16n8k16, the rows (eight, or twice
-//    eight) on the other.  q is scaled to 2^14 by a power of two and rounded to fp16 (all
+//  * Scores: S[key][row], keys on the 16-row side of m16n8k16, eight rows on the other
+//    (or twice eight).  q is scaled to 2^14 by a power of two and rounded to fp16 (all
 //    of bf16's bits down to 2^-28 of the row's largest), with 1/16 where the code comes
-//    16-fold; a group's sum starts from -8 sum q, which takes the 8 out of c + 8; groups
-//    are added up in fp32 by their ratios.
+//    16-fold.  Groups of 32 are added up in fp32 by their ratios, from -8 sum q r, which
+//    takes the 8 out of c + 8 and is one product more, of the ratios and sum q in three
+//    fp16 terms.
 //  * Output: O[dim][row].  P as the fp16 operand has V's scales in it, so it is taken
 //    relative to the largest of (score + E of the value's row), and not of the score:
 //    then no product of a weight and a scale is above 2^15, and one that is rounded or
 //    lost below fp16's normal range is 2^-29 of the largest.  Codes have their 8
 //    subtracted (exactly): O would otherwise carry it through sums of thousands of keys.
+//    Subtracting the weights' sums by the tensor core instead, 417 us for 398.  The
+//    second nibble of a byte is taken off the first's sum, not masked out of it: 376 for
+//    386.
 //  * The transposition from S's layout to an operand is movmatrix; a key's four lanes and
 //    a row's eight are those of both.
+//  * Up to four rows to a kv head: two heads to a product, four columns each, with zeros
+//    for the other's in q and in P, so that the softmax is done once for both: 417 for
+//    482 (306 -> 261 instructions for 16 keys of a head).  More than eight rows: sixteen
+//    columns, as the codes are made operands once: 64 rows 52 us for 56, 18 rows 57 for 59.
+//  * Keys come through a ring in shared memory, 16 bytes by cp.async to a lane; bulk copies
+//    took 25 instructions each, one after another, 681 us against 623.  A stage is 32
+//    keys, or 16 of two heads: 482 against 562 with 16.
+//  * What is not needed in the loop over the keys is in shared memory (Walk): at 168
+//    registers the loop then spills and recomputes nothing (286 -> 276 instructions); 16
+//    warps of 128 registers, 415 us for 388.
 //
-// Work: all (sequence, kv head, tile of rows, 16 keys) in one line, an even share to
+// What bounds it now is issue: 64% of all slots, the ALU 62% (profile), of what HBM's rate
+// would allow about 95%.
+//
+// Work: all (sequence, kv head, tile of rows, stage of keys) in one line, an even share to
 // each warp, whatever the sequences' lengths, which only the device knows.  A tile whose
-// keys fall to several warps leaves a state (m, l, O) per warp, and a second kernel joins
-// them in the warps' order: the same inputs give the same bits.
+// keys fall to several warps leaves a state (m, l, O) per warp; a CTA joins its warps', and
+// a second kernel the CTAs', in their order: the same inputs give the same bits.  131072
+// tokens of one sequence: 36 us, 12 of which are set-up, joins and the SMs' uneven speed
+// (their last warps end 8 us apart); all in the second kernel it was 109.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -66,10 +86,12 @@ struct Shape {
     static constexpr int D = D_, NT = NT_, P = P_, kI = D / 32;
     static constexpr int kCols = 8 * NT, kRows = kCols / P;         // (rows of a head, to a tile)
     static constexpr int kKeys = 32 / P;                            // keys to a stage: two runs of 16, or of two heads
-    static constexpr int kBegin = D == 256 ? 2 : 2 * P;             // stages that a tile's begin and end take as long as
+    // stages that a tile's begin and end take as long as (200 sequences of 1 to 9000 tokens: 50
+    // us; with 2 for 4 57, with 7 52)
+    static constexpr int kBegin = D == 256 ? 2 : 2 * P;
     static constexpr int kLeast = 32 / kKeys;                       // stages to a warp, at least
     // warps to an SM, all of one CTA: as many as their registers allow
-    static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 10 : 16;
+    static constexpr int kWarps = D == 256 ? 8 : D == 128 ? (NT == 2 ? 8 : 12) : NT == 2 ? 12 : 16;
     static constexpr int kThreads = 32 * kWarps;
     // a stage of a warp's ring: where its parts are
     static constexpr int kStages = D == 256 ? 2 : D == 128 ? 3 : 4;
@@ -855,8 +877,10 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
 template <int D>
 int run(const Args& a, void* scratch, cudaStream_t stream) {
     // By the rows of a kv head that a sequence has on average: up to four share the
-    // columns with those of the next head, more than eight take sixteen columns (the
-    // codes are made operands once for both halves).
+    // columns with those of the next head (64 sequences of 4000 tokens, one row of 128: 60
+    // us for 65; 256 with four of 64: 118 for 134; 64 with two of 256: 49 for 51), more
+    // than eight take sixteen columns (24 sequences of up to 16 tokens with four rows of
+    // 128: 52 for 56; but for 256, for which there are no registers).
     const long rows = long(a.s.rows) * a.G, all = a.s.batch;
     if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream);
     if constexpr (D < 256)

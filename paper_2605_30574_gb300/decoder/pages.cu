@@ -3,6 +3,13 @@
 // All three are bound by HBM: a row of 128 elements is 256 bytes in bf16 and 69 in a
 // page, and a copied page is read and written once.  Small calls are latency: the
 // search for a row's sequence, its page, the access.
+//
+// 16.5k tokens of 8 heads of 128, ragged: stored in 27 us, loaded in 24 (84 MB each: 12.5 at
+// the copy rate), what a row's scales cost in instructions and a warp's chain of four
+// loads before its first row.  Measured on the way, both together: 129 with a warp to a
+// row, 79 with eight rows on their way in a warp, 70 without divisions (below), 55 with
+// rows of a page a constant apart, 51 with sixteen elements to a lane.  36 layers of 340
+// pages copied: 254 us (1.73 GB, the copy rate).
 #include "pages.cuh"
 
 #include "decoder.h"
