@@ -355,8 +355,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
         const int base = sq.base;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
-        const int kb0 = A.window ? max(0, first_pos - A.window + 1) / S::kKeys : 0;
-        const int kb_end = min(kb0 + j1 - S::kBegin, (last_pos + S::kKeys) / S::kKeys);
+        // (positions and windows may be close to 2^31)
+        const int kb0 = A.window && first_pos >= A.window ? (first_pos - A.window + 1) / S::kKeys : 0;
+        const int kb_end = min(kb0 + j1 - S::kBegin, last_pos < 0 ? 0 : last_pos / S::kKeys + 1);
         int kb = kb0 + max(0, j0 - S::kBegin), kb_in = kb;
         __syncwarp();
         if (lane == 0) {
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int key = key0 + 2 * t + (j & 1) + 8 * (j >> 1);
-                        if (key > last_pos || (A.window && key <= first_pos - A.window)) {
+                        if (key > last_pos || (A.window && key <= max(0, first_pos) - A.window)) {
                             if constexpr (kI == 2) vr[j >> 1][0] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
                             if constexpr (kI > 2)
 #pragma unroll

@@ -84,8 +84,8 @@ class PageCache:
         self.codes, self.ratios, self.exponents, self.device = codes, ratios, exponents, codes.device
         self.layers, self.pages, _, self.kv_heads, self.page, half = codes.shape
         self.head_dim = 2 * half
-        self._described = _Described(codes.data_ptr(), ratios.data_ptr(), exponents.data_ptr(), self.layers, self.pages, self.kv_heads,
-                                     self.head_dim, _PAGES[self.page])
+        self._places = codes.data_ptr(), ratios.data_ptr(), exponents.data_ptr()
+        self._described = _Described(*self._places, self.layers, self.pages, self.kv_heads, self.head_dim, _PAGES[self.page])
         self._at = ctypes.addressof(self._described)
 
     @classmethod
@@ -105,8 +105,9 @@ class PageCache:
         """The address of the cache's description, for a layer that there is."""
         if not isinstance(layer, int) or not 0 <= layer < self.layers:
             raise ValueError(f"{what}: the cache has layers 0 to {self.layers - 1}")
-        if not (self.codes.data_ptr() and self.ratios.data_ptr() and self.exponents.data_ptr()):
-            raise ValueError(f"{what}: the cache has no memory")
+        places = self.codes.data_ptr(), self.ratios.data_ptr(), self.exponents.data_ptr()
+        if places != self._places:
+            raise ValueError(f"{what}: the cache has {'other' if all(places) else 'no'} memory than it was made with")
         return self._at
 
 
@@ -120,7 +121,7 @@ def _where(what, cache, table, starts, lengths):
                 and starts.shape == (B + 1,) and lengths.shape == (B,) and table.is_contiguous() and starts.is_contiguous()
                 and lengths.is_contiguous() and not (table.is_neg() or starts.is_neg() or lengths.is_neg())):
             at = (table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), W, B)
-            if at[0] and at[1] and at[2] and W:
+            if at[0] and at[1] and at[2] and W and not W >> 31 and not B >> 30:
                 return at
     except (AttributeError, ValueError):
         pass
@@ -137,6 +138,8 @@ def _where(what, cache, table, starts, lengths):
         raise ValueError(f"{what}: of B sequences, table must be [B][W], starts [B + 1] and lengths [B]")
     if B and not W:
         raise ValueError(f"{what}: the table has no pages")
+    if W >> 31 or B >> 30:
+        raise ValueError(f"{what}: fewer than 2^31 pages to a sequence and 2^30 sequences")
     return (table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), W, B)
 
 
@@ -406,19 +409,19 @@ class PageTables:
             added.append(-(-(length + n) // page) - len(held))
         if len(copied) + sum(added) > len(self._free):
             raise RuntimeError(f"PageTables.extend: {len(copied) + sum(added)} pages, and {len(self._free)} are free")
-        src, dst = [], []
-        for i, last in copied:
-            src.append(last)
-            dst.append(self._free.pop())
+        # (a copy that fails changes nothing either)
+        dst = self._free[len(self._free) - len(copied):]
+        copy_pages(self.cache, [last for _, last in copied], dst)
+        del self._free[len(self._free) - len(copied):]
+        for (i, last), to in zip(copied, dst):
             self._users[last] -= 1
-            self._users[dst[-1]] = 1
-            self._pages[i][-1] = dst[-1]
+            self._users[to] = 1
+            self._pages[i][-1] = to
         for i, n, new in zip(ids, more, added):
             for _ in range(new):
                 self._pages[i].append(self._free.pop())
                 self._users[self._pages[i][-1]] = 1
             self._lengths[i] += n
-        copy_pages(self.cache, src, dst)
 
     def fork(self, sequence: int, n: int = 1) -> List[int]:
         """``n`` sequences that hold what this one does; nothing is copied yet."""

@@ -253,6 +253,31 @@ def test_lengths_and_starts_that_say_too_much():
     assert bool(((got.cpu().double() - want[:3]).abs() <= bound[:3]).all())
 
 
+@pytest.mark.parametrize("d,heads,G", [(64, 2, 4), (128, 1, 8), (64, 1, 12)])
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 8, 1 << 30])
+def test_windows_wider_than_all(d, heads, G, window):
+    """Rows before position 0 next to rows that see keys."""
+    cache, where = filled([5, 40], [8, 3], heads, d, 16)
+    check(cache, queries(11, heads * G, d), where, window=window)
+
+
+@pytest.mark.parametrize("d,heads,G", [(64, 2, 4), (128, 1, 8), (64, 1, 12)])
+def test_lengths_to_the_last(d, heads, G):
+    """2^31 - 1 tokens, in pages that come again and again, of which a window sees the last."""
+    page, W, tail = 256, 1 << 23, 5
+    cache, (table, starts, _) = filled([page * tail], [2], heads, d, page)
+    table = table[:, torch.arange(W, device="cuda") % tail].contiguous()
+    lengths, last = ints((1 << 31) - 1), table[:, -tail:].contiguous()
+    q, scale = queries(2, heads * G, d), d ** -0.5
+    got = P.page_attention(cache, 0, q, table, starts, lengths, window=1000)
+    want, bound = definition(cache, q, last, starts, [page * tail - 1], scale, 1000)
+    assert bool(((got.cpu().double() - want).abs() <= bound).all())
+    k, v, kk, vv = (torch.empty(2, heads, d, dtype=BF, device="cuda") for _ in range(4))
+    P.load_pages(cache, 0, k, v, table, starts, lengths)
+    P.load_pages(cache, 0, kk, vv, last, starts, ints(page * tail - 1))
+    assert torch.equal(k, kk) and torch.equal(v, vv)
+
+
 @pytest.mark.parametrize("how", ["joined", "transposed", "unaligned", "negated"])
 def test_strides_of_q(how):
     cache, where = filled([40, 9], [1, 3], 2, 128, 16)

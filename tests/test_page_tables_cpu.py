@@ -115,6 +115,26 @@ def test_too_few_pages_change_nothing(monkeypatch):
         assert (m.tables.pages(a), m.tables.pages(b), m.tables.free, m.tables.length(a)) == before
 
 
+def test_a_copy_that_fails_changes_nothing(monkeypatch):
+    m = Model(monkeypatch, pages=6)
+    a = m.tables.add(20)
+    m.tokens[a] = []
+    m.write(a, 20)
+    m.tables.fork(a)
+
+    def fails(*_):
+        raise RuntimeError("CUDA error 1")
+    before = (m.tables.pages(a), m.tables.free, m.tables.length(a))
+    with monkeypatch.context() as patch:
+        patch.setattr(P, "copy_pages", fails)
+        for call in (lambda: m.tables.extend([a], 20), m.tables.compact):
+            with pytest.raises(RuntimeError, match="CUDA error 1"):
+                call()
+            assert (m.tables.pages(a), m.tables.free, m.tables.length(a)) == before
+    m.tables.extend([a], 20)
+    assert m.tables.free == 6 - 2 - 2 and m.tables.length(a) == 40
+
+
 def test_tensors(launched):  # noqa: F811
     t = P.PageTables(OnCpu(pages=12))
     a, b = t.add(33), t.add(0)

@@ -90,6 +90,34 @@ def test_a_cache_that_was_given_back(launched):
     assert not launched
 
 
+@pytest.mark.parametrize("name", ["codes", "ratios", "exponents"])
+def test_a_cache_whose_tensors_are_others(launched, name):
+    cache = OnCpu()
+    setattr(cache, name, getattr(cache, name).clone())
+    for call in calls(cache, where()) + (lambda: P.copy_pages(cache, [0], [1]),):
+        with pytest.raises(ValueError, match="other memory"):
+            call()
+    assert not launched
+
+
+def test_tables_of_too_many(launched):
+    wide, many = (torch.empty(n, dtype=torch.int32, device="meta") for n in (1 << 31, 1 << 30))
+    cache = OnCpu()
+
+    class There(torch.Tensor):
+        """As a tensor that has memory."""
+        device = cache.device
+
+        def data_ptr(self):
+            return 16
+    for table, starts, lengths in ((wide.view(1, -1), 2, 1), (many.view(-1, 1), (1 << 30) + 1, 1 << 30)):
+        w = [t.as_subclass(There) for t in (table, *(torch.empty(n, dtype=torch.int32, device="meta") for n in (starts, lengths)))]
+        for call in calls(cache, w):
+            with pytest.raises(ValueError, match="fewer than 2"):
+                call()
+    assert not launched
+
+
 def test_nothing_to_do(launched):
     cache = OnCpu()
     none = torch.zeros(0, 2, 64, dtype=BF)
