@@ -42,7 +42,8 @@
 // would allow about 95%.
 //
 // Work: all (sequence, kv head, tile of rows, stage of keys) in one line, an even share to
-// each warp, whatever the sequences' lengths, which only the device knows.  A tile whose
+// each warp, whatever the sequences' lengths, which only the device knows.  (Short tiles:
+// an even share of the tiles, not cut, to each CTA; see launch.)  A tile whose
 // keys fall to several warps leaves a state (m, l, O) per warp; a CTA joins its warps', and
 // a second kernel the CTAs', in their order: the same inputs give the same bits.  131072
 // tokens of one sequence: 36 us, 12 of which are set-up, joins and the SMs' uneven speed
@@ -66,6 +67,9 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -3e38f;         // the reference of rows that have seen nothing
 constexpr int kMinWarps = 4;            // warps to a CTA that are given keys, at least
+// Tiles are apart where they have so many stages to a warp at most, and so many more to
+// the one that has most than on the line (see launch).
+constexpr int kMost = 16, kMore = 3;
 
 struct Args {
     PageLayer c;
@@ -74,6 +78,7 @@ struct Args {
     long q_token, q_head;
     __nv_bfloat16* out;
     int G, window;
+    int apart;              // warps to a tile, each tile's to one CTA; 0: all on one line
     float scale;
     float *states, *joined; // of warps [each][columns][d + 4], and of CTAs [each][2][columns][d + 4]
     int4* begun;            // per CTA: the tile whose keys begin with it and go on
@@ -174,7 +179,7 @@ __device__ __forceinline__ long quotient(long a, long b) {
 }
 
 // The sequences' shares of the line of work.  All of a sequence's tiles count as many
-// stages of keys, and kBegin more, as the one that sees most.
+// stages of keys, and kBegin more (none where tiles are apart), as the one that sees most.
 struct Seq {
     int first, new_, base, length, tiles, blocks;       // (its first row of q, its rows; the first one's position)
     bool broken;                                        // (it is longer than its pages are)
@@ -193,14 +198,15 @@ __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     q.tiles = int((long(q.new_) * A.G + S::kRows - 1) / S::kRows);
     int blocks = q.length / S::kKeys + (q.length % S::kKeys != 0);
     if (A.window) blocks = min(blocks, int((long(A.window) + (S::kRows + A.G - 2) / A.G + 2 * S::kKeys - 2) / S::kKeys));
-    q.blocks = max(1, blocks) + S::kBegin;
+    q.blocks = max(1, blocks) + (A.apart ? 0 : S::kBegin);
     return q;
 }
 
 template <class S>
-__device__ __forceinline__ long size_of(const Args& A, const Seq& q) {
-    return long(q.tiles) * (A.c.hkv / S::P) * q.blocks;
-}
+__device__ __forceinline__ long tiles_of(const Args& A, const Seq& q) { return long(q.tiles) * (A.c.hkv / S::P); }
+
+template <class S>
+__device__ __forceinline__ long size_of(const Args& A, const Seq& q) { return tiles_of<S>(A, q) * q.blocks; }
 
 __device__ __forceinline__ void sts16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -215,7 +221,9 @@ __device__ __forceinline__ void cp16(uint32_t to, const uint8_t* from) {
 template <class S>
 struct Walk {
     long x, end, begin, at, item_at;            // on the line: where it is, its share, its sequence's begin, its tile's
+    long origin, each, longer;                  // where the shares begin, their stages, and how many have one more
     int b, line, first, new_, base, head, tile, rows;
+    int worker;                                 // of the first share
     int pos[S::kCols];                          // of the columns' rows
     int ids[64];                                // pages of the sequence, two times 32 places
 };
@@ -273,14 +281,16 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     __shared__ long sums[kThreads / 32];
     __shared__ float* places[S::kWarps][2];     // states of tiles that go on here, and that go on behind this warp
     __shared__ Walk<S> walks[S::kWarps];
-    __shared__ long shares_of[2];               // stages to a worker, and how many have one more
     __shared__ int4 runs[S::kWarps + 1];        // tiles that warps share: the one that goes on here, and each warp's that goes on
     wait_for_previous();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp_in = threadIdx.x / 32;
     const int run = (A.s.batch + kThreads - 1) / kThreads;
     {
         long mine = 0;
-        for (int b = threadIdx.x * run; b < min(A.s.batch, int(threadIdx.x + 1) * run); ++b) mine += size_of<S>(A, sequence<S>(A, b));
+        for (int b = threadIdx.x * run; b < min(A.s.batch, int(threadIdx.x + 1) * run); ++b) {
+            const Seq q = sequence<S>(A, b);
+            mine += A.apart ? tiles_of<S>(A, q) : size_of<S>(A, q);
+        }
         long x = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -297,27 +307,48 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     const long total = before[kThreads];
     // few keys: one CTA, or four warps and more of as many as there are shares for
     const long shares = max(1L, quotient(total, S::kLeast));
-    const int active = shares <= S::kWarps ? int(shares) : int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
-    const long workers = min(shares, long(active) * gridDim.x);
+    const int active = A.apart             ? S::kWarps
+                       : shares <= S::kWarps ? int(shares)
+                                             : int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
     const int worker0 = active * blockIdx.x;
-    // (the first total % workers have one stage more)
-    const long each = quotient(total, workers), longer = total - each * workers;
     Walk<S>& walk = walks[warp_in];
     if (lane == 0) {
-        const int worker = worker0 + warp_in;
-        const bool works = warp_in < active && worker < workers;
-        walk.x = walk.begin = works ? each * worker + min(long(worker), longer) : 0;
-        walk.end = works ? walk.begin + each + (worker < longer) : 0;
-        int lo = 0;                              // the run of sequences that x is in
+        // who gets equal parts of all stages: a warp; or, apart, of all tiles: some of a CTA's
+        const int slot = A.apart ? warp_in / A.apart : 0;
+        const long workers = A.apart ? long(S::kWarps / A.apart) * gridDim.x : min(shares, long(active) * gridDim.x);
+        long worker = A.apart ? long(slot) * gridDim.x + blockIdx.x : worker0 + warp_in;
+        walk.each = quotient(total, workers), walk.longer = total - walk.each * workers;
+        walk.origin = walk.worker = 0;
+        long from = walk.each * worker + min(worker, walk.longer), many = walk.each + (worker < walk.longer);
+        if (worker >= workers || (!A.apart && warp_in >= active)) from = many = 0;
+        int lo = 0;                              // the run of sequences that it is in
         for (int step = 256; step; step /= 2)
-            if (lo + step < kThreads && before[lo + step] <= walk.x) lo += step;
+            if (lo + step < kThreads && before[lo + step] <= from) lo += step;
         walk.at = before[lo];
         walk.b = min(lo * run, A.s.batch - 1);
-        runs[1 + warp_in].x = -1;
-        if (warp_in == 0) {
-            runs[0].x = -1;
-            shares_of[0] = each, shares_of[1] = longer;
+        if (A.apart) {
+            // the tiles' stages, on a line that begins with their first one's sequence, and
+            // the warp's part of them
+            long skipped = from - walk.at, stages = 0;
+            int b = walk.b;
+            for (bool found = false; many && b < A.s.batch; ++b) {
+                const Seq q = sequence<S>(A, b);
+                const long n = tiles_of<S>(A, q), taken = min(many, max(0L, n - skipped));
+                if (!found && taken) walk.b = b, walk.origin = skipped * q.blocks, found = true;
+                skipped = max(0L, skipped - n);
+                stages += taken * q.blocks;
+                many -= taken;
+            }
+            walk.at = 0;
+            walk.each = stages / A.apart, walk.longer = stages % A.apart;
+            worker = warp_in - slot * A.apart;
+            walk.worker = worker0 + slot * A.apart;
+            from = walk.origin + walk.each * worker + min(worker, walk.longer), many = walk.each + (worker < walk.longer);
         }
+        walk.x = walk.begin = from;
+        walk.end = from + many;
+        runs[1 + warp_in].x = -1;
+        if (warp_in == 0) runs[0].x = -1;
     }
     __syncthreads();
 
@@ -353,12 +384,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const int j1 = int(min(long(sq.blocks), j0 + (walk.end - x)));
         const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
-        const int base = sq.base;
+        const int base = sq.base, begin = A.apart ? 0 : S::kBegin;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
         // (positions and windows may be close to 2^31)
         const int kb0 = A.window && first_pos >= A.window ? (first_pos - A.window + 1) / S::kKeys : 0;
-        const int kb_end = min(kb0 + j1 - S::kBegin, last_pos < 0 ? 0 : last_pos / S::kKeys + 1);
-        int kb = kb0 + max(0, j0 - S::kBegin), kb_in = kb;
+        const int kb_end = min(kb0 + j1 - begin, last_pos < 0 ? 0 : last_pos / S::kKeys + 1);
+        int kb = kb0 + max(0, j0 - begin), kb_in = kb;
         __syncwarp();
         if (lane == 0) {
             walk.x = x + (j1 - j0), walk.at = at, walk.item_at = x - j0;
@@ -756,9 +787,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                                                 : A.states + size_t(worker0 + warp_in) * S::kCols * (D + 4);
         if (!whole && lane == 0) {
             const int slot = item_at <= walk.begin ? 0 : 1;
-            const long each = shares_of[0], longer = shares_of[1];
+            const long each = walk.each, longer = walk.longer;
             auto worker_of = [&](long at) {
-                return int(at < longer * (each + 1) ? quotient(at, each + 1) : longer + quotient(at - longer * (each + 1), max(1L, each)));
+                at -= walk.origin;
+                return walk.worker +
+                       int(at < longer * (each + 1) ? quotient(at, each + 1) : longer + quotient(at - longer * (each + 1), max(1L, each)));
             };
             places[warp_in][slot] = state;
             const int4 info = make_int4(walk.first, walk.tile | walk.rows << 24, walk.head | slot << 30, worker_of(item_end - 1));
@@ -868,10 +901,24 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
     A.states = static_cast<float*>(scratch);
     A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
     A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
+    // Tiles that are short, however long the sequences are, and even enough on the warps
+    // are apart: each with warps of one CTA, as many as there are, so that there is nothing
+    // to join across CTAs, and no second launch.  32 / 8 heads of 128, apart and on the line,
+    // us: 300 sequences of 100 tokens 14 and 24, 1000 of them 40 and 45, 32 of 200 9.5 and 14,
+    // one of 300 9.2 and 11, of 1000 14 and 11, of 4000 34 and 12; 8 of 600 11.9 and 10.7, but
+    // the host's call is shorter by 2.
+    // (a sequence's last tile may be begun, or each token's)
+    const long R = S::kRows, rows = long(a.s.rows) * a.G, warps = long(sms) * S::kWarps;
+    const long tiles = std::min((a.G + R - 1) / R * a.s.rows, (rows + a.s.batch * (R - 1)) / R) * (a.c.hkv / S::P);
+    long stages = ((long(a.s.width) << a.c.log_page) + S::kKeys - 1) / S::kKeys;
+    if (a.window) stages = std::min(stages, (a.window + (R + a.G - 2) / a.G + 2 * S::kKeys - 2) / S::kKeys);
+    int to_tile = 1;
+    for (int n = 2; n <= S::kWarps; ++n)
+        if (S::kWarps % n == 0 && tiles * n <= warps && to_tile * S::kLeast < stages) to_tile = n;
+    const long most = (tiles * to_tile + warps - 1) / warps * stages;       // (a warp's, times to_tile)
+    if (stages <= kMost * to_tile && most * warps <= to_tile * (kMore * warps + tiles * (stages + S::kBegin))) A.apart = to_tile;
     const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
-    // (no more work than one CTA takes, however long the sequences are: nothing to join)
-    const long tiles = a.s.batch + long(a.s.rows) * a.G / S::kRows, stages = ((long(a.s.width) << a.c.log_page) + S::kKeys - 1) / S::kKeys;
-    if (rc || tiles * (a.c.hkv / S::P) * (stages + S::kBegin) <= long(S::kLeast) * S::kWarps) return rc;
+    if (rc || A.apart) return rc;
     return dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
 

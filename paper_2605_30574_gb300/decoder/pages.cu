@@ -4,12 +4,13 @@
 // page, and a copied page is read and written once.  Small calls are latency: the
 // search for a row's sequence, its page, the access.
 //
-// 16.5k tokens of 8 heads of 128, ragged: stored in 27 us, loaded in 24 (84 MB each: 12.5 at
+// 16.5k tokens of 8 heads of 128, ragged: stored in 25 us, loaded in 24 (84 MB each: 12.5 at
 // the copy rate), what a row's scales cost in instructions and a warp's chain of four
 // loads before its first row.  Measured on the way, both together: 129 with a warp to a
 // row, 79 with eight rows on their way in a warp, 70 without divisions (below), 55 with
-// rows of a page a constant apart, 51 with sixteen elements to a lane.  36 layers of 340
-// pages copied: 254 us (1.73 GB, the copy rate).
+// rows of a page a constant apart, 51 with sixteen elements to a lane, 49 with CTAs of four
+// warps for eight and a row's successor fetched when it is rounded.  36 layers of 340 pages
+// copied: 254 us (1.73 GB, the copy rate).
 #include "pages.cuh"
 
 #include "decoder.h"
@@ -17,7 +18,7 @@
 namespace decoder {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128, kCopying = 256;
 constexpr unsigned kFull = 0xffffffffu;
 
 // The sequence of token `row`, starts[b] <= row < starts[b + 1], one that has tokens: 32
@@ -214,8 +215,8 @@ __device__ __forceinline__ uint4 values_of(const Held& x) {
 }
 
 // A warp takes up to 32 tokens, whose places its lanes find at once, and as many heads of
-// K or of V as fill its lanes.  N rows are on their way together; the first of those to
-// store, before their places are known.
+// K or of V as fill its lanes.  N rows are on their way together: those to store from before
+// the first's place is known, and another when one is rounded.
 template <int D, bool Store, int N, int E>
 __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s, Rows x, int per_warp, unsigned kinds) {
     wait_for_previous();
@@ -231,13 +232,13 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
     const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + E * (lane & (kLanes - 1)) + first * token;
     const Lane<D, E> at(c, kv, mine ? head : 0);
     uint4 data[N][E / 8];
-    auto fetch = [&](int from) {
+    auto fetch = [&](int i, int from) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int k = 0; k < E / 8; ++k) data[i][k] = reinterpret_cast<const uint4*>(p + min(from + i, n - 1) * token)[k];
+        for (int k = 0; k < E / 8; ++k) data[i][k] = reinterpret_cast<const uint4*>(p + min(from + i, n - 1) * token)[k];
     };
-    if (Store) fetch(0);
+    if (Store)
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(i, 0);
     int slot = 0;
     const int page = places_of(c, s, int(first), n, &slot);
     for (int from = 0; from < n; from += N) {
@@ -249,7 +250,10 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
         if (run) {
             if (Store) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) quantise_and_store<D, E>(first_at, i, data[i], kv, mine);
+                for (int i = 0; i < N; ++i) {
+                    quantise_and_store<D, E>(first_at, i, data[i], kv, mine);
+                    if (from + N < n) fetch(i, from + N);
+                }
             } else {
                 Held held[N];
 #pragma unroll
@@ -265,6 +269,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
                 const Place<D> place(at, max(to, 0), to < 0 ? 0 : in);
                 if (Store) {
                     quantise_and_store<D, E>(place, 0, data[i], kv, mine && to >= 0);
+                    if (from + N < n) fetch(i, from + N);
                 } else if (mine && to > -3) {
                     const uint32_t none = to == -1 ? 0u : 0x7fff7fffu;
                     *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) =
@@ -272,7 +277,6 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
                 }
             }
         }
-        if (Store && from + N < n) fetch(from + N);
     }
 }
 
@@ -288,7 +292,7 @@ struct Part {
     unsigned bytes;
 };
 
-__global__ void __launch_bounds__(kThreads) copy_kernel(Part a, Part b, Part e, int pages, const __grid_constant__ Copies copies) {
+__global__ void __launch_bounds__(kCopying) copy_kernel(Part a, Part b, Part e, int pages, const __grid_constant__ Copies copies) {
     wait_for_previous();
     const int src = copies.src[blockIdx.x], dst = copies.dst[blockIdx.x];
     const Part parts[3] = {a, b, e};
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(Part a, Part b, Part e, 
         const uint4* from = reinterpret_cast<const uint4*>(parts[i].base + (layer + src) * n);
         uint4* to = reinterpret_cast<uint4*>(parts[i].base + (layer + dst) * n);
 #pragma unroll 4
-        for (unsigned j = threadIdx.x; j < n / 16; j += kThreads) to[j] = from[j];
+        for (unsigned j = threadIdx.x; j < n / 16; j += kCopying) to[j] = from[j];
     }
 }
 
@@ -318,7 +322,7 @@ int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream
     // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
     // shortest chain of loads.
     const int per_warp = s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
-    const long blocks = (s.rows + 8L * per_warp - 1) / (8L * per_warp) * kinds;
+    const long blocks = (s.rows + kThreads / 32L * per_warp - 1) / (kThreads / 32L * per_warp) * kinds;
     if (blocks >= 1L << 31) return int(cudaErrorInvalidValue);
     auto kernel = per_warp > 1 ? kernel_of<Store, 8, 8>(d) : kernel_of<Store, 1, 8>(d);
     if constexpr (Store)
@@ -355,7 +359,7 @@ extern "C" int decoder_page_copy(const PageCache* cache, const int* src, const i
         const int m = n - at < kPairs ? n - at : kPairs;
         Copies copies;
         for (int i = 0; i < m; ++i) copies.src[i] = src[at + i], copies.dst[i] = dst[at + i];
-        const int rc = dependent(copy_kernel, dim3(unsigned(m), unsigned(cache->layers)), kThreads, 0, static_cast<cudaStream_t>(stream), a, b, e,
+        const int rc = dependent(copy_kernel, dim3(unsigned(m), unsigned(cache->layers)), kCopying, 0, static_cast<cudaStream_t>(stream), a, b, e,
                                  cache->pages, copies);
         if (rc) return rc;
     }

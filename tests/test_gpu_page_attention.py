@@ -135,6 +135,34 @@ def test_many_sequences_of_all_lengths():
     check(cache, queries(700, 2, 64), where)
 
 
+@pytest.mark.parametrize("d,heads,G,page", [(64, 2, 4, 16), (128, 2, 4, 64), (256, 1, 2, 32), (128, 1, 3, 16), (128, 1, 12, 16), (64, 1, 33, 32)])
+@pytest.mark.parametrize("new,lengths", [([3, 1, 0, 8], [3, 40, 9, 130]), ([17], [500]), ([1, 20, 1], [1, 20, 300]), ([1], [1]), ([1] * 6, [60] * 6)])
+@pytest.mark.parametrize("window", [0, 21])
+def test_tables_far_wider_than_lengths(d, heads, G, page, new, lengths, window):
+    """Work that is shared by the stage, of sequences that are short."""
+    cache, where = filled(lengths, new, heads, d, page, seed=window, width=40000 // page)
+    check(cache, queries(sum(new), heads * G, d), where, window=window)
+
+
+@pytest.mark.parametrize("d,heads,G,batch,page", [(64, 3, 1, 900, 16), (128, 2, 4, 2000, 16), (256, 1, 3, 1300, 32), (128, 1, 2, 300, 64), (64, 1, 40, 500, 16)])
+def test_many_short_sequences(d, heads, G, batch, page):
+    """More tiles than warps, and fewer; sequences without tokens among them."""
+    lengths = [(7 * i) % 41 for i in range(batch)]
+    new = [min(n, 1 + (i % 50 == 0)) for i, n in enumerate(lengths)]
+    cache, where = filled(lengths, new, heads, d, page, seed=batch)
+    check(cache, queries(sum(new), heads * G, d), where)
+
+
+@pytest.mark.parametrize("d,heads,G", [(64, 2, 4), (128, 8, 4), (128, 1, 16), (256, 4, 2)])
+@pytest.mark.parametrize("batch,length", [(1, 100), (1, 300), (5, 300), (20, 200)])
+def test_warps_that_share_a_tile(d, heads, G, batch, length):
+    lengths = [max(0, length - 13 * i) for i in range(batch)]
+    new = [min(1, n) for n in lengths]
+    cache, where = filled(lengths, new, heads, d, 16, seed=batch)
+    check(cache, queries(sum(new), heads * G, d), where)
+    check(cache, queries(sum(new), heads * G, d), where, window=70)
+
+
 def test_rows_that_see_nothing():
     # no tokens at all, more new tokens than the sequence has, none new
     cache, where = filled([0, 2, 5, -3], [1, 4, 0, 1], 2, 64, 16)
