@@ -55,10 +55,11 @@ def lib() -> ctypes.CDLL:
         L.decoder_attention_backward.argtypes = [vp] * 6 + [ctypes.POINTER(l), vp, vp, vp, vp, l, l, l, i, i, i, f, vp]
         L.decoder_page_rows.argtypes = [i, vp, i, vp, vp, l, l, l, l, vp, vp, vp, i, i, i, vp]
         L.decoder_page_copy.argtypes = [vp, ctypes.POINTER(i), ctypes.POINTER(i), i, vp]
+        L.decoder_page_copy_refused.argtypes = [ctypes.POINTER(i), ctypes.POINTER(i), i, i]
         L.decoder_page_attention_scratch.argtypes = [i]
         L.decoder_page_attention_scratch.restype = l
         L.decoder_page_attention.argtypes = [vp, i, vp, l, l, vp, vp, vp, i, i, i, i, f, i, vp, vp, vp]
-        for fn in (L.decoder_page_rows, L.decoder_page_copy, L.decoder_page_attention, L.decoder_attention, L.decoder_attention_backward, L.decoder_token_scores, L.decoder_distill, L.decoder_qkv, L.decoder_block, L.decoder_causal, L.decoder_gemm, L.decoder_gemm_plan, L.decoder_error, L.decoder_rms_norm, L.decoder_add_rms_norm, L.decoder_add, L.decoder_to_bf16, L.decoder_silu_mul,
+        for fn in (L.decoder_page_rows, L.decoder_page_copy, L.decoder_page_copy_refused, L.decoder_page_attention, L.decoder_attention, L.decoder_attention_backward, L.decoder_token_scores, L.decoder_distill, L.decoder_qkv, L.decoder_block, L.decoder_causal, L.decoder_gemm, L.decoder_gemm_plan, L.decoder_error, L.decoder_rms_norm, L.decoder_add_rms_norm, L.decoder_add, L.decoder_to_bf16, L.decoder_silu_mul,
                    L.decoder_qkv_post):
             fn.restype = i
         _LIB = L

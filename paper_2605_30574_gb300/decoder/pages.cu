@@ -13,6 +13,9 @@
 // copied: 254 us (1.73 GB, the copy rate).
 #include "pages.cuh"
 
+#include <algorithm>
+#include <cstdlib>
+
 #include "decoder.h"
 
 namespace decoder {
@@ -346,6 +349,34 @@ extern "C" int decoder_page_rows(int out, const PageCache* cache, int layer, con
     const Rows x = {static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), k_token, k_head, v_token, v_head};
     return out ? rows<false>(c, s, x, cache->d, static_cast<cudaStream_t>(stream))
                : rows<true>(c, s, x, cache->d, static_cast<cudaStream_t>(stream));
+}
+
+// What pages to copy are refused for: 1, there is no such page; 2, one is written twice, or
+// written and read; 3, no memory to find out.
+extern "C" int decoder_page_copy_refused(const int* src, const int* dst, int n, int pages) {
+    for (int i = 0; i < n; ++i)
+        if (src[i] < 0 || src[i] >= pages || dst[i] < 0 || dst[i] >= pages) return 1;
+    if (n > pages) return 2;
+    // what is written, hashed into at least twice the places (2^32 over the golden ratio)
+    int bits = 6;
+    while ((1L << bits) < 2L * n) ++bits;
+    int few[512], *const places = bits <= 9 ? few : static_cast<int*>(std::malloc(sizeof(int) << bits));
+    if (!places) return 3;
+    std::fill(places, places + (1L << bits), -1);
+    auto place_of_page = [&](int page) {
+        uint32_t at = uint32_t(page) * 2654435769u >> (32 - bits);
+        while (places[at] >= 0 && places[at] != page) at = (at + 1) & ((1u << bits) - 1);
+        return places + at;
+    };
+    int refused = 0;
+    for (int i = 0; i < n && !refused; ++i) {
+        int* const at = place_of_page(dst[i]);
+        refused = *at >= 0 ? 2 : 0;
+        *at = dst[i];
+    }
+    for (int i = 0; i < n && !refused; ++i) refused = *place_of_page(src[i]) >= 0 ? 2 : 0;
+    if (places != few) std::free(places);
+    return refused;
 }
 
 // Pages src[i] to dst[i] of all layers; no dst is another's, or a src.

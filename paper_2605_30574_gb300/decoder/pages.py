@@ -31,6 +31,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -315,20 +316,26 @@ def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None
         raise ValueError(f"{what}: as many pages to copy to as from")
     if n == 0:
         return
+    ints = ctypes.c_int * n
     try:
-        ints = (ctypes.c_int * n)(*src), (ctypes.c_int * n)(*dst)
+        # (2000 pages: 68 us, 590 with ctypes' own conversion and Python's min, max and set)
+        pages = ints.from_buffer(array("i", src)), ints.from_buffer(array("i", dst))
+        refused = lib().decoder_page_copy_refused(*pages, n, cache.pages)
     except TypeError:
         raise TypeError(f"{what}: pages must be whole numbers") from None
-    if min(src) < 0 or min(dst) < 0 or max(src) >= cache.pages or max(dst) >= cache.pages:
+    except OverflowError:
+        refused = 1
+    if refused == 1:
         raise ValueError(f"{what}: the cache has pages 0 to {cache.pages - 1}")
-    to = set(dst)
-    if len(to) != n or not to.isdisjoint(src):
+    if refused == 2:
         raise ValueError(f"{what}: a page is written twice, or written and read")
+    if refused:
+        raise MemoryError(f"{what}: {n} pages")
     at = cache._layer(what, 0)
     if cache.device.index != _current_device():
         with torch.cuda.device(cache.device):
             return copy_pages(cache, src, dst)
-    _launch("decoder_page_copy", at, *ints, n)
+    _launch("decoder_page_copy", at, *pages, n)
 
 
 class PageTables:
@@ -485,9 +492,12 @@ class PageTables:
         for n in new:
             starts.append(starts[-1] + n)
         width = max([1, width] + [len(self._pages[i]) for i in ids])
-        flat = [p for i in ids for p in self._pages[i] + [-1] * (width - len(self._pages[i]))]
-        B = len(ids)
-        t = torch.tensor(flat + starts + lengths, dtype=_I32).to(self.cache.device)
+        flat, none, B = array("i"), array("i", [-1]), len(ids)
+        for i in ids:
+            flat.extend(self._pages[i])
+            flat += none * (width - len(self._pages[i]))
+        flat.extend(starts + lengths)
+        t = torch.frombuffer(flat, dtype=_I32).to(self.cache.device)
         return t[:B * width].view(B, width), t[B * width:B * width + B + 1], t[B * width + B + 1:]
 
 

@@ -1,5 +1,7 @@
 """Arguments of the paged cache's calls that are refused, and what the kernels are
 handed, without a GPU: the cache's tensors are the CPU's, and no launch is made."""
+import random
+
 import pytest
 import torch
 from torch.fx.experimental.proxy_tensor import make_fx
@@ -203,6 +205,26 @@ def test_copies(launched):
     P.copy_pages(cache, torch.tensor([1]), (3,))
     name, at, src, dst, n = launched[0]
     assert (name, at, n) == ("decoder_page_copy", cache._at, 2) and list(src) == [0, 0] and list(dst) == [2, 4]
+
+
+@pytest.mark.parametrize("n", [1, 30, 256, 257, 3000])
+def test_copies_of_many(launched, n):
+    """Whatever the order of the pages, the one that is wrong is found."""
+    rng = random.Random(n)
+    cache = OnCpu(layers=1, pages=2 * n + 5, heads=1)
+    pages = rng.sample(range(2 * n + 5), 2 * n)
+    src, dst = pages[:n], pages[n:]
+    P.copy_pages(cache, src, dst)
+    assert len(launched) == 1 and list(launched[0][2]) == src and list(launched[0][3]) == dst
+    for i in {0, n // 2, n - 1}:
+        for bad, match in ((-1, "pages 0 to"), (2 * n + 5, "pages 0 to"), (1 << 31, "pages 0 to"), (src[(i + 1) % n], "twice")):
+            with pytest.raises(ValueError, match=match):
+                P.copy_pages(cache, src, dst[:i] + [bad] + dst[i + 1:])
+        with pytest.raises(ValueError, match="twice" if n > 1 else "pages 0 to"):
+            P.copy_pages(cache, src, dst[:i] + [dst[i - 1] if n > 1 else -5] + dst[i + 1:])
+    assert len(launched) == 1
+    with pytest.raises(ValueError, match="twice"):
+        P.copy_pages(cache, [0] * (2 * n + 6), [1] * (2 * n + 6))
 
 
 def test_the_library_refuses_sizes():
