@@ -136,6 +136,8 @@ def _launch(name, *args):
     # host time than the launch)
     rc = getattr(_LIB or lib(), name)(*args, _raw_stream(_current_device()))
     if rc != 0:
+        if rc < 0:          # (what the call was given does not do)
+            return False
         raise RuntimeError(f"{name} failed with CUDA error {rc}")
 
 

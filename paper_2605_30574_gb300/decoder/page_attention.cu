@@ -349,6 +349,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         walk.end = from + many;
         runs[1 + warp_in].x = -1;
         if (warp_in == 0) runs[0].x = -1;
+        places[warp_in][0] = places[warp_in][1] = reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes);
     }
     __syncthreads();
 
@@ -783,7 +784,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const long item_at = walk.item_at, item_end = item_at + walk.line;
         const bool whole = item_at >= walk.begin && item_end <= walk.x;
         // (a warp's last state goes where its ring was)
-        float* const state = walk.x >= walk.end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
+        float* const state = A.apart || walk.x >= walk.end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
                                                 : A.states + size_t(worker0 + warp_in) * S::kCols * (D + 4);
         if (!whole && lane == 0) {
             const int slot = item_at <= walk.begin ? 0 : 1;
@@ -796,7 +797,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             places[warp_in][slot] = state;
             const int4 info = make_int4(walk.first, walk.tile | walk.rows << 24, walk.head | slot << 30, worker_of(item_end - 1));
             if (item_at >= walk.begin) runs[1 + warp_in] = info;
-            if (item_at < walk.begin && warp_in == 0) runs[0] = info;
+            if (item_at < walk.begin && warp_in == 0 && !A.apart) runs[0] = info;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -844,12 +845,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll 4
         for (int w = w0; w <= last; ++w)
             st.add(places[w - worker0][r && w == w0 ? info.z >> 30 & 1 : 0] + col * (D + 4));
-        if (r && info.w < worker0 + active)
+        if (A.apart || (r && info.w < worker0 + active))
             st.write(A.out + row_of<S>(A, info, mine, row) * D);
         else
             st.keep(A.joined + ((size_t(blockIdx.x) * 2 + (r ? 1 : 0)) * S::kCols + col) * (D + 4));
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && !A.apart) {
         int4 going = make_int4(-1, 0, 0, 0);
         for (int r = 1; r <= active; ++r)
             if (runs[r].x >= 0 && runs[r].w >= worker0 + active) going = runs[r], going.w /= active;
@@ -898,9 +899,6 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
     const cudaError_t e = prepared<S>(&sms);
     if (e != cudaSuccess) return int(e);
     Args A = a;
-    A.states = static_cast<float*>(scratch);
-    A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
-    A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
     // Tiles that are short, however long the sequences are, and even enough on the warps
     // are apart: each with warps of one CTA, as many as there are, so that there is nothing
     // to join across CTAs, and no second launch.  32 / 8 heads of 128, apart and on the line,
@@ -917,6 +915,12 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
         if (S::kWarps % n == 0 && tiles * n <= warps && to_tile * S::kLeast < stages) to_tile = n;
     const long most = (tiles * to_tile + warps - 1) / warps * stages;       // (a warp's, times to_tile)
     if (stages <= kMost * to_tile && most * warps <= to_tile * (kMore * warps + tiles * (stages + S::kBegin))) A.apart = to_tile;
+    if (!A.apart) {
+        if (!scratch) return -1;
+        A.states = static_cast<float*>(scratch);
+        A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
+        A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
+    }
     const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
     if (rc || A.apart) return rc;
     return dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
@@ -953,7 +957,8 @@ extern "C" long decoder_page_attention_scratch(int d) {
                       : scratch_of<Shape<256, 1, 1>>(sms);
 }
 
-// q [rows][hq][d] (its strides: token, head) over the layer's pages; out [rows][hq][d].
+// q [rows][hq][d] (its strides: token, head) over the layer's pages; out [rows][hq][d].  -1:
+// nothing is done, as it takes scratch, and there is none.
 extern "C" int decoder_page_attention(const PageCache* cache, int layer, const void* q, long q_token, long q_head, const void* table,
                                       const void* starts, const void* lengths, int width, int batch, int rows, int hq, float scale, int window,
                                       void* out, void* scratch, void* stream) {

@@ -30,7 +30,6 @@ gradients.  The same inputs give the same bits.
 from __future__ import annotations
 
 import ctypes
-import math
 from array import array
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple, Union
 
@@ -272,15 +271,16 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     what = "page_attention"
     untraced(what)
     where = _where(what, cache, table, starts, lengths)
-    _bf16(what, "q", q, cache, (*q.shape[:-1], cache.head_dim) if isinstance(q, torch.Tensor) and q.dim() == 3 else None)
-    rows, hq, d = q.shape
+    shape = q.shape if isinstance(q, torch.Tensor) else ()
+    _bf16(what, "q", q, cache, shape if len(shape) == 3 and shape[2] == cache.head_dim else None)
+    rows, hq, d = shape
     if rows * hq >= 1 << 26:
         raise ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
     if hq == 0 or hq % cache.kv_heads:
         raise ValueError(f"{what}: the query heads must be a multiple of the cache's {cache.kv_heads}")
     if not isinstance(window, int) or not 0 <= window < 1 << 31:
         raise ValueError(f"{what}: window must be a whole number, 0 (none) to 2^31 - 1")
-    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    scale = d ** -0.5 if scale is None else float(scale)
     at = cache._layer(what, layer)
     if out is not None:
         _bf16(what, "out", out, cache, q.shape)
@@ -292,13 +292,20 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     if cache.device.index != _current_device():
         with torch.cuda.device(cache.device):
             return page_attention(cache, layer, q, table, starts, lengths, scale=scale, window=window, out=out)
-    y = torch.empty(q.shape, dtype=BF16, device=q.device) if out is None else out
+    y = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
     if not rows or not where[-1]:
         return y
     q = _readable(q)
-    scratch = torch.empty(cache._scratch, dtype=_U8, device=q.device)
-    _launch("decoder_page_attention", at, layer, q.data_ptr(), *q.stride()[:2], *where, rows, hq, scale, window, y.data_ptr(),
-            scratch.data_ptr())
+    token, head, _ = q.stride()
+    args = at, layer, q.data_ptr(), token, head, *where, rows, hq, scale, window, y.data_ptr()
+    # Short sequences take no scratch, whose allocation is 3 us of a call of 29, so that is
+    # tried first where it is likely (in vain, it costs 2.5).
+    most, short = where[3] * cache.page, False
+    if most <= 512 or (most <= 2048 and where[4] * cache.kv_heads >= 128):
+        short = _launch("decoder_page_attention", *args, None) is not False
+    if not short:
+        scratch = torch.empty(cache._scratch, dtype=_U8, device=q.device)
+        _launch("decoder_page_attention", *args, scratch.data_ptr())
     if out is not None:
         _written(out)
     return y

@@ -227,6 +227,18 @@ def test_copies_of_many(launched, n):
         P.copy_pages(cache, [0] * (2 * n + 6), [1] * (2 * n + 6))
 
 
+def test_scratch_where_it_is_needed(monkeypatch):
+    """Without, where the library may do; with it, when that said so."""
+    got = []
+    monkeypatch.setattr(P, "_current_device", lambda: None)
+    monkeypatch.setattr(P, "_launch", lambda *a: got.append(a[-1]) or (False if answers.pop(0) else None))
+    cache, q = OnCpu(), torch.zeros(2, 4, 64, dtype=BF)
+    for width, answers, none in ((2, [False], [True]), (2, [True, False], [True, False]), (257, [False], [False])):
+        P.page_attention(cache, 0, q, *where(2, width))
+        assert [x is None for x in got] == none and not answers
+        got.clear()
+
+
 def test_the_library_refuses_sizes():
     L = K.lib()
     assert L.decoder_page_attention_scratch(96) < 0
