@@ -185,7 +185,7 @@ struct Seq {
     bool broken;                                        // (it is longer than its pages are)
 };
 
-template <class S>
+template <class S, bool kApart>
 __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     Seq q;
     const int from = A.s.starts[b], to = A.s.starts[b + 1], length = A.s.lengths[b];
@@ -198,7 +198,7 @@ __device__ __forceinline__ Seq sequence(const Args& A, int b) {
     q.tiles = int((long(q.new_) * A.G + S::kRows - 1) / S::kRows);
     int blocks = q.length / S::kKeys + (q.length % S::kKeys != 0);
     if (A.window) blocks = min(blocks, int((long(A.window) + (S::kRows + A.G - 2) / A.G + 2 * S::kKeys - 2) / S::kKeys));
-    q.blocks = max(1, blocks) + (A.apart ? 0 : S::kBegin);
+    q.blocks = max(1, blocks) + (kApart ? 0 : S::kBegin);
     return q;
 }
 
@@ -273,7 +273,8 @@ __device__ __forceinline__ size_t row_of(const Args& A, const int4& info, int mi
     return (size_t(info.x + token) * A.c.hkv + (info.z & 0x3fffffff) + mine) * A.G + r - token * A.G;
 }
 
-template <class S>
+// (Two kernels: one for both takes 381 us for 375, and 7.0 for 6.7 of a short sequence.)
+template <class S, bool kApart>
 __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A) {
     constexpr int D = S::D, NT = S::NT, P = S::P, kI = S::kI, kThreads = S::kThreads, R = S::kRows;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -288,8 +289,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     {
         long mine = 0;
         for (int b = threadIdx.x * run; b < min(A.s.batch, int(threadIdx.x + 1) * run); ++b) {
-            const Seq q = sequence<S>(A, b);
-            mine += A.apart ? tiles_of<S>(A, q) : size_of<S>(A, q);
+            const Seq q = sequence<S, kApart>(A, b);
+            mine += kApart ? tiles_of<S>(A, q) : size_of<S>(A, q);
         }
         long x = mine;
 #pragma unroll
@@ -307,32 +308,32 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
     const long total = before[kThreads];
     // few keys: one CTA, or four warps and more of as many as there are shares for
     const long shares = max(1L, quotient(total, S::kLeast));
-    const int active = A.apart             ? S::kWarps
+    const int active = kApart                ? S::kWarps
                        : shares <= S::kWarps ? int(shares)
                                              : int(max(long(kMinWarps), min(long(S::kWarps), quotient(shares + gridDim.x - 1, gridDim.x))));
     const int worker0 = active * blockIdx.x;
     Walk<S>& walk = walks[warp_in];
     if (lane == 0) {
         // who gets equal parts of all stages: a warp; or, apart, of all tiles: some of a CTA's
-        const int slot = A.apart ? warp_in / A.apart : 0;
-        const long workers = A.apart ? long(S::kWarps / A.apart) * gridDim.x : min(shares, long(active) * gridDim.x);
-        long worker = A.apart ? long(slot) * gridDim.x + blockIdx.x : worker0 + warp_in;
+        const int slot = kApart ? warp_in / A.apart : 0;
+        const long workers = kApart ? long(S::kWarps / A.apart) * gridDim.x : min(shares, long(active) * gridDim.x);
+        long worker = kApart ? long(slot) * gridDim.x + blockIdx.x : worker0 + warp_in;
         walk.each = quotient(total, workers), walk.longer = total - walk.each * workers;
         walk.origin = walk.worker = 0;
         long from = walk.each * worker + min(worker, walk.longer), many = walk.each + (worker < walk.longer);
-        if (worker >= workers || (!A.apart && warp_in >= active)) from = many = 0;
+        if (worker >= workers || (!kApart && warp_in >= active)) from = many = 0;
         int lo = 0;                              // the run of sequences that it is in
         for (int step = 256; step; step /= 2)
             if (lo + step < kThreads && before[lo + step] <= from) lo += step;
         walk.at = before[lo];
         walk.b = min(lo * run, A.s.batch - 1);
-        if (A.apart) {
+        if (kApart) {
             // the tiles' stages, on a line that begins with their first one's sequence, and
             // the warp's part of them
             long skipped = from - walk.at, stages = 0;
             int b = walk.b;
             for (bool found = false; many && b < A.s.batch; ++b) {
-                const Seq q = sequence<S>(A, b);
+                const Seq q = sequence<S, kApart>(A, b);
                 const long n = tiles_of<S>(A, q), taken = min(many, max(0L, n - skipped));
                 if (!found && taken) walk.b = b, walk.origin = skipped * q.blocks, found = true;
                 skipped = max(0L, skipped - n);
@@ -373,11 +374,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const long x = walk.x;
         long at = walk.at;
         int b = walk.b;
-        Seq sq = sequence<S>(A, b);
+        Seq sq = sequence<S, kApart>(A, b);
         while (at + size_of<S>(A, sq) <= x) {
             at += size_of<S>(A, sq);
             if (++b >= A.s.batch) break;         // (lengths that changed under the call)
-            sq = sequence<S>(A, b);
+            sq = sequence<S, kApart>(A, b);
         }
         if (b >= A.s.batch) break;
         const long rel = x - at;
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const int j1 = int(min(long(sq.blocks), j0 + (walk.end - x)));
         const int group = item / sq.tiles, head = group * P, tile = item - group * sq.tiles;
         const int rows = int(min(long(R), long(sq.new_) * A.G - long(tile) * R));
-        const int base = sq.base, begin = A.apart ? 0 : S::kBegin;
+        const int base = sq.base, begin = kApart ? 0 : S::kBegin;
         const int first_pos = base + tile * R / A.G, last_pos = base + (tile * R + rows - 1) / A.G;
         // (positions and windows may be close to 2^31)
         const int kb0 = A.window && first_pos >= A.window ? (first_pos - A.window + 1) / S::kKeys : 0;
@@ -784,8 +785,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
         const long item_at = walk.item_at, item_end = item_at + walk.line;
         const bool whole = item_at >= walk.begin && item_end <= walk.x;
         // (a warp's last state goes where its ring was)
-        float* const state = A.apart || walk.x >= walk.end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
-                                                : A.states + size_t(worker0 + warp_in) * S::kCols * (D + 4);
+        float* const state = kApart || walk.x >= walk.end ? reinterpret_cast<float*>(smem + warp_in * S::kWarpBytes)
+                                                          : A.states + size_t(worker0 + warp_in) * S::kCols * (D + 4);
         if (!whole && lane == 0) {
             const int slot = item_at <= walk.begin ? 0 : 1;
             const long each = walk.each, longer = walk.longer;
@@ -797,7 +798,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
             places[warp_in][slot] = state;
             const int4 info = make_int4(walk.first, walk.tile | walk.rows << 24, walk.head | slot << 30, worker_of(item_end - 1));
             if (item_at >= walk.begin) runs[1 + warp_in] = info;
-            if (item_at < walk.begin && warp_in == 0 && !A.apart) runs[0] = info;
+            if (item_at < walk.begin && warp_in == 0 && !kApart) runs[0] = info;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -845,12 +846,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll 4
         for (int w = w0; w <= last; ++w)
             st.add(places[w - worker0][r && w == w0 ? info.z >> 30 & 1 : 0] + col * (D + 4));
-        if (A.apart || (r && info.w < worker0 + active))
+        if (kApart || (r && info.w < worker0 + active))
             st.write(A.out + row_of<S>(A, info, mine, row) * D);
         else
             st.keep(A.joined + ((size_t(blockIdx.x) * 2 + (r ? 1 : 0)) * S::kCols + col) * (D + 4));
     }
-    if (threadIdx.x == 0 && !A.apart) {
+    if (threadIdx.x == 0 && !kApart) {
         int4 going = make_int4(-1, 0, 0, 0);
         for (int r = 1; r <= active; ++r)
             if (runs[r].x >= 0 && runs[r].w >= worker0 + active) going = runs[r], going.w /= active;
@@ -885,7 +886,8 @@ template <class S>
 cudaError_t prepared(int* sms) {
     static splice::PerDevice<int> counts;
     return counts.get(sms, [](int dev, int* n) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        cudaError_t e = cudaFuncSetAttribute(attention_kernel<S, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(attention_kernel<S, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         return e == cudaSuccess ? cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev) : e;
     });
 }
@@ -921,7 +923,8 @@ int launch(const Args& a, void* scratch, cudaStream_t stream) {
         A.joined = A.states + long(sms) * S::kWarps * S::kCols * (S::D + 4);
         A.begun = reinterpret_cast<int4*>(A.joined + sms * 2L * S::kCols * (S::D + 4));
     }
-    const int rc = dependent(attention_kernel<S>, dim3(unsigned(sms)), S::kThreads, S::kSmem, stream, A);
+    const int rc = dependent(A.apart ? attention_kernel<S, true> : attention_kernel<S, false>, dim3(unsigned(sms)), S::kThreads, S::kSmem,
+                             stream, A);
     if (rc || A.apart) return rc;
     return dependent(join_kernel<S>, dim3(unsigned(sms), S::kCols), kJoin, 0, stream, A);
 }
