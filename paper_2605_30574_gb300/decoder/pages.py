@@ -166,9 +166,9 @@ def _readable(t):
 
 
 def _written(*ts):
-    for t in ts:
-        if not t.is_inference():
-            torch.autograd.graph.increment_version(t)
+    ts = [t for t in ts if not t.is_inference()]
+    if ts:
+        torch.autograd.graph.increment_version(ts)
 
 
 def _overlaps(t):
@@ -245,12 +245,11 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
     # (what the kernels cannot write to gets its rows by way of a copy)
     to, tv = _readable(k), _readable(v)
     _launch("decoder_page_rows", 1, at, layer, to.data_ptr(), tv.data_ptr(), *to.stride()[:2], *tv.stride()[:2], *where, rows)
-    for a, b in ((k, to), (v, tv)):
-        if a is b:
-            _written(a)
-        else:
-            with torch.no_grad():
-                a.copy_(b)
+    if k is to and v is tv:
+        return _written(k, v)
+    with torch.no_grad():
+        for a, b in ((k, to), (v, tv)):
+            _written(a) if a is b else a.copy_(b)
 
 
 def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,

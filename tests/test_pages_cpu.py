@@ -194,6 +194,22 @@ def test_outputs_that_are_refused(launched):
     assert len(launched) == 1
 
 
+def test_what_is_written_is_another_version(launched):
+    cache, w = OnCpu(), where()
+    k, v, q, out = (torch.zeros(2, n, 64, dtype=BF) for n in (2, 2, 4, 4))
+    before = [t._version for t in (k, v, q, out)]
+    P.load_pages(cache, 0, k, v, *w)
+    P.page_attention(cache, 0, q, *w, out=out)
+    P.store_pages(cache, 0, *(torch.zeros(2, 2, 64, dtype=BF) for _ in range(2)), *w)
+    assert [t._version - n for t, n in zip((k, v, q, out), before)] == [1, 1, 0, 1]
+    odd = torch.zeros(2, 2, 72, dtype=BF)[..., 1:65]
+    before = odd._version, v._version
+    P.load_pages(cache, 0, odd, v, *w)
+    assert odd._version > before[0] and v._version == before[1] + 1
+    with torch.inference_mode():
+        P.load_pages(cache, 0, k, torch.zeros(2, 2, 64, dtype=BF), *w)
+
+
 def test_copies(launched):
     cache = OnCpu()
     for src, dst, match in (([0], [5], "pages 0 to 4"), ([-1], [1], "pages 0 to 4"), ([0, 1], [2], "as many"), ([0, 1], [2, 2], "twice"),
