@@ -180,26 +180,46 @@ __device__ __forceinline__ void quantise_and_store(const Place<D>& at, int n, co
     if (w == 0) *at.exponent_at(n) = uint8_t(bad ? kBadExponent : E);
 }
 
-// What eight elements are held as.
+// What N elements are held as (a value's words still as they lie, for two groups).
+template <int N>
 struct Held {
-    uint32_t word;
+    uint32_t word[N / 8];
     uint8_t ratio, exponent;
 };
 
-template <int D>
-__device__ __forceinline__ Held read(const Place<D>& at, int n, int kv) {
-    Held x;
+template <int D, int N>
+__device__ __forceinline__ Held<N> read(const Place<D>& at, int n, int kv) {
+    constexpr int kI = D / 32;
+    Held<N> x;
     const uint8_t* codes = at.codes_at(n);
-    if (kv)
-        x.word = *reinterpret_cast<const uint16_t*>(codes) | uint32_t(*reinterpret_cast<const uint16_t*>(codes + 2 * (D / 32))) << 16;
-    else
-        x.word = *reinterpret_cast<const uint32_t*>(codes);
+    if (kv && N == 8) {
+        x.word[0] = *reinterpret_cast<const uint16_t*>(codes) | uint32_t(*reinterpret_cast<const uint16_t*>(codes + 2 * kI)) << 16;
+    } else {
+        const bool odd = threadIdx.x / (32 / N) & 1;
+        if (kv && odd) codes += N / 4 * kI - 2;
+#pragma unroll
+        for (int k = 0; k < N / 8; ++k) x.word[k] = *reinterpret_cast<const uint32_t*>(codes + k * (kv ? 2 : 4) * kI);
+    }
     x.ratio = *at.ratio_at(n);
     x.exponent = *at.exponent_at(n);
     return x;
 }
 
-__device__ __forceinline__ uint4 values_of(const Held& x) {
+// Lanes of two groups have read half of the runs of both, as they wrote them.
+template <int N>
+__device__ __forceinline__ void trade(Held<N>& x, int kv) {
+    if constexpr (N == 16) {
+        if (!kv) return;
+        const bool odd = threadIdx.x / (32 / N) & 1;
+        const uint32_t lo = __byte_perm(x.word[0], x.word[1], 0x5410), hi = __byte_perm(x.word[0], x.word[1], 0x7632);
+        const uint32_t got = __shfl_xor_sync(kFull, odd ? lo : hi, 32 / N);
+        x.word[0] = odd ? got : lo;
+        x.word[1] = odd ? hi : got;
+    }
+}
+
+template <int N>
+__device__ __forceinline__ uint4 values_of(const Held<N>& x, int k) {
     // c as bf16 is (128 + n) - 136, and c s, of three bits by four, is exact
     const uint32_t scale = x.exponent == kBadExponent ? 0x7fffu : (uint32_t(x.ratio) + (112u << 3) << 4) + uint32_t(x.exponent - 129) * 128u;
     const uint32_t s2 = scale * 0x10001u, k136 = 0xc308c308u;
@@ -207,7 +227,7 @@ __device__ __forceinline__ uint4 values_of(const Held& x) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         // elements j and j + 4
-        const uint32_t n = ((x.word >> (4 * j)) & 0x000f000fu) | 0x43004300u;
+        const uint32_t n = ((x.word[k] >> (4 * j)) & 0x000f000fu) | 0x43004300u;
         const __nv_bfloat162 c = __hadd2(reinterpret_cast<const __nv_bfloat162&>(n), reinterpret_cast<const __nv_bfloat162&>(k136));
         const __nv_bfloat162 y = __hmul2(c, reinterpret_cast<const __nv_bfloat162&>(s2));
         pair[j] = reinterpret_cast<const uint32_t&>(y);
@@ -224,7 +244,6 @@ template <int D, bool Store, int N, int E>
 __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s, Rows x, int per_warp, unsigned kinds) {
     wait_for_previous();
     constexpr int kLanes = D / E, kHeads = 32 / kLanes;
-    static_assert(Store || E == 8);
     const unsigned group = blockIdx.x / kinds, kind = blockIdx.x - group * kinds;
     const int kv = kind >= kinds / 2, lane = threadIdx.x & 31, head = int(kind - kv * (kinds / 2)) * kHeads + lane / kLanes;
     const long first = (long(group) * (kThreads / 32) + threadIdx.x / 32) * per_warp;
@@ -234,6 +253,10 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
     const long token = kv ? x.v_token : x.k_token;
     const __nv_bfloat16* p = (kv ? x.v : x.k) + (mine ? head : 0) * (kv ? x.v_head : x.k_head) + E * (lane & (kLanes - 1)) + first * token;
     const Lane<D, E> at(c, kv, mine ? head : 0);
+    auto write = [&](int row, const Held<E>& x) {
+#pragma unroll
+        for (int k = 0; k < E / 8; ++k) reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + row * token)[k] = values_of(x, k);
+    };
     uint4 data[N][E / 8];
     auto fetch = [&](int i, int from) {
 #pragma unroll
@@ -258,12 +281,14 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
                     if (from + N < n) fetch(i, from + N);
                 }
             } else {
-                Held held[N];
+                Held<E> held[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) held[i] = read<D>(first_at, i, kv);
-                if (mine)
+                for (int i = 0; i < N; ++i) held[i] = read<D, E>(first_at, i, kv);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) = values_of(held[i]);
+                for (int i = 0; i < N; ++i) {
+                    trade(held[i], kv);
+                    if (mine) write(from + i, held[i]);
+                }
             }
         } else {
 #pragma unroll
@@ -273,10 +298,16 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(PageLayer c, PageRows s,
                 if (Store) {
                     quantise_and_store<D, E>(place, 0, data[i], kv, mine && to >= 0);
                     if (from + N < n) fetch(i, from + N);
-                } else if (mine && to > -3) {
-                    const uint32_t none = to == -1 ? 0u : 0x7fff7fffu;
-                    *reinterpret_cast<uint4*>(const_cast<__nv_bfloat16*>(p) + (from + i) * token) =
-                        to < 0 ? make_uint4(none, none, none, none) : values_of(read<D>(place, 0, kv));
+                } else {
+                    // (no place: codes of 0, or a row of NaN)
+                    Held<E> x = read<D, E>(place, 0, kv);
+                    trade(x, kv);
+                    if (to < 0) {
+#pragma unroll
+                        for (int k = 0; k < E / 8; ++k) x.word[k] = to == -1 ? 0x88888888u : 0u;
+                        x.exponent = to == -1 ? 127 : kBadExponent;
+                    }
+                    if (mine && to > -3) write(from + i, x);
                 }
             }
         }
@@ -317,19 +348,22 @@ auto kernel_of(int d) {
 
 template <bool Store>
 int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream_t stream) {
-    // Sixteen elements to a lane halve what a row's scales cost, where a warp's lanes are
-    // filled by a row of all heads.
-    const bool wide = Store && c.hkv * d >= 1024;
-    const int heads = 32 * (wide ? 16 : 8) / d;
-    const long kinds = 2L * ((c.hkv + heads - 1) / heads);
     // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
     // shortest chain of loads.
-    const int per_warp = s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1;
+    auto kinds_of = [&](int each) { return 2L * ((c.hkv * d + 32 * each - 1) / (32 * each)); };
+    auto tokens_of = [&](long kinds) { return s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1; };
+    // Sixteen elements to a lane halve what a row's scales cost, where a warp's lanes are
+    // filled by a row of all heads.  Loads of more than a token to a warp are better off
+    // with eight (35k tokens of 8 heads of 128: 41 us for 43; 512: 8.2 with sixteen for 10.1).
+    const bool wide = c.hkv * d >= 1024 && (Store || tokens_of(kinds_of(8)) == 1);
+    const long kinds = kinds_of(wide ? 16 : 8);
+    const int per_warp = tokens_of(kinds);
     const long blocks = (s.rows + kThreads / 32L * per_warp - 1) / (kThreads / 32L * per_warp) * kinds;
     if (blocks >= 1L << 31) return int(cudaErrorInvalidValue);
     auto kernel = per_warp > 1 ? kernel_of<Store, 8, 8>(d) : kernel_of<Store, 1, 8>(d);
+    if (wide) kernel = kernel_of<Store, 1, 16>(d);
     if constexpr (Store)
-        if (wide) kernel = per_warp > 1 ? kernel_of<Store, 4, 16>(d) : kernel_of<Store, 1, 16>(d);
+        if (wide && per_warp > 1) kernel = kernel_of<Store, 4, 16>(d);
     return dependent(kernel, dim3(unsigned(blocks)), kThreads, 0, stream, c, s, x, per_warp, unsigned(kinds));
 }
 

@@ -131,11 +131,14 @@ def test_strides(how):
         assert same(y.resolve_neg(), expected(x.resolve_neg()))
 
 
-def test_rows_outside_of_all_sequences_and_places_that_are_none():
-    cache = P.PageCache.empty(1, 4, 2, 64, 16)
+@pytest.mark.parametrize("heads,d", [(2, 64), (8, 128), (17, 64), (4, 256)])
+@pytest.mark.parametrize("garbage", [False, True])
+def test_rows_outside_of_all_sequences_and_places_that_are_none(heads, d, garbage):
+    cache = P.PageCache.empty(1, 4, heads, d, 16)
     for t in (cache.codes, cache.ratios, cache.exponents):
-        t.zero_()
-    k, v = rows(12, 2, 64, 3)
+        t.random_(0, 256) if garbage else t.zero_()
+    before = cache.exponents.clone()
+    k, v = rows(12, heads, d, 3)
     # rows 0, 1 and 10, 11 are nobody's; the first sequence has two tokens before
     # position 0, the second a page that is none, the third one behind its table
     table, starts, lengths = ints([2, 0], [9, 1], [3, -1]), ints(2, 5, 8, 10), ints(1, 17, 33)
@@ -147,7 +150,8 @@ def test_rows_outside_of_all_sequences_and_places_that_are_none():
         assert bool((y[2:4] == 0).all()) and same(y[4], expected(x[4]))
         assert bool(y[5:7].isnan().all()) and same(y[7], expected(x[7]))
         assert bool(y[8:10].isnan().all())
-    assert int((cache.exponents != 0).sum()) == 2 * 2 * 2       # two tokens, two heads, keys and values
+    if not garbage:
+        assert int((cache.exponents != before).sum()) == 2 * heads * 2      # (two tokens, keys and values)
 
 
 def test_offsets_past_32_bits():
