@@ -20,7 +20,8 @@ POSITIONS = {torch.int64: 0, torch.int32: 1, torch.float32: 2}
 BF16, F32 = torch.bfloat16, torch.float32
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
-_current_device = torch.cuda.current_device
+# (likewise, of tensors that are on a device already)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def lib() -> ctypes.CDLL:
@@ -53,7 +54,7 @@ def lib() -> ctypes.CDLL:
         L.decoder_attention_scratch.argtypes = [l, l, i]
         L.decoder_attention_scratch.restype = l
         L.decoder_attention_backward.argtypes = [vp] * 6 + [ctypes.POINTER(l), vp, vp, vp, vp, l, l, l, i, i, i, f, vp]
-        L.decoder_page_rows.argtypes = [i, vp, i, vp, vp, l, l, l, l, vp, vp, vp, i, i, i, vp]
+        L.decoder_page_rows.argtypes = [i, vp, i, vp, l, l, vp, l, l, vp, vp, vp, i, i, i, vp]
         L.decoder_page_copy.argtypes = [vp, ctypes.POINTER(i), ctypes.POINTER(i), i, vp]
         L.decoder_page_copy_refused.argtypes = [ctypes.POINTER(i), ctypes.POINTER(i), i, i]
         L.decoder_page_attention_scratch.argtypes = [i]

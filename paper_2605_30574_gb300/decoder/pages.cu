@@ -372,9 +372,9 @@ int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream
 
 using namespace decoder;
 
-// Rows k, v [rows][hkv][d] (strides: token and head of k, then of v) into the layer's
+// Rows k, v [rows][hkv][d] (each with its strides, token and head) into the layer's
 // pages (out 0), or out of them (out 1).
-extern "C" int decoder_page_rows(int out, const PageCache* cache, int layer, const void* k, const void* v, long k_token, long k_head,
+extern "C" int decoder_page_rows(int out, const PageCache* cache, int layer, const void* k, long k_token, long k_head, const void* v,
                                  long v_token, long v_head, const void* table, const void* starts, const void* lengths, int width, int batch,
                                  int rows_, void* stream) {
     if (!cache->valid() || layer < 0 || layer >= cache->layers || width < 1 || batch < 1 || rows_ < 1) return int(cudaErrorInvalidValue);

@@ -144,25 +144,27 @@ def _where(what, cache, table, starts, lengths):
 
 
 def _bf16(what, name, t, cache, shape):
-    if isinstance(t, torch.Tensor) and t.dtype is BF16 and t.shape == shape and t.device == cache.device and t.data_ptr():
-        return t
+    """Where the kernels can read and write the tensor as it is: its address and its strides
+    of token and head; else None."""
+    if isinstance(t, torch.Tensor) and t.dtype is BF16 and t.shape == shape and t.device == cache.device:
+        at = t.data_ptr()
+        if at:
+            token, head, one = t.stride()
+            kernels = one == 1 and not (token | head | at >> 1) & 7 and not t.is_neg() and token < 1 << 38 and head < 1 << 38
+            return (at, token, head) if kernels else None
     if not isinstance(t, torch.Tensor) or t.dtype is not BF16:
         raise TypeError(f"{what}: {name} must be a bf16 tensor")
     if t.device != cache.device:
         raise ValueError(f"{what}: {name} must be on the cache's device")
     if t.dim() != 3 or t.shape[-1] != cache.head_dim or (shape is not None and t.shape != shape):
         raise ValueError(f"{what}: {name} must be [tokens][heads][{cache.head_dim}]" + (f", here {tuple(shape)}" if shape else ""))
-    return there(what, name, t)
+    there(what, name, t)
 
 
-def _reads(t):
-    """Whether the kernels can read the tensor where it is."""
-    token, head, one = t.stride()
-    return one == 1 and not (token | head | t.data_ptr() >> 1) & 7 and not t.is_neg() and token < 1 << 38 and head < 1 << 38
-
-
-def _readable(t):
-    return t if _reads(t) else t.resolve_neg().clone(memory_format=torch.contiguous_format)
+def _copied(t):
+    """A copy that the kernels can read and write, and where it is."""
+    t = t.resolve_neg().clone(memory_format=torch.contiguous_format)
+    return t, (t.data_ptr(), *t.stride()[:2])
 
 
 def _written(*ts):
@@ -204,8 +206,7 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
     where = _where(what, cache, table, starts, lengths)
     rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
     shape = (rows, cache.kv_heads, cache.head_dim)
-    _bf16(what, "k", k, cache, shape)
-    _bf16(what, "v", v, cache, shape)
+    at_k, at_v = _bf16(what, "k", k, cache, shape), _bf16(what, "v", v, cache, shape)
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
@@ -214,8 +215,11 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
     if cache.device.index != _current_device():
         with torch.cuda.device(cache.device):
             return store_pages(cache, layer, k, v, table, starts, lengths)
-    k, v = _readable(k), _readable(v)
-    _launch("decoder_page_rows", 0, at, layer, k.data_ptr(), v.data_ptr(), *k.stride()[:2], *v.stride()[:2], *where, rows)
+    if at_k is None:
+        k, at_k = _copied(k)
+    if at_v is None:
+        v, at_v = _copied(v)
+    _launch("decoder_page_rows", 0, at, layer, *at_k, *at_v, *where, rows)
 
 
 def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
@@ -229,9 +233,9 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
     where = _where(what, cache, table, starts, lengths)
     rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
     shape = (rows, cache.kv_heads, cache.head_dim)
-    for name, t in (("k", k), ("v", v)):
-        _bf16(what, name, t, cache, shape)
-        _target(what, name, t)
+    at_k, at_v = _bf16(what, "k", k, cache, shape), _bf16(what, "v", v, cache, shape)
+    _target(what, "k", k)
+    _target(what, "v", v)
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
@@ -243,8 +247,12 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
         with torch.cuda.device(cache.device):
             return load_pages(cache, layer, k, v, table, starts, lengths)
     # (what the kernels cannot write to gets its rows by way of a copy)
-    to, tv = _readable(k), _readable(v)
-    _launch("decoder_page_rows", 1, at, layer, to.data_ptr(), tv.data_ptr(), *to.stride()[:2], *tv.stride()[:2], *where, rows)
+    to, tv = k, v
+    if at_k is None:
+        to, at_k = _copied(k)
+    if at_v is None:
+        tv, at_v = _copied(v)
+    _launch("decoder_page_rows", 1, at, layer, *at_k, *at_v, *where, rows)
     if k is to and v is tv:
         return _written(k, v)
     with torch.no_grad():
@@ -271,7 +279,7 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     untraced(what)
     where = _where(what, cache, table, starts, lengths)
     shape = q.shape if isinstance(q, torch.Tensor) else ()
-    _bf16(what, "q", q, cache, shape if len(shape) == 3 and shape[2] == cache.head_dim else None)
+    at_q = _bf16(what, "q", q, cache, shape if len(shape) == 3 and shape[2] == cache.head_dim else None)
     rows, hq, d = shape
     if rows * hq >= 1 << 26:
         raise ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
@@ -294,9 +302,9 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     y = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
     if not rows or not where[-1]:
         return y
-    q = _readable(q)
-    token, head, _ = q.stride()
-    args = at, layer, q.data_ptr(), token, head, *where, rows, hq, scale, window, y.data_ptr()
+    if at_q is None:
+        q, at_q = _copied(q)
+    args = at, layer, *at_q, *where, rows, hq, scale, window, y.data_ptr()
     # Short sequences take no scratch, whose allocation is 3 us of a call of 29, so that is
     # tried first where it is likely (in vain, it costs 2.5).
     most, short = where[3] * cache.page, False

@@ -263,7 +263,7 @@ def test_the_library_refuses_sizes():
     for sizes, layer, width in (((0, 1, 1, 64, 4), 0, 1), ((1, 0, 1, 64, 4), 0, 1), ((1, 1, 0, 64, 4), 0, 1), ((1, 1, 1025, 64, 4), 0, 1),
                                 ((1, 1, 1, 32, 4), 0, 1), ((1, 1, 1, 64, 3), 0, 1), ((1, 1, 1, 64, 9), 0, 1), (good, 1, 1), (good, -1, 1), (good, 0, 0)):
         c = P._Described(None, None, None, *sizes)
-        assert L.decoder_page_rows(0, byref(c), layer, None, None, 0, 0, 0, 0, None, None, None, width, 1, 1, None) != 0
+        assert L.decoder_page_rows(0, byref(c), layer, None, 0, 0, None, 0, 0, None, None, None, width, 1, 1, None) != 0
         assert L.decoder_page_attention(byref(c), layer, None, 0, 0, None, None, None, width, 1, 1, 2, 1.0, 0, None, None, None) != 0
     c = P._Described(None, None, None, 1, 1, 2, 64, 4)
     for rows, hq, window in ((1, 3, 0), (1, 0, 0), (0, 2, 0), (1 << 25, 2, 0), (1, 2, -1)):
