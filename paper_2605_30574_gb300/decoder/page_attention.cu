@@ -935,7 +935,7 @@ int run(const Args& a, void* scratch, cudaStream_t stream) {
     // columns with those of the next head (64 sequences of 4000 tokens, one row of 128: 60
     // us for 65; 256 with four of 64: 118 for 134; 64 with two of 256: 49 for 51), more
     // than eight take sixteen columns (24 sequences of up to 16 tokens with four rows of
-    // 128: 52 for 56; but for 256, for which there are no registers).
+    // 128: 52 for 56; of 256 they spill, 48 sequences of 8 tokens with two rows 74 for 51).
     const long rows = long(a.s.rows) * a.G, all = a.s.batch;
     if (rows <= 4 * all && a.c.hkv % 2 == 0) return launch<Shape<D, 1, 2>>(a, scratch, stream);
     if constexpr (D < 256)
