@@ -270,7 +270,7 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     h // (Hq / heads).  A token that sees nothing gives 0; one whose keys or values hold NaN,
     NaN.  A page that a row looks into and that is none of the cache's makes its tile's rows
     NaN, and a sequence longer than the table is wide all its rows.  ``scale`` is
-    1 / sqrt(d) by default; scores have to be numbers of fp32.
+    1 / sqrt(d) by default; scores, and ``scale`` times q, have to be below 2^127.
 
     Returns [tokens][Hq][d], bf16: ``out`` (contiguous) if given, else a new tensor whose
     rows outside of all sequences hold anything.  Scores and sums are in fp32, q to the
