@@ -137,8 +137,8 @@ def _launch(name, *args):
     # host time than the launch)
     rc = getattr(_LIB or lib(), name)(*args, _raw_stream(_current_device()))
     if rc != 0:
-        if rc < 0:          # (what the call was given does not do)
-            return False
+        if rc == -1 and name == "decoder_page_attention" and args[-1] is None:
+            return False        # (it takes scratch, was given none, and has done nothing)
         raise RuntimeError(f"{name} failed with CUDA error {rc}")
 
 
