@@ -25,7 +25,8 @@ pages.
 Tensors are bf16, d 64, 128 or 256, pages of 16, 32, 64, 128 or 256 tokens; k, v and q
 may have any strides (those that the kernels cannot read are copied).  Kernels go to
 torch's current stream; tracers, which would not record them, are refused.  No
-gradients.  The same inputs give the same bits.
+gradients: tensors that require one, where they are recorded, or that have a tangent are
+refused.  The same inputs give the same bits.
 """
 from __future__ import annotations
 
@@ -34,6 +35,7 @@ from array import array
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple, Union
 
 import torch
+import torch.autograd.forward_ad as _fwad
 
 from . import BF16, _current_device, _launch, lib, there, untraced
 
@@ -185,9 +187,17 @@ def _meet(a, b):
     return a.numel() > 0 and b.numel() > 0 and a0 < b1 and b0 < a1
 
 
-def _target(what, name, t):
+def _underived(what, name, t):
+    """Only a tensor's values are read or written: one whose gradient or tangent would be lost
+    is refused."""
     if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{what}: {name} requires a gradient and is written to")
+        raise ValueError(f"{what}: {name} requires a gradient, and the call has none (detached, or under torch.no_grad())")
+    if _fwad._current_level >= 0 and _fwad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{what}: {name} has a tangent, and the call makes none")
+
+
+def _target(what, name, t):
+    _underived(what, name, t)
     if t.is_inference() and not torch.is_inference_mode_enabled():
         raise ValueError(f"{what}: {name} is an inference tensor and is written to")
     if not t.is_contiguous() and t.numel() and _overlaps(t):
@@ -207,6 +217,8 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
     rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
     shape = (rows, cache.kv_heads, cache.head_dim)
     at_k, at_v = _bf16(what, "k", k, cache, shape), _bf16(what, "v", v, cache, shape)
+    _underived(what, "k", k)
+    _underived(what, "v", v)
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
@@ -280,6 +292,7 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     where = _where(what, cache, table, starts, lengths)
     shape = q.shape if isinstance(q, torch.Tensor) else ()
     at_q = _bf16(what, "q", q, cache, shape if len(shape) == 3 and shape[2] == cache.head_dim else None)
+    _underived(what, "q", q)
     rows, hq, d = shape
     if rows * hq >= 1 << 26:
         raise ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
