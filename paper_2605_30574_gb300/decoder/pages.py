@@ -170,9 +170,8 @@ def _copied(t):
 
 
 def _written(*ts):
-    ts = [t for t in ts if not t.is_inference()]
-    if ts:
-        torch.autograd.graph.increment_version(ts)
+    # (inference tensors have no versions, and are passed over there)
+    torch.autograd.graph.increment_version(ts)
 
 
 def _overlaps(t):
@@ -232,6 +231,7 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
     if at_v is None:
         v, at_v = _copied(v)
     _launch("decoder_page_rows", 0, at, layer, *at_k, *at_v, *where, rows)
+    _written(cache.codes, cache.ratios, cache.exponents)
 
 
 def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
@@ -363,6 +363,7 @@ def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None
         with torch.cuda.device(cache.device):
             return copy_pages(cache, src, dst)
     _launch("decoder_page_copy", at, *pages, n)
+    _written(cache.codes, cache.ratios, cache.exponents)
 
 
 class PageTables:
