@@ -186,6 +186,31 @@ def _meet(a, b):
     return a.numel() > 0 and b.numel() > 0 and a0 < b1 and b0 < a1
 
 
+def _apart(a, b):
+    """Whether two tensors [tokens][heads][d] of one shape, each without places that overlap,
+    have none in common: by their strides, if those are the same, else by their first and last
+    places."""
+    x, y = a.data_ptr(), b.data_ptr()
+    if x > y:
+        a, b, x, y = b, a, y, x
+    shape, strides, gap = a.shape, a.stride(), (y - x) // 2
+    (n, heads, d), (token, head, one) = shape, strides
+    row = (heads - 1) * head + (d - 1) * one + 1
+    if gap >= (n - 1) * token + row or (row <= gap <= token - row and b.stride() == strides):
+        return True
+    dims = sorted([(s, n) for s, n in zip(strides, shape) if n > 1])
+    if dims != sorted([(s, n) for s, n in zip(b.stride(), shape) if n > 1]):
+        return False
+
+    def met(gap, i):
+        # (what the smaller strides reach is less than this one)
+        if i < 0:
+            return gap == 0
+        s, n = dims[i]
+        return any(-n < j < n and met(gap - j * s, i - 1) for j in (gap // s, gap // s + 1))
+    return not met(gap, len(dims) - 1)
+
+
 def _underived(what, name, t):
     """Only a tensor's values are read or written: one whose gradient or tangent would be lost
     is refused."""
@@ -236,10 +261,10 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
 
 def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, starts: torch.Tensor,
                lengths: torch.Tensor) -> None:
-    """Writes the values that the newest tokens are held as to k and v [tokens][heads][d], which
-    have no place in common; with ``starts`` that go by the lengths, those of whole sequences.  A token before
-    position 0 is zeros, one in a page that is none of the cache's, or behind the
-    table's, NaN."""
+    """Writes the values that the newest tokens are held as to k and v [tokens][heads][d]; with
+    ``starts`` that go by the lengths, those of whole sequences.  A token before position 0 is
+    zeros, one in a page that is none of the cache's, or behind the table's, NaN.  k and v have
+    no place in common (with strides of their own, neither lies between the other's)."""
     what = "load_pages"
     untraced(what)
     where = _where(what, cache, table, starts, lengths)
@@ -251,8 +276,8 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
-    if rows and k.data_ptr() == v.data_ptr():
-        raise ValueError(f"{what}: k and v are in the same place")
+    if rows and not _apart(k, v):
+        raise ValueError(f"{what}: rows of k and v are in the same place")
     if not rows or not where[-1]:
         return
     if cache.device.index != _current_device():
