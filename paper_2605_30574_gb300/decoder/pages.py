@@ -393,8 +393,9 @@ def copy_pages(cache: PageCache, src: Sequence[int], dst: Sequence[int]) -> None
 
 class PageTables:
     """Which pages of a cache hold which sequences, and how many tokens: kept on the host,
-    by numbers that sequences are given.  Sequences may share pages; a page that others
-    hold too is never written, ``extend`` copies one that is begun.
+    by numbers that sequences are given.  Sequences may share pages.  A page that others hold
+    too must not be written to: ``extend`` copies one that is begun, so that the tokens it
+    gives may be stored, and ``tensors`` for a store refuses what lies in any other.
 
     The calls that copy pages do so on torch's current stream, in that order with the
     calls that read and write them; ``tensors`` gives what those take, as of then."""
@@ -532,15 +533,23 @@ class PageTables:
         return k
 
     def tensors(self, sequences: Iterable[int], new: Union[None, int, Iterable[int]] = 1,
-                width: int = 0) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+                width: int = 0, store: bool = False) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """``table``, ``starts`` and ``lengths`` of the sequences on the cache's device, of
         which the ``new`` last tokens are stored, loaded or attend (one number, or one for
-        each; None: all).  The table has ``width`` columns, or as many more as it needs."""
+        each; None: all).  The table has ``width`` columns, or as many more as it needs.
+        With ``store`` new tokens whose page another sequence holds too are refused, and a
+        sequence that is named twice: tables that a call stores by are to be asked for so."""
         ids = self._known("tensors", sequences)
         lengths = [self._lengths[i] for i in ids]
         new = lengths if new is None else [new] * len(ids) if isinstance(new, int) else list(new)
         if len(new) != len(ids) or any(not isinstance(n, int) or not 0 <= n <= m for n, m in zip(new, lengths)):
             raise ValueError("PageTables.tensors: as many new tokens as each sequence has, at most")
+        if store:
+            if len(set(ids)) != len(ids):
+                raise ValueError("PageTables.tensors: each sequence once, for a store")
+            for i, n, length in zip(ids, new, lengths):
+                if n and max([self._users[p] for p in self._pages[i][(length - n) // self.cache.page:]]) > 1:
+                    raise ValueError(f"PageTables.tensors: sequence {i}'s last {n} tokens lie in a page that another sequence holds too")
         starts = [0]
         for n in new:
             starts.append(starts[-1] + n)

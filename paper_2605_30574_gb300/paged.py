@@ -62,7 +62,7 @@ class PagedDecode:
             """The sequence of a prefill, and its last logits."""
             logits = model.prefill(tokens, k, v)
             i = self.tables.add(Tp)
-            where = self.tables.tensors([i], None)
+            where = self.tables.tensors([i], None, store=True)
             for l in range(N):
                 P.store_pages(self.cache, l, k[l].transpose(0, 1), v[l].transpose(0, 1), *where)
             return i, logits
@@ -80,7 +80,7 @@ class PagedDecode:
         zero = self.tables.add(page)
         nothing = torch.zeros((page, Hkv, d), dtype=torch.bfloat16, device=dev)
         for l in range(N):
-            P.store_pages(self.cache, l, nothing, nothing, *self.tables.tensors([zero], None))
+            P.store_pages(self.cache, l, nothing, nothing, *self.tables.tensors([zero], None, store=True))
         zeros = torch.full((spans,), self.tables.pages(zero)[0], dtype=torch.int32)
         # a cell's pages of the span, at its layers l >= L
         self._spans = [zeros if kinds[c.slot] == W.ZERO else donors[c.prompt, c.slot] for c in self.seqs]
@@ -108,7 +108,7 @@ class PagedDecode:
     def _tables(self):
         """Every layer's table, starts and lengths for the rows, each with one new token."""
         self.tables.extend(self._ids)
-        table, starts, lengths = self.tables.tensors(self._ids)
+        table, starts, lengths = self.tables.tensors(self._ids, store=True)
         dev, clean, spans = self.model.device, len(self.runs), self.Tp // self.page
         spliced = table.clone()
         if self.cells:
