@@ -88,7 +88,6 @@ class PagedDecode:
         # the rows of a step: the clean runs, then the cells, as they are forked
         self.cells: List[int] = []
         self._ids: List[int] = list(self.runs)
-        self._table: Optional[list] = None
         self.check()
 
     def check(self):
@@ -119,7 +118,9 @@ class PagedDecode:
     @torch.no_grad()
     def step(self, t: int, tokens: torch.Tensor) -> torch.Tensor:
         """Forward pass of step t (1 <= t < T) for all rows: tokens are their y_{t-1}; returns
-        the logits whose argmax is y_t.  Does not wait for the GPU: see ``check``."""
+        the logits whose argmax is y_t.  Its tables come from the host's memory, so it begins
+        when the GPU has done what was given to it before, and does not wait for what it gives
+        it: see ``check``."""
         model, cache = self.model, self.cache
         tables, starts, lengths = self._tables()
         pos = torch.full((len(self._ids),), self.Tp + t - 1, device=model.device)
