@@ -211,17 +211,18 @@ def _apart(a, b):
     return not met(gap, len(dims) - 1)
 
 
-def _underived(what, name, t):
-    """Only a tensor's values are read or written: one whose gradient or tangent would be lost
-    is refused."""
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{what}: {name} requires a gradient, and the call has none (detached, or under torch.no_grad())")
-    if _fwad._current_level >= 0 and _fwad.unpack_dual(t).tangent is not None:
-        raise ValueError(f"{what}: {name} has a tangent, and the call makes none")
+def _underived(what, names, *ts):
+    """Only tensors' values are read or written: those whose gradient or tangent would be lost
+    are refused."""
+    for name, t in zip(names, ts):
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what}: {name} requires a gradient, and the call has none (detached, or under torch.no_grad())")
+        if _fwad._current_level >= 0 and _fwad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{what}: {name} has a tangent, and the call makes none")
 
 
 def _target(what, name, t):
-    _underived(what, name, t)
+    _underived(what, [name], t)
     if t.is_inference() and not torch.is_inference_mode_enabled():
         raise ValueError(f"{what}: {name} is an inference tensor and is written to")
     if not t.is_contiguous() and t.numel() and _overlaps(t):
@@ -241,8 +242,8 @@ def store_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, 
     rows = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
     shape = (rows, cache.kv_heads, cache.head_dim)
     at_k, at_v = _bf16(what, "k", k, cache, shape), _bf16(what, "v", v, cache, shape)
-    _underived(what, "k", k)
-    _underived(what, "v", v)
+    if k.requires_grad or v.requires_grad or _fwad._current_level >= 0:
+        _underived(what, "kv", k, v)
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
@@ -317,7 +318,8 @@ def page_attention(cache: PageCache, layer: int, q: torch.Tensor, table: torch.T
     where = _where(what, cache, table, starts, lengths)
     shape = q.shape if isinstance(q, torch.Tensor) else ()
     at_q = _bf16(what, "q", q, cache, shape if len(shape) == 3 and shape[2] == cache.head_dim else None)
-    _underived(what, "q", q)
+    if q.requires_grad or _fwad._current_level >= 0:
+        _underived(what, "q", q)
     rows, hq, d = shape
     if rows * hq >= 1 << 26:
         raise ValueError(f"{what}: fewer than 2^26 rows (tokens times heads)")
