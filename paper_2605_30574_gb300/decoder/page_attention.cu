@@ -114,6 +114,11 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// x 2^d, d at most 0.  A sum of weights is taken so: its reference goes by the values' sizes
+// too, and may rise by 200 bits where it does not become nothing (keys of zeros next to one
+// of large values).
+__device__ __forceinline__ float lowered(float x, float d) { return x * ex2(fmaxf(d, -100.f)) * ex2(fminf(d + 100.f, 0.f)); }
+
 __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -243,8 +248,8 @@ struct State {
         for (int i = 0; i < kVec; ++i) y[i] = reinterpret_cast<const float4*>(from)[lane + 8 * i];
         const float2 ml = *reinterpret_cast<const float2*>(from + D);
         const float M = fmaxf(m, ml.x), f = ex2(m - M), fy = ex2(ml.x - M);
+        l = lowered(l, m - M) + lowered(ml.y, ml.x - M);
         m = M;
-        l = l * f + ml.y * fy;
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
             o[i] = make_float4(o[i].x * f + y[i].x * fy, o[i].y * f + y[i].y * fy, o[i].z * f + y[i].z * fy, o[i].w * f + y[i].w * fy);
@@ -692,8 +697,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll
                         for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
                         const float m = fmaxf(ref[n][c], top), f = ex2(ref[n][c] - m);
+                        l[n][c] = lowered(l[n][c], ref[n][c] - m);
                         ref[n][c] = m;
-                        l[n][c] *= f;
 #pragma unroll
                         for (int i = 0; i < kI; ++i)
 #pragma unroll
@@ -705,8 +710,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                         pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
                     }
                 }
-                l[n][0] += p[0] + p[2];
-                l[n][1] += p[1] + p[3];
+                // (a weight is up to 2^108, of values of 2^-100)
+                l[n][0] = fmaf(p[0] + p[2], 0x1p-20f, l[n][0]);
+                l[n][1] = fmaf(p[1] + p[3], 0x1p-20f, l[n][1]);
                 w[n][0] = transposed(half2_of(pv[0], pv[1]));
                 w[n][1] = transposed(half2_of(pv[2], pv[3]));
             }
@@ -815,7 +821,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 if (__any_sync(kFull, broken)) sum = __int_as_float(0x7fffffff);
                 const int col = 8 * n + 2 * t + c, mine = P == 2 ? col >> 2 : 0, row = P == 2 ? col & 3 : col;
                 if (row >= walk.rows) continue;
-                const float f = whole ? (sum == 0.f ? 0.f : 0x1p16f / sum) : 0x1p16f;
+                const float f = whole ? (sum == 0.f ? 0.f : 0x1p-4f / sum) : 0x1p-4f;
                 if (whole) {
                     const int r = walk.tile * R + row, token = r / A.G;
                     __nv_bfloat16* to = A.out + ((size_t(walk.first + token) * A.c.hkv + walk.head + mine) * A.G + r - token * A.G) * D;
