@@ -20,7 +20,9 @@
 //  * Output: O[dim][row].  P as the fp16 operand has V's scales in it, so it is taken
 //    relative to the largest of (score + E of the value's row), and not of the score:
 //    then no product of a weight and a scale is above 2^15, and one that is rounded or
-//    lost below fp16's normal range is 2^-29 of the largest.  Codes have their 8
+//    lost below fp16's normal range is 2^-29 of the largest.  That reference is two
+//    numbers, a score and the rest: in one, E would be lost in scores from 2^24 on (60.7
+//    us for 61.5 with 8 new tokens, 63 for 65.4 with 16).  Codes have their 8
 //    subtracted (exactly): O would otherwise carry it through sums of thousands of keys.
 //    Subtracting the weights' sums by the tensor core instead, 417 us for 398.  The
 //    second nibble of a byte is taken off the first's sum, not masked out of it: 376 for
@@ -233,12 +235,12 @@ struct Walk {
     int ids[64];                                // pages of the sequence, two times 32 places
 };
 
-// Rows' states joined, 8 lanes to a row: O for the reference m and the sum l, at D and
-// D + 1.
+// Rows' states joined, 8 lanes to a row: O for the reference m + size, at D and D + 2, and the
+// sum l, at D + 1.
 template <int D>
 struct State {
     static constexpr int kVec = D / 32;         // by four elements
-    float m = kNone, l = 0.f;
+    float m = kNone, l = 0.f, size = 0.f;
     float4 o[kVec] = {};
 
     __device__ __forceinline__ void add(const float* from) {
@@ -246,10 +248,11 @@ struct State {
         float4 y[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) y[i] = reinterpret_cast<const float4*>(from)[lane + 8 * i];
-        const float2 ml = *reinterpret_cast<const float2*>(from + D);
-        const float M = fmaxf(m, ml.x), f = ex2(m - M), fy = ex2(ml.x - M);
-        l = lowered(l, m - M) + lowered(ml.y, ml.x - M);
-        m = M;
+        const float4 it = *reinterpret_cast<const float4*>(from + D);
+        const float above = (it.x - m) + (it.z - size), down = fminf(-above, 0.f), its = fminf(above, 0.f);
+        const float f = ex2(down), fy = ex2(its);
+        l = lowered(l, down) + lowered(it.y, its);
+        if (above > 0.f) m = it.x, size = it.z;
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
             o[i] = make_float4(o[i].x * f + y[i].x * fy, o[i].y * f + y[i].y * fy, o[i].z * f + y[i].z * fy, o[i].w * f + y[i].w * fy);
@@ -258,7 +261,7 @@ struct State {
         const int lane = threadIdx.x & 7;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) reinterpret_cast<float4*>(to)[lane + 8 * i] = o[i];
-        if (lane == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
+        if (lane == 0) *reinterpret_cast<float4*>(to + D) = make_float4(m, l, size, 0.f);
     }
     __device__ __forceinline__ void write(__nv_bfloat16* to) const {
         const int lane = threadIdx.x & 7;
@@ -492,7 +495,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 
         // ---- the rows: q as an operand, and what is known of each column ----
         uint32_t minus[P][NT][kI > 4 ? 4 : 2];
-        float factor[NT][2], l[NT][2], ref[NT][2];
+        float factor[NT][2], l[NT][2], ref[NT][2], size[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int mine = P == 2 ? g >> 2 : 0;
@@ -560,6 +563,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                 if (g == 0) walk.pos[8 * n + 2 * t + c] = column < rows ? base + (tile * R + column) / A.G : -1;
                 l[n][c] = 0.f;
                 ref[n][c] = kNone;
+                size[n][c] = 0.f;
             }
         }
         __syncwarp();
@@ -667,7 +671,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     // taken first, which may be none, 512 sequences took 391 us for 395, and 48
                     // with 8 new tokens 60.4 for 59.4)
                     s[n][j] = __fmul_rn(__fmul_rn(s[n][j], ek[j >> 1]), factor[n][j & 1]);
-                    x[j] = __fsub_rn(s[n][j], ref[n][j & 1]);
+                    x[j] = __fsub_rn(__fsub_rn(s[n][j], ref[n][j & 1]), size[n][j & 1]);
                 }
                 if (kEdge) {
 #pragma unroll
@@ -691,14 +695,22 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (kEdge && x[j] == -INFINITY) s[n][j] = -INFINITY;
+                    const float e[2] = {float(int(ex[0] >> 8) - 127), float(int(ex[1] >> 8) - 127)};
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float top = fmaxf(__fadd_rn(s[n][c], float(int(ex[0] >> 8) - 127)), __fadd_rn(s[n][2 + c], float(int(ex[1] >> 8) - 127)));
+                        float m = fmaxf(s[n][c], s[n][2 + c]);
 #pragma unroll
-                        for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-                        const float m = fmaxf(ref[n][c], top), f = ex2(ref[n][c] - m);
-                        l[n][c] = lowered(l[n][c], ref[n][c] - m);
-                        ref[n][c] = m;
+                        for (int o = 4; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+                        m = fmaxf(ref[n][c], m);
+                        // (what the largest of score + E, the old one's too, is above the largest score)
+                        float down = (ref[n][c] - m) + size[n][c];
+                        float rest = fmaxf(fmaxf((s[n][c] - m) + e[0], (s[n][2 + c] - m) + e[1]), down);
+#pragma unroll
+                        for (int o = 4; o < 32; o *= 2) rest = fmaxf(rest, __shfl_xor_sync(kFull, rest, o));
+                        down -= rest;
+                        ref[n][c] = m, size[n][c] = rest;
+                        l[n][c] = lowered(l[n][c], down);
+                        const float f = ex2(down);
 #pragma unroll
                         for (int i = 0; i < kI; ++i)
 #pragma unroll
@@ -706,7 +718,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        p[j] = ex2(__fsub_rn(s[n][j], ref[n][j & 1]));
+                        p[j] = ex2(__fsub_rn(__fsub_rn(s[n][j], ref[n][j & 1]), size[n][j & 1]));
                         pv[j] = kEdge && x[j] == -INFINITY ? 0.f : p[j] * up[j >> 1];
                     }
                 }
@@ -839,7 +851,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                         *reinterpret_cast<float4*>(to + 32 * i + 4 * g) =
                             make_float4((acc[n][i][0][c] - acc[n][i][0][2 + c]) * f, acc[n][i][0][2 + c] * (f * 0.0625f),
                                         (acc[n][i][1][c] - acc[n][i][1][2 + c]) * f, acc[n][i][1][2 + c] * (f * 0.0625f));
-                    if (g == 0) to[D] = ref[n][c], to[D + 1] = sum;
+                    if (g == 0) to[D] = ref[n][c], to[D + 1] = sum, to[D + 2] = size[n][c];
                 }
             }
         }
