@@ -169,9 +169,12 @@ def _copied(t):
     return t, (t.data_ptr(), *t.stride()[:2])
 
 
+_increment = torch.autograd.graph.increment_version
+
+
 def _written(*ts):
     # (inference tensors have no versions, and are passed over there)
-    torch.autograd.graph.increment_version(ts)
+    _increment(ts)
 
 
 def _overlaps(t):
@@ -222,7 +225,8 @@ def _underived(what, names, *ts):
 
 
 def _target(what, name, t):
-    _underived(what, [name], t)
+    if t.requires_grad or _fwad._current_level >= 0:
+        _underived(what, [name], t)
     if t.is_inference() and not torch.is_inference_mode_enabled():
         raise ValueError(f"{what}: {name} is an inference tensor and is written to")
     if not t.is_contiguous() and t.numel() and _overlaps(t):
@@ -277,7 +281,10 @@ def load_pages(cache: PageCache, layer: int, k: torch.Tensor, v: torch.Tensor, t
     at = cache._layer(what, layer)
     if rows >= 1 << 31:
         raise ValueError(f"{what}: fewer than 2^31 tokens")
-    if rows and not _apart(k, v):
+    # (mostly one lies behind the other, which is seen from their places and strides)
+    if rows and not (at_k and at_v and at_k[1:] == at_v[1:]
+                     and abs(at_k[0] - at_v[0]) >= 2 * ((rows - 1) * at_k[1] + (cache.kv_heads - 1) * at_k[2] + cache.head_dim)) \
+            and not _apart(k, v):
         raise ValueError(f"{what}: rows of k and v are in the same place")
     if not rows or not where[-1]:
         return

@@ -45,6 +45,17 @@ def test_places_between_each_other(launched, k, v):  # noqa: F811
     assert len(launched) == 2
 
 
+@pytest.mark.parametrize("heads,rows,strides", [(1, 1, (0, 0, 1)), (1, 2, (64, 0, 1)), (2, 1, (0, 64, 1)), (1, 1, (8, 8, 1))])
+def test_strides_of_one(launched, heads, rows, strides):  # noqa: F811
+    """Strides of dimensions of one say nothing of where rows are."""
+    flat, cache, w = torch.zeros(4096, dtype=BF), OnCpu(heads=heads), where(rows)
+    k, v, apart = (flat.as_strided((rows, heads, 64), strides, at) for at in (0, 32, 64 * rows * heads))
+    with pytest.raises(ValueError, match="same place"):
+        P.load_pages(cache, 0, k, v, *w)
+    P.load_pages(cache, 0, k, apart, *w)
+    assert len(launched) == 1
+
+
 def test_by_all_places():
     """Of any equal strides: as the places say, one by one."""
     rng = random.Random(0)
