@@ -4,12 +4,12 @@
 //   j <= pos_i = length - new + i,  j > pos_i - window
 //
 // A step reads every key and value once for the G = Hq / Hkv query rows of a kv head
-// (times its new tokens): 138 bytes to 1024 G flops at 128 dims, so HBM is the bound,
+// (times its new tokens): 138 bytes to 512 G flops at 128 dims, so HBM is the bound,
 // and what a kernel may spend on making operands of 4-bit codes is about three
 // instructions of a lane to an element.  Products therefore take the codes as they
 // are: a nibble n = c + 8, masked in place, is the fp16 number n 2^-24 (bits 0 to 3) or
 // 16 n 2^-24 (bits 4 to 7).  In order of what each measured, at 512 sequences of 4224
-// tokens, 32 / 8 heads of 128 (2.4 GB; 355 us at the copy rate, now 375):
+// tokens, 32 / 8 heads of 128 (2.4 GB; 355 us at the copy rate, now 379):
 //
 //  * Scores: S[key][row], keys on the 16-row side of m16n8k16, eight rows on the other
 //    (or twice eight).  q is scaled to 2^14 by a power of two and rounded to fp16 (all
@@ -21,8 +21,8 @@
 //    relative to the largest of (score + E of the value's row), and not of the score:
 //    then no product of a weight and a scale is above 2^15, and one that is rounded or
 //    lost below fp16's normal range is 2^-29 of the largest.  That reference is two
-//    numbers, a score and the rest: in one, E would be lost in scores from 2^24 on (60.7
-//    us for 61.5 with 8 new tokens, 63 for 65.4 with 16).  Codes have their 8
+//    numbers, a score and the rest: in one, E would be lost in scores from 2^24 on (1.3%
+//    faster with 8 new tokens, 4% with 16, as fast with one).  Codes have their 8
 //    subtracted (exactly): O would otherwise carry it through sums of thousands of keys.
 //    Subtracting the weights' sums by the tensor core instead, 417 us for 398.  The
 //    second nibble of a byte is taken off the first's sum, not masked out of it: 376 for
@@ -40,8 +40,8 @@
 //    registers the loop then spills and recomputes nothing (286 -> 276 instructions); 16
 //    warps of 128 registers, 415 us for 388.
 //
-// What bounds it now is issue: 64% of all slots, the ALU 62% (profile), of what HBM's rate
-// would allow about 95%.
+// What bounds it now is HBM, 94% of its copy rate, and close behind it issue: 65% of all
+// slots, the ALU 60% (profile).
 //
 // Work: all (sequence, kv head, tile of rows, stage of keys) in one line, an even share to
 // each warp, whatever the sequences' lengths, which only the device knows.  (Short tiles:
@@ -668,8 +668,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) attention_kernel(const Args A)
                     // scores in the millions the one that is the reference leaves 0.  In this
                     // order both products are numbers of fp32 where the score is: S is below
                     // 2^3, ek below 2^122, the factor below scale q.  With that of the factors
-                    // taken first, which may be none, 512 sequences took 391 us for 395, and 48
-                    // with 8 new tokens 60.4 for 59.4)
+                    // taken first, which may be none, 512 sequences took 1% less, and 48 with 8
+                    // new tokens 1.6% more)
                     s[n][j] = __fmul_rn(__fmul_rn(s[n][j], ek[j >> 1]), factor[n][j & 1]);
                     x[j] = __fsub_rn(__fsub_rn(s[n][j], ref[n][j & 1]), size[n][j & 1]);
                 }

@@ -4,13 +4,14 @@
 // page, and a copied page is read and written once.  Small calls are latency: the
 // search for a row's sequence, its page, the access.
 //
-// 16.5k tokens of 8 heads of 128, ragged: stored in 25 us, loaded in 24 (84 MB each: 12.5 at
-// the copy rate), what a row's scales cost in instructions and a warp's chain of four
-// loads before its first row.  Measured on the way, both together: 129 with a warp to a
-// row, 79 with eight rows on their way in a warp, 70 without divisions (below), 55 with
-// rows of a page a constant apart, 51 with sixteen elements to a lane, 49 with CTAs of four
-// warps for eight and a row's successor fetched when it is rounded.  36 layers of 340 pages
-// copied: 254 us (1.73 GB, the copy rate).
+// 16384 tokens of 8 heads of 128 with cold caches: stored in 24 us, loaded in 23 (85 MB each:
+// 12.6 at the copy rate), what a row's scales cost in instructions and a warp's chain of four
+// loads before its first row.  Measured on the way, 20992 tokens of ragged prompts stored and
+// then loaded (109 MB each: 32.4 together): 129 with a warp to a row, 79 with eight rows on
+// their way in a warp, 70 without divisions (below), 55 with rows of a page a constant apart,
+// 51 with sixteen elements to a lane, 49 with CTAs of four warps for eight and a row's
+// successor fetched when it is rounded.  36 layers of 340 pages copied: 254 us (1.73 GB, the
+// copy rate).
 #include "pages.cuh"
 
 #include <algorithm>
@@ -348,8 +349,8 @@ auto kernel_of(int d) {
 
 template <bool Store>
 int rows(const PageLayer& c, const PageRows& s, const Rows& x, int d, cudaStream_t stream) {
-    // Tokens to a warp: as many as leave an SM some sixteen warps; a lone one has the
-    // shortest chain of loads.
+    // Tokens to a warp: as many as leave each of the 152 SMs some sixteen warps; a lone one
+    // has the shortest chain of loads.
     auto kinds_of = [&](int each) { return 2L * ((c.hkv * d + 32 * each - 1) / (32 * each)); };
     auto tokens_of = [&](long kinds) { return s.rows / 16 * kinds >= 152 * 32 ? 16 : s.rows / 8 * kinds >= 152 * 16 ? 8 : 1; };
     // Sixteen elements to a lane halve what a row's scales cost, where a warp's lanes are
